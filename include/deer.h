@@ -85,7 +85,9 @@ typedef enum {
 } deer_status;
 
 typedef enum { DEER_CELL_GRU = 0, DEER_CELL_MLP_ODE = 1, DEER_CELL_LSTM = 2, DEER_CELL_LEM = 3 } deer_cell;
-typedef enum { DEER_F32 = 0, DEER_F64 = 1 } deer_dtype;
+typedef enum { DEER_F32 = 0, DEER_F64 = 1, DEER_BF16 = 2, DEER_F16 = 3 } deer_dtype; /* 16 bits: sequence operators only */
+/* factor a_t of a gated recurrence, from its gate g: a = g; a = exp(g); a = 1 / (1 + exp(-g)), the input weighted with 1 - a */
+typedef enum { DEER_GATE_FACTOR = 0, DEER_GATE_LOG = 1, DEER_GATE_SIGMOID = 2 } deer_gate;
 typedef enum { DEER_ACT_TANH = 0, DEER_ACT_SOFTPLUS = 1 } deer_activation;
 
 typedef struct {
@@ -230,6 +232,74 @@ deer_status deer_linrec_solve(deer_ctx* ctx, const void* d_A, const void* d_b, c
 deer_status deer_linrec_solve_static(int32_t dtype, int32_t B, int32_t T, int32_t n, const void* d_A, const void* d_b,
                                      const void* d_y0, void* d_y, int32_t reverse, void* hip_stream,
                                      int32_t* d_status);
+
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Sequence operators: recurrences that are linear from the start (deer_eval() makes linear ones of a non-linear one), with gates,
+ * for every length from one token on, and dropout.
+ *
+ * Conventions, beyond those at the top of this file
+ *   - No context.  Every call enqueues its kernels on hip_stream (a stream of the current device; NULL = the default stream) and
+ *     returns without synchronising; nothing is allocated, so a call may be captured into a HIP graph (each captured call with a workspace
+ *     of its own, or never replayed at the same time).  Errors are reported through deer_last_error(NULL).
+ *   - Types: DEER_F32, DEER_F64 (deer_diagrec_*, deer_dropout), DEER_BF16, DEER_F16 (deer_diagrec_*, deer_dropout).  Sums and states are held in
+ *     32 bits (fp64: 64); h0, last, dlast, dh0, states and their gradients are arrays of that wider type, dense.
+ *   - Rows.  packed = 0: N sequences of T rows, row t of sequence n is row n T + t of every array; d_bounds (device, int64 [N], or NULL) holds how
+ *     many rows of each count.  packed = 1: the sequences lie one behind the other in T rows; d_bounds (device, int64 [N + 1], not NULL) holds
+ *     where they begin, its last entry where the last one ends.  Sequences may be empty: their final state is the initial
+ *     one.  Rows that belong to no sequence are neither read nor written.  Bounds outside 0 .. T are clamped;
+ *     packed bounds that decrease give results without meaning, within the arrays.
+ *   - stride_*: elements from one row to the next (0: dense), so that slices of a wider array can be handed in; the
+ *     last dimension is dense.
+ *   - Pointers are aligned to the element; where all rows are aligned to more, wider loads are used.  Outputs must not overlap
+ *     inputs, except where an operator says so.
+ *   - What is NaN or infinite in a sequence stays in that sequence. */
+typedef struct {
+    int32_t dtype;       /* deer_dtype                                                                     */
+    int32_t gate;        /* deer_gate                                                                      */
+    int32_t N;           /* sequences (deer_diagrec_step: rows), >= 1                                      */
+    int32_t D;           /* channels, >= 1                                                                 */
+    int64_t T;           /* rows of a sequence, packed: of all of them; >= 0                               */
+    int32_t packed;      /* 0 or 1                                                                         */
+    uint32_t draw;       /* dropout: number of the draw under this seed                                    */
+    int64_t stride_gate; /* rows of d_gate and d_dgate                                                     */
+    int64_t stride_in;   /* rows of d_in and d_din                                                         */
+    int64_t stride_out;  /* rows of d_h and d_dh                                                           */
+    double drop;         /* share of the inputs that is dropped, 0 <= drop < 1 (see deer_dropout)          */
+    uint64_t seed;       /* dropout: seed                                                                  */
+} deer_diagrec_config;
+
+/* Bytes of device workspace (256-byte aligned) that deer_diagrec_solve() (grad = 0) or deer_diagrec_grad() (grad = 1) needs: some
+ * 8 bytes a channel for every 64 or 128 rows. */
+deer_status deer_diagrec_workspace_bytes(const deer_diagrec_config* cfg, int32_t grad, size_t* bytes);
+
+/* Gated linear recurrence, a state for every channel: h_t = a_t h_{t-1} + u_t, u_t = x_t (DEER_GATE_SIGMOID: (1 - a_t) x_t), x after dropout.
+ *   d_gate, d_in  in  [rows, D]      d_h0  in  [N, D] or NULL (zeros)
+ *   d_h           out [rows, D] (may be d_in, with the same stride)      d_last  out [N, D] state behind every sequence's last row, or NULL
+ * One pass over the data; two calls with the same inputs return the same bits.  The product of the factors over 128 rows has to be
+ * representable (gates that make the state grow can overflow it). */
+deer_status deer_diagrec_solve(const deer_diagrec_config* cfg, const void* d_gate, const void* d_in, const void* d_h0,
+                               const int64_t* d_bounds, void* d_h, void* d_last, void* d_workspace, size_t workspace_bytes,
+                               void* hip_stream);
+
+/* Its gradient, at the trajectory d_h that is handed in (deer_diagrec_solve()'s).
+ *   d_dh     in  dL/dh [rows, D]            d_dlast  in  dL/dlast [N, D] or NULL (zeros)
+ *   d_dgate  out dL/dgate [rows, D]         d_din    out dL/din [rows, D]          d_dh0  out [N, D] or NULL */
+deer_status deer_diagrec_grad(const deer_diagrec_config* cfg, const void* d_gate, const void* d_in, const void* d_h0,
+                              const int64_t* d_bounds, const void* d_h, const void* d_dh, const void* d_dlast, void* d_dgate,
+                              void* d_din, void* d_dh0, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One token for each of N rows (T, packed and drop are not looked at): the states lie in n_slots slots [n_slots, D] and are updated
+ * in place; row n has slot d_slots[n] (device, int32 [N]; NULL: slot n).  A row whose slot is out of range, as in a
+ * padded batch, or is the slot of a row in front of it is passed over: its row of d_h and the state stay as they are. */
+deer_status deer_diagrec_step(const deer_diagrec_config* cfg, const void* d_gate, const void* d_in, const int32_t* d_slots,
+                              int32_t n_slots, void* d_state, void* d_h, void* hip_stream);
+
+/* Dropout: y = x / (1 - p) where an element is kept, 0 where it is dropped.  Which ones are kept follows from (seed, draw) and the element's
+ * sequence, row and channel alone, so the backward pass is the same call on the gradient and no mask is stored; deer_diagrec_*
+ * with drop = p draws the same mask.  p is rounded to 2^-16 (and the scale taken from the rounded value).
+ *   d_x in, d_y out [N, T, D], rows stride_in and stride_out apart (0: dense); d_y may be d_x with the same stride. */
+deer_status deer_dropout(int32_t dtype, int32_t N, int64_t T, int32_t D, const void* d_x, int64_t stride_in, void* d_y,
+                         int64_t stride_out, double p, uint64_t seed, uint32_t draw, void* hip_stream);
 
 /* Switch per-kernel timing with HIP events on the context's stream on or off (off by default;
  * turning it on resets the accumulated numbers), and read the numbers accumulated so far. */

@@ -15,6 +15,7 @@
 
 #include "../../include/deer.h"
 #include "deer_common.h"
+#include "seq_common.h"
 
 using namespace deer;
 
@@ -1441,6 +1442,18 @@ deer_status deer_linrec_solve_static(int32_t dtype, int32_t B, int32_t T, int32_
     }
     return DEER_OK;
 }
+
+}  // extern "C"
+
+// for the entry points of seq_api.hip
+void deer::set_last_error(const char* text) noexcept {
+    try {
+        g_last_error = text;
+    } catch (...) {   // no memory for the text: the status says enough
+    }
+}
+
+extern "C" {
 
 const char* deer_last_error(const deer_ctx* c) {
     return c ? c->last_error.c_str() : g_last_error.c_str();

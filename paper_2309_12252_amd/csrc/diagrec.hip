@@ -1,0 +1,514 @@
+// Gated linear recurrences with one state a channel: h_t = a_t h_{t-1} + u_t, forward and backward in one pass over the data,
+// and the step of one token.
+//
+//   factor   a = g           u = x                        LOG      a = exp(g)      u = x
+//   sigmoid  a = 1/(1+e^-g)  u = (1 - a) x                (x may be multiplied by the dropout mask first)
+// Backward: with mu_{T+1} = dL/dh_T of the final state, lambda_t = dh_t + mu_{t+1} and mu_t = a_t lambda_t,
+//   dL/da_t = lambda_t h_{t-1}   dL/du_t = lambda_t   dL/dh_0 = mu_1,
+// again a recurrence of the same form, mu_t = a_t mu_{t+1} + a_t dh_t, along the reversed rows.
+#include "seq_common.h"
+
+namespace deer {
+namespace {
+
+constexpr int kGroup = 16;                        // tiles of a group: the carry is passed on from group to group
+constexpr unsigned long long kUnset = ~0ull;      // a word that has not been published (two NaNs that are never published)
+constexpr long long kPolls = 1ll << 22;           // polls before a tile gives up on its predecessors (seconds; its rows become NaN)
+
+// tile of W wavefronts, R rows each; a lane has V channels
+template <typename T, bool REV> struct Shape {
+    static constexpr int W = 8;
+    static constexpr int V = sizeof(T) == 8 ? 1 : 2;
+    static constexpr int R = (REV && sizeof(T) > 2) ? 8 : 16;
+};
+
+template <typename T> __device__ __forceinline__ T fast_exp(T v) { return exp(v); }
+template <> __device__ __forceinline__ float fast_exp<float>(float v) { return __expf(v); }
+
+// a and the weight of x.  The 16-bit types take the hardware's exp and reciprocal (2^-21 off, far below their rounding).
+template <typename T, int KIND>
+__device__ __forceinline__ void gate_factors(wide_t<T> g, wide_t<T>& a, wide_t<T>& w) {
+    using S = wide_t<T>;
+    if constexpr (KIND == DEER_GATE_FACTOR) {
+        a = g;
+        w = S(1);
+    } else if constexpr (KIND == DEER_GATE_LOG) {
+        a = sizeof(T) == 2 ? fast_exp(g) : exp(g);
+        w = S(1);
+    } else {   // both a and 1 - a without cancellation
+        const S m = g < S(0) ? g : -g;
+        const S e = sizeof(T) == 2 ? fast_exp(m) : exp(m);
+        S r;
+        if constexpr (sizeof(T) == 2) r = __builtin_amdgcn_rcpf(S(1) + e);
+        else r = S(1) / (S(1) + e);
+        const S er = e * r;
+        a = g < S(0) ? er : r;
+        w = g < S(0) ? r : er;
+    }
+}
+
+// Published words: (a, h) of a tile as one word of two floats, or two words of a double each.  A word is valid as soon as it
+// is not kUnset, so no flag and no fence goes with it; NaNs are published as the one quiet NaN.
+__device__ __forceinline__ unsigned long long word_of(float a, float h) {
+    const unsigned ua = a != a ? 0x7FC00000u : __float_as_uint(a), uh = h != h ? 0x7FC00000u : __float_as_uint(h);
+    return ((unsigned long long)uh << 32) | ua;
+}
+__device__ __forceinline__ unsigned long long word_of(double v) {
+    return v != v ? 0x7FF8000000000000ull : (unsigned long long)__double_as_longlong(v);
+}
+__device__ __forceinline__ void put_word(unsigned long long* p, unsigned long long v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long get_word(const unsigned long long* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// K words `step` apart, once all of them are there; kUnset in their place after kPolls polls
+template <int K>
+__device__ __forceinline__ void wait_words(const unsigned long long* p, long long step, int count, unsigned long long (&w)[K]) {
+    for (long long poll = 0; poll < kPolls; ++poll) {
+        bool all = true;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            w[k] = k < count ? get_word(p + k * step) : 0;
+            all = all && w[k] != kUnset;
+        }
+        if (__all(all)) return;
+        __builtin_amdgcn_s_sleep(2);
+    }
+}
+
+template <typename S, int V> struct Carry;
+// fold of tiles first .. last - 1 (count of them) into h
+template <int V>
+__device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long long step, int count, bool first_resets, float (&h)[V]) {
+    constexpr int K = 8;
+    for (int at = 0; at < count; at += K) {
+        const int some = count - at < K ? count - at : K;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            unsigned long long w[K];
+            wait_words<K>(agg + (long long)at * step + v, step, some, w);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (k < some) {
+                    const float a = __uint_as_float((unsigned)w[k]), u = __uint_as_float((unsigned)(w[k] >> 32));
+                    h[v] = (first_resets && at + k == 0) ? u : a * h[v] + u;
+                }
+        }
+    }
+}
+template <int V>
+__device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long long step, int count, bool first_resets, double (&h)[V]) {
+    constexpr int K = 4;
+    for (int at = 0; at < count; at += K) {
+        const int some = count - at < K ? count - at : K;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            unsigned long long wa[K], wu[K];
+            wait_words<K>(agg + (long long)at * step + 2 * v, step, some, wa);
+            wait_words<K>(agg + (long long)at * step + 2 * v + 1, step, some, wu);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (k < some) {
+                    const double a = __longlong_as_double((long long)wa[k]), u = __longlong_as_double((long long)wu[k]);
+                    h[v] = (first_resets && at + k == 0) ? u : a * h[v] + u;
+                }
+        }
+    }
+}
+
+// Memory bound: every input is read once and every output written once.  A lane keeps V channels and R rows of the inputs in
+// registers (raw: 16 rows of two bf16 arrays are 32 registers), so the rows are gone over twice without a second read: once
+// for the tile's own map (product of the factors, state from zero), once more from the carry.  The carry of a tile is the fold, in a fixed
+// order, of its predecessors' maps since the last group of kGroup tiles and that group's carry, so two runs give the
+// same bits.  Tiles are dealt out by a ticket in the order of the rows: a tile waits for tiles that are running or done only.
+template <typename T, int KIND, int V, int R, int W, bool REV, bool DROP>
+__global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) {
+    using S = wide_t<T>;
+    using TV = vec_t<T, V>;
+    constexpr int C = 64 * V;     // channels of a tile
+    constexpr int L = R * W;      // rows of a tile
+    constexpr int WORDS = sizeof(S) == 8 ? 2 : 1;
+    static_assert(R + 1 <= 64 && R % 8 == 0, "a lane looks up one row's sequence; the mask's blocks are eight rows");
+    __shared__ S sh_a[W][C], sh_h[W][C], sh_carry[C];
+    __shared__ int sh_reset[W];
+    __shared__ unsigned sh_ticket;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (threadIdx.x == 0) sh_ticket = atomicAdd(p.ticket, 1u);
+    __syncthreads();
+    const unsigned ticket = __builtin_amdgcn_readfirstlane(sh_ticket);
+    const unsigned dgroups = (p.D + C - 1) / C, seqs = p.rows.packed ? 1u : (unsigned)p.rows.N, per = dgroups * seqs;
+    const int c = (int)(ticket / per);                 // tile along the scan
+    const unsigned rest = ticket - (unsigned)c * per;
+    const int n = (int)(rest / dgroups);
+    const int ch = (int)(rest % dgroups) * C + lane * V;
+    const bool on = ch < p.D;
+    const int chl = on ? ch : 0;                       // lanes without a channel read the first one's and write nothing
+    const long long tile_row = (long long)(REV ? p.chunks - 1 - c : c) * L;
+    const long long row0 = tile_row + (REV ? W - 1 - wave : wave) * R;
+
+    // lane j: the sequence of row row0 + j, and whether a sequence begins there (or the last one ends)
+    int seq;
+    bool live, edge;
+    {
+        const long long r = row0 + (lane <= R ? lane : R);
+        if (p.rows.packed) {
+            const int u = bounds_up_to(p.rows, r);
+            seq = u - 1;
+            live = u >= 1 && u <= p.rows.N && r < p.rows.T;
+            edge = u >= 1 && clamp_row(p.rows.bounds[u - 1], p.rows.T) == r;
+        } else {
+            const long long len = seq_length(p.rows, n);
+            seq = n;
+            live = r < len;
+            edge = r == 0 || r == len;
+        }
+    }
+    const unsigned long long live_bits = __ballot(live && lane < R), edge_bits = __ballot(edge && lane <= R);
+    const unsigned long long begins = live_bits & edge_bits, finishes = live_bits & (edge_bits >> 1);
+    const unsigned long long starts = REV ? finishes : begins, ends = REV ? begins : finishes;   // in the order of the scan
+
+    const T* g = reinterpret_cast<const T*>(p.g);
+    const T* x = reinterpret_cast<const T*>(p.x);
+    const S* init = reinterpret_cast<const S*>(REV ? p.dlast : p.h0);
+    S* fin = reinterpret_cast<S*>(REV ? p.dh0 : p.last);
+    const long long base = p.rows.packed ? 0 : (long long)n * p.rows.T;
+
+    // ---- the rows' inputs, all reads at a time ----
+    constexpr bool NEED_X = !REV || KIND == DEER_GATE_SIGMOID;
+    TV rg[R], rx[NEED_X ? R : 1], rh[REV ? R : 1], rd[REV ? R : 1];
+    unsigned keep[DROP ? V : 1];
+    if (live_bits) {
+        const int first = __builtin_ctzll(live_bits), last = 63 - __builtin_clzll(live_bits);
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int jj = j < first ? first : j > last ? last : j;      // a row that is none reads the nearest
+            const long long r = base + row0 + jj;
+            rg[j] = *reinterpret_cast<const TV*>(g + r * p.stride_gate + chl);
+            if constexpr (NEED_X) rx[j] = *reinterpret_cast<const TV*>(x + r * p.stride_in + chl);
+            if constexpr (REV) {
+                rd[j] = *reinterpret_cast<const TV*>(reinterpret_cast<const T*>(p.dh) + r * p.stride_out + chl);
+                const long long rb = r > base ? r - 1 : r;               // (the row in front of the first is h0's)
+                rh[j] = *reinterpret_cast<const TV*>(reinterpret_cast<const T*>(p.h) + rb * p.stride_out + chl);
+            }
+        }
+        if constexpr (DROP) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                keep[v] = 0;
+#pragma unroll
+                for (int b = 0; b < R / 8; ++b)
+                    keep[v] |= drop_keep8(p.drop, (unsigned)(chl + v), (unsigned)((row0 >> 3) + b), (unsigned)n) << (8 * b);
+            }
+        }
+    }
+    const S scale = DROP ? (S)p.drop.scale : S(1);
+    auto input = [&](int j, int v) -> S {
+        S xv = (S)vec_at<T, V>(rx[j], v);
+        if constexpr (DROP) xv = (keep[v] >> j) & 1u ? xv * scale : S(0);
+        return xv;
+    };
+
+    // ---- this wavefront's map ----
+    S A[V], H[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        A[v] = S(1);
+        H[v] = S(0);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = REV ? R - 1 - i : i;
+        if ((starts >> j) & 1) {
+            const long long s = __builtin_amdgcn_readlane(seq, j);
+#pragma unroll
+            for (int v = 0; v < V; ++v) H[v] = init ? init[s * p.D + chl + v] : S(0);
+        }
+        if ((live_bits >> j) & 1) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                S a, w;
+                gate_factors<T, KIND>((S)vec_at<T, V>(rg[j], v), a, w);
+                if constexpr (REV) H[v] = a * ((S)vec_at<T, V>(rd[j], v) + H[v]);
+                else H[v] = a * H[v] + w * input(j, v);
+                A[v] *= a;
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        sh_a[wave][lane * V + v] = A[v];
+        sh_h[wave][lane * V + v] = H[v];
+    }
+    if (lane == 0) sh_reset[wave] = starts != 0;
+    __syncthreads();
+
+    // ---- the first wavefront publishes the tile's map and finds its carry ----
+    if (wave == 0) {
+        S ta[V], th[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            ta[v] = A[v];
+            th[v] = H[v];
+        }
+        bool reset = starts != 0;
+        for (int w = 1; w < W; ++w) {
+            const bool r = sh_reset[w] != 0;
+            reset = reset || r;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const S a = sh_a[w][lane * V + v], h = sh_h[w][lane * V + v];
+                th[v] = r ? h : a * th[v] + h;
+                ta[v] *= a;
+            }
+        }
+        const long long D = p.D;
+        unsigned long long* agg = p.agg + ((long long)n * p.chunks * D + ch) * WORDS;
+        unsigned long long* inc = p.inc + (long long)n * p.groups * D + ch;
+        if (on) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if constexpr (WORDS == 1) {
+                    put_word(agg + (long long)c * D + v, word_of(ta[v], th[v]));
+                } else {
+                    put_word(agg + ((long long)c * D + v) * 2, word_of(ta[v]));
+                    put_word(agg + ((long long)c * D + v) * 2 + 1, word_of(th[v]));
+                }
+            }
+        }
+        S carry[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) carry[v] = S(0);
+        constexpr int j0 = REV ? R - 1 : 0;            // the tile's first row along the scan
+        if (((live_bits >> j0) & 1) && !((starts >> j0) & 1)) {
+            // the tile in which the sequence of that row began
+            long long begin;
+            if (!p.rows.packed) begin = REV ? seq_length(p.rows, n) - 1 : 0;
+            else {
+                const int s = __builtin_amdgcn_readlane(seq, j0);
+                begin = REV ? clamp_row(p.rows.bounds[s + 1], p.rows.T) - 1 : clamp_row(p.rows.bounds[s], p.rows.T);
+            }
+            const int c_first = (int)(REV ? p.chunks - 1 - begin / L : begin / L);
+            const int c_group = c / kGroup * kGroup;
+            const bool from_group = c_first < c_group;
+            const int from = from_group ? c_group : (c_first < c ? c_first : c);
+            if (on) {
+                if (from_group) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        unsigned long long w[1];
+                        wait_words<1>(inc + (long long)(c / kGroup - 1) * D + v, 0, 1, w);
+                        if constexpr (WORDS == 1) carry[v] = __uint_as_float((unsigned)(w[0] >> 32));
+                        else carry[v] = __longlong_as_double((long long)w[0]);
+                    }
+                }
+                fold_tiles<V>(agg + (long long)from * D * WORDS, D * WORDS, c - from, !from_group, carry);
+            }
+        }
+        if (on && c % kGroup == kGroup - 1) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const S out = reset ? th[v] : ta[v] * carry[v] + th[v];
+                if constexpr (WORDS == 1) put_word(inc + (long long)(c / kGroup) * D + v, word_of(0.0f, out));
+                else put_word(inc + (long long)(c / kGroup) * D + v, word_of(out));
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) sh_carry[lane * V + v] = carry[v];
+    }
+    __syncthreads();
+
+    // ---- the rows once more, from the carry ----
+    S h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = sh_carry[lane * V + v];
+    for (int w = 0; w < wave; ++w) {
+        const bool r = sh_reset[w] != 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = r ? sh_h[w][lane * V + v] : sh_a[w][lane * V + v] * h[v] + sh_h[w][lane * V + v];
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = REV ? R - 1 - i : i;
+        if (!((live_bits >> j) & 1)) continue;
+        const long long r = base + row0 + j;
+        if ((starts >> j) & 1) {
+            const long long s = __builtin_amdgcn_readlane(seq, j);
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = init ? init[s * p.D + chl + v] : S(0);
+        }
+        TV o1, o2;
+        S before[V];
+        if constexpr (REV) {
+            if ((ends >> j) & 1) {   // the row in front of the sequence's first is the initial state
+                const long long s = __builtin_amdgcn_readlane(seq, j);
+#pragma unroll
+                for (int v = 0; v < V; ++v) before[v] = p.h0 ? reinterpret_cast<const S*>(p.h0)[s * p.D + chl + v] : S(0);
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) before[v] = (S)vec_at<T, V>(rh[j], v);
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            S a, w;
+            gate_factors<T, KIND>((S)vec_at<T, V>(rg[j], v), a, w);
+            if constexpr (REV) {
+                const S lam = (S)vec_at<T, V>(rd[j], v) + h[v];
+                h[v] = a * lam;
+                S dg, du = lam;
+                if constexpr (KIND == DEER_GATE_FACTOR) dg = lam * before[v];
+                else if constexpr (KIND == DEER_GATE_LOG) dg = h[v] * before[v];
+                else {
+                    dg = h[v] * w * (before[v] - input(j, v));
+                    du = w * lam;
+                }
+                if constexpr (DROP) du = (keep[v] >> j) & 1u ? du * scale : S(0);
+                vec_set<T, V>(o1, v, (T)dg);
+                vec_set<T, V>(o2, v, (T)du);
+            } else {
+                h[v] = a * h[v] + w * input(j, v);
+                vec_set<T, V>(o1, v, (T)h[v]);
+            }
+        }
+        if (on) {
+            if constexpr (REV) {
+                *reinterpret_cast<TV*>(reinterpret_cast<T*>(p.dg) + r * p.stride_gate + ch) = o1;
+                *reinterpret_cast<TV*>(reinterpret_cast<T*>(p.dx) + r * p.stride_in + ch) = o2;
+            } else {
+                *reinterpret_cast<TV*>(reinterpret_cast<T*>(p.h) + r * p.stride_out + ch) = o1;
+            }
+            if (((ends >> j) & 1) && fin) {
+                const long long s = __builtin_amdgcn_readlane(seq, j);
+#pragma unroll
+                for (int v = 0; v < V; ++v) fin[s * p.D + ch + v] = h[v];
+            }
+        }
+    }
+}
+
+// Clears the published words and the ticket, and gives sequences without rows their final state (in the gradient: the
+// gradient of their initial state).  A kernel and no memset: the call may be captured into a graph.
+template <typename S>
+__global__ void diagrec_prepare_kernel(const DiagrecParams p, bool grad) {
+    const size_t at = (size_t)blockIdx.x * blockDim.x + threadIdx.x, all = (size_t)gridDim.x * blockDim.x;
+    for (size_t i = at; i < p.words; i += all) p.agg[i] = kUnset;
+    if (at == 0) *p.ticket = 0;
+    const S* from = reinterpret_cast<const S*>(grad ? p.dlast : p.h0);
+    S* to = reinterpret_cast<S*>(grad ? p.dh0 : p.last);
+    if (!to) return;
+    for (long long i = at; i < (long long)p.rows.N * p.D; i += all) {
+        if (seq_length(p.rows, (int)(i / p.D)) == 0) to[i] = from ? from[i] : S(0);
+    }
+}
+
+template <typename T, int KIND, bool REV, bool DROP>
+hipError_t launch_one(const DiagrecParams& p, int V, hipStream_t stream) {
+    using Sh = Shape<T, REV>;
+    const long long seqs = p.rows.packed ? 1 : p.rows.N, groups = (p.D + 64 * V - 1) / (64 * V);
+    const dim3 grid((unsigned)(seqs * groups * p.chunks)), block(64 * Sh::W);
+    if (grid.x == 0) return hipSuccess;
+    if (V == 1) hipLaunchKernelGGL((diagrec_kernel<T, KIND, 1, Sh::R, Sh::W, REV, DROP>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((diagrec_kernel<T, KIND, Sh::V, Sh::R, Sh::W, REV, DROP>), grid, block, 0, stream, p);
+    return hipGetLastError();
+}
+
+template <typename T, bool REV>
+hipError_t launch_type(const DiagrecParams& p, hipStream_t stream) {
+    using S = wide_t<T>;
+    const long long cells = (long long)p.rows.N * p.D;
+    const size_t work = p.words > (size_t)cells ? p.words : (size_t)cells;
+    const unsigned blocks = (unsigned)(work / 1024 < 1 ? 1 : work / 1024 > 2048 ? 2048 : work / 1024);
+    hipLaunchKernelGGL((diagrec_prepare_kernel<S>), dim3(blocks), dim3(256), 0, stream, p, REV);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    // vectors of V channels where every row of every array begins at a multiple of them
+    constexpr int VV = Shape<T, REV>::V;
+    auto fits = [](const void* q, long long stride) {
+        return reinterpret_cast<uintptr_t>(q) % (VV * sizeof(T)) == 0 && stride % VV == 0;
+    };
+    bool vec = p.D % VV == 0 && p.D > 64 && fits(p.g, p.stride_gate) && fits(p.x, p.stride_in) && fits(p.h, p.stride_out);
+    if (REV) vec = vec && fits(p.dh, p.stride_out) && fits(p.dg, p.stride_gate) && fits(p.dx, p.stride_in);
+    const int V = vec ? VV : 1;
+    const bool drop = p.drop.cut != 0;
+    switch (p.gate) {
+        case DEER_GATE_FACTOR: return drop ? launch_one<T, DEER_GATE_FACTOR, REV, true>(p, V, stream) : launch_one<T, DEER_GATE_FACTOR, REV, false>(p, V, stream);
+        case DEER_GATE_LOG: return drop ? launch_one<T, DEER_GATE_LOG, REV, true>(p, V, stream) : launch_one<T, DEER_GATE_LOG, REV, false>(p, V, stream);
+        default: return drop ? launch_one<T, DEER_GATE_SIGMOID, REV, true>(p, V, stream) : launch_one<T, DEER_GATE_SIGMOID, REV, false>(p, V, stream);
+    }
+}
+
+// One token for every row: state <- a state + u in place.  A row whose slot is out of range, or has come in an earlier row, is
+// passed over.  Latency bound: one launch, every lane one channel, the slots in front looked at while the operands are on their way.
+template <typename T, int KIND>
+__global__ __launch_bounds__(256) void diagstep_kernel(const DiagstepParams p) {
+    using S = wide_t<T>;
+    const int per = (p.D + 255) / 256, n = blockIdx.x / per, ch = (blockIdx.x % per) * 256 + threadIdx.x;
+    int slot = n;
+    bool twice = false;
+    if (p.rows.slots) {
+        slot = p.rows.slots[n];
+        for (int m = threadIdx.x; m < n; m += 256) twice = twice || p.rows.slots[m] == slot;
+    }
+    const bool in = ch < p.D && slot >= 0 && slot < p.rows.n_slots;
+    S g = S(0), x = S(0), h = S(0);
+    S* state = reinterpret_cast<S*>(p.state) + (long long)slot * p.D + ch;
+    if (in) {
+        g = (S)reinterpret_cast<const T*>(p.g)[(long long)n * p.stride_gate + ch];
+        x = (S)reinterpret_cast<const T*>(p.x)[(long long)n * p.stride_in + ch];
+        h = *state;
+    }
+    twice = p.rows.slots ? __syncthreads_or(twice) != 0 : false;
+    if (!in || twice) return;
+    S a, w;
+    gate_factors<T, KIND>(g, a, w);
+    h = a * h + w * x;
+    *state = h;
+    reinterpret_cast<T*>(p.h)[(long long)n * p.stride_out + ch] = (T)h;
+}
+
+template <typename T>
+hipError_t launch_step_type(const DiagstepParams& p, hipStream_t stream) {
+    const dim3 grid((unsigned)((long long)((p.D + 255) / 256) * p.rows.N)), block(256);
+    if (p.gate == DEER_GATE_FACTOR) hipLaunchKernelGGL((diagstep_kernel<T, DEER_GATE_FACTOR>), grid, block, 0, stream, p);
+    else if (p.gate == DEER_GATE_LOG) hipLaunchKernelGGL((diagstep_kernel<T, DEER_GATE_LOG>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((diagstep_kernel<T, DEER_GATE_SIGMOID>), grid, block, 0, stream, p);
+    return hipGetLastError();
+}
+
+template <typename T, bool REV> constexpr int tile_rows() { return Shape<T, REV>::R * Shape<T, REV>::W; }
+
+}  // namespace
+
+size_t diagrec_words(int dtype, int gate, int N, long long T, int D, bool grad, int* chunks, int* groups, size_t* agg_words) {
+    (void)gate;
+    const int L = dtype == DEER_F64   ? (grad ? tile_rows<double, true>() : tile_rows<double, false>())
+                  : dtype == DEER_F32 ? (grad ? tile_rows<float, true>() : tile_rows<float, false>())
+                                      : (grad ? tile_rows<BF16, true>() : tile_rows<BF16, false>());
+    const long long c = (T + L - 1) / L, g = (c + kGroup - 1) / kGroup;
+    *chunks = (int)c;
+    *groups = (int)g;
+    *agg_words = (size_t)N * c * D * (dtype == DEER_F64 ? 2 : 1);
+    return *agg_words + (size_t)N * g * D;
+}
+
+hipError_t launch_diagrec(int dtype, bool grad, const DiagrecParams& p, hipStream_t stream) {
+    switch (dtype) {
+        case DEER_F32: return grad ? launch_type<float, true>(p, stream) : launch_type<float, false>(p, stream);
+        case DEER_F64: return grad ? launch_type<double, true>(p, stream) : launch_type<double, false>(p, stream);
+        case DEER_BF16: return grad ? launch_type<BF16, true>(p, stream) : launch_type<BF16, false>(p, stream);
+        default: return grad ? launch_type<F16, true>(p, stream) : launch_type<F16, false>(p, stream);
+    }
+}
+
+hipError_t launch_diagstep(int dtype, const DiagstepParams& p, hipStream_t stream) {
+    switch (dtype) {
+        case DEER_F32: return launch_step_type<float>(p, stream);
+        case DEER_F64: return launch_step_type<double>(p, stream);
+        case DEER_BF16: return launch_step_type<BF16>(p, stream);
+        default: return launch_step_type<F16>(p, stream);
+    }
+}
+
+}  // namespace deer

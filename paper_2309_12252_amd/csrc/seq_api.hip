@@ -1,0 +1,210 @@
+// C entry points of the sequence operators (include/deer.h): checks of the arguments, the workspace's layout, launches.  Nothing
+// here allocates or synchronises.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdio>
+
+#include "seq_common.h"
+
+using namespace deer;
+
+namespace {
+
+constexpr size_t kAlign = 256;
+size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+
+deer_status fail(deer_status st, const char* text) {
+    set_last_error(text);
+    return st;
+}
+deer_status launched(const char* what, hipError_t e) {
+    if (e == hipSuccess) return DEER_OK;
+    char text[160];
+    std::snprintf(text, sizeof(text), "%s: %s", what, hipGetErrorString(e));
+    return fail(DEER_ERR_HIP, text);
+}
+
+bool known_type(int dtype) { return dtype == DEER_F32 || dtype == DEER_F64 || dtype == DEER_BF16 || dtype == DEER_F16; }
+size_t type_bytes(int dtype) { return dtype == DEER_F64 ? 8 : dtype == DEER_F32 ? 4 : 2; }
+bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+// The mask's counter has 32 bits for blocks of eight rows and for channels; rows and columns are kept where products of them with
+// element sizes stay far from 63 bits.
+constexpr int64_t kMostRows = (int64_t)1 << 33;
+
+const char* bad_drop(double p) {
+    if (!(p >= 0.0 && p < 1.0)) return "dropout: the share that is dropped must lie in [0, 1)";
+    if (std::lround(p * 65536.0) > 65535) return "dropout: the share that is dropped must be at most 1 - 2^-16";
+    return nullptr;
+}
+DropParams drop_params(double p, uint64_t seed, uint32_t draw) {
+    DropParams d;
+    d.seed_lo = (unsigned)seed;
+    d.seed_hi = (unsigned)(seed >> 32);
+    d.draw = draw;
+    d.cut = (unsigned)std::lround(p * 65536.0);
+    d.scale = 65536.0 / (65536.0 - d.cut);
+    return d;
+}
+
+const char* bad_config(const deer_diagrec_config* c, bool step) {
+    if (!c) return "config is NULL";
+    if (!known_type(c->dtype)) return "unknown dtype";
+    if (c->gate != DEER_GATE_FACTOR && c->gate != DEER_GATE_LOG && c->gate != DEER_GATE_SIGMOID) return "unknown gate";
+    if (c->N < 1 || c->D < 1) return "N and D must be positive";
+    if (c->stride_gate < 0 || c->stride_in < 0 || c->stride_out < 0) return "strides must not be negative";
+    if ((c->stride_gate && c->stride_gate < c->D) || (c->stride_in && c->stride_in < c->D) || (c->stride_out && c->stride_out < c->D))
+        return "a stride is smaller than a row";
+    if (step) return nullptr;
+    if (c->T < 0 || (c->packed != 0 && c->packed != 1)) return "T must not be negative, packed 0 or 1";
+    return bad_drop(c->drop);
+}
+bool too_large(const deer_diagrec_config* c) {
+    const long long seqs = c->packed ? 1 : c->N;
+    if (c->T > kMostRows) return true;
+    const long long tiles = (c->T + 63) / 64, cols = (c->D + 63) / 64;   // (the smallest tiles of any type)
+    return (long double)tiles * cols * seqs > 2147483647.0L || (long double)c->N * c->D > 1e15L;
+}
+
+struct DiagLayout {
+    int chunks, groups;
+    size_t agg_words, words, total;
+};
+DiagLayout diag_layout(const deer_diagrec_config* c, bool grad) {
+    DiagLayout l;
+    l.words = diagrec_words(c->dtype, c->gate, c->packed ? 1 : c->N, c->T, c->D, grad, &l.chunks, &l.groups, &l.agg_words);
+    l.total = kAlign + align_up(l.words * 8);
+    return l;
+}
+
+DiagrecParams diag_params(const deer_diagrec_config* c, const DiagLayout& l, const int64_t* bounds, void* ws) {
+    DiagrecParams p{};
+    p.rows = SeqRows{reinterpret_cast<const long long*>(bounds), c->T, c->N, c->packed};
+    p.D = c->D;
+    p.gate = c->gate;
+    p.stride_gate = c->stride_gate ? c->stride_gate : c->D;
+    p.stride_in = c->stride_in ? c->stride_in : c->D;
+    p.stride_out = c->stride_out ? c->stride_out : c->D;
+    p.drop = drop_params(c->drop, c->seed, c->draw);
+    p.chunks = l.chunks;
+    p.groups = l.groups;
+    p.ticket = reinterpret_cast<unsigned*>(ws);
+    p.agg = reinterpret_cast<unsigned long long*>(reinterpret_cast<char*>(ws) + kAlign);
+    p.inc = p.agg + l.agg_words;
+    p.words = l.words;
+    return p;
+}
+
+deer_status check_workspace(const void* ws, size_t have, size_t need) {
+    if (!ws || misaligned(ws, kAlign) || have < need) {
+        char text[160];
+        std::snprintf(text, sizeof(text), "workspace NULL, misaligned or smaller than the %zu bytes needed", need);
+        return fail(DEER_ERR_WORKSPACE, text);
+    }
+    return DEER_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+deer_status deer_diagrec_workspace_bytes(const deer_diagrec_config* c, int32_t grad, size_t* bytes) {
+    if (!bytes) return fail(DEER_ERR_INVALID_ARG, "bytes is NULL");
+    if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds");
+    *bytes = diag_layout(c, grad != 0).total;
+    return DEER_OK;
+}
+
+deer_status deer_diagrec_solve(const deer_diagrec_config* c, const void* d_gate, const void* d_in, const void* d_h0, const int64_t* d_bounds,
+                               void* d_h, void* d_last, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds");
+    if ((c->T > 0 && (!d_gate || !d_in || !d_h)) || (c->packed && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
+    if (misaligned(d_gate, e) || misaligned(d_in, e) || misaligned(d_h, e) || misaligned(d_h0, w) || misaligned(d_last, w) || misaligned(d_bounds, 8))
+        return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
+    const DiagLayout l = diag_layout(c, false);
+    if (deer_status st = check_workspace(d_workspace, workspace_bytes, l.total)) return st;
+    DiagrecParams p = diag_params(c, l, d_bounds, d_workspace);
+    p.g = d_gate;
+    p.x = d_in;
+    p.h0 = d_h0;
+    p.h = d_h;
+    p.last = d_last;
+    return launched("deer_diagrec_solve", launch_diagrec(c->dtype, false, p, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+deer_status deer_diagrec_grad(const deer_diagrec_config* c, const void* d_gate, const void* d_in, const void* d_h0, const int64_t* d_bounds,
+                              const void* d_h, const void* d_dh, const void* d_dlast, void* d_dgate, void* d_din, void* d_dh0,
+                              void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds");
+    if ((c->T > 0 && (!d_gate || !d_in || !d_h || !d_dh || !d_dgate || !d_din)) || (c->packed && !d_bounds))
+        return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
+    if (misaligned(d_gate, e) || misaligned(d_in, e) || misaligned(d_h, e) || misaligned(d_dh, e) || misaligned(d_dgate, e) || misaligned(d_din, e) ||
+        misaligned(d_h0, w) || misaligned(d_dlast, w) || misaligned(d_dh0, w) || misaligned(d_bounds, 8))
+        return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
+    const DiagLayout l = diag_layout(c, true);
+    if (deer_status st = check_workspace(d_workspace, workspace_bytes, l.total)) return st;
+    DiagrecParams p = diag_params(c, l, d_bounds, d_workspace);
+    p.g = d_gate;
+    p.x = d_in;
+    p.h0 = d_h0;
+    p.h = const_cast<void*>(d_h);   // (read only in this direction)
+    p.dh = d_dh;
+    p.dlast = d_dlast;
+    p.dg = d_dgate;
+    p.dx = d_din;
+    p.dh0 = d_dh0;
+    return launched("deer_diagrec_grad", launch_diagrec(c->dtype, true, p, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+deer_status deer_diagrec_step(const deer_diagrec_config* c, const void* d_gate, const void* d_in, const int32_t* d_slots, int32_t n_slots,
+                              void* d_state, void* d_h, void* hip_stream) {
+    if (const char* why = bad_config(c, true)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (n_slots < 1) return fail(DEER_ERR_INVALID_ARG, "n_slots must be positive");
+    if (!d_gate || !d_in || !d_state || !d_h) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
+    if (misaligned(d_gate, e) || misaligned(d_in, e) || misaligned(d_h, e) || misaligned(d_state, w) || misaligned(d_slots, 4))
+        return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
+    if ((long long)c->N * ((c->D + 255) / 256) > 2147483647ll) return fail(DEER_ERR_UNSUPPORTED, "more rows than a launch holds");
+    DiagstepParams p{};
+    p.rows = StepRows{d_slots, c->N, n_slots};
+    p.D = c->D;
+    p.gate = c->gate;
+    p.stride_gate = c->stride_gate ? c->stride_gate : c->D;
+    p.stride_in = c->stride_in ? c->stride_in : c->D;
+    p.stride_out = c->stride_out ? c->stride_out : c->D;
+    p.g = d_gate;
+    p.x = d_in;
+    p.state = d_state;
+    p.h = d_h;
+    return launched("deer_diagrec_step", launch_diagstep(c->dtype, p, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+deer_status deer_dropout(int32_t dtype, int32_t N, int64_t T, int32_t D, const void* d_x, int64_t stride_in, void* d_y, int64_t stride_out,
+                         double p, uint64_t seed, uint32_t draw, void* hip_stream) {
+    if (!known_type(dtype)) return fail(DEER_ERR_INVALID_ARG, "unknown dtype");
+    if (N < 1 || D < 1 || T < 0) return fail(DEER_ERR_INVALID_ARG, "N and D must be positive, T not negative");
+    if (stride_in < 0 || stride_out < 0 || (stride_in && stride_in < D) || (stride_out && stride_out < D))
+        return fail(DEER_ERR_INVALID_ARG, "a stride is negative or smaller than a row");
+    if (const char* why = bad_drop(p)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (T > 0 && (!d_x || !d_y)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    if (misaligned(d_x, type_bytes(dtype)) || misaligned(d_y, type_bytes(dtype))) return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
+    if (T > kMostRows || (long double)N * ((T + 7) / 8) * D > 256.0L * 2147483647.0L) return fail(DEER_ERR_UNSUPPORTED, "more elements than a launch holds");
+    DropoutParams q{};
+    q.N = N;
+    q.D = D;
+    q.T = T;
+    q.stride_in = stride_in ? stride_in : D;
+    q.stride_out = stride_out ? stride_out : D;
+    q.x = d_x;
+    q.y = d_y;
+    q.drop = drop_params(p, seed, draw);
+    return launched("deer_dropout", launch_dropout(dtype, q, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+}  // extern "C"

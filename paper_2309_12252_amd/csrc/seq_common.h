@@ -1,0 +1,137 @@
+// Shared declarations of the sequence operators (gated linear recurrences, dropout): element types, the way rows belong to
+// sequences, the counter-based generator, and the launch interface between seq_api.hip and the kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/deer.h"
+
+namespace deer {
+
+// How the rows of an array belong to sequences.  Packed: N sequences one behind the other in T rows, sequence s in rows
+// bounds[s] .. bounds[s + 1] - 1.  Otherwise N sequences of T rows each, of which the first bounds[n] count (all without bounds).
+// Bounds are device data that the host has not seen: whatever they hold is clamped to 0 .. T before it is used as a row.
+struct SeqRows {
+    const long long* bounds;
+    long long T;
+    int N;
+    int packed;
+};
+
+__device__ __forceinline__ long long clamp_row(long long v, long long T) { return v < 0 ? 0 : v > T ? T : v; }
+
+// how many of the packed sequences' N + 1 bounds are at most `row`
+__device__ __forceinline__ int bounds_up_to(const SeqRows& s, long long row) {
+    int lo = 0, hi = s.N + 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (clamp_row(s.bounds[mid], s.T) <= row) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ long long seq_length(const SeqRows& s, int n) {
+    if (s.packed) {
+        const long long a = clamp_row(s.bounds[n], s.T), b = clamp_row(s.bounds[n + 1], s.T);
+        return b > a ? b - a : 0;
+    }
+    return s.bounds ? clamp_row(s.bounds[n], s.T) : s.T;
+}
+
+// ---- element types: arithmetic in 32 bits for the 16-bit types and fp32, in 64 for fp64 ----
+using BF16 = __bf16;
+using F16 = _Float16;
+template <typename T> struct Wide { using type = float; };
+template <> struct Wide<double> { using type = double; };
+template <typename T> using wide_t = typename Wide<T>::type;
+template <typename T, int V> struct Vec { using type = T __attribute__((ext_vector_type(V))); };
+template <typename T> struct Vec<T, 1> { using type = T; };
+template <typename T, int V> using vec_t = typename Vec<T, V>::type;
+template <typename T, int V>
+__device__ __forceinline__ T vec_at(const vec_t<T, V>& v, int i) {
+    if constexpr (V == 1) return v;
+    else return v[i];
+}
+template <typename T, int V>
+__device__ __forceinline__ void vec_set(vec_t<T, V>& v, int i, T x) {
+    if constexpr (V == 1) v = x;
+    else v[i] = x;
+}
+
+// ---- dropout: Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) ----
+// One block of 128 bits serves eight rows of one channel, 16 bits a row: counter (channel, row / 8, sequence, draw), key = seed.
+// Eight rows of a channel rather than eight channels of a row: a lane of the recurrence keeps one channel and runs over
+// rows, so it uses a whole block whatever the vector width of its loads.
+struct DropParams {
+    unsigned seed_lo, seed_hi, draw;
+    unsigned cut;        // an element is dropped where its 16 bits are below cut
+    double scale;        // 2^16 / (2^16 - cut)
+};
+
+// bit i: row 8 * block + i is kept
+__device__ __forceinline__ unsigned drop_keep8(const DropParams& d, unsigned channel, unsigned block, unsigned seq) {
+    unsigned c0 = channel, c1 = block, c2 = seq, c3 = d.draw, k0 = d.seed_lo, k1 = d.seed_hi;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const unsigned long long p = (unsigned long long)c0 * 0xD2511F53u, q = (unsigned long long)c2 * 0xCD9E8D57u;
+        c0 = (unsigned)(q >> 32) ^ c1 ^ k0;
+        c2 = (unsigned)(p >> 32) ^ c3 ^ k1;
+        c1 = (unsigned)q;
+        c3 = (unsigned)p;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    const unsigned w[4] = {c0, c1, c2, c3};
+    unsigned keep = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        keep |= ((w[i] & 0xFFFFu) >= d.cut ? 1u : 0u) << (2 * i);
+        keep |= ((w[i] >> 16) >= d.cut ? 1u : 0u) << (2 * i + 1);
+    }
+    return keep;
+}
+
+// ---- launches ----
+void set_last_error(const char* text) noexcept;   // what deer_last_error(NULL) returns on this thread
+
+struct DiagrecParams {
+    SeqRows rows;
+    int D, gate;
+    long long stride_gate, stride_in, stride_out;   // elements from a row to the next
+    const void *g, *x, *h0;
+    void *h, *last;                                 // forward: outputs; gradient: h is an input
+    const void *dh, *dlast;                         // gradient
+    void *dg, *dx, *dh0;
+    DropParams drop;
+    // words that tiles publish for each other
+    int chunks, groups;                             // tiles and groups of tiles along a sequence
+    unsigned long long *agg, *inc;
+    unsigned* ticket;
+    size_t words;                                   // 8-byte words from agg on, cleared before the launch
+};
+struct StepRows {
+    const int* slots;      // [N] or nullptr (row n has slot n)
+    int N, n_slots;
+};
+struct DiagstepParams {
+    StepRows rows;
+    int D, gate;
+    long long stride_gate, stride_in, stride_out;
+    const void *g, *x;
+    void *state, *h;
+};
+struct DropoutParams {
+    int N, D;
+    long long T, stride_in, stride_out;
+    const void* x;
+    void* y;
+    DropParams drop;
+};
+
+size_t diagrec_words(int dtype, int gate, int N, long long T, int D, bool grad, int* chunks, int* groups, size_t* agg_words);
+hipError_t launch_diagrec(int dtype, bool grad, const DiagrecParams& p, hipStream_t stream);
+hipError_t launch_diagstep(int dtype, const DiagstepParams& p, hipStream_t stream);
+hipError_t launch_dropout(int dtype, const DropoutParams& p, hipStream_t stream);
+
+}  // namespace deer

@@ -6,6 +6,7 @@ library has not been built (``python -m paper_2309_12252_amd.build``); there is 
 CPU fallback.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -15,10 +16,12 @@ LIB_PATH = os.path.join(_HERE, "libdeer_hip.so")
 
 DEER_OK, DEER_ERR_INVALID_ARG, DEER_ERR_UNSUPPORTED, DEER_ERR_WORKSPACE, DEER_ERR_HIP, DEER_ERR_NONFINITE = range(6)
 DEER_CELL_GRU, DEER_CELL_MLP_ODE, DEER_CELL_LSTM, DEER_CELL_LEM = 0, 1, 2, 3
-DEER_F32, DEER_F64 = 0, 1
+DEER_F32, DEER_F64, DEER_BF16, DEER_F16 = 0, 1, 2, 3
+DEER_GATE_FACTOR, DEER_GATE_LOG, DEER_GATE_SIGMOID = 0, 1, 2
 
 EXPORTS = ["deer_theta_count", "deer_workspace_bytes", "deer_create", "deer_eval", "deer_grad",
-           "deer_linrec_solve", "deer_linrec_solve_static", "deer_set_profiling", "deer_get_profile", "deer_last_error", "deer_destroy"]
+           "deer_linrec_solve", "deer_linrec_solve_static", "deer_set_profiling", "deer_get_profile", "deer_last_error", "deer_destroy",
+           "deer_diagrec_workspace_bytes", "deer_diagrec_solve", "deer_diagrec_grad", "deer_diagrec_step", "deer_dropout"]
 
 
 class DeerConfig(ctypes.Structure):
@@ -37,6 +40,13 @@ class DeerProfile(ctypes.Structure):
                 ("fused_ms", ctypes.c_double), ("fused_launches", ctypes.c_int64),
                 ("newton_ms", ctypes.c_double), ("newton_launches", ctypes.c_int64),
                 ("newton_iterations", ctypes.c_int64)]
+
+
+class DiagrecConfig(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("N", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("T", ctypes.c_int64), ("packed", ctypes.c_int32), ("draw", ctypes.c_uint32),
+                ("stride_gate", ctypes.c_int64), ("stride_in", ctypes.c_int64), ("stride_out", ctypes.c_int64),
+                ("drop", ctypes.c_double), ("seed", ctypes.c_uint64)]
 
 
 class DeerError(RuntimeError):
@@ -81,6 +91,15 @@ def load_library():
     lib.deer_last_error.argtypes = [vp]
     lib.deer_destroy.restype = None
     lib.deer_destroy.argtypes = [vp]
+    size, i64, u32, u64 = ctypes.c_size_t, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64
+    dcp = ctypes.POINTER(DiagrecConfig)
+    for name, args in (("deer_diagrec_workspace_bytes", [dcp, i32, ctypes.POINTER(size)]),
+                       ("deer_diagrec_solve", [dcp] + [vp] * 7 + [size, vp]),
+                       ("deer_diagrec_grad", [dcp] + [vp] * 11 + [size, vp]),
+                       ("deer_diagrec_step", [dcp] + [vp] * 3 + [i32] + [vp] * 3),
+                       ("deer_dropout", [i32, i32, i64, i32, vp, i64, vp, i64, dbl, u64, u32, vp])):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
     _lib = lib
     return lib
 
@@ -232,6 +251,206 @@ def linrec_solve_static(A, b, y0=None, reverse=False, out=None, status=None, str
                                       ctypes.c_void_p(stream.cuda_stream), _ptr(status))
     if st != DEER_OK:
         raise DeerError(st, lib.deer_last_error(None).decode())
+    return y
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Sequence operators.  Every call is asynchronous on `stream` (default: torch's current stream of the tensors' device); outputs
+# and workspaces come from torch's allocator on that stream, a workspace for every call, so calls on several
+# streams, in several threads and captured into several graphs do not meet in one.
+# ---------------------------------------------------------------------------------------------------------------------
+_DTYPES = {torch.float32: DEER_F32, torch.float64: DEER_F64, torch.bfloat16: DEER_BF16, torch.float16: DEER_F16}
+
+
+def _need(ok, text):
+    if not ok:
+        raise DeerError(DEER_ERR_INVALID_ARG, text)
+
+
+def _raise(lib, st):
+    raise DeerError(st, lib.deer_last_error(None).decode())
+
+
+def _on_stream(f):
+    """Runs f with the device of its first argument current, and with its keyword `stream` as that device's current stream."""
+    @functools.wraps(f)
+    def call(first, *args, stream=None, **kw):
+        _need(isinstance(first, torch.Tensor) and first.is_cuda, "need device tensors")
+        if stream is not None:
+            _need(stream.device == first.device, "the stream belongs to another device than the tensors")
+            with torch.cuda.stream(stream):
+                return f(first, *args, **kw)
+        if first.device.index == torch.cuda.current_device():
+            return f(first, *args, **kw)
+        with torch.cuda.device(first.device):
+            return f(first, *args, **kw)
+    return call
+
+
+def _stream_of(t):
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _wide(dtype):
+    return torch.float64 if dtype == torch.float64 else torch.float32
+
+
+def _row_stride(t, what, lead):
+    """Elements from a row of t to the next: the last dimension dense, `lead` leading dimensions that lie like rows one behind another."""
+    _need(t.stride(-1) == 1 or t.shape[-1] <= 1, what + ": the last dimension must be dense")
+    inner = 1
+    for k in range(t.dim() - 1, lead - 1, -1):
+        _need(t.shape[k] <= 1 or t.stride(k) == inner, what + ": the dimensions behind the rows must be dense")
+        inner *= t.shape[k]
+    if lead == 1:
+        rows, first = t.shape[0], t.stride(0)
+    else:
+        rows, first = t.shape[0] * t.shape[1], t.stride(1) if t.shape[1] > 1 else t.stride(0)
+        _need(t.shape[0] <= 1 or t.shape[1] <= 1 or t.stride(0) == t.shape[1] * t.stride(1), what + ": sequences must lie one behind another")
+    if rows <= 1 or first < inner:
+        _need(rows <= 1 or t.numel() == 0, what + ": rows must not overlap")
+        return inner
+    return first
+
+
+def _check_like(t, what, shape, dtype, device):
+    _need(isinstance(t, torch.Tensor) and t.device == device, what + ": need a tensor on the same device")
+    _need(t.dtype == dtype, "%s: need %s, got %s" % (what, dtype, t.dtype))
+    _need(tuple(t.shape) == tuple(shape), "%s: need shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+
+
+def _dense(t, what, shape, dtype, device):
+    if t is None:
+        return 0
+    _check_like(t, what, shape, dtype, device)
+    _need(t.is_contiguous(), what + ": must be contiguous")
+    return t.data_ptr()
+
+
+def _rows_of(x, inner, offsets, lengths):
+    """(N, T, packed, pointer of the bounds, leading dimensions) of x [N, T, ...] with optional `lengths` int64 [N], or of packed
+    rows [rows, ...] with `offsets` int64 [N + 1]"""
+    if offsets is not None:
+        _need(lengths is None, "offsets (packed rows) and lengths (a padded batch) exclude each other")
+        _need(x.dim() == 1 + inner, "packed rows have no dimension for the sequences")
+        _need(offsets.dim() == 1 and offsets.shape[0] >= 2, "offsets: need [N + 1], N >= 1")
+        return offsets.shape[0] - 1, x.shape[0], 1, _dense(offsets, "offsets", offsets.shape, torch.int64, x.device), 1
+    _need(x.dim() == 2 + inner, "need [N, T, ...], or [rows, ...] with offsets")
+    return x.shape[0], x.shape[1], 0, _dense(lengths, "lengths", (x.shape[0],), torch.int64, x.device), 2
+
+
+def _diag_config(x, gate, h, kind, offsets, lengths, drop, seed, draw):
+    _need(isinstance(gate, torch.Tensor) and isinstance(x, torch.Tensor), "need device tensors")
+    _need(x.dtype in _DTYPES, "need float32, float64, bfloat16 or float16")
+    _check_like(x, "x", gate.shape, gate.dtype, gate.device)
+    N, T, packed, bounds, lead = _rows_of(x, 1, offsets, lengths)
+    D = x.shape[-1]
+    cfg = DiagrecConfig(_DTYPES[x.dtype], int(kind), N, D, T, packed, int(draw) & 0xFFFFFFFF, _row_stride(gate, "gate", lead),
+                        _row_stride(x, "x", lead), _row_stride(h, "h", lead) if h is not None else D, float(drop),
+                        int(seed) & 0xFFFFFFFFFFFFFFFF)
+    return cfg, bounds
+
+
+def _diag_workspace(lib, cfg, grad, device):
+    size = ctypes.c_size_t(0)
+    st = lib.deer_diagrec_workspace_bytes(ctypes.byref(cfg), grad, ctypes.byref(size))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return torch.empty(size.value, dtype=torch.uint8, device=device)   # (torch's blocks are aligned to 512 bytes)
+
+
+@_on_stream
+def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, lengths=None, drop=0.0, seed=0, draw=0, out=None):
+    """deer_diagrec_solve: h_t = a_t h_{t-1} + u_t for every channel (a, u from gate and x: see deer_gate).  gate, x [N, T, D] with
+    optional int64 `lengths` [N], or packed [rows, D] with int64 `offsets` [N + 1]; rows may be slices of wider ones.  h0 [N, D] in
+    float32 (float64 with float64).  Rows of no sequence are left as they are in `out`.  Returns (h, state behind the last rows)."""
+    lib = load_library()
+    h = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check_like(h, "out", x.shape, x.dtype, x.device)
+    cfg, bounds = _diag_config(x, gate, h, kind, offsets, lengths, drop, seed, draw)
+    w = _wide(x.dtype)
+    h0p = _dense(h0, "h0", (cfg.N, cfg.D), w, x.device)
+    last = torch.empty((cfg.N, cfg.D), dtype=w, device=x.device)
+    ws = _diag_workspace(lib, cfg, 0, x.device)
+    st = lib.deer_diagrec_solve(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), last.data_ptr(), ws.data_ptr(),
+                                ws.numel(), _stream_of(x))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return h, last
+
+
+@_on_stream
+def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, offsets=None, lengths=None, drop=0.0, seed=0, draw=0,
+                 dgate=None, dx=None):
+    """deer_diagrec_grad at the trajectory h: (dL/dgate, dL/dx, dL/dh0) from dh = dL/dh and dlast = dL/d(final state).  dgate and dx, where
+    given, have the row strides of gate and x."""
+    lib = load_library()
+    cfg, bounds = _diag_config(x, gate, h, kind, offsets, lengths, drop, seed, draw)
+    lead, w, dev = 1 if cfg.packed else 2, _wide(x.dtype), x.device
+    _check_like(h, "h", x.shape, x.dtype, dev)
+    _check_like(dh, "dh", x.shape, x.dtype, dev)
+    if _row_stride(dh, "dh", lead) != cfg.stride_out:
+        h, dh = h.contiguous(), dh.contiguous()
+        cfg.stride_out = cfg.D
+    if dgate is None:
+        dgate = torch.empty_strided(gate.shape, gate.stride(), dtype=x.dtype, device=dev) if gate.is_contiguous() else _rows_like(gate, cfg.stride_gate)
+    if dx is None:
+        dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=dev) if x.is_contiguous() else _rows_like(x, cfg.stride_in)
+    for t, name, stride in ((dgate, "dgate", cfg.stride_gate), (dx, "dx", cfg.stride_in)):
+        _check_like(t, name, x.shape, x.dtype, dev)
+        _need(_row_stride(t, name, lead) == stride, name + ": rows must lie like those of what it is the gradient of")
+    h0p, dlp = _dense(h0, "h0", (cfg.N, cfg.D), w, dev), _dense(dlast, "dlast", (cfg.N, cfg.D), w, dev)
+    dh0 = torch.empty((cfg.N, cfg.D), dtype=w, device=dev)
+    ws = _diag_workspace(lib, cfg, 1, dev)
+    st = lib.deer_diagrec_grad(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), dh.data_ptr(), dlp, dgate.data_ptr(),
+                               dx.data_ptr(), dh0.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(x))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return dgate, dx, dh0
+
+
+def _rows_like(t, stride):
+    """an array of t's shape whose rows lie `stride` elements apart, as slices of a wider one do"""
+    strides = [1] * t.dim()
+    for k in range(t.dim() - 2, -1, -1):
+        strides[k] = stride if k == t.dim() - 2 else strides[k + 1] * t.shape[k + 1]
+    return torch.empty_strided(t.shape, strides, dtype=t.dtype, device=t.device)
+
+
+@_on_stream
+def diagrec_step(gate, x, state, *, kind=DEER_GATE_FACTOR, slots=None, out=None):
+    """deer_diagrec_step: one token for each of N rows, gate and x [N, D]; `state` [slots, D] (float32; float64 with float64) is updated
+    in place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over.  Returns h [N, D]."""
+    lib = load_library()
+    _need(isinstance(x, torch.Tensor) and x.dtype in _DTYPES and x.dim() == 2, "need x [N, D] in float32, float64, bfloat16 or float16")
+    _check_like(gate, "gate", x.shape, x.dtype, x.device)
+    h = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check_like(h, "out", x.shape, x.dtype, x.device)
+    _need(state.dim() == 2, "state: need [slots, D]")
+    sp = _dense(state, "state", (state.shape[0], x.shape[1]), _wide(x.dtype), x.device)
+    tp = _dense(slots, "slots", (x.shape[0],), torch.int32, x.device)
+    cfg = DiagrecConfig(_DTYPES[x.dtype], int(kind), x.shape[0], x.shape[1], 1, 0, 0, _row_stride(gate, "gate", 1), _row_stride(x, "x", 1),
+                        _row_stride(h, "out", 1), 0.0, 0)
+    st = lib.deer_diagrec_step(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), tp, state.shape[0], sp, h.data_ptr(), _stream_of(x))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return h
+
+
+@_on_stream
+def dropout(x, p, seed, draw=0, *, out=None):
+    """deer_dropout: x [N, T, D] or packed [rows, D] with a share p dropped and the rest divided by 1 - p; the backward pass is the same
+    call on the gradient.  `out` may be x."""
+    lib = load_library()
+    _need(x.dtype in _DTYPES and x.dim() in (2, 3), "need x [N, T, D] or [rows, D] in float32, float64, bfloat16 or float16")
+    y = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check_like(y, "out", x.shape, x.dtype, x.device)
+    lead = x.dim() - 1
+    N, T, D = (x.shape[0], x.shape[1], x.shape[2]) if lead == 2 else (1, x.shape[0], x.shape[1])
+    st = lib.deer_dropout(_DTYPES[x.dtype], N, T, D, x.data_ptr(), _row_stride(x, "x", lead), y.data_ptr(), _row_stride(y, "out", lead), float(p),
+                          int(seed) & 0xFFFFFFFFFFFFFFFF, int(draw) & 0xFFFFFFFF, _stream_of(x))
+    if st != DEER_OK:
+        _raise(lib, st)
     return y
 
 

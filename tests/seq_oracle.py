@@ -1,0 +1,104 @@
+"""Plain 64-bit forms of the sequence operators, row by row on the host, with running bounds of the rounding errors that 32-bit
+(or 64-bit) arithmetic may make, for the tests' tolerances.
+
+The bounds: a state h_t = a_t h_{t-1} + u_t computed in any association of its products and sums is off by at most E_t,
+E_t = |a_t| E_{t-1} + c u (|a_t| M_{t-1} + |u_t|), where M is the same recurrence over absolute values, u the unit roundoff and c counts the
+roundings that one row adds to every term that passes it: the factor itself (its exp or sigmoid), its product into the running
+product of the factors, the product with the state and the sum, of the term's input likewise.
+"""
+import numpy as np
+import torch
+
+TYPES = {"f32": torch.float32, "f64": torch.float64, "bf16": torch.bfloat16, "f16": torch.float16}
+# half a step of the output type, relative; smallest step, absolute (16-bit floats and below have numbers without leading one)
+HALF = {"f32": 2.0 ** -24, "f64": 2.0 ** -53, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 2.0 ** -126, "f64": 1e-300, "bf16": 2.0 ** -126, "f16": 2.0 ** -24}
+UNIT = {"f32": 2.0 ** -24, "f64": 2.0 ** -53, "bf16": 2.0 ** -24, "f16": 2.0 ** -24}
+# roundings a row adds: 2 sums and products and 1 product of factors, 2 more for the carry's, and the factor: exp within 1 ulp = 2 u (sigmoid: exp, sum,
+# reciprocal, product = 5 u).  With 16-bit inputs the hardware's exp and reciprocal: 2 ulp of 2^x, and the product
+# with log2 e in front of it rounds an argument of up to |g| = 12 to 2^-24 * 12 * 1.44 relative to one: 24 in all.
+ROUNDINGS = {"f32": 12, "f64": 12, "bf16": 32, "f16": 32}
+
+
+def sequences(T, N, offsets=None, lengths=None):
+    """(first row, length) of every sequence in the flat rows"""
+    if offsets is not None:
+        return [(offsets[n], offsets[n + 1] - offsets[n]) for n in range(len(offsets) - 1)]
+    return [(n * T, T if lengths is None else lengths[n]) for n in range(N)]
+
+
+def factors(kind, g):
+    with np.errstate(over="ignore"):
+        if kind == 2:
+            a = np.where(g >= 0, 1 / (1 + np.exp(-np.abs(g))), np.exp(-np.abs(g)) / (1 + np.exp(-np.abs(g))))
+            return a, np.where(g >= 0, np.exp(-np.abs(g)) / (1 + np.exp(-np.abs(g))), 1 / (1 + np.exp(-np.abs(g))))
+        return (np.exp(g) if kind == 1 else g), np.ones_like(g)
+
+
+def philox_keep(N, T, D, p, seed, draw):
+    """[N, T, D]: 2^16 / (2^16 - cut) where an element is kept, else 0"""
+    cut = int(round(p * 65536))
+    c = [np.empty((N, (T + 7) // 8, D), dtype=np.uint64) for _ in range(4)]
+    c[0][:], c[1][:] = np.arange(D, dtype=np.uint64), np.arange(c[0].shape[1], dtype=np.uint64)[:, None]
+    c[2][:], c[3][:] = np.arange(N, dtype=np.uint64)[:, None, None], np.uint64(draw)
+    k0, k1 = seed & 0xFFFFFFFF, seed >> 32
+    low = np.uint64(0xFFFFFFFF)
+    for _ in range(10):
+        p0, p1 = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(p1 >> np.uint64(32)) ^ c[1] ^ np.uint64(k0), p1 & low, (p0 >> np.uint64(32)) ^ c[3] ^ np.uint64(k1), p0 & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    bits = np.stack([w >> np.uint64(s) & np.uint64(0xFFFF) for w in c for s in (0, 16)], axis=2)   # N, block, row of the block, D
+    keep = bits.reshape(N, -1, D)[:, :T] >= cut
+    return np.where(keep, 65536.0 / (65536 - cut), 0.0)
+
+
+def diag_forward(kind, g, x, h0, seqs, c_u):
+    """flat rows -> h, last, bounds of both"""
+    a, w = factors(kind, g)
+    u = w * x
+    h, E = np.zeros_like(x), np.zeros_like(x)
+    last, Elast = np.array(h0), np.zeros_like(h0)
+    for s, (r0, length) in enumerate(seqs):
+        now, M, e = h0[s].copy(), np.abs(h0[s]), np.zeros_like(h0[s])
+        for r in range(r0, r0 + length):
+            e = np.abs(a[r]) * e + c_u * (np.abs(a[r]) * M + np.abs(u[r]))
+            now = a[r] * now + u[r]
+            M = np.abs(a[r]) * M + np.abs(u[r])
+            h[r], E[r] = now, e
+        last[s], Elast[s] = now, e
+    return h, last, E, Elast
+
+
+def diag_backward(kind, g, x, h, dh, h0, dlast, seqs, c_u):
+    """at the trajectory h: dgate, dx, dh0 and their bounds"""
+    a, w = factors(kind, g)
+    dg, dx, Eg, Ex = (np.zeros_like(x) for _ in range(4))
+    dh0, E0 = np.array(dlast), np.zeros_like(dlast)
+    for s, (r0, length) in enumerate(seqs):
+        mu, M, e = dlast[s].copy(), np.abs(dlast[s]), np.zeros_like(dlast[s])
+        for r in range(r0 + length - 1, r0 - 1, -1):
+            before = h[r - 1] if r > r0 else h0[s]
+            lam, el, al = dh[r] + mu, e + c_u * (np.abs(dh[r]) + M), np.abs(dh[r]) + M
+            if kind == 2:
+                size = np.abs(before) + np.abs(x[r])
+                dg[r], Eg[r] = lam * a[r] * w[r] * (before - x[r]), a[r] * w[r] * size * (el + c_u * al)
+                dx[r], Ex[r] = lam * w[r], w[r] * (el + c_u * al)
+            else:
+                f = a[r] if kind == 1 else np.ones_like(a[r])
+                dg[r], Eg[r] = lam * before * f, np.abs(f * before) * (el + c_u * al)
+                dx[r], Ex[r] = lam, el
+            mu, e, M = a[r] * lam, np.abs(a[r]) * el + c_u * np.abs(a[r]) * al, np.abs(a[r]) * al
+        dh0[s], E0[s] = mu, e
+    return dg, dx, dh0, Eg, Ex, E0
+
+
+def check(name, got, want, bound, dtype):
+    """|got - want| <= bound + half a step of the type (of the true value, and of the bound's worth), element by element"""
+    got = got.detach().cpu().double().numpy().reshape(want.shape)
+    tol = bound + HALF[dtype] * (np.abs(want) + bound) * (1 + 2.0 ** -7) + TINY[dtype]
+    off = np.abs(got - want)
+    bad = ~(off <= tol)
+    worst = float((off / tol).max()) if off.size else 0.0
+    print("%s: largest error over its bound %.3f" % (name, worst), flush=True)
+    assert not bad.any(), "%s: %d of %d outside, worst %.3g at %s (want %.6g got %.6g)" % (
+        name, bad.sum(), bad.size, worst, np.unravel_index((off / tol).argmax(), off.shape), want.flat[(off / tol).argmax()], got.flat[(off / tol).argmax()])

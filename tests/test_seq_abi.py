@@ -1,0 +1,69 @@
+"""Host-side checks of the sequence operators' C entry points: argument validation without a GPU, no compute calls."""
+import ctypes
+
+import pytest
+
+from paper_2309_12252_amd import deer
+
+WORD = ctypes.c_void_p(256)   # (looked at for NULL and alignment only)
+
+
+def diag(**kw):
+    c = dict(dtype=deer.DEER_F32, gate=0, N=2, D=8, T=100, packed=0, draw=0, stride_gate=0, stride_in=0, stride_out=0, drop=0.0, seed=0)
+    c.update(kw)
+    return deer.DiagrecConfig(*[c[name] for name, _ in deer.DiagrecConfig._fields_])
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=4), 1), (dict(dtype=-1), 1), (dict(gate=3), 1), (dict(N=0), 1), (dict(D=0), 1), (dict(T=-1), 1), (dict(packed=2), 1),
+    (dict(stride_in=7), 1), (dict(stride_out=-8), 1), (dict(drop=-0.5), 1), (dict(drop=1.0), 1), (dict(drop=float("nan")), 1),
+    (dict(T=(1 << 33) + 1), 2), (dict(N=2000000000, T=1 << 20), 2)])
+def test_diagrec_refuses(change, status):
+    lib, cfg, size = deer.load_library(), diag(**change), ctypes.c_size_t(0)
+    assert lib.deer_diagrec_workspace_bytes(ctypes.byref(cfg), 0, ctypes.byref(size)) == status
+    assert lib.deer_diagrec_solve(ctypes.byref(cfg), WORD, WORD, None, None, WORD, None, WORD, 1 << 40, None) == status
+    assert lib.deer_diagrec_grad(ctypes.byref(cfg), WORD, WORD, None, None, WORD, WORD, None, WORD, WORD, None, WORD, 1 << 40, None) == status
+    assert lib.deer_last_error(None)
+
+
+def test_diagrec_pointers_and_workspace():
+    lib, cfg, size = deer.load_library(), diag(), ctypes.c_size_t(0)
+    ref = ctypes.byref(cfg)
+    assert lib.deer_diagrec_workspace_bytes(None, 0, ctypes.byref(size)) == deer.DEER_ERR_INVALID_ARG
+    assert lib.deer_diagrec_workspace_bytes(ref, 0, None) == deer.DEER_ERR_INVALID_ARG
+    assert lib.deer_diagrec_workspace_bytes(ref, 0, ctypes.byref(size)) == deer.DEER_OK and size.value > 0
+    solve = lambda c, g=WORD, x=WORD, b=None, h=WORD, ws=WORD, n=1 << 40: lib.deer_diagrec_solve(c, g, x, None, b, h, None, ws, n, None)   # noqa: E731
+    for bad in (dict(g=None), dict(x=None), dict(h=None), dict(g=ctypes.c_void_p(258)), dict(b=ctypes.c_void_p(260))):
+        assert solve(ref, **bad) == deer.DEER_ERR_INVALID_ARG
+    assert solve(ref, ws=None) == deer.DEER_ERR_WORKSPACE
+    assert solve(ref, ws=ctypes.c_void_p(512 + 64)) == deer.DEER_ERR_WORKSPACE
+    assert solve(ref, n=size.value - 1) == deer.DEER_ERR_WORKSPACE
+    packed = diag(packed=1)
+    assert solve(ctypes.byref(packed)) == deer.DEER_ERR_INVALID_ARG   # no bounds
+    # the words of the tiles: 8 bytes a channel and tile, little beside the arrays themselves
+    big = diag(dtype=deer.DEER_BF16, N=1, T=1 << 20, D=2048)
+    assert lib.deer_diagrec_workspace_bytes(ctypes.byref(big), 0, ctypes.byref(size)) == deer.DEER_OK
+    assert size.value < (1 << 20) * 2048 * 2 / 16
+
+
+def test_step_and_dropout_refuse():
+    lib, cfg = deer.load_library(), diag()
+    step = lambda c, g=WORD, slots=None, n=4, s=WORD, h=WORD: lib.deer_diagrec_step(ctypes.byref(c), g, WORD, slots, n, s, h, None)   # noqa: E731
+    for bad in (dict(g=None), dict(n=0), dict(s=None), dict(h=None), dict(slots=ctypes.c_void_p(258)), dict(s=ctypes.c_void_p(258))):
+        assert step(cfg, **bad) == deer.DEER_ERR_INVALID_ARG
+    assert step(diag(N=0)) == deer.DEER_ERR_INVALID_ARG
+    drop = lambda dtype=0, N=1, T=8, D=4, x=WORD, si=0, y=WORD, so=0, p=0.5: lib.deer_dropout(dtype, N, T, D, x, si, y, so, p, 1, 0, None)   # noqa: E731
+    for bad in (dict(dtype=7), dict(N=0), dict(T=-1), dict(D=0), dict(x=None), dict(y=None), dict(si=3), dict(so=-4), dict(p=1.0), dict(p=-0.1),
+                dict(p=0.999999), dict(p=float("nan")), dict(x=ctypes.c_void_p(257))):
+        assert drop(**bad) == deer.DEER_ERR_INVALID_ARG
+    assert drop(T=1 << 40) == deer.DEER_ERR_UNSUPPORTED
+
+
+def test_binding_needs_device_tensors():
+    import torch
+    x = torch.zeros(2, 8, 4)
+    for call in (lambda: deer.diagrec_solve(x, x), lambda: deer.diagrec_step(x[0], x[0], x[0]), lambda: deer.dropout(x, 0.5, 1),
+                 lambda: deer.diagrec_solve(None, x)):
+        with pytest.raises(deer.DeerError) as e:
+            call()
+        assert e.value.status == deer.DEER_ERR_INVALID_ARG
