@@ -241,7 +241,7 @@ deer_status deer_linrec_solve_static(int32_t dtype, int32_t B, int32_t T, int32_
  *   - No context.  Every call enqueues its kernels on hip_stream (a stream of the current device; NULL = the default stream) and
  *     returns without synchronising; nothing is allocated, so a call may be captured into a HIP graph (each captured call with a workspace
  *     of its own, or never replayed at the same time).  Errors are reported through deer_last_error(NULL).
- *   - Types: DEER_F32, DEER_F64 (deer_diagrec_*, deer_dropout), DEER_BF16, DEER_F16 (deer_diagrec_*, deer_dropout).  Sums and states are held in
+ *   - Types: DEER_F32, DEER_F64 (deer_diagrec_*, deer_dropout), DEER_BF16, DEER_F16 (deer_diagrec_*, deer_dropout).  deer_matrec_*: DEER_F32 and DEER_BF16.  Sums and states are held in
  *     32 bits (fp64: 64); h0, last, dlast, dh0, states and their gradients are arrays of that wider type, dense.
  *   - Rows.  packed = 0: N sequences of T rows, row t of sequence n is row n T + t of every array; d_bounds (device, int64 [N], or NULL) holds how
  *     many rows of each count.  packed = 1: the sequences lie one behind the other in T rows; d_bounds (device, int64 [N + 1], not NULL) holds
@@ -300,6 +300,42 @@ deer_status deer_diagrec_step(const deer_diagrec_config* cfg, const void* d_gate
  *   d_x in, d_y out [N, T, D], rows stride_in and stride_out apart (0: dense); d_y may be d_x with the same stride. */
 deer_status deer_dropout(int32_t dtype, int32_t N, int64_t T, int32_t D, const void* d_x, int64_t stride_in, void* d_y,
                          int64_t stride_out, double p, uint64_t seed, uint32_t draw, void* hip_stream);
+
+/* Gated linear recurrence with a matrix as the state of every head: S_t = exp(g_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t, S [Dk, Dv]. */
+typedef struct {
+    int32_t dtype;     /* DEER_F32 or DEER_BF16: q, k, v, o and their gradients                            */
+    int32_t N;         /* sequences (deer_matrec_step: rows), >= 1                                         */
+    int64_t T;         /* rows of a sequence, packed: of all of them; >= 0                                 */
+    int32_t packed;    /* 0 or 1                                                                           */
+    int32_t Hk, Hv;    /* heads of q and k, heads of v: a multiple; head h goes with h / (Hv / Hk)         */
+    int32_t Dk, Dv;    /* 1 .. 128                                                                         */
+    int32_t reserved;  /* must be 0                                                                        */
+    double scale;      /* of the outputs                                                                   */
+    int64_t stride_q, stride_k, stride_v, stride_o;   /* rows (0: Hk Dk, Hk Dk, Hv Dv, Hv Dv); gradients lie like their arrays, dL/do like o */
+} deer_matrec_config;
+
+/* Bytes of device workspace (256-byte aligned) that deer_matrec_solve() (grad = 0) or deer_matrec_grad() (grad = 1) needs.  The gradient keeps two
+ * states of a head, Dk Dv floats each, for every 64 rows. */
+deer_status deer_matrec_workspace_bytes(const deer_matrec_config* cfg, int32_t grad, size_t* bytes);
+
+/* d_q, d_k in [rows, Hk, Dk]   d_v in [rows, Hv, Dv]   d_gate in [rows, Hv] float32, the logarithms of the factors (dense)   d_s0 in [N, Hv, Dk, Dv]
+ * float32 or NULL (zeros)   d_o out [rows, Hv, Dv]   d_last out [N, Hv, Dk, Dv] float32 or NULL.  By chunks of 64 rows on the matrix cores; states
+ * in fp32 (bf16: sums of exact products, their weights in two bf16 pieces), two calls with the same inputs return the same bits.
+ * What is not finite in a row reaches the outputs of its chunk, also in front of it, and all that come later. */
+deer_status deer_matrec_solve(const deer_matrec_config* cfg, const void* d_q, const void* d_k, const void* d_v, const float* d_gate,
+                              const float* d_s0, const int64_t* d_bounds, void* d_o, float* d_last, void* d_workspace,
+                              size_t workspace_bytes, void* hip_stream);
+
+/* Its gradient.  d_do in dL/do   d_dlast in [N, Hv, Dk, Dv] or NULL (zeros)   d_dq, d_dk, d_dv out   d_dgate out [rows, Hv] float32 or NULL   d_ds0 out
+ * [N, Hv, Dk, Dv] float32 or NULL.  The states are computed again; gradients of shared heads are summed in a fixed order. */
+deer_status deer_matrec_grad(const deer_matrec_config* cfg, const void* d_q, const void* d_k, const void* d_v, const float* d_gate,
+                             const float* d_s0, const int64_t* d_bounds, const void* d_do, const float* d_dlast, void* d_dq, void* d_dk,
+                             void* d_dv, float* d_dgate, float* d_ds0, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One token for each of N rows (T and packed are not looked at): states in n_slots slots [n_slots, Hv, Dk, Dv], float32, updated in place; slots as in
+ * deer_diagrec_step(). */
+deer_status deer_matrec_step(const deer_matrec_config* cfg, const void* d_q, const void* d_k, const void* d_v, const float* d_gate,
+                             const int32_t* d_slots, int32_t n_slots, float* d_state, void* d_o, void* hip_stream);
 
 /* Switch per-kernel timing with HIP events on the context's stream on or off (off by default;
  * turning it on resets the accumulated numbers), and read the numbers accumulated so far. */

@@ -5,7 +5,7 @@
 #include <cmath>
 #include <cstdio>
 
-#include "seq_common.h"
+#include "matrec_common.h"
 
 using namespace deer;
 
@@ -103,6 +103,105 @@ deer_status check_workspace(const void* ws, size_t have, size_t need) {
         return fail(DEER_ERR_WORKSPACE, text);
     }
     return DEER_OK;
+}
+
+// ---- matrix states ----
+const char* bad_config(const deer_matrec_config* c, bool step) {
+    if (!c) return "config is NULL";
+    if (!known_type(c->dtype)) return "unknown dtype";
+    if (c->N < 1 || c->Hk < 1 || c->Hv < 1 || c->Dk < 1 || c->Dv < 1) return "N, Hk, Hv, Dk and Dv must be positive";
+    if (c->Hv % c->Hk) return "Hv must be a multiple of Hk";
+    if (c->reserved != 0) return "reserved must be 0";
+    if (!std::isfinite(c->scale)) return "scale must be finite";
+    if (c->stride_q < 0 || c->stride_k < 0 || c->stride_v < 0 || c->stride_o < 0) return "strides must not be negative";
+    const int64_t keys = (int64_t)c->Hk * c->Dk, values = (int64_t)c->Hv * c->Dv;
+    if ((c->stride_q && c->stride_q < keys) || (c->stride_k && c->stride_k < keys) || (c->stride_v && c->stride_v < values) || (c->stride_o && c->stride_o < values))
+        return "a stride is smaller than a row";
+    if (!step && (c->T < 0 || (c->packed != 0 && c->packed != 1))) return "T must not be negative, packed 0 or 1";
+    return nullptr;
+}
+
+// How the rows are cut into segments, each a workgroup a head.  A sequence is cut only where whole sequences do not make enough workgroups
+// for 256 CUs, and then into as many as do.
+struct MatLayout {
+    long long chunks, max_segs;   // at most
+    int per;
+    bool split;
+    size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_chunk, off_rchunk, total;
+};
+MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
+    MatLayout l{};
+    const long long longest = (c->T + kChunk - 1) / kChunk;
+    l.chunks = c->packed ? longest + c->N : longest * c->N;
+    long long per = longest < 1 ? 1 : longest;
+    if (c->packed || (long long)c->N * c->Hv < 256) {
+        const long long want = l.chunks * c->Hv / 512;
+        per = want < 4 ? 4 : want;
+        if (per > longest) per = longest < 1 ? 1 : longest;
+    }
+    l.per = (int)per;
+    l.split = per < longest;
+    l.max_segs = c->packed ? l.chunks / per + c->N : (longest + per - 1) / per * c->N;
+    const size_t states = (size_t)c->Hv * c->Dk * c->Dv * 4;
+    size_t at = kAlign;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align_up(bytes);
+        return here;
+    };
+    l.off_segs = take((size_t)l.max_segs * sizeof(MatSegment));
+    l.off_seq = take(((size_t)c->N + 1) * 4);
+    if (l.split) {
+        l.off_state = take((size_t)l.max_segs * states);
+        if (grad) l.off_rstate = take((size_t)l.max_segs * states);
+        l.off_decay = take((size_t)l.max_segs * c->Hv * 8);
+    }
+    if (grad) {
+        l.off_chunk = take((size_t)l.chunks * states);
+        l.off_rchunk = take((size_t)l.chunks * states);
+    }
+    l.total = at;
+    return l;
+}
+const char* unsupported(const deer_matrec_config* c, bool step) {
+    if (c->dtype != DEER_F32 && c->dtype != DEER_BF16) return "matrix states: fp32 and bf16 only";
+    if (c->Dk > 128 || c->Dv > 128) return "matrix states: Dk and Dv up to 128";
+    if (step) return (long long)c->N * c->Hv > 2147483647ll ? "more rows than a launch holds" : nullptr;
+    if (c->T > kMostRows || (long double)c->N * c->Hv * 64 > 2147483647.0L || ((long double)(c->T + 63) / 64 + 4) * (c->packed ? 1 : c->N) * c->Hv > 2147483647.0L)
+        return "more rows than a launch holds";
+    const MatLayout l = mat_layout(c, true);
+    if ((long double)l.max_segs * l.per * c->Hv > 2147483647.0L || (long double)l.max_segs * c->Hv > 2147483647.0L) return "more rows than a launch holds";
+    return nullptr;
+}
+MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool grad, const int64_t* bounds, void* workspace) {
+    char* ws = reinterpret_cast<char*>(workspace);
+    MatrecParams p{};
+    p.rows = SeqRows{reinterpret_cast<const long long*>(bounds), c->T, c->N, c->packed};
+    p.plan.count = reinterpret_cast<int*>(ws);
+    p.plan.segs = reinterpret_cast<MatSegment*>(ws + l.off_segs);
+    p.plan.seq_seg = reinterpret_cast<int*>(ws + l.off_seq);
+    p.plan.max_segs = (int)l.max_segs;
+    p.plan.per = l.per;
+    p.Hk = c->Hk;
+    p.Hv = c->Hv;
+    p.Dk = c->Dk;
+    p.Dv = c->Dv;
+    p.scale = (float)c->scale;
+    p.stride_q = c->stride_q ? c->stride_q : (long long)c->Hk * c->Dk;
+    p.stride_k = c->stride_k ? c->stride_k : (long long)c->Hk * c->Dk;
+    p.stride_v = c->stride_v ? c->stride_v : (long long)c->Hv * c->Dv;
+    p.stride_o = c->stride_o ? c->stride_o : (long long)c->Hv * c->Dv;
+    p.split = l.split;
+    if (l.split) {
+        p.seg_state = reinterpret_cast<float*>(ws + l.off_state);
+        if (grad) p.seg_rstate = reinterpret_cast<float*>(ws + l.off_rstate);
+        p.seg_decay = reinterpret_cast<float*>(ws + l.off_decay);
+    }
+    if (grad) {
+        p.chunk_state = reinterpret_cast<float*>(ws + l.off_chunk);
+        p.chunk_rstate = reinterpret_cast<float*>(ws + l.off_rchunk);
+    }
+    return p;
 }
 
 }  // namespace
@@ -205,6 +304,102 @@ deer_status deer_dropout(int32_t dtype, int32_t N, int64_t T, int32_t D, const v
     q.y = d_y;
     q.drop = drop_params(p, seed, draw);
     return launched("deer_dropout", launch_dropout(dtype, q, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+deer_status deer_matrec_workspace_bytes(const deer_matrec_config* c, int32_t grad, size_t* bytes) {
+    if (!bytes) return fail(DEER_ERR_INVALID_ARG, "bytes is NULL");
+    if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (const char* why = unsupported(c, false)) return fail(DEER_ERR_UNSUPPORTED, why);
+    *bytes = mat_layout(c, grad != 0).total;
+    return DEER_OK;
+}
+
+deer_status deer_matrec_solve(const deer_matrec_config* c, const void* d_q, const void* d_k, const void* d_v, const float* d_gate, const float* d_s0,
+                              const int64_t* d_bounds, void* d_o, float* d_last, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (const char* why = unsupported(c, false)) return fail(DEER_ERR_UNSUPPORTED, why);
+    if ((c->T > 0 && (!d_q || !d_k || !d_v || !d_gate || !d_o)) || (c->packed && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    const size_t e = type_bytes(c->dtype);
+    if (misaligned(d_q, e) || misaligned(d_k, e) || misaligned(d_v, e) || misaligned(d_o, e) || misaligned(d_gate, 4) || misaligned(d_s0, 4) ||
+        misaligned(d_last, 4) || misaligned(d_bounds, 8))
+        return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
+    const MatLayout l = mat_layout(c, false);
+    if (deer_status st = check_workspace(d_workspace, workspace_bytes, l.total)) return st;
+    MatrecParams p = mat_params(c, l, false, d_bounds, d_workspace);
+    p.q = d_q;
+    p.k = d_k;
+    p.v = d_v;
+    p.gate = d_gate;
+    p.s0 = d_s0;
+    p.o = d_o;
+    p.last = d_last;
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t err = launch_matrec_plan(p, stream);
+    if (err == hipSuccess) err = launch_matrec_out(c->dtype, p, stream);
+    return launched("deer_matrec_solve", err);
+}
+
+deer_status deer_matrec_grad(const deer_matrec_config* c, const void* d_q, const void* d_k, const void* d_v, const float* d_gate, const float* d_s0,
+                             const int64_t* d_bounds, const void* d_do, const float* d_dlast, void* d_dq, void* d_dk, void* d_dv, float* d_dgate,
+                             float* d_ds0, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (const char* why = unsupported(c, false)) return fail(DEER_ERR_UNSUPPORTED, why);
+    if ((c->T > 0 && (!d_q || !d_k || !d_v || !d_gate || !d_do || !d_dq || !d_dk || !d_dv)) || (c->packed && !d_bounds))
+        return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    const size_t e = type_bytes(c->dtype);
+    if (misaligned(d_q, e) || misaligned(d_k, e) || misaligned(d_v, e) || misaligned(d_do, e) || misaligned(d_dq, e) || misaligned(d_dk, e) ||
+        misaligned(d_dv, e) || misaligned(d_gate, 4) || misaligned(d_s0, 4) || misaligned(d_dlast, 4) || misaligned(d_dgate, 4) || misaligned(d_ds0, 4) ||
+        misaligned(d_bounds, 8))
+        return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
+    const MatLayout l = mat_layout(c, true);
+    if (deer_status st = check_workspace(d_workspace, workspace_bytes, l.total)) return st;
+    MatrecParams p = mat_params(c, l, true, d_bounds, d_workspace);
+    p.q = d_q;
+    p.k = d_k;
+    p.v = d_v;
+    p.gate = d_gate;
+    p.s0 = d_s0;
+    p.dout = d_do;
+    p.dlast = d_dlast;
+    p.dq = d_dq;
+    p.dk = d_dk;
+    p.dv = d_dv;
+    p.dgate = d_dgate;
+    p.ds0 = d_ds0;
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    hipError_t err = launch_matrec_plan(p, stream);
+    if (err == hipSuccess) err = launch_matrec_states(c->dtype, p, stream);
+    if (err == hipSuccess) err = launch_matrec_grad(c->dtype, p, stream);
+    return launched("deer_matrec_grad", err);
+}
+
+deer_status deer_matrec_step(const deer_matrec_config* c, const void* d_q, const void* d_k, const void* d_v, const float* d_gate, const int32_t* d_slots,
+                             int32_t n_slots, float* d_state, void* d_o, void* hip_stream) {
+    if (const char* why = bad_config(c, true)) return fail(DEER_ERR_INVALID_ARG, why);
+    if (const char* why = unsupported(c, true)) return fail(DEER_ERR_UNSUPPORTED, why);
+    if (n_slots < 1) return fail(DEER_ERR_INVALID_ARG, "n_slots must be positive");
+    if (!d_q || !d_k || !d_v || !d_gate || !d_state || !d_o) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    const size_t e = type_bytes(c->dtype);
+    if (misaligned(d_q, e) || misaligned(d_k, e) || misaligned(d_v, e) || misaligned(d_o, e) || misaligned(d_gate, 4) || misaligned(d_state, 4) || misaligned(d_slots, 4))
+        return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
+    MatstepParams p{};
+    p.rows = StepRows{d_slots, c->N, n_slots};
+    p.Hk = c->Hk;
+    p.Hv = c->Hv;
+    p.Dk = c->Dk;
+    p.Dv = c->Dv;
+    p.scale = (float)c->scale;
+    p.stride_q = c->stride_q ? c->stride_q : (long long)c->Hk * c->Dk;
+    p.stride_k = c->stride_k ? c->stride_k : (long long)c->Hk * c->Dk;
+    p.stride_v = c->stride_v ? c->stride_v : (long long)c->Hv * c->Dv;
+    p.stride_o = c->stride_o ? c->stride_o : (long long)c->Hv * c->Dv;
+    p.q = d_q;
+    p.k = d_k;
+    p.v = d_v;
+    p.gate = d_gate;
+    p.state = d_state;
+    p.o = d_o;
+    return launched("deer_matrec_step", launch_matstep(c->dtype, p, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

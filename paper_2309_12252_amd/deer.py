@@ -21,7 +21,8 @@ DEER_GATE_FACTOR, DEER_GATE_LOG, DEER_GATE_SIGMOID = 0, 1, 2
 
 EXPORTS = ["deer_theta_count", "deer_workspace_bytes", "deer_create", "deer_eval", "deer_grad",
            "deer_linrec_solve", "deer_linrec_solve_static", "deer_set_profiling", "deer_get_profile", "deer_last_error", "deer_destroy",
-           "deer_diagrec_workspace_bytes", "deer_diagrec_solve", "deer_diagrec_grad", "deer_diagrec_step", "deer_dropout"]
+           "deer_diagrec_workspace_bytes", "deer_diagrec_solve", "deer_diagrec_grad", "deer_diagrec_step", "deer_dropout",
+           "deer_matrec_workspace_bytes", "deer_matrec_solve", "deer_matrec_grad", "deer_matrec_step"]
 
 
 class DeerConfig(ctypes.Structure):
@@ -47,6 +48,13 @@ class DiagrecConfig(ctypes.Structure):
                 ("T", ctypes.c_int64), ("packed", ctypes.c_int32), ("draw", ctypes.c_uint32),
                 ("stride_gate", ctypes.c_int64), ("stride_in", ctypes.c_int64), ("stride_out", ctypes.c_int64),
                 ("drop", ctypes.c_double), ("seed", ctypes.c_uint64)]
+
+
+class MatrecConfig(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("N", ctypes.c_int32), ("T", ctypes.c_int64), ("packed", ctypes.c_int32),
+                ("Hk", ctypes.c_int32), ("Hv", ctypes.c_int32), ("Dk", ctypes.c_int32), ("Dv", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("scale", ctypes.c_double), ("stride_q", ctypes.c_int64),
+                ("stride_k", ctypes.c_int64), ("stride_v", ctypes.c_int64), ("stride_o", ctypes.c_int64)]
 
 
 class DeerError(RuntimeError):
@@ -92,11 +100,15 @@ def load_library():
     lib.deer_destroy.restype = None
     lib.deer_destroy.argtypes = [vp]
     size, i64, u32, u64 = ctypes.c_size_t, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64
-    dcp = ctypes.POINTER(DiagrecConfig)
+    dcp, mcp = ctypes.POINTER(DiagrecConfig), ctypes.POINTER(MatrecConfig)
     for name, args in (("deer_diagrec_workspace_bytes", [dcp, i32, ctypes.POINTER(size)]),
                        ("deer_diagrec_solve", [dcp] + [vp] * 7 + [size, vp]),
                        ("deer_diagrec_grad", [dcp] + [vp] * 11 + [size, vp]),
                        ("deer_diagrec_step", [dcp] + [vp] * 3 + [i32] + [vp] * 3),
+                       ("deer_matrec_workspace_bytes", [mcp, i32, ctypes.POINTER(size)]),
+                       ("deer_matrec_solve", [mcp] + [vp] * 9 + [size, vp]),
+                       ("deer_matrec_grad", [mcp] + [vp] * 14 + [size, vp]),
+                       ("deer_matrec_step", [mcp] + [vp] * 5 + [i32] + [vp] * 3),
                        ("deer_dropout", [i32, i32, i64, i32, vp, i64, vp, i64, dbl, u64, u32, vp])):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = args
@@ -435,6 +447,101 @@ def diagrec_step(gate, x, state, *, kind=DEER_GATE_FACTOR, slots=None, out=None)
     if st != DEER_OK:
         _raise(lib, st)
     return h
+
+
+def _mat_config(q, k, v, gate, o, offsets, lengths, scale, lead=None):
+    """lead: given for a step, whose rows are not sequences"""
+    _need(all(isinstance(t, torch.Tensor) for t in (q, k, v, gate)), "need device tensors")
+    _need(q.dtype in _DTYPES, "need float32 or bfloat16")
+    if lead is None:
+        N, T, packed, bounds, lead = _rows_of(q, 2, offsets, lengths)
+    else:
+        _need(q.dim() == 3, "need q [N, Hk, Dk]")
+        N, T, packed, bounds = q.shape[0], 1, 0, 0
+    rows, dev = tuple(q.shape[:lead]), q.device
+    Hk, Dk = q.shape[lead:]
+    _check_like(k, "k", q.shape, q.dtype, dev)
+    _need(v.dim() == q.dim(), "v: need as many dimensions as q")
+    Hv, Dv = v.shape[lead:]
+    _check_like(v, "v", rows + (Hv, Dv), q.dtype, dev)
+    _need(Hk >= 1 and Hv % Hk == 0, "the heads of v must be a multiple of those of q and k")
+    gp = _dense(gate, "gate", rows + (Hv,), torch.float32, dev)
+    cfg = MatrecConfig(_DTYPES[q.dtype], N, T, packed, Hk, Hv, Dk, Dv, 0, float(Dk ** -0.5 if scale is None else scale), _row_stride(q, "q", lead),
+                       _row_stride(k, "k", lead), _row_stride(v, "v", lead), _row_stride(o, "o", lead) if o is not None else Hv * Dv)
+    return cfg, bounds, gp, lead
+
+
+def _mat_workspace(lib, cfg, grad, device):
+    size = ctypes.c_size_t(0)
+    st = lib.deer_matrec_workspace_bytes(ctypes.byref(cfg), grad, ctypes.byref(size))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return torch.empty(size.value, dtype=torch.uint8, device=device)
+
+
+@_on_stream
+def matrec_solve(q, k, v, gate, s0=None, *, offsets=None, lengths=None, scale=None, out=None):
+    """deer_matrec_solve: S_t = exp(gate_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t for every head of v.  q, k [N, T, Hk, Dk], v [N, T, Hv, Dv] in
+    float32 or bfloat16, gate [N, T, Hv] float32, with optional int64 `lengths` [N]; or packed [rows, ...] with int64 `offsets` [N + 1].  s0 [N, Hv, Dk, Dv]
+    float32.  scale: Dk^-1/2 by default.  Returns (o, states behind the last rows)."""
+    lib = load_library()
+    o = out if out is not None else torch.empty(v.shape, dtype=v.dtype, device=q.device)
+    cfg, bounds, gp, _ = _mat_config(q, k, v, gate, o, offsets, lengths, scale)
+    _check_like(o, "out", v.shape, v.dtype, q.device)
+    shape = (cfg.N, cfg.Hv, cfg.Dk, cfg.Dv)
+    s0p = _dense(s0, "s0", shape, torch.float32, q.device)
+    ws = _mat_workspace(lib, cfg, 0, q.device)
+    last = torch.empty(shape, dtype=torch.float32, device=q.device)
+    st = lib.deer_matrec_solve(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, s0p, bounds, o.data_ptr(), last.data_ptr(),
+                               ws.data_ptr(), ws.numel(), _stream_of(q))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return o, last
+
+
+@_on_stream
+def matrec_grad(q, k, v, gate, do, s0=None, dlast=None, *, offsets=None, lengths=None, scale=None, dq=None, dk=None, dv=None):
+    """deer_matrec_grad: (dq, dk, dv, dgate, ds0) from do = dL/do and dlast = dL/d(final states).  dq, dk and dv, where given, have the row
+    strides of q, k and v."""
+    lib = load_library()
+    cfg, bounds, gp, lead = _mat_config(q, k, v, gate, None, offsets, lengths, scale)
+    dev = q.device
+    _check_like(do, "do", v.shape, v.dtype, dev)
+    cfg.stride_o = _row_stride(do, "do", lead)
+    outs = []
+    for t, d, name, stride in ((q, dq, "dq", cfg.stride_q), (k, dk, "dk", cfg.stride_k), (v, dv, "dv", cfg.stride_v)):
+        if d is None:
+            d = torch.empty(t.shape, dtype=t.dtype, device=dev) if t.is_contiguous() else _rows_like(t.flatten(-2), stride).unflatten(-1, t.shape[-2:])
+        _check_like(d, name, t.shape, t.dtype, dev)
+        _need(_row_stride(d, name, lead) == stride, name + ": rows must lie like those of what it is the gradient of")
+        outs.append(d)
+    shape = (cfg.N, cfg.Hv, cfg.Dk, cfg.Dv)
+    s0p, dlp = _dense(s0, "s0", shape, torch.float32, dev), _dense(dlast, "dlast", shape, torch.float32, dev)
+    ws = _mat_workspace(lib, cfg, 1, dev)
+    dgate = torch.empty(gate.shape, dtype=torch.float32, device=dev)
+    ds0 = torch.empty(shape, dtype=torch.float32, device=dev)
+    st = lib.deer_matrec_grad(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, s0p, bounds, do.data_ptr(), dlp, outs[0].data_ptr(),
+                              outs[1].data_ptr(), outs[2].data_ptr(), dgate.data_ptr(), ds0.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(q))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return outs[0], outs[1], outs[2], dgate, ds0
+
+
+@_on_stream
+def matrec_step(q, k, v, gate, state, *, slots=None, scale=None, out=None):
+    """deer_matrec_step: one token for each of N rows, q, k [N, Hk, Dk], v [N, Hv, Dv], gate [N, Hv]; `state` [slots, Hv, Dk, Dv] float32 is updated
+    in place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over.  Returns o."""
+    lib = load_library()
+    o = out if out is not None else torch.empty(v.shape, dtype=v.dtype, device=q.device)
+    cfg, _, gp, _ = _mat_config(q, k, v, gate, o, None, None, scale, lead=1)
+    _check_like(o, "out", v.shape, v.dtype, q.device)
+    _need(isinstance(state, torch.Tensor) and state.dim() == 4, "state: need [slots, Hv, Dk, Dv]")
+    sp = _dense(state, "state", (state.shape[0], cfg.Hv, cfg.Dk, cfg.Dv), torch.float32, q.device)
+    tp = _dense(slots, "slots", (cfg.N,), torch.int32, q.device)
+    st = lib.deer_matrec_step(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, tp, state.shape[0], sp, o.data_ptr(), _stream_of(q))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return o
 
 
 @_on_stream

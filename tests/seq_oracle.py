@@ -102,3 +102,61 @@ def check(name, got, want, bound, dtype):
     print("%s: largest error over its bound %.3f" % (name, worst), flush=True)
     assert not bad.any(), "%s: %d of %d outside, worst %.3g at %s (want %.6g got %.6g)" % (
         name, bad.sum(), bad.size, worst, np.unravel_index((off / tol).argmax(), off.shape), want.flat[(off / tol).argmax()], got.flat[(off / tol).argmax()])
+
+
+# ---- matrix states ----
+# For every output its value and the same formula over absolute values ("abs"), which the errors are measured by: a rounding of a factor or of
+# a partial sum moves an output by at most half a step of it times abs.  In bf16 an output has one rounded factor in every term (the 64 x 64 factors,
+# or the state): 2^-8; states and gates only factors of two pieces: 2^-16.  In fp32 sums of T rows and 128 columns: 4 (T + 128) roundings.
+def matrix(q, k, v, g, s0, seqs, scale, do=None, dlast=None):
+    """flat rows: q, k [rows, Hk, Dk], v [rows, Hv, Dv], g [rows, Hv] -> dict of (value, abs)"""
+    rows, Hv, Dv = v.shape
+    kv = np.arange(Hv) * q.shape[1] // Hv
+    Q, K = q[:, kv], k[:, kv]
+    out = {n: np.zeros(sh) for n, sh in (("o", v.shape), ("last", s0.shape), ("dq", Q.shape), ("dk", Q.shape), ("dv", v.shape), ("dgate", g.shape), ("ds0", s0.shape))}
+    absolute = {n: x.copy() for n, x in out.items()}
+    with np.errstate(over="ignore", under="ignore"):
+        for sign, res in ((False, out), (True, absolute)):
+            f = np.abs if sign else (lambda x: x)
+            for s, (r0, n) in enumerate(seqs):
+                S, states = f(s0[s]).copy(), []
+                for r in range(r0, r0 + n):
+                    states.append(S)
+                    S = np.exp(g[r])[:, None, None] * S + f(K[r])[:, :, None] * f(v[r])[:, None, :]
+                    res["o"][r] = scale * np.einsum("hd,hdv->hv", f(Q[r]), S)
+                res["last"][s] = S
+                if do is None:
+                    continue
+                states.append(S)
+                R = f(dlast[s]).copy()
+                for i in range(n - 1, -1, -1):
+                    r = r0 + i
+                    R = R + scale * f(Q[r])[:, :, None] * f(do[r])[:, None, :]
+                    res["dq"][r] = scale * np.einsum("hdv,hv->hd", states[i + 1], f(do[r]))
+                    res["dk"][r] = np.einsum("hdv,hv->hd", R, f(v[r]))
+                    res["dv"][r] = np.einsum("hdv,hd->hv", R, f(K[r]))
+                    R = np.exp(g[r])[:, None, None] * R
+                    res["dgate"][r] = np.einsum("hdv,hdv->h", states[i], R)
+                res["ds0"][s] = R
+    shared = lambda x: np.stack([x[:, kv == h].sum(1) for h in range(q.shape[1])], 1)   # noqa: E731
+    for res in (out, absolute):
+        res["dq"], res["dk"] = shared(res["dq"]), shared(res["dk"])
+    return out, absolute
+
+
+def check_matrix(got, want, absolute, dtype, T):
+    sums = 4 * (T + 128) * 2.0 ** -24
+    for name, t in got.items():
+        w, a = want[name], absolute[name]
+        if name in ("last", "ds0", "dgate"):
+            bound, kind = (sums + (2.0 ** -16 if dtype == "bf16" else 0.0)) * a, "f32"
+        else:
+            bound, kind = (sums + (2.0 ** -8 + 2.0 ** -14 if dtype == "bf16" else 0.0)) * a, dtype
+        check(name, t, w, bound, kind)
+        # all together: one output of many is off by a random walk of its roundings (each half a step / sqrt 3 at most): in bf16 two of
+        # 2^-8 / sqrt 3, for what is fp32 with pieces one of 2^-16 / sqrt 3; fp32: sqrt(4 (T + 128)) of 2^-24 / sqrt 3, rounded up
+        if w.size >= 500 and np.linalg.norm(w) > 0:
+            rel = np.linalg.norm(t.detach().cpu().double().numpy().reshape(w.shape) - w) / np.linalg.norm(w)
+            most = (4 * (T + 128)) ** 0.5 * 2.0 ** -24 + (2.0 ** -16 if dtype == "bf16" else 0.0) if kind == "f32" else 2.0 ** -8
+            print("%s: all together %.2g of at most %.2g" % (name, rel, most), flush=True)
+            assert rel <= most, (name, rel, most)

@@ -67,3 +67,41 @@ def test_binding_needs_device_tensors():
         with pytest.raises(deer.DeerError) as e:
             call()
         assert e.value.status == deer.DEER_ERR_INVALID_ARG
+
+
+def mat(**kw):
+    c = dict(dtype=deer.DEER_BF16, N=2, T=100, packed=0, Hk=2, Hv=4, Dk=64, Dv=64, reserved=0, scale=1.0, stride_q=0, stride_k=0, stride_v=0, stride_o=0)
+    c.update(kw)
+    return deer.MatrecConfig(*[c[name] for name, _ in deer.MatrecConfig._fields_])
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=4), 1), (dict(dtype=deer.DEER_F64), 2), (dict(dtype=deer.DEER_F16), 2), (dict(N=0), 1), (dict(Hk=0), 1), (dict(Hv=3), 1), (dict(Dk=0), 1),
+    (dict(Dk=129), 2), (dict(Dv=129), 2), (dict(T=-1), 1), (dict(packed=2), 1), (dict(reserved=1), 1), (dict(scale=float("inf")), 1), (dict(stride_q=127), 1),
+    (dict(stride_o=-256), 1), (dict(T=(1 << 33) + 1), 2), (dict(N=1 << 30, T=1 << 20), 2)])
+def test_matrec_refuses(change, status):
+    lib, cfg, size = deer.load_library(), mat(**change), ctypes.c_size_t(0)
+    ref = ctypes.byref(cfg)
+    assert lib.deer_matrec_workspace_bytes(ref, 1, ctypes.byref(size)) == status
+    assert lib.deer_matrec_solve(ref, WORD, WORD, WORD, WORD, None, None, WORD, None, WORD, 1 << 50, None) == status
+    assert lib.deer_matrec_grad(ref, WORD, WORD, WORD, WORD, None, None, WORD, None, WORD, WORD, WORD, None, None, WORD, 1 << 50, None) == status
+
+
+def test_matrec_pointers_and_workspace():
+    lib, cfg, size = deer.load_library(), mat(), ctypes.c_size_t(0)
+    ref = ctypes.byref(cfg)
+    for grad in (0, 1):
+        assert lib.deer_matrec_workspace_bytes(ref, grad, ctypes.byref(size)) == deer.DEER_OK and size.value > 0
+    need = size.value
+    solve = lambda c, q=WORD, o=WORD, g=WORD, b=None, ws=WORD, n=1 << 40: lib.deer_matrec_solve(c, q, WORD, WORD, g, None, b, o, None, ws, n, None)   # noqa: E731
+    for bad in (dict(q=None), dict(o=None), dict(g=None), dict(q=ctypes.c_void_p(257)), dict(g=ctypes.c_void_p(258)), dict(b=ctypes.c_void_p(260))):
+        assert solve(ref, **bad) == deer.DEER_ERR_INVALID_ARG
+    assert solve(ref, ws=None) == deer.DEER_ERR_WORKSPACE and solve(ref, ws=ctypes.c_void_p(320)) == deer.DEER_ERR_WORKSPACE
+    grad = lib.deer_matrec_grad(ref, WORD, WORD, WORD, WORD, None, None, WORD, None, WORD, WORD, WORD, None, None, WORD, need - 1, None)
+    assert grad == deer.DEER_ERR_WORKSPACE
+    packed = mat(packed=1)
+    assert solve(ctypes.byref(packed)) == deer.DEER_ERR_INVALID_ARG
+    step = lambda c, q=WORD, n=4, s=WORD: lib.deer_matrec_step(ctypes.byref(c), q, WORD, WORD, WORD, None, n, s, WORD, None)   # noqa: E731
+    for c, bad in ((cfg, dict(q=None)), (cfg, dict(n=0)), (cfg, dict(s=None)), (cfg, dict(s=ctypes.c_void_p(258))), (mat(Hv=3), {})):
+        assert step(c, **bad) == deer.DEER_ERR_INVALID_ARG
+    assert step(mat(Dk=200)) == deer.DEER_ERR_UNSUPPORTED
