@@ -2,8 +2,8 @@
 // cores.  With c_i the sum of a chunk's log gates up to row i, inclusive, and S the state in front of the chunk,
 //   o_i = scale (e^{c_i} S^T q_i + sum_{j <= i} e^{c_i - c_j} (q_i . k_j) v_j)
 //   S'  = e^{c_64} S + sum_j e^{c_64 - c_j} k_j v_j^T.
-// States are sums over many rows and stay in fp32 accumulators; v_j e^{c_64 - c_j} enters their update as two bf16 pieces, so a state is as exact as
-// fp32 sums make it (7e-7 measured).  The products of the output take S and the 64 x 64 factors rounded to bf16 once: an output
+// States are sums over many rows and stay in fp32 accumulators; v_j e^{c_64 - c_j} enters their update as three bf16 pieces, so a state is as exact as
+// fp32 sums make it.  The products of the output take S and the 64 x 64 factors rounded to bf16 once: an output
 // is rounded to bf16 itself.  What is NaN or infinite in a row reaches its chunk (products with factors that are zero) and what follows.
 #include "matrec_common.h"
 
@@ -69,136 +69,120 @@ __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p)
 }
 
 // ---- states ----
-// S[d][v] of a workgroup: wavefront w has columns 16 VT w .. of v and all rows d, as accumulators
-template <int KD, int VT>
-struct StateTile {
-    F32x4 s[4 * KD][VT];
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int t = 0; t < 4 * KD; ++t)
-#pragma unroll
-            for (int u = 0; u < VT; ++u) s[t][u] = F32x4{0, 0, 0, 0};
-    }
-    __device__ __forceinline__ void scale(float f) {
-#pragma unroll
-        for (int t = 0; t < 4 * KD; ++t)
-#pragma unroll
-            for (int u = 0; u < VT; ++u) s[t][u] *= f;
-    }
-    template <typename F>
-    __device__ __forceinline__ void each(int wave, int lane, int Dk, int Dv, F f) {
-#pragma unroll
-        for (int t = 0; t < 4 * KD; ++t)
-#pragma unroll
-            for (int u = 0; u < VT; ++u)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = 16 * t + 4 * (lane >> 4) + r, v = 16 * (VT * wave + u) + (lane & 15);
-                    if (d < Dk && v < Dv) s[t][u][r] = f(d * Dv + v, (float)s[t][u][r]);
-                }
-    }
-    __device__ __forceinline__ void load(const float* from, int wave, int lane, int Dk, int Dv) {
-        zero();
-        if (from) each(wave, lane, Dk, Dv, [&](int at, float) { return from[at]; });
-    }
-    __device__ __forceinline__ void store(float* to, int wave, int lane, int Dk, int Dv) {
-        each(wave, lane, Dk, Dv, [&](int at, float x) {
-            to[at] = x;
-            return x;
-        });
-    }
-};
-
-// S += K^T (weight V) over the 64 rows of a chunk; `weight` holds the rows' factors in LDS
-template <typename T, int KD, int VT, int LDK, int LDV>
-__device__ __forceinline__ void update_state(StateTile<KD, VT>& S, const T* tk, const T* tv, const float* weight, int wave, int lane) {
-    const int g = lane >> 4;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const F32x4 w0 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 4 * g), w1 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 16 + 4 * g);
-        frag_t<T> vp[VT][Op<T>::PIECES];
-#pragma unroll
-        for (int u = 0; u < VT; ++u) pieces_of<T>(widened(col_frag<LDV>(tv, s, VT * wave + u, lane)) * joined(w0, w1), vp[u]);
-#pragma unroll
-        for (int t = 0; t < 4 * KD; ++t) {
-            const frag_t<T> kf = col_frag<LDK>(tk, s, t, lane);
-#pragma unroll
-            for (int u = 0; u < VT; ++u)
-#pragma unroll
-                for (int q = Op<T>::PIECES - 1; q >= 0; --q) S.s[t][u] = mma(kf, vp[u][q], S.s[t][u]);
-        }
-    }
-}
-
 // One segment and head: the state's own part of the segment (STORE = false: into seg_state / seg_rstate, with the segment's decay), or with the state in
 // front of the segment known, the state in front of every chunk (REV: the gradient of the state behind it).  REV: rows backwards,
 // (k, v) = (scale q, dout), the gradient of the state in front of a chunk is e^{c_64} R + sum_i e^{c_i} scale q_i dout_i^T.
-template <typename T, int KD, int VT, bool REV, bool STORE>
+// Wavefront w keeps columns 16 w .. of v, transposed: a lane has four neighbouring v of every 16th d, so that states go to memory 16 bytes a lane.
+template <typename T, int DK, int DV, bool REV, bool STORE>
 __device__ __forceinline__ void states_of(const MatrecParams& p, int seg_no, int head, T* tk, T* tv, float* weight) {
-    constexpr int LDK = 64 * KD + Op<T>::PAD, LDV = 64 * VT + Op<T>::PAD;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int W = DV / 16, NT = DK / 16, P = Op<T>::PIECES;
+    using TK = Tile<T, DK>;
+    using TV = Tile<T, DV>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
     const MatSegment seg = p.plan.segs[seg_no];
     if (!STORE && seg.index == (REV ? 0 : seg.count - 1)) return;   // nothing comes behind it
     const long long cells = (long long)p.Dk * p.Dv;
     const int kh = head / (p.Hv / p.Hk);
     const long long stride_k = REV ? p.stride_q : p.stride_k, stride_v = REV ? p.stride_o : p.stride_v;
-    const T* k = reinterpret_cast<const T*>(REV ? p.q : p.k) + (long long)kh * p.Dk;
-    const T* v = reinterpret_cast<const T*>(REV ? p.dout : p.v) + (long long)head * p.Dv;
+    const T* k = reinterpret_cast<const T*>(REV ? p.q : p.k) + (long long)kh * p.Dk + seg.row0 * stride_k;
+    const T* v = reinterpret_cast<const T*>(REV ? p.dout : p.v) + (long long)head * p.Dv + seg.row0 * stride_v;
+    const float* gate = p.gate + seg.row0 * p.Hv + head;
     float* seg_states = REV ? p.seg_rstate : p.seg_state;
-    StateTile<KD, VT> S;
+    const int v0 = 16 * wave + 4 * g;
+    F32x4 S[NT];
+    const bool whole_rows = (p.Dv & 3) == 0;
+    auto store = [&](float* to) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            if (16 * t + l < p.Dk && v0 < p.Dv) store_four<float>(to + (long long)(16 * t + l) * p.Dv + v0, S[t], p.Dv - v0, whole_rows && reinterpret_cast<uintptr_t>(to) % 16 == 0);
+    };
+    const float* from = nullptr;
     if (STORE) {
         const float* ends = REV ? p.dlast : p.s0;
         const bool at_end = seg.index == (REV ? seg.count - 1 : 0);
-        const float* from = at_end ? (ends ? ends + ((long long)seg.seq * p.Hv + head) * cells : nullptr) : seg_states + ((long long)seg_no * p.Hv + head) * cells;
-        S.load(from, wave, lane, p.Dk, p.Dv);
-    } else {
-        S.zero();
+        from = at_end ? (ends ? ends + ((long long)seg.seq * p.Hv + head) * cells : nullptr) : seg_states + ((long long)seg_no * p.Hv + head) * cells;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        S[t] = F32x4{0, 0, 0, 0};
+        if (from && 16 * t + l < p.Dk) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (v0 + r < p.Dv) S[t][r] = from[(long long)(16 * t + l) * p.Dv + v0 + r];
+        }
     }
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
     double total = 0.0;
+    Stage<T, DK, 64 * W> fk;
+    Stage<T, DV, 64 * W> fv;
+    float fg = 0.0f;
+    auto fetch = [&](int i) {
+        const int c = REV ? chunks - 1 - i : i;
+        const long long row = (long long)c * kChunk;
+        const int rows = seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
+        fk.fetch(k + row * stride_k, stride_k, rows, p.Dk);
+        fv.fetch(v + row * stride_v, stride_v, rows, p.Dv);
+        fg = gate_of(gate + row * p.Hv, p.Hv, rows);
+    };
+    const int updates = STORE && !REV ? chunks - 1 : chunks;   // (the state behind the last chunk is somebody else's)
+    if (updates > 0) fetch(0);
     for (int i = 0; i < chunks; ++i) {
         const int c = REV ? chunks - 1 - i : i;
-        const long long row = seg.row0 + (long long)c * kChunk;
-        const int rows = seg.rows - (long long)c * kChunk < kChunk ? (int)(seg.rows - (long long)c * kChunk) : kChunk;
-        if (STORE) {
-            float* to = (REV ? p.chunk_rstate : p.chunk_state) + ((long long)(seg.chunk0 + c) * p.Hv + head) * cells;
-            S.store(to, wave, lane, p.Dk, p.Dv);
-            if (!REV && i == chunks - 1) break;
+        if (STORE) {   // whole tiles: what lies outside the head is zero in S too
+            float* to = (REV ? p.chunk_rstate : p.chunk_state) + ((long long)(seg.chunk0 + c) * p.Hv + head) * (DK * DV) + l * DV + v0;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) *reinterpret_cast<F32x4*>(to + 16 * t * DV) = S[t];
         }
-        const Cum cum = chunk_cum(p.gate + row * p.Hv + head, p.Hv, rows, lane);
+        if (i >= updates) break;
+        const Cum cum = chunk_cum(fg);
         const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63);
         __syncthreads();
-        load_tile<T, LDK>(tk, k + row * stride_k, stride_k, rows, p.Dk);
-        load_tile<T, LDV>(tv, v + row * stride_v, stride_v, rows, p.Dv);
+        fk.put(tk);
+        fv.put(tv);
         if (wave == 0) weight[lane] = REV ? p.scale * expf(cum.hi + cum.lo) : decay_between(end_hi, end_lo, cum.hi, cum.lo);
         __syncthreads();
-        S.scale(expf(end_hi + end_lo));
+        if (i + 1 < updates) fetch(i + 1);
+        const float whole = expf(end_hi + end_lo);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t] *= whole;
         total += (double)end_hi + (double)end_lo;
-        update_state<T, KD, VT, LDK, LDV>(S, tk, tv, weight, wave, lane);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const F32x4 w0 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 4 * g), w1 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 16 + 4 * g);
+            frag_t<T> vp[P];
+            pieces_of<T>(widened(TV::col_frag(tv, s, wave, lane)) * joined(w0, w1), vp);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const frag_t<T> kf = TK::col_frag(tk, s, t, lane);
+#pragma unroll
+                for (int q = P - 1; q >= 0; --q) S[t] = mma(vp[q], kf, S[t]);
+            }
+        }
     }
     if (STORE) {
-        if (REV && seg.index == 0 && p.ds0) S.store(p.ds0 + ((long long)seg.seq * p.Hv + head) * cells, wave, lane, p.Dk, p.Dv);
+        if (REV && seg.index == 0 && p.ds0) store(p.ds0 + ((long long)seg.seq * p.Hv + head) * cells);
     } else {
-        S.store(seg_states + ((long long)seg_no * p.Hv + head) * cells, wave, lane, p.Dk, p.Dv);
+        store(seg_states + ((long long)seg_no * p.Hv + head) * cells);
         if (threadIdx.x == 0) p.seg_decay[(REV ? (long long)p.plan.max_segs * p.Hv : 0) + (long long)seg_no * p.Hv + head] = (float)exp(total);
     }
 }
 
 // blockIdx.y: 0 the states, 1 their gradients
-template <typename T, int KD, int VT, bool STORE>
-__global__ __launch_bounds__(64 * kWaves) void matrec_states_kernel(const MatrecParams p) {
+template <typename T, int DK, int DV, bool STORE>
+__global__ __launch_bounds__(4 * DV) void matrec_states_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     T* tk = reinterpret_cast<T*>(lds);
-    T* tv = tk + kChunk * (64 * KD + Op<T>::PAD);
-    float* weight = reinterpret_cast<float*>(tv + kChunk * (64 * VT + Op<T>::PAD));
+    T* tv = reinterpret_cast<T*>(lds + Tile<T, DK>::bytes);
+    float* weight = reinterpret_cast<float*>(lds + Tile<T, DK>::bytes + Tile<T, DV>::bytes);
     const int seg = blockIdx.x / p.Hv, head = blockIdx.x % p.Hv;
     if (seg >= *p.plan.count) return;
-    if (blockIdx.y == 0) states_of<T, KD, VT, false, STORE>(p, seg, head, tk, tv, weight);
-    else states_of<T, KD, VT, true, STORE>(p, seg, head, tk, tv, weight);
+    if (blockIdx.y == 0) states_of<T, DK, DV, false, STORE>(p, seg, head, tk, tv, weight);
+    else states_of<T, DK, DV, true, STORE>(p, seg, head, tk, tv, weight);
 }
 
 // The segments' own parts joined along a sequence, in their order: seg_state becomes the state in front of each segment (REV: seg_rstate the gradient
-// of the state behind it).  A lane has one cell.  Also what a sequence without rows has in the place of a final state (REV: of ds0).
+// of the state behind it).  A lane has one cell and reads eight segments at a time.  Also what a sequence without rows has in the place of
+// a final state (REV: of ds0).
 template <bool REV>
 __device__ __forceinline__ void join_cell(const MatrecParams& p, int n, int head, int cell) {
     const long long cells = (long long)p.Dk * p.Dv, at = ((long long)n * p.Hv + head) * cells + cell;
@@ -213,11 +197,23 @@ __device__ __forceinline__ void join_cell(const MatrecParams& p, int n, int head
     if (!p.split) return;
     float* states = REV ? p.seg_rstate : p.seg_state;
     const float* decay = p.seg_decay + (REV ? (long long)p.plan.max_segs * p.Hv : 0);
-    for (int i = 0; i < count; ++i) {
-        const long long seg = first + (REV ? count - 1 - i : i), cellat = (seg * p.Hv + head) * cells + cell;
-        const float own = states[cellat];   // (of the last one along the way: not written, not used)
-        states[cellat] = s;
-        s = decay[seg * p.Hv + head] * s + own;
+    constexpr int K = 8;
+    for (int i0 = 0; i0 < count; i0 += K) {
+        float own[K], f[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) {   // (of the last one along the way nothing is written or used)
+            const int j = i0 + i < count - 1 ? i0 + i : 0;
+            const long long seg = (first + (REV ? count - 1 - j : j)) * (long long)p.Hv + head;
+            own[i] = states[seg * cells + cell];
+            f[i] = decay[seg];
+        }
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            if (i0 + i >= count) break;
+            const long long seg = (first + (REV ? count - 1 - i0 - i : i0 + i)) * (long long)p.Hv + head;
+            states[seg * cells + cell] = s;
+            s = f[i] * s + own[i];
+        }
     }
 }
 __global__ __launch_bounds__(256) void matrec_join_kernel(const MatrecParams p, int blocks_per) {
@@ -229,15 +225,23 @@ __global__ __launch_bounds__(256) void matrec_join_kernel(const MatrecParams p, 
 }
 
 // ---- outputs: one segment and head, chunk after chunk, the state in registers ----
-template <typename T, int KD, int VT>
-__global__ __launch_bounds__(64 * kWaves) void matrec_out_kernel(const MatrecParams p) {
-    constexpr int LDK = 64 * KD + Op<T>::PAD, LDV = 64 * VT + Op<T>::PAD, LDP = kChunk + Op<T>::PAD, KS = 2 * KD;
+// Wavefront w has columns 16 w .. of v: S[d][v] for all d as accumulators, which are an operand of S^T q as they stand; outputs are computed
+// transposed, a lane four neighbouring v of a row.  The next chunk's rows are fetched into registers while this one is computed.
+template <typename T, int DK, int DV>
+struct OutLds {
+    static constexpr size_t q = 0, k = Tile<T, DK>::bytes, v = k + Tile<T, DK>::bytes, pairs = v + Tile<T, DV>::bytes, sums = pairs + Tile<T, kChunk>::bytes,
+                            total = sums + 4 * 64 * 4;
+};
+template <typename T, int DK, int DV>
+__global__ __launch_bounds__(4 * DV, sizeof(T) == 2 ? (DV == 128 ? 4 : 3) : 1) void matrec_out_kernel(const MatrecParams p) {
+    constexpr int W = DV / 16, KS = DK / 32, NT = DK / 16, P = Op<T>::PIECES;
+    using L = OutLds<T, DK, DV>;
+    using TK = Tile<T, DK>;
+    using TV = Tile<T, DV>;
+    using TP = Tile<T, kChunk>;
     extern __shared__ __align__(16) unsigned char lds[];
-    T* tq = reinterpret_cast<T*>(lds);
-    T* tk = tq + kChunk * LDK;
-    T* tv = tk + kChunk * LDK;
-    T* tp = tv + kChunk * LDV;
-    float* cum_hi = reinterpret_cast<float*>(tp + kChunk * LDP);
+    T *tq = reinterpret_cast<T*>(lds + L::q), *tk = reinterpret_cast<T*>(lds + L::k), *tv = reinterpret_cast<T*>(lds + L::v), *tp = reinterpret_cast<T*>(lds + L::pairs);
+    float* cum_hi = reinterpret_cast<float*>(lds + L::sums);
     float *cum_lo = cum_hi + 64, *since = cum_lo + 64, *until = since + 64;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
     const int seg_no = blockIdx.x / p.Hv, head = blockIdx.x % p.Hv;
@@ -245,25 +249,55 @@ __global__ __launch_bounds__(64 * kWaves) void matrec_out_kernel(const MatrecPar
     const MatSegment seg = p.plan.segs[seg_no];
     const long long cells = (long long)p.Dk * p.Dv;
     const int kh = head / (p.Hv / p.Hk);
-    const T* q = reinterpret_cast<const T*>(p.q) + (long long)kh * p.Dk;
-    const T* k = reinterpret_cast<const T*>(p.k) + (long long)kh * p.Dk;
-    const T* v = reinterpret_cast<const T*>(p.v) + (long long)head * p.Dv;
-    T* o = reinterpret_cast<T*>(p.o) + (long long)head * p.Dv;
-    StateTile<KD, VT> S;
-    const float* from = p.split && seg.index > 0 ? p.seg_state + ((long long)seg_no * p.Hv + head) * cells
-                                                 : (p.s0 ? p.s0 + ((long long)seg.seq * p.Hv + head) * cells : nullptr);
-    S.load(from, wave, lane, p.Dk, p.Dv);
+    const T* q = reinterpret_cast<const T*>(p.q) + (long long)kh * p.Dk + seg.row0 * p.stride_q;
+    const T* k = reinterpret_cast<const T*>(p.k) + (long long)kh * p.Dk + seg.row0 * p.stride_k;
+    const T* v = reinterpret_cast<const T*>(p.v) + (long long)head * p.Dv + seg.row0 * p.stride_v;
+    T* o = reinterpret_cast<T*>(p.o) + (long long)head * p.Dv + seg.row0 * p.stride_o;
+    const float* gate = p.gate + seg.row0 * p.Hv + head;
+    const bool wide_o = four_wide(o, p.stride_o, p.Dv);
+    const int vcol = 16 * wave + l;
+    F32x4 S[NT];
+    {
+        const float* from = p.split && seg.index > 0 ? p.seg_state + ((long long)seg_no * p.Hv + head) * cells
+                                                     : (p.s0 ? p.s0 + ((long long)seg.seq * p.Hv + head) * cells : nullptr);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            S[t] = F32x4{0, 0, 0, 0};
+            if (from && vcol < p.Dv) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * t + 4 * g + r < p.Dk) S[t][r] = from[(long long)(16 * t + 4 * g + r) * p.Dv + vcol];
+            }
+        }
+    }
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
     const bool ends = seg.index == seg.count - 1;
+    Stage<T, DK, 64 * W> fq, fk;
+    Stage<T, DV, 64 * W> fv;
+    float fg = 0.0f;
+    auto fetch = [&](int c) {
+        const long long row = (long long)c * kChunk;
+        const int rows = seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
+        fq.fetch(q + row * p.stride_q, p.stride_q, rows, p.Dk);
+        fk.fetch(k + row * p.stride_k, p.stride_k, rows, p.Dk);
+        fv.fetch(v + row * p.stride_v, p.stride_v, rows, p.Dv);
+        fg = gate_of(gate + row * p.Hv, p.Hv, rows);
+    };
+    fetch(0);
+    if (wave == 0) {   // the two tiles above the diagonal that a product of 32 terms takes in are zero and stay it
+        using V4 = T __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<V4*>(tp + TP::four(l, 16 + 4 * g)) = V4{};
+        *reinterpret_cast<V4*>(tp + TP::four(32 + l, 48 + 4 * g)) = V4{};
+    }
     for (int c = 0; c < chunks; ++c) {
-        const long long row = seg.row0 + (long long)c * kChunk;
-        const int rows = seg.rows - (long long)c * kChunk < kChunk ? (int)(seg.rows - (long long)c * kChunk) : kChunk;
-        const Cum cum = chunk_cum(p.gate + row * p.Hv + head, p.Hv, rows, lane);
+        const long long row = (long long)c * kChunk;
+        const int rows = seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
+        const Cum cum = chunk_cum(fg);
         const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63);
         __syncthreads();
-        load_tile<T, LDK>(tq, q + row * p.stride_q, p.stride_q, rows, p.Dk);
-        load_tile<T, LDK>(tk, k + row * p.stride_k, p.stride_k, rows, p.Dk);
-        load_tile<T, LDV>(tv, v + row * p.stride_v, p.stride_v, rows, p.Dv);
+        fq.put(tq);
+        fk.put(tk);
+        fv.put(tv);
         if (wave == 0) {
             cum_hi[lane] = cum.hi;
             cum_lo[lane] = cum.lo;
@@ -271,80 +305,70 @@ __global__ __launch_bounds__(64 * kWaves) void matrec_out_kernel(const MatrecPar
             until[lane] = decay_between(end_hi, end_lo, cum.hi, cum.lo);
         }
         __syncthreads();
-        // this wavefront's 16 rows i of the factors e^{c_i - c_j} q_i . k_j, as their transpose: a lane has one i and four neighbouring j
-        {
-            const int i = 16 * wave + l;
-            frag_t<T> qf[KS];
+        // the factors e^{c_i - c_j} q_i . k_j, tile by tile, transposed: a lane has one i and four neighbouring j
+        for (int n = wave; n < 10; n += W) {
+            int ti, tj;
+            lower_tile(n, ti, tj);
+            const int i = 16 * ti + l, j = 16 * tj + 4 * g;
+            F32x4 a = {0, 0, 0, 0};
 #pragma unroll
-            for (int s = 0; s < KS; ++s) qf[s] = row_frag<T, LDK>(tq, i, s, g);
+            for (int s = 0; s < KS; ++s) a = mma(TK::row_frag(tk, 16 * tj + l, s, g), TK::row_frag(tq, i, s, g), a);
             const float hi_i = cum_hi[i], lo_i = cum_lo[i];
+            const F32x4 hj = *reinterpret_cast<const F32x4*>(cum_hi + j), lj = *reinterpret_cast<const F32x4*>(cum_lo + j);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                if (t > (wave | 1)) break;
-                T f[4];
-                if (t <= wave) {
-                    F32x4 a = {0, 0, 0, 0};
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) a = mma(row_frag<T, LDK>(tk, 16 * t + l, s, g), qf[s], a);
-                    const F32x4 hj = *reinterpret_cast<const F32x4*>(cum_hi + 16 * t + 4 * g), lj = *reinterpret_cast<const F32x4*>(cum_lo + 16 * t + 4 * g);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) f[r] = 16 * t + 4 * g + r <= i ? (T)(a[r] * decay_between(hi_i, lo_i, hj[r], lj[r])) : T(0);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) f[r] = T(0);
-                }
-                T* to = tp + i * LDP + place(16 * t + 4 * g);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) to[r] = f[r];
-            }
+            for (int r = 0; r < 4; ++r) a[r] = j + r <= i ? a[r] * decay_between(hi_i, lo_i, hj[r], lj[r]) : 0.0f;
+            store_four<T>(tp + TP::four(i, j), a, 4, true);
         }
+        if (c + 1 < chunks) fetch(c + 1);
         __syncthreads();
-        frag_t<T> vf[2][VT];
+        frag_t<T> vf[2], sf[KS];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s) vf[s] = TV::col_frag(tv, s, wave, lane);
 #pragma unroll
-            for (int u = 0; u < VT; ++u) vf[s][u] = col_frag<LDV>(tv, s, VT * wave + u, lane);
-        frag_t<T> sf[KS][VT];
+        for (int s = 0; s < KS; ++s) sf[s] = rounded<T>(joined(S[2 * s], S[2 * s + 1]));
+        F32x4 acc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] = F32x4{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int u = 0; u < VT; ++u) sf[s][u] = rounded<T>(joined(S.s[2 * s][u], S.s[2 * s + 1][u]));
+            for (int t = 0; t < 4; ++t) acc[t] = mma(sf[s], TK::row_frag(tq, 16 * t + l, s, g), acc[t]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] *= since[16 * t + l];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int t = 2 * s; t < 4; ++t) acc[t] = mma(vf[s], TP::row_frag(tp, 16 * t + l, s, g), acc[t]);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            F32x4 acc[VT];
+            const int i = 16 * t + l, v0 = 16 * wave + 4 * g;
+            if (i < rows && v0 < p.Dv) store_four<T>(o + (row + i) * p.stride_o + v0, p.scale * acc[t], p.Dv - v0, wide_o);
+        }
+        if (c == chunks - 1 && !(ends && p.last)) break;   // the next segment's state comes from the join
+        const float whole = expf(end_hi + end_lo);
 #pragma unroll
-            for (int u = 0; u < VT; ++u) acc[u] = F32x4{0, 0, 0, 0};
+        for (int t = 0; t < NT; ++t) S[t] *= whole;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const frag_t<T> qf = row_frag<T, LDK>(tq, 16 * t + l, s, g);
+        for (int s = 0; s < 2; ++s) {
+            const F32x4 w0 = *reinterpret_cast<const F32x4*>(until + 32 * s + 4 * g), w1 = *reinterpret_cast<const F32x4*>(until + 32 * s + 16 + 4 * g);
+            frag_t<T> vp[P];
+            pieces_of<T>(widened(vf[s]) * joined(w0, w1), vp);
 #pragma unroll
-                for (int u = 0; u < VT; ++u) acc[u] = mma(qf, sf[s][u], acc[u]);
-            }
-            const F32x4 f = *reinterpret_cast<const F32x4*>(since + 16 * t + 4 * g);
+            for (int t = 0; t < NT; ++t) {
+                const frag_t<T> kf = TK::col_frag(tk, s, t, lane);
 #pragma unroll
-            for (int u = 0; u < VT; ++u) acc[u] *= f;
-#pragma unroll
-            for (int s = 0; s <= t / 2; ++s) {
-                const frag_t<T> pf = row_frag<T, LDP>(tp, 16 * t + l, s, g);
-#pragma unroll
-                for (int u = 0; u < VT; ++u) acc[u] = mma(pf, vf[s][u], acc[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < VT; ++u) {
-                const int col = 16 * (VT * wave + u) + l;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * t + 4 * g + r;
-                    if (i < rows && col < p.Dv) o[(row + i) * p.stride_o + col] = (T)(p.scale * acc[u][r]);
-                }
+                for (int q2 = P - 1; q2 >= 0; --q2) S[t] = mma(kf, vp[q2], S[t]);
             }
         }
-        if (ends && c == chunks - 1 && !p.last) break;
-        if (!ends && c == chunks - 1) break;   // the next segment's state comes from the join
-        S.scale(expf(end_hi + end_lo));
-        update_state<T, KD, VT, LDK, LDV>(S, tk, tv, until, wave, lane);
     }
-    if (ends && p.last) S.store(p.last + ((long long)seg.seq * p.Hv + head) * cells, wave, lane, p.Dk, p.Dv);
+    if (ends && p.last && vcol < p.Dv) {
+        float* to = p.last + ((long long)seg.seq * p.Hv + head) * cells;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * t + 4 * g + r < p.Dk) to[(long long)(16 * t + 4 * g + r) * p.Dv + vcol] = S[t][r];
+    }
 }
 
 // ---- one token ----
@@ -400,48 +424,41 @@ __global__ __launch_bounds__(256) void matstep_kernel(const MatstepParams p) {
     }
 }
 
-template <typename T, int KD, int VT>
-constexpr size_t states_lds() { return sizeof(T) * kChunk * (64 * KD + 64 * VT + 2 * Op<T>::PAD) + 4 * 64; }
-template <typename T, int KD, int VT>
-constexpr size_t out_lds() { return sizeof(T) * kChunk * (128 * KD + 64 * VT + 64 + 4 * Op<T>::PAD) + 4 * 64 * 4; }
-
 template <typename K>
-hipError_t launch_lds(K kernel, dim3 grid, size_t lds, const MatrecParams& p, hipStream_t stream) {
+hipError_t launch_lds(K kernel, dim3 grid, int threads, size_t lds, const MatrecParams& p, hipStream_t stream) {
     if (grid.x == 0) return hipSuccess;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), lds, stream, p);
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, stream, p);
     return hipGetLastError();
 }
 
-template <typename T, int KD, int VT>
+// the segments' own parts, and the join; `both`: of the states and of their gradients
+template <typename T, int DK, int DV>
+hipError_t join_shape(const MatrecParams& p, int both, hipStream_t stream) {
+    constexpr size_t lds = Tile<T, DK>::bytes + Tile<T, DV>::bytes + 4 * 64;
+    hipError_t e = hipSuccess;
+    if (p.split) e = launch_lds(matrec_states_kernel<T, DK, DV, false>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), 1 + both), 4 * DV, lds, p, stream);
+    if (e != hipSuccess || !(p.split || p.rows.bounds || p.rows.T == 0)) return e;
+    const int per = (p.Dk * p.Dv + 255) / 256;
+    hipLaunchKernelGGL(matrec_join_kernel, dim3((unsigned)((long long)p.rows.N * p.Hv * per), 1 + both), dim3(256), 0, stream, p, per);
+    return hipGetLastError();
+}
+template <typename T, int DK, int DV>
 hipError_t out_shape(const MatrecParams& p, hipStream_t stream) {
-    const unsigned grid = (unsigned)((long long)p.plan.max_segs * p.Hv);
-    hipError_t e = hipSuccess;
-    if (p.split) e = launch_lds(matrec_states_kernel<T, KD, VT, false>, dim3(grid, 1), states_lds<T, KD, VT>(), p, stream);
+    const hipError_t e = join_shape<T, DK, DV>(p, 0, stream);
     if (e != hipSuccess) return e;
-    if (p.split || p.rows.bounds || p.rows.T == 0) {
-        const int per = (p.Dk * p.Dv + 255) / 256;
-        hipLaunchKernelGGL(matrec_join_kernel, dim3((unsigned)((long long)p.rows.N * p.Hv * per), 1), dim3(256), 0, stream, p, per);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    return launch_lds(matrec_out_kernel<T, KD, VT>, dim3(grid), out_lds<T, KD, VT>(), p, stream);
+    return launch_lds(matrec_out_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv)), 4 * DV, OutLds<T, DK, DV>::total, p, stream);
 }
-template <typename T, int KD, int VT>
+template <typename T, int DK, int DV>
 hipError_t states_shape(const MatrecParams& p, hipStream_t stream) {
-    const unsigned grid = (unsigned)((long long)p.plan.max_segs * p.Hv);
-    hipError_t e = hipSuccess;
-    if (p.split) e = launch_lds(matrec_states_kernel<T, KD, VT, false>, dim3(grid, 2), states_lds<T, KD, VT>(), p, stream);
+    constexpr size_t lds = Tile<T, DK>::bytes + Tile<T, DV>::bytes + 4 * 64;
+    const hipError_t e = join_shape<T, DK, DV>(p, 1, stream);
     if (e != hipSuccess) return e;
-    if (p.split || p.rows.bounds || p.rows.T == 0) {
-        const int per = (p.Dk * p.Dv + 255) / 256;
-        hipLaunchKernelGGL(matrec_join_kernel, dim3((unsigned)((long long)p.rows.N * p.Hv * per), 2), dim3(256), 0, stream, p, per);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    return launch_lds(matrec_states_kernel<T, KD, VT, true>, dim3(grid, 2), states_lds<T, KD, VT>(), p, stream);
+    return launch_lds(matrec_states_kernel<T, DK, DV, true>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), 2), 4 * DV, lds, p, stream);
 }
-#define DEER_BY_SHAPE(F, T, p, stream) \
-    ((p).Dk <= 64 ? ((p).Dv <= 64 ? F<T, 1, 1>(p, stream) : F<T, 1, 2>(p, stream)) : ((p).Dv <= 64 ? F<T, 2, 1>(p, stream) : F<T, 2, 2>(p, stream)))
+#define DEER_BY_SHAPE(F, T, p, stream)                                                                        \
+    ((p).Dk <= 64 ? ((p).Dv <= 64 ? F<T, 64, 64>(p, stream) : F<T, 64, 128>(p, stream)) : ((p).Dv <= 64 ? F<T, 128, 64>(p, stream) : F<T, 128, 128>(p, stream)))
 
 }  // namespace
 

@@ -21,17 +21,14 @@ using I16x4 = short __attribute__((ext_vector_type(4)));
 using I16x8 = short __attribute__((ext_vector_type(8)));
 
 constexpr int kChunk = 64;
-constexpr int kWaves = 4;
 
 template <typename T> struct Op;
 template <> struct Op<BF16> {
     using Frag = BF16x8;
-    static constexpr int PAD = 8;       // elements behind a row of a tile: rows 16 bytes apart in the banks
-    static constexpr int PIECES = 2;    // an fp32 number as the sum of two bf16 ones: 2^-17 off at most (half a step of each part)
+    static constexpr int PIECES = 3;    // an fp32 number as the sum of three bf16 ones: exact to 2^-24 (two: 2.7e-6 measured on states)
 };
 template <> struct Op<float> {
     using Frag = F32x8;
-    static constexpr int PAD = 4;
     static constexpr int PIECES = 1;
 };
 template <typename T> using frag_t = typename Op<T>::Frag;
@@ -43,14 +40,17 @@ __device__ __forceinline__ F32x4 mma(F32x8 a, F32x8 b, F32x4 c) {
     return c;
 }
 
-// fp32 values as an operand: rounded once (the first piece), and what that leaves (the second)
+// fp32 values as an operand: rounded, what that leaves rounded, and so on
 template <typename T>
 __device__ __forceinline__ void pieces_of(F32x8 x, frag_t<T> (&p)[Op<T>::PIECES]) {
     if constexpr (Op<T>::PIECES == 1) {
         p[0] = x;
     } else {
-        p[0] = __builtin_convertvector(x, BF16x8);
-        p[1] = __builtin_convertvector(x - __builtin_convertvector(p[0], F32x8), BF16x8);
+#pragma unroll
+        for (int q = 0; q < Op<T>::PIECES; ++q) {
+            p[q] = __builtin_convertvector(x, BF16x8);
+            x -= __builtin_convertvector(p[q], F32x8);
+        }
     }
 }
 template <typename T>
@@ -62,85 +62,144 @@ __device__ __forceinline__ F32x8 widened(BF16x8 x) { return __builtin_convertvec
 __device__ __forceinline__ F32x8 widened(F32x8 x) { return x; }
 __device__ __forceinline__ F32x8 joined(F32x4 a, F32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// place of column c of a tile's row: columns 4 a .. 4 a + 3 of a block of 32 stay together
-__device__ __forceinline__ int place(int c) {
-    const int a = (c >> 2) & 7;
-    return (c & ~31) + (a & 3) * 8 + (a >> 2) * 4 + (c & 3);
-}
-
-// rows `row` (this lane's), terms of the block of 32 columns s
-template <typename T, int LD>
-__device__ __forceinline__ frag_t<T> row_frag(const T* tile, int row, int s, int g) {
-    return *reinterpret_cast<const frag_t<T>*>(tile + row * LD + 32 * s + 8 * g);
-}
-
-// column 16 t + lane % 16, terms of the block of 32 rows s: the transposed operand
-template <int LD>
-__device__ __forceinline__ BF16x8 col_frag(const BF16* tile, int s, int t, int lane) {
-    typedef __attribute__((address_space(3))) I16x4* LdsPtr;
-    // a group of 16 lanes hands in four rows of 16 columns, four columns a lane; lane l gets column l of them
-    const int g = lane >> 4, l = lane & 15;
-    const BF16* at = tile + (32 * s + 4 * g + (l >> 2)) * LD + place(16 * t + 4 * (l & 3));
-    const I16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at);
-    const I16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + 16 * LD));
-    return __builtin_bit_cast(BF16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-template <int LD>
-__device__ __forceinline__ F32x8 col_frag(const float* tile, int s, int t, int lane) {
-    const int g = lane >> 4, c = place(16 * t + (lane & 15));
-    F32x8 f;
+// A tile of 64 rows and C (64 or 128) columns in LDS.  A block of 32 columns lies in the order of the terms: a lane group's eight terms are
+// one unit.  bf16: units of 16 bytes, their place in the row turned by the row so that neither 16 rows of one unit (row_frag) nor
+// four units of four rows (col_frag) meet in a bank.  fp32: rows 16 bytes apart in the banks.
+template <typename T, int C> struct Tile {
+    static constexpr int LD = sizeof(T) == 2 ? C : C + 4;
+    static constexpr size_t bytes = sizeof(T) * kChunk * LD;
+    static __device__ __forceinline__ int turn(int row) { return C == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (row >> 1) & 7; }
+    // columns c .. c + 3, c a multiple of four
+    static __device__ __forceinline__ int four(int row, int c) {
+        const int unit = (c >> 5) * 4 + ((c >> 2) & 3), half = (c >> 4) & 1;
+        if constexpr (sizeof(T) == 2) return row * LD + ((unit ^ turn(row)) << 3) + half * 4;
+        else return row * LD + unit * 8 + half * 4;
+    }
+    // rows `row` (this lane's), terms of the block of 32 columns s
+    static __device__ __forceinline__ frag_t<T> row_frag(const T* t, int row, int s, int g) { return *reinterpret_cast<const frag_t<T>*>(t + four(row, 32 * s + 4 * g)); }
+    // column 16 n + lane % 16, terms of the block of 32 rows s: the transposed operand
+    static __device__ __forceinline__ frag_t<T> col_frag(const T* t, int s, int n, int lane) {
+        const int g = lane >> 4, l = lane & 15;
+        if constexpr (sizeof(T) == 2) {
+            typedef __attribute__((address_space(3))) I16x4* LdsPtr;
+            // a group of 16 lanes hands in four rows of 16 columns, four columns a lane; lane l gets column l of them
+            const BF16* at = t + four(32 * s + 4 * g + (l >> 2), 16 * n + 4 * (l & 3));
+            const I16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at);
+            const I16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + 16 * LD));   // (turn() is the same 16 rows on)
+            return __builtin_bit_cast(BF16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const float* at = t + four(32 * s + 4 * g, 16 * n + (l & 12)) + (l & 3);
+            F32x8 f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = tile[(32 * s + 4 * g + (e & 3) + (e >= 4 ? 16 : 0)) * LD + c];
-    return f;
-}
-
-// 64 rows of `cols` columns from memory into a tile of LD - PAD columns; what is not there is zero
-template <typename T, int LD>
-__device__ __forceinline__ void load_tile(T* tile, const T* from, long long stride, int rows, int cols) {
-    using V4 = T __attribute__((ext_vector_type(4)));
-    using V8 = T __attribute__((ext_vector_type(8)));
-    constexpr int C = LD - Op<T>::PAD;
-    const bool wide = cols % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(from) % 16 == 0;
-    if (wide) {
-        constexpr int PER = C / 8;
-#pragma unroll
-        for (int i = 0; i < kChunk * PER / (64 * kWaves); ++i) {
-            const int at = i * 64 * kWaves + threadIdx.x, r = at / PER, c = at % PER * 8;
-            V8 v = {};
-            if (r < rows && c < cols) v = *reinterpret_cast<const V8*>(from + r * stride + c);
-            *reinterpret_cast<V4*>(tile + r * LD + place(c)) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-            *reinterpret_cast<V4*>(tile + r * LD + place(c + 4)) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-        }
-    } else {
-        for (int at = threadIdx.x; at < kChunk * C; at += 64 * kWaves) {
-            const int r = at / C, c = at % C;
-            tile[r * LD + place(c)] = r < rows && c < cols ? from[r * stride + c] : T(0);
+            for (int e = 0; e < 8; ++e) f[e] = at[((e & 3) + (e >= 4 ? 16 : 0)) * LD];
+            return f;
         }
     }
+};
+
+// 64 rows of `cols` columns on their way from memory into a tile: fetched into registers, put into LDS later.  What is not there is zero.
+template <typename T, int C, int THREADS> struct Stage {
+    using V8 = T __attribute__((ext_vector_type(8)));
+    using V4 = T __attribute__((ext_vector_type(4)));
+    static constexpr int PER = C / 8, N = kChunk * PER / THREADS;
+    static_assert(kChunk * PER % THREADS == 0, "every thread has as many units");
+    V8 r[N];
+    __device__ __forceinline__ void fetch(const T* from, long long stride, int rows, int cols) {
+        const bool wide = cols % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(from) % 16 == 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = i * THREADS + threadIdx.x, row = at / PER, c = at % PER * 8;
+            r[i] = V8{};
+            if (row < rows) {
+                const T* src = from + row * stride + c;
+                if (wide) {
+                    if (c < cols) r[i] = *reinterpret_cast<const V8*>(src);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (c + e < cols) r[i][e] = src[e];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void put(T* tile) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = i * THREADS + threadIdx.x, row = at / PER, c = at % PER * 8;
+            *reinterpret_cast<V4*>(tile + Tile<T, C>::four(row, c)) = __builtin_shufflevector(r[i], r[i], 0, 1, 2, 3);
+            *reinterpret_cast<V4*>(tile + Tile<T, C>::four(row, c + 4)) = __builtin_shufflevector(r[i], r[i], 4, 5, 6, 7);
+        }
+    }
+};
+
+// four values of a row, rounded: one store where the rows allow it
+template <typename T>
+__device__ __forceinline__ void store_four(T* to, F32x4 x, int count, bool wide) {
+    using V4 = T __attribute__((ext_vector_type(4)));
+    if (wide) {
+        if (count >= 4) *reinterpret_cast<V4*>(to) = __builtin_convertvector(x, V4);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < count) to[r] = (T)x[r];
+    }
+}
+template <typename T>
+__device__ __forceinline__ bool four_wide(const T* base, long long stride, int cols) {
+    return cols % 4 == 0 && stride % 4 == 0 && reinterpret_cast<uintptr_t>(base) % (4 * sizeof(T)) == 0;
 }
 
-// Running sum of a chunk's log gates, inclusive, of which differences are taken: as the sum of two floats (a sum of 64
+// Running sum of a chunk's log gates, inclusive, lane by lane, of which differences are taken: as the sum of two floats (a sum of 64
 // gates of down to -1e4, 2^-46 of it off).  A gate below -1e4 stands for it: its factor is zero either way.
 struct Cum {
     float hi, lo;
 };
-__device__ __forceinline__ Cum chunk_cum(const float* gate, long long stride, int rows, int lane) {
-    float g = lane < rows ? gate[lane * stride] : 0.0f;
-    g = g < -1e4f ? -1e4f : g;
-    double c = g;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double o = __shfl_up(c, d);
-        c += lane >= d ? o : 0.0;
-    }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double shifted(double v) {
+    const long long b = __double_as_longlong(v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)b, CTRL, ROWS, 0xF, true);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)((unsigned long long)b >> 32), CTRL, ROWS, 0xF, true);
+    return __longlong_as_double((long long)(((unsigned long long)hi << 32) | lo));
+}
+__device__ __forceinline__ Cum chunk_cum(float g) {
+    double c = g < -1e4f ? -1e4f : g;
+    c += shifted<0x111, 0xF>(c);   // one, two, four, eight lanes on within rows of 16
+    c += shifted<0x112, 0xF>(c);
+    c += shifted<0x114, 0xF>(c);
+    c += shifted<0x118, 0xF>(c);
+    c += shifted<0x142, 0xA>(c);   // the last lane of a row to the next row, the second's to the upper half
+    c += shifted<0x143, 0xC>(c);
     Cum r;
     r.hi = (float)c;
     r.lo = (float)(c - (double)r.hi);
     return r;
 }
+__device__ __forceinline__ float gate_of(const float* gate, long long stride, int rows) {
+    const int lane = threadIdx.x & 63;
+    return lane < rows ? gate[lane * stride] : 0.0f;
+}
 __device__ __forceinline__ float decay_between(float hi_i, float lo_i, float hi_j, float lo_j) { return expf((hi_i - hi_j) + (lo_i - lo_j)); }
 
 __device__ __forceinline__ float lane_value(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+
+// sum over the 16 lanes of a group, in all of them (DPP rotations of a row of 16 lanes by 8, 4, 2, 1)
+template <int CTRL>
+__device__ __forceinline__ float rotated(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float group_sum(float v) {
+    v += rotated<0x128>(v);
+    v += rotated<0x124>(v);
+    v += rotated<0x122>(v);
+    v += rotated<0x121>(v);
+    return v;
+}
+
+// tile n of the ten 16 x 16 tiles on and below the diagonal of a chunk's 64 x 64 pairs
+__device__ __forceinline__ void lower_tile(int n, int& ti, int& tj) {
+    ti = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3;
+    tj = n - ti * (ti + 1) / 2;
+}
 
 }  // namespace
 
@@ -171,7 +230,7 @@ struct MatrecParams {
     bool split;                      // several segments a sequence: their states are joined through memory
     float *seg_state, *seg_rstate;   // [max_segs][Hv][Dk][Dv]: sums, then states in front of (behind) each
     float *seg_decay;                // [max_segs][Hv]
-    float *chunk_state, *chunk_rstate;   // [chunks][Hv][Dk][Dv], gradient only
+    float *chunk_state, *chunk_rstate;   // [chunks][Hv][64 or 128][64 or 128] (the next from Dk, Dv), gradient only
 };
 struct MatstepParams {
     StepRows rows;

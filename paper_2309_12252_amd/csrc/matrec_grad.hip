@@ -6,79 +6,58 @@
 // the chunk, what comes from S and is read at i >= t, what j < t adds and R takes on, and what goes through from S to R:
 //   dgate_t = sum_{i >= t > j} E_ij A_ij B_ij + sum_{i >= t} q_i . (scale e^{c_i} S dout_i) + sum_{j < t} k_j . (e^{c_64 - c_j} R v_j) + e^{c_64} <S, R>,
 // each of them a sum of what belongs to it alone, so that a strong gate's small gradient is no difference of large numbers.  The pairs: running
-// sums over j along every row i, of which t takes those of the rows i >= t at j = t - 1.  A and B are exact products of the inputs, S and R enter dgate's products as two bf16 pieces.
+// sums over j along every row i, of which t takes those of the rows i >= t at j = t - 1.  A and B are exact products of the inputs, S and R enter dgate's products as three bf16 pieces.
 // Heads of v that share one of q and k are gone through one after another, their dq and dk added in registers, always in the same order.
 #include "matrec_common.h"
 
 namespace deer {
 namespace {
 
-// sum over the 16 lanes of a group, in all of them (DPP rotations of a row of 16 lanes by 8, 4, 2, 1)
-template <int CTRL>
-__device__ __forceinline__ float rotated(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+// Chunk states lie in memory as whole tiles of DK x DV floats, zero outside the head.  Eight terms of row d, the block of 32 columns s:
+template <int DV>
+__device__ __forceinline__ F32x8 state_row(const float* S, int d, int s, int g) {
+    const float* at = S + d * DV + 32 * s + 4 * g;
+    return joined(*reinterpret_cast<const F32x4*>(at), *reinterpret_cast<const F32x4*>(at + 16));
 }
-__device__ __forceinline__ float group_sum(float v) {
-    v += rotated<0x128>(v);
-    v += rotated<0x124>(v);
-    v += rotated<0x122>(v);
-    v += rotated<0x121>(v);
-    return v;
-}
-
-// eight terms of S (rows of Dv columns in memory, fp32), the block of 32 columns s of row d; zero outside
-__device__ __forceinline__ F32x8 state_row(const float* S, int d, int s, int g, int Dk, int Dv) {
-    F32x8 x = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int c0 = 32 * s + 4 * g;
-    if (d >= Dk) return x;
-    const float* at = S + (long long)d * Dv + c0;
-    if ((Dv & 3) == 0) {   // rows 16 bytes aligned, as the states' array is
-        if (c0 < Dv) {
-            const F32x4 v = *reinterpret_cast<const F32x4*>(at);
+// column v, the block of 32 rows s
+template <int DV>
+__device__ __forceinline__ F32x8 state_col(const float* S, int v, int s, int g) {
+    F32x8 x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = v[e];
-        }
-        if (c0 + 16 < Dv) {
-            const F32x4 v = *reinterpret_cast<const F32x4*>(at + 16);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 + e] = v[e];
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int c = (e & 3) + (e >= 4 ? 16 : 0);
-            if (c0 + c < Dv) x[e] = at[c];
-        }
-    }
-    return x;
-}
-// column v of S, the block of 32 rows s
-__device__ __forceinline__ F32x8 state_col(const float* S, int v, int s, int g, int Dk, int Dv) {
-    F32x8 x = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (v >= Dv) return x;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int d = 32 * s + 4 * g + (e & 3) + (e >= 4 ? 16 : 0);
-        if (d < Dk) x[e] = S[(long long)d * Dv + v];
-    }
+    for (int e = 0; e < 8; ++e) x[e] = S[(32 * s + 4 * g + (e & 3) + (e >= 4 ? 16 : 0)) * DV + v];
     return x;
 }
 
-template <typename T, int KD, int VT>
-__global__ __launch_bounds__(64 * kWaves) void matrec_grad_kernel(const MatrecParams p) {
-    constexpr int LDK = 64 * KD + Op<T>::PAD, LDV = 64 * VT + Op<T>::PAD, LDP = kChunk + Op<T>::PAD, KS = 2 * KD, VS = 2 * VT, P = Op<T>::PIECES;
+template <typename T, int DK, int DV>
+struct GradLds {
+    static constexpr size_t q = 0, k = Tile<T, DK>::bytes, v = k + Tile<T, DK>::bytes, d = v + Tile<T, DV>::bytes, pairs = d + Tile<T, DV>::bytes,
+                            sums = pairs + Tile<T, kChunk>::bytes;
+    static constexpr int W = (DK > DV ? DK : DV) / 16;
+    // cum_hi, cum_lo, since, until; by wavefront: in, out, pairs; totals of four tiles; by wavefront: through
+    static constexpr size_t total = sums + 4 * (4 * 64 + (2 * W + 4) * 64 + 4 * 64 + 8);
+    static_assert(total <= 160 * 1024, "a workgroup's tiles fit the CU's LDS");
+};
+
+// One chunk and head of q and k.  Wavefront w has the columns 16 w .. of d, for dq and dk, and of v, for dv; all of them are computed transposed, a lane
+// four neighbouring columns of a row.  States are read from memory straight into operands: every cell once by the wavefront that has
+// its row d, R's once more by columns.
+template <typename T, int DK, int DV>
+__global__ __launch_bounds__(4 * (DK > DV ? DK : DV), sizeof(T) == 2 ? 2 : 1) void matrec_grad_kernel(const MatrecParams p) {
+    using L = GradLds<T, DK, DV>;
+    using TK = Tile<T, DK>;
+    using TV = Tile<T, DV>;
+    using TP = Tile<T, kChunk>;
+    constexpr int W = L::W, KS = DK / 32, VS = DV / 32, P = Op<T>::PIECES;
     extern __shared__ __align__(16) unsigned char lds[];
-    T* tq = reinterpret_cast<T*>(lds);
-    T* tk = tq + kChunk * LDK;
-    T* tv = tk + kChunk * LDK;
-    T* td = tv + kChunk * LDV;
-    T* tp = td + kChunk * LDV;
-    float* cum_hi = reinterpret_cast<float*>(tp + kChunk * LDP);
+    T *tq = reinterpret_cast<T*>(lds + L::q), *tk = reinterpret_cast<T*>(lds + L::k), *tv = reinterpret_cast<T*>(lds + L::v), *td = reinterpret_cast<T*>(lds + L::d),
+      *tp = reinterpret_cast<T*>(lds + L::pairs);
+    float* cum_hi = reinterpret_cast<float*>(lds + L::sums);
     float *cum_lo = cum_hi + 64, *since = cum_lo + 64, *until = since + 64;
-    float* sum_in = until + 64;          // [4][64]: q_i . (...) by wavefront
-    float* sum_out = sum_in + 256;       // [4][64]
-    float* sum_pairs = sum_out + 256;    // [4][64]: at j what passes row j + 1
-    float* sum_through = sum_pairs + 256;   // [4]
+    float* sum_in = until + 64;              // [W][64]: scale e^{c_i} q_i . (S dout_i), the part of a wavefront's columns
+    float* sum_out = sum_in + 64 * W;        // [W][64]: e^{c_64 - c_j} k_j . (R v_j)
+    float* sum_pairs = sum_out + 64 * W;     // [row tile][64]: at j the pairs (i, j' <= j) of j's tile with i > j, over the rows i of a row tile
+    float* row_total = sum_pairs + 256;      // [column tile][64]: the pairs of row i in a tile
+    float* sum_through = row_total + 256;    // [W]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
     const int kh = blockIdx.x % p.Hk, chunk_no = (int)(blockIdx.x / p.Hk), seg_no = chunk_no / p.plan.per, c = chunk_no % p.plan.per;
     if (seg_no >= *p.plan.count) return;
@@ -86,282 +65,262 @@ __global__ __launch_bounds__(64 * kWaves) void matrec_grad_kernel(const MatrecPa
     const long long left = seg.rows - (long long)c * kChunk;
     if (left <= 0) return;
     const int rows = left < kChunk ? (int)left : kChunk, group = p.Hv / p.Hk;
-    const long long row = seg.row0 + (long long)c * kChunk, cells = (long long)p.Dk * p.Dv;
+    const long long row = seg.row0 + (long long)c * kChunk;
+    const int d0 = 16 * wave + 4 * g;        // a lane's four columns of d, and of v
+    const bool has_d = 16 * wave < DK, has_v = 16 * wave < DV;
 
-    F32x4 dq[4][KD], dk[4][KD];
+    Stage<T, DV, 64 * W> fv, fd;
+    {
+        Stage<T, DK, 64 * W> fq, fk;
+        fq.fetch(reinterpret_cast<const T*>(p.q) + row * p.stride_q + (long long)kh * p.Dk, p.stride_q, rows, p.Dk);
+        fk.fetch(reinterpret_cast<const T*>(p.k) + row * p.stride_k + (long long)kh * p.Dk, p.stride_k, rows, p.Dk);
+        fv.fetch(reinterpret_cast<const T*>(p.v) + row * p.stride_v + (long long)kh * group * p.Dv, p.stride_v, rows, p.Dv);
+        fd.fetch(reinterpret_cast<const T*>(p.dout) + row * p.stride_o + (long long)kh * group * p.Dv, p.stride_o, rows, p.Dv);
+        fq.put(tq);
+        fk.put(tk);
+    }
+    // pairs above the diagonal that a product of 32 terms takes in are zero
+    using V4 = T __attribute__((ext_vector_type(4)));
+    if (wave == 0) {
+        *reinterpret_cast<V4*>(tp + TP::four(l, 16 + 4 * g)) = V4{};
+        *reinterpret_cast<V4*>(tp + TP::four(32 + l, 48 + 4 * g)) = V4{};
+    }
+    F32x4 dq[4], dk[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int u = 0; u < KD; ++u) dq[t][u] = dk[t][u] = F32x4{0, 0, 0, 0};
-    load_tile<T, LDK>(tq, reinterpret_cast<const T*>(p.q) + row * p.stride_q + (long long)kh * p.Dk, p.stride_q, rows, p.Dk);
-    load_tile<T, LDK>(tk, reinterpret_cast<const T*>(p.k) + row * p.stride_k + (long long)kh * p.Dk, p.stride_k, rows, p.Dk);
+    for (int t = 0; t < 4; ++t) dq[t] = dk[t] = F32x4{0, 0, 0, 0};
 
     for (int member = 0; member < group; ++member) {
         const int head = kh * group + member;
-        const Cum cum = chunk_cum(p.gate + row * p.Hv + head, p.Hv, rows, lane);
+        const Cum cum = chunk_cum(gate_of(p.gate + row * p.Hv + head, p.Hv, rows));
         const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63), whole = expf(end_hi + end_lo);
-        load_tile<T, LDV>(tv, reinterpret_cast<const T*>(p.v) + row * p.stride_v + (long long)head * p.Dv, p.stride_v, rows, p.Dv);
-        load_tile<T, LDV>(td, reinterpret_cast<const T*>(p.dout) + row * p.stride_o + (long long)head * p.Dv, p.stride_o, rows, p.Dv);
+        fv.put(tv);
+        fd.put(td);
         if (wave == 0) {
             cum_hi[lane] = cum.hi;
             cum_lo[lane] = cum.lo;
             since[lane] = p.scale * expf(cum.hi + cum.lo);
             until[lane] = decay_between(end_hi, end_lo, cum.hi, cum.lo);
         }
+        if (threadIdx.x < 256) sum_pairs[threadIdx.x] = row_total[threadIdx.x] = 0.0f;
         __syncthreads();
-        const float* S = p.chunk_state + ((long long)(seg.chunk0 + c) * p.Hv + head) * cells;
-        const float* R = p.chunk_rstate + ((long long)(seg.chunk0 + c) * p.Hv + head) * cells;
+        const float* S = p.chunk_state + ((long long)(seg.chunk0 + c) * p.Hv + head) * (DK * DV);
+        const float* R = p.chunk_rstate + ((long long)(seg.chunk0 + c) * p.Hv + head) * (DK * DV);
 
-        // ---- the pairs: rows i of this wavefront, as transposes: a lane has one i and four neighbouring j of every tile ----
-        F32x4 ea[4];   // E_ij A_ij, for later
-        {
-            const int i = 16 * wave + l;
-            frag_t<T> qf[KS], df[VS];
+        // ---- pairs, tile by tile, as transposes: a lane has one i and four neighbouring j ----
+        F32x4 ea[10 / W + 1];   // E_ij A_ij of this wavefront's tiles, for dv
 #pragma unroll
-            for (int s = 0; s < KS; ++s) qf[s] = row_frag<T, LDK>(tq, i, s, g);
+        for (int m = 0; m < 10 / W + 1; ++m) {
+            const int n = wave + m * W;
+            if (n >= 10) break;
+            int ti, tj;
+            lower_tile(n, ti, tj);
+            const int i = 16 * ti + l, j0 = 16 * tj + 4 * g;
+            F32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
 #pragma unroll
-            for (int s = 0; s < VS; ++s) df[s] = row_frag<T, LDV>(td, i, s, g);
+            for (int s = 0; s < KS; ++s) a = mma(TK::row_frag(tk, 16 * tj + l, s, g), TK::row_frag(tq, i, s, g), a);
+#pragma unroll
+            for (int s = 0; s < VS; ++s) b = mma(TV::row_frag(tv, 16 * tj + l, s, g), TV::row_frag(td, i, s, g), b);
             const float hi_i = cum_hi[i], lo_i = cum_lo[i];
-            float run = 0.0f;   // sum of the row's pairs in the tiles so far
+            const F32x4 hj = *reinterpret_cast<const F32x4*>(cum_hi + j0), lj = *reinterpret_cast<const F32x4*>(cum_lo + j0);
+            F32x4 upto;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                F32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-                F32x4 upto = {0, 0, 0, 0};
-                if (t <= wave) {
+            for (int r = 0; r < 4; ++r) {
+                const int j = j0 + r;
+                const float e = j <= i ? p.scale * decay_between(hi_i, lo_i, hj[r], lj[r]) : 0.0f;
+                upto[r] = (r > 0 ? upto[r > 0 ? r - 1 : 0] : 0.0f) + (j < i ? e * a[r] * b[r] : 0.0f);
+                a[r] = j <= i ? e * a[r] : 0.0f;
+                b[r] = j <= i ? e * b[r] : 0.0f;
+            }
+            ea[m] = a;
+            store_four<T>(tp + TP::four(i, j0), b, 4, true);
+            // the lane groups in front of this one have the smaller j
+            float front = upto[3];
+            const float one = __shfl_up(front, 16);
+            front += g >= 1 ? one : 0.0f;
+            const float two = __shfl_up(front, 32);
+            front += g >= 2 ? two : 0.0f;
+            const float before = __shfl_up(front, 16);
+            if (g == 3) row_total[64 * tj + i] = front;
 #pragma unroll
-                    for (int s = 0; s < KS; ++s) a = mma(row_frag<T, LDK>(tk, 16 * t + l, s, g), qf[s], a);
-#pragma unroll
-                    for (int s = 0; s < VS; ++s) b = mma(row_frag<T, LDV>(tv, 16 * t + l, s, g), df[s], b);
-                    const F32x4 hj = *reinterpret_cast<const F32x4*>(cum_hi + 16 * t + 4 * g), lj = *reinterpret_cast<const F32x4*>(cum_lo + 16 * t + 4 * g);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int j = 16 * t + 4 * g + r;
-                        const float e = j <= i ? p.scale * decay_between(hi_i, lo_i, hj[r], lj[r]) : 0.0f;
-                        upto[r] = (r > 0 ? upto[r > 0 ? r - 1 : 0] : 0.0f) + (j < i ? e * a[r] * b[r] : 0.0f);
-                        a[r] = j <= i ? e * a[r] : 0.0f;
-                        b[r] = j <= i ? e * b[r] : 0.0f;
-                    }
-                    // the lane groups in front of this one have the smaller j
-                    float front = upto[3];   // this group's and those of the groups in front
-                    const float one = __shfl_up(front, 16);
-                    front += g >= 1 ? one : 0.0f;
-                    const float two = __shfl_up(front, 32);
-                    front += g >= 2 ? two : 0.0f;
-                    const float before = __shfl_up(front, 16);
-                    const float offset = run + (g >= 1 ? before : 0.0f);
-                    run += __shfl(front, 48 + l);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) upto[r] = 16 * t + 4 * g + r < i ? upto[r] + offset : 0.0f;
-                }
-                ea[t] = a;
-                T* to = tp + i * LDP + place(16 * t + 4 * g);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) to[r] = (T)b[r];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float s = group_sum(upto[r]);
-                    if (l == 0) sum_pairs[64 * wave + 16 * t + 4 * g + r] = s;
-                }
+            for (int r = 0; r < 4; ++r) {
+                float s = j0 + r < i ? upto[r] + (g >= 1 ? before : 0.0f) : 0.0f;
+                s = group_sum(s);
+                if (l == 0) sum_pairs[64 * ti + j0 + r] = s;
             }
         }
         __syncthreads();
 
-        // ---- dq and dk: this wavefront's columns d ----
-        {
+        // ---- dq and dk ----
+        if (has_d) {
+            F32x4 in[4], out[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) in[t] = out[t] = F32x4{0, 0, 0, 0};
             float through = 0.0f;
-            frag_t<T> sf[VS][KD][P], rf[VS][KD][P];
 #pragma unroll
-            for (int s = 0; s < VS; ++s)
+            for (int s = 0; s < VS; ++s) {
+                const F32x8 x = state_row<DV>(S, 16 * wave + l, s, g), y = state_row<DV>(R, 16 * wave + l, s, g);
 #pragma unroll
-                for (int u = 0; u < KD; ++u) {
-                    const int d = 16 * (KD * wave + u) + l;
-                    const F32x8 x = state_row(S, d, s, g, p.Dk, p.Dv), y = state_row(R, d, s, g, p.Dk, p.Dv);
+                for (int e = 0; e < 8; ++e) through += x[e] * y[e];
+                frag_t<T> xp[P], yp[P];
+                pieces_of<T>(x, xp);
+                pieces_of<T>(y, yp);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) through += x[e] * y[e];
-                    pieces_of<T>(x, sf[s][u]);
-                    pieces_of<T>(y, rf[s][u]);
+                for (int t = 0; t < 4; ++t) {
+                    const frag_t<T> df = TV::row_frag(td, 16 * t + l, s, g), vf = TV::row_frag(tv, 16 * t + l, s, g);
+#pragma unroll
+                    for (int q = P - 1; q >= 0; --q) {
+                        in[t] = mma(xp[q], df, in[t]);
+                        out[t] = mma(yp[q], vf, out[t]);
+                    }
                 }
+            }
             through += __shfl_xor(through, 16);
             through += __shfl_xor(through, 32);
             through = group_sum(through);
             if (lane == 0) sum_through[wave] = through;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                F32x4 in[KD], out[KD];
-#pragma unroll
-                for (int u = 0; u < KD; ++u) in[u] = out[u] = F32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int s = 0; s < VS; ++s) {
-                    const frag_t<T> df = row_frag<T, LDV>(td, 16 * t + l, s, g), vf = row_frag<T, LDV>(tv, 16 * t + l, s, g);
-#pragma unroll
-                    for (int u = 0; u < KD; ++u)
-#pragma unroll
-                        for (int q = P - 1; q >= 0; --q) {
-                            in[u] = mma(df, sf[s][u][q], in[u]);
-                            out[u] = mma(vf, rf[s][u][q], out[u]);
-                        }
-                }
-                const F32x4 fi = *reinterpret_cast<const F32x4*>(since + 16 * t + 4 * g), fo = *reinterpret_cast<const F32x4*>(until + 16 * t + 4 * g);
-                F32x4 dot_in = {0, 0, 0, 0}, dot_out = {0, 0, 0, 0};
-#pragma unroll
-                for (int u = 0; u < KD; ++u) {
-                    in[u] *= fi;
-                    out[u] *= fo;
-                    const int col = place(16 * (KD * wave + u) + l);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        dot_in[r] += (float)tq[(16 * t + 4 * g + r) * LDK + col] * in[u][r];
-                        dot_out[r] += (float)tk[(16 * t + 4 * g + r) * LDK + col] * out[u][r];
-                    }
-                    dq[t][u] += in[u];
-                    dk[t][u] += out[u];
-                }
+                const int i = 16 * t + l;
+                in[t] *= since[i];
+                out[t] *= until[i];
+                const V4 q4 = *reinterpret_cast<const V4*>(tq + TK::four(i, d0)), k4 = *reinterpret_cast<const V4*>(tk + TK::four(i, d0));
+                float x = 0.0f, y = 0.0f;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float x = group_sum(dot_in[r]), y = group_sum(dot_out[r]);
-                    if (l == 0) {
-                        sum_in[64 * wave + 16 * t + 4 * g + r] = x;
-                        sum_out[64 * wave + 16 * t + 4 * g + r] = y;
-                    }
+                    x += (float)q4[r] * in[t][r];
+                    y += (float)k4[r] * out[t][r];
                 }
+                x += __shfl_xor(x, 16);
+                y += __shfl_xor(y, 16);
+                x += __shfl_xor(x, 32);
+                y += __shfl_xor(y, 32);
+                if (g == 0) {
+                    sum_in[64 * wave + i] = x;
+                    sum_out[64 * wave + i] = y;
+                }
+                dq[t] += in[t];
+                dk[t] += out[t];
             }
-            // inside the chunk
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                frag_t<T> kf[KD], qf[KD];
-#pragma unroll
-                for (int u = 0; u < KD; ++u) {
-                    kf[u] = col_frag<LDK>(tk, s, KD * wave + u, lane);
-                    qf[u] = col_frag<LDK>(tq, s, KD * wave + u, lane);
-                }
+                const frag_t<T> kf = TK::col_frag(tk, s, wave, lane), qf = TK::col_frag(tq, s, wave, lane);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    if (s <= t / 2) {   // rows i of tile t take the columns j of the block s
-                        const frag_t<T> pf = row_frag<T, LDP>(tp, 16 * t + l, s, g);
-#pragma unroll
-                        for (int u = 0; u < KD; ++u) dq[t][u] = mma(pf, kf[u], dq[t][u]);
-                    }
-                    if (s >= t / 2) {   // columns j of tile t take the rows i of the block s
-                        const frag_t<T> pf = col_frag<LDP>(tp, s, t, lane);
-#pragma unroll
-                        for (int u = 0; u < KD; ++u) dk[t][u] = mma(pf, qf[u], dk[t][u]);
-                    }
+                    if (s <= t / 2) dq[t] = mma(kf, TP::row_frag(tp, 16 * t + l, s, g), dq[t]);   // rows i of tile t take the columns j of block s
+                    if (s >= t / 2) dk[t] = mma(qf, TP::col_frag(tp, s, t, lane), dk[t]);         // columns j of tile t the rows i of block s
                 }
             }
+        } else if (lane == 0) {
+            sum_through[wave] = 0.0f;
         }
+        if (!has_d) sum_in[64 * wave + lane] = sum_out[64 * wave + lane] = 0.0f;
         __syncthreads();
 
-        // ---- dv: this wavefront's columns v; and the gates ----
+        // ---- the other pairs, the gates, and dv ----
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            T* to = tp + (16 * wave + l) * LDP + place(16 * t + 4 * g);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) to[r] = (T)ea[t][r];
+        for (int m = 0; m < 10 / W + 1; ++m) {
+            const int n = wave + m * W;
+            if (n >= 10) break;
+            int ti, tj;
+            lower_tile(n, ti, tj);
+            store_four<T>(tp + TP::four(16 * ti + l, 16 * tj + 4 * g), ea[m], 4, true);
         }
-        if (wave == 0 && p.dgate) {
+        if (wave == W - 1 && p.dgate) {
             // a lane has row t: sums from t on of what is read there, sums in front of t of what is added there
-            float later = 0.0f, earlier = 0.0f, pairs = 0.0f;
+            float later = 0.0f, earlier = 0.0f, pairs = 0.0f, through = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < W; ++w) {
                 later += sum_in[64 * w + lane];
                 earlier += sum_out[64 * w + lane];
-                pairs += lane > 0 ? sum_pairs[64 * w + lane - 1] : 0.0f;
+                through += sum_through[w];
             }
+            float tile[3];   // pairs (i >= t, j) of whole tiles in front of t - 1's
+#pragma unroll
+            for (int w = 0; w < 4; ++w) pairs += lane > 0 ? sum_pairs[64 * w + lane - 1] : 0.0f;
+#pragma unroll
+            for (int w = 0; w < 3; ++w) tile[w] = row_total[64 * w + lane];
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
                 const float a = __shfl_down(later, d), b = __shfl_up(earlier, d);
                 later += lane + d < 64 ? a : 0.0f;
                 earlier += lane >= d ? b : 0.0f;
+#pragma unroll
+                for (int w = 0; w < 3; ++w) {
+                    const float x = __shfl_down(tile[w], d);
+                    tile[w] += lane + d < 64 ? x : 0.0f;
+                }
             }
             earlier = __shfl_up(earlier, 1);
             if (lane == 0) earlier = 0.0f;
-            const float through = whole * (sum_through[0] + sum_through[1] + sum_through[2] + sum_through[3]);
-            if (lane < rows) p.dgate[(row + lane) * p.Hv + head] = pairs + later + earlier + through;
+#pragma unroll
+            for (int w = 0; w < 3; ++w) pairs += lane > 16 * (w + 1) ? tile[w] : 0.0f;
+            if (lane < rows) p.dgate[(row + lane) * p.Hv + head] = pairs + later + earlier + whole * through;
         }
-        F32x4 dv[4][VT];
-        {
-            frag_t<T> rc[KS][VT];
+        F32x4 dv[4];
 #pragma unroll
-            for (int s = 0; s < KS; ++s)
+        for (int t = 0; t < 4; ++t) dv[t] = F32x4{0, 0, 0, 0};
+        if (has_v) {
 #pragma unroll
-                for (int u = 0; u < VT; ++u) rc[s][u] = rounded<T>(state_col(R, 16 * (VT * wave + u) + l, s, g, p.Dk, p.Dv));
+            for (int s = 0; s < KS; ++s) {
+                const frag_t<T> rc = rounded<T>(state_col<DV>(R, 16 * wave + l, s, g));
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int u = 0; u < VT; ++u) dv[t][u] = F32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const frag_t<T> kf = row_frag<T, LDK>(tk, 16 * t + l, s, g);
-#pragma unroll
-                    for (int u = 0; u < VT; ++u) dv[t][u] = mma(kf, rc[s][u], dv[t][u]);
-                }
-                const F32x4 fo = *reinterpret_cast<const F32x4*>(until + 16 * t + 4 * g);
-#pragma unroll
-                for (int u = 0; u < VT; ++u) dv[t][u] *= fo;
+                for (int t = 0; t < 4; ++t) dv[t] = mma(rc, TK::row_frag(tk, 16 * t + l, s, g), dv[t]);
             }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) dv[t] *= until[16 * t + l];
+        }
+        if (member + 1 < group) {   // the next head's rows on their way
+            fv.fetch(reinterpret_cast<const T*>(p.v) + row * p.stride_v + (long long)(head + 1) * p.Dv, p.stride_v, rows, p.Dv);
+            fd.fetch(reinterpret_cast<const T*>(p.dout) + row * p.stride_o + (long long)(head + 1) * p.Dv, p.stride_o, rows, p.Dv);
         }
         __syncthreads();
+        if (has_v) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            frag_t<T> df[VT];
+            for (int s = 0; s < 2; ++s) {
+                const frag_t<T> df = TV::col_frag(td, s, wave, lane);
 #pragma unroll
-            for (int u = 0; u < VT; ++u) df[u] = col_frag<LDV>(td, s, VT * wave + u, lane);
+                for (int t = 0; t < 4; ++t)
+                    if (s >= t / 2) dv[t] = mma(df, TP::col_frag(tp, s, t, lane), dv[t]);
+            }
+            T* to = reinterpret_cast<T*>(p.dv) + (long long)head * p.Dv;
+            const bool wide = four_wide(to, p.stride_v, p.Dv);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                if (s >= t / 2) {
-                    const frag_t<T> pf = col_frag<LDP>(tp, s, t, lane);
-#pragma unroll
-                    for (int u = 0; u < VT; ++u) dv[t][u] = mma(pf, df[u], dv[t][u]);
-                }
+                const int j = 16 * t + l;
+                if (j < rows && d0 < p.Dv) store_four<T>(to + (row + j) * p.stride_v + d0, dv[t], p.Dv - d0, wide);
             }
         }
-        T* dvp = reinterpret_cast<T*>(p.dv) + (long long)head * p.Dv;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int u = 0; u < VT; ++u) {
-                const int col = 16 * (VT * wave + u) + l;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 16 * t + 4 * g + r;
-                    if (j < rows && col < p.Dv) dvp[(row + j) * p.stride_v + col] = (T)dv[t][u][r];
-                }
-            }
         __syncthreads();   // the next head's tiles come over these
     }
-    T *dqp = reinterpret_cast<T*>(p.dq) + (long long)kh * p.Dk, *dkp = reinterpret_cast<T*>(p.dk) + (long long)kh * p.Dk;
+    if (has_d) {
+        T *to_q = reinterpret_cast<T*>(p.dq) + (long long)kh * p.Dk, *to_k = reinterpret_cast<T*>(p.dk) + (long long)kh * p.Dk;
+        const bool wide_q = four_wide(to_q, p.stride_q, p.Dk), wide_k = four_wide(to_k, p.stride_k, p.Dk);
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int u = 0; u < KD; ++u) {
-            const int col = 16 * (KD * wave + u) + l;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + 4 * g + r;
-                if (i < rows && col < p.Dk) {
-                    dqp[(row + i) * p.stride_q + col] = (T)dq[t][u][r];
-                    dkp[(row + i) * p.stride_k + col] = (T)dk[t][u][r];
-                }
+        for (int t = 0; t < 4; ++t) {
+            const int i = 16 * t + l;
+            if (i < rows && d0 < p.Dk) {
+                store_four<T>(to_q + (row + i) * p.stride_q + d0, dq[t], p.Dk - d0, wide_q);
+                store_four<T>(to_k + (row + i) * p.stride_k + d0, dk[t], p.Dk - d0, wide_k);
             }
         }
+    }
 }
 
-template <typename T, int KD, int VT>
+template <typename T, int DK, int DV>
 hipError_t grad_shape(const MatrecParams& p, hipStream_t stream) {
-    constexpr size_t lds = sizeof(T) * kChunk * (128 * KD + 128 * VT + 64 + 5 * Op<T>::PAD) + 4 * (4 * 64 + 3 * 256 + 4);
-    static_assert(lds <= 160 * 1024, "a workgroup's tiles fit the CU's LDS");
+    using L = GradLds<T, DK, DV>;
     const dim3 grid((unsigned)((long long)p.plan.max_segs * p.plan.per * p.Hk));
     if (grid.x == 0) return hipSuccess;
-    auto kernel = matrec_grad_kernel<T, KD, VT>;
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    auto kernel = matrec_grad_kernel<T, DK, DV>;
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)L::total);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), lds, stream, p);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * L::W), L::total, stream, p);
     return hipGetLastError();
 }
 template <typename T>
 hipError_t grad_type(const MatrecParams& p, hipStream_t stream) {
-    if (p.Dk <= 64) return p.Dv <= 64 ? grad_shape<T, 1, 1>(p, stream) : grad_shape<T, 1, 2>(p, stream);
-    return p.Dv <= 64 ? grad_shape<T, 2, 1>(p, stream) : grad_shape<T, 2, 2>(p, stream);
+    if (p.Dk <= 64) return p.Dv <= 64 ? grad_shape<T, 64, 64>(p, stream) : grad_shape<T, 64, 128>(p, stream);
+    return p.Dv <= 64 ? grad_shape<T, 128, 64>(p, stream) : grad_shape<T, 128, 128>(p, stream);
 }
 
 }  // namespace

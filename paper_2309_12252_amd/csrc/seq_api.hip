@@ -157,8 +157,9 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
         l.off_decay = take((size_t)l.max_segs * c->Hv * 8);
     }
     if (grad) {
-        l.off_chunk = take((size_t)l.chunks * states);
-        l.off_rchunk = take((size_t)l.chunks * states);
+        const size_t tiles = (size_t)c->Hv * (c->Dk <= 64 ? 64 : 128) * (c->Dv <= 64 ? 64 : 128) * 4;
+        l.off_chunk = take((size_t)l.chunks * tiles);
+        l.off_rchunk = take((size_t)l.chunks * tiles);
     }
     l.total = at;
     return l;
