@@ -314,8 +314,8 @@ typedef struct {
     int64_t stride_q, stride_k, stride_v, stride_o;   /* rows (0: Hk Dk, Hk Dk, Hv Dv, Hv Dv); gradients lie like their arrays, dL/do like o */
 } deer_matrec_config;
 
-/* Bytes of device workspace (256-byte aligned) that deer_matrec_solve() (grad = 0) or deer_matrec_grad() (grad = 1) needs.  The gradient keeps two
- * states of a head (rounded up to 64 or 128 rows and columns of floats) for every 64 rows. */
+/* Bytes of device workspace (256-byte aligned) that deer_matrec_solve() (grad = 0) or deer_matrec_grad() (grad = 1) needs: the
+ * states between the segments that long sequences are cut into, and for the gradient dq and dk by heads of v in float32 where several share one. */
 deer_status deer_matrec_workspace_bytes(const deer_matrec_config* cfg, int32_t grad, size_t* bytes);
 
 /* d_q, d_k in [rows, Hk, Dk]   d_v in [rows, Hv, Dv]   d_gate in [rows, Hv] float32, the logarithms of the factors (dense)   d_s0 in [N, Hv, Dk, Dv]

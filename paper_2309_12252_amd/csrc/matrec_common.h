@@ -104,6 +104,8 @@ template <typename T, int C, int THREADS> struct Stage {
     static constexpr int PER = C / 8, N = kChunk * PER / THREADS;
     static_assert(kChunk * PER % THREADS == 0, "every thread has as many units");
     V8 r[N];
+    // BACK: row r of the tile is row rows - 1 - r in memory
+    template <bool BACK = false>
     __device__ __forceinline__ void fetch(const T* from, long long stride, int rows, int cols) {
         const bool wide = cols % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(from) % 16 == 0;
 #pragma unroll
@@ -111,7 +113,7 @@ template <typename T, int C, int THREADS> struct Stage {
             const int at = i * THREADS + threadIdx.x, row = at / PER, c = at % PER * 8;
             r[i] = V8{};
             if (row < rows) {
-                const T* src = from + row * stride + c;
+                const T* src = from + (BACK ? rows - 1 - row : row) * stride + c;
                 if (wide) {
                     if (c < cols) r[i] = *reinterpret_cast<const V8*>(src);
                 } else {
@@ -149,8 +151,8 @@ __device__ __forceinline__ bool four_wide(const T* base, long long stride, int c
     return cols % 4 == 0 && stride % 4 == 0 && reinterpret_cast<uintptr_t>(base) % (4 * sizeof(T)) == 0;
 }
 
-// Running sum of a chunk's log gates, inclusive, lane by lane, of which differences are taken: as the sum of two floats (a sum of 64
-// gates of down to -1e4, 2^-46 of it off).  A gate below -1e4 stands for it: its factor is zero either way.
+// Running sum of a chunk's log gates, inclusive, lane by lane, in units of log 2: as the sum of two floats, of which differences
+// are taken (a sum of 64 gates of down to -1e4, 2^-46 of it off).  A gate below -1e4 stands for it: its factor is zero either way.
 struct Cum {
     float hi, lo;
 };
@@ -162,7 +164,7 @@ __device__ __forceinline__ double shifted(double v) {
     return __longlong_as_double((long long)(((unsigned long long)hi << 32) | lo));
 }
 __device__ __forceinline__ Cum chunk_cum(float g) {
-    double c = g < -1e4f ? -1e4f : g;
+    double c = (g < -1e4f ? -1e4f : g) * 1.4426950408889634;
     c += shifted<0x111, 0xF>(c);   // one, two, four, eight lanes on within rows of 16
     c += shifted<0x112, 0xF>(c);
     c += shifted<0x114, 0xF>(c);
@@ -178,7 +180,8 @@ __device__ __forceinline__ float gate_of(const float* gate, long long stride, in
     const int lane = threadIdx.x & 63;
     return lane < rows ? gate[lane * stride] : 0.0f;
 }
-__device__ __forceinline__ float decay_between(float hi_i, float lo_i, float hi_j, float lo_j) { return expf((hi_i - hi_j) + (lo_i - lo_j)); }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }   // 1 ulp; what is below 2^-126 becomes zero
+__device__ __forceinline__ float decay_between(float hi_i, float lo_i, float hi_j, float lo_j) { return exp2_of((hi_i - hi_j) + (lo_i - lo_j)); }
 
 __device__ __forceinline__ float lane_value(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
 
@@ -207,7 +210,7 @@ __device__ __forceinline__ void lower_tile(int n, int& ti, int& tj) {
 struct MatSegment {
     long long row0;      // first row in the arrays
     long long rows;      // of this segment
-    int seq, chunk0;     // sequence; number of its first chunk among all
+    int seq, chunk0;     // sequence; number of the segment's first chunk among all
     int index, count;    // place among the sequence's segments, and how many there are
 };
 struct MatPlan {
@@ -228,9 +231,15 @@ struct MatrecParams {
     void *o, *dq, *dk, *dv;
     float *last, *dgate, *ds0;
     bool split;                      // several segments a sequence: their states are joined through memory
-    float *seg_state, *seg_rstate;   // [max_segs][Hv][Dk][Dv]: sums, then states in front of (behind) each
-    float *seg_decay;                // [max_segs][Hv]
-    float *chunk_state, *chunk_rstate;   // [chunks][Hv][64 or 128][64 or 128] (the next from Dk, Dv), gradient only
+    // states in memory between kernels are whole tiles of 64 or 128 rows and columns (the next from Dk and Dv), zero outside the head
+    float *seg_state, *seg_rstate;   // [max_segs][Hv][tile]: a segment's own part, then the state in front of it (gradient: behind it)
+    float *seg_decay;                // [2][max_segs][Hv]
+    // gradient only
+    float *part_q, *part_k;          // [rows][Hv][Dk]: dq and dk by heads of v, where several share one
+    float *gate_k;                   // [rows][Hv]: the part of dgate that the run of dk has
+    float *read_in, *put_out;        // [chunks][Hv]: sums of q_i . (...) and k_j . (...) over a chunk
+    float *whole;                    // [chunks][Hv]: the factor of a chunk
+    float *front;                    // [max_segs][Hv]: <state, its gradient> in front of a segment
 };
 struct MatstepParams {
     StepRows rows;
@@ -245,7 +254,7 @@ struct MatstepParams {
 
 hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream);
 hipError_t launch_matrec_out(int dtype, const MatrecParams& p, hipStream_t stream);
-hipError_t launch_matrec_states(int dtype, const MatrecParams& p, hipStream_t stream);
+hipError_t launch_matrec_join(int dtype, const MatrecParams& p, bool both, hipStream_t stream);   // states in front of the segments (both: behind them too)
 hipError_t launch_matrec_grad(int dtype, const MatrecParams& p, hipStream_t stream);
 hipError_t launch_matstep(int dtype, const MatstepParams& p, hipStream_t stream);
 

@@ -127,7 +127,7 @@ struct MatLayout {
     long long chunks, max_segs;   // at most
     int per;
     bool split;
-    size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_chunk, off_rchunk, total;
+    size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_part_q, off_part_k, off_gate, off_read, off_put, off_whole, off_front, total;
 };
 MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
     MatLayout l{};
@@ -135,14 +135,18 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
     l.chunks = c->packed ? longest + c->N : longest * c->N;
     long long per = longest < 1 ? 1 : longest;
     if (c->packed || (long long)c->N * c->Hv < 256) {
-        const long long want = l.chunks * c->Hv / 512;
+        // 256 workgroups run at a time; every sequence's last segment is a short one, half of the others' length on average
+        long long segs = 256 / c->Hv - (c->packed ? c->N / 2 : 0);
+        if (segs < 1) segs = 1;
+        const long long want = ((c->packed ? longest : l.chunks) + segs - 1) / segs;
         per = want < 4 ? 4 : want;
         if (per > longest) per = longest < 1 ? 1 : longest;
     }
+    if (grad && per > 32) per = 32;   // what goes through the chunks of a segment (matrec_grad.hip) takes the rounding errors of all of them
     l.per = (int)per;
     l.split = per < longest;
     l.max_segs = c->packed ? l.chunks / per + c->N : (longest + per - 1) / per * c->N;
-    const size_t states = (size_t)c->Hv * c->Dk * c->Dv * 4;
+    const size_t states = (size_t)c->Hv * (c->Dk <= 64 ? 64 : 128) * (c->Dv <= 64 ? 64 : 128) * 4;
     size_t at = kAlign;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -157,9 +161,16 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
         l.off_decay = take((size_t)l.max_segs * c->Hv * 8);
     }
     if (grad) {
-        const size_t tiles = (size_t)c->Hv * (c->Dk <= 64 ? 64 : 128) * (c->Dv <= 64 ? 64 : 128) * 4;
-        l.off_chunk = take((size_t)l.chunks * tiles);
-        l.off_rchunk = take((size_t)l.chunks * tiles);
+        const size_t rows = (size_t)c->T * (c->packed ? 1 : c->N), by_head = (size_t)c->Hv * 4;
+        if (c->Hv != c->Hk) {
+            l.off_part_q = take(rows * by_head * c->Dk);
+            l.off_part_k = take(rows * by_head * c->Dk);
+        }
+        l.off_gate = take(rows * by_head);
+        l.off_read = take((size_t)l.chunks * by_head);
+        l.off_put = take((size_t)l.chunks * by_head);
+        l.off_whole = take((size_t)l.chunks * by_head);
+        l.off_front = take((size_t)l.max_segs * by_head);
     }
     l.total = at;
     return l;
@@ -199,8 +210,15 @@ MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool gr
         p.seg_decay = reinterpret_cast<float*>(ws + l.off_decay);
     }
     if (grad) {
-        p.chunk_state = reinterpret_cast<float*>(ws + l.off_chunk);
-        p.chunk_rstate = reinterpret_cast<float*>(ws + l.off_rchunk);
+        if (c->Hv != c->Hk) {
+            p.part_q = reinterpret_cast<float*>(ws + l.off_part_q);
+            p.part_k = reinterpret_cast<float*>(ws + l.off_part_k);
+        }
+        p.gate_k = reinterpret_cast<float*>(ws + l.off_gate);
+        p.read_in = reinterpret_cast<float*>(ws + l.off_read);
+        p.put_out = reinterpret_cast<float*>(ws + l.off_put);
+        p.whole = reinterpret_cast<float*>(ws + l.off_whole);
+        p.front = reinterpret_cast<float*>(ws + l.off_front);
     }
     return p;
 }
@@ -369,7 +387,7 @@ deer_status deer_matrec_grad(const deer_matrec_config* c, const void* d_q, const
     p.ds0 = d_ds0;
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     hipError_t err = launch_matrec_plan(p, stream);
-    if (err == hipSuccess) err = launch_matrec_states(c->dtype, p, stream);
+    if (err == hipSuccess) err = launch_matrec_join(c->dtype, p, true, stream);
     if (err == hipSuccess) err = launch_matrec_grad(c->dtype, p, stream);
     return launched("deer_matrec_grad", err);
 }

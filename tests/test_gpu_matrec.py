@@ -34,7 +34,7 @@ def both(d, **more):
 def compare(d, got, seqs, dtype, scale):
     flat = {n: host(t).reshape((-1,) + t.shape[-2:] if n != "g" else (-1, t.shape[-1])) for n, t in d.items() if n not in ("s0", "dlast")}
     s0, dlast = host(d["s0"]), host(d["dlast"])
-    want, absolute = so.matrix(flat["q"], flat["k"], flat["v"], flat["g"], s0, seqs, scale, flat["do"], dlast)
+    want, absolute, passing = so.matrix(flat["q"], flat["k"], flat["v"], flat["g"], s0, seqs, scale, flat["do"], dlast)
     alive = np.zeros(flat["g"].shape[0], dtype=bool)
     for r0, n in seqs:
         alive[r0:r0 + n] = True
@@ -46,7 +46,7 @@ def compare(d, got, seqs, dtype, scale):
             continue
         g2[n] = t.reshape((alive.size,) + want[n].shape[1:])[at]
         want[n], absolute[n] = want[n][alive], absolute[n][alive]
-    so.check_matrix(g2, want, absolute, dtype, max(n for _, n in seqs))
+    so.check_matrix(g2, want, absolute, passing[alive], dtype, max(n for _, n in seqs))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -217,7 +217,7 @@ def test_step(dtype, N, Hk, Hv, Dk, Dv):
     slots = torch.randperm(N + 3)[:N].to(torch.int32)
     before = state.clone()
     o = deer.matrec_step(d["q"], d["k"], d["v"], d["g"], state, slots=slots.to(DEV))
-    want, absolute = so.matrix(host(d["q"]), host(d["k"]), host(d["v"]), host(d["g"]), host(before)[slots.numpy()], [(n, 1) for n in range(N)], Dk ** -0.5)
+    want, absolute, _ = so.matrix(host(d["q"]), host(d["k"]), host(d["v"]), host(d["g"]), host(before)[slots.numpy()], [(n, 1) for n in range(N)], Dk ** -0.5)
     # fp32 throughout: factor, two products, a sum; then the sum over Dk columns
     so.check("state", state[slots.long().to(DEV)], want["last"], 6 * 2.0 ** -24 * absolute["last"], "f32")
     so.check("o", o, want["o"], (Dk + 8) * 2.0 ** -24 * absolute["o"], dtype)
