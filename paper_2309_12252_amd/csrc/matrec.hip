@@ -70,20 +70,20 @@ __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p)
 
 // ---- states ----
 // A segment's own part of the state, and its decay, into seg_state (REV: of the gradient of the state in front of it, into seg_rstate: rows backwards,
-// (k, v) = (scale q, dout), R <- e^{c_64} R + sum_i e^{c_i} scale q_i dout_i^T).  Wavefront w keeps columns 16 w .. of v, transposed: a lane has
-// four neighbouring v of every 16th d, so that states go to memory 16 bytes a lane.  One barrier a chunk, as in matrec_run.
+// (k, v) = (scale q, dout), R <- e^{c_64} R + sum_i e^{c_i} scale q_i dout_i^T).  Wavefront w keeps a quarter of v's columns, transposed: a lane has
+// four neighbouring v of one d in 16, so that states go to memory 16 bytes a lane.  The update and its cost are matrec_run's.
+constexpr int kStateWaves = 4;
 template <typename T, int DK, int DV>
 struct StatesLds {
-    static constexpr int BUF = sizeof(T) == 2 ? 2 : 1;
-    static constexpr size_t k = 0, v = Tile<T, DK>::bytes, w = v + Tile<T, DV>::bytes, one = w + 4 * 64, total = BUF * one;
+    static constexpr size_t k = 0, v = Tile<T, DK>::bytes, w = v + Tile<T, DV>::bytes, total = w + 4 * 68;
 };
 template <typename T, int DK, int DV, bool REV>
 __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* lds) {
-    constexpr int W = DV / 16, NT = DK / 16, P = Op<T>::PIECES;
+    constexpr int W = kStateWaves, VT = DV / (16 * W), NT = DK / 16, P = Op<T>::PIECES;
     using L = StatesLds<T, DK, DV>;
     using TK = Tile<T, DK>;
     using TV = Tile<T, DV>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15, n0 = VT * wave;
     const int seg_no = blockIdx.x / p.Hv, head = blockIdx.x % p.Hv, kh = head / (p.Hv / p.Hk);
     if (seg_no >= *p.plan.count) return;
     const MatSegment seg = p.plan.segs[seg_no];
@@ -92,69 +92,73 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
     const T* k = reinterpret_cast<const T*>(REV ? p.q : p.k) + (long long)kh * p.Dk + seg.row0 * stride_k;
     const T* v = reinterpret_cast<const T*>(REV ? p.dout : p.v) + (long long)head * p.Dv + seg.row0 * stride_v;
     const float* gate = p.gate + seg.row0 * p.Hv + head;
-    F32x4 S[NT];
+    const bool wide_k = wide_rows(k, stride_k, p.Dk), wide_v = wide_rows(v, stride_v, p.Dv);
+    T *tk = reinterpret_cast<T*>(lds + L::k), *tv = reinterpret_cast<T*>(lds + L::v);
+    float* weight = reinterpret_cast<float*>(lds + L::w);
+    F32x4 S[NT][VT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) S[t] = F32x4{0, 0, 0, 0};
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int u = 0; u < VT; ++u) S[t][u] = F32x4{0, 0, 0, 0};
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
     double total = 0.0;
     Stage<T, DK, 64 * W> fk;
     Stage<T, DV, 64 * W> fv;
-    float fg = 0.0f, end_hi = 0.0f, end_lo = 0.0f;
+    float fg = 0.0f;
     auto fetch = [&](int i) {
         const long long row = (long long)(REV ? chunks - 1 - i : i) * kChunk;
         const int rows = seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
-        fk.fetch(k + row * stride_k, stride_k, rows, p.Dk);
-        fv.fetch(v + row * stride_v, stride_v, rows, p.Dv);
-        fg = gate_of(gate + row * p.Hv, p.Hv, rows);
-    };
-    auto put = [&](int i) {
-        unsigned char* at = lds + (L::BUF == 2 ? (i & 1) * L::one : 0);
-        fk.put(reinterpret_cast<T*>(at + L::k));
-        fv.put(reinterpret_cast<T*>(at + L::v));
-        const Cum cum = chunk_cum(fg);
-        end_hi = lane_value(cum.hi, 63);
-        end_lo = lane_value(cum.lo, 63);
-        if (wave == 0) reinterpret_cast<float*>(at + L::w)[lane] = REV ? p.scale * exp2_of(cum.hi + cum.lo) : decay_between(end_hi, end_lo, cum.hi, cum.lo);
+        fk.fetch(k + row * stride_k, stride_k, rows, p.Dk, wide_k);
+        fv.fetch(v + row * stride_v, stride_v, rows, p.Dv, wide_v);
+        if (wave == W - 1) fg = gate_of(gate + row * p.Hv, p.Hv, rows);
     };
     fetch(0);
-    put(0);
-    __syncthreads();
     for (int i = 0; i < chunks; ++i) {
-        const unsigned char* at = lds + (L::BUF == 2 ? (i & 1) * L::one : 0);
-        const T *tk = reinterpret_cast<const T*>(at + L::k), *tv = reinterpret_cast<const T*>(at + L::v);
-        const float* weight = reinterpret_cast<const float*>(at + L::w);
-        const bool more = i + 1 < chunks;
-        if (more) fetch(i + 1);
-        const float whole = exp2_of(end_hi + end_lo);
-        total += (double)end_hi + (double)end_lo;
+        fk.put(tk);
+        fv.put(tv);
+        if (wave == W - 1) {
+            const Cum cum = chunk_cum(fg);
+            const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63);
+            weight[lane] = REV ? p.scale * exp2_of(cum.hi + cum.lo) : decay_between(end_hi, end_lo, cum.hi, cum.lo);
+            if (lane == 0) weight[64] = exp2_of(end_hi + end_lo);
+            total += (double)end_hi + (double)end_lo;
+        }
+        __syncthreads();
+        if (i + 1 < chunks) fetch(i + 1);
+        const float whole = weight[64];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) S[t] *= whole;
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int u = 0; u < VT; ++u) S[t][u] *= whole;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const F32x4 w0 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 4 * g), w1 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 16 + 4 * g);
-            frag_t<T> vp[P];
-            pieces_of<T>(widened(TV::col_frag(tv, s, wave, lane)) * joined(w0, w1), vp);
+            const F32x4 w0 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 8 * g), w1 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 8 * g + 4);
+            frag_t<T> vp[VT][P];
+#pragma unroll
+            for (int u = 0; u < VT; ++u) pieces_of<T>(widened(TV::col_frag(tv, s, n0 + u, lane)) * joined(w0, w1), vp[u]);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const frag_t<T> kf = TK::col_frag(tk, s, t, lane);
 #pragma unroll
-                for (int q = P - 1; q >= 0; --q) S[t] = mma(vp[q], kf, S[t]);
+                for (int q = P - 1; q >= 0; --q)
+#pragma unroll
+                    for (int u = 0; u < VT; ++u) S[t][u] = mma(vp[u][q], kf, S[t][u]);
             }
         }
-        if (L::BUF == 1) __syncthreads();
-        if (more) put(i + 1);
         __syncthreads();
     }
     const long long at = (long long)seg_no * p.Hv + head;
-    float* to = (REV ? p.seg_rstate : p.seg_state) + at * (DK * DV) + l * DV + 16 * wave + 4 * g;   // (outside the head: zero in S too)
+    float* to = (REV ? p.seg_rstate : p.seg_state) + at * (DK * DV);   // (outside the head: zero in S too)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) *reinterpret_cast<F32x4*>(to + 16 * t * DV) = S[t];
-    if (threadIdx.x == 0) p.seg_decay[(REV ? (long long)p.plan.max_segs * p.Hv : 0) + at] = (float)exp2(total);
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int u = 0; u < VT; ++u) *reinterpret_cast<F32x4*>(to + column_of(t, l) * DV + column_of(n0 + u, 4 * g)) = S[t][u];
+    if (threadIdx.x == 64 * (W - 1)) p.seg_decay[(REV ? (long long)p.plan.max_segs * p.Hv : 0) + at] = (float)exp2(total);
 }
 
 // blockIdx.y: 0 the states, 1 their gradients
 template <typename T, int DK, int DV>
-__global__ __launch_bounds__(4 * DV) void matrec_states_kernel(const MatrecParams p) {
+__global__ __launch_bounds__(64 * kStateWaves, 2) void matrec_states_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     if (blockIdx.y == 0) states_of<T, DK, DV, false>(p, lds);
     else states_of<T, DK, DV, true>(p, lds);
@@ -207,10 +211,11 @@ __global__ __launch_bounds__(256) void matrec_join_kernel(const MatrecParams p) 
     else join_cell<DK, DV, true>(p, n, head, cell);
 }
 
+template <int DK, int DV> constexpr int out_waves() { return DV == 128 ? 8 : 4; }
 template <typename T, int DK, int DV>
-__global__ __launch_bounds__(4 * DV, sizeof(T) == 2 ? 2 : 1) void matrec_out_kernel(const MatrecParams p) {
+__global__ __launch_bounds__(DV == 128 ? 512 : 256, sizeof(T) == 2 ? 2 : 1) void matrec_out_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    matrec_run<T, DK, DV, DV / 16, RUN_OUT>(p, lds);
+    matrec_run<T, DK, DV, out_waves<DK, DV>(), RUN_OUT>(p, lds);
 }
 
 // ---- one token ----
@@ -270,7 +275,7 @@ template <typename T, int DK, int DV>
 hipError_t join_shape(const MatrecParams& p, bool both, hipStream_t stream) {
     hipError_t e = hipSuccess;
     const unsigned y = both ? 2 : 1;
-    if (p.split) e = launch_lds(matrec_states_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), y), 4 * DV, StatesLds<T, DK, DV>::total, p, stream);
+    if (p.split) e = launch_lds(matrec_states_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), y), 64 * kStateWaves, StatesLds<T, DK, DV>::total, p, stream);
     if (e != hipSuccess || !(p.split || p.rows.bounds || p.rows.T == 0)) return e;
     hipLaunchKernelGGL((matrec_join_kernel<DK, DV>), dim3((unsigned)((long long)p.rows.N * p.Hv * (DK * DV / 256)), y), dim3(256), 0, stream, p);
     return hipGetLastError();
@@ -279,7 +284,7 @@ template <typename T, int DK, int DV>
 hipError_t out_shape(const MatrecParams& p, hipStream_t stream) {
     const hipError_t e = join_shape<T, DK, DV>(p, false, stream);
     if (e != hipSuccess) return e;
-    return launch_lds(matrec_out_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv)), 4 * DV, RunLds<T, DK, DV, DV / 16, RUN_OUT>::total, p, stream);
+    return launch_lds(matrec_out_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv)), 64 * out_waves<DK, DV>(), RunLds<T, DK, DV, out_waves<DK, DV>(), RUN_OUT>::total, p, stream);
 }
 
 }  // namespace

@@ -1,12 +1,10 @@
 // Building blocks of the matrix-state recurrence (matrec.hip, matrec_grad.hip): tiles of 64 rows in LDS, operands of the matrix
 // instructions, decays of a chunk.
 //
-// A chunk has 64 rows.  Matrix products are 16 x 16 x 32 tiles; the order of the 32 terms of a contraction is the same for both
-// operands and otherwise free.  Everywhere it is
-//     element e of lane group g (lanes 16 g .. 16 g + 15) is term 4 g + e for e < 4, 16 + 4 g + e - 4 for e >= 4,
-// which is how the accumulators of two neighbouring 16 x 16 tiles hold their rows: a state kept in accumulators is an operand of
-// the next product without leaving its registers.  Tiles in LDS keep every 32 columns in that order too, so that a lane's eight
-// terms of a row are 16 contiguous bytes (bf16).
+// A chunk has 64 rows.  Matrix products are 16 x 16 x 32 tiles: operand A has rows lane % 16, operand B columns lane % 16, and lane group g (lanes 16 g ..
+// 16 g + 15) of both has the terms 8 g .. 8 g + 7 of the 32; a result has rows 4 g .. 4 g + 3 of column lane % 16.  A state kept as results is to be
+// an operand of the next product without leaving its registers: so the columns of an array are dealt out to tiles of 16 in such an order, column_of(), that
+// the results of two neighbouring tiles hold, in lane group g, the columns 8 g .. 8 g + 7 of their 32.
 #pragma once
 #include "seq_common.h"
 
@@ -62,61 +60,78 @@ __device__ __forceinline__ F32x8 widened(BF16x8 x) { return __builtin_convertvec
 __device__ __forceinline__ F32x8 widened(F32x8 x) { return x; }
 __device__ __forceinline__ F32x8 joined(F32x4 a, F32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// A tile of 64 rows and C (64 or 128) columns in LDS.  A block of 32 columns lies in the order of the terms: a lane group's eight terms are
-// one unit.  bf16: units of 16 bytes, their place in the row turned by the row so that neither 16 rows of one unit (row_frag) nor
-// four units of four rows (col_frag) meet in a bank.  fp32: rows 16 bytes apart in the banks.
+// column (or row, of a state) that place i of tile n has
+__device__ __forceinline__ int column_of(int n, int i) { return 32 * (n >> 1) + 8 * (i >> 2) + 4 * (n & 1) + (i & 3); }
+
+// A tile of 64 rows and C (64 or 128) columns in LDS, in units of eight columns.  bf16: the units' places in a row are turned by the row so that neither
+// 16 rows of one unit (row_frag) nor four half units of four rows (col_frag) meet in a bank.  fp32: rows 16 bytes apart in the banks.
 template <typename T, int C> struct Tile {
     static constexpr int LD = sizeof(T) == 2 ? C : C + 4;
     static constexpr size_t bytes = sizeof(T) * kChunk * LD;
-    static __device__ __forceinline__ int turn(int row) { return C == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (row >> 1) & 7; }
-    // columns c .. c + 3, c a multiple of four
-    static __device__ __forceinline__ int four(int row, int c) {
-        const int unit = (c >> 5) * 4 + ((c >> 2) & 3), half = (c >> 4) & 1;
-        if constexpr (sizeof(T) == 2) return row * LD + ((unit ^ turn(row)) << 3) + half * 4;
-        else return row * LD + unit * 8 + half * 4;
+    static __device__ __forceinline__ int turn(int row) { return C == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : ((row & 2) << 1) | ((row >> 2) & 3); }
+    // column c of a row (the next three, or seven, behind it where c is a multiple of four, or eight)
+    static __device__ __forceinline__ int at(int row, int c) {
+        if constexpr (sizeof(T) == 2) return row * LD + (((c >> 3) ^ turn(row)) << 3) + (c & 7);
+        else return row * LD + c;
     }
     // rows `row` (this lane's), terms of the block of 32 columns s
-    static __device__ __forceinline__ frag_t<T> row_frag(const T* t, int row, int s, int g) { return *reinterpret_cast<const frag_t<T>*>(t + four(row, 32 * s + 4 * g)); }
-    // column 16 n + lane % 16, terms of the block of 32 rows s: the transposed operand
+    static __device__ __forceinline__ frag_t<T> row_frag(const T* t, int row, int s, int g) { return *reinterpret_cast<const frag_t<T>*>(t + at(row, 32 * s + 8 * g)); }
+    // columns column_of(n, lane % 16), terms of the block of 32 rows s: the transposed operand
     static __device__ __forceinline__ frag_t<T> col_frag(const T* t, int s, int n, int lane) {
         const int g = lane >> 4, l = lane & 15;
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) I16x4* LdsPtr;
             // a group of 16 lanes hands in four rows of 16 columns, four columns a lane; lane l gets column l of them
-            const BF16* at = t + four(32 * s + 4 * g + (l >> 2), 16 * n + 4 * (l & 3));
-            const I16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at);
-            const I16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + 16 * LD));   // (turn() is the same 16 rows on)
+            const int row = 32 * s + 8 * g + (l >> 2), c = 32 * (n >> 1) + 8 * (l & 3) + 4 * (n & 1);
+            const I16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(t + at(row, c)));
+            const I16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(t + at(row + 4, c)));
             return __builtin_bit_cast(BF16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const float* at = t + four(32 * s + 4 * g, 16 * n + (l & 12)) + (l & 3);
+            const float* from = t + (32 * s + 8 * g) * LD + column_of(n, l);
             F32x8 f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = at[((e & 3) + (e >= 4 ? 16 : 0)) * LD];
+            for (int e = 0; e < 8; ++e) f[e] = from[e * LD];
             return f;
         }
     }
 };
 
 // 64 rows of `cols` columns on their way from memory into a tile: fetched into registers, put into LDS later.  What is not there is zero.
+// `wide`: every row is aligned to 16 bytes and a multiple of eight columns (wide_rows()): then by buffer loads, whose bounds make the zeros.
+template <typename T>
+__device__ __forceinline__ bool wide_rows(const T* base, long long stride, int cols) {
+    return cols % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(base) % 16 == 0 && stride < (1 << 20);
+}
 template <typename T, int C, int THREADS> struct Stage {
     using V8 = T __attribute__((ext_vector_type(8)));
-    using V4 = T __attribute__((ext_vector_type(4)));
-    static constexpr int PER = C / 8, N = kChunk * PER / THREADS;
-    static_assert(kChunk * PER % THREADS == 0, "every thread has as many units");
+    using U4 = unsigned __attribute__((ext_vector_type(4)));
+    static constexpr int PER = C / 8, N = kChunk * PER / THREADS, STEP = THREADS / PER;   // units of a row, units of a thread, rows between them
+    static_assert(kChunk * PER % THREADS == 0 && THREADS % PER == 0, "every thread has as many units, all of the same columns");
     V8 r[N];
     // BACK: row r of the tile is row rows - 1 - r in memory
     template <bool BACK = false>
-    __device__ __forceinline__ void fetch(const T* from, long long stride, int rows, int cols) {
-        const bool wide = cols % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(from) % 16 == 0;
+    __device__ __forceinline__ void fetch(const T* from, long long stride, int rows, int cols, bool wide) {
+        const int row0 = threadIdx.x / PER, c = threadIdx.x % PER * 8;
+        if (wide) {
+            const int pitch = (int)stride * (int)sizeof(T);
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, rows * pitch, 0x00020000);
+            // (a row in front of the first is far behind the end as an unsigned offset)
+            const int at = c < cols ? (BACK ? rows - 1 - row0 : row0) * pitch + c * (int)sizeof(T) : 0x60000000;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = i * THREADS + threadIdx.x, row = at / PER, c = at % PER * 8;
-            r[i] = V8{};
-            if (row < rows) {
-                const T* src = from + (BACK ? rows - 1 - row : row) * stride + c;
-                if (wide) {
-                    if (c < cols) r[i] = *reinterpret_cast<const V8*>(src);
-                } else {
+            for (int i = 0; i < N; ++i) {
+                U4 u[sizeof(T) / 2];
+#pragma unroll
+                for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+                    u[h] = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + (BACK ? -i : i) * STEP * pitch + 16 * h, 0, 0));
+                r[i] = __builtin_bit_cast(V8, u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int row = row0 + i * STEP;
+                r[i] = V8{};
+                if (row < rows) {
+                    const T* src = from + (BACK ? rows - 1 - row : row) * stride + c;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         if (c + e < cols) r[i][e] = src[e];
@@ -125,12 +140,9 @@ template <typename T, int C, int THREADS> struct Stage {
         }
     }
     __device__ __forceinline__ void put(T* tile) const {
+        const int row0 = threadIdx.x / PER, c = threadIdx.x % PER * 8;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = i * THREADS + threadIdx.x, row = at / PER, c = at % PER * 8;
-            *reinterpret_cast<V4*>(tile + Tile<T, C>::four(row, c)) = __builtin_shufflevector(r[i], r[i], 0, 1, 2, 3);
-            *reinterpret_cast<V4*>(tile + Tile<T, C>::four(row, c + 4)) = __builtin_shufflevector(r[i], r[i], 4, 5, 6, 7);
-        }
+        for (int i = 0; i < N; ++i) *reinterpret_cast<V8*>(tile + Tile<T, C>::at(row0 + i * STEP, c)) = r[i];
     }
 };
 

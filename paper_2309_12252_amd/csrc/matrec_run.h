@@ -5,11 +5,10 @@
 //   Dq   a, b, c = dout, v, k      M = S^T   the same
 //   Dk   a, b, c = v, dout, q      M = R^T   rows and chunks backwards: c_i stands for -c_i, f_i = e^{c_64 - c_i}, w_j = scale e^{c_j}
 //   Dv   a, b, c = k, q, dout      M = R     backwards, the same
-// (S the state in front of a chunk, R the gradient of the state behind it.)  Wavefront w has columns 16 w .. of c: M's, as accumulators, which are
-// operands of M^T a as they stand, and the outputs', transposed, a lane four neighbouring columns of a row.
-// What bounds it: 60 to 110 matrix instructions of 16 cycles and some 500 vector instructions a wavefront and chunk, 64 KiB of rows a chunk and head
-// of 128 columns.  Eight wavefronts at 256 registers fill a CU; so a chunk has one barrier only (two buffers of tiles) and the next
-// one's rows are on their way to registers while it is computed.
+// (S the state in front of a chunk, R the gradient of the state behind it.)  Wavefront w has a quarter of c's columns, one or two tiles of 16: M's, as
+// results, which are operands of M^T a as they stand, and the outputs', transposed, a lane four or eight neighbouring columns of a row.
+// What bounds it: 120 to 210 matrix instructions of 16 cycles and some 500 vector instructions a wavefront and chunk of 128 columns, which a SIMD does one
+// after another, and 64 KiB of rows a chunk.  The next chunk's rows are on their way to registers while this one is computed.
 #pragma once
 #include "matrec_common.h"
 
@@ -22,13 +21,12 @@ template <typename T, int D1, int D2, int W, int MODE>
 struct RunLds {
     static constexpr bool FOUR = MODE == RUN_DQ;        // q, for the gates
     static constexpr bool SUMS = MODE == RUN_DQ || MODE == RUN_DK;
-    static constexpr int BUF = sizeof(T) == 2 && !(W == 4 && D1 == 128) ? 2 : 1;
     static constexpr size_t a = 0, b = Tile<T, D1>::bytes, c = b + Tile<T, D1>::bytes, q = c + Tile<T, D2>::bytes, pairs = q + (FOUR ? Tile<T, D2>::bytes : 0),
-                            rows = pairs + Tile<T, kChunk>::bytes,       // cum_hi, cum_lo, f, w
-                            dots = rows + 4 * 4 * 64,                    // [W][64]
-                            by_col = dots + (SUMS ? 4 * 64 * W : 0),     // [row tile][64]
+                            rows = pairs + Tile<T, kChunk>::bytes,       // cum_hi, cum_lo, f, w, and the chunk's factor
+                            dots = rows + 4 * (4 * 64 + 4),              // [W][64]
+                            by_col = dots + (SUMS ? 4 * 64 * W : 0),   // [row tile][64]
                             by_row = by_col + (FOUR ? 4 * 256 : 0),      // [column tile][64]
-                            one = by_row + (FOUR ? 4 * 256 : 0), total = BUF * one;
+                            total = by_row + (FOUR ? 4 * 256 : 0);
     static_assert(total <= 160 * 1024, "a workgroup's tiles fit the CU's LDS");
 };
 
@@ -42,7 +40,7 @@ struct StateAt {
 template <typename T, int DK, int DV, int W, int MODE>
 __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char* lds) {
     constexpr bool BACK = MODE == RUN_DK || MODE == RUN_DV, KEYS = MODE == RUN_DQ || MODE == RUN_DK;   // KEYS: D1 is the values', D2 the keys'
-    constexpr int D1 = KEYS ? DV : DK, D2 = KEYS ? DK : DV, KS = D1 / 32, NT = D1 / 16, P = Op<T>::PIECES;
+    constexpr int D1 = KEYS ? DV : DK, D2 = KEYS ? DK : DV, KS = D1 / 32, NT = D1 / 16, VT = D2 / (16 * W) > 0 ? D2 / (16 * W) : 1, P = Op<T>::PIECES;
     using L = RunLds<T, D1, D2, W, MODE>;
     using T1 = Tile<T, D1>;
     using T2 = Tile<T, D2>;
@@ -52,8 +50,9 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     const int seg_no = blockIdx.x / p.Hv, head = blockIdx.x % p.Hv, kh = head / (p.Hv / p.Hk);
     if (seg_no >= *p.plan.count) return;
     const MatSegment seg = p.plan.segs[seg_no];
-    const bool strip = 16 * wave < D2;        // this wavefront has columns
-    const int d1 = KEYS ? p.Dv : p.Dk, d2 = KEYS ? p.Dk : p.Dv, col0 = 16 * wave + 4 * g;
+    const int d1 = KEYS ? p.Dv : p.Dk, d2 = KEYS ? p.Dk : p.Dv, n0 = VT * wave;   // this wavefront's first tile of columns
+    const bool strip = 16 * n0 < D2;                                             // (it has some)
+    const int col0 = column_of(n0, 4 * g);                                       // a lane's first column of 4 VT
 
     // ---- arrays of rows ----
     const T* q = reinterpret_cast<const T*>(p.q) + (long long)kh * p.Dk + seg.row0 * p.stride_q;
@@ -72,14 +71,14 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     const long long so = MODE == RUN_OUT ? p.stride_o : MODE == RUN_DV ? p.stride_v : MODE == RUN_DQ ? p.stride_q : p.stride_k;
     out += seg.row0 * so;
     float* out_part = parts ? (MODE == RUN_DQ ? p.part_q : p.part_k) + (seg.row0 * p.Hv + head) * p.Dk : nullptr;
-    const bool wide_out = parts ? p.Dk % 4 == 0 : four_wide(out, so, d2);
+    const bool wide_out = parts ? p.Dk % 4 == 0 : four_wide(out, so, d2), wide_out8 = wide_rows(out, so, d2);
     const float* gate = p.gate + seg.row0 * p.Hv + head;
 
     // ---- the state ----
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
     const bool first = seg.index == 0, last = seg.index == seg.count - 1;
     const long long cells = (long long)p.Dk * p.Dv, of_seq = ((long long)seg.seq * p.Hv + head) * cells, of_seg = ((long long)seg_no * p.Hv + head) * (DK * DV);
-    F32x4 M[NT];
+    F32x4 M[NT][VT];
     {
         const bool given = BACK ? last : first;
         const StateAt st = given ? StateAt{BACK ? (p.dlast ? p.dlast + of_seq : nullptr) : (p.s0 ? p.s0 + of_seq : nullptr), p.Dk, p.Dv, p.Dv}
@@ -87,14 +86,22 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) M[t][r] = !strip ? 0.0f : KEYS ? st(16 * wave + l, 16 * t + 4 * g + r) : st(16 * t + 4 * g + r, 16 * wave + l);
+            for (int u = 0; u < VT; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int x = column_of(t, 4 * g + r), y = column_of(n0 + u, l);
+                    M[t][u][r] = KEYS ? st(y, x) : st(x, y);
+                }
     }
     // the state behind the run's last chunk is wanted: the final one, or what the gates and ds0 need
     const bool to_the_end = MODE == RUN_OUT ? last && p.last : MODE == RUN_DK;
+    // pieces that rows enter the state as: all where it is handed out or sums are taken of it as it is, two where it is rounded itself
+    const int pieces = to_the_end || L::SUMS || P == 1 ? P : 2;
 
     // ---- a chunk's rows: fetched into registers, put into LDS ----
     Stage<T, D1, 64 * W> fa, fb;
     Stage<T, D2, 64 * W> fc, fq;
+    const bool wide_a = wide_rows(ra, sa, d1), wide_b = wide_rows(rb, sb, d1), wide_c = wide_rows(rc, sc, d2), wide_q = wide_rows(q, p.stride_q, p.Dk);
     float fg = 0.0f;
     auto rows_of = [&](int c, long long& row) {
         row = (long long)(BACK ? chunks - 1 - c : c) * kChunk;
@@ -103,57 +110,49 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     auto fetch = [&](int c) {
         long long row;
         const int rows = rows_of(c, row);
-        fa.template fetch<BACK>(ra + row * sa, sa, rows, d1);
-        fb.template fetch<BACK>(rb + row * sb, sb, rows, d1);
-        fc.template fetch<BACK>(rc + row * sc, sc, rows, d2);
-        if constexpr (L::FOUR) fq.template fetch<BACK>(q + row * p.stride_q, p.stride_q, rows, d2);
-        fg = gate_of(gate + row * p.Hv, p.Hv, rows);
+        fa.template fetch<BACK>(ra + row * sa, sa, rows, d1, wide_a);
+        fb.template fetch<BACK>(rb + row * sb, sb, rows, d1, wide_b);
+        fc.template fetch<BACK>(rc + row * sc, sc, rows, d2, wide_c);
+        if constexpr (L::FOUR) fq.template fetch<BACK>(q + row * p.stride_q, p.stride_q, rows, d2, wide_q);
+        if (wave == W - 1) fg = gate_of(gate + row * p.Hv, p.Hv, rows);
     };
-    float end_hi = 0.0f, end_lo = 0.0f;   // the gates' sum of the chunk that was put last
+    T *ta = reinterpret_cast<T*>(lds + L::a), *tb = reinterpret_cast<T*>(lds + L::b), *tc = reinterpret_cast<T*>(lds + L::c), *tq = reinterpret_cast<T*>(lds + L::q),
+      *tp = reinterpret_cast<T*>(lds + L::pairs);
+    float *cum_hi = reinterpret_cast<float*>(lds + L::rows), *cum_lo = cum_hi + 64, *f_out = cum_hi + 128, *w_in = cum_hi + 192;
+    float *dots = reinterpret_cast<float*>(lds + L::dots), *by_col = reinterpret_cast<float*>(lds + L::by_col), *by_row = reinterpret_cast<float*>(lds + L::by_row);
     auto put = [&](int c) {
-        unsigned char* at = lds + (L::BUF == 2 ? (c & 1) * L::one : 0);
-        long long row;
-        const int rows = rows_of(c, row);
-        const Cum cum = chunk_cum(fg);
-        end_hi = lane_value(cum.hi, 63);
-        end_lo = lane_value(cum.lo, 63);
-        fa.put(reinterpret_cast<T*>(at + L::a));
-        fb.put(reinterpret_cast<T*>(at + L::b));
-        fc.put(reinterpret_cast<T*>(at + L::c));
-        if constexpr (L::FOUR) fq.put(reinterpret_cast<T*>(at + L::q));
+        fa.put(ta);
+        fb.put(tb);
+        fc.put(tc);
+        if constexpr (L::FOUR) fq.put(tq);
         if (wave == W - 1) {
-            float* r = reinterpret_cast<float*>(at + L::rows);
+            long long row;
+            const int rows = rows_of(c, row);
+            const Cum cum = chunk_cum(fg);
+            const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63);
             const float since = p.scale * exp2_of(cum.hi + cum.lo), until = decay_between(end_hi, end_lo, cum.hi, cum.lo);
             const int i = BACK && lane < rows ? rows - 1 - lane : lane;
-            r[i] = BACK ? -cum.hi : cum.hi;
-            r[64 + i] = BACK ? -cum.lo : cum.lo;
-            r[128 + i] = BACK ? until : since;
-            r[192 + i] = BACK ? since : until;
+            cum_hi[i] = BACK ? -cum.hi : cum.hi;
+            cum_lo[i] = BACK ? -cum.lo : cum.lo;
+            f_out[i] = BACK ? until : since;
+            w_in[i] = BACK ? since : until;
+            if (lane == 0) w_in[64] = exp2_of(end_hi + end_lo);
         }
     };
     fetch(0);
-    for (int b = 0; b < L::BUF; ++b) {   // what is never written but taken in: pairs above the diagonal, sums of tiles there
-        unsigned char* at = lds + b * L::one;
-        T* tp = reinterpret_cast<T*>(at + L::pairs);
-        if (wave == 0) {
-            *reinterpret_cast<V4*>(tp + TP::four(l, 16 + 4 * g)) = V4{};
-            *reinterpret_cast<V4*>(tp + TP::four(32 + l, 48 + 4 * g)) = V4{};
-        }
-        if constexpr (L::FOUR) {
-            if (threadIdx.x < 256) reinterpret_cast<float*>(at + L::by_col)[threadIdx.x] = reinterpret_cast<float*>(at + L::by_row)[threadIdx.x] = 0.0f;
-        }
+    // what is never written but taken in: pairs above the diagonal, sums of tiles there
+    if (wave == 0) {
+        *reinterpret_cast<V4*>(tp + TP::at(l, 16 + 4 * g)) = V4{};
+        *reinterpret_cast<V4*>(tp + TP::at(32 + l, 48 + 4 * g)) = V4{};
+    }
+    if constexpr (L::FOUR) {
+        if (threadIdx.x < 256) by_col[threadIdx.x] = by_row[threadIdx.x] = 0.0f;
     }
     put(0);
     __syncthreads();
 
     for (int c = 0; c < chunks; ++c) {
-        unsigned char* at = lds + (L::BUF == 2 ? (c & 1) * L::one : 0);
-        const T *ta = reinterpret_cast<const T*>(at + L::a), *tb = reinterpret_cast<const T*>(at + L::b), *tc = reinterpret_cast<const T*>(at + L::c),
-                *tq = reinterpret_cast<const T*>(at + L::q);
-        T* tp = reinterpret_cast<T*>(at + L::pairs);
-        const float *cum_hi = reinterpret_cast<const float*>(at + L::rows), *cum_lo = cum_hi + 64, *f_out = cum_hi + 128, *w_in = cum_hi + 192;
-        float *dots = reinterpret_cast<float*>(at + L::dots), *by_col = reinterpret_cast<float*>(at + L::by_col), *by_row = reinterpret_cast<float*>(at + L::by_row);
-        const float whole = exp2_of(end_hi + end_lo);
+        const float whole = w_in[64];
         long long row;
         const int rows = rows_of(c, row);
         const bool more = c + 1 < chunks;
@@ -171,7 +170,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
             const F32x4 hj = *reinterpret_cast<const F32x4*>(cum_hi + j0), lj = *reinterpret_cast<const F32x4*>(cum_lo + j0);
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = j0 + r <= i ? p.scale * x[r] * decay_between(hi_i, lo_i, hj[r], lj[r]) : 0.0f;
-            store_four<T>(tp + TP::four(i, j0), x, 4, true);
+            store_four<T>(tp + TP::at(i, j0), x, 4, true);
             if constexpr (MODE == RUN_DQ) {
                 // the gates' pairs: (dout_i . v_j) (q_i . k_j), summed over j along every row i, over the rows by groups of 16
                 F32x4 y = {0, 0, 0, 0};
@@ -197,85 +196,116 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         }
 
         // ---- the state: what it gives to the outputs, then the chunk's rows into it ----
-        F32x4 acc[4];
-        frag_t<T> cf[2];
+        F32x4 acc[4][VT];
+        frag_t<T> cf[2][VT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t] = F32x4{0, 0, 0, 0};
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int u = 0; u < VT; ++u) acc[t][u] = F32x4{0, 0, 0, 0};
         if (strip) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                constexpr int PIECES = L::SUMS ? P : 1;   // an output's rounded factor; the gates' sums take M as it is
-                frag_t<T> m[P];
-                if constexpr (PIECES > 1) pieces_of<T>(joined(M[2 * s], M[2 * s + 1]), m);
-                else m[0] = rounded<T>(joined(M[2 * s], M[2 * s + 1]));
+        for (int s = 0; s < KS; ++s) {
+            constexpr int PIECES = L::SUMS ? P : 1;   // an output's rounded factor; the gates' sums take M as it is
+            frag_t<T> m[VT][P];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const frag_t<T> af = T1::row_frag(ta, 16 * t + l, s, g);
-#pragma unroll
-                    for (int n = PIECES - 1; n >= 0; --n) acc[t] = mma(m[n], af, acc[t]);
-                }
+            for (int u = 0; u < VT; ++u) {
+                if constexpr (PIECES > 1) pieces_of<T>(joined(M[2 * s][u], M[2 * s + 1][u]), m[u]);
+                else m[u][0] = rounded<T>(joined(M[2 * s][u], M[2 * s + 1][u]));
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t] *= f_out[16 * t + l];
-            if constexpr (L::SUMS) {
+            for (int t = 0; t < 4; ++t) {
+                const frag_t<T> af = T1::row_frag(ta, 16 * t + l, s, g);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {   // q_i (MODE Dk: k_j) with what came in
-                    const int i = 16 * t + l;
-                    float x = 0.0f;
+                for (int n = PIECES - 1; n >= 0; --n)
+#pragma unroll
+                    for (int u = 0; u < VT; ++u) acc[t][u] = mma(m[u][n], af, acc[t][u]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int i = 16 * t + l;
+            const float f = f_out[i];
+#pragma unroll
+            for (int u = 0; u < VT; ++u) acc[t][u] *= f;
+            if constexpr (L::SUMS) {   // q_i (Dk: k_i) with what came in
+                float x = 0.0f;
+#pragma unroll
+                for (int u = 0; u < VT; ++u) {
                     if constexpr (MODE == RUN_DQ) {
-                        const V4 q4 = *reinterpret_cast<const V4*>(tq + T2::four(i, col0));
+                        const V4 q4 = *reinterpret_cast<const V4*>(tq + T2::at(i, col0 + 4 * u));
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) x += (float)q4[r] * acc[t][r];
+                        for (int r = 0; r < 4; ++r) x += (float)q4[r] * acc[t][u][r];
                     } else if (i < rows) {
-                        const T* kr = k + (row + rows - 1 - i) * p.stride_k + col0;
+                        const T* kr = k + (row + rows - 1 - i) * p.stride_k + col0 + 4 * u;
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (col0 + r < p.Dk) x += (float)kr[r] * acc[t][r];
-                    }
-                    x += __shfl_xor(x, 16);
-                    x += __shfl_xor(x, 32);
-                    if (g == 0) dots[64 * wave + i] = x;
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) cf[s] = T2::col_frag(tc, s, wave, lane);
-            if (more || to_the_end) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t) M[t] *= whole;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const F32x4 w0 = *reinterpret_cast<const F32x4*>(w_in + 32 * s + 4 * g), w1 = *reinterpret_cast<const F32x4*>(w_in + 32 * s + 16 + 4 * g);
-                    frag_t<T> cp[P];
-                    pieces_of<T>(widened(cf[s]) * joined(w0, w1), cp);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const frag_t<T> bf = T1::col_frag(tb, s, t, lane);
-#pragma unroll
-                        for (int n = P - 1; n >= 0; --n) M[t] = mma(bf, cp[n], M[t]);
+                            if (col0 + 4 * u + r < p.Dk) x += (float)kr[r] * acc[t][u][r];
                     }
                 }
+                x += __shfl_xor(x, 16);
+                x += __shfl_xor(x, 32);
+                if (g == 0) dots[64 * wave + i] = x;
             }
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int u = 0; u < VT; ++u) cf[s][u] = T2::col_frag(tc, s, n0 + u, lane);
+        if (more || to_the_end) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int u = 0; u < VT; ++u) M[t][u] *= whole;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const F32x4 w0 = *reinterpret_cast<const F32x4*>(w_in + 32 * s + 8 * g), w1 = *reinterpret_cast<const F32x4*>(w_in + 32 * s + 8 * g + 4);
+                frag_t<T> cp[VT][P];
+#pragma unroll
+                for (int u = 0; u < VT; ++u) pieces_of<T>(widened(cf[s][u]) * joined(w0, w1), cp[u]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const frag_t<T> bf = T1::col_frag(tb, s, t, lane);
+#pragma unroll
+                    for (int n = P - 1; n >= 0; --n) {
+                        if (n >= pieces) continue;
+#pragma unroll
+                        for (int u = 0; u < VT; ++u) M[t][u] = mma(bf, cp[u][n], M[t][u]);
+                    }
+                }
+            }
+        }
         } else if (L::SUMS) {
             dots[64 * wave + lane] = 0.0f;
         }
-        if (L::BUF == 2 && more) put(c + 1);
         __syncthreads();
-        if (L::BUF == 1 && more) put(c + 1);   // (the pairs and the sums are no part of it)
+        if (more) put(c + 1);   // (the pairs and the sums are no part of it)
 
         // ---- the pairs' part ----
         if (strip) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int t = 2 * s; t < 4; ++t) acc[t] = mma(cf[s], TP::row_frag(tp, 16 * t + l, s, g), acc[t]);
+            for (int t = 2 * s; t < 4; ++t) {
+                const frag_t<T> pf = TP::row_frag(tp, 16 * t + l, s, g);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int i = 16 * t + l;
-                if (i >= rows || col0 >= d2) continue;
-                const long long r = row + (BACK ? rows - 1 - i : i);
-                if (parts) store_four<float>(out_part + r * p.Hv * p.Dk + col0, acc[t], d2 - col0, wide_out);
-                else store_four<T>(out + r * so + col0, acc[t], d2 - col0, wide_out);
+                for (int u = 0; u < VT; ++u) acc[t][u] = mma(cf[s][u], pf, acc[t][u]);
             }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int i = 16 * t + l;
+            if (i >= rows || col0 >= d2) continue;
+            const long long r = row + (BACK ? rows - 1 - i : i);
+            if (parts) {
+#pragma unroll
+                for (int u = 0; u < VT; ++u) store_four<float>(out_part + r * p.Hv * p.Dk + col0 + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
+            } else if (VT == 2 && wide_out8) {
+                using V8 = T __attribute__((ext_vector_type(8)));
+                *reinterpret_cast<V8*>(out + r * so + col0) = __builtin_convertvector(joined(acc[t][0], acc[t][VT - 1]), V8);
+            } else {
+#pragma unroll
+                for (int u = 0; u < VT; ++u) store_four<T>(out + r * so + col0 + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
+            }
+        }
         }
         if (L::SUMS && p.dgate && wave == W - 1) {
             // A lane has row i.  Dq: sums from i on of what is read there, and the pairs that pass i.  Dk (backwards): sums behind i of
@@ -290,8 +320,6 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
                 for (int w = 0; w < 3; ++w) tile[w] = by_row[64 * w + lane];
             }
-            const float own = x;
-            (void)own;
 #pragma unroll
             for (int n = 1; n < 64; n *= 2) {
                 const float a = __shfl_down(x, n);
@@ -318,33 +346,36 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                 if (lane < rows) p.gate_k[(seg.row0 + row + rows - 1 - lane) * p.Hv + head] = lane < 63 ? next : 0.0f;
             }
         }
-        if (L::BUF == 1) __syncthreads();
+        __syncthreads();
     }
 
     // ---- the state at the run's end ----
-    if (MODE == RUN_OUT && to_the_end && strip) {
+    if (MODE == RUN_OUT && to_the_end) {
         float* to = p.last + of_seq;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (16 * t + 4 * g + r < p.Dk && 16 * wave + l < p.Dv) to[(long long)(16 * t + 4 * g + r) * p.Dv + 16 * wave + l] = M[t][r];
+            for (int u = 0; u < VT; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int x = column_of(t, 4 * g + r), y = column_of(n0 + u, l);
+                    if (x < p.Dk && y < p.Dv) to[(long long)x * p.Dv + y] = M[t][u][r];
+                }
     }
     if constexpr (MODE == RUN_DK) {
         // the gradient of the state in front of the segment: ds0 of its sequence, and its product with that state for the gates
         const StateAt st = first ? StateAt{p.s0 ? p.s0 + of_seq : nullptr, p.Dk, p.Dv, p.Dv} : StateAt{p.seg_state + of_seg, DK, DV, DV};
         float x = 0.0f;
-        const int dd = 16 * wave + l;
-        if (strip) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int u = 0; u < VT; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int vv = 16 * t + 4 * g + r;
-                    x += st(dd, vv) * M[t][r];
-                    if (first && p.ds0 && dd < p.Dk && vv < p.Dv) p.ds0[of_seq + (long long)dd * p.Dv + vv] = M[t][r];
+                    const int vv = column_of(t, 4 * g + r), dd = column_of(n0 + u, l);
+                    x += st(dd, vv) * M[t][u][r];
+                    if (first && p.ds0 && dd < p.Dk && vv < p.Dv) p.ds0[of_seq + (long long)dd * p.Dv + vv] = M[t][u][r];
                 }
-        }
         x = group_sum(x);
         x += __shfl_xor(x, 16);
         x += __shfl_xor(x, 32);
