@@ -68,6 +68,28 @@ __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p)
     }
 }
 
+// The gates of every chunk, once for all that use them: their running sum is a chain of dependent steps, and 64 gates of a head lie in as many
+// cache lines.  A workgroup has a chunk, a wavefront one head after another.
+__global__ __launch_bounds__(256) void matrec_rows_kernel(const MatrecParams p) {
+    const int seg_no = blockIdx.x / p.plan.per, c = blockIdx.x % p.plan.per, lane = threadIdx.x & 63;
+    if (seg_no >= *p.plan.count) return;
+    const MatSegment seg = p.plan.segs[seg_no];
+    const long long left = seg.rows - (long long)c * kChunk;
+    if (left <= 0) return;
+    const int rows = left < kChunk ? (int)left : kChunk;
+    const long long row = seg.row0 + (long long)c * kChunk;
+    for (int head = threadIdx.x >> 6; head < p.Hv; head += 4) {
+        const Cum cum = chunk_cum(lane < rows ? p.gate[(row + lane) * p.Hv + head] : 0.0f);
+        const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63);
+        float* to = p.rows_of + ((long long)(seg.chunk0 + c) * p.Hv + head) * kRowFloats;
+        to[lane] = cum.hi;
+        to[64 + lane] = cum.lo;
+        to[128 + lane] = p.scale * exp2_of(cum.hi + cum.lo);
+        to[192 + lane] = decay_between(end_hi, end_lo, cum.hi, cum.lo);
+        if (lane < 4) to[256 + lane] = lane == 0 ? exp2_of(end_hi + end_lo) : lane == 1 ? end_hi : lane == 2 ? end_lo : 0.0f;
+    }
+}
+
 // ---- states ----
 // A segment's own part of the state, and its decay, into seg_state (REV: of the gradient of the state in front of it, into seg_rstate: rows backwards,
 // (k, v) = (scale q, dout), R <- e^{c_64} R + sum_i e^{c_i} scale q_i dout_i^T).  Wavefront w keeps a quarter of v's columns, transposed: a lane has
@@ -91,7 +113,7 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
     const long long stride_k = REV ? p.stride_q : p.stride_k, stride_v = REV ? p.stride_o : p.stride_v;
     const T* k = reinterpret_cast<const T*>(REV ? p.q : p.k) + (long long)kh * p.Dk + seg.row0 * stride_k;
     const T* v = reinterpret_cast<const T*>(REV ? p.dout : p.v) + (long long)head * p.Dv + seg.row0 * stride_v;
-    const float* gate = p.gate + seg.row0 * p.Hv + head;
+    const float* gates = p.rows_of + ((long long)seg.chunk0 * p.Hv + head) * kRowFloats;
     const bool wide_k = wide_rows(k, stride_k, p.Dk), wide_v = wide_rows(v, stride_v, p.Dv);
     T *tk = reinterpret_cast<T*>(lds + L::k), *tv = reinterpret_cast<T*>(lds + L::v);
     float* weight = reinterpret_cast<float*>(lds + L::w);
@@ -110,22 +132,18 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
         const int rows = seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
         fk.fetch(k + row * stride_k, stride_k, rows, p.Dk, wide_k);
         fv.fetch(v + row * stride_v, stride_v, rows, p.Dv, wide_v);
-        if (wave == W - 1) fg = gate_of(gate + row * p.Hv, p.Hv, rows);
+        const float* from = gates + (long long)(REV ? chunks - 1 - i : i) * p.Hv * kRowFloats;
+        if (threadIdx.x < 67) fg = from[threadIdx.x < 64 ? (REV ? 128 : 192) + threadIdx.x : 192 + threadIdx.x];
     };
     fetch(0);
     for (int i = 0; i < chunks; ++i) {
         fk.put(tk);
         fv.put(tv);
-        if (wave == W - 1) {
-            const Cum cum = chunk_cum(fg);
-            const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63);
-            weight[lane] = REV ? p.scale * exp2_of(cum.hi + cum.lo) : decay_between(end_hi, end_lo, cum.hi, cum.lo);
-            if (lane == 0) weight[64] = exp2_of(end_hi + end_lo);
-            total += (double)end_hi + (double)end_lo;
-        }
+        if (threadIdx.x < 67) weight[threadIdx.x] = fg;
         __syncthreads();
         if (i + 1 < chunks) fetch(i + 1);
         const float whole = weight[64];
+        total += (double)weight[65] + (double)weight[66];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -153,7 +171,7 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int u = 0; u < VT; ++u) *reinterpret_cast<F32x4*>(to + column_of(t, l) * DV + column_of(n0 + u, 4 * g)) = S[t][u];
-    if (threadIdx.x == 64 * (W - 1)) p.seg_decay[(REV ? (long long)p.plan.max_segs * p.Hv : 0) + at] = (float)exp2(total);
+    if (threadIdx.x == 0) p.seg_decay[(REV ? (long long)p.plan.max_segs * p.Hv : 0) + at] = (float)exp2(total);
 }
 
 // blockIdx.y: 0 the states, 1 their gradients
@@ -291,6 +309,10 @@ hipError_t out_shape(const MatrecParams& p, hipStream_t stream) {
 
 hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream) {
     hipLaunchKernelGGL(matrec_plan_kernel, dim3(1), dim3(1024), 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    const unsigned chunks = (unsigned)((long long)p.plan.max_segs * p.plan.per);
+    if (e != hipSuccess || chunks == 0) return e;
+    hipLaunchKernelGGL(matrec_rows_kernel, dim3(chunks), dim3(256), 0, stream, p);
     return hipGetLastError();
 }
 hipError_t launch_matrec_out(int dtype, const MatrecParams& p, hipStream_t stream) {

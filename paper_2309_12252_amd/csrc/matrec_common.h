@@ -19,6 +19,7 @@ using I16x4 = short __attribute__((ext_vector_type(4)));
 using I16x8 = short __attribute__((ext_vector_type(8)));
 
 constexpr int kChunk = 64;
+constexpr int kRowFloats = 4 * 64 + 4;   // c_i as two floats, scale e^{c_i}, e^{c_64 - c_i}; e^{c_64} and c_64 as two floats
 
 template <typename T> struct Op;
 template <> struct Op<BF16> {
@@ -188,10 +189,6 @@ __device__ __forceinline__ Cum chunk_cum(float g) {
     r.lo = (float)(c - (double)r.hi);
     return r;
 }
-__device__ __forceinline__ float gate_of(const float* gate, long long stride, int rows) {
-    const int lane = threadIdx.x & 63;
-    return lane < rows ? gate[lane * stride] : 0.0f;
-}
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }   // 1 ulp; what is below 2^-126 becomes zero
 __device__ __forceinline__ float decay_between(float hi_i, float lo_i, float hi_j, float lo_j) { return exp2_of((hi_i - hi_j) + (lo_i - lo_j)); }
 
@@ -246,11 +243,11 @@ struct MatrecParams {
     // states in memory between kernels are whole tiles of 64 or 128 rows and columns (the next from Dk and Dv), zero outside the head
     float *seg_state, *seg_rstate;   // [max_segs][Hv][tile]: a segment's own part, then the state in front of it (gradient: behind it)
     float *seg_decay;                // [2][max_segs][Hv]
+    float *rows_of;                  // [chunks][Hv][kRowFloats]: a chunk's running gates and the factors that follow from them
     // gradient only
     float *part_q, *part_k;          // [rows][Hv][Dk]: dq and dk by heads of v, where several share one
     float *gate_k;                   // [rows][Hv]: the part of dgate that the run of dk has
     float *read_in, *put_out;        // [chunks][Hv]: sums of q_i . (...) and k_j . (...) over a chunk
-    float *whole;                    // [chunks][Hv]: the factor of a chunk
     float *front;                    // [max_segs][Hv]: <state, its gradient> in front of a segment
 };
 struct MatstepParams {
@@ -264,7 +261,7 @@ struct MatstepParams {
     void* o;
 };
 
-hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream);
+hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream);   // segments, and the gates of their chunks
 hipError_t launch_matrec_out(int dtype, const MatrecParams& p, hipStream_t stream);
 hipError_t launch_matrec_join(int dtype, const MatrecParams& p, bool both, hipStream_t stream);   // states in front of the segments (both: behind them too)
 hipError_t launch_matrec_grad(int dtype, const MatrecParams& p, hipStream_t stream);

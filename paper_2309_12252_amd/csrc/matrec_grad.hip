@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256) void matrec_through_kernel(const MatrecParams 
             const long long c = (long long)(seg.chunk0 + (c0 + i < chunks ? c0 + i : chunks - 1)) * p.Hv + head;
             u[i] = p.read_in[c];
             w[i] = p.put_out[c];
-            f[i] = p.whole[c];
+            f[i] = p.rows_of[c * kRowFloats + 256];
         }
 #pragma unroll
         for (int i = 0; i < K; ++i) {

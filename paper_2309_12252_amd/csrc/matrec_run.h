@@ -72,7 +72,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     out += seg.row0 * so;
     float* out_part = parts ? (MODE == RUN_DQ ? p.part_q : p.part_k) + (seg.row0 * p.Hv + head) * p.Dk : nullptr;
     const bool wide_out = parts ? p.Dk % 4 == 0 : four_wide(out, so, d2), wide_out8 = wide_rows(out, so, d2);
-    const float* gate = p.gate + seg.row0 * p.Hv + head;
+    const float* gates = p.rows_of + ((long long)seg.chunk0 * p.Hv + head) * kRowFloats;
 
     // ---- the state ----
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
@@ -102,7 +102,8 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     Stage<T, D1, 64 * W> fa, fb;
     Stage<T, D2, 64 * W> fc, fq;
     const bool wide_a = wide_rows(ra, sa, d1), wide_b = wide_rows(rb, sb, d1), wide_c = wide_rows(rc, sc, d2), wide_q = wide_rows(q, p.stride_q, p.Dk);
-    float fg = 0.0f;
+    constexpr int NG = (257 + 64 * W - 1) / (64 * W);
+    float fg[NG];
     auto rows_of = [&](int c, long long& row) {
         row = (long long)(BACK ? chunks - 1 - c : c) * kChunk;
         return seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
@@ -114,7 +115,13 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         fb.template fetch<BACK>(rb + row * sb, sb, rows, d1, wide_b);
         fc.template fetch<BACK>(rc + row * sc, sc, rows, d2, wide_c);
         if constexpr (L::FOUR) fq.template fetch<BACK>(q + row * p.stride_q, p.stride_q, rows, d2, wide_q);
-        if (wave == W - 1) fg = gate_of(gate + row * p.Hv, p.Hv, rows);
+        const float* from = gates + (long long)(BACK ? chunks - 1 - c : c) * p.Hv * kRowFloats;
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {   // cum_hi, cum_lo, f, w, whole; backwards: rows turned round, f and w the other way round
+            const int at = threadIdx.x + n * 64 * W, i = at & 63;
+            const int src = !BACK || at >= 256 ? at : (at < 128 ? at - i : 320 - (at - i)) + (i < rows ? rows - 1 - i : i);
+            if (at < 257) fg[n] = BACK && at < 128 ? -from[src] : from[src];
+        }
     };
     T *ta = reinterpret_cast<T*>(lds + L::a), *tb = reinterpret_cast<T*>(lds + L::b), *tc = reinterpret_cast<T*>(lds + L::c), *tq = reinterpret_cast<T*>(lds + L::q),
       *tp = reinterpret_cast<T*>(lds + L::pairs);
@@ -125,19 +132,9 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         fb.put(tb);
         fc.put(tc);
         if constexpr (L::FOUR) fq.put(tq);
-        if (wave == W - 1) {
-            long long row;
-            const int rows = rows_of(c, row);
-            const Cum cum = chunk_cum(fg);
-            const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63);
-            const float since = p.scale * exp2_of(cum.hi + cum.lo), until = decay_between(end_hi, end_lo, cum.hi, cum.lo);
-            const int i = BACK && lane < rows ? rows - 1 - lane : lane;
-            cum_hi[i] = BACK ? -cum.hi : cum.hi;
-            cum_lo[i] = BACK ? -cum.lo : cum.lo;
-            f_out[i] = BACK ? until : since;
-            w_in[i] = BACK ? since : until;
-            if (lane == 0) w_in[64] = exp2_of(end_hi + end_lo);
-        }
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+            if (threadIdx.x + n * 64 * W < 257) cum_hi[threadIdx.x + n * 64 * W] = fg[n];
     };
     fetch(0);
     // what is never written but taken in: pairs above the diagonal, sums of tiles there
@@ -159,7 +156,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         if (more) fetch(c + 1);
 
         // ---- pairs, tile by tile, transposed: a lane has one i and four neighbouring j ----
-        for (int n = wave; n < 10; n += W) {
+        auto pair_tile = [&](int n) {
             int ti, tj;
             lower_tile(n, ti, tj);
             const int i = 16 * ti + l, j0 = 16 * tj + 4 * g;
@@ -193,7 +190,10 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                     if (l == 0) by_col[64 * ti + j0 + r] = s;
                 }
             }
-        }
+        };
+        pair_tile(wave);
+        if (W < 8) pair_tile(wave + W);
+        if (wave < 10 % W) pair_tile(wave + 10 / W * W);
 
         // ---- the state: what it gives to the outputs, then the chunk's rows into it ----
         F32x4 acc[4][VT];
@@ -333,10 +333,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                 }
             }
             const long long chunk = (long long)(seg.chunk0 + (BACK ? chunks - 1 - c : c)) * p.Hv + head;
-            if (lane == 0) {
-                (MODE == RUN_DQ ? p.read_in : p.put_out)[chunk] = x;
-                if (MODE == RUN_DQ) p.whole[chunk] = whole;
-            }
+            if (lane == 0) (MODE == RUN_DQ ? p.read_in : p.put_out)[chunk] = x;
             if constexpr (MODE == RUN_DQ) {
 #pragma unroll
                 for (int w = 0; w < 3; ++w) pairs += lane > 16 * (w + 1) ? tile[w] : 0.0f;

@@ -127,7 +127,7 @@ struct MatLayout {
     long long chunks, max_segs;   // at most
     int per;
     bool split;
-    size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_part_q, off_part_k, off_gate, off_read, off_put, off_whole, off_front, total;
+    size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_part_q, off_part_k, off_gate, off_read, off_put, off_rows, off_front, total;
 };
 MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
     MatLayout l{};
@@ -155,6 +155,7 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
     };
     l.off_segs = take((size_t)l.max_segs * sizeof(MatSegment));
     l.off_seq = take(((size_t)c->N + 1) * 4);
+    l.off_rows = take((size_t)l.chunks * c->Hv * kRowFloats * 4);
     if (l.split) {
         l.off_state = take((size_t)l.max_segs * states);
         if (grad) l.off_rstate = take((size_t)l.max_segs * states);
@@ -169,7 +170,6 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
         l.off_gate = take(rows * by_head);
         l.off_read = take((size_t)l.chunks * by_head);
         l.off_put = take((size_t)l.chunks * by_head);
-        l.off_whole = take((size_t)l.chunks * by_head);
         l.off_front = take((size_t)l.max_segs * by_head);
     }
     l.total = at;
@@ -204,6 +204,7 @@ MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool gr
     p.stride_v = c->stride_v ? c->stride_v : (long long)c->Hv * c->Dv;
     p.stride_o = c->stride_o ? c->stride_o : (long long)c->Hv * c->Dv;
     p.split = l.split;
+    p.rows_of = reinterpret_cast<float*>(ws + l.off_rows);
     if (l.split) {
         p.seg_state = reinterpret_cast<float*>(ws + l.off_state);
         if (grad) p.seg_rstate = reinterpret_cast<float*>(ws + l.off_rstate);
@@ -217,7 +218,6 @@ MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool gr
         p.gate_k = reinterpret_cast<float*>(ws + l.off_gate);
         p.read_in = reinterpret_cast<float*>(ws + l.off_read);
         p.put_out = reinterpret_cast<float*>(ws + l.off_put);
-        p.whole = reinterpret_cast<float*>(ws + l.off_whole);
         p.front = reinterpret_cast<float*>(ws + l.off_front);
     }
     return p;
