@@ -94,14 +94,13 @@ __global__ __launch_bounds__(256) void matrec_rows_kernel(const MatrecParams p) 
 // A segment's own part of the state, and its decay, into seg_state (REV: of the gradient of the state in front of it, into seg_rstate: rows backwards,
 // (k, v) = (scale q, dout), R <- e^{c_64} R + sum_i e^{c_i} scale q_i dout_i^T).  Wavefront w keeps a quarter of v's columns, transposed: a lane has
 // four neighbouring v of one d in 16, so that states go to memory 16 bytes a lane.  The update and its cost are matrec_run's.
-constexpr int kStateWaves = 4;
 template <typename T, int DK, int DV>
 struct StatesLds {
     static constexpr size_t k = 0, v = Tile<T, DK>::bytes, w = v + Tile<T, DV>::bytes, total = w + 4 * 68;
 };
 template <typename T, int DK, int DV, bool REV>
 __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* lds) {
-    constexpr int W = kStateWaves, VT = DV / (16 * W), NT = DK / 16, P = Op<T>::PIECES;
+    constexpr int W = DV / 16, VT = 1, NT = DK / 16, P = Op<T>::PIECES;
     using L = StatesLds<T, DK, DV>;
     using TK = Tile<T, DK>;
     using TV = Tile<T, DV>;
@@ -124,24 +123,19 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
         for (int u = 0; u < VT; ++u) S[t][u] = F32x4{0, 0, 0, 0};
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
     double total = 0.0;
-    Stage<T, DK, 64 * W> fk;
-    Stage<T, DV, 64 * W> fv;
-    float fg = 0.0f;
-    auto fetch = [&](int i) {
-        const long long row = (long long)(REV ? chunks - 1 - i : i) * kChunk;
+    auto load = [&](int i) {
+        const int c = REV ? chunks - 1 - i : i;
+        const long long row = (long long)c * kChunk;
         const int rows = seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
-        fk.fetch(k + row * stride_k, stride_k, rows, p.Dk, wide_k);
-        fv.fetch(v + row * stride_v, stride_v, rows, p.Dv, wide_v);
-        const float* from = gates + (long long)(REV ? chunks - 1 - i : i) * p.Hv * kRowFloats;
-        if (threadIdx.x < 67) fg = from[threadIdx.x < 64 ? (REV ? 128 : 192) + threadIdx.x : 192 + threadIdx.x];
+        load_tile<T, DK, W, false>(tk, k + row * stride_k, stride_k, rows, p.Dk, wide_k);
+        load_tile<T, DV, W, false>(tv, v + row * stride_v, stride_v, rows, p.Dv, wide_v);
+        const float* from = gates + (long long)c * p.Hv * kRowFloats;
+        if (threadIdx.x < 67) weight[threadIdx.x] = from[threadIdx.x < 64 ? (REV ? 128 : 192) + threadIdx.x : 192 + threadIdx.x];
     };
-    fetch(0);
+    load(0);
     for (int i = 0; i < chunks; ++i) {
-        fk.put(tk);
-        fv.put(tv);
-        if (threadIdx.x < 67) weight[threadIdx.x] = fg;
+        wait_loads();
         __syncthreads();
-        if (i + 1 < chunks) fetch(i + 1);
         const float whole = weight[64];
         total += (double)weight[65] + (double)weight[66];
 #pragma unroll
@@ -164,6 +158,7 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
             }
         }
         __syncthreads();
+        if (i + 1 < chunks) load(i + 1);
     }
     const long long at = (long long)seg_no * p.Hv + head;
     float* to = (REV ? p.seg_rstate : p.seg_state) + at * (DK * DV);   // (outside the head: zero in S too)
@@ -176,7 +171,7 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
 
 // blockIdx.y: 0 the states, 1 their gradients
 template <typename T, int DK, int DV>
-__global__ __launch_bounds__(64 * kStateWaves, 2) void matrec_states_kernel(const MatrecParams p) {
+__global__ __launch_bounds__(4 * DV, sizeof(T) == 2 ? 4 : 2) void matrec_states_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     if (blockIdx.y == 0) states_of<T, DK, DV, false>(p, lds);
     else states_of<T, DK, DV, true>(p, lds);
@@ -229,11 +224,10 @@ __global__ __launch_bounds__(256) void matrec_join_kernel(const MatrecParams p) 
     else join_cell<DK, DV, true>(p, n, head, cell);
 }
 
-template <int DK, int DV> constexpr int out_waves() { return DV == 128 ? 8 : 4; }
 template <typename T, int DK, int DV>
-__global__ __launch_bounds__(DV == 128 ? 512 : 256, sizeof(T) == 2 ? 2 : 1) void matrec_out_kernel(const MatrecParams p) {
+__global__ __launch_bounds__(4 * DV, sizeof(T) == 2 ? (DV == 128 ? 4 : 3) : 2) void matrec_out_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    matrec_run<T, DK, DV, out_waves<DK, DV>(), RUN_OUT>(p, lds);
+    matrec_run<T, DK, DV, DV / 16, RUN_OUT>(p, lds);
 }
 
 // ---- one token ----
@@ -293,7 +287,7 @@ template <typename T, int DK, int DV>
 hipError_t join_shape(const MatrecParams& p, bool both, hipStream_t stream) {
     hipError_t e = hipSuccess;
     const unsigned y = both ? 2 : 1;
-    if (p.split) e = launch_lds(matrec_states_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), y), 64 * kStateWaves, StatesLds<T, DK, DV>::total, p, stream);
+    if (p.split) e = launch_lds(matrec_states_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), y), 4 * DV, StatesLds<T, DK, DV>::total, p, stream);
     if (e != hipSuccess || !(p.split || p.rows.bounds || p.rows.T == 0)) return e;
     hipLaunchKernelGGL((matrec_join_kernel<DK, DV>), dim3((unsigned)((long long)p.rows.N * p.Hv * (DK * DV / 256)), y), dim3(256), 0, stream, p);
     return hipGetLastError();
@@ -302,7 +296,7 @@ template <typename T, int DK, int DV>
 hipError_t out_shape(const MatrecParams& p, hipStream_t stream) {
     const hipError_t e = join_shape<T, DK, DV>(p, false, stream);
     if (e != hipSuccess) return e;
-    return launch_lds(matrec_out_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv)), 64 * out_waves<DK, DV>(), RunLds<T, DK, DV, out_waves<DK, DV>(), RUN_OUT>::total, p, stream);
+    return launch_lds(matrec_out_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv)), 4 * DV, RunLds<T, DK, DV, DV / 16, RUN_OUT>::total, p, stream);
 }
 
 }  // namespace

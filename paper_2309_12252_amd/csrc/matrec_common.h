@@ -67,6 +67,7 @@ __device__ __forceinline__ int column_of(int n, int i) { return 32 * (n >> 1) + 
 // A tile of 64 rows and C (64 or 128) columns in LDS, in units of eight columns.  bf16: the units' places in a row are turned by the row so that neither
 // 16 rows of one unit (row_frag) nor four half units of four rows (col_frag) meet in a bank.  fp32: rows 16 bytes apart in the banks.
 template <typename T, int C> struct Tile {
+    static_assert(C == 64 || C == 128, "units of a row fill a half or a whole turn of the banks");
     static constexpr int LD = sizeof(T) == 2 ? C : C + 4;
     static constexpr size_t bytes = sizeof(T) * kChunk * LD;
     static __device__ __forceinline__ int turn(int row) { return C == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : ((row & 2) << 1) | ((row >> 2) & 3); }
@@ -97,55 +98,58 @@ template <typename T, int C> struct Tile {
     }
 };
 
-// 64 rows of `cols` columns on their way from memory into a tile: fetched into registers, put into LDS later.  What is not there is zero.
-// `wide`: every row is aligned to 16 bytes and a multiple of eight columns (wide_rows()): then by buffer loads, whose bounds make the zeros.
+// ---- 64 rows of `cols` columns from memory into a tile; what is not there is zero ----
 template <typename T>
-__device__ __forceinline__ bool wide_rows(const T* base, long long stride, int cols) {
+__device__ __forceinline__ bool wide_rows(const T* base, long long stride, int cols) {   // every row aligned to 16 bytes, a multiple of eight columns
     return cols % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(base) % 16 == 0 && stride < (1 << 20);
 }
-template <typename T, int C, int THREADS> struct Stage {
-    using V8 = T __attribute__((ext_vector_type(8)));
-    using U4 = unsigned __attribute__((ext_vector_type(4)));
-    static constexpr int PER = C / 8, N = kChunk * PER / THREADS, STEP = THREADS / PER;   // units of a row, units of a thread, rows between them
-    static_assert(kChunk * PER % THREADS == 0 && THREADS % PER == 0, "every thread has as many units, all of the same columns");
-    V8 r[N];
-    // BACK: row r of the tile is row rows - 1 - r in memory
-    template <bool BACK = false>
-    __device__ __forceinline__ void fetch(const T* from, long long stride, int rows, int cols, bool wide) {
-        const int row0 = threadIdx.x / PER, c = threadIdx.x % PER * 8;
-        if (wide) {
-            const int pitch = (int)stride * (int)sizeof(T);
-            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, rows * pitch, 0x00020000);
+// a value that the compiler computes addresses from anew: kept across a loop they would take registers that are better used
+__device__ __forceinline__ int again(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // all of this wavefront's, also those into LDS
+
+// bf16: straight into LDS, 16 bytes a lane; a wavefront fills 64 units one behind the other, so a lane reads the unit whose turned place it has.
+// Bounds of the buffer make the zeros.  `load` returns while rows of wide arrays are on their way: wait_loads() before the barrier.
+// BACK: row r of the tile is row rows - 1 - r in memory.
+template <typename T, int C, int W, bool BACK>
+__device__ __forceinline__ void load_tile(T* tile, const T* from, long long stride, int rows, int cols, bool wide) {
+    constexpr int PER = C / 8;
+    const int lane = again(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (sizeof(T) == 2 && wide) {
+        typedef __attribute__((address_space(3))) void* LdsPtr;
+        constexpr int STEP = 64 / PER, N = kChunk / STEP;   // rows of an instruction; instructions of a tile
+        const int pitch = (int)stride * 2;
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, rows * pitch, 0x00020000);
+#pragma unroll
+        for (int n = 0; n < (N + W - 1) / W; ++n) {
+            const int at = wave + n * W;
+            if (N % W && at >= N) break;
+            const int row = at * STEP + lane / PER, c = ((lane % PER) ^ Tile<T, C>::turn(row)) * 8;
             // (a row in front of the first is far behind the end as an unsigned offset)
-            const int at = c < cols ? (BACK ? rows - 1 - row0 : row0) * pitch + c * (int)sizeof(T) : 0x60000000;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                U4 u[sizeof(T) / 2];
-#pragma unroll
-                for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-                    u[h] = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + (BACK ? -i : i) * STEP * pitch + 16 * h, 0, 0));
-                r[i] = __builtin_bit_cast(V8, u);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int row = row0 + i * STEP;
-                r[i] = V8{};
-                if (row < rows) {
-                    const T* src = from + (BACK ? rows - 1 - row : row) * stride + c;
+            const int off = c < cols ? (BACK ? rows - 1 - row : row) * pitch + c * 2 : 0x60000000;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LdsPtr)(tile + at * STEP * C), 16, off, 0, 0, 0);
+        }
+    } else {
+        for (int at = threadIdx.x; at < kChunk * PER; at += 64 * W) {
+            using V8 = T __attribute__((ext_vector_type(8)));
+            const int row = at / PER, c = at % PER * 8;
+            V8 v = {};
+            if (row < rows) {
+                const T* src = from + (BACK ? rows - 1 - row : row) * stride + c;
+                if (wide) {
+                    if (c < cols) v = *reinterpret_cast<const V8*>(src);
+                } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (c + e < cols) r[i][e] = src[e];
+                        if (c + e < cols) v[e] = src[e];
                 }
             }
+            *reinterpret_cast<V8*>(tile + Tile<T, C>::at(row, c)) = v;
         }
     }
-    __device__ __forceinline__ void put(T* tile) const {
-        const int row0 = threadIdx.x / PER, c = threadIdx.x % PER * 8;
-#pragma unroll
-        for (int i = 0; i < N; ++i) *reinterpret_cast<V8*>(tile + Tile<T, C>::at(row0 + i * STEP, c)) = r[i];
-    }
-};
+}
 
 // four values of a row, rounded: one store where the rows allow it
 template <typename T>

@@ -27,7 +27,7 @@ struct GradShape {
 
 // blockIdx.y: dq, dk, dv
 template <typename T, int DK, int DV>
-__global__ __launch_bounds__(4 * (DK > DV ? DK : DV), sizeof(T) == 2 ? 2 : 1) void matrec_grad_kernel(const MatrecParams p) {
+__global__ __launch_bounds__(4 * (DK > DV ? DK : DV), sizeof(T) == 2 ? (DK == 128 || DV == 128 ? 4 : 3) : 2) void matrec_grad_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     constexpr int W = GradShape<T, DK, DV>::W;
     if (blockIdx.y == 0) matrec_run<T, DK, DV, W, RUN_DQ>(p, lds);

@@ -5,10 +5,11 @@
 //   Dq   a, b, c = dout, v, k      M = S^T   the same
 //   Dk   a, b, c = v, dout, q      M = R^T   rows and chunks backwards: c_i stands for -c_i, f_i = e^{c_64 - c_i}, w_j = scale e^{c_j}
 //   Dv   a, b, c = k, q, dout      M = R     backwards, the same
-// (S the state in front of a chunk, R the gradient of the state behind it.)  Wavefront w has a quarter of c's columns, one or two tiles of 16: M's, as
+// (S the state in front of a chunk, R the gradient of the state behind it.)  Wavefront w has 16 of c's columns: M's, as
 // results, which are operands of M^T a as they stand, and the outputs', transposed, a lane four or eight neighbouring columns of a row.
 // What bounds it: 120 to 210 matrix instructions of 16 cycles and some 500 vector instructions a wavefront and chunk of 128 columns, which a SIMD does one
-// after another, and 64 KiB of rows a chunk.  The next chunk's rows are on their way to registers while this one is computed.
+// after another, and 64 KiB of rows a chunk.  Two workgroups fill a CU and go on while the other one waits for its rows, which go straight to LDS: no
+// registers for them, so that 128 are enough.
 #pragma once
 #include "matrec_common.h"
 
@@ -46,7 +47,8 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     using T2 = Tile<T, D2>;
     using TP = Tile<T, kChunk>;
     using V4 = T __attribute__((ext_vector_type(4)));
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
+    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int lane = lane0, g = lane >> 4, l = lane & 15;
     const int seg_no = blockIdx.x / p.Hv, head = blockIdx.x % p.Hv, kh = head / (p.Hv / p.Hk);
     if (seg_no >= *p.plan.count) return;
     const MatSegment seg = p.plan.segs[seg_no];
@@ -71,7 +73,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     const long long so = MODE == RUN_OUT ? p.stride_o : MODE == RUN_DV ? p.stride_v : MODE == RUN_DQ ? p.stride_q : p.stride_k;
     out += seg.row0 * so;
     float* out_part = parts ? (MODE == RUN_DQ ? p.part_q : p.part_k) + (seg.row0 * p.Hv + head) * p.Dk : nullptr;
-    const bool wide_out = parts ? p.Dk % 4 == 0 : four_wide(out, so, d2), wide_out8 = wide_rows(out, so, d2);
+    const bool wide_out = parts ? p.Dk % 4 == 0 : four_wide(out, so, d2);
     const float* gates = p.rows_of + ((long long)seg.chunk0 * p.Hv + head) * kRowFloats;
 
     // ---- the state ----
@@ -98,45 +100,30 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     // pieces that rows enter the state as: all where it is handed out or sums are taken of it as it is, two where it is rounded itself
     const int pieces = to_the_end || L::SUMS || P == 1 ? P : 2;
 
-    // ---- a chunk's rows: fetched into registers, put into LDS ----
-    Stage<T, D1, 64 * W> fa, fb;
-    Stage<T, D2, 64 * W> fc, fq;
+    // ---- a chunk's rows into LDS ----
     const bool wide_a = wide_rows(ra, sa, d1), wide_b = wide_rows(rb, sb, d1), wide_c = wide_rows(rc, sc, d2), wide_q = wide_rows(q, p.stride_q, p.Dk);
-    constexpr int NG = (257 + 64 * W - 1) / (64 * W);
-    float fg[NG];
     auto rows_of = [&](int c, long long& row) {
         row = (long long)(BACK ? chunks - 1 - c : c) * kChunk;
         return seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
-    };
-    auto fetch = [&](int c) {
-        long long row;
-        const int rows = rows_of(c, row);
-        fa.template fetch<BACK>(ra + row * sa, sa, rows, d1, wide_a);
-        fb.template fetch<BACK>(rb + row * sb, sb, rows, d1, wide_b);
-        fc.template fetch<BACK>(rc + row * sc, sc, rows, d2, wide_c);
-        if constexpr (L::FOUR) fq.template fetch<BACK>(q + row * p.stride_q, p.stride_q, rows, d2, wide_q);
-        const float* from = gates + (long long)(BACK ? chunks - 1 - c : c) * p.Hv * kRowFloats;
-#pragma unroll
-        for (int n = 0; n < NG; ++n) {   // cum_hi, cum_lo, f, w, whole; backwards: rows turned round, f and w the other way round
-            const int at = threadIdx.x + n * 64 * W, i = at & 63;
-            const int src = !BACK || at >= 256 ? at : (at < 128 ? at - i : 320 - (at - i)) + (i < rows ? rows - 1 - i : i);
-            if (at < 257) fg[n] = BACK && at < 128 ? -from[src] : from[src];
-        }
     };
     T *ta = reinterpret_cast<T*>(lds + L::a), *tb = reinterpret_cast<T*>(lds + L::b), *tc = reinterpret_cast<T*>(lds + L::c), *tq = reinterpret_cast<T*>(lds + L::q),
       *tp = reinterpret_cast<T*>(lds + L::pairs);
     float *cum_hi = reinterpret_cast<float*>(lds + L::rows), *cum_lo = cum_hi + 64, *f_out = cum_hi + 128, *w_in = cum_hi + 192;
     float *dots = reinterpret_cast<float*>(lds + L::dots), *by_col = reinterpret_cast<float*>(lds + L::by_col), *by_row = reinterpret_cast<float*>(lds + L::by_row);
-    auto put = [&](int c) {
-        fa.put(ta);
-        fb.put(tb);
-        fc.put(tc);
-        if constexpr (L::FOUR) fq.put(tq);
-#pragma unroll
-        for (int n = 0; n < NG; ++n)
-            if (threadIdx.x + n * 64 * W < 257) cum_hi[threadIdx.x + n * 64 * W] = fg[n];
+    auto load = [&](int c) {
+        long long row;
+        const int rows = rows_of(c, row);
+        load_tile<T, D1, W, BACK>(ta, ra + row * sa, sa, rows, d1, wide_a);
+        load_tile<T, D1, W, BACK>(tb, rb + row * sb, sb, rows, d1, wide_b);
+        load_tile<T, D2, W, BACK>(tc, rc + row * sc, sc, rows, d2, wide_c);
+        if constexpr (L::FOUR) load_tile<T, D2, W, BACK>(tq, q + row * p.stride_q, p.stride_q, rows, d2, wide_q);
+        // cum_hi, cum_lo, f, w, whole; backwards: rows turned round, f and w the other way round
+        const float* from = gates + (long long)(BACK ? chunks - 1 - c : c) * p.Hv * kRowFloats;
+        for (int at = threadIdx.x; at < 257; at += 64 * W) {
+            const int i = at & 63;
+            cum_hi[at] = from[!BACK || at >= 256 ? at : (at < 128 ? at - i : 320 - (at - i)) + (i < rows ? rows - 1 - i : i)];
+        }
     };
-    fetch(0);
     // what is never written but taken in: pairs above the diagonal, sums of tiles there
     if (wave == 0) {
         *reinterpret_cast<V4*>(tp + TP::at(l, 16 + 4 * g)) = V4{};
@@ -145,15 +132,18 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     if constexpr (L::FOUR) {
         if (threadIdx.x < 256) by_col[threadIdx.x] = by_row[threadIdx.x] = 0.0f;
     }
-    put(0);
+    load(0);
+    wait_loads();
     __syncthreads();
 
     for (int c = 0; c < chunks; ++c) {
+        lane = again(lane0);
+        g = lane >> 4;
+        l = lane & 15;
         const float whole = w_in[64];
         long long row;
         const int rows = rows_of(c, row);
         const bool more = c + 1 < chunks;
-        if (more) fetch(c + 1);
 
         // ---- pairs, tile by tile, transposed: a lane has one i and four neighbouring j ----
         auto pair_tile = [&](int n) {
@@ -166,7 +156,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
             const float hi_i = cum_hi[i], lo_i = cum_lo[i];
             const F32x4 hj = *reinterpret_cast<const F32x4*>(cum_hi + j0), lj = *reinterpret_cast<const F32x4*>(cum_lo + j0);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = j0 + r <= i ? p.scale * x[r] * decay_between(hi_i, lo_i, hj[r], lj[r]) : 0.0f;
+            for (int r = 0; r < 4; ++r) x[r] = j0 + r <= i ? p.scale * x[r] * (BACK ? decay_between(hj[r], lj[r], hi_i, lo_i) : decay_between(hi_i, lo_i, hj[r], lj[r])) : 0.0f;
             store_four<T>(tp + TP::at(i, j0), x, 4, true);
             if constexpr (MODE == RUN_DQ) {
                 // the gates' pairs: (dout_i . v_j) (q_i . k_j), summed over j along every row i, over the rows by groups of 16
@@ -278,34 +268,17 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
             dots[64 * wave + lane] = 0.0f;
         }
         __syncthreads();
-        if (more) put(c + 1);   // (the pairs and the sums are no part of it)
 
         // ---- the pairs' part ----
         if (strip) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int t = 2 * s; t < 4; ++t) {
-                const frag_t<T> pf = TP::row_frag(tp, 16 * t + l, s, g);
+                for (int t = 2 * s; t < 4; ++t) {
+                    const frag_t<T> pf = TP::row_frag(tp, 16 * t + l, s, g);
 #pragma unroll
-                for (int u = 0; u < VT; ++u) acc[t][u] = mma(cf[s][u], pf, acc[t][u]);
-            }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int i = 16 * t + l;
-            if (i >= rows || col0 >= d2) continue;
-            const long long r = row + (BACK ? rows - 1 - i : i);
-            if (parts) {
-#pragma unroll
-                for (int u = 0; u < VT; ++u) store_four<float>(out_part + r * p.Hv * p.Dk + col0 + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
-            } else if (VT == 2 && wide_out8) {
-                using V8 = T __attribute__((ext_vector_type(8)));
-                *reinterpret_cast<V8*>(out + r * so + col0) = __builtin_convertvector(joined(acc[t][0], acc[t][VT - 1]), V8);
-            } else {
-#pragma unroll
-                for (int u = 0; u < VT; ++u) store_four<T>(out + r * so + col0 + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
-            }
-        }
+                    for (int u = 0; u < VT; ++u) acc[t][u] = mma(cf[s][u], pf, acc[t][u]);
+                }
         }
         if (L::SUMS && p.dgate && wave == W - 1) {
             // A lane has row i.  Dq: sums from i on of what is read there, and the pairs that pass i.  Dk (backwards): sums behind i of
@@ -343,6 +316,23 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                 if (lane < rows) p.gate_k[(seg.row0 + row + rows - 1 - lane) * p.Hv + head] = lane < 63 ? next : 0.0f;
             }
         }
+        if (more) load(c + 1);   // over the tiles; the pairs and the sums lie beside them
+        if (strip && col0 < d2) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int i = 16 * t + l;
+                if (i >= rows) continue;
+                const long long r = row + (BACK ? rows - 1 - i : i);
+                if (parts) {
+#pragma unroll
+                    for (int u = 0; u < VT; ++u) store_four<float>(out_part + r * p.Hv * p.Dk + col0 + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < VT; ++u) store_four<T>(out + r * so + col0 + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
+                }
+            }
+        }
+        wait_loads();
         __syncthreads();
     }
 

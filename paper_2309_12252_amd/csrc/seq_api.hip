@@ -136,7 +136,7 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
     long long per = longest < 1 ? 1 : longest;
     if (c->packed || (long long)c->N * c->Hv < 256) {
         // 512 workgroups run at a time; every sequence's last segment is a short one, half of the others' length on average
-        long long segs = 256 / c->Hv - (c->packed ? c->N / 2 : 0);
+        long long segs = 512 / c->Hv - (c->packed ? c->N / 2 : 0);
         if (segs < 1) segs = 1;
         const long long want = ((c->packed ? longest : l.chunks) + segs - 1) / segs;
         per = want < 4 ? 4 : want;
