@@ -72,8 +72,8 @@ __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p)
 // cache lines.  A workgroup has a chunk, a wavefront one head after another.
 __global__ __launch_bounds__(256) void matrec_rows_kernel(const MatrecParams p) {
     const int seg_no = blockIdx.x / p.plan.per, c = blockIdx.x % p.plan.per, lane = threadIdx.x & 63;
-    if (seg_no >= *p.plan.count) return;
-    const MatSegment seg = p.plan.segs[seg_no];
+    MatSegment seg;
+    if (!segment_of(p, seg_no, seg)) return;
     const long long left = seg.rows - (long long)c * kChunk;
     if (left <= 0) return;
     const int rows = left < kChunk ? (int)left : kChunk;
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void matrec_rows_kernel(const MatrecParams p) 
 // four neighbouring v of one d in 16, so that states go to memory 16 bytes a lane.  The update and its cost are matrec_run's.
 template <typename T, int DK, int DV>
 struct StatesLds {
-    static constexpr size_t k = 0, v = Tile<T, DK>::bytes, w = v + Tile<T, DV>::bytes, total = w + 4 * 68;
+    static constexpr size_t k = 0, v = Tile<T, DK>::bytes, w = v + Tile<T, DV>::bytes, total = w + 4 * 128;
 };
 template <typename T, int DK, int DV, bool REV>
 __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* lds) {
@@ -106,8 +106,8 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
     using TV = Tile<T, DV>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15, n0 = VT * wave;
     const int seg_no = blockIdx.x / p.Hv, head = blockIdx.x % p.Hv, kh = head / (p.Hv / p.Hk);
-    if (seg_no >= *p.plan.count) return;
-    const MatSegment seg = p.plan.segs[seg_no];
+    MatSegment seg;
+    if (!segment_of(p, seg_no, seg)) return;
     if (seg.index == (REV ? 0 : seg.count - 1)) return;   // nothing comes behind it
     const long long stride_k = REV ? p.stride_q : p.stride_k, stride_v = REV ? p.stride_o : p.stride_v;
     const T* k = reinterpret_cast<const T*>(REV ? p.q : p.k) + (long long)kh * p.Dk + seg.row0 * stride_k;
@@ -130,7 +130,7 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
         load_tile<T, DK, W, false>(tk, k + row * stride_k, stride_k, rows, p.Dk, wide_k);
         load_tile<T, DV, W, false>(tv, v + row * stride_v, stride_v, rows, p.Dv, wide_v);
         const float* from = gates + (long long)c * p.Hv * kRowFloats;
-        if (threadIdx.x < 67) weight[threadIdx.x] = from[threadIdx.x < 64 ? (REV ? 128 : 192) + threadIdx.x : 192 + threadIdx.x];
+        if (wave < 2) load_floats(weight + 64 * wave, from, wave == 0 ? (REV ? 128 : 192) + lane : 256 + lane);
     };
     load(0);
     for (int i = 0; i < chunks; ++i) {
@@ -187,7 +187,7 @@ __device__ __forceinline__ void join_cell(const MatrecParams& p, int n, int head
     const long long at = (((long long)n * p.Hv + head) * p.Dk + d) * p.Dv + v;
     const float* ends = REV ? p.dlast : p.s0;
     float* outs = REV ? p.ds0 : p.last;
-    const int first = p.plan.seq_seg[n], count = p.plan.seq_seg[n + 1] - first;
+    const int first = first_segment(p, n), count = first_segment(p, n + 1) - first;
     float s = ends && inside ? ends[at] : 0.0f;
     if (count == 0) {
         if (outs && inside) outs[at] = s;
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(256) void matrec_join_kernel(const MatrecParams p) 
 template <typename T, int DK, int DV>
 __global__ __launch_bounds__(4 * DV, sizeof(T) == 2 ? (DV == 128 ? 4 : 3) : 2) void matrec_out_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    matrec_run<T, DK, DV, DV / 16, RUN_OUT>(p, lds);
+    matrec_run<T, DK, DV, DV / 16, RUN_OUT>(p, lds, blockIdx.x);
 }
 
 // ---- one token ----
@@ -302,8 +302,11 @@ hipError_t out_shape(const MatrecParams& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream) {
-    hipLaunchKernelGGL(matrec_plan_kernel, dim3(1), dim3(1024), 0, stream, p);
-    const hipError_t e = hipGetLastError();
+    hipError_t e = hipSuccess;
+    if (p.rows.bounds) {
+        hipLaunchKernelGGL(matrec_plan_kernel, dim3(1), dim3(1024), 0, stream, p);
+        e = hipGetLastError();
+    }
     const unsigned chunks = (unsigned)((long long)p.plan.max_segs * p.plan.per);
     if (e != hipSuccess || chunks == 0) return e;
     hipLaunchKernelGGL(matrec_rows_kernel, dim3(chunks), dim3(256), 0, stream, p);

@@ -151,6 +151,13 @@ __device__ __forceinline__ void load_tile(T* tile, const T* from, long long stri
     }
 }
 
+// 64 floats of a chunk's kRowFloats straight into LDS: lane i's is from[place]; zero where place lies behind them
+__device__ __forceinline__ void load_floats(float* to, const float* from, int place) {
+    typedef __attribute__((address_space(3))) void* LdsPtr;
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, kRowFloats * 4, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LdsPtr)to, 4, place * 4, 0, 0, 0);
+}
+
 // four values of a row, rounded: one store where the rows allow it
 template <typename T>
 __device__ __forceinline__ void store_four(T* to, F32x4 x, int count, bool wide) {
@@ -227,6 +234,7 @@ struct MatSegment {
     int index, count;    // place among the sequence's segments, and how many there are
 };
 struct MatPlan {
+    // with bounds: filled by the plan's kernel; without, every sequence is cut alike and a segment follows from its number
     int* count;          // segments
     MatSegment* segs;    // [max_segs]
     int* seq_seg;        // [N + 1]: a sequence's first segment
@@ -264,6 +272,31 @@ struct MatstepParams {
     float* state;
     void* o;
 };
+
+// segment number `no`; false behind the last
+__device__ __forceinline__ bool segment_of(const MatrecParams& p, int no, MatSegment& s) {
+    if (p.rows.bounds) {
+        if (no >= *p.plan.count) return false;
+        s = p.plan.segs[no];
+        return true;
+    }
+    const int chunks = (int)((p.rows.T + 63) / 64);
+    s.count = (chunks + p.plan.per - 1) / p.plan.per;
+    if (s.count == 0 || no >= s.count * p.rows.N) return false;
+    s.seq = no / s.count;
+    s.index = no % s.count;
+    s.chunk0 = s.seq * chunks + s.index * p.plan.per;
+    const long long first = (long long)s.index * p.plan.per * 64, most = (long long)p.plan.per * 64;
+    s.row0 = s.seq * p.rows.T + first;
+    s.rows = p.rows.T - first < most ? p.rows.T - first : most;
+    return true;
+}
+// first segment of sequence n (n = N: how many there are)
+__device__ __forceinline__ int first_segment(const MatrecParams& p, int n) {
+    if (p.rows.bounds) return p.plan.seq_seg[n];
+    const int chunks = (int)((p.rows.T + 63) / 64);
+    return n * ((chunks + p.plan.per - 1) / p.plan.per);
+}
 
 hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream);   // segments, and the gates of their chunks
 hipError_t launch_matrec_out(int dtype, const MatrecParams& p, hipStream_t stream);

@@ -25,22 +25,23 @@ struct GradShape {
     static constexpr size_t lds = a > b ? (a > c ? a : c) : (b > c ? b : c);
 };
 
-// blockIdx.y: dq, dk, dv
+// dq, dk and dv of a segment and head at the same time and on the same XCD (workgroups go to the 8 XCDs in turn): they read the same rows
 template <typename T, int DK, int DV>
 __global__ __launch_bounds__(4 * (DK > DV ? DK : DV), sizeof(T) == 2 ? (DK == 128 || DV == 128 ? 4 : 3) : 2) void matrec_grad_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     constexpr int W = GradShape<T, DK, DV>::W;
-    if (blockIdx.y == 0) matrec_run<T, DK, DV, W, RUN_DQ>(p, lds);
-    else if (blockIdx.y == 1) matrec_run<T, DK, DV, W, RUN_DK>(p, lds);
-    else matrec_run<T, DK, DV, W, RUN_DV>(p, lds);
+    const int run = blockIdx.x / 8 % 3, id = blockIdx.x / 24 * 8 + blockIdx.x % 8;
+    if (run == 0) matrec_run<T, DK, DV, W, RUN_DQ>(p, lds, id);
+    else if (run == 1) matrec_run<T, DK, DV, W, RUN_DK>(p, lds, id);
+    else matrec_run<T, DK, DV, W, RUN_DV>(p, lds, id);
 }
 
 // what goes through every chunk, in the place of what is read in it: along a segment from <S, dS> in front of it; a lane has a head of a segment
 __global__ __launch_bounds__(256) void matrec_through_kernel(const MatrecParams p) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
     const int seg_no = (int)(at / p.Hv), head = (int)(at % p.Hv);
-    if (seg_no >= *p.plan.count) return;
-    const MatSegment seg = p.plan.segs[seg_no];
+    MatSegment seg;
+    if (!segment_of(p, seg_no, seg)) return;
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
     float here = p.front[at];
     constexpr int K = 8;
@@ -66,8 +67,8 @@ __global__ __launch_bounds__(256) void matrec_through_kernel(const MatrecParams 
 // dgate: the parts of the two runs and what goes through; a workgroup has a chunk of a segment
 __global__ __launch_bounds__(256) void matrec_gates_kernel(const MatrecParams p) {
     const int seg_no = blockIdx.x / p.plan.per, c = blockIdx.x % p.plan.per;
-    if (seg_no >= *p.plan.count) return;
-    const MatSegment seg = p.plan.segs[seg_no];
+    MatSegment seg;
+    if (!segment_of(p, seg_no, seg)) return;
     const long long left = seg.rows - (long long)c * kChunk;
     if (left <= 0) return;
     const int rows = left < kChunk ? (int)left : kChunk;
@@ -79,8 +80,8 @@ __global__ __launch_bounds__(256) void matrec_gates_kernel(const MatrecParams p)
 template <typename T>
 __global__ __launch_bounds__(256) void matrec_shared_kernel(const MatrecParams p) {
     const int seg_no = blockIdx.x / p.plan.per, c = blockIdx.x % p.plan.per;
-    if (seg_no >= *p.plan.count) return;
-    const MatSegment seg = p.plan.segs[seg_no];
+    MatSegment seg;
+    if (!segment_of(p, seg_no, seg)) return;
     const long long left = seg.rows - (long long)c * kChunk;
     if (left <= 0) return;
     const int rows = left < kChunk ? (int)left : kChunk, group = p.Hv / p.Hk, cols = p.Hk * p.Dk;
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256) void matrec_shared_kernel(const MatrecParams p
 template <typename T, int DK, int DV>
 hipError_t grad_shape(const MatrecParams& p, hipStream_t stream) {
     using G = GradShape<T, DK, DV>;
-    return launch_lds(matrec_grad_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), 3), 64 * G::W, G::lds, p, stream);
+    return launch_lds(matrec_grad_kernel<T, DK, DV>, dim3((unsigned)(((long long)p.plan.max_segs * p.Hv + 7) / 8 * 24)), 64 * G::W, G::lds, p, stream);
 }
 
 }  // namespace

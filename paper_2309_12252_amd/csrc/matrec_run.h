@@ -24,22 +24,37 @@ struct RunLds {
     static constexpr bool SUMS = MODE == RUN_DQ || MODE == RUN_DK;
     static constexpr size_t a = 0, b = Tile<T, D1>::bytes, c = b + Tile<T, D1>::bytes, q = c + Tile<T, D2>::bytes, pairs = q + (FOUR ? Tile<T, D2>::bytes : 0),
                             rows = pairs + Tile<T, kChunk>::bytes,       // cum_hi, cum_lo, f, w, and the chunk's factor
-                            dots = rows + 4 * (4 * 64 + 4),              // [W][64]
+                            dots = rows + 4 * 5 * 64,                    // [W][64]
                             by_col = dots + (SUMS ? 4 * 64 * W : 0),   // [row tile][64]
                             by_row = by_col + (FOUR ? 4 * 256 : 0),      // [column tile][64]
                             total = by_row + (FOUR ? 4 * 256 : 0);
     static_assert(total <= 160 * 1024, "a workgroup's tiles fit the CU's LDS");
 };
 
-// a state of Dk x Dv in the caller's layout, or a whole tile DK x DV: element (k row, v column)
+// a state of Dk x Dv in the caller's layout, or a whole tile DK x DV: element (k row, v column), and four neighbouring columns
 struct StateAt {
     const float* at;
     int Dk, Dv, ld;
-    __device__ __forceinline__ float operator()(int d, int v) const { return at && d < Dk && v < Dv ? at[(long long)d * ld + v] : 0.0f; }
+    bool fours;      // every row aligned to 16 bytes
+    __device__ __forceinline__ StateAt(const float* from, int dk, int dv, int pitch)
+        : at(from), Dk(dk), Dv(dv), ld(pitch), fours(dv % 4 == 0 && pitch % 4 == 0 && reinterpret_cast<uintptr_t>(from) % 16 == 0) {}
+    __device__ __forceinline__ float operator()(int d, int v) const { return at && d < Dk && v < Dv ? at[d * ld + v] : 0.0f; }
+    __device__ __forceinline__ F32x4 four(int d, int v) const {
+        F32x4 x = {0, 0, 0, 0};
+        if (!at || d >= Dk) return x;
+        if (fours) {
+            if (v < Dv) x = *reinterpret_cast<const F32x4*>(at + d * ld + v);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (v + r < Dv) x[r] = at[d * ld + v + r];
+        }
+        return x;
+    }
 };
 
 template <typename T, int DK, int DV, int W, int MODE>
-__device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char* lds) {
+__device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char* lds, int id) {
     constexpr bool BACK = MODE == RUN_DK || MODE == RUN_DV, KEYS = MODE == RUN_DQ || MODE == RUN_DK;   // KEYS: D1 is the values', D2 the keys'
     constexpr int D1 = KEYS ? DV : DK, D2 = KEYS ? DK : DV, KS = D1 / 32, NT = D1 / 16, VT = D2 / (16 * W) > 0 ? D2 / (16 * W) : 1, P = Op<T>::PIECES;
     using L = RunLds<T, D1, D2, W, MODE>;
@@ -49,9 +64,9 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     using V4 = T __attribute__((ext_vector_type(4)));
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int lane = lane0, g = lane >> 4, l = lane & 15;
-    const int seg_no = blockIdx.x / p.Hv, head = blockIdx.x % p.Hv, kh = head / (p.Hv / p.Hk);
-    if (seg_no >= *p.plan.count) return;
-    const MatSegment seg = p.plan.segs[seg_no];
+    const int seg_no = id / p.Hv, head = id % p.Hv, kh = head / (p.Hv / p.Hk);
+    MatSegment seg;
+    if (!segment_of(p, seg_no, seg)) return;
     const int d1 = KEYS ? p.Dv : p.Dk, d2 = KEYS ? p.Dk : p.Dv, n0 = VT * wave;   // this wavefront's first tile of columns
     const bool strip = 16 * n0 < D2;                                             // (it has some)
     const int col0 = column_of(n0, 4 * g);                                       // a lane's first column of 4 VT
@@ -88,12 +103,11 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int u = 0; u < VT; ++u)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int x = column_of(t, 4 * g + r), y = column_of(n0 + u, l);
-                    M[t][u][r] = KEYS ? st(y, x) : st(x, y);
-                }
+            for (int u = 0; u < VT; ++u) {
+                const int x = column_of(t, 4 * g), y = column_of(n0 + u, l);   // (and the three rows behind x)
+                if constexpr (KEYS) M[t][u] = st.four(y, x);
+                else M[t][u] = F32x4{st(x, y), st(x + 1, y), st(x + 2, y), st(x + 3, y)};
+            }
     }
     // the state behind the run's last chunk is wanted: the final one, or what the gates and ds0 need
     const bool to_the_end = MODE == RUN_OUT ? last && p.last : MODE == RUN_DK;
@@ -101,7 +115,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     const int pieces = to_the_end || L::SUMS || P == 1 ? P : 2;
 
     // ---- a chunk's rows into LDS ----
-    const bool wide_a = wide_rows(ra, sa, d1), wide_b = wide_rows(rb, sb, d1), wide_c = wide_rows(rc, sc, d2), wide_q = wide_rows(q, p.stride_q, p.Dk);
+    const bool wide_a = wide_rows(ra, sa, d1), wide_b = wide_rows(rb, sb, d1), wide_c = wide_rows(rc, sc, d2), wide_q = wide_rows(q, p.stride_q, p.Dk), wide_k = wide_rows(k, p.stride_k, p.Dk);
     auto rows_of = [&](int c, long long& row) {
         row = (long long)(BACK ? chunks - 1 - c : c) * kChunk;
         return seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
@@ -119,10 +133,8 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         if constexpr (L::FOUR) load_tile<T, D2, W, BACK>(tq, q + row * p.stride_q, p.stride_q, rows, d2, wide_q);
         // cum_hi, cum_lo, f, w, whole; backwards: rows turned round, f and w the other way round
         const float* from = gates + (long long)(BACK ? chunks - 1 - c : c) * p.Hv * kRowFloats;
-        for (int at = threadIdx.x; at < 257; at += 64 * W) {
-            const int i = at & 63;
-            cum_hi[at] = from[!BACK || at >= 256 ? at : (at < 128 ? at - i : 320 - (at - i)) + (i < rows ? rows - 1 - i : i)];
-        }
+        const int i = again(lane0);
+        for (int n = wave; n < 5; n += W) load_floats(cum_hi + 64 * n, from, 64 * (!BACK || n < 2 || n > 3 ? n : 5 - n) + (BACK && n < 4 && i < rows ? rows - 1 - i : i));
     };
     // what is never written but taken in: pairs above the diagonal, sums of tiles there
     if (wave == 0) {
@@ -144,6 +156,29 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         long long row;
         const int rows = rows_of(c, row);
         const bool more = c + 1 < chunks;
+
+        // Dk: this lane's columns of k, for the gates, on their way while the pairs are computed
+        V4 kr[MODE == RUN_DK ? 4 * VT : 1];
+        if constexpr (MODE == RUN_DK) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int u = 0; u < VT; ++u) {
+                    const int i = 16 * t + l, col = col0 + 4 * u;
+                    const T* from = k + (row + rows - 1 - i) * p.stride_k + col;
+                    V4 x = {};
+                    if (strip && i < rows) {
+                        if (wide_k) {
+                            if (col < p.Dk) x = *reinterpret_cast<const V4*>(from);
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (col + r < p.Dk) x[r] = from[r];
+                        }
+                    }
+                    kr[t * VT + u] = x;
+                }
+        }
 
         // ---- pairs, tile by tile, transposed: a lane has one i and four neighbouring j ----
         auto pair_tile = [&](int n) {
@@ -225,11 +260,9 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                         const V4 q4 = *reinterpret_cast<const V4*>(tq + T2::at(i, col0 + 4 * u));
 #pragma unroll
                         for (int r = 0; r < 4; ++r) x += (float)q4[r] * acc[t][u][r];
-                    } else if (i < rows) {
-                        const T* kr = k + (row + rows - 1 - i) * p.stride_k + col0 + 4 * u;
+                    } else {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (col0 + 4 * u + r < p.Dk) x += (float)kr[r] * acc[t][u][r];
+                        for (int r = 0; r < 4; ++r) x += (float)kr[t * VT + u][r] * acc[t][u][r];
                     }
                 }
                 x += __shfl_xor(x, 16);
@@ -316,7 +349,6 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                 if (lane < rows) p.gate_k[(seg.row0 + row + rows - 1 - lane) * p.Hv + head] = lane < 63 ? next : 0.0f;
             }
         }
-        if (more) load(c + 1);   // over the tiles; the pairs and the sums lie beside them
         if (strip && col0 < d2) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -332,6 +364,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                 }
             }
         }
+        if (more) load(c + 1);   // over the tiles; the pairs and the sums lie beside them
         wait_loads();
         __syncthreads();
     }
@@ -352,17 +385,18 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     if constexpr (MODE == RUN_DK) {
         // the gradient of the state in front of the segment: ds0 of its sequence, and its product with that state for the gates
         const StateAt st = first ? StateAt{p.s0 ? p.s0 + of_seq : nullptr, p.Dk, p.Dv, p.Dv} : StateAt{p.seg_state + of_seg, DK, DV, DV};
+        const bool wide_ds0 = p.Dv % 4 == 0 && reinterpret_cast<uintptr_t>(p.ds0) % 16 == 0;
         float x = 0.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int u = 0; u < VT; ++u)
+            for (int u = 0; u < VT; ++u) {
+                const int vv = column_of(t, 4 * g), dd = column_of(n0 + u, l);
+                const F32x4 y = st.four(dd, vv);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int vv = column_of(t, 4 * g + r), dd = column_of(n0 + u, l);
-                    x += st(dd, vv) * M[t][u][r];
-                    if (first && p.ds0 && dd < p.Dk && vv < p.Dv) p.ds0[of_seq + (long long)dd * p.Dv + vv] = M[t][u][r];
-                }
+                for (int r = 0; r < 4; ++r) x += y[r] * M[t][u][r];
+                if (first && p.ds0 && dd < p.Dk && vv < p.Dv) store_four<float>(p.ds0 + of_seq + (long long)dd * p.Dv + vv, M[t][u], p.Dv - vv, wide_ds0);
+            }
         x = group_sum(x);
         x += __shfl_xor(x, 16);
         x += __shfl_xor(x, 32);
