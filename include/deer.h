@@ -249,7 +249,7 @@ deer_status deer_linrec_solve_static(int32_t dtype, int32_t B, int32_t T, int32_
  *     one.  Rows that belong to no sequence are neither read nor written.  Bounds outside 0 .. T are clamped;
  *     packed bounds that decrease give results without meaning, within the arrays.
  *   - stride_*: elements from one row to the next (0: dense), so that slices of a wider array can be handed in; the
- *     last dimension is dense.
+ *     last dimension is dense (deer_diagrec_solve(), deer_diagrec_grad(): at most 2^22).
  *   - Pointers are aligned to the element; where all rows are aligned to more, wider loads are used.  Outputs must not overlap
  *     inputs, except where an operator says so.
  *   - What is NaN or infinite in a sequence stays in that sequence. */

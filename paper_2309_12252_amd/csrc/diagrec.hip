@@ -78,43 +78,57 @@ __device__ __forceinline__ void wait_words(const unsigned long long* p, long lon
     }
 }
 
-template <typename S, int V> struct Carry;
-// fold of tiles first .. last - 1 (count of them) into h
-template <int V>
-__device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long long step, int count, bool first_resets, float (&h)[V]) {
+// V values of a row as the bits that they were read as: arrays of 16-bit values would be kept a register each
+template <int BYTES> struct Bits;
+template <> struct Bits<2> { using type = unsigned short; };
+template <> struct Bits<4> { using type = unsigned; };
+template <> struct Bits<8> { using type = unsigned long long; };
+template <typename T, int V> using bits_t = typename Bits<sizeof(T) * V>::type;
+template <typename T, int V>
+__device__ __forceinline__ wide_t<T> value_of(bits_t<T, V> b, int v) {
+    if constexpr (sizeof(T) == 2 && V == 2) {
+        const unsigned short h = (unsigned short)(v == 0 ? b : b >> 16);
+        return (wide_t<T>)__builtin_bit_cast(T, h);
+    } else if constexpr (sizeof(T) == 4 && V == 2) {
+        return __builtin_bit_cast(T, (unsigned)(v == 0 ? b : b >> 32));
+    } else {
+        return (wide_t<T>)__builtin_bit_cast(T, b);
+    }
+}
+// the compiler is not to keep what it derived from x: what is needed again is computed again
+template <typename X>
+__device__ __forceinline__ void forget(X& x) {
+    asm volatile("" : "+v"(x));
+}
+
+// fold of `count` tiles' maps into h
+__device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long long step, int count, bool first_resets, float& h) {
     constexpr int K = 8;
     for (int at = 0; at < count; at += K) {
         const int some = count - at < K ? count - at : K;
+        unsigned long long w[K];
+        wait_words<K>(agg + (long long)at * step, step, some, w);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            unsigned long long w[K];
-            wait_words<K>(agg + (long long)at * step + v, step, some, w);
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (k < some) {
-                    const float a = __uint_as_float((unsigned)w[k]), u = __uint_as_float((unsigned)(w[k] >> 32));
-                    h[v] = (first_resets && at + k == 0) ? u : a * h[v] + u;
-                }
-        }
+        for (int k = 0; k < K; ++k)
+            if (k < some) {
+                const float a = __uint_as_float((unsigned)w[k]), u = __uint_as_float((unsigned)(w[k] >> 32));
+                h = (first_resets && at + k == 0) ? u : a * h + u;
+            }
     }
 }
-template <int V>
-__device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long long step, int count, bool first_resets, double (&h)[V]) {
+__device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long long step, int count, bool first_resets, double& h) {
     constexpr int K = 4;
     for (int at = 0; at < count; at += K) {
         const int some = count - at < K ? count - at : K;
+        unsigned long long wa[K], wu[K];
+        wait_words<K>(agg + (long long)at * step, step, some, wa);
+        wait_words<K>(agg + (long long)at * step + 1, step, some, wu);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            unsigned long long wa[K], wu[K];
-            wait_words<K>(agg + (long long)at * step + 2 * v, step, some, wa);
-            wait_words<K>(agg + (long long)at * step + 2 * v + 1, step, some, wu);
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (k < some) {
-                    const double a = __longlong_as_double((long long)wa[k]), u = __longlong_as_double((long long)wu[k]);
-                    h[v] = (first_resets && at + k == 0) ? u : a * h[v] + u;
-                }
-        }
+        for (int k = 0; k < K; ++k)
+            if (k < some) {
+                const double a = __longlong_as_double((long long)wa[k]), u = __longlong_as_double((long long)wu[k]);
+                h = (first_resets && at + k == 0) ? u : a * h + u;
+            }
     }
 }
 
@@ -124,7 +138,7 @@ __device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long l
 // order, of its predecessors' maps since the last group of kGroup tiles and that group's carry, so two runs give the
 // same bits.  Tiles are dealt out by a ticket in the order of the rows: a tile waits for tiles that are running or done only.
 template <typename T, int KIND, int V, int R, int W, bool REV, bool DROP>
-__global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) {
+__global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams p) {
     using S = wide_t<T>;
     using TV = vec_t<T, V>;
     constexpr int C = 64 * V;     // channels of a tile
@@ -132,7 +146,7 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
     constexpr int WORDS = sizeof(S) == 8 ? 2 : 1;
     static_assert(R + 1 <= 64 && R % 8 == 0, "a lane looks up one row's sequence; the mask's blocks are eight rows");
     __shared__ S sh_a[W][C], sh_h[W][C], sh_carry[C];
-    __shared__ int sh_reset[W];
+    __shared__ int sh_reset[W], sh_begin;
     __shared__ unsigned sh_ticket;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (threadIdx.x == 0) sh_ticket = atomicAdd(p.ticket, 1u);
@@ -144,7 +158,8 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
     const int n = (int)(rest / dgroups);
     const int ch = (int)(rest % dgroups) * C + lane * V;
     const bool on = ch < p.D;
-    const int chl = on ? ch : 0;                       // lanes without a channel read the first one's and write nothing
+    const int chl = on ? ch : 0;                       // (lanes without a channel look at the first one's states, and write nothing)
+    const int col = on ? ch * (int)sizeof(T) : kNoColumn;
     const long long tile_row = (long long)(REV ? p.chunks - 1 - c : c) * L;
     const long long row0 = tile_row + (REV ? W - 1 - wave : wave) * R;
 
@@ -177,20 +192,24 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
 
     // ---- the rows' inputs, all reads at a time ----
     constexpr bool NEED_X = !REV || KIND == DEER_GATE_SIGMOID;
-    TV rg[R], rx[NEED_X ? R : 1], rh[REV ? R : 1], rd[REV ? R : 1];
+    using B = bits_t<T, V>;
+    B rg[R], rx[NEED_X ? R : 1], rh[REV ? R : 1], rd[REV ? R : 1];
     unsigned keep[DROP ? V : 1];
     if (live_bits) {
         const int first = __builtin_ctzll(live_bits), last = 63 - __builtin_clzll(live_bits);
+        const long long r0 = base + row0;
+        const int ahead = row0 > 0 ? 1 : 0;              // (the row in front of the first is h0's)
+        const RowsAt ag(g + r0 * p.stride_gate, p.stride_gate), ax(x + r0 * p.stride_in, p.stride_in);
+        const RowsAt ad(reinterpret_cast<const T*>(p.dh) + r0 * p.stride_out, p.stride_out);
+        const RowsAt ah(reinterpret_cast<const T*>(p.h) + (r0 - ahead) * p.stride_out, p.stride_out);
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int jj = j < first ? first : j > last ? last : j;      // a row that is none reads the nearest
-            const long long r = base + row0 + jj;
-            rg[j] = *reinterpret_cast<const TV*>(g + r * p.stride_gate + chl);
-            if constexpr (NEED_X) rx[j] = *reinterpret_cast<const TV*>(x + r * p.stride_in + chl);
+            rg[j] = ag.template load<B>(col, jj);
+            if constexpr (NEED_X) rx[j] = ax.template load<B>(col, jj);
             if constexpr (REV) {
-                rd[j] = *reinterpret_cast<const TV*>(reinterpret_cast<const T*>(p.dh) + r * p.stride_out + chl);
-                const long long rb = r > base ? r - 1 : r;               // (the row in front of the first is h0's)
-                rh[j] = *reinterpret_cast<const TV*>(reinterpret_cast<const T*>(p.h) + rb * p.stride_out + chl);
+                rd[j] = ad.template load<B>(col, jj);
+                rh[j] = ah.template load<B>(col, jj - 1 + ahead > 0 ? jj - 1 + ahead : 0);
             }
         }
         if constexpr (DROP) {
@@ -205,7 +224,7 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
     }
     const S scale = DROP ? (S)p.drop.scale : S(1);
     auto input = [&](int j, int v) -> S {
-        S xv = (S)vec_at<T, V>(rx[j], v);
+        S xv = value_of<T, V>(rx[j], v);
         if constexpr (DROP) xv = (keep[v] >> j) & 1u ? xv * scale : S(0);
         return xv;
     };
@@ -229,8 +248,8 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 S a, w;
-                gate_factors<T, KIND>((S)vec_at<T, V>(rg[j], v), a, w);
-                if constexpr (REV) H[v] = a * ((S)vec_at<T, V>(rd[j], v) + H[v]);
+                gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
+                if constexpr (REV) H[v] = a * (value_of<T, V>(rd[j], v) + H[v]);
                 else H[v] = a * H[v] + w * input(j, v);
                 A[v] *= a;
             }
@@ -242,84 +261,82 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
         sh_h[wave][lane * V + v] = H[v];
     }
     if (lane == 0) sh_reset[wave] = starts != 0;
-    __syncthreads();
-
-    // ---- the first wavefront publishes the tile's map and finds its carry ----
     if (wave == 0) {
-        S ta[V], th[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            ta[v] = A[v];
-            th[v] = H[v];
-        }
-        bool reset = starts != 0;
-        for (int w = 1; w < W; ++w) {
-            const bool r = sh_reset[w] != 0;
-            reset = reset || r;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const S a = sh_a[w][lane * V + v], h = sh_h[w][lane * V + v];
-                th[v] = r ? h : a * th[v] + h;
-                ta[v] *= a;
-            }
-        }
-        const long long D = p.D;
-        unsigned long long* agg = p.agg + ((long long)n * p.chunks * D + ch) * WORDS;
-        unsigned long long* inc = p.inc + (long long)n * p.groups * D + ch;
-        if (on) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if constexpr (WORDS == 1) {
-                    put_word(agg + (long long)c * D + v, word_of(ta[v], th[v]));
-                } else {
-                    put_word(agg + ((long long)c * D + v) * 2, word_of(ta[v]));
-                    put_word(agg + ((long long)c * D + v) * 2 + 1, word_of(th[v]));
-                }
-            }
-        }
-        S carry[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) carry[v] = S(0);
-        constexpr int j0 = REV ? R - 1 : 0;            // the tile's first row along the scan
+        constexpr int j0 = REV ? R - 1 : 0;   // the tile's first row along the scan
+        int begin_c = -1;
         if (((live_bits >> j0) & 1) && !((starts >> j0) & 1)) {
-            // the tile in which the sequence of that row began
             long long begin;
             if (!p.rows.packed) begin = REV ? seq_length(p.rows, n) - 1 : 0;
             else {
                 const int s = __builtin_amdgcn_readlane(seq, j0);
                 begin = REV ? clamp_row(p.rows.bounds[s + 1], p.rows.T) - 1 : clamp_row(p.rows.bounds[s], p.rows.T);
             }
-            const int c_first = (int)(REV ? p.chunks - 1 - begin / L : begin / L);
+            begin_c = (int)(REV ? p.chunks - 1 - begin / L : begin / L);
+            if (begin_c < 0) begin_c = 0;     // (bounds that decrease)
+        }
+        if (lane == 0) sh_begin = begin_c;
+    }
+    __syncthreads();
+
+    // ---- the first V wavefronts publish the tile's map and find its carry, a channel a lane ----
+    if (wave < V) {
+        const int tc = 64 * wave + lane, tch = (int)(rest % dgroups) * C + tc;
+        const bool has = tch < p.D;
+        S ta = sh_a[0][tc], th = sh_h[0][tc];
+        bool reset = sh_reset[0] != 0;
+        for (int w = 1; w < W; ++w) {
+            const bool r = sh_reset[w] != 0;
+            reset = reset || r;
+            const S a = sh_a[w][tc], h = sh_h[w][tc];
+            th = r ? h : a * th + h;
+            ta *= a;
+        }
+        const long long D = p.D;
+        unsigned long long* agg = p.agg + ((long long)n * p.chunks * D + tch) * WORDS;
+        unsigned long long* inc = p.inc + (long long)n * p.groups * D + tch;
+        if (has) {
+            if constexpr (WORDS == 1) {
+                put_word(agg + (long long)c * D, word_of(ta, th));
+            } else {
+                put_word(agg + (long long)c * D * 2, word_of(ta));
+                put_word(agg + (long long)c * D * 2 + 1, word_of(th));
+            }
+        }
+        S carry = S(0);
+        const int begin_c = sh_begin;       // the tile in which the sequence of the tile's first row began; -1: this one needs no carry
+        if (begin_c >= 0 && has) {
             const int c_group = c / kGroup * kGroup;
-            const bool from_group = c_first < c_group;
-            const int from = from_group ? c_group : (c_first < c ? c_first : c);
-            if (on) {
-                if (from_group) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        unsigned long long w[1];
-                        wait_words<1>(inc + (long long)(c / kGroup - 1) * D + v, 0, 1, w);
-                        if constexpr (WORDS == 1) carry[v] = __uint_as_float((unsigned)(w[0] >> 32));
-                        else carry[v] = __longlong_as_double((long long)w[0]);
-                    }
-                }
-                fold_tiles<V>(agg + (long long)from * D * WORDS, D * WORDS, c - from, !from_group, carry);
+            const bool from_group = begin_c < c_group;
+            const int from = from_group ? c_group : (begin_c < c ? begin_c : c);
+            if (from_group) {
+                unsigned long long w[1];
+                wait_words<1>(inc + (long long)(c / kGroup - 1) * D, 0, 1, w);
+                if constexpr (WORDS == 1) carry = __uint_as_float((unsigned)(w[0] >> 32));
+                else carry = __longlong_as_double((long long)w[0]);
             }
+            fold_tiles(agg + (long long)from * D * WORDS, D * WORDS, c - from, !from_group, carry);
         }
-        if (on && c % kGroup == kGroup - 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const S out = reset ? th[v] : ta[v] * carry[v] + th[v];
-                if constexpr (WORDS == 1) put_word(inc + (long long)(c / kGroup) * D + v, word_of(0.0f, out));
-                else put_word(inc + (long long)(c / kGroup) * D + v, word_of(out));
-            }
+        if (has && c % kGroup == kGroup - 1) {
+            const S out = reset ? th : ta * carry + th;
+            if constexpr (WORDS == 1) put_word(inc + (long long)(c / kGroup) * D, word_of(0.0f, out));
+            else put_word(inc + (long long)(c / kGroup) * D, word_of(out));
         }
-#pragma unroll
-        for (int v = 0; v < V; ++v) sh_carry[lane * V + v] = carry[v];
+        sh_carry[tc] = carry;
     }
     __syncthreads();
 
     // ---- the rows once more, from the carry ----
+    const RowsAt oh(reinterpret_cast<const T*>(p.h) + (base + row0) * p.stride_out, p.stride_out);
+    const RowsAt odg(reinterpret_cast<const T*>(p.dg) + (base + row0) * p.stride_gate, p.stride_gate);
+    const RowsAt odx(reinterpret_cast<const T*>(p.dx) + (base + row0) * p.stride_in, p.stride_in);
+    if (live_bits) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            forget(rg[j]);
+            if constexpr (NEED_X) forget(rx[j]);
+            if constexpr (REV) forget(rd[j]);
+        }
+    }
     S h[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = sh_carry[lane * V + v];
@@ -332,7 +349,6 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
     for (int i = 0; i < R; ++i) {
         const int j = REV ? R - 1 - i : i;
         if (!((live_bits >> j) & 1)) continue;
-        const long long r = base + row0 + j;
         if ((starts >> j) & 1) {
             const long long s = __builtin_amdgcn_readlane(seq, j);
 #pragma unroll
@@ -347,15 +363,15 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
                 for (int v = 0; v < V; ++v) before[v] = p.h0 ? reinterpret_cast<const S*>(p.h0)[s * p.D + chl + v] : S(0);
             } else {
 #pragma unroll
-                for (int v = 0; v < V; ++v) before[v] = (S)vec_at<T, V>(rh[j], v);
+                for (int v = 0; v < V; ++v) before[v] = value_of<T, V>(rh[j], v);
             }
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             S a, w;
-            gate_factors<T, KIND>((S)vec_at<T, V>(rg[j], v), a, w);
+            gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
             if constexpr (REV) {
-                const S lam = (S)vec_at<T, V>(rd[j], v) + h[v];
+                const S lam = value_of<T, V>(rd[j], v) + h[v];
                 h[v] = a * lam;
                 S dg, du = lam;
                 if constexpr (KIND == DEER_GATE_FACTOR) dg = lam * before[v];
@@ -372,13 +388,13 @@ __global__ __launch_bounds__(64 * W) void diagrec_kernel(const DiagrecParams p) 
                 vec_set<T, V>(o1, v, (T)h[v]);
             }
         }
+        if constexpr (REV) {
+            odg.store(o1, col, j);
+            odx.store(o2, col, j);
+        } else {
+            oh.store(o1, col, j);
+        }
         if (on) {
-            if constexpr (REV) {
-                *reinterpret_cast<TV*>(reinterpret_cast<T*>(p.dg) + r * p.stride_gate + ch) = o1;
-                *reinterpret_cast<TV*>(reinterpret_cast<T*>(p.dx) + r * p.stride_in + ch) = o2;
-            } else {
-                *reinterpret_cast<TV*>(reinterpret_cast<T*>(p.h) + r * p.stride_out + ch) = o1;
-            }
             if (((ends >> j) & 1) && fin) {
                 const long long s = __builtin_amdgcn_readlane(seq, j);
 #pragma unroll

@@ -62,7 +62,7 @@ const char* bad_config(const deer_diagrec_config* c, bool step) {
 }
 bool too_large(const deer_diagrec_config* c) {
     const long long seqs = c->packed ? 1 : c->N;
-    if (c->T > kMostRows) return true;
+    if (c->T > kMostRows || c->D > kMostStride || c->stride_gate > kMostStride || c->stride_in > kMostStride || c->stride_out > kMostStride) return true;
     const long long tiles = (c->T + 63) / 64, cols = (c->D + 63) / 64;   // (the smallest tiles of any type)
     return (long double)tiles * cols * seqs > 2147483647.0L || (long double)c->N * c->D > 1e15L;
 }
@@ -230,7 +230,7 @@ extern "C" {
 deer_status deer_diagrec_workspace_bytes(const deer_diagrec_config* c, int32_t grad, size_t* bytes) {
     if (!bytes) return fail(DEER_ERR_INVALID_ARG, "bytes is NULL");
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
-    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds");
+    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
     *bytes = diag_layout(c, grad != 0).total;
     return DEER_OK;
 }
@@ -238,7 +238,7 @@ deer_status deer_diagrec_workspace_bytes(const deer_diagrec_config* c, int32_t g
 deer_status deer_diagrec_solve(const deer_diagrec_config* c, const void* d_gate, const void* d_in, const void* d_h0, const int64_t* d_bounds,
                                void* d_h, void* d_last, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
-    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds");
+    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
     if ((c->T > 0 && (!d_gate || !d_in || !d_h)) || (c->packed && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
     if (misaligned(d_gate, e) || misaligned(d_in, e) || misaligned(d_h, e) || misaligned(d_h0, w) || misaligned(d_last, w) || misaligned(d_bounds, 8))
@@ -258,7 +258,7 @@ deer_status deer_diagrec_grad(const deer_diagrec_config* c, const void* d_gate, 
                               const void* d_h, const void* d_dh, const void* d_dlast, void* d_dgate, void* d_din, void* d_dh0,
                               void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
-    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds");
+    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
     if ((c->T > 0 && (!d_gate || !d_in || !d_h || !d_dh || !d_dgate || !d_din)) || (c->packed && !d_bounds))
         return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;

@@ -17,7 +17,7 @@ def diag(**kw):
 @pytest.mark.parametrize("change,status", [
     (dict(dtype=4), 1), (dict(dtype=-1), 1), (dict(gate=3), 1), (dict(N=0), 1), (dict(D=0), 1), (dict(T=-1), 1), (dict(packed=2), 1),
     (dict(stride_in=7), 1), (dict(stride_out=-8), 1), (dict(drop=-0.5), 1), (dict(drop=1.0), 1), (dict(drop=float("nan")), 1),
-    (dict(T=(1 << 33) + 1), 2), (dict(N=2000000000, T=1 << 20), 2)])
+    (dict(T=(1 << 33) + 1), 2), (dict(N=2000000000, T=1 << 20), 2), (dict(stride_in=(1 << 22) + 1), 2)])
 def test_diagrec_refuses(change, status):
     lib, cfg, size = deer.load_library(), diag(**change), ctypes.c_size_t(0)
     assert lib.deer_diagrec_workspace_bytes(ctypes.byref(cfg), 0, ctypes.byref(size)) == status
