@@ -6,6 +6,8 @@
 // Backward: with mu_{T+1} = dL/dh_T of the final state, lambda_t = dh_t + mu_{t+1} and mu_t = a_t lambda_t,
 //   dL/da_t = lambda_t h_{t-1}   dL/du_t = lambda_t   dL/dh_0 = mu_1,
 // again a recurrence of the same form, mu_t = a_t mu_{t+1} + a_t dh_t, along the reversed rows.
+#include <type_traits>
+
 #include "seq_common.h"
 
 namespace deer {
@@ -35,13 +37,15 @@ __device__ __forceinline__ void gate_factors(wide_t<T> g, wide_t<T>& a, wide_t<T
     } else if constexpr (KIND == DEER_GATE_LOG) {
         a = sizeof(T) == 2 ? fast_exp(g) : exp(g);
         w = S(1);
-    } else {   // both a and 1 - a without cancellation
+    } else if constexpr (sizeof(T) == 2) {   // both a and 1 - a without cancellation; 2^126 stands for what is more (a NaN stays one)
+        float t = g * -1.442695041f;
+        t = t > 126.0f ? 126.0f : t;
+        const float e = __builtin_amdgcn_exp2f(t);
+        a = __builtin_amdgcn_rcpf(1.0f + e);
+        w = e * a;
+    } else {
         const S m = g < S(0) ? g : -g;
-        const S e = sizeof(T) == 2 ? fast_exp(m) : exp(m);
-        S r;
-        if constexpr (sizeof(T) == 2) r = __builtin_amdgcn_rcpf(S(1) + e);
-        else r = S(1) / (S(1) + e);
-        const S er = e * r;
+        const S e = exp(m), r = S(1) / (S(1) + e), er = e * r;
         a = g < S(0) ? er : r;
         w = g < S(0) ? r : er;
     }
@@ -236,25 +240,32 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
         A[v] = S(1);
         H[v] = S(0);
     }
+    // PLAIN: all rows are live and none begins or ends a sequence, the ordinary case inside a long one
+    const bool plain = live_bits == (1ull << R) - 1 && !starts && !ends;
+    auto first_pass = [&](auto all) {
+        constexpr bool PLAIN = decltype(all)::value;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int j = REV ? R - 1 - i : i;
-        if ((starts >> j) & 1) {
-            const long long s = __builtin_amdgcn_readlane(seq, j);
-#pragma unroll
-            for (int v = 0; v < V; ++v) H[v] = init ? init[s * p.D + chl + v] : S(0);
-        }
-        if ((live_bits >> j) & 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                S a, w;
-                gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
-                if constexpr (REV) H[v] = a * (value_of<T, V>(rd[j], v) + H[v]);
-                else H[v] = a * H[v] + w * input(j, v);
-                A[v] *= a;
+        for (int i = 0; i < R; ++i) {
+            const int j = REV ? R - 1 - i : i;
+            if (!PLAIN && ((starts >> j) & 1)) {
+                const long long s = __builtin_amdgcn_readlane(seq, j);
+    #pragma unroll
+                for (int v = 0; v < V; ++v) H[v] = init ? init[s * p.D + chl + v] : S(0);
+            }
+            if (PLAIN || ((live_bits >> j) & 1)) {
+    #pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    S a, w;
+                    gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
+                    if constexpr (REV) H[v] = a * (value_of<T, V>(rd[j], v) + H[v]);
+                    else H[v] = a * H[v] + w * input(j, v);
+                    A[v] *= a;
+                }
             }
         }
-    }
+    };
+    if (plain) first_pass(std::true_type{});
+    else first_pass(std::false_type{});
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         sh_a[wave][lane * V + v] = A[v];
@@ -345,63 +356,68 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = r ? sh_h[w][lane * V + v] : sh_a[w][lane * V + v] * h[v] + sh_h[w][lane * V + v];
     }
+    auto second_pass = [&](auto all) {
+        constexpr bool PLAIN = decltype(all)::value;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int j = REV ? R - 1 - i : i;
-        if (!((live_bits >> j) & 1)) continue;
-        if ((starts >> j) & 1) {
-            const long long s = __builtin_amdgcn_readlane(seq, j);
-#pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = init ? init[s * p.D + chl + v] : S(0);
-        }
-        TV o1, o2;
-        S before[V];
-        if constexpr (REV) {
-            if ((ends >> j) & 1) {   // the row in front of the sequence's first is the initial state
+        for (int i = 0; i < R; ++i) {
+            const int j = REV ? R - 1 - i : i;
+            if (!PLAIN && !((live_bits >> j) & 1)) continue;
+            if (!PLAIN && ((starts >> j) & 1)) {
                 const long long s = __builtin_amdgcn_readlane(seq, j);
-#pragma unroll
-                for (int v = 0; v < V; ++v) before[v] = p.h0 ? reinterpret_cast<const S*>(p.h0)[s * p.D + chl + v] : S(0);
-            } else {
-#pragma unroll
-                for (int v = 0; v < V; ++v) before[v] = value_of<T, V>(rh[j], v);
+    #pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = init ? init[s * p.D + chl + v] : S(0);
             }
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            S a, w;
-            gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
+            TV o1, o2;
+            S before[V];
             if constexpr (REV) {
-                const S lam = value_of<T, V>(rd[j], v) + h[v];
-                h[v] = a * lam;
-                S dg, du = lam;
-                if constexpr (KIND == DEER_GATE_FACTOR) dg = lam * before[v];
-                else if constexpr (KIND == DEER_GATE_LOG) dg = h[v] * before[v];
-                else {
-                    dg = h[v] * w * (before[v] - input(j, v));
-                    du = w * lam;
+                if (!PLAIN && ((ends >> j) & 1)) {   // the row in front of the sequence's first is the initial state
+                    const long long s = __builtin_amdgcn_readlane(seq, j);
+    #pragma unroll
+                    for (int v = 0; v < V; ++v) before[v] = p.h0 ? reinterpret_cast<const S*>(p.h0)[s * p.D + chl + v] : S(0);
+                } else {
+    #pragma unroll
+                    for (int v = 0; v < V; ++v) before[v] = value_of<T, V>(rh[j], v);
                 }
-                if constexpr (DROP) du = (keep[v] >> j) & 1u ? du * scale : S(0);
-                vec_set<T, V>(o1, v, (T)dg);
-                vec_set<T, V>(o2, v, (T)du);
+            }
+    #pragma unroll
+            for (int v = 0; v < V; ++v) {
+                S a, w;
+                gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
+                if constexpr (REV) {
+                    const S lam = value_of<T, V>(rd[j], v) + h[v];
+                    h[v] = a * lam;
+                    S dg, du = lam;
+                    if constexpr (KIND == DEER_GATE_FACTOR) dg = lam * before[v];
+                    else if constexpr (KIND == DEER_GATE_LOG) dg = h[v] * before[v];
+                    else {
+                        dg = h[v] * w * (before[v] - input(j, v));
+                        du = w * lam;
+                    }
+                    if constexpr (DROP) du = (keep[v] >> j) & 1u ? du * scale : S(0);
+                    vec_set<T, V>(o1, v, (T)dg);
+                    vec_set<T, V>(o2, v, (T)du);
+                } else {
+                    h[v] = a * h[v] + w * input(j, v);
+                    vec_set<T, V>(o1, v, (T)h[v]);
+                }
+            }
+            if constexpr (REV) {
+                odg.store(o1, col, j);
+                odx.store(o2, col, j);
             } else {
-                h[v] = a * h[v] + w * input(j, v);
-                vec_set<T, V>(o1, v, (T)h[v]);
+                oh.store(o1, col, j);
+            }
+            if (!PLAIN && on) {
+                if (((ends >> j) & 1) && fin) {
+                    const long long s = __builtin_amdgcn_readlane(seq, j);
+    #pragma unroll
+                    for (int v = 0; v < V; ++v) fin[s * p.D + ch + v] = h[v];
+                }
             }
         }
-        if constexpr (REV) {
-            odg.store(o1, col, j);
-            odx.store(o2, col, j);
-        } else {
-            oh.store(o1, col, j);
-        }
-        if (on) {
-            if (((ends >> j) & 1) && fin) {
-                const long long s = __builtin_amdgcn_readlane(seq, j);
-#pragma unroll
-                for (int v = 0; v < V; ++v) fin[s * p.D + ch + v] = h[v];
-            }
-        }
-    }
+    };
+    if (plain) second_pass(std::true_type{});
+    else second_pass(std::false_type{});
 }
 
 // Clears the published words and the ticket, and gives sequences without rows their final state (in the gradient: the
