@@ -269,13 +269,13 @@ typedef struct {
 } deer_diagrec_config;
 
 /* Bytes of device workspace (256-byte aligned) that deer_diagrec_solve() (grad = 0) or deer_diagrec_grad() (grad = 1) needs: some
- * 8 bytes a channel for every 64 or 128 rows. */
+ * 8 bytes a channel for every 64 to 256 rows (fp64: 16). */
 deer_status deer_diagrec_workspace_bytes(const deer_diagrec_config* cfg, int32_t grad, size_t* bytes);
 
 /* Gated linear recurrence, a state for every channel: h_t = a_t h_{t-1} + u_t, u_t = x_t (DEER_GATE_SIGMOID: (1 - a_t) x_t), x after dropout.
  *   d_gate, d_in  in  [rows, D]      d_h0  in  [N, D] or NULL (zeros)
  *   d_h           out [rows, D] (may be d_in, with the same stride)      d_last  out [N, D] state behind every sequence's last row, or NULL
- * One pass over the data; two calls with the same inputs return the same bits.  The product of the factors over 128 rows has to be
+ * One pass over the data; two calls with the same inputs return the same bits.  The product of the factors over 256 rows has to be
  * representable (gates that make the state grow can overflow it). */
 deer_status deer_diagrec_solve(const deer_diagrec_config* cfg, const void* d_gate, const void* d_in, const void* d_h0,
                                const int64_t* d_bounds, void* d_h, void* d_last, void* d_workspace, size_t workspace_bytes,

@@ -21,7 +21,7 @@ constexpr long long kPolls = 1ll << 22;           // polls before a tile gives u
 template <typename T, bool REV> struct Shape {
     static constexpr int W = 8;
     static constexpr int V = sizeof(T) == 8 ? 1 : 2;
-    static constexpr int R = (REV && sizeof(T) > 2) ? 8 : 16;
+    static constexpr int R = sizeof(T) == 2 ? (REV ? 16 : 32) : REV ? 8 : 16;
 };
 
 template <typename T> __device__ __forceinline__ T fast_exp(T v) { return exp(v); }
@@ -98,6 +98,12 @@ __device__ __forceinline__ wide_t<T> value_of(bits_t<T, V> b, int v) {
     } else {
         return (wide_t<T>)__builtin_bit_cast(T, b);
     }
+}
+template <typename T, int V, bool DROP>
+__device__ __forceinline__ wide_t<T> input_of(bits_t<T, V> b, int v, unsigned kept, wide_t<T> scale) {
+    const wide_t<T> x = value_of<T, V>(b, v);
+    if constexpr (DROP) return kept ? x * scale : wide_t<T>(0);
+    else return x;
 }
 // the compiler is not to keep what it derived from x: what is needed again is computed again
 template <typename X>
@@ -198,7 +204,7 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
     constexpr bool NEED_X = !REV || KIND == DEER_GATE_SIGMOID;
     using B = bits_t<T, V>;
     B rg[R], rx[NEED_X ? R : 1], rh[REV ? R : 1], rd[REV ? R : 1];
-    unsigned keep[DROP ? V : 1];
+    unsigned keep[DROP ? V : 1] = {};
     if (live_bits) {
         const int first = __builtin_ctzll(live_bits), last = 63 - __builtin_clzll(live_bits);
         const long long r0 = base + row0;
@@ -206,14 +212,21 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
         const RowsAt ag(g + r0 * p.stride_gate, p.stride_gate), ax(x + r0 * p.stride_in, p.stride_in);
         const RowsAt ad(reinterpret_cast<const T*>(p.dh) + r0 * p.stride_out, p.stride_out);
         const RowsAt ah(reinterpret_cast<const T*>(p.h) + (r0 - ahead) * p.stride_out, p.stride_out);
+        // a row that is none reads the nearest one that is
+        int at_g = col + first * ag.pitch, at_x = col + first * ax.pitch, at_d = col + first * ad.pitch, at_h = col + (first + ahead > 0 ? first + ahead - 1 : 0) * ad.pitch;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int jj = j < first ? first : j > last ? last : j;      // a row that is none reads the nearest
-            rg[j] = ag.template load<B>(col, jj);
-            if constexpr (NEED_X) rx[j] = ax.template load<B>(col, jj);
+            rg[j] = ag.template load<B>(at_g);
+            if constexpr (NEED_X) rx[j] = ax.template load<B>(at_x);
             if constexpr (REV) {
-                rd[j] = ad.template load<B>(col, jj);
-                rh[j] = ah.template load<B>(col, jj - 1 + ahead > 0 ? jj - 1 + ahead : 0);
+                rd[j] = ad.template load<B>(at_d);
+                rh[j] = ah.template load<B>(at_h);
+            }
+            if (j >= first && j < last) {
+                at_g += ag.pitch;
+                at_x += ax.pitch;
+                at_d += ad.pitch;
+                if (j + ahead > 0) at_h += ad.pitch;
             }
         }
         if constexpr (DROP) {
@@ -227,12 +240,6 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
         }
     }
     const S scale = DROP ? (S)p.drop.scale : S(1);
-    auto input = [&](int j, int v) -> S {
-        S xv = value_of<T, V>(rx[j], v);
-        if constexpr (DROP) xv = (keep[v] >> j) & 1u ? xv * scale : S(0);
-        return xv;
-    };
-
     // ---- this wavefront's map ----
     S A[V], H[V];
 #pragma unroll
@@ -242,23 +249,23 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
     }
     // PLAIN: all rows are live and none begins or ends a sequence, the ordinary case inside a long one
     const bool plain = live_bits == (1ull << R) - 1 && !starts && !ends;
-    auto first_pass = [&](auto all) {
+    auto first_pass = [&](auto all) __attribute__((always_inline)) {
         constexpr bool PLAIN = decltype(all)::value;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int j = REV ? R - 1 - i : i;
             if (!PLAIN && ((starts >> j) & 1)) {
                 const long long s = __builtin_amdgcn_readlane(seq, j);
-    #pragma unroll
+#pragma unroll
                 for (int v = 0; v < V; ++v) H[v] = init ? init[s * p.D + chl + v] : S(0);
             }
             if (PLAIN || ((live_bits >> j) & 1)) {
-    #pragma unroll
+#pragma unroll
                 for (int v = 0; v < V; ++v) {
                     S a, w;
                     gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
                     if constexpr (REV) H[v] = a * (value_of<T, V>(rd[j], v) + H[v]);
-                    else H[v] = a * H[v] + w * input(j, v);
+                    else H[v] = a * H[v] + w * input_of<T, V, DROP>(rx[j], v, (keep[DROP ? v : 0] >> j) & 1u, scale);
                     A[v] *= a;
                 }
             }
@@ -348,23 +355,28 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
             if constexpr (REV) forget(rd[j]);
         }
     }
-    S h[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = sh_carry[lane * V + v];
-    for (int w = 0; w < wave; ++w) {
-        const bool r = sh_reset[w] != 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = r ? sh_h[w][lane * V + v] : sh_a[w][lane * V + v] * h[v] + sh_h[w][lane * V + v];
-    }
-    auto second_pass = [&](auto all) {
+    auto second_pass = [&](auto all) __attribute__((always_inline)) {
         constexpr bool PLAIN = decltype(all)::value;
+        S h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = sh_carry[lane * V + v];
+        for (int w = 0; w < wave; ++w) {
+            const bool r = sh_reset[w] != 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = r ? sh_h[w][lane * V + v] : sh_a[w][lane * V + v] * h[v] + sh_h[w][lane * V + v];
+        }
+        const int pitch_1 = REV ? odg.pitch : oh.pitch, pitch_2 = odx.pitch;
+        int next_1 = col + (REV ? (R - 1) * pitch_1 : 0), next_2 = col + (R - 1) * pitch_2;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int j = REV ? R - 1 - i : i;
+            const int at_1 = next_1, at_2 = next_2;
+            next_1 += REV ? -pitch_1 : pitch_1;
+            next_2 -= pitch_2;
             if (!PLAIN && !((live_bits >> j) & 1)) continue;
             if (!PLAIN && ((starts >> j) & 1)) {
                 const long long s = __builtin_amdgcn_readlane(seq, j);
-    #pragma unroll
+#pragma unroll
                 for (int v = 0; v < V; ++v) h[v] = init ? init[s * p.D + chl + v] : S(0);
             }
             TV o1, o2;
@@ -372,14 +384,14 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
             if constexpr (REV) {
                 if (!PLAIN && ((ends >> j) & 1)) {   // the row in front of the sequence's first is the initial state
                     const long long s = __builtin_amdgcn_readlane(seq, j);
-    #pragma unroll
+#pragma unroll
                     for (int v = 0; v < V; ++v) before[v] = p.h0 ? reinterpret_cast<const S*>(p.h0)[s * p.D + chl + v] : S(0);
                 } else {
-    #pragma unroll
+#pragma unroll
                     for (int v = 0; v < V; ++v) before[v] = value_of<T, V>(rh[j], v);
                 }
             }
-    #pragma unroll
+#pragma unroll
             for (int v = 0; v < V; ++v) {
                 S a, w;
                 gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
@@ -390,27 +402,27 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
                     if constexpr (KIND == DEER_GATE_FACTOR) dg = lam * before[v];
                     else if constexpr (KIND == DEER_GATE_LOG) dg = h[v] * before[v];
                     else {
-                        dg = h[v] * w * (before[v] - input(j, v));
+                        dg = h[v] * w * (before[v] - input_of<T, V, DROP>(rx[j], v, (keep[DROP ? v : 0] >> j) & 1u, scale));
                         du = w * lam;
                     }
                     if constexpr (DROP) du = (keep[v] >> j) & 1u ? du * scale : S(0);
                     vec_set<T, V>(o1, v, (T)dg);
                     vec_set<T, V>(o2, v, (T)du);
                 } else {
-                    h[v] = a * h[v] + w * input(j, v);
+                    h[v] = a * h[v] + w * input_of<T, V, DROP>(rx[j], v, (keep[DROP ? v : 0] >> j) & 1u, scale);
                     vec_set<T, V>(o1, v, (T)h[v]);
                 }
             }
             if constexpr (REV) {
-                odg.store(o1, col, j);
-                odx.store(o2, col, j);
+                odg.store(o1, at_1);
+                odx.store(o2, at_2);
             } else {
-                oh.store(o1, col, j);
+                oh.store(o1, at_1);
             }
             if (!PLAIN && on) {
                 if (((ends >> j) & 1) && fin) {
                     const long long s = __builtin_amdgcn_readlane(seq, j);
-    #pragma unroll
+#pragma unroll
                     for (int v = 0; v < V; ++v) fin[s * p.D + ch + v] = h[v];
                 }
             }
