@@ -274,9 +274,8 @@ def linrec_solve_static(A, b, y0=None, reverse=False, out=None, status=None, str
 _DTYPES = {torch.float32: DEER_F32, torch.float64: DEER_F64, torch.bfloat16: DEER_BF16, torch.float16: DEER_F16}
 
 
-def _need(ok, text):
-    if not ok:
-        raise DeerError(DEER_ERR_INVALID_ARG, text)
+def _refuse(text):
+    raise DeerError(DEER_ERR_INVALID_ARG, text)
 
 
 def _raise(lib, st):
@@ -287,9 +286,11 @@ def _on_stream(f):
     """Runs f with the device of its first argument current, and with its keyword `stream` as that device's current stream."""
     @functools.wraps(f)
     def call(first, *args, stream=None, **kw):
-        _need(isinstance(first, torch.Tensor) and first.is_cuda, "need device tensors")
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            _refuse("need device tensors")
         if stream is not None:
-            _need(stream.device == first.device, "the stream belongs to another device than the tensors")
+            if stream.device != first.device:
+                _refuse("the stream belongs to another device than the tensors")
             with torch.cuda.stream(stream):
                 return f(first, *args, **kw)
         if first.device.index == torch.cuda.current_device():
@@ -299,76 +300,97 @@ def _on_stream(f):
     return call
 
 
-def _stream_of(t):
-    return torch.cuda.current_stream(t.device).cuda_stream
-
-
-def _wide(dtype):
-    return torch.float64 if dtype == torch.float64 else torch.float32
+def _stream_of(device):
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _row_stride(t, what, lead):
-    """Elements from a row of t to the next: the last dimension dense, `lead` leading dimensions that lie like rows one behind another."""
-    _need(t.stride(-1) == 1 or t.shape[-1] <= 1, what + ": the last dimension must be dense")
+    """Elements from a row of t to the next: `lead` leading dimensions that lie like rows one behind another, the dimensions behind them dense."""
+    shape = t.shape
     inner = 1
-    for k in range(t.dim() - 1, lead - 1, -1):
-        _need(t.shape[k] <= 1 or t.stride(k) == inner, what + ": the dimensions behind the rows must be dense")
-        inner *= t.shape[k]
-    if lead == 1:
-        rows, first = t.shape[0], t.stride(0)
-    else:
-        rows, first = t.shape[0] * t.shape[1], t.stride(1) if t.shape[1] > 1 else t.stride(0)
-        _need(t.shape[0] <= 1 or t.shape[1] <= 1 or t.stride(0) == t.shape[1] * t.stride(1), what + ": sequences must lie one behind another")
-    if rows <= 1 or first < inner:
-        _need(rows <= 1 or t.numel() == 0, what + ": rows must not overlap")
+    for n in shape[lead:]:
+        inner *= n
+    if t.is_contiguous():
         return inner
+    strides, dense = t.stride(), 1
+    for k in range(len(shape) - 1, lead - 1, -1):
+        if shape[k] > 1 and strides[k] != dense:
+            _refuse(what + ": the dimensions behind the rows must be dense")
+        dense *= shape[k]
+    if lead == 2 and shape[0] > 1 and shape[1] > 1 and strides[0] != shape[1] * strides[1]:
+        _refuse(what + ": sequences must lie one behind another")
+    first = strides[1] if lead == 2 and shape[1] > 1 else strides[0]
+    if t.numel() == 0 or (shape[0] if lead == 1 else shape[0] * shape[1]) <= 1:
+        return inner
+    if first < inner:
+        _refuse(what + ": rows must not overlap")
     return first
 
 
 def _check_like(t, what, shape, dtype, device):
-    _need(isinstance(t, torch.Tensor) and t.device == device, what + ": need a tensor on the same device")
-    _need(t.dtype == dtype, "%s: need %s, got %s" % (what, dtype, t.dtype))
-    _need(tuple(t.shape) == tuple(shape), "%s: need shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        _refuse(what + ": need a tensor on the same device")
+    if t.dtype is not dtype:
+        _refuse("%s: need %s, got %s" % (what, dtype, t.dtype))
+    if t.shape != shape:
+        _refuse("%s: need shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
 
 
 def _dense(t, what, shape, dtype, device):
+    """pointer of a contiguous tensor, or of none"""
     if t is None:
         return 0
     _check_like(t, what, shape, dtype, device)
-    _need(t.is_contiguous(), what + ": must be contiguous")
+    if not t.is_contiguous():
+        _refuse(what + ": must be contiguous")
     return t.data_ptr()
 
 
 def _rows_of(x, inner, offsets, lengths):
     """(N, T, packed, pointer of the bounds, leading dimensions) of x [N, T, ...] with optional `lengths` int64 [N], or of packed
     rows [rows, ...] with `offsets` int64 [N + 1]"""
+    shape = x.shape
     if offsets is not None:
-        _need(lengths is None, "offsets (packed rows) and lengths (a padded batch) exclude each other")
-        _need(x.dim() == 1 + inner, "packed rows have no dimension for the sequences")
-        _need(offsets.dim() == 1 and offsets.shape[0] >= 2, "offsets: need [N + 1], N >= 1")
-        return offsets.shape[0] - 1, x.shape[0], 1, _dense(offsets, "offsets", offsets.shape, torch.int64, x.device), 1
-    _need(x.dim() == 2 + inner, "need [N, T, ...], or [rows, ...] with offsets")
-    return x.shape[0], x.shape[1], 0, _dense(lengths, "lengths", (x.shape[0],), torch.int64, x.device), 2
+        if lengths is not None:
+            _refuse("offsets (packed rows) and lengths (a padded batch) exclude each other")
+        if len(shape) != 1 + inner:
+            _refuse("packed rows have no dimension for the sequences")
+        if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.shape[0] < 2:
+            _refuse("offsets: need [N + 1], N >= 1")
+        return offsets.shape[0] - 1, shape[0], 1, _dense(offsets, "offsets", offsets.shape, torch.int64, x.device), 1
+    if len(shape) != 2 + inner:
+        _refuse("need [N, T, ...], or [rows, ...] with offsets")
+    return shape[0], shape[1], 0, _dense(lengths, "lengths", shape[:1], torch.int64, x.device), 2
 
 
-def _diag_config(x, gate, h, kind, offsets, lengths, drop, seed, draw):
-    _need(isinstance(gate, torch.Tensor) and isinstance(x, torch.Tensor), "need device tensors")
-    _need(x.dtype in _DTYPES, "need float32, float64, bfloat16 or float16")
-    _check_like(x, "x", gate.shape, gate.dtype, gate.device)
-    N, T, packed, bounds, lead = _rows_of(x, 1, offsets, lengths)
-    D = x.shape[-1]
-    cfg = DiagrecConfig(_DTYPES[x.dtype], int(kind), N, D, T, packed, int(draw) & 0xFFFFFFFF, _row_stride(gate, "gate", lead),
-                        _row_stride(x, "x", lead), _row_stride(h, "h", lead) if h is not None else D, float(drop),
-                        int(seed) & 0xFFFFFFFFFFFFFFFF)
-    return cfg, bounds
+def _rows_like(t, stride):
+    """an array of t's shape whose rows lie `stride` elements apart, as slices of a wider one do"""
+    strides = [1] * t.dim()
+    for k in range(t.dim() - 2, -1, -1):
+        strides[k] = stride if k == t.dim() - 2 else strides[k + 1] * t.shape[k + 1]
+    return torch.empty_strided(t.shape, strides, dtype=t.dtype, device=t.device)
 
 
-def _diag_workspace(lib, cfg, grad, device):
-    size = ctypes.c_size_t(0)
+@functools.lru_cache(maxsize=512)
+def _diag_workspace(grad, dtype, gate, N, D, T, packed):
+    lib, size = load_library(), ctypes.c_size_t(0)
+    cfg = DiagrecConfig(dtype, gate, N, D, T, packed, 0, 0, 0, 0, 0.0, 0)
     st = lib.deer_diagrec_workspace_bytes(ctypes.byref(cfg), grad, ctypes.byref(size))
     if st != DEER_OK:
         _raise(lib, st)
-    return torch.empty(size.value, dtype=torch.uint8, device=device)   # (torch's blocks are aligned to 512 bytes)
+    return size.value
+
+
+def _diag_inputs(gate, x, kind, offsets, lengths):
+    """(dtype, kind, N, D, T, packed, bounds, leading dimensions) of a diagonal recurrence's arrays"""
+    if not isinstance(x, torch.Tensor):
+        _refuse("need device tensors")
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
+        _refuse("need float32, float64, bfloat16 or float16")
+    _check_like(x, "x", gate.shape, gate.dtype, gate.device)
+    N, T, packed, bounds, lead = _rows_of(x, 1, offsets, lengths)
+    return dtype, int(kind), N, x.shape[-1], T, packed, bounds, lead
 
 
 @_on_stream
@@ -377,15 +399,21 @@ def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, leng
     optional int64 `lengths` [N], or packed [rows, D] with int64 `offsets` [N + 1]; rows may be slices of wider ones.  h0 [N, D] in
     float32 (float64 with float64).  Rows of no sequence are left as they are in `out`.  Returns (h, state behind the last rows)."""
     lib = load_library()
-    h = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _check_like(h, "out", x.shape, x.dtype, x.device)
-    cfg, bounds = _diag_config(x, gate, h, kind, offsets, lengths, drop, seed, draw)
-    w = _wide(x.dtype)
-    h0p = _dense(h0, "h0", (cfg.N, cfg.D), w, x.device)
-    last = torch.empty((cfg.N, cfg.D), dtype=w, device=x.device)
-    ws = _diag_workspace(lib, cfg, 0, x.device)
-    st = lib.deer_diagrec_solve(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), last.data_ptr(), ws.data_ptr(),
-                                ws.numel(), _stream_of(x))
+    dtype, kind, N, D, T, packed, bounds, lead = _diag_inputs(gate, x, kind, offsets, lengths)
+    dev, w = x.device, torch.float64 if dtype == DEER_F64 else torch.float32
+    if out is None:
+        h = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    else:
+        h = out
+        _check_like(h, "out", x.shape, x.dtype, dev)
+    cfg = DiagrecConfig(dtype, kind, N, D, T, packed, draw & 0xFFFFFFFF, _row_stride(gate, "gate", lead), _row_stride(x, "x", lead),
+                        _row_stride(h, "out", lead), drop, seed & 0xFFFFFFFFFFFFFFFF)
+    last = torch.empty((N, D), dtype=w, device=dev)
+    h0p = _dense(h0, "h0", last.shape, w, dev)
+    size = _diag_workspace(0, dtype, kind, N, D, T, packed)
+    ws = torch.empty(size, dtype=torch.uint8, device=dev)   # (torch's blocks are aligned to 512 bytes)
+    st = lib.deer_diagrec_solve(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), last.data_ptr(), ws.data_ptr(), size,
+                                _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
     return h, last
@@ -397,36 +425,36 @@ def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, 
     """deer_diagrec_grad at the trajectory h: (dL/dgate, dL/dx, dL/dh0) from dh = dL/dh and dlast = dL/d(final state).  dgate and dx, where
     given, have the row strides of gate and x."""
     lib = load_library()
-    cfg, bounds = _diag_config(x, gate, h, kind, offsets, lengths, drop, seed, draw)
-    lead, w, dev = 1 if cfg.packed else 2, _wide(x.dtype), x.device
+    dtype, kind, N, D, T, packed, bounds, lead = _diag_inputs(gate, x, kind, offsets, lengths)
+    dev, w = x.device, torch.float64 if dtype == DEER_F64 else torch.float32
     _check_like(h, "h", x.shape, x.dtype, dev)
     _check_like(dh, "dh", x.shape, x.dtype, dev)
-    if _row_stride(dh, "dh", lead) != cfg.stride_out:
-        h, dh = h.contiguous(), dh.contiguous()
-        cfg.stride_out = cfg.D
+    stride_h = _row_stride(h, "h", lead)
+    if _row_stride(dh, "dh", lead) != stride_h:
+        h, dh, stride_h = h.contiguous(), dh.contiguous(), D
+    stride_g, stride_x = _row_stride(gate, "gate", lead), _row_stride(x, "x", lead)
     if dgate is None:
-        dgate = torch.empty_strided(gate.shape, gate.stride(), dtype=x.dtype, device=dev) if gate.is_contiguous() else _rows_like(gate, cfg.stride_gate)
+        dgate = torch.empty(gate.shape, dtype=x.dtype, device=dev) if stride_g == D else _rows_like(gate, stride_g)
+    else:
+        _check_like(dgate, "dgate", x.shape, x.dtype, dev)
+        if _row_stride(dgate, "dgate", lead) != stride_g:
+            _refuse("dgate: rows must lie like those of gate")
     if dx is None:
-        dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=dev) if x.is_contiguous() else _rows_like(x, cfg.stride_in)
-    for t, name, stride in ((dgate, "dgate", cfg.stride_gate), (dx, "dx", cfg.stride_in)):
-        _check_like(t, name, x.shape, x.dtype, dev)
-        _need(_row_stride(t, name, lead) == stride, name + ": rows must lie like those of what it is the gradient of")
-    h0p, dlp = _dense(h0, "h0", (cfg.N, cfg.D), w, dev), _dense(dlast, "dlast", (cfg.N, cfg.D), w, dev)
-    dh0 = torch.empty((cfg.N, cfg.D), dtype=w, device=dev)
-    ws = _diag_workspace(lib, cfg, 1, dev)
+        dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if stride_x == D else _rows_like(x, stride_x)
+    else:
+        _check_like(dx, "dx", x.shape, x.dtype, dev)
+        if _row_stride(dx, "dx", lead) != stride_x:
+            _refuse("dx: rows must lie like those of x")
+    cfg = DiagrecConfig(dtype, kind, N, D, T, packed, draw & 0xFFFFFFFF, stride_g, stride_x, stride_h, drop, seed & 0xFFFFFFFFFFFFFFFF)
+    dh0 = torch.empty((N, D), dtype=w, device=dev)
+    h0p, dlp = _dense(h0, "h0", dh0.shape, w, dev), _dense(dlast, "dlast", dh0.shape, w, dev)
+    size = _diag_workspace(1, dtype, kind, N, D, T, packed)
+    ws = torch.empty(size, dtype=torch.uint8, device=dev)
     st = lib.deer_diagrec_grad(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), dh.data_ptr(), dlp, dgate.data_ptr(),
-                               dx.data_ptr(), dh0.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(x))
+                               dx.data_ptr(), dh0.data_ptr(), ws.data_ptr(), size, _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
     return dgate, dx, dh0
-
-
-def _rows_like(t, stride):
-    """an array of t's shape whose rows lie `stride` elements apart, as slices of a wider one do"""
-    strides = [1] * t.dim()
-    for k in range(t.dim() - 2, -1, -1):
-        strides[k] = stride if k == t.dim() - 2 else strides[k + 1] * t.shape[k + 1]
-    return torch.empty_strided(t.shape, strides, dtype=t.dtype, device=t.device)
 
 
 @_on_stream
@@ -434,49 +462,67 @@ def diagrec_step(gate, x, state, *, kind=DEER_GATE_FACTOR, slots=None, out=None)
     """deer_diagrec_step: one token for each of N rows, gate and x [N, D]; `state` [slots, D] (float32; float64 with float64) is updated
     in place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over.  Returns h [N, D]."""
     lib = load_library()
-    _need(isinstance(x, torch.Tensor) and x.dtype in _DTYPES and x.dim() == 2, "need x [N, D] in float32, float64, bfloat16 or float16")
-    _check_like(gate, "gate", x.shape, x.dtype, x.device)
-    h = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _check_like(h, "out", x.shape, x.dtype, x.device)
-    _need(state.dim() == 2, "state: need [slots, D]")
-    sp = _dense(state, "state", (state.shape[0], x.shape[1]), _wide(x.dtype), x.device)
-    tp = _dense(slots, "slots", (x.shape[0],), torch.int32, x.device)
-    cfg = DiagrecConfig(_DTYPES[x.dtype], int(kind), x.shape[0], x.shape[1], 1, 0, 0, _row_stride(gate, "gate", 1), _row_stride(x, "x", 1),
+    dtype = _DTYPES.get(x.dtype) if isinstance(x, torch.Tensor) else None
+    if dtype is None or x.dim() != 2:
+        _refuse("need x [N, D] in float32, float64, bfloat16 or float16")
+    dev, shape = x.device, x.shape
+    _check_like(gate, "gate", shape, x.dtype, dev)
+    if out is None:
+        h = torch.empty(shape, dtype=x.dtype, device=dev)
+    else:
+        h = out
+        _check_like(h, "out", shape, x.dtype, dev)
+    if not isinstance(state, torch.Tensor) or state.dim() != 2 or state.shape[1] != shape[1]:
+        _refuse("state: need [slots, D]")
+    sp = _dense(state, "state", state.shape, torch.float64 if dtype == DEER_F64 else torch.float32, dev)
+    tp = _dense(slots, "slots", shape[:1], torch.int32, dev)
+    cfg = DiagrecConfig(dtype, int(kind), shape[0], shape[1], 1, 0, 0, _row_stride(gate, "gate", 1), _row_stride(x, "x", 1),
                         _row_stride(h, "out", 1), 0.0, 0)
-    st = lib.deer_diagrec_step(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), tp, state.shape[0], sp, h.data_ptr(), _stream_of(x))
+    st = lib.deer_diagrec_step(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), tp, state.shape[0], sp, h.data_ptr(), _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
     return h
 
 
-def _mat_config(q, k, v, gate, o, offsets, lengths, scale, lead=None):
-    """lead: given for a step, whose rows are not sequences"""
-    _need(all(isinstance(t, torch.Tensor) for t in (q, k, v, gate)), "need device tensors")
-    _need(q.dtype in _DTYPES, "need float32 or bfloat16")
-    if lead is None:
-        N, T, packed, bounds, lead = _rows_of(q, 2, offsets, lengths)
-    else:
-        _need(q.dim() == 3, "need q [N, Hk, Dk]")
-        N, T, packed, bounds = q.shape[0], 1, 0, 0
-    rows, dev = tuple(q.shape[:lead]), q.device
-    Hk, Dk = q.shape[lead:]
-    _check_like(k, "k", q.shape, q.dtype, dev)
-    _need(v.dim() == q.dim(), "v: need as many dimensions as q")
-    Hv, Dv = v.shape[lead:]
-    _check_like(v, "v", rows + (Hv, Dv), q.dtype, dev)
-    _need(Hk >= 1 and Hv % Hk == 0, "the heads of v must be a multiple of those of q and k")
-    gp = _dense(gate, "gate", rows + (Hv,), torch.float32, dev)
-    cfg = MatrecConfig(_DTYPES[q.dtype], N, T, packed, Hk, Hv, Dk, Dv, 0, float(Dk ** -0.5 if scale is None else scale), _row_stride(q, "q", lead),
-                       _row_stride(k, "k", lead), _row_stride(v, "v", lead), _row_stride(o, "o", lead) if o is not None else Hv * Dv)
-    return cfg, bounds, gp, lead
-
-
-def _mat_workspace(lib, cfg, grad, device):
-    size = ctypes.c_size_t(0)
+@functools.lru_cache(maxsize=512)
+def _mat_workspace(grad, dtype, N, T, packed, Hk, Hv, Dk, Dv):
+    lib, size = load_library(), ctypes.c_size_t(0)
+    cfg = MatrecConfig(dtype, N, T, packed, Hk, Hv, Dk, Dv, 0, 1.0, 0, 0, 0, 0)
     st = lib.deer_matrec_workspace_bytes(ctypes.byref(cfg), grad, ctypes.byref(size))
     if st != DEER_OK:
         _raise(lib, st)
-    return torch.empty(size.value, dtype=torch.uint8, device=device)
+    return size.value
+
+
+def _mat_config(q, k, v, gate, o, offsets, lengths, scale, lead=None):
+    """configuration, pointers of the bounds and of the gates, leading dimensions; lead: given for a step, whose rows are not sequences"""
+    for t in (k, v, gate):
+        if not isinstance(t, torch.Tensor):
+            _refuse("need device tensors")
+    dtype = _DTYPES.get(q.dtype)
+    if dtype is None:
+        _refuse("need float32 or bfloat16")
+    if lead is None:
+        N, T, packed, bounds, lead = _rows_of(q, 2, offsets, lengths)
+    else:
+        if q.dim() != 3:
+            _refuse("need q [N, Hk, Dk]")
+        N, T, packed, bounds = q.shape[0], 1, 0, 0
+    dev, rows = q.device, q.shape[:lead]
+    Hk, Dk = q.shape[lead:]
+    _check_like(k, "k", q.shape, q.dtype, dev)
+    if v.dim() != q.dim():
+        _refuse("v: need as many dimensions as q")
+    Hv, Dv = v.shape[lead:]
+    _check_like(v, "v", rows + v.shape[lead:], q.dtype, dev)
+    if Hk < 1 or Hv % Hk:
+        _refuse("the heads of v must be a multiple of those of q and k")
+    gp = _dense(gate, "gate", rows + v.shape[lead:lead + 1], torch.float32, dev)
+    if o is not None:
+        _check_like(o, "out", v.shape, v.dtype, dev)
+    cfg = MatrecConfig(dtype, N, T, packed, Hk, Hv, Dk, Dv, 0, Dk ** -0.5 if scale is None else scale, _row_stride(q, "q", lead),
+                       _row_stride(k, "k", lead), _row_stride(v, "v", lead), _row_stride(o, "out", lead) if o is not None else Hv * Dv)
+    return cfg, bounds, gp, lead
 
 
 @_on_stream
@@ -485,15 +531,15 @@ def matrec_solve(q, k, v, gate, s0=None, *, offsets=None, lengths=None, scale=No
     float32 or bfloat16, gate [N, T, Hv] float32, with optional int64 `lengths` [N]; or packed [rows, ...] with int64 `offsets` [N + 1].  s0 [N, Hv, Dk, Dv]
     float32.  scale: Dk^-1/2 by default.  Returns (o, states behind the last rows)."""
     lib = load_library()
-    o = out if out is not None else torch.empty(v.shape, dtype=v.dtype, device=q.device)
+    o = out if out is not None else torch.empty_like(v, memory_format=torch.contiguous_format) if isinstance(v, torch.Tensor) else None
     cfg, bounds, gp, _ = _mat_config(q, k, v, gate, o, offsets, lengths, scale)
-    _check_like(o, "out", v.shape, v.dtype, q.device)
-    shape = (cfg.N, cfg.Hv, cfg.Dk, cfg.Dv)
-    s0p = _dense(s0, "s0", shape, torch.float32, q.device)
-    ws = _mat_workspace(lib, cfg, 0, q.device)
-    last = torch.empty(shape, dtype=torch.float32, device=q.device)
+    dev, shape = q.device, (cfg.N, cfg.Hv, cfg.Dk, cfg.Dv)
+    s0p = _dense(s0, "s0", shape, torch.float32, dev)
+    size = _mat_workspace(0, cfg.dtype, cfg.N, cfg.T, cfg.packed, cfg.Hk, cfg.Hv, cfg.Dk, cfg.Dv)
+    ws = torch.empty(size, dtype=torch.uint8, device=dev)
+    last = torch.empty(shape, dtype=torch.float32, device=dev)
     st = lib.deer_matrec_solve(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, s0p, bounds, o.data_ptr(), last.data_ptr(),
-                               ws.data_ptr(), ws.numel(), _stream_of(q))
+                               ws.data_ptr(), size, _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
     return o, last
@@ -504,24 +550,25 @@ def matrec_grad(q, k, v, gate, do, s0=None, dlast=None, *, offsets=None, lengths
     """deer_matrec_grad: (dq, dk, dv, dgate, ds0) from do = dL/do and dlast = dL/d(final states).  dq, dk and dv, where given, have the row
     strides of q, k and v."""
     lib = load_library()
-    cfg, bounds, gp, lead = _mat_config(q, k, v, gate, None, offsets, lengths, scale)
+    cfg, bounds, gp, lead = _mat_config(q, k, v, gate, do, offsets, lengths, scale)
     dev = q.device
-    _check_like(do, "do", v.shape, v.dtype, dev)
-    cfg.stride_o = _row_stride(do, "do", lead)
     outs = []
     for t, d, name, stride in ((q, dq, "dq", cfg.stride_q), (k, dk, "dk", cfg.stride_k), (v, dv, "dv", cfg.stride_v)):
         if d is None:
             d = torch.empty(t.shape, dtype=t.dtype, device=dev) if t.is_contiguous() else _rows_like(t.flatten(-2), stride).unflatten(-1, t.shape[-2:])
-        _check_like(d, name, t.shape, t.dtype, dev)
-        _need(_row_stride(d, name, lead) == stride, name + ": rows must lie like those of what it is the gradient of")
+        else:
+            _check_like(d, name, t.shape, t.dtype, dev)
+            if _row_stride(d, name, lead) != stride:
+                _refuse(name + ": rows must lie like those of what it is the gradient of")
         outs.append(d)
     shape = (cfg.N, cfg.Hv, cfg.Dk, cfg.Dv)
     s0p, dlp = _dense(s0, "s0", shape, torch.float32, dev), _dense(dlast, "dlast", shape, torch.float32, dev)
-    ws = _mat_workspace(lib, cfg, 1, dev)
+    size = _mat_workspace(1, cfg.dtype, cfg.N, cfg.T, cfg.packed, cfg.Hk, cfg.Hv, cfg.Dk, cfg.Dv)
+    ws = torch.empty(size, dtype=torch.uint8, device=dev)
     dgate = torch.empty(gate.shape, dtype=torch.float32, device=dev)
     ds0 = torch.empty(shape, dtype=torch.float32, device=dev)
     st = lib.deer_matrec_grad(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, s0p, bounds, do.data_ptr(), dlp, outs[0].data_ptr(),
-                              outs[1].data_ptr(), outs[2].data_ptr(), dgate.data_ptr(), ds0.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(q))
+                              outs[1].data_ptr(), outs[2].data_ptr(), dgate.data_ptr(), ds0.data_ptr(), ws.data_ptr(), size, _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
     return outs[0], outs[1], outs[2], dgate, ds0
@@ -532,13 +579,14 @@ def matrec_step(q, k, v, gate, state, *, slots=None, scale=None, out=None):
     """deer_matrec_step: one token for each of N rows, q, k [N, Hk, Dk], v [N, Hv, Dv], gate [N, Hv]; `state` [slots, Hv, Dk, Dv] float32 is updated
     in place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over.  Returns o."""
     lib = load_library()
-    o = out if out is not None else torch.empty(v.shape, dtype=v.dtype, device=q.device)
+    o = out if out is not None else torch.empty_like(v, memory_format=torch.contiguous_format) if isinstance(v, torch.Tensor) else None
     cfg, _, gp, _ = _mat_config(q, k, v, gate, o, None, None, scale, lead=1)
-    _check_like(o, "out", v.shape, v.dtype, q.device)
-    _need(isinstance(state, torch.Tensor) and state.dim() == 4, "state: need [slots, Hv, Dk, Dv]")
-    sp = _dense(state, "state", (state.shape[0], cfg.Hv, cfg.Dk, cfg.Dv), torch.float32, q.device)
-    tp = _dense(slots, "slots", (cfg.N,), torch.int32, q.device)
-    st = lib.deer_matrec_step(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, tp, state.shape[0], sp, o.data_ptr(), _stream_of(q))
+    dev = q.device
+    if not isinstance(state, torch.Tensor) or state.dim() != 4:
+        _refuse("state: need [slots, Hv, Dk, Dv]")
+    sp = _dense(state, "state", (state.shape[0], cfg.Hv, cfg.Dk, cfg.Dv), torch.float32, dev)
+    tp = _dense(slots, "slots", q.shape[:1], torch.int32, dev)
+    st = lib.deer_matrec_step(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, tp, state.shape[0], sp, o.data_ptr(), _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
     return o
@@ -549,13 +597,17 @@ def dropout(x, p, seed, draw=0, *, out=None):
     """deer_dropout: x [N, T, D] or packed [rows, D] with a share p dropped and the rest divided by 1 - p; the backward pass is the same
     call on the gradient.  `out` may be x."""
     lib = load_library()
-    _need(x.dtype in _DTYPES and x.dim() in (2, 3), "need x [N, T, D] or [rows, D] in float32, float64, bfloat16 or float16")
-    y = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _check_like(y, "out", x.shape, x.dtype, x.device)
-    lead = x.dim() - 1
-    N, T, D = (x.shape[0], x.shape[1], x.shape[2]) if lead == 2 else (1, x.shape[0], x.shape[1])
-    st = lib.deer_dropout(_DTYPES[x.dtype], N, T, D, x.data_ptr(), _row_stride(x, "x", lead), y.data_ptr(), _row_stride(y, "out", lead), float(p),
-                          int(seed) & 0xFFFFFFFFFFFFFFFF, int(draw) & 0xFFFFFFFF, _stream_of(x))
+    dtype, lead, dev = _DTYPES.get(x.dtype), x.dim() - 1, x.device
+    if dtype is None or lead not in (1, 2):
+        _refuse("need x [N, T, D] or [rows, D] in float32, float64, bfloat16 or float16")
+    if out is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    else:
+        y = out
+        _check_like(y, "out", x.shape, x.dtype, dev)
+    N, T, D = x.shape if lead == 2 else (1,) + tuple(x.shape)
+    st = lib.deer_dropout(dtype, N, T, D, x.data_ptr(), _row_stride(x, "x", lead), y.data_ptr(), _row_stride(y, "out", lead), p,
+                          seed & 0xFFFFFFFFFFFFFFFF, draw & 0xFFFFFFFF, _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
     return y
