@@ -76,24 +76,28 @@ __global__ __launch_bounds__(256) void matrec_gates_kernel(const MatrecParams p)
     for (int i = threadIdx.x; i < rows * p.Hv; i += 256) p.dgate[first + i] += p.gate_k[first + i] + p.read_in[chunk + i % p.Hv];
 }
 
-// dq and dk of shared heads: the heads of v that go with one, in their order; a workgroup has a chunk of a segment
+// dq and dk of shared heads: the heads of v that go with one, in their order; a workgroup has 16 rows of a chunk
+constexpr int kSharedRows = 16;
 template <typename T>
 __global__ __launch_bounds__(256) void matrec_shared_kernel(const MatrecParams p) {
-    const int seg_no = blockIdx.x / p.plan.per, c = blockIdx.x % p.plan.per;
+    constexpr int PARTS = kChunk / kSharedRows;
+    const int chunk = blockIdx.x / PARTS, seg_no = chunk / p.plan.per, c = chunk % p.plan.per;
     MatSegment seg;
     if (!segment_of(p, seg_no, seg)) return;
-    const long long left = seg.rows - (long long)c * kChunk;
+    const long long first = (long long)c * kChunk + blockIdx.x % PARTS * kSharedRows, left = seg.rows - first;
     if (left <= 0) return;
-    const int rows = left < kChunk ? (int)left : kChunk, group = p.Hv / p.Hk, cols = p.Hk * p.Dk;
+    const int rows = left < kSharedRows ? (int)left : kSharedRows, group = p.Hv / p.Hk, cols = p.Hk * p.Dk;
     const float* part = blockIdx.y == 0 ? p.part_q : p.part_k;
     T* to = reinterpret_cast<T*>(blockIdx.y == 0 ? p.dq : p.dk);
-    const long long stride = blockIdx.y == 0 ? p.stride_q : p.stride_k, row0 = seg.row0 + (long long)c * kChunk;
-    for (int i = threadIdx.x; i < rows * cols; i += 256) {
-        const int r = i / cols, col = i % cols, kh = col / p.Dk, d = col % p.Dk;
-        const float* from = part + ((row0 + r) * p.Hv + (long long)kh * group) * p.Dk + d;
-        float s = 0.0f;
-        for (int m = 0; m < group; ++m) s += from[(long long)m * p.Dk];
-        to[(row0 + r) * stride + col] = (T)s;
+    const long long stride = blockIdx.y == 0 ? p.stride_q : p.stride_k, row0 = seg.row0 + first;
+    for (int col = threadIdx.x % 64; col < cols; col += 64) {
+        const int kh = col / p.Dk, d = col % p.Dk;
+        for (int r = threadIdx.x / 64; r < rows; r += 4) {
+            const float* from = part + ((row0 + r) * p.Hv + (long long)kh * group) * p.Dk + d;
+            float s = 0.0f;
+            for (int m = 0; m < group; ++m) s += from[(long long)m * p.Dk];
+            to[(row0 + r) * stride + col] = (T)s;
+        }
     }
 }
 
@@ -110,8 +114,8 @@ hipError_t launch_matrec_grad(int dtype, const MatrecParams& p, hipStream_t stre
     const unsigned chunks = (unsigned)((long long)p.plan.max_segs * p.plan.per);
     if (e != hipSuccess || chunks == 0) return e;
     if (p.Hv != p.Hk) {
-        if (dtype == DEER_BF16) hipLaunchKernelGGL((matrec_shared_kernel<BF16>), dim3(chunks, 2), dim3(256), 0, stream, p);
-        else hipLaunchKernelGGL((matrec_shared_kernel<float>), dim3(chunks, 2), dim3(256), 0, stream, p);
+        if (dtype == DEER_BF16) hipLaunchKernelGGL((matrec_shared_kernel<BF16>), dim3(chunks * (kChunk / kSharedRows), 2), dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((matrec_shared_kernel<float>), dim3(chunks * (kChunk / kSharedRows), 2), dim3(256), 0, stream, p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (!p.dgate) return hipSuccess;

@@ -182,7 +182,7 @@ const char* unsupported(const deer_matrec_config* c, bool step) {
     if (c->T > kMostRows || (long double)c->N * c->Hv * 64 > 2147483647.0L || ((long double)(c->T + 63) / 64 + 4) * (c->packed ? 1 : c->N) * c->Hv > 2147483647.0L)
         return "more rows than a launch holds";
     const MatLayout l = mat_layout(c, true);
-    if ((long double)l.max_segs * l.per * c->Hv > 2147483647.0L || ((long double)l.max_segs * c->Hv + 8) * 3 > 2147483647.0L || (long double)l.max_segs * c->Hv > 2147483647.0L) return "more rows than a launch holds";
+    if ((long double)l.max_segs * l.per * c->Hv > 2147483647.0L || (long double)l.max_segs * l.per * 4 > 2147483647.0L || ((long double)l.max_segs * c->Hv + 8) * 3 > 2147483647.0L || (long double)l.max_segs * c->Hv > 2147483647.0L) return "more rows than a launch holds";
     return nullptr;
 }
 MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool grad, const int64_t* bounds, void* workspace) {
