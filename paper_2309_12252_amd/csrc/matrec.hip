@@ -127,8 +127,8 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
         const int c = REV ? chunks - 1 - i : i;
         const long long row = (long long)c * kChunk;
         const int rows = seg.rows - row < kChunk ? (int)(seg.rows - row) : kChunk;
-        load_tile<T, DK, W, false>(tk, k + row * stride_k, stride_k, rows, p.Dk, wide_k);
-        load_tile<T, DV, W, false>(tv, v + row * stride_v, stride_v, rows, p.Dv, wide_v);
+        load_tile<T, DK, W, false>(tk, k + row * stride_k, stride_k, rows, p.Dk, wide_k, lane);
+        load_tile<T, DV, W, false>(tv, v + row * stride_v, stride_v, rows, p.Dv, wide_v, lane);
         const float* from = gates + (long long)c * p.Hv * kRowFloats;
         if (wave < 2) load_floats(weight + 64 * wave, from, wave == 0 ? (REV ? 128 : 192) + lane : 256 + lane);
     };

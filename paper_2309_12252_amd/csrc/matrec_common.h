@@ -114,22 +114,23 @@ __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70
 // Bounds of the buffer make the zeros.  `load` returns while rows of wide arrays are on their way: wait_loads() before the barrier.
 // BACK: row r of the tile is row rows - 1 - r in memory.
 template <typename T, int C, int W, bool BACK>
-__device__ __forceinline__ void load_tile(T* tile, const T* from, long long stride, int rows, int cols, bool wide) {
+__device__ __forceinline__ void load_tile(T* tile, const T* from, long long stride, int rows, int cols, bool wide, int lane) {
     constexpr int PER = C / 8;
-    const int lane = again(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (sizeof(T) == 2 && wide) {
         typedef __attribute__((address_space(3))) void* LdsPtr;
         constexpr int STEP = 64 / PER, N = kChunk / STEP;   // rows of an instruction; instructions of a tile
         const int pitch = (int)stride * 2;
         const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, rows * pitch, 0x00020000);
+        // A wavefront's instructions are W apart, a multiple of 16 rows: the same turn in all of them.
+        static_assert(N <= W || W * STEP % 16 == 0, "turn() has a period of 16 rows");
+        const int row = wave * STEP + lane / PER, c = ((lane % PER) ^ Tile<T, C>::turn(row)) * 8;
+        // (a row in front of the first is far behind the end as an unsigned offset)
+        const int off = c < cols ? (BACK ? rows - 1 - row : row) * pitch + c * 2 : 0x60000000;
 #pragma unroll
         for (int n = 0; n < (N + W - 1) / W; ++n) {
-            const int at = wave + n * W;
-            if (N % W && at >= N) break;
-            const int row = at * STEP + lane / PER, c = ((lane % PER) ^ Tile<T, C>::turn(row)) * 8;
-            // (a row in front of the first is far behind the end as an unsigned offset)
-            const int off = c < cols ? (BACK ? rows - 1 - row : row) * pitch + c * 2 : 0x60000000;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LdsPtr)(tile + at * STEP * C), 16, off, 0, 0, 0);
+            if (N % W && wave + n * W >= N) break;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LdsPtr)(tile + (wave + n * W) * STEP * C), 16, off + (BACK ? -n : n) * W * STEP * pitch, 0, 0, 0);
         }
     } else {
         for (int at = threadIdx.x; at < kChunk * PER; at += 64 * W) {

@@ -126,14 +126,13 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     float *dots = reinterpret_cast<float*>(lds + L::dots), *by_col = reinterpret_cast<float*>(lds + L::by_col), *by_row = reinterpret_cast<float*>(lds + L::by_row);
     auto load = [&](int c) {
         long long row;
-        const int rows = rows_of(c, row);
-        load_tile<T, D1, W, BACK>(ta, ra + row * sa, sa, rows, d1, wide_a);
-        load_tile<T, D1, W, BACK>(tb, rb + row * sb, sb, rows, d1, wide_b);
-        load_tile<T, D2, W, BACK>(tc, rc + row * sc, sc, rows, d2, wide_c);
-        if constexpr (L::FOUR) load_tile<T, D2, W, BACK>(tq, q + row * p.stride_q, p.stride_q, rows, d2, wide_q);
+        const int rows = rows_of(c, row), i = again(lane0);
+        load_tile<T, D1, W, BACK>(ta, ra + row * sa, sa, rows, d1, wide_a, i);
+        load_tile<T, D1, W, BACK>(tb, rb + row * sb, sb, rows, d1, wide_b, i);
+        load_tile<T, D2, W, BACK>(tc, rc + row * sc, sc, rows, d2, wide_c, i);
+        if constexpr (L::FOUR) load_tile<T, D2, W, BACK>(tq, q + row * p.stride_q, p.stride_q, rows, d2, wide_q, i);
         // cum_hi, cum_lo, f, w, whole; backwards: rows turned round, f and w the other way round
         const float* from = gates + (long long)(BACK ? chunks - 1 - c : c) * p.Hv * kRowFloats;
-        const int i = again(lane0);
         for (int n = wave; n < 5; n += W) load_floats(cum_hi + 64 * n, from, 64 * (!BACK || n < 2 || n > 3 ? n : 5 - n) + (BACK && n < 4 && i < rows ? rows - 1 - i : i));
     };
     // what is never written but taken in: pairs above the diagonal, sums of tiles there
@@ -350,17 +349,19 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
             }
         }
         if (strip && col0 < d2) {
+            const int i0 = again(lane0) & 15;
+            const long long first_row = row + (BACK ? rows - 1 - i0 : i0);
+            const int back = BACK ? -16 : 16;
+            T* to = out + first_row * so + col0;
+            float* to_part = parts ? out_part + first_row * p.Hv * p.Dk + col0 : nullptr;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const int i = 16 * t + l;
-                if (i >= rows) continue;
-                const long long r = row + (BACK ? rows - 1 - i : i);
-                if (parts) {
+                if (16 * t + i0 < rows) {
 #pragma unroll
-                    for (int u = 0; u < VT; ++u) store_four<float>(out_part + r * p.Hv * p.Dk + col0 + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
-                } else {
-#pragma unroll
-                    for (int u = 0; u < VT; ++u) store_four<T>(out + r * so + col0 + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
+                    for (int u = 0; u < VT; ++u) {
+                        if (parts) store_four<float>(to_part + (long long)t * back * p.Hv * p.Dk + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
+                        else store_four<T>(to + (long long)t * back * so + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
+                    }
                 }
             }
         }
