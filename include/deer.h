@@ -249,7 +249,8 @@ deer_status deer_linrec_solve_static(int32_t dtype, int32_t B, int32_t T, int32_
  *     one.  Rows that belong to no sequence are neither read nor written.  Bounds outside 0 .. T are clamped;
  *     packed bounds that decrease give results without meaning, within the arrays.
  *   - stride_*: elements from one row to the next (0: dense), so that slices of a wider array can be handed in; the
- *     last dimension is dense (deer_diagrec_solve(), deer_diagrec_grad(): at most 2^22).
+ *     last dimension is dense (deer_diagrec_solve(), deer_diagrec_grad(): rows and strides of at most 2^22).  A call whose largest launch
+ *     would have 2^32 work items or more is refused (DEER_ERR_UNSUPPORTED).
  *   - Pointers are aligned to the element; where all rows are aligned to more, wider loads are used.  Outputs must not overlap
  *     inputs, except where an operator says so.
  *   - What is NaN or infinite in a sequence stays in that sequence. */
@@ -296,7 +297,7 @@ deer_status deer_diagrec_step(const deer_diagrec_config* cfg, const void* d_gate
 
 /* Dropout: y = x / (1 - p) where an element is kept, 0 where it is dropped.  Which ones are kept follows from (seed, draw) and the element's
  * sequence, row and channel alone, so the backward pass is the same call on the gradient and no mask is stored; deer_diagrec_*
- * with drop = p draws the same mask.  p is rounded to 2^-16 (and the scale taken from the rounded value).
+ * with drop = p draws the same mask (packed rows count as one sequence, in either call).  p is rounded to 2^-16 (and the scale taken from the rounded value).
  *   d_x in, d_y out [N, T, D], rows stride_in and stride_out apart (0: dense); d_y may be d_x with the same stride. */
 deer_status deer_dropout(int32_t dtype, int32_t N, int64_t T, int32_t D, const void* d_x, int64_t stride_in, void* d_y,
                          int64_t stride_out, double p, uint64_t seed, uint32_t draw, void* hip_stream);
@@ -320,7 +321,7 @@ deer_status deer_matrec_workspace_bytes(const deer_matrec_config* cfg, int32_t g
 
 /* d_q, d_k in [rows, Hk, Dk]   d_v in [rows, Hv, Dv]   d_gate in [rows, Hv] float32, the logarithms of the factors (dense)   d_s0 in [N, Hv, Dk, Dv]
  * float32 or NULL (zeros)   d_o out [rows, Hv, Dv]   d_last out [N, Hv, Dk, Dv] float32 or NULL.  By chunks of 64 rows on the matrix cores; states
- * in fp32 (bf16: sums of exact products, their weights in two bf16 pieces), two calls with the same inputs return the same bits.
+ * in fp32 (bf16: sums of products in fp32, whose weights enter as three bf16 pieces, two where a state is only read by a product that rounds it), two calls with the same inputs return the same bits.
  * What is not finite in a row reaches the outputs of its chunk, also in front of it, and all that come later. */
 deer_status deer_matrec_solve(const deer_matrec_config* cfg, const void* d_q, const void* d_k, const void* d_v, const float* d_gate,
                               const float* d_s0, const int64_t* d_bounds, void* d_o, float* d_last, void* d_workspace,

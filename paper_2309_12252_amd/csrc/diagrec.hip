@@ -19,7 +19,7 @@ constexpr long long kPolls = 1ll << 22;           // polls before a tile gives u
 
 // tile of W wavefronts, R rows each; a lane has V channels
 template <typename T, bool REV> struct Shape {
-    static constexpr int W = 8;
+    static constexpr int W = kDiagLanes / 64;
     static constexpr int V = sizeof(T) == 8 ? 1 : 2;
     static constexpr int R = sizeof(T) == 2 ? (REV ? 16 : 32) : REV ? 8 : 16;
 };

@@ -218,10 +218,13 @@ __device__ __forceinline__ void join_cell(const MatrecParams& p, int n, int head
 template <int DK, int DV>
 __global__ __launch_bounds__(256) void matrec_join_kernel(const MatrecParams p) {
     constexpr int PER = DK * DV / 256;
-    const long long id = blockIdx.x / PER;
-    const int cell = (int)(blockIdx.x % PER) * 256 + threadIdx.x, n = (int)(id / p.Hv), head = (int)(id % p.Hv);
-    if (blockIdx.y == 0) join_cell<DK, DV, false>(p, n, head, cell);
-    else join_cell<DK, DV, true>(p, n, head, cell);
+    const long long all = (long long)p.rows.N * p.Hv * PER;
+    for (long long id = blockIdx.x; id < all; id += gridDim.x) {   // (once, but for more sequences than a launch has work items for)
+        const long long at = id / PER;
+        const int cell = (int)(id % PER) * 256 + threadIdx.x, n = (int)(at / p.Hv), head = (int)(at % p.Hv);
+        if (blockIdx.y == 0) join_cell<DK, DV, false>(p, n, head, cell);
+        else join_cell<DK, DV, true>(p, n, head, cell);
+    }
 }
 
 template <typename T, int DK, int DV>
@@ -288,8 +291,10 @@ hipError_t join_shape(const MatrecParams& p, bool both, hipStream_t stream) {
     hipError_t e = hipSuccess;
     const unsigned y = both ? 2 : 1;
     if (p.split) e = launch_lds(matrec_states_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), y), 4 * DV, StatesLds<T, DK, DV>::total, p, stream);
-    if (e != hipSuccess || !(p.split || p.rows.bounds || p.rows.T == 0)) return e;
-    hipLaunchKernelGGL((matrec_join_kernel<DK, DV>), dim3((unsigned)((long long)p.rows.N * p.Hv * (DK * DV / 256)), y), dim3(256), 0, stream, p);
+    const bool empty = p.rows.bounds || p.rows.T == 0;   // (there may be sequences without rows)
+    if (e != hipSuccess || !(p.split || (empty && (p.last || p.ds0)))) return e;
+    const long long blocks = (long long)p.rows.N * p.Hv * (DK * DV / 256);
+    hipLaunchKernelGGL((matrec_join_kernel<DK, DV>), dim3((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22), y), dim3(256), 0, stream, p);
     return hipGetLastError();
 }
 template <typename T, int DK, int DV>

@@ -32,6 +32,7 @@ bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t
 // The mask's counter has 32 bits for blocks of eight rows and for channels; rows and columns are kept where products of them with
 // element sizes stay far from 63 bits.
 constexpr int64_t kMostRows = (int64_t)1 << 33;
+constexpr long double kMostLanes = 4294967295.0L;   // of a launch: its size in work items is a number of 32 bits
 
 const char* bad_drop(double p) {
     if (!(p >= 0.0 && p < 1.0)) return "dropout: the share that is dropped must lie in [0, 1)";
@@ -60,13 +61,6 @@ const char* bad_config(const deer_diagrec_config* c, bool step) {
     if (c->T < 0 || (c->packed != 0 && c->packed != 1)) return "T must not be negative, packed 0 or 1";
     return bad_drop(c->drop);
 }
-bool too_large(const deer_diagrec_config* c) {
-    const long long seqs = c->packed ? 1 : c->N;
-    if (c->T > kMostRows || c->D > kMostStride || c->stride_gate > kMostStride || c->stride_in > kMostStride || c->stride_out > kMostStride) return true;
-    const long long tiles = (c->T + 63) / 64, cols = (c->D + 63) / 64;   // (the smallest tiles of any type)
-    return (long double)tiles * cols * seqs > 2147483647.0L || (long double)c->N * c->D > 1e15L;
-}
-
 struct DiagLayout {
     int chunks, groups;
     size_t agg_words, words, total;
@@ -76,6 +70,13 @@ DiagLayout diag_layout(const deer_diagrec_config* c, bool grad) {
     l.words = diagrec_words(c->dtype, c->gate, c->packed ? 1 : c->N, c->T, c->D, grad, &l.chunks, &l.groups, &l.agg_words);
     l.total = kAlign + align_up(l.words * 8);
     return l;
+}
+
+bool too_large(const deer_diagrec_config* c, bool grad) {
+    if (c->T > kMostRows || c->D > kMostStride || c->stride_gate > kMostStride || c->stride_in > kMostStride || c->stride_out > kMostStride) return true;
+    if ((long double)c->N * c->D > 1e15L) return true;
+    const long double seqs = c->packed ? 1 : c->N, cols = (c->D + 63) / 64;   // (a channel a lane: most workgroups)
+    return cols * seqs * diag_layout(c, grad).chunks * kDiagLanes > kMostLanes;
 }
 
 DiagrecParams diag_params(const deer_diagrec_config* c, const DiagLayout& l, const int64_t* bounds, void* ws) {
@@ -178,11 +179,12 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
 const char* unsupported(const deer_matrec_config* c, bool step) {
     if (c->dtype != DEER_F32 && c->dtype != DEER_BF16) return "matrix states: fp32 and bf16 only";
     if (c->Dk > 128 || c->Dv > 128) return "matrix states: Dk and Dv up to 128";
-    if (step) return (long long)c->N * c->Hv > 2147483647ll ? "more rows than a launch holds" : nullptr;
+    if (step) return (long double)c->N * c->Hv * 256 > kMostLanes ? "more rows than a launch holds" : nullptr;
     if (c->T > kMostRows || (long double)c->N * c->Hv * 64 > 2147483647.0L || ((long double)(c->T + 63) / 64 + 4) * (c->packed ? 1 : c->N) * c->Hv > 2147483647.0L)
         return "more rows than a launch holds";
+    // the gradient's: three workgroups of up to 512 lanes a segment and head; four of 256 a chunk
     const MatLayout l = mat_layout(c, true);
-    if ((long double)l.max_segs * l.per * c->Hv > 2147483647.0L || (long double)l.max_segs * l.per * 4 > 2147483647.0L || ((long double)l.max_segs * c->Hv + 8) * 3 > 2147483647.0L || (long double)l.max_segs * c->Hv > 2147483647.0L) return "more rows than a launch holds";
+    if (((long double)l.max_segs * c->Hv + 8) * 3 * 512 > kMostLanes || (long double)l.max_segs * l.per * 4 * 256 > kMostLanes) return "more rows than a launch holds";
     return nullptr;
 }
 MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool grad, const int64_t* bounds, void* workspace) {
@@ -230,7 +232,7 @@ extern "C" {
 deer_status deer_diagrec_workspace_bytes(const deer_diagrec_config* c, int32_t grad, size_t* bytes) {
     if (!bytes) return fail(DEER_ERR_INVALID_ARG, "bytes is NULL");
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
-    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
+    if (too_large(c, grad != 0)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
     *bytes = diag_layout(c, grad != 0).total;
     return DEER_OK;
 }
@@ -238,7 +240,7 @@ deer_status deer_diagrec_workspace_bytes(const deer_diagrec_config* c, int32_t g
 deer_status deer_diagrec_solve(const deer_diagrec_config* c, const void* d_gate, const void* d_in, const void* d_h0, const int64_t* d_bounds,
                                void* d_h, void* d_last, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
-    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
+    if (too_large(c, false)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
     if ((c->T > 0 && (!d_gate || !d_in || !d_h)) || (c->packed && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
     if (misaligned(d_gate, e) || misaligned(d_in, e) || misaligned(d_h, e) || misaligned(d_h0, w) || misaligned(d_last, w) || misaligned(d_bounds, 8))
@@ -258,7 +260,7 @@ deer_status deer_diagrec_grad(const deer_diagrec_config* c, const void* d_gate, 
                               const void* d_h, const void* d_dh, const void* d_dlast, void* d_dgate, void* d_din, void* d_dh0,
                               void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
-    if (too_large(c)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
+    if (too_large(c, true)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
     if ((c->T > 0 && (!d_gate || !d_in || !d_h || !d_dh || !d_dgate || !d_din)) || (c->packed && !d_bounds))
         return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
@@ -288,7 +290,7 @@ deer_status deer_diagrec_step(const deer_diagrec_config* c, const void* d_gate, 
     const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
     if (misaligned(d_gate, e) || misaligned(d_in, e) || misaligned(d_h, e) || misaligned(d_state, w) || misaligned(d_slots, 4))
         return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
-    if ((long long)c->N * ((c->D + 255) / 256) > 2147483647ll) return fail(DEER_ERR_UNSUPPORTED, "more rows than a launch holds");
+    if (c->D > (1 << 30) || (long double)c->N * ((c->D + 255) / 256) * 256 > kMostLanes) return fail(DEER_ERR_UNSUPPORTED, "more rows or channels than a launch holds");
     DiagstepParams p{};
     p.rows = StepRows{d_slots, c->N, n_slots};
     p.D = c->D;
@@ -312,7 +314,7 @@ deer_status deer_dropout(int32_t dtype, int32_t N, int64_t T, int32_t D, const v
     if (const char* why = bad_drop(p)) return fail(DEER_ERR_INVALID_ARG, why);
     if (T > 0 && (!d_x || !d_y)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     if (misaligned(d_x, type_bytes(dtype)) || misaligned(d_y, type_bytes(dtype))) return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
-    if (T > kMostRows || (long double)N * ((T + 7) / 8) * D > 256.0L * 2147483647.0L) return fail(DEER_ERR_UNSUPPORTED, "more elements than a launch holds");
+    if (T > kMostRows || (long double)N * ((T + 7) / 8) * D > kMostLanes - 256) return fail(DEER_ERR_UNSUPPORTED, "more elements than a launch holds");
     DropoutParams q{};
     q.N = N;
     q.D = D;

@@ -283,20 +283,33 @@ def _raise(lib, st):
 
 
 def _on_stream(f):
-    """Runs f with the device of its first argument current, and with its keyword `stream` as that device's current stream."""
+    """Runs f with the device of its first argument current, and with its keyword `stream` as that device's current stream.  Where that is
+    another stream than the caller's, tensors that go in and come out are marked as used on both, so that neither's allocations take
+    their memory early; waiting for what the other stream has to do is left to the caller."""
+    name = f.__code__.co_varnames[0]
+
     @functools.wraps(f)
-    def call(first, *args, stream=None, **kw):
+    def call(*args, stream=None, **kw):
+        first = args[0] if args else kw.get(name)
         if not isinstance(first, torch.Tensor) or not first.is_cuda:
             _refuse("need device tensors")
         if stream is not None:
             if stream.device != first.device:
                 _refuse("the stream belongs to another device than the tensors")
+            here = torch.cuda.current_stream(first.device)
             with torch.cuda.stream(stream):
-                return f(first, *args, **kw)
+                result = f(*args, **kw)
+            if stream != here:
+                for t in args + tuple(kw.values()):
+                    if isinstance(t, torch.Tensor) and t.is_cuda:
+                        t.record_stream(stream)
+                for t in result if isinstance(result, tuple) else (result,):
+                    t.record_stream(here)
+            return result
         if first.device.index == torch.cuda.current_device():
-            return f(first, *args, **kw)
+            return f(*args, **kw)
         with torch.cuda.device(first.device):
-            return f(first, *args, **kw)
+            return f(*args, **kw)
     return call
 
 
@@ -305,6 +318,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (a step's
 
 def _stream_of(device):
     return _raw_stream(device.index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _int32(*sizes):
+    for n in sizes:
+        if n > 0x7FFFFFFF:
+            _refuse("sequences, channels and slots are counted in 32 bits")
 
 
 def _row_stride(t, what, lead):
@@ -393,6 +412,7 @@ def _diag_inputs(gate, x, kind, offsets, lengths):
         _refuse("need float32, float64, bfloat16 or float16")
     _check_like(x, "x", gate.shape, gate.dtype, gate.device)
     N, T, packed, bounds, lead = _rows_of(x, 1, offsets, lengths)
+    _int32(N, x.shape[-1])
     return dtype, int(kind), N, x.shape[-1], T, packed, bounds, lead
 
 
@@ -479,6 +499,7 @@ def diagrec_step(gate, x, state, *, kind=DEER_GATE_FACTOR, slots=None, out=None)
         _refuse("state: need [slots, D]")
     sp = _dense(state, "state", state.shape, torch.float64 if dtype == DEER_F64 else torch.float32, dev)
     tp = _dense(slots, "slots", shape[:1], torch.int32, dev)
+    _int32(shape[0], shape[1], state.shape[0])
     cfg = DiagrecConfig(dtype, int(kind), shape[0], shape[1], 1, 0, 0, _row_stride(gate, "gate", 1), _row_stride(x, "x", 1),
                         _row_stride(h, "out", 1), 0.0, 0)
     st = lib.deer_diagrec_step(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), tp, state.shape[0], sp, h.data_ptr(), _stream_of(dev))
@@ -517,6 +538,7 @@ def _mat_config(q, k, v, gate, o, offsets, lengths, scale, lead=None):
     if v.dim() != q.dim():
         _refuse("v: need as many dimensions as q")
     Hv, Dv = v.shape[lead:]
+    _int32(N, Hk, Hv, Dk, Dv)
     _check_like(v, "v", rows + v.shape[lead:], q.dtype, dev)
     if Hk < 1 or Hv % Hk:
         _refuse("the heads of v must be a multiple of those of q and k")
@@ -589,6 +611,7 @@ def matrec_step(q, k, v, gate, state, *, slots=None, scale=None, out=None):
         _refuse("state: need [slots, Hv, Dk, Dv]")
     sp = _dense(state, "state", (state.shape[0], cfg.Hv, cfg.Dk, cfg.Dv), torch.float32, dev)
     tp = _dense(slots, "slots", q.shape[:1], torch.int32, dev)
+    _int32(state.shape[0])
     st = lib.deer_matrec_step(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, tp, state.shape[0], sp, o.data_ptr(), _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
@@ -609,6 +632,7 @@ def dropout(x, p, seed, draw=0, *, out=None):
         y = out
         _check_like(y, "out", x.shape, x.dtype, dev)
     N, T, D = x.shape if lead == 2 else (1,) + tuple(x.shape)
+    _int32(N, D)
     st = lib.deer_dropout(dtype, N, T, D, x.data_ptr(), _row_stride(x, "x", lead), y.data_ptr(), _row_stride(y, "out", lead), p,
                           seed & 0xFFFFFFFFFFFFFFFF, draw & 0xFFFFFFFF, _stream_of(dev))
     if st != DEER_OK:

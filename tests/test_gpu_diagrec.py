@@ -364,3 +364,34 @@ def test_refusals():
         with pytest.raises(deer.DeerError) as e:
             call()
         assert e.value.status == deer.DEER_ERR_INVALID_ARG
+
+
+def test_inputs_given_up_while_another_stream_reads_them():
+    gate, x, h0 = make("sigmoid", "bf16", (1, 4000), 1, 512, 21)[:3]
+    want = deer.diagrec_solve(gate=gate, x=x, h0=h0, kind=2)[0]
+    side = torch.cuda.Stream()
+    mine = x.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    got = deer.diagrec_solve(gate, mine, h0, kind=2, stream=side)[0]
+    del mine
+    other = [torch.full_like(x, 7.0) for _ in range(4)]   # would take the memory of `mine` on this stream, with nothing to wait for
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(other) == 4
+
+
+def test_rows_beyond_32_bits():
+    T, far = 1100, 1 << 22                                 # 1,100 rows 2^22 elements apart: offsets up to 4.6e9 elements
+    gate, x, h0, dh, dlast = make("sigmoid", "bf16", (T,), 2, 128, 22)
+    offsets = torch.tensor([0, 700, T], device=DEV)
+    h, last = deer.diagrec_solve(gate, x, h0, kind=2, offsets=offsets)
+    want = (h, last) + deer.diagrec_grad(gate, x, h, dh, h0, dlast, kind=2, offsets=offsets) + (deer.dropout(x, 0.3, 5),)
+    wide = torch.empty(T, far, dtype=torch.bfloat16, device=DEV)
+    g, u, d, y, dg, du, z = (wide[:, 128 * i:128 * i + 128] for i in range(7))
+    for a, b in ((g, gate), (u, x), (d, dh)):
+        a.copy_(b)
+    got = deer.diagrec_solve(g, u, h0, kind=2, offsets=offsets, out=y)
+    got += deer.diagrec_grad(g, u, y, d, h0, dlast, kind=2, offsets=offsets, dgate=dg, dx=du) + (deer.dropout(u, 0.3, 5, out=z),)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)

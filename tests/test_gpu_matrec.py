@@ -339,3 +339,47 @@ def test_refusals():
         with pytest.raises(deer.DeerError) as e:
             call()
         assert e.value.status == status
+
+
+def test_rows_beyond_32_bits():
+    T, far = 1100, 1 << 22                                 # 1,100 rows 2^22 elements apart: offsets up to 4.6e9 elements
+    d = make("bf16", (T,), 2, 1, 2, 32, 64, 6)
+    offsets = torch.tensor([0, 300, T], device=DEV)
+    want = both(d, offsets=offsets)
+    wide = torch.empty(T, far, dtype=torch.bfloat16, device=DEV)
+    e, at = dict(d), 0
+    for n in ("q", "k", "v", "do"):
+        H, D = d[n].shape[1:]
+        e[n] = wide[:, at:at + H * D].unflatten(-1, (H, D))
+        e[n].copy_(d[n])
+        at += H * D
+    grads = {}
+    for n, like in (("dq", "q"), ("dk", "k"), ("dv", "v")):
+        H, D = d[like].shape[1:]
+        grads[n] = wide[:, at:at + H * D].unflatten(-1, (H, D))
+        at += H * D
+    got = deer.matrec_solve(e["q"], e["k"], e["v"], e["g"], e["s0"], offsets=offsets)
+    got += deer.matrec_grad(e["q"], e["k"], e["v"], e["g"], e["do"], e["s0"], e["dlast"], offsets=offsets, **grads)
+    for n, a in zip(NAMES, got):
+        assert torch.equal(a, want[n]), n
+
+
+def test_many_sequences_of_a_row_or_none():
+    """more cells of states than a launch has work items"""
+    N, H, K, V = 16400, 64, 4, 4
+    rng = torch.Generator(device="cuda").manual_seed(3)
+    lengths = torch.randint(0, 2, (N,), device=DEV, generator=rng)
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), lengths.cumsum(0)])
+    T = int(offsets[-1])
+    q, k = torch.randn(T, H, K, device=DEV, generator=rng), torch.randn(T, H, K, device=DEV, generator=rng)
+    v, g = torch.randn(T, H, V, device=DEV, generator=rng), -torch.rand(T, H, device=DEV, generator=rng)
+    s0 = torch.randn(N, H, K, V, device=DEV, generator=rng)
+    o, last = deer.matrec_solve(q, k, v, g, s0, offsets=offsets, scale=1.0)
+    want, some = s0.double(), lengths == 1
+    want[some] = want[some] * g.double().exp()[..., None, None] + k.double()[..., :, None] * v.double()[..., None, :]
+    size = s0.abs().max().double() + k.abs().max() * v.abs().max()
+    # two products and a sum, and a factor of 2 units in the last place: five roundings
+    assert float((last - want).abs().max()) <= 5 * 2.0 ** -24 * float(size)
+    assert torch.equal(last[~some], s0[~some])
+    wo = (want[some] * q.double()[..., :, None]).sum(-2)
+    assert float((o - wo).abs().max()) <= (5 + 1 + K) * 2.0 ** -24 * K * float(size * q.abs().max())

@@ -105,3 +105,30 @@ def test_matrec_pointers_and_workspace():
     for c, bad in ((cfg, dict(q=None)), (cfg, dict(n=0)), (cfg, dict(s=None)), (cfg, dict(s=ctypes.c_void_p(258))), (mat(Hv=3), {})):
         assert step(c, **bad) == deer.DEER_ERR_INVALID_ARG
     assert step(mat(Dk=200)) == deer.DEER_ERR_UNSUPPORTED
+
+
+def test_more_work_items_than_a_launch_holds():
+    """2^32 - 1 of them: a workgroup has 512 (recurrences) or 256 (single tokens)"""
+    lib, size = deer.load_library(), ctypes.c_size_t(0)
+    for grad in (0, 1):
+        assert lib.deer_diagrec_workspace_bytes(ctypes.byref(diag(N=(1 << 23) - 1, T=1, D=1)), grad, ctypes.byref(size)) == deer.DEER_OK
+        assert lib.deer_diagrec_workspace_bytes(ctypes.byref(diag(N=1 << 23, T=1, D=1)), grad, ctypes.byref(size)) == deer.DEER_ERR_UNSUPPORTED
+        assert lib.deer_diagrec_workspace_bytes(ctypes.byref(diag(N=1 << 17, T=1 << 12, D=1024)), grad, ctypes.byref(size)) == deer.DEER_ERR_UNSUPPORTED
+    step = lambda **kw: lib.deer_diagrec_step(ctypes.byref(diag(**kw)), WORD, WORD, None, 4, WORD, WORD, None)   # noqa: E731
+    assert step(D=0x7FFFFFFF) == deer.DEER_ERR_UNSUPPORTED and step(N=1 << 24, D=1) == deer.DEER_ERR_UNSUPPORTED
+    assert lib.deer_dropout(0, 1 << 20, 1 << 16, 1, WORD, 0, WORD, 0, 0.5, 1, 0, None) == deer.DEER_ERR_UNSUPPORTED
+    assert lib.deer_matrec_workspace_bytes(ctypes.byref(mat(N=1 << 18, T=1)), 0, ctypes.byref(size)) == deer.DEER_OK
+    assert lib.deer_matrec_workspace_bytes(ctypes.byref(mat(N=1 << 20, T=1)), 0, ctypes.byref(size)) == deer.DEER_ERR_UNSUPPORTED
+    assert lib.deer_matrec_step(ctypes.byref(mat(N=1 << 22)), WORD, WORD, WORD, WORD, None, 4, WORD, WORD, None) == deer.DEER_ERR_UNSUPPORTED
+
+
+def test_binding_takes_keywords_and_counts_in_32_bits():
+    import torch
+    x = torch.zeros(2, 8, 4)
+    for call in (lambda: deer.diagrec_solve(gate=x, x=x), lambda: deer.diagrec_solve(x=x), lambda: deer.dropout(x=x, p=0.5, seed=1)):
+        with pytest.raises(deer.DeerError) as e:
+            call()
+        assert e.value.status == deer.DEER_ERR_INVALID_ARG
+    deer._int32(0x7FFFFFFF)
+    with pytest.raises(deer.DeerError):
+        deer._int32(1, 0x80000000)
