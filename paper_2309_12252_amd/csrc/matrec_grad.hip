@@ -76,10 +76,12 @@ __global__ __launch_bounds__(256) void matrec_gates_kernel(const MatrecParams p)
     for (int i = threadIdx.x; i < rows * p.Hv; i += 256) p.dgate[first + i] += p.gate_k[first + i] + p.read_in[chunk + i % p.Hv];
 }
 
-// dq and dk of shared heads: the heads of v that go with one, in their order; a workgroup has 16 rows of a chunk
+// dq and dk of shared heads: the heads of v that go with one, in their order; a workgroup has 16 rows of a chunk and up to 64 V columns
 constexpr int kSharedRows = 16;
-template <typename T>
+template <typename T, int V>
 __global__ __launch_bounds__(256) void matrec_shared_kernel(const MatrecParams p) {
+    using FV = vec_t<float, V>;
+    using TV = vec_t<T, V>;
     constexpr int PARTS = kChunk / kSharedRows;
     const int chunk = blockIdx.x / PARTS, seg_no = chunk / p.plan.per, c = chunk % p.plan.per;
     MatSegment seg;
@@ -87,18 +89,33 @@ __global__ __launch_bounds__(256) void matrec_shared_kernel(const MatrecParams p
     const long long first = (long long)c * kChunk + blockIdx.x % PARTS * kSharedRows, left = seg.rows - first;
     if (left <= 0) return;
     const int rows = left < kSharedRows ? (int)left : kSharedRows, group = p.Hv / p.Hk, cols = p.Hk * p.Dk;
-    const float* part = blockIdx.y == 0 ? p.part_q : p.part_k;
-    T* to = reinterpret_cast<T*>(blockIdx.y == 0 ? p.dq : p.dk);
-    const long long stride = blockIdx.y == 0 ? p.stride_q : p.stride_k, row0 = seg.row0 + first;
-    for (int col = threadIdx.x % 64; col < cols; col += 64) {
+    const bool of_q = blockIdx.y == 0;
+    const float* part = of_q ? p.part_q : p.part_k;
+    T* to = reinterpret_cast<T*>(of_q ? p.dq : p.dk);
+    const long long stride = of_q ? p.stride_q : p.stride_k, row0 = seg.row0 + first;
+    for (int col = ((int)blockIdx.z * 64 + threadIdx.x % 64) * V; col < cols; col += (int)gridDim.z * 64 * V) {
         const int kh = col / p.Dk, d = col % p.Dk;
-        for (int r = threadIdx.x / 64; r < rows; r += 4) {
+#pragma unroll
+        for (int i = 0; i < kSharedRows / 4; ++i) {
+            const int r = threadIdx.x / 64 + 4 * i;
+            if (r >= rows) break;
             const float* from = part + ((row0 + r) * p.Hv + (long long)kh * group) * p.Dk + d;
-            float s = 0.0f;
-            for (int m = 0; m < group; ++m) s += from[(long long)m * p.Dk];
-            to[(row0 + r) * stride + col] = (T)s;
+            FV s = *reinterpret_cast<const FV*>(from);
+            for (int m = 1; m < group; ++m) s += *reinterpret_cast<const FV*>(from + (long long)m * p.Dk);
+            T* at = to + (row0 + r) * stride + col;
+            if constexpr (V == 1) *at = (T)s;
+            else *reinterpret_cast<TV*>(at) = __builtin_convertvector(s, TV);
         }
     }
+}
+template <typename T>
+hipError_t launch_shared(const MatrecParams& p, unsigned chunks, hipStream_t stream) {
+    const bool wide = four_wide(reinterpret_cast<const T*>(p.dq), p.stride_q, p.Dk) && four_wide(reinterpret_cast<const T*>(p.dk), p.stride_k, p.Dk);
+    const int per = wide ? 256 : 64, parts = (p.Hk * p.Dk + per - 1) / per;
+    const dim3 grid(chunks * (kChunk / kSharedRows), 2, parts > 16 ? 16 : parts);
+    if (wide) hipLaunchKernelGGL((matrec_shared_kernel<T, 4>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((matrec_shared_kernel<T, 1>), grid, dim3(256), 0, stream, p);
+    return hipGetLastError();
 }
 
 template <typename T, int DK, int DV>
@@ -114,9 +131,8 @@ hipError_t launch_matrec_grad(int dtype, const MatrecParams& p, hipStream_t stre
     const unsigned chunks = (unsigned)((long long)p.plan.max_segs * p.plan.per);
     if (e != hipSuccess || chunks == 0) return e;
     if (p.Hv != p.Hk) {
-        if (dtype == DEER_BF16) hipLaunchKernelGGL((matrec_shared_kernel<BF16>), dim3(chunks * (kChunk / kSharedRows), 2), dim3(256), 0, stream, p);
-        else hipLaunchKernelGGL((matrec_shared_kernel<float>), dim3(chunks * (kChunk / kSharedRows), 2), dim3(256), 0, stream, p);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = dtype == DEER_BF16 ? launch_shared<BF16>(p, chunks, stream) : launch_shared<float>(p, chunks, stream);
+        if (e != hipSuccess) return e;
     }
     if (!p.dgate) return hipSuccess;
     hipLaunchKernelGGL(matrec_through_kernel, dim3((unsigned)(((long long)p.plan.max_segs * p.Hv + 255) / 256)), dim3(256), 0, stream, p);

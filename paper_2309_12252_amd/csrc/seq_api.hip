@@ -135,13 +135,12 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
     const long long longest = (c->T + kChunk - 1) / kChunk;
     l.chunks = c->packed ? longest + c->N : longest * c->N;
     long long per = longest < 1 ? 1 : longest;
-    if (c->packed || (long long)c->N * c->Hv < 256) {
+    if (longest > 4 && (c->packed || (long long)c->N * c->Hv < 256)) {
         // 512 workgroups run at a time; every sequence's last segment is a short one, half of the others' length on average
         long long segs = 512 / c->Hv - (c->packed ? c->N / 2 : 0);
         if (segs < 1) segs = 1;
-        const long long want = ((c->packed ? longest : l.chunks) + segs - 1) / segs;
-        per = want < 4 ? 4 : want;
-        if (per > longest) per = longest < 1 ? 1 : longest;
+        per = ((c->packed ? longest : l.chunks) + segs - 1) / segs;
+        if (per > longest) per = longest;
     }
     if (grad && per > 32) per = 32;   // what goes through the chunks of a segment (matrec_grad.hip) takes the rounding errors of all of them
     l.per = (int)per;
