@@ -25,7 +25,7 @@ struct GradShape {
     static constexpr size_t lds = a > b ? (a > c ? a : c) : (b > c ? b : c);
 };
 
-// dq, dk and dv of a segment and head at the same time and on the same XCD (workgroups go to the 8 XCDs in turn): they read the same rows
+// Registers and what bounds it: matrec_run.h.  dq, dk and dv of a segment and head at the same time and on the same XCD (workgroups go to the 8 XCDs in turn): they read the same rows
 template <typename T, int DK, int DV>
 __global__ __launch_bounds__(4 * (DK > DV ? DK : DV), sizeof(T) == 2 ? (DK == 128 || DV == 128 ? 4 : 3) : 2) void matrec_grad_kernel(const MatrecParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
@@ -76,7 +76,9 @@ __global__ __launch_bounds__(256) void matrec_gates_kernel(const MatrecParams p)
     for (int i = threadIdx.x; i < rows * p.Hv; i += 256) p.dgate[first + i] += p.gate_k[first + i] + p.read_in[chunk + i % p.Hv];
 }
 
-// dq and dk of shared heads: the heads of v that go with one, in their order; a workgroup has 16 rows of a chunk and up to 64 V columns
+// dq and dk of shared heads: the heads of v that go with one, in their order; a workgroup has 16 rows of a chunk and up to 64 V columns.
+// Memory bound; the columns are spread over workgroups because a short call is one chain of loads after another (gradient of 128 rows, 8 heads of 128
+// for 16: 69 us with all columns of 16 rows in a workgroup, one a lane; 33 so).
 constexpr int kSharedRows = 16;
 template <typename T, int V>
 __global__ __launch_bounds__(256) void matrec_shared_kernel(const MatrecParams p) {

@@ -9,7 +9,10 @@
 // results, which are operands of M^T a as they stand, and the outputs', transposed, a lane four or eight neighbouring columns of a row.
 // What bounds it: 120 to 210 matrix instructions of 16 cycles and some 500 vector instructions a wavefront and chunk of 128 columns, which a SIMD does one
 // after another, and 64 KiB of rows a chunk.  Two workgroups fill a CU and go on while the other one waits for its rows, which go straight to LDS: no
-// registers for them, so that 128 are enough.
+// registers for them, so that 128 are enough (one workgroup a CU with its next rows in registers: gradient of 4 x 4,096 rows, 16 heads of
+// 128 x 128, 431 us; so 310 to 350).  Vector instructions take 62 % of a SIMD's cycles there and matrix instructions 24 %, and they do not overlap.  Outputs: 46 us for prompts of 8,192 rows
+// and 16 heads of 128 x 128, 52 for 1 x 32,768 rows and 8 heads of 128 x 64, 78 for 4 x 4,096 rows and 16 heads of 128 x 128 (110 TFLOP/s).  fp32: the
+// products are four-term instructions of 32 cycles and bound it.
 #pragma once
 #include "matrec_common.h"
 
