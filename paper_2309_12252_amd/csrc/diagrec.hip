@@ -70,17 +70,18 @@ __device__ __forceinline__ unsigned long long get_word(const unsigned long long*
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// K words `step` apart, once all of them are there; kUnset in their place after kPolls polls
-template <int K>
-__device__ __forceinline__ void wait_words(const unsigned long long* p, long long step, int count, unsigned long long (&w)[K]) {
+// `count` of K items of E words each, `step` words apart, and what `front` points to, once all of them are there; kUnset in their place after kPolls polls
+template <int K, int E>
+__device__ __forceinline__ void wait_words(const unsigned long long* p, long long step, int count, unsigned long long (&w)[K * E], const unsigned long long* front,
+                                           unsigned long long& f) {
     for (long long poll = 0; poll < kPolls; ++poll) {
+        f = front ? get_word(front) : 0;
         bool all = true;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            w[k] = k < count ? get_word(p + k * step) : 0;
-            all = all && w[k] != kUnset;
-        }
-        if (__all(all)) return;
+        for (int k = 0; k < K * E; ++k) w[k] = k / E < count ? get_word(p + k / E * step + k % E) : 0;
+#pragma unroll
+        for (int k = 0; k < K * E; ++k) all = all && w[k] != kUnset;
+        if (__all(all && f != kUnset)) return;
         __builtin_amdgcn_s_sleep(2);
     }
 }
@@ -102,6 +103,15 @@ __device__ __forceinline__ wide_t<T> value_of(bits_t<T, V> b, int v) {
         return (wide_t<T>)__builtin_bit_cast(T, b);
     }
 }
+template <typename T, int V>
+__device__ __forceinline__ void set_value(bits_t<T, V>& b, int v, T x) {
+    if constexpr (sizeof(T) == 4 && V == 2) {
+        const unsigned long long u = __builtin_bit_cast(unsigned, x);
+        b = v == 0 ? (b & ~0xFFFFFFFFull) | u : (b & 0xFFFFFFFFull) | u << 32;
+    } else {
+        b = __builtin_bit_cast(bits_t<T, V>, x);
+    }
+}
 template <typename T, int V, bool DROP>
 __device__ __forceinline__ wide_t<T> input_of(bits_t<T, V> b, int v, unsigned kept, wide_t<T> scale) {
     const wide_t<T> x = value_of<T, V>(b, v);
@@ -114,35 +124,39 @@ __device__ __forceinline__ void forget(X& x) {
     asm volatile("" : "+v"(x));
 }
 
-// fold of `count` tiles' maps into h
-__device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long long step, int count, bool first_resets, float& h) {
+// The state behind `front` (nullptr: a first tile that sets it) and `count` tiles' maps.  What is in front comes with the first of the maps: they are there
+// before it, so that one trip to memory is left when it arrives.
+__device__ __forceinline__ float fold_tiles(const unsigned long long* agg, long long step, int count, const unsigned long long* front, float) {
     constexpr int K = 8;
-    for (int at = 0; at < count; at += K) {
-        const int some = count - at < K ? count - at : K;
-        unsigned long long w[K];
-        wait_words<K>(agg + (long long)at * step, step, some, w);
+    float h = 0.0f;
+    for (int at = 0; at == 0 || at < count; at += K) {
+        unsigned long long w[K], f;
+        wait_words<K, 1>(agg + (long long)at * step, step, count - at, w, at == 0 ? front : nullptr, f);
+        if (at == 0 && front) h = __uint_as_float((unsigned)(f >> 32));
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (k < some) {
+            if (at + k < count) {
                 const float a = __uint_as_float((unsigned)w[k]), u = __uint_as_float((unsigned)(w[k] >> 32));
-                h = (first_resets && at + k == 0) ? u : a * h + u;
+                h = (!front && at + k == 0) ? u : a * h + u;
             }
     }
+    return h;
 }
-__device__ __forceinline__ void fold_tiles(const unsigned long long* agg, long long step, int count, bool first_resets, double& h) {
-    constexpr int K = 4;
-    for (int at = 0; at < count; at += K) {
-        const int some = count - at < K ? count - at : K;
-        unsigned long long wa[K], wu[K];
-        wait_words<K>(agg + (long long)at * step, step, some, wa);
-        wait_words<K>(agg + (long long)at * step + 1, step, some, wu);
+__device__ __forceinline__ double fold_tiles(const unsigned long long* agg, long long step, int count, const unsigned long long* front, double) {
+    constexpr int K = 8;
+    double h = 0.0;
+    for (int at = 0; at == 0 || at < count; at += K) {
+        unsigned long long w[2 * K], f;
+        wait_words<K, 2>(agg + (long long)at * step, step, count - at, w, at == 0 ? front : nullptr, f);
+        if (at == 0 && front) h = __longlong_as_double((long long)f);
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (k < some) {
-                const double a = __longlong_as_double((long long)wa[k]), u = __longlong_as_double((long long)wu[k]);
-                h = (first_resets && at + k == 0) ? u : a * h + u;
+            if (at + k < count) {
+                const double a = __longlong_as_double((long long)w[2 * k]), u = __longlong_as_double((long long)w[2 * k + 1]);
+                h = (!front && at + k == 0) ? u : a * h + u;
             }
     }
+    return h;
 }
 
 // Memory bound: every input is read once and every output written once (805 MB of bf16 in 156 us with log gates, 5.2 TB/s, the rate of a large copy;
@@ -207,6 +221,9 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
 
     // ---- the rows' inputs, all reads at a time ----
     constexpr bool NEED_X = !REV || KIND == DEER_GATE_SIGMOID;
+    // an exponential that has as many bits as its gate takes the gate's place once it is known
+    constexpr bool IN_PLACE = KIND == DEER_GATE_LOG && sizeof(T) >= 4;
+    constexpr int SECOND = IN_PLACE ? (int)DEER_GATE_FACTOR : KIND;
     using B = bits_t<T, V>;
     B rg[R], rx[NEED_X ? R : 1], rh[REV ? R : 1], rd[REV ? R : 1];
     unsigned keep[DROP ? V : 1] = {};
@@ -269,6 +286,7 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
                 for (int v = 0; v < V; ++v) {
                     S a, w;
                     gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
+                    if constexpr (IN_PLACE) set_value<T, V>(rg[j], v, a);
                     if constexpr (REV) H[v] = a * (value_of<T, V>(rd[j], v) + H[v]);
                     else H[v] = a * H[v] + w * input_of<T, V, DROP>(rx[j], v, (keep[DROP ? v : 0] >> j) & 1u, scale);
                     A[v] *= a;
@@ -331,13 +349,7 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
             const int c_group = c / kGroup * kGroup;
             const bool from_group = begin_c < c_group;
             const int from = from_group ? c_group : (begin_c < c ? begin_c : c);
-            if (from_group) {
-                unsigned long long w[1];
-                wait_words<1>(inc + (long long)(c / kGroup - 1) * D, 0, 1, w);
-                if constexpr (WORDS == 1) carry = __uint_as_float((unsigned)(w[0] >> 32));
-                else carry = __longlong_as_double((long long)w[0]);
-            }
-            fold_tiles(agg + (long long)from * D * WORDS, D * WORDS, c - from, !from_group, carry);
+            carry = fold_tiles(agg + (long long)from * D * WORDS, D * WORDS, c - from, from_group ? inc + (long long)(c / kGroup - 1) * D : nullptr, S(0));
         }
         if (has && c % kGroup == kGroup - 1) {
             const S out = reset ? th : ta * carry + th;
@@ -399,7 +411,7 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 S a, w;
-                gate_factors<T, KIND>(value_of<T, V>(rg[j], v), a, w);
+                gate_factors<T, SECOND>(value_of<T, V>(rg[j], v), a, w);
                 if constexpr (REV) {
                     const S lam = value_of<T, V>(rd[j], v) + h[v];
                     h[v] = a * lam;
