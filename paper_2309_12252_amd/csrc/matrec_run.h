@@ -10,8 +10,8 @@
 // What bounds it: 120 to 210 matrix instructions of 16 cycles and some 500 vector instructions a wavefront and chunk of 128 columns, which a SIMD does one
 // after another, and 64 KiB of rows a chunk.  Two workgroups fill a CU and go on while the other one waits for its rows, which go straight to LDS: no
 // registers for them, so that 128 are enough (one workgroup a CU with its next rows in registers: gradient of 4 x 4,096 rows, 16 heads of
-// 128 x 128, 431 us; so 310 to 350).  Vector instructions take 62 % of a SIMD's cycles there and matrix instructions 24 %, and they do not overlap.  Outputs: 46 us for prompts of 8,192 rows
-// and 16 heads of 128 x 128, 52 for 1 x 32,768 rows and 8 heads of 128 x 64, 78 for 4 x 4,096 rows and 16 heads of 128 x 128 (110 TFLOP/s).  fp32: the
+// 128 x 128, 431 us; so 295 to 320).  Vector instructions take 62 % of a SIMD's cycles there and matrix instructions 24 %, and they do not overlap.  Outputs: 42 us for prompts of 8,192 rows
+// and 16 heads of 128 x 128, 48 for 1 x 32,768 rows and 8 heads of 128 x 64, 75 for 4 x 4,096 rows and 16 heads of 128 x 128.  fp32: the
 // products are four-term instructions of 32 cycles and bound it.
 #pragma once
 #include "matrec_common.h"
@@ -183,7 +183,6 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         }
 
         // ---- pairs, tile by tile, transposed: a lane has one i and four neighbouring j ----
-        __builtin_amdgcn_s_setprio(1);   // (over wavefronts of the other workgroup, which wait or store: outputs of 4 x 4,096 rows 86 -> 76 us, gradient 351 -> 304)
         auto pair_tile = [&](int n) {
             int ti, tj;
             lower_tile(n, ti, tj);
@@ -219,10 +218,14 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                 }
             }
         };
+        // Products go in front of the other workgroup's wavefronts, which load or store, the state's in front of all: outputs of 4 x 4,096 rows
+        // and 16 heads of 128 x 128 86 -> 75 us, gradient 351 -> 305.
+        __builtin_amdgcn_s_setprio(1);
         pair_tile(wave);
         if (W < 8) pair_tile(wave + W);
         if (wave < 10 % W) pair_tile(wave + 10 / W * W);
 
+        __builtin_amdgcn_s_setprio(2);
         // ---- the state: what it gives to the outputs, then the chunk's rows into it ----
         F32x4 acc[4][VT];
         frag_t<T> cf[2][VT];
