@@ -425,7 +425,7 @@ def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, leng
     dtype, kind, N, D, T, packed, bounds, lead = _diag_inputs(gate, x, kind, offsets, lengths)
     dev, w = x.device, torch.float64 if dtype == DEER_F64 else torch.float32
     if out is None:
-        h = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        h = torch.empty_like(x, memory_format=torch.contiguous_format)
     else:
         h = out
         _check_like(h, "out", x.shape, x.dtype, dev)
@@ -434,7 +434,7 @@ def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, leng
     last = torch.empty((N, D), dtype=w, device=dev)
     h0p = _dense(h0, "h0", last.shape, w, dev)
     size = _diag_workspace(0, dtype, kind, N, D, T, packed)
-    ws = torch.empty(size, dtype=torch.uint8, device=dev)   # (torch's blocks are aligned to 512 bytes)
+    ws = x.new_empty(size, dtype=torch.uint8)   # (torch's blocks are aligned to 512 bytes)
     st = lib.deer_diagrec_solve(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), last.data_ptr(), ws.data_ptr(), size,
                                 _stream_of(dev))
     if st != DEER_OK:
@@ -457,13 +457,13 @@ def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, 
         h, dh, stride_h = h.contiguous(), dh.contiguous(), D
     stride_g, stride_x = _row_stride(gate, "gate", lead), _row_stride(x, "x", lead)
     if dgate is None:
-        dgate = torch.empty(gate.shape, dtype=x.dtype, device=dev) if stride_g == D else _rows_like(gate, stride_g)
+        dgate = torch.empty_like(gate, memory_format=torch.contiguous_format) if stride_g == D else _rows_like(gate, stride_g)
     else:
         _check_like(dgate, "dgate", x.shape, x.dtype, dev)
         if _row_stride(dgate, "dgate", lead) != stride_g:
             _refuse("dgate: rows must lie like those of gate")
     if dx is None:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if stride_x == D else _rows_like(x, stride_x)
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format) if stride_x == D else _rows_like(x, stride_x)
     else:
         _check_like(dx, "dx", x.shape, x.dtype, dev)
         if _row_stride(dx, "dx", lead) != stride_x:
@@ -472,7 +472,7 @@ def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, 
     dh0 = torch.empty((N, D), dtype=w, device=dev)
     h0p, dlp = _dense(h0, "h0", dh0.shape, w, dev), _dense(dlast, "dlast", dh0.shape, w, dev)
     size = _diag_workspace(1, dtype, kind, N, D, T, packed)
-    ws = torch.empty(size, dtype=torch.uint8, device=dev)
+    ws = x.new_empty(size, dtype=torch.uint8)
     st = lib.deer_diagrec_grad(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), dh.data_ptr(), dlp, dgate.data_ptr(),
                                dx.data_ptr(), dh0.data_ptr(), ws.data_ptr(), size, _stream_of(dev))
     if st != DEER_OK:
@@ -491,7 +491,7 @@ def diagrec_step(gate, x, state, *, kind=DEER_GATE_FACTOR, slots=None, out=None)
     dev, shape = x.device, x.shape
     _check_like(gate, "gate", shape, x.dtype, dev)
     if out is None:
-        h = torch.empty(shape, dtype=x.dtype, device=dev)
+        h = torch.empty_like(x, memory_format=torch.contiguous_format)
     else:
         h = out
         _check_like(h, "out", shape, x.dtype, dev)
@@ -561,7 +561,7 @@ def matrec_solve(q, k, v, gate, s0=None, *, offsets=None, lengths=None, scale=No
     dev, shape = q.device, (cfg.N, cfg.Hv, cfg.Dk, cfg.Dv)
     s0p = _dense(s0, "s0", shape, torch.float32, dev)
     size = _mat_workspace(0, cfg.dtype, cfg.N, cfg.T, cfg.packed, cfg.Hk, cfg.Hv, cfg.Dk, cfg.Dv)
-    ws = torch.empty(size, dtype=torch.uint8, device=dev)
+    ws = q.new_empty(size, dtype=torch.uint8)
     last = torch.empty(shape, dtype=torch.float32, device=dev)
     st = lib.deer_matrec_solve(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, s0p, bounds, o.data_ptr(), last.data_ptr(),
                                ws.data_ptr(), size, _stream_of(dev))
@@ -589,7 +589,7 @@ def matrec_grad(q, k, v, gate, do, s0=None, dlast=None, *, offsets=None, lengths
     shape = (cfg.N, cfg.Hv, cfg.Dk, cfg.Dv)
     s0p, dlp = _dense(s0, "s0", shape, torch.float32, dev), _dense(dlast, "dlast", shape, torch.float32, dev)
     size = _mat_workspace(1, cfg.dtype, cfg.N, cfg.T, cfg.packed, cfg.Hk, cfg.Hv, cfg.Dk, cfg.Dv)
-    ws = torch.empty(size, dtype=torch.uint8, device=dev)
+    ws = q.new_empty(size, dtype=torch.uint8)
     dgate = torch.empty(gate.shape, dtype=torch.float32, device=dev)
     ds0 = torch.empty(shape, dtype=torch.float32, device=dev)
     st = lib.deer_matrec_grad(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, s0p, bounds, do.data_ptr(), dlp, outs[0].data_ptr(),
@@ -627,7 +627,7 @@ def dropout(x, p, seed, draw=0, *, out=None):
     if dtype is None or lead not in (1, 2):
         _refuse("need x [N, T, D] or [rows, D] in float32, float64, bfloat16 or float16")
     if out is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
     else:
         y = out
         _check_like(y, "out", x.shape, x.dtype, dev)
