@@ -246,7 +246,7 @@ deer_status deer_linrec_solve_static(int32_t dtype, int32_t B, int32_t T, int32_
  *   - Rows.  packed = 0: N sequences of T rows, row t of sequence n is row n T + t of every array; d_bounds (device, int64 [N], or NULL) holds how
  *     many rows of each count.  packed = 1: the sequences lie one behind the other in T rows; d_bounds (device, int64 [N + 1], not NULL) holds
  *     where they begin, its last entry where the last one ends.  Sequences may be empty: their final state is the initial
- *     one.  Rows that belong to no sequence are neither read nor written.  Bounds outside 0 .. T are clamped;
+ *     one.  Rows that belong to no sequence have no influence and are not written.  Bounds outside 0 .. T are clamped;
  *     packed bounds that decrease give results without meaning, within the arrays.
  *   - stride_*: elements from one row to the next (0: dense), so that slices of a wider array can be handed in; the
  *     last dimension is dense (deer_diagrec_solve(), deer_diagrec_grad(): rows and strides of at most 2^22).  A call whose largest launch
