@@ -88,6 +88,8 @@ typedef enum { DEER_CELL_GRU = 0, DEER_CELL_MLP_ODE = 1, DEER_CELL_LSTM = 2, DEE
 typedef enum { DEER_F32 = 0, DEER_F64 = 1, DEER_BF16 = 2, DEER_F16 = 3 } deer_dtype; /* 16 bits: sequence operators only */
 /* factor a_t of a gated recurrence, from its gate g: a = g; a = exp(g); a = 1 / (1 + exp(-g)), the input weighted with 1 - a */
 typedef enum { DEER_GATE_FACTOR = 0, DEER_GATE_LOG = 1, DEER_GATE_SIGMOID = 2 } deer_gate;
+/* how rows lie (member `packed`), and what becomes of rows in the outputs that belong to no sequence: left as they are, or zeroed */
+typedef enum { DEER_ROWS_PADDED = 0, DEER_ROWS_PACKED = 1, DEER_REST_ZERO = 256 } deer_rows;
 typedef enum { DEER_ACT_TANH = 0, DEER_ACT_SOFTPLUS = 1 } deer_activation;
 
 typedef struct {
@@ -246,7 +248,8 @@ deer_status deer_linrec_solve_static(int32_t dtype, int32_t B, int32_t T, int32_
  *   - Rows.  packed = 0: N sequences of T rows, row t of sequence n is row n T + t of every array; d_bounds (device, int64 [N], or NULL) holds how
  *     many rows of each count.  packed = 1: the sequences lie one behind the other in T rows; d_bounds (device, int64 [N + 1], not NULL) holds
  *     where they begin, its last entry where the last one ends.  Sequences may be empty: their final state is the initial
- *     one.  Rows that belong to no sequence have no influence and are not written.  Bounds outside 0 .. T are clamped;
+ *     one.  Rows that belong to no sequence have no influence; in the outputs they are not written, or zeroed where
+ *     DEER_REST_ZERO is added to packed.  Bounds outside 0 .. T are clamped;
  *     packed bounds that decrease give results without meaning, within the arrays.
  *   - stride_*: elements from one row to the next (0: dense), so that slices of a wider array can be handed in; the
  *     last dimension is dense (deer_diagrec_solve(), deer_diagrec_grad(): rows and strides of at most 2^22).  A call whose largest launch
@@ -260,7 +263,7 @@ typedef struct {
     int32_t N;           /* sequences (deer_diagrec_step: rows), >= 1                                      */
     int32_t D;           /* channels, >= 1                                                                 */
     int64_t T;           /* rows of a sequence, packed: of all of them; >= 0                               */
-    int32_t packed;      /* 0 or 1                                                                         */
+    int32_t packed;      /* 0 or 1, and DEER_REST_ZERO                                                     */
     uint32_t draw;       /* dropout: number of the draw under this seed                                    */
     int64_t stride_gate; /* rows of d_gate and d_dgate                                                     */
     int64_t stride_in;   /* rows of d_in and d_din                                                         */
@@ -289,9 +292,9 @@ deer_status deer_diagrec_grad(const deer_diagrec_config* cfg, const void* d_gate
                               const int64_t* d_bounds, const void* d_h, const void* d_dh, const void* d_dlast, void* d_dgate,
                               void* d_din, void* d_dh0, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
-/* One token for each of N rows (T, packed and drop are not looked at): the states lie in n_slots slots [n_slots, D] and are updated
+/* One token for each of N rows (T and drop are not looked at, of packed DEER_REST_ZERO only): the states lie in n_slots slots [n_slots, D] and are updated
  * in place; row n has slot d_slots[n] (device, int32 [N]; NULL: slot n).  A row whose slot is out of range, as in a
- * padded batch, or is the slot of a row in front of it is passed over: its row of d_h and the state stay as they are. */
+ * padded batch, or is the slot of a row in front of it is passed over: the state stays as it is, and so does its row of d_h, or is zeroed with DEER_REST_ZERO. */
 deer_status deer_diagrec_step(const deer_diagrec_config* cfg, const void* d_gate, const void* d_in, const int32_t* d_slots,
                               int32_t n_slots, void* d_state, void* d_h, void* hip_stream);
 
@@ -307,7 +310,7 @@ typedef struct {
     int32_t dtype;     /* DEER_F32 or DEER_BF16: q, k, v, o and their gradients                            */
     int32_t N;         /* sequences (deer_matrec_step: rows), >= 1                                         */
     int64_t T;         /* rows of a sequence, packed: of all of them; >= 0                                 */
-    int32_t packed;    /* 0 or 1                                                                           */
+    int32_t packed;    /* 0 or 1, and DEER_REST_ZERO                                                       */
     int32_t Hk, Hv;    /* heads of q and k, heads of v: a multiple; head h goes with h / (Hv / Hk)         */
     int32_t Dk, Dv;    /* 1 .. 128                                                                         */
     int32_t reserved;  /* must be 0                                                                        */
@@ -333,7 +336,7 @@ deer_status deer_matrec_grad(const deer_matrec_config* cfg, const void* d_q, con
                              const float* d_s0, const int64_t* d_bounds, const void* d_do, const float* d_dlast, void* d_dq, void* d_dk,
                              void* d_dv, float* d_dgate, float* d_ds0, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
-/* One token for each of N rows (T and packed are not looked at): states in n_slots slots [n_slots, Hv, Dk, Dv], float32, updated in place; slots as in
+/* One token for each of N rows (T is not looked at, of packed DEER_REST_ZERO only): states in n_slots slots [n_slots, Hv, Dk, Dv], float32, updated in place; slots as in
  * deer_diagrec_step(). */
 deer_status deer_matrec_step(const deer_matrec_config* cfg, const void* d_q, const void* d_k, const void* d_v, const float* d_gate,
                              const int32_t* d_slots, int32_t n_slots, float* d_state, void* d_o, void* hip_stream);

@@ -451,10 +451,11 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
     else second_pass(std::false_type{});
 }
 
-// Clears the published words and the ticket, and gives sequences without rows their final state (in the gradient: the
+// Clears the published words, the ticket and, on request, rows of no sequence, and gives sequences without rows their final state (in the gradient: the
 // gradient of their initial state).  A kernel and no memset: the call may be captured into a graph.
 template <typename S>
-__global__ void diagrec_prepare_kernel(const DiagrecParams p, bool grad) {
+__global__ __launch_bounds__(256) void diagrec_prepare_kernel(const DiagrecParams p, bool grad, const RestRows rest) {
+    clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
     const size_t at = (size_t)blockIdx.x * blockDim.x + threadIdx.x, all = (size_t)gridDim.x * blockDim.x;
     for (size_t i = at; i < p.words; i += all) p.agg[i] = kUnset;
     if (at == 0) *p.ticket = 0;
@@ -482,8 +483,20 @@ hipError_t launch_type(const DiagrecParams& p, hipStream_t stream) {
     using S = wide_t<T>;
     const long long cells = (long long)p.rows.N * p.D;
     const size_t work = p.words > (size_t)cells ? p.words : (size_t)cells;
-    const unsigned blocks = (unsigned)(work / 1024 < 1 ? 1 : work / 1024 > 2048 ? 2048 : work / 1024);
-    hipLaunchKernelGGL((diagrec_prepare_kernel<S>), dim3(blocks), dim3(256), 0, stream, p, REV);
+    RestRows rest{};
+    if (p.zero_rest) {
+        auto add = [&](void* first, long long stride) { rest.array[rest.count++] = RestArray{first, stride * (long long)sizeof(T), p.D * (long long)sizeof(T)}; };
+        if (REV) {
+            add(p.dg, p.stride_gate);
+            add(p.dx, p.stride_in);
+        } else {
+            add(p.h, p.stride_out);
+        }
+    }
+    const long long tiles = rest.count ? (p.rows.T + 15) / 16 * (p.rows.packed ? 1 : p.rows.N) : 0;
+    const long long want = (long long)(work / 1024) > tiles ? (long long)(work / 1024) : tiles;
+    const unsigned blocks = (unsigned)(want < 1 ? 1 : want > 2048 ? 2048 : want);
+    hipLaunchKernelGGL((diagrec_prepare_kernel<S>), dim3(blocks), dim3(256), 0, stream, p, REV, rest);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // Vectors of V channels where every row of every array begins at a multiple of them: 4 x 16,384 x 1,024 in bf16 98 + 141 us (forward + backward), a
@@ -525,7 +538,10 @@ __global__ __launch_bounds__(256) void diagstep_kernel(const DiagstepParams p) {
         h = *state;
     }
     twice = p.rows.slots ? __syncthreads_or(twice) != 0 : false;
-    if (!in || twice) return;
+    if (!in || twice) {
+        if (p.rows.zero_rest && ch < p.D) reinterpret_cast<T*>(p.h)[(long long)n * p.stride_out + ch] = (T)0;
+        return;
+    }
     S a, w;
     gate_factors<T, KIND>(g, a, w);
     h = a * h + w * x;

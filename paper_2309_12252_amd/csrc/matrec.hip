@@ -71,8 +71,9 @@ __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p)
 
 // The gates of every chunk, once for all that use them: their running sum is a chain of dependent steps, and 64 gates of a head lie in as many
 // cache lines.  A workgroup has a chunk, a wavefront one head after another.  5 us for 16,384 rows of 16 heads; summed again by every run: outputs
-// 91 us against 85, gradient 452 against 431.
-__global__ __launch_bounds__(256) void matrec_rows_kernel(const MatrecParams p) {
+// 91 us against 85, gradient 452 against 431.  On request also zeroes rows of no sequence.
+__global__ __launch_bounds__(256) void matrec_rows_kernel(const MatrecParams p, const RestRows rest) {
+    clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
     const int seg_no = blockIdx.x / p.plan.per, c = blockIdx.x % p.plan.per, lane = threadIdx.x & 63;
     MatSegment seg;
     if (!segment_of(p, seg_no, seg)) return;
@@ -258,7 +259,11 @@ __global__ __launch_bounds__(256) void matstep_kernel(const MatstepParams p) {
         for (int m = threadIdx.x; m < n; m += 256) twice = twice || p.rows.slots[m] == slot;
         twice = __syncthreads_or(twice) != 0;
     }
-    if (slot < 0 || slot >= p.rows.n_slots || twice) return;
+    if (slot < 0 || slot >= p.rows.n_slots || twice) {
+        if (p.rows.zero_rest)
+            for (int col = threadIdx.x; col < p.Dv; col += 256) reinterpret_cast<T*>(p.o)[n * p.stride_o + (long long)head * p.Dv + col] = (T)0.0f;
+        return;
+    }
     const int cols = p.Dv / V, per = 256 / cols;               // lanes of a row of the state, rows at a time
     const int c = threadIdx.x % cols, d0 = threadIdx.x / cols;
     const bool on = d0 < per;
@@ -317,7 +322,7 @@ hipError_t out_shape(const MatrecParams& p, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream) {
+hipError_t launch_matrec_plan(const MatrecParams& p, const RestRows& rest, hipStream_t stream) {
     hipError_t e = hipSuccess;
     if (p.rows.bounds) {
         hipLaunchKernelGGL(matrec_plan_kernel, dim3(1), dim3(1024), 0, stream, p);
@@ -325,7 +330,7 @@ hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream) {
     }
     const unsigned chunks = (unsigned)((long long)p.plan.max_segs * p.plan.per);
     if (e != hipSuccess || chunks == 0) return e;
-    hipLaunchKernelGGL(matrec_rows_kernel, dim3(chunks), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(matrec_rows_kernel, dim3(chunks), dim3(256), 0, stream, p, rest);
     return hipGetLastError();
 }
 hipError_t launch_matrec_out(int dtype, const MatrecParams& p, hipStream_t stream) {

@@ -301,7 +301,7 @@ __device__ __forceinline__ int first_segment(const MatrecParams& p, int n) {
     return n * ((chunks + p.plan.per - 1) / p.plan.per);
 }
 
-hipError_t launch_matrec_plan(const MatrecParams& p, hipStream_t stream);   // segments, and the gates of their chunks
+hipError_t launch_matrec_plan(const MatrecParams& p, const RestRows& rest, hipStream_t stream);   // segments, the gates of their chunks, rows of no sequence
 hipError_t launch_matrec_out(int dtype, const MatrecParams& p, hipStream_t stream);
 hipError_t launch_matrec_join(int dtype, const MatrecParams& p, bool both, hipStream_t stream);   // states in front of the segments (both: behind them too)
 hipError_t launch_matrec_grad(int dtype, const MatrecParams& p, hipStream_t stream);

@@ -25,6 +25,8 @@ deer_status launched(const char* what, hipError_t e) {
     return fail(DEER_ERR_HIP, text);
 }
 
+template <typename C> bool is_packed(const C* c) { return (c->packed & 1) != 0; }
+template <typename C> bool zero_rest(const C* c) { return (c->packed & (int)DEER_REST_ZERO) != 0; }
 bool known_type(int dtype) { return dtype == DEER_F32 || dtype == DEER_F64 || dtype == DEER_BF16 || dtype == DEER_F16; }
 size_t type_bytes(int dtype) { return dtype == DEER_F64 ? 8 : dtype == DEER_F32 ? 4 : 2; }
 bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
@@ -58,7 +60,7 @@ const char* bad_config(const deer_diagrec_config* c, bool step) {
     if ((c->stride_gate && c->stride_gate < c->D) || (c->stride_in && c->stride_in < c->D) || (c->stride_out && c->stride_out < c->D))
         return "a stride is smaller than a row";
     if (step) return nullptr;
-    if (c->T < 0 || (c->packed != 0 && c->packed != 1)) return "T must not be negative, packed 0 or 1";
+    if (c->T < 0 || (c->packed & ~(int)DEER_REST_ZERO & ~1)) return "T must not be negative, packed 0 or 1 (and DEER_REST_ZERO)";
     return bad_drop(c->drop);
 }
 struct DiagLayout {
@@ -67,7 +69,7 @@ struct DiagLayout {
 };
 DiagLayout diag_layout(const deer_diagrec_config* c, bool grad) {
     DiagLayout l;
-    l.words = diagrec_words(c->dtype, c->gate, c->packed ? 1 : c->N, c->T, c->D, grad, &l.chunks, &l.groups, &l.agg_words);
+    l.words = diagrec_words(c->dtype, c->gate, is_packed(c) ? 1 : c->N, c->T, c->D, grad, &l.chunks, &l.groups, &l.agg_words);
     l.total = kAlign + align_up(l.words * 8);
     return l;
 }
@@ -75,19 +77,20 @@ DiagLayout diag_layout(const deer_diagrec_config* c, bool grad) {
 bool too_large(const deer_diagrec_config* c, bool grad) {
     if (c->T > kMostRows || c->D > kMostStride || c->stride_gate > kMostStride || c->stride_in > kMostStride || c->stride_out > kMostStride) return true;
     if ((long double)c->N * c->D > 1e15L) return true;
-    const long double seqs = c->packed ? 1 : c->N, cols = (c->D + 63) / 64;   // (a channel a lane: most workgroups)
+    const long double seqs = is_packed(c) ? 1 : c->N, cols = (c->D + 63) / 64;   // (a channel a lane: most workgroups)
     return cols * seqs * diag_layout(c, grad).chunks * kDiagLanes > kMostLanes;
 }
 
 DiagrecParams diag_params(const deer_diagrec_config* c, const DiagLayout& l, const int64_t* bounds, void* ws) {
     DiagrecParams p{};
-    p.rows = SeqRows{reinterpret_cast<const long long*>(bounds), c->T, c->N, c->packed};
+    p.rows = SeqRows{reinterpret_cast<const long long*>(bounds), c->T, c->N, is_packed(c)};
     p.D = c->D;
     p.gate = c->gate;
     p.stride_gate = c->stride_gate ? c->stride_gate : c->D;
     p.stride_in = c->stride_in ? c->stride_in : c->D;
     p.stride_out = c->stride_out ? c->stride_out : c->D;
     p.drop = drop_params(c->drop, c->seed, c->draw);
+    p.zero_rest = zero_rest(c);
     p.chunks = l.chunks;
     p.groups = l.groups;
     p.ticket = reinterpret_cast<unsigned*>(ws);
@@ -118,7 +121,7 @@ const char* bad_config(const deer_matrec_config* c, bool step) {
     const int64_t keys = (int64_t)c->Hk * c->Dk, values = (int64_t)c->Hv * c->Dv;
     if ((c->stride_q && c->stride_q < keys) || (c->stride_k && c->stride_k < keys) || (c->stride_v && c->stride_v < values) || (c->stride_o && c->stride_o < values))
         return "a stride is smaller than a row";
-    if (!step && (c->T < 0 || (c->packed != 0 && c->packed != 1))) return "T must not be negative, packed 0 or 1";
+    if (!step && (c->T < 0 || (c->packed & ~(int)DEER_REST_ZERO & ~1))) return "T must not be negative, packed 0 or 1 (and DEER_REST_ZERO)";
     return nullptr;
 }
 
@@ -137,19 +140,19 @@ struct MatLayout {
 MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
     MatLayout l{};
     const long long longest = (c->T + kChunk - 1) / kChunk;
-    l.chunks = c->packed ? longest + c->N : longest * c->N;
+    l.chunks = is_packed(c) ? longest + c->N : longest * c->N;
     long long per = longest < 1 ? 1 : longest;
-    if (longest > 4 && (c->packed || (long long)c->N * c->Hv < 256)) {
+    if (longest > 4 && (is_packed(c) || (long long)c->N * c->Hv < 256)) {
         // 512 workgroups run at a time; every sequence's last segment is a short one, half of the others' length on average
-        long long segs = 512 / c->Hv - (c->packed ? c->N / 2 : 0);
+        long long segs = 512 / c->Hv - (is_packed(c) ? c->N / 2 : 0);
         if (segs < 1) segs = 1;
-        per = ((c->packed ? longest : l.chunks) + segs - 1) / segs;
+        per = ((is_packed(c) ? longest : l.chunks) + segs - 1) / segs;
         if (per > longest) per = longest;
     }
     if (grad && per > 32) per = 32;   // what goes through the chunks of a segment (matrec_grad.hip) takes the rounding errors of all of them
     l.per = (int)per;
     l.split = per < longest;
-    l.max_segs = c->packed ? l.chunks / per + c->N : (longest + per - 1) / per * c->N;
+    l.max_segs = is_packed(c) ? l.chunks / per + c->N : (longest + per - 1) / per * c->N;
     const size_t states = (size_t)c->Hv * (c->Dk <= 64 ? 64 : 128) * (c->Dv <= 64 ? 64 : 128) * 4;
     size_t at = kAlign;
     auto take = [&](size_t bytes) {
@@ -166,7 +169,7 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
         l.off_decay = take((size_t)l.max_segs * c->Hv * 8);
     }
     if (grad) {
-        const size_t rows = (size_t)c->T * (c->packed ? 1 : c->N), by_head = (size_t)c->Hv * 4;
+        const size_t rows = (size_t)c->T * (is_packed(c) ? 1 : c->N), by_head = (size_t)c->Hv * 4;
         if (c->Hv != c->Hk) {
             l.off_part_q = take(rows * by_head * c->Dk);
             l.off_part_k = take(rows * by_head * c->Dk);
@@ -183,17 +186,35 @@ const char* unsupported(const deer_matrec_config* c, bool step) {
     if (c->dtype != DEER_F32 && c->dtype != DEER_BF16) return "matrix states: fp32 and bf16 only";
     if (c->Dk > 128 || c->Dv > 128) return "matrix states: Dk and Dv up to 128";
     if (step) return (long double)c->N * c->Hv * 256 > kMostLanes ? "more rows than a launch holds" : nullptr;
-    if (c->T > kMostRows || (long double)c->N * c->Hv * 64 > 2147483647.0L || ((long double)(c->T + 63) / 64 + 4) * (c->packed ? 1 : c->N) * c->Hv > 2147483647.0L)
+    if (c->T > kMostRows || (long double)c->N * c->Hv * 64 > 2147483647.0L || ((long double)(c->T + 63) / 64 + 4) * (is_packed(c) ? 1 : c->N) * c->Hv > 2147483647.0L)
         return "more rows than a launch holds";
     // the gradient's: three workgroups of up to 512 lanes a segment and head; four of 256 a chunk
     const MatLayout l = mat_layout(c, true);
     if (((long double)l.max_segs * c->Hv + 8) * 3 * 512 > kMostLanes || (long double)l.max_segs * l.per * 4 * 256 > kMostLanes) return "more rows than a launch holds";
     return nullptr;
 }
+// the row outputs of a direction, to be zeroed where no sequence is
+RestRows mat_rest(const deer_matrec_config* c, const MatrecParams& p, bool grad) {
+    RestRows rest{};
+    if (!zero_rest(c)) return rest;
+    const long long e = (long long)type_bytes(c->dtype), keys = (long long)c->Hk * c->Dk * e, values = (long long)c->Hv * c->Dv * e;
+    auto add = [&](void* first, long long pitch, long long width) {
+        if (first) rest.array[rest.count++] = RestArray{first, pitch, width};
+    };
+    if (grad) {
+        add(p.dq, p.stride_q * e, keys);
+        add(p.dk, p.stride_k * e, keys);
+        add(p.dv, p.stride_v * e, values);
+        add(p.dgate, 4ll * c->Hv, 4ll * c->Hv);
+    } else {
+        add(p.o, p.stride_o * e, values);
+    }
+    return rest;
+}
 MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool grad, const int64_t* bounds, void* workspace) {
     char* ws = reinterpret_cast<char*>(workspace);
     MatrecParams p{};
-    p.rows = SeqRows{reinterpret_cast<const long long*>(bounds), c->T, c->N, c->packed};
+    p.rows = SeqRows{reinterpret_cast<const long long*>(bounds), c->T, c->N, is_packed(c)};
     p.plan.count = reinterpret_cast<int*>(ws);
     p.plan.segs = reinterpret_cast<MatSegment*>(ws + l.off_segs);
     p.plan.seq_seg = reinterpret_cast<int*>(ws + l.off_seq);
@@ -244,7 +265,7 @@ deer_status deer_diagrec_solve(const deer_diagrec_config* c, const void* d_gate,
                                void* d_h, void* d_last, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
     if (too_large(c, false)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
-    if ((c->T > 0 && (!d_gate || !d_in || !d_h)) || (c->packed && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    if ((c->T > 0 && (!d_gate || !d_in || !d_h)) || (is_packed(c) && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
     if (misaligned(d_gate, e) || misaligned(d_in, e) || misaligned(d_h, e) || misaligned(d_h0, w) || misaligned(d_last, w) || misaligned(d_bounds, 8))
         return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
@@ -264,7 +285,7 @@ deer_status deer_diagrec_grad(const deer_diagrec_config* c, const void* d_gate, 
                               void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
     if (too_large(c, true)) return fail(DEER_ERR_UNSUPPORTED, "more rows or tiles than a launch holds, or rows more than 2^22 elements apart");
-    if ((c->T > 0 && (!d_gate || !d_in || !d_h || !d_dh || !d_dgate || !d_din)) || (c->packed && !d_bounds))
+    if ((c->T > 0 && (!d_gate || !d_in || !d_h || !d_dh || !d_dgate || !d_din)) || (is_packed(c) && !d_bounds))
         return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t e = type_bytes(c->dtype), w = c->dtype == DEER_F64 ? 8 : 4;
     if (misaligned(d_gate, e) || misaligned(d_in, e) || misaligned(d_h, e) || misaligned(d_dh, e) || misaligned(d_dgate, e) || misaligned(d_din, e) ||
@@ -295,7 +316,7 @@ deer_status deer_diagrec_step(const deer_diagrec_config* c, const void* d_gate, 
         return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
     if (c->D > (1 << 30) || (long double)c->N * ((c->D + 255) / 256) * 256 > kMostLanes) return fail(DEER_ERR_UNSUPPORTED, "more rows or channels than a launch holds");
     DiagstepParams p{};
-    p.rows = StepRows{d_slots, c->N, n_slots};
+    p.rows = StepRows{d_slots, c->N, n_slots, zero_rest(c)};
     p.D = c->D;
     p.gate = c->gate;
     p.stride_gate = c->stride_gate ? c->stride_gate : c->D;
@@ -342,7 +363,7 @@ deer_status deer_matrec_solve(const deer_matrec_config* c, const void* d_q, cons
                               const int64_t* d_bounds, void* d_o, float* d_last, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
     if (const char* why = unsupported(c, false)) return fail(DEER_ERR_UNSUPPORTED, why);
-    if ((c->T > 0 && (!d_q || !d_k || !d_v || !d_gate || !d_o)) || (c->packed && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
+    if ((c->T > 0 && (!d_q || !d_k || !d_v || !d_gate || !d_o)) || (is_packed(c) && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t e = type_bytes(c->dtype);
     if (misaligned(d_q, e) || misaligned(d_k, e) || misaligned(d_v, e) || misaligned(d_o, e) || misaligned(d_gate, 4) || misaligned(d_s0, 4) ||
         misaligned(d_last, 4) || misaligned(d_bounds, 8))
@@ -358,7 +379,7 @@ deer_status deer_matrec_solve(const deer_matrec_config* c, const void* d_q, cons
     p.o = d_o;
     p.last = d_last;
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
-    hipError_t err = launch_matrec_plan(p, stream);
+    hipError_t err = launch_matrec_plan(p, mat_rest(c, p, false), stream);
     if (err == hipSuccess) err = launch_matrec_out(c->dtype, p, stream);
     return launched("deer_matrec_solve", err);
 }
@@ -368,7 +389,7 @@ deer_status deer_matrec_grad(const deer_matrec_config* c, const void* d_q, const
                              float* d_ds0, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
     if (const char* why = unsupported(c, false)) return fail(DEER_ERR_UNSUPPORTED, why);
-    if ((c->T > 0 && (!d_q || !d_k || !d_v || !d_gate || !d_do || !d_dq || !d_dk || !d_dv)) || (c->packed && !d_bounds))
+    if ((c->T > 0 && (!d_q || !d_k || !d_v || !d_gate || !d_do || !d_dq || !d_dk || !d_dv)) || (is_packed(c) && !d_bounds))
         return fail(DEER_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t e = type_bytes(c->dtype);
     if (misaligned(d_q, e) || misaligned(d_k, e) || misaligned(d_v, e) || misaligned(d_do, e) || misaligned(d_dq, e) || misaligned(d_dk, e) ||
@@ -391,7 +412,7 @@ deer_status deer_matrec_grad(const deer_matrec_config* c, const void* d_q, const
     p.dgate = d_dgate;
     p.ds0 = d_ds0;
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
-    hipError_t err = launch_matrec_plan(p, stream);
+    hipError_t err = launch_matrec_plan(p, mat_rest(c, p, true), stream);
     if (err == hipSuccess) err = launch_matrec_join(c->dtype, p, true, stream);
     if (err == hipSuccess) err = launch_matrec_grad(c->dtype, p, stream);
     return launched("deer_matrec_grad", err);
@@ -407,7 +428,7 @@ deer_status deer_matrec_step(const deer_matrec_config* c, const void* d_q, const
     if (misaligned(d_q, e) || misaligned(d_k, e) || misaligned(d_v, e) || misaligned(d_o, e) || misaligned(d_gate, 4) || misaligned(d_state, 4) || misaligned(d_slots, 4))
         return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
     MatstepParams p{};
-    p.rows = StepRows{d_slots, c->N, n_slots};
+    p.rows = StepRows{d_slots, c->N, n_slots, zero_rest(c)};
     p.Hk = c->Hk;
     p.Hv = c->Hv;
     p.Dk = c->Dk;

@@ -39,6 +39,42 @@ __device__ __forceinline__ long long seq_length(const SeqRows& s, int n) {
     return s.bounds ? clamp_row(s.bounds[n], s.T) : s.T;
 }
 
+// Arrays whose rows that belong to no sequence are zeroed on request, by the call's first kernel over rows (16 rows of a sequence at a time, 256 lanes a
+// workgroup).  Packed sequences lie one behind the other, so that these rows are those in front of the first and behind the last.
+struct RestArray {
+    void* first;
+    long long pitch, width;   // bytes from a row to the next, and of a row: multiples of two
+};
+struct RestRows {
+    int count;
+    RestArray array[4];
+};
+template <typename U>
+__device__ __forceinline__ void clear_row(char* row, long long width) {
+    for (long long i = threadIdx.x; i < width / (long long)sizeof(U); i += 256) reinterpret_cast<U*>(row)[i] = U{};
+}
+__device__ __forceinline__ void clear_rest(const SeqRows& s, const RestRows& rest, long long block, long long blocks) {
+    using U4 = unsigned __attribute__((ext_vector_type(4)));
+    if (rest.count == 0 || !s.bounds) return;
+    const long long tiles = (s.T + 15) / 16, all = tiles * (s.packed ? 1 : s.N);
+    for (long long i = block; i < all; i += blocks) {
+        const long long n = i / tiles, from = i % tiles * 16, to = from + 16 < s.T ? from + 16 : s.T;
+        const long long lo = s.packed ? clamp_row(s.bounds[0], s.T) : 0, hi = s.packed ? clamp_row(s.bounds[s.N], s.T) : seq_length(s, (int)n);
+        if (from >= lo && to <= hi) continue;
+        for (long long r = from; r < to; ++r) {
+            if (r >= lo && r < hi) continue;
+            for (int a = 0; a < rest.count; ++a) {
+                const long long pitch = rest.array[a].pitch, width = rest.array[a].width;
+                char* row = reinterpret_cast<char*>(rest.array[a].first) + (n * s.T + r) * pitch;
+                const unsigned long long low = reinterpret_cast<unsigned long long>(row) | (unsigned long long)width;
+                if (low % 16 == 0) clear_row<U4>(row, width);
+                else if (low % 4 == 0) clear_row<unsigned>(row, width);
+                else clear_row<unsigned short>(row, width);
+            }
+        }
+    }
+}
+
 // ---- element types: arithmetic in 32 bits for the 16-bit types and fp32, in 64 for fp64 ----
 using BF16 = __bf16;
 using F16 = _Float16;
@@ -129,6 +165,7 @@ struct DiagrecParams {
     const void *dh, *dlast;                         // gradient
     void *dg, *dx, *dh0;
     DropParams drop;
+    bool zero_rest;                                 // rows of no sequence
     // words that tiles publish for each other
     int chunks, groups;                             // tiles and groups of tiles along a sequence
     unsigned long long *agg, *inc;
@@ -138,6 +175,7 @@ struct DiagrecParams {
 struct StepRows {
     const int* slots;      // [N] or nullptr (row n has slot n)
     int N, n_slots;
+    bool zero_rest;        // rows that are passed over
 };
 struct DiagstepParams {
     StepRows rows;

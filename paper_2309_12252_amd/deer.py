@@ -18,6 +18,7 @@ DEER_OK, DEER_ERR_INVALID_ARG, DEER_ERR_UNSUPPORTED, DEER_ERR_WORKSPACE, DEER_ER
 DEER_CELL_GRU, DEER_CELL_MLP_ODE, DEER_CELL_LSTM, DEER_CELL_LEM = 0, 1, 2, 3
 DEER_F32, DEER_F64, DEER_BF16, DEER_F16 = 0, 1, 2, 3
 DEER_GATE_FACTOR, DEER_GATE_LOG, DEER_GATE_SIGMOID = 0, 1, 2
+DEER_ROWS_PADDED, DEER_ROWS_PACKED, DEER_REST_ZERO = 0, 1, 256
 
 EXPORTS = ["deer_theta_count", "deer_workspace_bytes", "deer_create", "deer_eval", "deer_grad",
            "deer_linrec_solve", "deer_linrec_solve_static", "deer_set_profiling", "deer_get_profile", "deer_last_error", "deer_destroy",
@@ -269,7 +270,8 @@ def linrec_solve_static(A, b, y0=None, reverse=False, out=None, status=None, str
 # ---------------------------------------------------------------------------------------------------------------------
 # Sequence operators.  Every call is asynchronous on `stream` (default: torch's current stream of the tensors' device); outputs
 # and workspaces come from torch's allocator on that stream, a workspace for every call, so calls on several
-# streams, in several threads and captured into several graphs do not meet in one.
+# streams, in several threads and captured into several graphs do not meet in one.  Rows that belong to no sequence (behind `lengths`,
+# outside `offsets`) or that a step passes over are zero in arrays that the call makes and left as they are in arrays that are handed in.
 # ---------------------------------------------------------------------------------------------------------------------
 _DTYPES = {torch.float32: DEER_F32, torch.float64: DEER_F64, torch.bfloat16: DEER_BF16, torch.float16: DEER_F16}
 
@@ -393,6 +395,19 @@ def _rows_like(t, stride):
     return torch.empty_strided(t.shape, strides, dtype=t.dtype, device=t.device)
 
 
+def _zero_rest(bounds, *made):
+    """Flag for the kernels to zero rows of no sequence, where every output of rows is the call's own; where some are the caller's, the call's own are
+    zeroed here.  made: arrays that the call has made, None for the caller's"""
+    if not bounds:
+        return 0
+    own = [t for t in made if t is not None]
+    if len(own) == len(made):
+        return DEER_REST_ZERO
+    for t in own:
+        t.zero_()
+    return 0
+
+
 @functools.lru_cache(maxsize=512)
 def _diag_workspace(grad, dtype, gate, N, D, T, packed):
     lib, size = load_library(), ctypes.c_size_t(0)
@@ -420,7 +435,7 @@ def _diag_inputs(gate, x, kind, offsets, lengths):
 def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, lengths=None, drop=0.0, seed=0, draw=0, out=None):
     """deer_diagrec_solve: h_t = a_t h_{t-1} + u_t for every channel (a, u from gate and x: see deer_gate).  gate, x [N, T, D] with
     optional int64 `lengths` [N], or packed [rows, D] with int64 `offsets` [N + 1]; rows may be slices of wider ones.  h0 [N, D] in
-    float32 (float64 with float64).  Rows of no sequence are left as they are in `out`.  Returns (h, state behind the last rows)."""
+    float32 (float64 with float64).  Rows of no sequence are zero in the result, left as they are in `out`.  Returns (h, state behind the last rows)."""
     lib = load_library()
     dtype, kind, N, D, T, packed, bounds, lead = _diag_inputs(gate, x, kind, offsets, lengths)
     dev, w = x.device, torch.float64 if dtype == DEER_F64 else torch.float32
@@ -429,7 +444,8 @@ def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, leng
     else:
         h = out
         _check_like(h, "out", x.shape, x.dtype, dev)
-    cfg = DiagrecConfig(dtype, kind, N, D, T, packed, draw & 0xFFFFFFFF, _row_stride(gate, "gate", lead), _row_stride(x, "x", lead),
+    rest = _zero_rest(bounds, h if out is None else None)
+    cfg = DiagrecConfig(dtype, kind, N, D, T, packed | rest, draw & 0xFFFFFFFF, _row_stride(gate, "gate", lead), _row_stride(x, "x", lead),
                         _row_stride(h, "out", lead), drop, seed & 0xFFFFFFFFFFFFFFFF)
     last = torch.empty((N, D), dtype=w, device=dev)
     h0p = _dense(h0, "h0", last.shape, w, dev)
@@ -446,7 +462,7 @@ def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, leng
 def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, offsets=None, lengths=None, drop=0.0, seed=0, draw=0,
                  dgate=None, dx=None):
     """deer_diagrec_grad at the trajectory h: (dL/dgate, dL/dx, dL/dh0) from dh = dL/dh and dlast = dL/d(final state).  dgate and dx, where
-    given, have the row strides of gate and x."""
+    given, have the row strides of gate and x, and their rows of no sequence are left as they are; otherwise these are zero."""
     lib = load_library()
     dtype, kind, N, D, T, packed, bounds, lead = _diag_inputs(gate, x, kind, offsets, lengths)
     dev, w = x.device, torch.float64 if dtype == DEER_F64 else torch.float32
@@ -456,6 +472,7 @@ def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, 
     if _row_stride(dh, "dh", lead) != stride_h:
         h, dh, stride_h = h.contiguous(), dh.contiguous(), D
     stride_g, stride_x = _row_stride(gate, "gate", lead), _row_stride(x, "x", lead)
+    given = (dgate is not None, dx is not None)
     if dgate is None:
         dgate = torch.empty_like(gate, memory_format=torch.contiguous_format) if stride_g == D else _rows_like(gate, stride_g)
     else:
@@ -468,7 +485,8 @@ def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, 
         _check_like(dx, "dx", x.shape, x.dtype, dev)
         if _row_stride(dx, "dx", lead) != stride_x:
             _refuse("dx: rows must lie like those of x")
-    cfg = DiagrecConfig(dtype, kind, N, D, T, packed, draw & 0xFFFFFFFF, stride_g, stride_x, stride_h, drop, seed & 0xFFFFFFFFFFFFFFFF)
+    rest = _zero_rest(bounds, *(None if g else t for g, t in zip(given, (dgate, dx))))
+    cfg = DiagrecConfig(dtype, kind, N, D, T, packed | rest, draw & 0xFFFFFFFF, stride_g, stride_x, stride_h, drop, seed & 0xFFFFFFFFFFFFFFFF)
     dh0 = torch.empty((N, D), dtype=w, device=dev)
     h0p, dlp = _dense(h0, "h0", dh0.shape, w, dev), _dense(dlast, "dlast", dh0.shape, w, dev)
     size = _diag_workspace(1, dtype, kind, N, D, T, packed)
@@ -483,7 +501,8 @@ def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, 
 @_on_stream
 def diagrec_step(gate, x, state, *, kind=DEER_GATE_FACTOR, slots=None, out=None):
     """deer_diagrec_step: one token for each of N rows, gate and x [N, D]; `state` [slots, D] (float32; float64 with float64) is updated
-    in place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over.  Returns h [N, D]."""
+    in place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over: zero in
+    the result, left as they are in `out`.  Returns h [N, D]."""
     lib = load_library()
     dtype = _DTYPES.get(x.dtype) if isinstance(x, torch.Tensor) else None
     if dtype is None or x.dim() != 2:
@@ -500,7 +519,7 @@ def diagrec_step(gate, x, state, *, kind=DEER_GATE_FACTOR, slots=None, out=None)
     sp = _dense(state, "state", state.shape, torch.float64 if dtype == DEER_F64 else torch.float32, dev)
     tp = _dense(slots, "slots", shape[:1], torch.int32, dev)
     _int32(shape[0], shape[1], state.shape[0])
-    cfg = DiagrecConfig(dtype, int(kind), shape[0], shape[1], 1, 0, 0, _row_stride(gate, "gate", 1), _row_stride(x, "x", 1),
+    cfg = DiagrecConfig(dtype, int(kind), shape[0], shape[1], 1, DEER_REST_ZERO if out is None else 0, 0, _row_stride(gate, "gate", 1), _row_stride(x, "x", 1),
                         _row_stride(h, "out", 1), 0.0, 0)
     st = lib.deer_diagrec_step(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), tp, state.shape[0], sp, h.data_ptr(), _stream_of(dev))
     if st != DEER_OK:
@@ -554,7 +573,7 @@ def _mat_config(q, k, v, gate, o, offsets, lengths, scale, lead=None):
 def matrec_solve(q, k, v, gate, s0=None, *, offsets=None, lengths=None, scale=None, out=None):
     """deer_matrec_solve: S_t = exp(gate_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t for every head of v.  q, k [N, T, Hk, Dk], v [N, T, Hv, Dv] in
     float32 or bfloat16, gate [N, T, Hv] float32, with optional int64 `lengths` [N]; or packed [rows, ...] with int64 `offsets` [N + 1].  s0 [N, Hv, Dk, Dv]
-    float32.  scale: Dk^-1/2 by default.  Returns (o, states behind the last rows)."""
+    float32.  scale: Dk^-1/2 by default.  Rows of no sequence are zero in the result, left as they are in `out`.  Returns (o, states behind the last rows)."""
     lib = load_library()
     o = out if out is not None else torch.empty_like(v, memory_format=torch.contiguous_format) if isinstance(v, torch.Tensor) else None
     cfg, bounds, gp, _ = _mat_config(q, k, v, gate, o, offsets, lengths, scale)
@@ -563,6 +582,7 @@ def matrec_solve(q, k, v, gate, s0=None, *, offsets=None, lengths=None, scale=No
     size = _mat_workspace(0, cfg.dtype, cfg.N, cfg.T, cfg.packed, cfg.Hk, cfg.Hv, cfg.Dk, cfg.Dv)
     ws = q.new_empty(size, dtype=torch.uint8)
     last = torch.empty(shape, dtype=torch.float32, device=dev)
+    cfg.packed |= _zero_rest(bounds, o if out is None else None)
     st = lib.deer_matrec_solve(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, s0p, bounds, o.data_ptr(), last.data_ptr(),
                                ws.data_ptr(), size, _stream_of(dev))
     if st != DEER_OK:
@@ -571,14 +591,15 @@ def matrec_solve(q, k, v, gate, s0=None, *, offsets=None, lengths=None, scale=No
 
 
 @_on_stream
-def matrec_grad(q, k, v, gate, do, s0=None, dlast=None, *, offsets=None, lengths=None, scale=None, dq=None, dk=None, dv=None):
+def matrec_grad(q, k, v, gate, do, s0=None, dlast=None, *, offsets=None, lengths=None, scale=None, dq=None, dk=None, dv=None, dgate=None):
     """deer_matrec_grad: (dq, dk, dv, dgate, ds0) from do = dL/do and dlast = dL/d(final states).  dq, dk and dv, where given, have the row
-    strides of q, k and v."""
+    strides of q, k and v, dgate is dense; their rows of no sequence are left as they are, and are zero in arrays that are not given."""
     lib = load_library()
     cfg, bounds, gp, lead = _mat_config(q, k, v, gate, do, offsets, lengths, scale)
     dev = q.device
-    outs = []
-    for t, d, name, stride in ((q, dq, "dq", cfg.stride_q), (k, dk, "dk", cfg.stride_k), (v, dv, "dv", cfg.stride_v)):
+    outs, made = [], []
+    for t, given, name, stride in ((q, dq, "dq", cfg.stride_q), (k, dk, "dk", cfg.stride_k), (v, dv, "dv", cfg.stride_v)):
+        d = given
         if d is None:
             d = torch.empty(t.shape, dtype=t.dtype, device=dev) if t.is_contiguous() else _rows_like(t.flatten(-2), stride).unflatten(-1, t.shape[-2:])
         else:
@@ -586,11 +607,18 @@ def matrec_grad(q, k, v, gate, do, s0=None, dlast=None, *, offsets=None, lengths
             if _row_stride(d, name, lead) != stride:
                 _refuse(name + ": rows must lie like those of what it is the gradient of")
         outs.append(d)
+        made.append(d if given is None else None)
     shape = (cfg.N, cfg.Hv, cfg.Dk, cfg.Dv)
     s0p, dlp = _dense(s0, "s0", shape, torch.float32, dev), _dense(dlast, "dlast", shape, torch.float32, dev)
     size = _mat_workspace(1, cfg.dtype, cfg.N, cfg.T, cfg.packed, cfg.Hk, cfg.Hv, cfg.Dk, cfg.Dv)
     ws = q.new_empty(size, dtype=torch.uint8)
-    dgate = torch.empty(gate.shape, dtype=torch.float32, device=dev)
+    if dgate is None:
+        dgate = torch.empty(gate.shape, dtype=torch.float32, device=dev)
+        made.append(dgate)
+    else:
+        _dense(dgate, "dgate", gate.shape, torch.float32, dev)
+        made.append(None)
+    cfg.packed |= _zero_rest(bounds, *made)
     ds0 = torch.empty(shape, dtype=torch.float32, device=dev)
     st = lib.deer_matrec_grad(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, s0p, bounds, do.data_ptr(), dlp, outs[0].data_ptr(),
                               outs[1].data_ptr(), outs[2].data_ptr(), dgate.data_ptr(), ds0.data_ptr(), ws.data_ptr(), size, _stream_of(dev))
@@ -602,7 +630,8 @@ def matrec_grad(q, k, v, gate, do, s0=None, dlast=None, *, offsets=None, lengths
 @_on_stream
 def matrec_step(q, k, v, gate, state, *, slots=None, scale=None, out=None):
     """deer_matrec_step: one token for each of N rows, q, k [N, Hk, Dk], v [N, Hv, Dv], gate [N, Hv]; `state` [slots, Hv, Dk, Dv] float32 is updated
-    in place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over.  Returns o."""
+    in place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over: zero in
+    the result, left as they are in `out`.  Returns o."""
     lib = load_library()
     o = out if out is not None else torch.empty_like(v, memory_format=torch.contiguous_format) if isinstance(v, torch.Tensor) else None
     cfg, _, gp, _ = _mat_config(q, k, v, gate, o, None, None, scale, lead=1)
@@ -612,6 +641,7 @@ def matrec_step(q, k, v, gate, state, *, slots=None, scale=None, out=None):
     sp = _dense(state, "state", (state.shape[0], cfg.Hv, cfg.Dk, cfg.Dv), torch.float32, dev)
     tp = _dense(slots, "slots", q.shape[:1], torch.int32, dev)
     _int32(state.shape[0])
+    cfg.packed = DEER_REST_ZERO if out is None else 0
     st = lib.deer_matrec_step(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, tp, state.shape[0], sp, o.data_ptr(), _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)

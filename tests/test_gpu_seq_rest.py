@@ -1,0 +1,160 @@
+"""Rows that belong to no sequence, and rows that a step passes over: zero in arrays that the binding makes, whatever the allocator had there;
+left as they are in arrays that are handed in."""
+import pytest
+import torch
+
+from paper_2309_12252_amd import deer
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "f64": torch.float64, "bf16": torch.bfloat16, "f16": torch.float16}
+LENS = [40, 0, 1, 17, 33]                      # of five sequences of 40 rows
+OFFS = [5, 45, 45, 46, 63, 96]                 # five rows in front of the first, 27 behind the last of 123
+
+
+@pytest.fixture
+def poisoned(monkeypatch):
+    """what is allocated without a value holds NaN"""
+    def fill(make):
+        def made(*args, **kw):
+            t = make(*args, **kw)
+            return t.fill_(float("nan")) if t.is_floating_point() else t
+        return made
+    for name in ("empty", "empty_like", "empty_strided"):
+        monkeypatch.setattr(torch, name, fill(getattr(torch, name)))
+
+
+def arrays(seed, dtype, lead, *shapes):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    return [torch.randn(lead + s, generator=gen, device=DEV).to(TYPES[dtype]) for s in shapes]
+
+
+def layout(packed):
+    """leading dimensions, the keyword, and whether a row belongs to a sequence"""
+    if packed:
+        rows = torch.arange(123, device=DEV)
+        return (123,), {"offsets": torch.tensor(OFFS, device=DEV)}, (rows >= OFFS[0]) & (rows < OFFS[-1])
+    return (5, 40), {"lengths": torch.tensor(LENS, device=DEV)}, torch.arange(40, device=DEV)[None] < torch.tensor(LENS, device=DEV)[:, None]
+
+
+def check(alive, got, marked, mark):
+    """got: rows of no sequence zero; marked: `mark` there; the same bits in rows of a sequence"""
+    for g, m in zip(got, marked):
+        assert bool((g[~alive] == 0).all()) and bool((m[~alive] == mark).all())
+        assert torch.equal(g[alive], m[alive])
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 64), ("f32", 3), ("bf16", 128), ("bf16", 33), ("f16", 6), ("f64", 5)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_diagonal(poisoned, packed, dtype, D):
+    lead, more, alive = layout(packed)
+    gate, x, dh = arrays(D, dtype, lead, (D,), (D,), (D,))
+    more["kind"] = deer.DEER_GATE_SIGMOID
+    mark = lambda: torch.full_like(x, 5.0)   # noqa: E731
+    h, last = deer.diagrec_solve(gate, x, **more)
+    h2, last2 = deer.diagrec_solve(gate, x, out=mark(), **more)
+    assert torch.equal(last, last2)
+    check(alive, [h], [h2], 5.0)
+    got, marked = deer.diagrec_grad(gate, x, h, dh, **more), deer.diagrec_grad(gate, x, h, dh, dgate=mark(), dx=mark(), **more)
+    check(alive, got[:2], marked[:2], 5.0)
+    # one of them handed in
+    dgate, dx, _ = deer.diagrec_grad(gate, x, h, dh, dx=mark(), **more)
+    check(alive, [dgate], marked[:1], 5.0)
+    assert torch.equal(dx, marked[1])
+
+
+@pytest.mark.parametrize("dtype,Hk,Hv,Dk,Dv", [("bf16", 1, 2, 32, 48), ("bf16", 1, 1, 5, 7), ("f32", 2, 2, 17, 9)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_matrix(poisoned, packed, dtype, Hk, Hv, Dk, Dv):
+    lead, more, alive = layout(packed)
+    q, k, v, do = arrays(Dk, dtype, lead, (Hk, Dk), (Hk, Dk), (Hv, Dv), (Hv, Dv))
+    gate = -arrays(Dv, "f32", lead, (Hv,))[0].abs()
+    mark = lambda t: torch.full_like(t, 5.0)   # noqa: E731
+    o, last = deer.matrec_solve(q, k, v, gate, **more)
+    o2, last2 = deer.matrec_solve(q, k, v, gate, out=mark(v), **more)
+    assert torch.equal(last, last2)
+    check(alive, [o], [o2], 5.0)
+    got = deer.matrec_grad(q, k, v, gate, do, **more)
+    marked = deer.matrec_grad(q, k, v, gate, do, dq=mark(q), dk=mark(k), dv=mark(v), dgate=mark(gate), **more)
+    check(alive, got[:4], marked[:4], 5.0)
+    assert torch.equal(got[4], marked[4])
+    some = deer.matrec_grad(q, k, v, gate, do, dk=mark(k), dgate=mark(gate), **more)
+    check(alive, [some[0], some[2]], [marked[0], marked[2]], 5.0)
+    assert torch.equal(some[1], marked[1]) and torch.equal(some[3], marked[3])
+
+
+def test_slices(poisoned):
+    """gradients that the binding makes like slices of a wider array; what lies between their rows is nobody's"""
+    lead, more, alive = layout(False)
+    both, dh = arrays(3, "bf16", lead, (64,), (32,))
+    gate, x = both[..., :32], both[..., 32:]
+    h, _ = deer.diagrec_solve(gate, x, **more)
+    for t in deer.diagrec_grad(gate, x, h, dh, **more)[:2]:
+        assert t.stride(1) == 64 and bool((t[~alive] == 0).all()) and bool(torch.isfinite(t).all())
+    qkv, do = arrays(4, "bf16", lead, (3, 2, 16), (2, 16))
+    g = -arrays(5, "f32", lead, (2,))[0].abs()
+    for t in deer.matrec_grad(*(qkv[:, :, i] for i in range(3)), g, do, **more)[:4]:
+        assert bool((t[~alive] == 0).all()) and bool(torch.isfinite(t).all())
+    # the caller's slices: no neighbour is touched
+    wide = torch.full(lead + (96,), 5.0, dtype=torch.bfloat16, device=DEV)
+    deer.diagrec_solve(gate, x, out=wide[..., 32:64], **more)
+    assert bool((wide[..., :32] == 5).all()) and bool((wide[..., 64:] == 5).all()) and bool((wide[~alive] == 5).all())
+
+
+def test_all_rows_and_none(poisoned):
+    x = torch.randn(2, 70, 16, device=DEV)
+    none, every = torch.zeros(2, dtype=torch.int64, device=DEV), torch.full((2,), 70, device=DEV)
+    h0 = torch.randn(2, 16, device=DEV)
+    h, last = deer.diagrec_solve(x, x, h0, lengths=none)
+    assert bool((h == 0).all()) and torch.equal(last, h0)
+    assert torch.equal(deer.diagrec_solve(x, x, h0, lengths=every)[0], deer.diagrec_solve(x, x, h0)[0])
+    g = -torch.rand(140, 2, device=DEV)
+    q = torch.randn(140, 2, 8, device=DEV)
+    o, _ = deer.matrec_solve(q, q, q, g, offsets=torch.tensor([0, 0], device=DEV))
+    assert bool((o == 0).all())
+
+
+def test_steps(poisoned):
+    gate, x = arrays(1, "bf16", (6,), (300,), (300,))
+    slots = torch.tensor([2, -1, 4, 2, 0, 2000000000], dtype=torch.int32, device=DEV)
+    state, good = torch.randn(4, 300, device=DEV), torch.tensor([0, 4], device=DEV)
+    over = torch.tensor([1, 2, 3, 5], device=DEV)
+    other = state.clone()
+    h = deer.diagrec_step(gate, x, state, slots=slots)
+    want = deer.diagrec_step(gate, x, other, slots=slots, out=torch.full_like(x, 5.0))
+    assert bool((h[over] == 0).all()) and bool((want[over] == 5).all())
+    assert torch.equal(h[good], want[good]) and torch.equal(state, other)
+    q, v = arrays(2, "bf16", (6,), (1, 32), (2, 24))
+    g = -torch.rand(6, 2, device=DEV)
+    state = torch.randn(4, 2, 32, 24, device=DEV)
+    other = state.clone()
+    o = deer.matrec_step(q, q, v, g, state, slots=slots)
+    want = deer.matrec_step(q, q, v, g, other, slots=slots, out=torch.full_like(v, 5.0))
+    assert bool((o[over] == 0).all()) and bool((want[over] == 5).all())
+    assert torch.equal(o[good], want[good]) and torch.equal(state, other)
+
+
+def test_captured(poisoned):
+    lead, more, alive = layout(True)
+    gate, x, dh = arrays(9, "bf16", lead, (64,), (64,), (64,))
+
+    def step():
+        h, last = deer.diagrec_solve(gate, x, kind=1, **more)
+        return (h,) + deer.diagrec_grad(gate, x, h, dh, kind=1, **more)[:2]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for _ in range(3):
+        x.copy_(torch.randn(x.shape, device=DEV))
+        for t in outs:
+            t.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, step()):
+            assert torch.equal(a, b) and bool((a[~alive] == 0).all())

@@ -132,3 +132,17 @@ def test_binding_takes_keywords_and_counts_in_32_bits():
     deer._int32(0x7FFFFFFF)
     with pytest.raises(deer.DeerError):
         deer._int32(1, 0x80000000)
+
+
+def test_rows_of_no_sequence_are_zeroed_on_request():
+    lib, size, plain = deer.load_library(), ctypes.c_size_t(0), ctypes.c_size_t(0)
+    for make, ask in ((diag, lib.deer_diagrec_workspace_bytes), (mat, lib.deer_matrec_workspace_bytes)):
+        for grad in (0, 1):
+            for packed in (deer.DEER_ROWS_PADDED, deer.DEER_ROWS_PACKED):
+                assert ask(ctypes.byref(make(packed=packed)), grad, ctypes.byref(plain)) == deer.DEER_OK
+                assert ask(ctypes.byref(make(packed=packed | deer.DEER_REST_ZERO)), grad, ctypes.byref(size)) == deer.DEER_OK
+                assert size.value == plain.value
+            for bad in (2, deer.DEER_REST_ZERO | 2, 512, -1):
+                assert ask(ctypes.byref(make(packed=bad)), grad, ctypes.byref(size)) == deer.DEER_ERR_INVALID_ARG
+    packed = diag(packed=deer.DEER_ROWS_PACKED | deer.DEER_REST_ZERO)   # (still needs bounds)
+    assert lib.deer_diagrec_solve(ctypes.byref(packed), WORD, WORD, None, None, WORD, None, WORD, 1 << 40, None) == deer.DEER_ERR_INVALID_ARG
