@@ -64,7 +64,8 @@ __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p)
     }
     __syncthreads();
     if (tid == 0) {
-        *plan.count = run_s;
+        plan.count[0] = run_s;
+        plan.count[1] = run_c;
         plan.seq_seg[p.rows.N] = run_s;
     }
 }
@@ -74,17 +75,17 @@ __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p)
 // 91 us against 85, gradient 452 against 431.  On request also zeroes rows of no sequence.
 __global__ __launch_bounds__(256) void matrec_rows_kernel(const MatrecParams p, const RestRows rest) {
     clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
-    const int seg_no = blockIdx.x / p.plan.per, c = blockIdx.x % p.plan.per, lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63;
+    int c;
     MatSegment seg;
-    if (!segment_of(p, seg_no, seg)) return;
+    if (!segment_of_chunk(p, blockIdx.x, seg, c)) return;
     const long long left = seg.rows - (long long)c * kChunk;
-    if (left <= 0) return;
     const int rows = left < kChunk ? (int)left : kChunk;
     const long long row = seg.row0 + (long long)c * kChunk;
     for (int head = threadIdx.x >> 6; head < p.Hv; head += 4) {
         const Cum cum = chunk_cum(lane < rows ? p.gate[(row + lane) * p.Hv + head] : 0.0f);
         const float end_hi = lane_value(cum.hi, 63), end_lo = lane_value(cum.lo, 63);
-        float* to = p.rows_of + ((long long)(seg.chunk0 + c) * p.Hv + head) * kRowFloats;
+        float* to = p.rows_of + ((long long)blockIdx.x * p.Hv + head) * kRowFloats;
         to[lane] = cum.hi;
         to[64 + lane] = cum.lo;
         to[128 + lane] = p.scale * exp2_of(cum.hi + cum.lo);
@@ -328,9 +329,8 @@ hipError_t launch_matrec_plan(const MatrecParams& p, const RestRows& rest, hipSt
         hipLaunchKernelGGL(matrec_plan_kernel, dim3(1), dim3(1024), 0, stream, p);
         e = hipGetLastError();
     }
-    const unsigned chunks = (unsigned)((long long)p.plan.max_segs * p.plan.per);
-    if (e != hipSuccess || chunks == 0) return e;
-    hipLaunchKernelGGL(matrec_rows_kernel, dim3(chunks), dim3(256), 0, stream, p, rest);
+    if (e != hipSuccess || p.plan.max_chunks == 0) return e;
+    hipLaunchKernelGGL(matrec_rows_kernel, dim3((unsigned)p.plan.max_chunks), dim3(256), 0, stream, p, rest);
     return hipGetLastError();
 }
 hipError_t launch_matrec_out(int dtype, const MatrecParams& p, hipStream_t stream) {

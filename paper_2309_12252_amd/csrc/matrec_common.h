@@ -238,10 +238,10 @@ struct MatSegment {
 };
 struct MatPlan {
     // with bounds: filled by the plan's kernel; without, every sequence is cut alike and a segment follows from its number
-    int* count;          // segments
+    int* count;          // segments, and chunks
     MatSegment* segs;    // [max_segs]
     int* seq_seg;        // [N + 1]: a sequence's first segment
-    int max_segs, per;
+    int max_segs, max_chunks, per;
 };
 
 struct MatrecParams {
@@ -292,6 +292,27 @@ __device__ __forceinline__ bool segment_of(const MatrecParams& p, int no, MatSeg
     const long long first = (long long)s.index * p.plan.per * 64, most = (long long)p.plan.per * 64;
     s.row0 = s.seq * p.rows.T + first;
     s.rows = p.rows.T - first < most ? p.rows.T - first : most;
+    return true;
+}
+// The segment of chunk number `chunk` of all sequences', and which of its chunks that is; false behind the last.  With bounds all lanes of a wavefront
+// take part: they look at 64 segments at a time, so that up to 4,096 segments are two loads one after another.
+__device__ __forceinline__ bool segment_of_chunk(const MatrecParams& p, int chunk, MatSegment& s, int& place) {
+    if (p.rows.bounds) {
+        if (chunk >= p.plan.count[1]) return false;
+        int lo = 0, hi = p.plan.count[0];   // segment lo begins at the chunk or in front of it, segment hi behind it
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 63) / 64, at = lo + (int)(threadIdx.x & 63) * step;
+            const bool front = at < hi && p.plan.segs[at < hi ? at : lo].chunk0 <= chunk;
+            lo += (__popcll(__ballot(front)) - 1) * step;
+            if (lo + step < hi) hi = lo + step;
+        }
+        s = p.plan.segs[lo];
+    } else {
+        const int chunks = (int)((p.rows.T + 63) / 64);
+        if (chunks == 0 || chunk / chunks >= p.rows.N) return false;
+        if (!segment_of(p, chunk / chunks * ((chunks + p.plan.per - 1) / p.plan.per) + chunk % chunks / p.plan.per, s)) return false;
+    }
+    place = chunk - s.chunk0;
     return true;
 }
 // first segment of sequence n (n = N: how many there are)

@@ -64,15 +64,14 @@ __global__ __launch_bounds__(256) void matrec_through_kernel(const MatrecParams 
     }
 }
 
-// dgate: the parts of the two runs and what goes through; a workgroup has a chunk of a segment
+// dgate: the parts of the two runs and what goes through; a workgroup has a chunk
 __global__ __launch_bounds__(256) void matrec_gates_kernel(const MatrecParams p) {
-    const int seg_no = blockIdx.x / p.plan.per, c = blockIdx.x % p.plan.per;
+    int c;
     MatSegment seg;
-    if (!segment_of(p, seg_no, seg)) return;
+    if (!segment_of_chunk(p, blockIdx.x, seg, c)) return;
     const long long left = seg.rows - (long long)c * kChunk;
-    if (left <= 0) return;
     const int rows = left < kChunk ? (int)left : kChunk;
-    const long long first = (seg.row0 + (long long)c * kChunk) * p.Hv, chunk = (long long)(seg.chunk0 + c) * p.Hv;
+    const long long first = (seg.row0 + (long long)c * kChunk) * p.Hv, chunk = (long long)blockIdx.x * p.Hv;
     for (int i = threadIdx.x; i < rows * p.Hv; i += 256) p.dgate[first + i] += p.gate_k[first + i] + p.read_in[chunk + i % p.Hv];
 }
 
@@ -85,9 +84,9 @@ __global__ __launch_bounds__(256) void matrec_shared_kernel(const MatrecParams p
     using FV = vec_t<float, V>;
     using TV = vec_t<T, V>;
     constexpr int PARTS = kChunk / kSharedRows;
-    const int chunk = blockIdx.x / PARTS, seg_no = chunk / p.plan.per, c = chunk % p.plan.per;
+    int c;
     MatSegment seg;
-    if (!segment_of(p, seg_no, seg)) return;
+    if (!segment_of_chunk(p, blockIdx.x / PARTS, seg, c)) return;
     const long long first = (long long)c * kChunk + blockIdx.x % PARTS * kSharedRows, left = seg.rows - first;
     if (left <= 0) return;
     const int rows = left < kSharedRows ? (int)left : kSharedRows, group = p.Hv / p.Hk, cols = p.Hk * p.Dk;
@@ -130,7 +129,7 @@ hipError_t grad_shape(const MatrecParams& p, hipStream_t stream) {
 
 hipError_t launch_matrec_grad(int dtype, const MatrecParams& p, hipStream_t stream) {
     hipError_t e = dtype == DEER_BF16 ? DEER_BY_SHAPE(grad_shape, BF16, stream) : DEER_BY_SHAPE(grad_shape, float, stream);
-    const unsigned chunks = (unsigned)((long long)p.plan.max_segs * p.plan.per);
+    const unsigned chunks = (unsigned)p.plan.max_chunks;
     if (e != hipSuccess || chunks == 0) return e;
     if (p.Hv != p.Hk) {
         e = dtype == DEER_BF16 ? launch_shared<BF16>(p, chunks, stream) : launch_shared<float>(p, chunks, stream);

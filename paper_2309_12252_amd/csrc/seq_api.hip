@@ -188,9 +188,12 @@ const char* unsupported(const deer_matrec_config* c, bool step) {
     if (step) return (long double)c->N * c->Hv * 256 > kMostLanes ? "more rows than a launch holds" : nullptr;
     if (c->T > kMostRows || (long double)c->N * c->Hv * 64 > 2147483647.0L || ((long double)(c->T + 63) / 64 + 4) * (is_packed(c) ? 1 : c->N) * c->Hv > 2147483647.0L)
         return "more rows than a launch holds";
-    // the gradient's: three workgroups of up to 512 lanes a segment and head; four of 256 a chunk
-    const MatLayout l = mat_layout(c, true);
-    if (((long double)l.max_segs * c->Hv + 8) * 3 * 512 > kMostLanes || (long double)l.max_segs * l.per * 4 * 256 > kMostLanes) return "more rows than a launch holds";
+    // Launches of both directions, so that no forward runs whose gradient is refused: a workgroup of up to 512 lanes a segment and head (gradient: three); four
+    // of 256 a chunk
+    for (const bool grad : {false, true}) {
+        const MatLayout l = mat_layout(c, grad);
+        if (((long double)l.max_segs * c->Hv + 8) * (grad ? 3 : 1) * 512 > kMostLanes || (long double)l.chunks * 4 * 256 > kMostLanes) return "more rows than a launch holds";
+    }
     return nullptr;
 }
 // the row outputs of a direction, to be zeroed where no sequence is
@@ -219,6 +222,7 @@ MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool gr
     p.plan.segs = reinterpret_cast<MatSegment*>(ws + l.off_segs);
     p.plan.seq_seg = reinterpret_cast<int*>(ws + l.off_seq);
     p.plan.max_segs = (int)l.max_segs;
+    p.plan.max_chunks = (int)l.chunks;
     p.plan.per = l.per;
     p.Hk = c->Hk;
     p.Hv = c->Hv;

@@ -146,3 +146,14 @@ def test_rows_of_no_sequence_are_zeroed_on_request():
                 assert ask(ctypes.byref(make(packed=bad)), grad, ctypes.byref(size)) == deer.DEER_ERR_INVALID_ARG
     packed = diag(packed=deer.DEER_ROWS_PACKED | deer.DEER_REST_ZERO)   # (still needs bounds)
     assert lib.deer_diagrec_solve(ctypes.byref(packed), WORD, WORD, None, None, WORD, None, WORD, 1 << 40, None) == deer.DEER_ERR_INVALID_ARG
+
+
+def test_launches_of_both_directions_are_looked_at():
+    """a workgroup a chunk that there can be: T / 64 + N of them for packed rows, however these are cut"""
+    lib, size = deer.load_library(), ctypes.c_size_t(0)
+    for grad in (0, 1):
+        ask = lambda **kw: lib.deer_matrec_workspace_bytes(ctypes.byref(mat(packed=1, **kw)), grad, ctypes.byref(size))   # noqa: E731
+        for N, T, H in ((4096, 1 << 18, 16), (1024, 1 << 20, 16), (1 << 16, 1 << 22, 4)):
+            assert ask(N=N, T=T, Hk=H, Hv=H) == deer.DEER_OK
+        # 2^32 / 1,024 lanes: up to 4,194,303 chunks
+        assert ask(N=1, T=4194302 * 64, Hk=1, Hv=1) == deer.DEER_OK and ask(N=1, T=4194303 * 64, Hk=1, Hv=1) == deer.DEER_ERR_UNSUPPORTED
