@@ -131,24 +131,30 @@ const char* bad_config(const deer_matrec_config* c, bool step) {
 //   512 workgroups at a time: training step of 4 x 4,096 rows and 16 heads with 256 of them 568 us, 384 544, 512 529, 768 538, 1,024 559
 //   up to 4 chunks whole: 64 heads of 256 rows 32 + 52 us whole, 39 + 82 cut; 4 heads of them 25 + 40 and 21 + 31; with no other least length: 4 heads
 //   of 2,048 rows 30 + 46 us, with segments of 4 chunks at least 40 + 59
+// What the sequences' lengths are is not known here; nearly all rows may be one sequence's.  Forward, 16 heads:
+//   packed, a segment has at most two 512ths of all rows: one sequence of 32,768 rows and 63 of one, 128 x 128, 378 us (cut by the number of sequences
+//   alone 2,830); one of 16,384 and 127 of 128 420 us (1,510); 64 of 1,024 325 us (340); 48 of 2,048 490 us either way
+//   a padded batch with lengths, at most 32 chunks: 16 to 4,096 rows, 128 x 128, all of them 399 us (whole 414), one long 241 us (324); 16 to 32,768, 64 x 64, one long 164 us (1,500)
 struct MatLayout {
     long long chunks, max_segs;   // at most
     int per;
     bool split;
     size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_part_q, off_part_k, off_gate, off_read, off_put, off_rows, off_front, total;
 };
-MatLayout mat_layout(const deer_matrec_config* c, bool grad) {
+MatLayout mat_layout(const deer_matrec_config* c, bool grad, bool bounds) {
     MatLayout l{};
     const long long longest = (c->T + kChunk - 1) / kChunk;
     l.chunks = is_packed(c) ? longest + c->N : longest * c->N;
     long long per = longest < 1 ? 1 : longest;
     if (longest > 4 && (is_packed(c) || (long long)c->N * c->Hv < 256)) {
         // 512 workgroups run at a time; every sequence's last segment is a short one, half of the others' length on average
-        long long segs = 512 / c->Hv - (is_packed(c) ? c->N / 2 : 0);
-        if (segs < 1) segs = 1;
+        const long long all = 512 / c->Hv, least = all / 2 > 1 ? all / 2 : 1;
+        long long segs = all - (is_packed(c) ? c->N / 2 : 0);
+        if (segs < least) segs = least;
         per = ((is_packed(c) ? longest : l.chunks) + segs - 1) / segs;
         if (per > longest) per = longest;
     }
+    if (bounds && !is_packed(c) && per > 32) per = 32;
     if (grad && per > 32) per = 32;   // what goes through the chunks of a segment (matrec_grad.hip) takes the rounding errors of all of them
     l.per = (int)per;
     l.split = per < longest;
@@ -191,7 +197,7 @@ const char* unsupported(const deer_matrec_config* c, bool step) {
     // Launches of both directions, so that no forward runs whose gradient is refused: a workgroup of up to 512 lanes a segment and head (gradient: three); four
     // of 256 a chunk
     for (const bool grad : {false, true}) {
-        const MatLayout l = mat_layout(c, grad);
+        const MatLayout l = mat_layout(c, grad, true);   // (no fewer segments than without bounds)
         if (((long double)l.max_segs * c->Hv + 8) * (grad ? 3 : 1) * 512 > kMostLanes || (long double)l.chunks * 4 * 256 > kMostLanes) return "more rows than a launch holds";
     }
     return nullptr;
@@ -359,7 +365,8 @@ deer_status deer_matrec_workspace_bytes(const deer_matrec_config* c, int32_t gra
     if (!bytes) return fail(DEER_ERR_INVALID_ARG, "bytes is NULL");
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
     if (const char* why = unsupported(c, false)) return fail(DEER_ERR_UNSUPPORTED, why);
-    *bytes = mat_layout(c, grad != 0).total;
+    const size_t with = mat_layout(c, grad != 0, true).total, without = mat_layout(c, grad != 0, false).total;
+    *bytes = with > without ? with : without;
     return DEER_OK;
 }
 
@@ -372,7 +379,7 @@ deer_status deer_matrec_solve(const deer_matrec_config* c, const void* d_q, cons
     if (misaligned(d_q, e) || misaligned(d_k, e) || misaligned(d_v, e) || misaligned(d_o, e) || misaligned(d_gate, 4) || misaligned(d_s0, 4) ||
         misaligned(d_last, 4) || misaligned(d_bounds, 8))
         return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
-    const MatLayout l = mat_layout(c, false);
+    const MatLayout l = mat_layout(c, false, d_bounds != nullptr);
     if (deer_status st = check_workspace(d_workspace, workspace_bytes, l.total)) return st;
     MatrecParams p = mat_params(c, l, false, d_bounds, d_workspace);
     p.q = d_q;
@@ -400,7 +407,7 @@ deer_status deer_matrec_grad(const deer_matrec_config* c, const void* d_q, const
         misaligned(d_dv, e) || misaligned(d_gate, 4) || misaligned(d_s0, 4) || misaligned(d_dlast, 4) || misaligned(d_dgate, 4) || misaligned(d_ds0, 4) ||
         misaligned(d_bounds, 8))
         return fail(DEER_ERR_INVALID_ARG, "a pointer is not aligned to its element");
-    const MatLayout l = mat_layout(c, true);
+    const MatLayout l = mat_layout(c, true, d_bounds != nullptr);
     if (deer_status st = check_workspace(d_workspace, workspace_bytes, l.total)) return st;
     MatrecParams p = mat_params(c, l, true, d_bounds, d_workspace);
     p.q = d_q;

@@ -157,3 +157,18 @@ def test_launches_of_both_directions_are_looked_at():
             assert ask(N=N, T=T, Hk=H, Hv=H) == deer.DEER_OK
         # 2^32 / 1,024 lanes: up to 4,194,303 chunks
         assert ask(N=1, T=4194302 * 64, Hk=1, Hv=1) == deer.DEER_OK and ask(N=1, T=4194303 * 64, Hk=1, Hv=1) == deer.DEER_ERR_UNSUPPORTED
+
+
+def test_one_long_sequence_among_many_is_cut():
+    """seen by the room for the states of its segments: 64 x 64 floats a segment and head"""
+    lib, size = deer.load_library(), ctypes.c_size_t(0)
+
+    def room(**kw):
+        assert lib.deer_matrec_workspace_bytes(ctypes.byref(mat(Hk=16, Hv=16, **kw)), 0, ctypes.byref(size)) == deer.DEER_OK
+        chunks = kw["T"] // 64 + kw["N"] if kw.get("packed") else kw["T"] // 64 * kw["N"]
+        return (size.value - chunks * 16 * 260 * 4) / (16 * 64 * 64 * 4)   # (260 floats a chunk and head for the gates)
+
+    # 512 chunks on 256 CUs and 16 heads: at least 16 segments where one sequence may have them all
+    for N in (1, 8, 64, 1024):
+        assert room(packed=1, N=N, T=32768) >= 16
+    assert room(N=16, T=32768) >= 16 * 16   # a padded batch, for all may be long
