@@ -2,7 +2,10 @@
 import pytest
 import torch
 
+import seq_oracle as so
+import test_gpu_matrec as tm
 from paper_2309_12252_amd import deer
+from test_seq_abi import LONG
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -52,3 +55,18 @@ def test_many_sequences_of_any_length():
         # the absolute sums behind them stay below 100 of the largest result
         for x, y in zip((o[a:b], last[n]) + tuple(t[a:b] for t in grads[:4]), (wo[0], wlast[0]) + tuple(t[0] for t in wants[:4])):
             assert float((x - y).abs().max()) <= 2 * 4 * (b - a + 128) * 2.0 ** -24 * 100 * float(y.abs().max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", list(LONG))
+def test_segments_of_several_chunks(name, dtype):
+    """cut sequences whose segments have more than one chunk: their own parts, the states that are joined, the runs from these"""
+    c = LONG[name]
+    H, lens, packed = c["H"], c["lens"], c["packed"]
+    N, T = len(lens), sum(lens) if packed else max(lens)
+    off = [0]
+    for n in lens:
+        off.append(off[-1] + n)
+    d = tm.make(dtype, (T,) if packed else (N, T), N, c["Hk"], H, c["Dk"], c["Dv"], len(name))
+    more = {"offsets": torch.tensor(off, device=DEV)} if packed else {"lengths": torch.tensor(lens, device=DEV)} if min(lens) < T else {}
+    tm.compare(d, tm.both(d, **more), so.sequences(T, N, offsets=off if packed else None, lengths=lens), dtype, c["Dk"] ** -0.5)

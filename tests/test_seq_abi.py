@@ -172,3 +172,26 @@ def test_one_long_sequence_among_many_is_cut():
     for N in (1, 8, 64, 1024):
         assert room(packed=1, N=N, T=32768) >= 16
     assert room(N=16, T=32768) >= 16 * 16   # a padded batch, for all may be long
+
+
+# Matrix states: calls whose sequences are cut into segments of several chunks.  segs: for how many there is room
+LONG = {
+    "six": dict(H=64, Hk=64, Dk=8, Dv=8, lens=[3001], packed=0, segs=8),                     # 47 chunks on 512 workgroups: 8 segments of 6, the last of 5
+    "twelve": dict(H=128, Hk=64, Dk=5, Dv=9, lens=[3001], packed=0, segs=4),                 # 12 chunks, the last 11
+    "cap": dict(H=256, Hk=256, Dk=4, Dv=4, lens=[3001], packed=0, segs=2),                   # forward whole (room as with lengths), gradient 32 and 15 chunks
+    "packed": dict(H=64, Hk=32, Dk=8, Dv=4, lens=[1500, 3, 0, 2000, 64, 700], packed=1, segs=11),   # 67 + 6 chunks, by 14
+    "padded": dict(H=128, Hk=128, Dk=4, Dv=4, lens=[2200, 100], packed=0, segs=4),           # 35 chunks: 32 and 3, in either direction
+    "wide": dict(H=64, Hk=64, Dk=128, Dv=72, lens=[1100], packed=0, segs=6),                 # 18 chunks by 3
+}
+
+
+def test_shapes_with_segments_of_several_chunks():
+    lib, size = deer.load_library(), ctypes.c_size_t(0)
+    for name, c in LONG.items():
+        N, T = len(c["lens"]), sum(c["lens"]) if c["packed"] else max(c["lens"])
+        chunks = (T + 63) // 64 + N if c["packed"] else (T + 63) // 64 * N
+        cfg = mat(N=N, T=T, packed=c["packed"], Hk=c["Hk"], Hv=c["H"], Dk=c["Dk"], Dv=c["Dv"])
+        tile = c["H"] * (64 if c["Dk"] <= 64 else 128) * (64 if c["Dv"] <= 64 else 128) * 4
+        assert lib.deer_matrec_workspace_bytes(ctypes.byref(cfg), 0, ctypes.byref(size)) == deer.DEER_OK
+        segs = (size.value - chunks * c["H"] * 260 * 4) / tile   # what is left beside the states is less than one of them
+        assert c["segs"] <= segs < c["segs"] + 1, (name, segs)
