@@ -221,6 +221,14 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
+// sum over the wavefront, in lane 63: the rows' sums, the first, second and third row's handed on
+__device__ __forceinline__ float wave_sum(float v) {
+    v = group_sum(v);
+    v += rotated<0x142>(v);
+    v += rotated<0x143>(v);
+    return v;
+}
+
 // tile n of the ten 16 x 16 tiles on and below the diagonal of a chunk's 64 x 64 pairs
 __device__ __forceinline__ void lower_tile(int n, int& ti, int& tj) {
     ti = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3;
@@ -263,6 +271,7 @@ struct MatrecParams {
     float *part_q, *part_k;          // [rows][Hv][Dk]: dq and dk by heads of v, where several share one
     float *gate_k;                   // [rows][Hv]: the part of dgate that the run of dk has
     float *read_in, *put_out;        // [chunks][Hv]: sums of q_i . (...) and k_j . (...) over a chunk
+    float *size_in, *size_out;       // [chunks][Hv]: sums of the squares of the state in front of a chunk, and of the gradient of the state behind it
     float *front;                    // [max_segs][Hv]: <state, its gradient> in front of a segment
 };
 struct MatstepParams {

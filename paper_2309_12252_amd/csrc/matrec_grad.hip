@@ -10,8 +10,9 @@
 // The runs have u, w and the pairs: running sums over j along every row i, of which t takes those of the rows i >= t at j = t - 1.  z is not
 // computed from S and R, which are never in one place: <S, dS> in front of a chunk is z + sum u, behind it z + sum w, and in front of a
 // segment it is taken from both states.  So z comes with the rounding errors of the sums of u and w of a segment's chunks (2^-24 of their terms
-// each, 32 chunks at most), and is nothing where a chunk's factor is nothing; the rest loses nothing to cancellation.  M in the sums of u and w is taken as three bf16
-// pieces, A and B are exact products of the inputs.  Heads of v that share one of q and k: dq and dk as floats by head first, then
+// each, 32 chunks at most), which a state that was large in front leaves behind after it is forgotten: the difference is therefore kept within
+// e^{c_64} |S| |R| (sums of squares of S and R, which the runs of dq and dk take in front of every chunk), and with it the error; the rest loses nothing to
+// cancellation.  M in the sums of u and w is taken as three bf16 pieces, A and B are exact products of the inputs.  Heads of v that share one of q and k: dq and dk as floats by head first, then
 // summed in the heads' order.
 #include "matrec_run.h"
 
@@ -46,18 +47,21 @@ __global__ __launch_bounds__(256) void matrec_through_kernel(const MatrecParams 
     float here = p.front[at];
     constexpr int K = 8;
     for (int c0 = 0; c0 < chunks; c0 += K) {
-        float u[K], w[K], f[K];
+        float u[K], w[K], f[K], most[K];
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             const long long c = (long long)(seg.chunk0 + (c0 + i < chunks ? c0 + i : chunks - 1)) * p.Hv + head;
             u[i] = p.read_in[c];
             w[i] = p.put_out[c];
             f[i] = p.rows_of[c * kRowFloats + 256];
+            // (squares below the smallest number are lost, 16,384 of them at most; pieces of a state are off by 2^-8, its size by less than 2^-7)
+            most[i] = 1.02f * f[i] * __builtin_amdgcn_sqrtf(p.size_in[c] + 1e-33f) * __builtin_amdgcn_sqrtf(p.size_out[c] + 1e-33f);
         }
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             if (c0 + i >= chunks) break;
-            const float z = f[i] < 0x1p-60f ? 0.0f : here - u[i];   // (a factor that leaves nothing of <S, R>)
+            float z = f[i] < 0x1p-60f ? 0.0f : here - u[i];   // (a factor that leaves nothing of <S, R>)
+            if (fabsf(z) > most[i]) z = copysignf(most[i], z);
             p.read_in[(long long)(seg.chunk0 + c0 + i) * p.Hv + head] = z;
             here = z + w[i];
         }

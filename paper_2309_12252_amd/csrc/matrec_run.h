@@ -30,7 +30,8 @@ struct RunLds {
                             dots = rows + 4 * 5 * 64,                    // [W][64]
                             by_col = dots + (SUMS ? 4 * 64 * W : 0),   // [row tile][64]
                             by_row = by_col + (FOUR ? 4 * 256 : 0),      // [column tile][64]
-                            total = by_row + (FOUR ? 4 * 256 : 0);
+                            size = by_row + (FOUR ? 4 * 256 : 0),        // [W][16]: squares of the state's columns
+                            total = size + (SUMS ? 4 * 16 * W : 0);
     static_assert(total <= 160 * 1024, "a workgroup's tiles fit the CU's LDS");
 };
 
@@ -126,7 +127,8 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     T *ta = reinterpret_cast<T*>(lds + L::a), *tb = reinterpret_cast<T*>(lds + L::b), *tc = reinterpret_cast<T*>(lds + L::c), *tq = reinterpret_cast<T*>(lds + L::q),
       *tp = reinterpret_cast<T*>(lds + L::pairs);
     float *cum_hi = reinterpret_cast<float*>(lds + L::rows), *cum_lo = cum_hi + 64, *f_out = cum_hi + 128, *w_in = cum_hi + 192;
-    float *dots = reinterpret_cast<float*>(lds + L::dots), *by_col = reinterpret_cast<float*>(lds + L::by_col), *by_row = reinterpret_cast<float*>(lds + L::by_row);
+    float *dots = reinterpret_cast<float*>(lds + L::dots), *by_col = reinterpret_cast<float*>(lds + L::by_col), *by_row = reinterpret_cast<float*>(lds + L::by_row),
+          *size = reinterpret_cast<float*>(lds + L::size);
     auto load = [&](int c) {
         long long row;
         const int rows = rows_of(c, row), i = again(lane0);
@@ -234,6 +236,9 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
             for (int u = 0; u < VT; ++u) acc[t][u] = F32x4{0, 0, 0, 0};
         if (strip) {
+        // L::SUMS: how large the state is, for the bound of what goes through the chunk, from its first pieces: products of its columns with each other, of
+        // which the diagonal is taken (four matrix instructions, which have time; fp32: sums of squares)
+        F32x4 square = {0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             constexpr int PIECES = L::SUMS ? P : 1;   // an output's rounded factor; the gates' sums take M as it is
@@ -243,6 +248,13 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                 if constexpr (PIECES > 1) pieces_of<T>(joined(M[2 * s][u], M[2 * s + 1][u]), m[u]);
                 else m[u][0] = rounded<T>(joined(M[2 * s][u], M[2 * s + 1][u]));
             }
+            if constexpr (L::SUMS) {
+#pragma unroll
+                for (int u = 0; u < VT; ++u) {
+                    if constexpr (P > 1) square = mma(m[u][0], m[u][0], square);
+                    else square += M[2 * s][u] * M[2 * s][u] + M[2 * s + 1][u] * M[2 * s + 1][u];
+                }
+            }
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const frag_t<T> af = T1::row_frag(ta, 16 * t + l, s, g);
@@ -251,6 +263,15 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
                     for (int u = 0; u < VT; ++u) acc[t][u] = mma(m[u][n], af, acc[t][u]);
             }
+        }
+        if constexpr (L::SUMS) {
+            float x = (l & 2) != 0 ? ((l & 1) != 0 ? square[3] : square[2]) : (l & 1) != 0 ? square[1] : square[0];
+            if constexpr (P == 1) {
+                x = (square[0] + square[1]) + (square[2] + square[3]);
+                x += __shfl_xor(x, 16);
+                x += __shfl_xor(x, 32);
+            }
+            if (g == l >> 2) size[16 * wave + l] = x;
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -305,6 +326,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         }
         } else if (L::SUMS) {
             dots[64 * wave + lane] = 0.0f;
+            if (g == 0) size[16 * wave + l] = 0.0f;
         }
         __syncthreads();
 
@@ -319,6 +341,11 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
                     for (int u = 0; u < VT; ++u) acc[t][u] = mma(cf[s][u], pf, acc[t][u]);
                 }
+        }
+        const long long chunk = (long long)(seg.chunk0 + (BACK ? chunks - 1 - c : c)) * p.Hv + head;
+        if (L::SUMS && p.dgate && wave == 0) {
+            const float squares = wave_sum(size[lane] + (W > 4 ? size[W > 4 ? 64 + lane : 0] : 0.0f));
+            if (lane == 63) (MODE == RUN_DQ ? p.size_in : p.size_out)[chunk] = squares;
         }
         if (L::SUMS && p.dgate && wave == W - 1) {
             // A lane has row i.  Dq: sums from i on of what is read there, and the pairs that pass i.  Dk (backwards): sums behind i of
@@ -345,7 +372,6 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
                     }
                 }
             }
-            const long long chunk = (long long)(seg.chunk0 + (BACK ? chunks - 1 - c : c)) * p.Hv + head;
             if (lane == 0) (MODE == RUN_DQ ? p.read_in : p.put_out)[chunk] = x;
             if constexpr (MODE == RUN_DQ) {
 #pragma unroll

@@ -139,7 +139,7 @@ struct MatLayout {
     long long chunks, max_segs;   // at most
     int per;
     bool split;
-    size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_part_q, off_part_k, off_gate, off_read, off_put, off_rows, off_front, total;
+    size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_part_q, off_part_k, off_gate, off_read, off_put, off_size_in, off_size_out, off_rows, off_front, total;
 };
 MatLayout mat_layout(const deer_matrec_config* c, bool grad, bool bounds) {
     MatLayout l{};
@@ -183,6 +183,8 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad, bool bounds) {
         l.off_gate = take(rows * by_head);
         l.off_read = take((size_t)l.chunks * by_head);
         l.off_put = take((size_t)l.chunks * by_head);
+        l.off_size_in = take((size_t)l.chunks * by_head);
+        l.off_size_out = take((size_t)l.chunks * by_head);
         l.off_front = take((size_t)l.max_segs * by_head);
     }
     l.total = at;
@@ -254,6 +256,8 @@ MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool gr
         p.gate_k = reinterpret_cast<float*>(ws + l.off_gate);
         p.read_in = reinterpret_cast<float*>(ws + l.off_read);
         p.put_out = reinterpret_cast<float*>(ws + l.off_put);
+        p.size_in = reinterpret_cast<float*>(ws + l.off_size_in);
+        p.size_out = reinterpret_cast<float*>(ws + l.off_size_out);
         p.front = reinterpret_cast<float*>(ws + l.off_front);
     }
     return p;
