@@ -190,7 +190,7 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
     const int ch = (int)(rest % dgroups) * C + lane * V;
     const bool on = ch < p.D;
     const int chl = on ? ch : 0;                       // (lanes without a channel look at the first one's states, and write nothing)
-    const int col = on ? ch * (int)sizeof(T) : kNoColumn;
+    const unsigned col = on ? (unsigned)ch * (unsigned)sizeof(T) : kNoColumn;
     const long long tile_row = (long long)(REV ? p.chunks - 1 - c : c) * L;
     const long long row0 = tile_row + (REV ? W - 1 - wave : wave) * R;
 
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
         const RowsAt ad(reinterpret_cast<const T*>(p.dh) + r0 * p.stride_out, p.stride_out);
         const RowsAt ah(reinterpret_cast<const T*>(p.h) + (r0 - ahead) * p.stride_out, p.stride_out);
         // a row that is none reads the nearest one that is
-        int at_g = col + first * ag.pitch, at_x = col + first * ax.pitch, at_d = col + first * ad.pitch, at_h = col + (first + ahead > 0 ? first + ahead - 1 : 0) * ad.pitch;
+        unsigned at_g = col + first * ag.pitch, at_x = col + first * ax.pitch, at_d = col + first * ad.pitch, at_h = col + (first + ahead > 0 ? first + ahead - 1 : 0) * ad.pitch;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             rg[j] = ag.template load<B>(at_g);
@@ -384,13 +384,13 @@ __global__ __launch_bounds__(64 * W, 4) void diagrec_kernel(const DiagrecParams 
 #pragma unroll
             for (int v = 0; v < V; ++v) h[v] = r ? sh_h[w][lane * V + v] : sh_a[w][lane * V + v] * h[v] + sh_h[w][lane * V + v];
         }
-        const int pitch_1 = REV ? odg.pitch : oh.pitch, pitch_2 = odx.pitch;
-        int next_1 = col + (REV ? (R - 1) * pitch_1 : 0), next_2 = col + (R - 1) * pitch_2;
+        const unsigned pitch_1 = REV ? odg.pitch : oh.pitch, pitch_2 = odx.pitch;
+        unsigned next_1 = col + (REV ? (R - 1) * pitch_1 : 0), next_2 = col + (R - 1) * pitch_2;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int j = REV ? R - 1 - i : i;
-            const int at_1 = next_1, at_2 = next_2;
-            next_1 += REV ? -pitch_1 : pitch_1;
+            const unsigned at_1 = next_1, at_2 = next_2;
+            next_1 = REV ? next_1 - pitch_1 : next_1 + pitch_1;
             next_2 -= pitch_2;
             if (!PLAIN && !((live_bits >> j) & 1)) continue;
             if (!PLAIN && ((starts >> j) & 1)) {

@@ -96,23 +96,23 @@ __device__ __forceinline__ void vec_set(vec_t<T, V>& v, int i, T x) {
 }
 
 // Rows of an array by buffer instructions, by a lane's offset in bytes: one register where an address takes two, and a lane without a
-// column is out of bounds (reads zero, writes nothing) at kNoColumn and beyond.  The caller has the rows in bounds.
-constexpr int kNoColumn = 0x7FFFFFF0;
+// column is out of bounds (reads zero, writes nothing) at kNoColumn and beyond, up to 2^32: offsets are unsigned.  The caller has the rows in bounds.
+constexpr unsigned kNoColumn = 0x7FFFFFF0;
 constexpr long long kMostStride = 1 << 22;   // elements: 64 rows of 8 bytes each stay below kNoColumn, and it plus them below 2^32
 struct RowsAt {
     __amdgpu_buffer_rsrc_t rsrc;
-    int pitch;
+    unsigned pitch;
     template <typename T>
     __device__ __forceinline__ RowsAt(const T* first, long long stride)
-        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(first), 0, kNoColumn, 0x00020000)), pitch((int)(stride * (long long)sizeof(T))) {}
+        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(first), 0, (int)kNoColumn, 0x00020000)), pitch((unsigned)(stride * (long long)sizeof(T))) {}
     template <typename X>
-    __device__ __forceinline__ X load(int at) const {
+    __device__ __forceinline__ X load(unsigned at) const {
         if constexpr (sizeof(X) == 8) return __builtin_bit_cast(X, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0));
         else if constexpr (sizeof(X) == 4) return __builtin_bit_cast(X, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0));
         else return __builtin_bit_cast(X, (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0));
     }
     template <typename X>
-    __device__ __forceinline__ void store(X x, int at) const {
+    __device__ __forceinline__ void store(X x, unsigned at) const {
         using U2 = unsigned __attribute__((ext_vector_type(2)));
         if constexpr (sizeof(X) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(U2, x), rsrc, at, 0, 0);
         else if constexpr (sizeof(X) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), rsrc, at, 0, 0);

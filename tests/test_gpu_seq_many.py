@@ -70,3 +70,25 @@ def test_segments_of_several_chunks(name, dtype):
     d = tm.make(dtype, (T,) if packed else (N, T), N, c["Hk"], H, c["Dk"], c["Dv"], len(name))
     more = {"offsets": torch.tensor(off, device=DEV)} if packed else {"lengths": torch.tensor(lens, device=DEV)} if min(lens) < T else {}
     tm.compare(d, tm.both(d, **more), so.sequences(T, N, offsets=off if packed else None, lengths=lens), dtype, c["Dk"] ** -0.5)
+
+
+@pytest.mark.parametrize("dtype,D", [(torch.float64, 65), (torch.bfloat16, 65), (torch.float32, 130)])
+def test_lanes_without_a_channel_at_the_largest_stride(dtype, D):
+    """their offsets pass 2^31 on the way along the rows"""
+    T, far = 40, 1 << 22
+    wide = torch.full((T, far), 5.0, dtype=dtype, device=DEV)
+    gate, x, dh = (torch.randn(T, D, device=DEV).to(dtype) for _ in range(3))
+    g, u, d, h, dg, du = (wide[:, 200 * i:200 * i + D] for i in range(6))
+    for a, b in ((g, gate), (u, x), (d, dh)):
+        a.copy_(b)
+    offsets = torch.tensor([0, 7, T], device=DEV)
+    more = {"kind": deer.DEER_GATE_SIGMOID, "offsets": offsets}
+    want = deer.diagrec_solve(gate, x, **more)
+    want += deer.diagrec_grad(gate, x, want[0], dh, **more)
+    got = deer.diagrec_solve(g, u, out=h, **more)
+    got += deer.diagrec_grad(g, u, h, d, dgate=dg, dx=du, **more)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for i in range(6):   # nothing beside the rows
+        assert bool((wide[:, 200 * i + D:200 * i + 200] == 5).all())
+    assert bool((wide[:, 1200:1 << 20] == 5).all())
