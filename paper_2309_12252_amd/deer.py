@@ -328,6 +328,15 @@ def _int32(*sizes):
             _refuse("sequences, channels and slots are counted in 32 bits")
 
 
+def _draw_of(seed, draw):
+    """number of the draw and seed as the library takes them, in 32 and 64 bits"""
+    if not 0 <= draw < 1 << 32:
+        _refuse("draw: must lie in 0 .. 2^32 - 1")
+    if not -(1 << 63) <= seed < 1 << 64:
+        _refuse("seed: must be a number of 64 bits")
+    return draw, seed & 0xFFFFFFFFFFFFFFFF
+
+
 def _row_stride(t, what, lead):
     """Elements from a row of t to the next: `lead` leading dimensions that lie like rows one behind another, the dimensions behind them dense."""
     shape = t.shape
@@ -445,8 +454,9 @@ def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, leng
         h = out
         _check_like(h, "out", x.shape, x.dtype, dev)
     rest = _zero_rest(bounds, h if out is None else None)
-    cfg = DiagrecConfig(dtype, kind, N, D, T, packed | rest, draw & 0xFFFFFFFF, _row_stride(gate, "gate", lead), _row_stride(x, "x", lead),
-                        _row_stride(h, "out", lead), drop, seed & 0xFFFFFFFFFFFFFFFF)
+    draw, seed = _draw_of(seed, draw)
+    cfg = DiagrecConfig(dtype, kind, N, D, T, packed | rest, draw, _row_stride(gate, "gate", lead), _row_stride(x, "x", lead),
+                        _row_stride(h, "out", lead), drop, seed)
     last = torch.empty((N, D), dtype=w, device=dev)
     h0p = _dense(h0, "h0", last.shape, w, dev)
     size = _diag_workspace(0, dtype, kind, N, D, T, packed)
@@ -485,8 +495,9 @@ def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, 
         _check_like(dx, "dx", x.shape, x.dtype, dev)
         if _row_stride(dx, "dx", lead) != stride_x:
             _refuse("dx: rows must lie like those of x")
+    draw, seed = _draw_of(seed, draw)
     rest = _zero_rest(bounds, *(None if g else t for g, t in zip(given, (dgate, dx))))
-    cfg = DiagrecConfig(dtype, kind, N, D, T, packed | rest, draw & 0xFFFFFFFF, stride_g, stride_x, stride_h, drop, seed & 0xFFFFFFFFFFFFFFFF)
+    cfg = DiagrecConfig(dtype, kind, N, D, T, packed | rest, draw, stride_g, stride_x, stride_h, drop, seed)
     dh0 = torch.empty((N, D), dtype=w, device=dev)
     h0p, dlp = _dense(h0, "h0", dh0.shape, w, dev), _dense(dlast, "dlast", dh0.shape, w, dev)
     size = _diag_workspace(1, dtype, kind, N, D, T, packed)
@@ -661,10 +672,11 @@ def dropout(x, p, seed, draw=0, *, out=None):
     else:
         y = out
         _check_like(y, "out", x.shape, x.dtype, dev)
+    draw, seed = _draw_of(seed, draw)
     N, T, D = x.shape if lead == 2 else (1,) + tuple(x.shape)
     _int32(N, D)
     st = lib.deer_dropout(dtype, N, T, D, x.data_ptr(), _row_stride(x, "x", lead), y.data_ptr(), _row_stride(y, "out", lead), p,
-                          seed & 0xFFFFFFFFFFFFFFFF, draw & 0xFFFFFFFF, _stream_of(dev))
+                          seed, draw, _stream_of(dev))
     if st != DEER_OK:
         _raise(lib, st)
     return y

@@ -195,3 +195,11 @@ def test_shapes_with_segments_of_several_chunks():
         assert lib.deer_matrec_workspace_bytes(ctypes.byref(cfg), 0, ctypes.byref(size)) == deer.DEER_OK
         segs = (size.value - chunks * c["H"] * 260 * 4) / tile   # what is left beside the states is less than one of them
         assert c["segs"] <= segs < c["segs"] + 1, (name, segs)
+
+
+def test_draws_and_seeds_are_not_cut_short():
+    assert deer._draw_of(-1, 0) == (0, 2 ** 64 - 1) and deer._draw_of(2 ** 64 - 1, 2 ** 32 - 1) == (2 ** 32 - 1, 2 ** 64 - 1)
+    for seed, draw in ((0, 2 ** 32), (0, -1), (2 ** 64, 0), (-2 ** 63 - 1, 0)):
+        with pytest.raises(deer.DeerError) as e:
+            deer._draw_of(seed, draw)
+        assert e.value.status == deer.DEER_ERR_INVALID_ARG
