@@ -314,7 +314,7 @@ typedef struct {
     int32_t Hk, Hv;    /* heads of q and k, heads of v: a multiple; head h goes with h / (Hv / Hk)         */
     int32_t Dk, Dv;    /* 1 .. 128                                                                         */
     int32_t reserved;  /* must be 0                                                                        */
-    double scale;      /* of the outputs                                                                   */
+    double scale;      /* of the outputs; a finite number of 32 bits                                       */
     int64_t stride_q, stride_k, stride_v, stride_o;   /* rows (0: Hk Dk, Hk Dk, Hv Dv, Hv Dv); gradients lie like their arrays, dL/do like o */
 } deer_matrec_config;
 

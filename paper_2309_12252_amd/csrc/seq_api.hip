@@ -116,7 +116,7 @@ const char* bad_config(const deer_matrec_config* c, bool step) {
     if (c->N < 1 || c->Hk < 1 || c->Hv < 1 || c->Dk < 1 || c->Dv < 1) return "N, Hk, Hv, Dk and Dv must be positive";
     if (c->Hv % c->Hk) return "Hv must be a multiple of Hk";
     if (c->reserved != 0) return "reserved must be 0";
-    if (!std::isfinite(c->scale)) return "scale must be finite";
+    if (!std::isfinite((float)c->scale)) return "scale must be finite in 32 bits";
     if (c->stride_q < 0 || c->stride_k < 0 || c->stride_v < 0 || c->stride_o < 0) return "strides must not be negative";
     const int64_t keys = (int64_t)c->Hk * c->Dk, values = (int64_t)c->Hv * c->Dv;
     if ((c->stride_q && c->stride_q < keys) || (c->stride_k && c->stride_k < keys) || (c->stride_v && c->stride_v < values) || (c->stride_o && c->stride_o < values))

@@ -203,3 +203,12 @@ def test_draws_and_seeds_are_not_cut_short():
         with pytest.raises(deer.DeerError) as e:
             deer._draw_of(seed, draw)
         assert e.value.status == deer.DEER_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e300, float("nan")])
+def test_scale_is_a_number_of_32_bits(scale):
+    lib, cfg, size = deer.load_library(), mat(scale=scale), ctypes.c_size_t(0)
+    ref = ctypes.byref(cfg)
+    assert lib.deer_matrec_workspace_bytes(ref, 0, ctypes.byref(size)) == deer.DEER_ERR_INVALID_ARG
+    assert lib.deer_matrec_solve(ref, WORD, WORD, WORD, WORD, None, None, WORD, None, WORD, 1 << 40, None) == deer.DEER_ERR_INVALID_ARG
+    assert lib.deer_matrec_step(ref, WORD, WORD, WORD, WORD, None, 4, WORD, WORD, None) == deer.DEER_ERR_INVALID_ARG
