@@ -562,8 +562,7 @@ template <typename T, bool REV> constexpr int tile_rows() { return Shape<T, REV>
 
 }  // namespace
 
-size_t diagrec_words(int dtype, int gate, int N, long long T, int D, bool grad, int* chunks, int* groups, size_t* agg_words) {
-    (void)gate;
+size_t diagrec_words(int dtype, int N, long long T, int D, bool grad, int* chunks, int* groups, size_t* agg_words) {
     const int L = dtype == DEER_F64   ? (grad ? tile_rows<double, true>() : tile_rows<double, false>())
                   : dtype == DEER_F32 ? (grad ? tile_rows<float, true>() : tile_rows<float, false>())
                                       : (grad ? tile_rows<BF16, true>() : tile_rows<BF16, false>());

@@ -107,11 +107,11 @@ struct StatesLds {
 };
 template <typename T, int DK, int DV, bool REV>
 __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* lds) {
-    constexpr int W = DV / 16, VT = 1, NT = DK / 16, P = Op<T>::PIECES;
+    constexpr int W = DV / 16, NT = DK / 16, P = Op<T>::PIECES;
     using L = StatesLds<T, DK, DV>;
     using TK = Tile<T, DK>;
     using TV = Tile<T, DV>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15, n0 = VT * wave;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, l = lane & 15;
     const int seg_no = blockIdx.x / p.Hv, head = blockIdx.x % p.Hv, kh = head / (p.Hv / p.Hk);
     MatSegment seg;
     if (!segment_of(p, seg_no, seg)) return;
@@ -123,11 +123,9 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
     const bool wide_k = wide_rows(k, stride_k, p.Dk), wide_v = wide_rows(v, stride_v, p.Dv);
     T *tk = reinterpret_cast<T*>(lds + L::k), *tv = reinterpret_cast<T*>(lds + L::v);
     float* weight = reinterpret_cast<float*>(lds + L::w);
-    F32x4 S[NT][VT];
+    F32x4 S[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int u = 0; u < VT; ++u) S[t][u] = F32x4{0, 0, 0, 0};
+    for (int t = 0; t < NT; ++t) S[t] = F32x4{0, 0, 0, 0};
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
     double total = 0.0;
     auto load = [&](int i) {
@@ -146,22 +144,17 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
         const float whole = weight[64];
         total += (double)weight[65] + (double)weight[66];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int u = 0; u < VT; ++u) S[t][u] *= whole;
+        for (int t = 0; t < NT; ++t) S[t] *= whole;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const F32x4 w0 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 8 * g), w1 = *reinterpret_cast<const F32x4*>(weight + 32 * s + 8 * g + 4);
-            frag_t<T> vp[VT][P];
-#pragma unroll
-            for (int u = 0; u < VT; ++u) pieces_of<T>(widened(TV::col_frag(tv, s, n0 + u, lane)) * joined(w0, w1), vp[u]);
+            frag_t<T> vp[P];
+            pieces_of<T>(widened(TV::col_frag(tv, s, wave, lane)) * joined(w0, w1), vp);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const frag_t<T> kf = TK::col_frag(tk, s, t, lane);
 #pragma unroll
-                for (int q = P - 1; q >= 0; --q)
-#pragma unroll
-                    for (int u = 0; u < VT; ++u) S[t][u] = mma(vp[u][q], kf, S[t][u]);
+                for (int q = P - 1; q >= 0; --q) S[t] = mma(vp[q], kf, S[t]);
             }
         }
         __syncthreads();
@@ -170,9 +163,7 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
     const long long at = (long long)seg_no * p.Hv + head;
     float* to = (REV ? p.seg_rstate : p.seg_state) + at * (DK * DV);   // (outside the head: zero in S too)
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int u = 0; u < VT; ++u) *reinterpret_cast<F32x4*>(to + column_of(t, l) * DV + column_of(n0 + u, 4 * g)) = S[t][u];
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<F32x4*>(to + column_of(t, l) * DV + column_of(wave, 4 * g)) = S[t];
     if (threadIdx.x == 0) p.seg_decay[(REV ? (long long)p.plan.max_segs * p.Hv : 0) + at] = (float)exp2(total);
 }
 

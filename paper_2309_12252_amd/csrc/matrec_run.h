@@ -6,7 +6,7 @@
 //   Dk   a, b, c = v, dout, q      M = R^T   rows and chunks backwards: c_i stands for -c_i, f_i = e^{c_64 - c_i}, w_j = scale e^{c_j}
 //   Dv   a, b, c = k, q, dout      M = R     backwards, the same
 // (S the state in front of a chunk, R the gradient of the state behind it.)  Wavefront w has 16 of c's columns: M's, as
-// results, which are operands of M^T a as they stand, and the outputs', transposed, a lane four or eight neighbouring columns of a row.
+// results, which are operands of M^T a as they stand, and the outputs', transposed, a lane four neighbouring columns of a row.
 // What bounds it: 120 to 210 matrix instructions of 16 cycles and some 500 vector instructions a wavefront and chunk of 128 columns, which a SIMD does one
 // after another, and 64 KiB of rows a chunk.  Two workgroups fill a CU and go on while the other one waits for its rows, which go straight to LDS: no
 // registers for them, so that 128 are enough (one workgroup a CU with its next rows in registers: gradient of 4 x 4,096 rows, 16 heads of
@@ -60,7 +60,8 @@ struct StateAt {
 template <typename T, int DK, int DV, int W, int MODE>
 __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char* lds, int id) {
     constexpr bool BACK = MODE == RUN_DK || MODE == RUN_DV, KEYS = MODE == RUN_DQ || MODE == RUN_DK;   // KEYS: D1 is the values', D2 the keys'
-    constexpr int D1 = KEYS ? DV : DK, D2 = KEYS ? DK : DV, KS = D1 / 32, NT = D1 / 16, VT = D2 / (16 * W) > 0 ? D2 / (16 * W) : 1, P = Op<T>::PIECES;
+    constexpr int D1 = KEYS ? DV : DK, D2 = KEYS ? DK : DV, KS = D1 / 32, NT = D1 / 16, P = Op<T>::PIECES;
+    static_assert(16 * W >= D2, "a wavefront has 16 of c's columns");
     using L = RunLds<T, D1, D2, W, MODE>;
     using T1 = Tile<T, D1>;
     using T2 = Tile<T, D2>;
@@ -71,9 +72,9 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     const int seg_no = id / p.Hv, head = id % p.Hv, kh = head / (p.Hv / p.Hk);
     MatSegment seg;
     if (!segment_of(p, seg_no, seg)) return;
-    const int d1 = KEYS ? p.Dv : p.Dk, d2 = KEYS ? p.Dk : p.Dv, n0 = VT * wave;   // this wavefront's first tile of columns
-    const bool strip = 16 * n0 < D2;                                             // (it has some)
-    const int col0 = column_of(n0, 4 * g);                                       // a lane's first column of 4 VT
+    const int d1 = KEYS ? p.Dv : p.Dk, d2 = KEYS ? p.Dk : p.Dv;
+    const bool strip = 16 * wave < D2;                                           // (this wavefront has columns)
+    const int col0 = column_of(wave, 4 * g);                                     // a lane's first of four
 
     // ---- arrays of rows ----
     const T* q = reinterpret_cast<const T*>(p.q) + (long long)kh * p.Dk + seg.row0 * p.stride_q;
@@ -99,19 +100,17 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     const int chunks = (int)((seg.rows + kChunk - 1) / kChunk);
     const bool first = seg.index == 0, last = seg.index == seg.count - 1;
     const long long cells = (long long)p.Dk * p.Dv, of_seq = ((long long)seg.seq * p.Hv + head) * cells, of_seg = ((long long)seg_no * p.Hv + head) * (DK * DV);
-    F32x4 M[NT][VT];
+    F32x4 M[NT];
     {
         const bool given = BACK ? last : first;
         const StateAt st = given ? StateAt{BACK ? (p.dlast ? p.dlast + of_seq : nullptr) : (p.s0 ? p.s0 + of_seq : nullptr), p.Dk, p.Dv, p.Dv}
                                  : StateAt{(BACK ? p.seg_rstate : p.seg_state) + of_seg, DK, DV, DV};
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int u = 0; u < VT; ++u) {
-                const int x = column_of(t, 4 * g), y = column_of(n0 + u, l);   // (and the three rows behind x)
-                if constexpr (KEYS) M[t][u] = st.four(y, x);
-                else M[t][u] = F32x4{st(x, y), st(x + 1, y), st(x + 2, y), st(x + 3, y)};
-            }
+        for (int t = 0; t < NT; ++t) {
+            const int x = column_of(t, 4 * g), y = column_of(wave, l);   // (and the three rows behind x)
+            if constexpr (KEYS) M[t] = st.four(y, x);
+            else M[t] = F32x4{st(x, y), st(x + 1, y), st(x + 2, y), st(x + 3, y)};
+        }
     }
     // the state behind the run's last chunk is wanted: the final one, or what the gates and ds0 need
     const bool to_the_end = MODE == RUN_OUT ? last && p.last : MODE == RUN_DK;
@@ -162,26 +161,24 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         const bool more = c + 1 < chunks;
 
         // Dk: this lane's columns of k, for the gates, on their way while the pairs are computed
-        V4 kr[MODE == RUN_DK ? 4 * VT : 1];
+        V4 kr[MODE == RUN_DK ? 4 : 1];
         if constexpr (MODE == RUN_DK) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 4; ++t) {
+                const int i = 16 * t + l;
+                const T* from = k + (row + rows - 1 - i) * p.stride_k + col0;
+                V4 x = {};
+                if (strip && i < rows) {
+                    if (wide_k) {
+                        if (col0 < p.Dk) x = *reinterpret_cast<const V4*>(from);
+                    } else {
 #pragma unroll
-                for (int u = 0; u < VT; ++u) {
-                    const int i = 16 * t + l, col = col0 + 4 * u;
-                    const T* from = k + (row + rows - 1 - i) * p.stride_k + col;
-                    V4 x = {};
-                    if (strip && i < rows) {
-                        if (wide_k) {
-                            if (col < p.Dk) x = *reinterpret_cast<const V4*>(from);
-                        } else {
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (col + r < p.Dk) x[r] = from[r];
-                        }
+                        for (int r = 0; r < 4; ++r)
+                            if (col0 + r < p.Dk) x[r] = from[r];
                     }
-                    kr[t * VT + u] = x;
                 }
+                kr[t] = x;
+            }
         }
 
         // ---- pairs, tile by tile, transposed: a lane has one i and four neighbouring j ----
@@ -229,12 +226,10 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 
         __builtin_amdgcn_s_setprio(2);
         // ---- the state: what it gives to the outputs, then the chunk's rows into it ----
-        F32x4 acc[4][VT];
-        frag_t<T> cf[2][VT];
+        F32x4 acc[4];
+        frag_t<T> cf[2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int u = 0; u < VT; ++u) acc[t][u] = F32x4{0, 0, 0, 0};
+        for (int t = 0; t < 4; ++t) acc[t] = F32x4{0, 0, 0, 0};
         if (strip) {
         // L::SUMS: how large the state is, for the bound of what goes through the chunk, from its first pieces: products of its columns with each other, of
         // which the diagonal is taken (four matrix instructions, which have time; fp32: sums of squares)
@@ -242,26 +237,18 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             constexpr int PIECES = L::SUMS ? P : 1;   // an output's rounded factor; the gates' sums take M as it is
-            frag_t<T> m[VT][P];
-#pragma unroll
-            for (int u = 0; u < VT; ++u) {
-                if constexpr (PIECES > 1) pieces_of<T>(joined(M[2 * s][u], M[2 * s + 1][u]), m[u]);
-                else m[u][0] = rounded<T>(joined(M[2 * s][u], M[2 * s + 1][u]));
-            }
+            frag_t<T> m[P];
+            if constexpr (PIECES > 1) pieces_of<T>(joined(M[2 * s], M[2 * s + 1]), m);
+            else m[0] = rounded<T>(joined(M[2 * s], M[2 * s + 1]));
             if constexpr (L::SUMS) {
-#pragma unroll
-                for (int u = 0; u < VT; ++u) {
-                    if constexpr (P > 1) square = mma(m[u][0], m[u][0], square);
-                    else square += M[2 * s][u] * M[2 * s][u] + M[2 * s + 1][u] * M[2 * s + 1][u];
-                }
+                if constexpr (P > 1) square = mma(m[0], m[0], square);
+                else square += M[2 * s] * M[2 * s] + M[2 * s + 1] * M[2 * s + 1];
             }
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const frag_t<T> af = T1::row_frag(ta, 16 * t + l, s, g);
 #pragma unroll
-                for (int n = PIECES - 1; n >= 0; --n)
-#pragma unroll
-                    for (int u = 0; u < VT; ++u) acc[t][u] = mma(m[u][n], af, acc[t][u]);
+                for (int n = PIECES - 1; n >= 0; --n) acc[t] = mma(m[n], af, acc[t]);
             }
         }
         if constexpr (L::SUMS) {
@@ -277,49 +264,36 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         for (int t = 0; t < 4; ++t) {
             const int i = 16 * t + l;
             const float f = f_out[i];
-#pragma unroll
-            for (int u = 0; u < VT; ++u) acc[t][u] *= f;
+            acc[t] *= f;
             if constexpr (L::SUMS) {   // q_i (Dk: k_i) with what came in
                 float x = 0.0f;
+                V4 with;
+                if constexpr (MODE == RUN_DQ) with = *reinterpret_cast<const V4*>(tq + T2::at(i, col0));
+                else with = kr[t];
 #pragma unroll
-                for (int u = 0; u < VT; ++u) {
-                    if constexpr (MODE == RUN_DQ) {
-                        const V4 q4 = *reinterpret_cast<const V4*>(tq + T2::at(i, col0 + 4 * u));
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x += (float)q4[r] * acc[t][u][r];
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x += (float)kr[t * VT + u][r] * acc[t][u][r];
-                    }
-                }
+                for (int r = 0; r < 4; ++r) x += (float)with[r] * acc[t][r];
                 x += __shfl_xor(x, 16);
                 x += __shfl_xor(x, 32);
                 if (g == 0) dots[64 * wave + i] = x;
             }
         }
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int u = 0; u < VT; ++u) cf[s][u] = T2::col_frag(tc, s, n0 + u, lane);
+        for (int s = 0; s < 2; ++s) cf[s] = T2::col_frag(tc, s, wave, lane);
         if (more || to_the_end) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int u = 0; u < VT; ++u) M[t][u] *= whole;
+            for (int t = 0; t < NT; ++t) M[t] *= whole;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const F32x4 w0 = *reinterpret_cast<const F32x4*>(w_in + 32 * s + 8 * g), w1 = *reinterpret_cast<const F32x4*>(w_in + 32 * s + 8 * g + 4);
-                frag_t<T> cp[VT][P];
-#pragma unroll
-                for (int u = 0; u < VT; ++u) pieces_of<T>(widened(cf[s][u]) * joined(w0, w1), cp[u]);
+                frag_t<T> cp[P];
+                pieces_of<T>(widened(cf[s]) * joined(w0, w1), cp);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const frag_t<T> bf = T1::col_frag(tb, s, t, lane);
 #pragma unroll
                     for (int n = P - 1; n >= 0; --n) {
                         if (n >= pieces) continue;
-#pragma unroll
-                        for (int u = 0; u < VT; ++u) M[t][u] = mma(bf, cp[u][n], M[t][u]);
+                        M[t] = mma(bf, cp[n], M[t]);
                     }
                 }
             }
@@ -338,8 +312,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
                 for (int t = 2 * s; t < 4; ++t) {
                     const frag_t<T> pf = TP::row_frag(tp, 16 * t + l, s, g);
-#pragma unroll
-                    for (int u = 0; u < VT; ++u) acc[t][u] = mma(cf[s][u], pf, acc[t][u]);
+                    acc[t] = mma(cf[s], pf, acc[t]);
                 }
         }
         const long long chunk = (long long)(seg.chunk0 + (BACK ? chunks - 1 - c : c)) * p.Hv + head;
@@ -391,11 +364,8 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 if (16 * t + i0 < rows) {
-#pragma unroll
-                    for (int u = 0; u < VT; ++u) {
-                        if (parts) store_four<float>(to_part + (long long)t * back * p.Hv * p.Dk + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
-                        else store_four<T>(to + (long long)t * back * so + 4 * u, acc[t][u], d2 - col0 - 4 * u, wide_out);
-                    }
+                    if (parts) store_four<float>(to_part + (long long)t * back * p.Hv * p.Dk, acc[t], d2 - col0, wide_out);
+                    else store_four<T>(to + (long long)t * back * so, acc[t], d2 - col0, wide_out);
                 }
             }
         }
@@ -410,12 +380,10 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int u = 0; u < VT; ++u)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int x = column_of(t, 4 * g + r), y = column_of(n0 + u, l);
-                    if (x < p.Dk && y < p.Dv) to[(long long)x * p.Dv + y] = M[t][u][r];
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int x = column_of(t, 4 * g + r), y = column_of(wave, l);
+                if (x < p.Dk && y < p.Dv) to[(long long)x * p.Dv + y] = M[t][r];
+            }
     }
     if constexpr (MODE == RUN_DK) {
         // the gradient of the state in front of the segment: ds0 of its sequence, and its product with that state for the gates
@@ -423,15 +391,13 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         const bool wide_ds0 = p.Dv % 4 == 0 && reinterpret_cast<uintptr_t>(p.ds0) % 16 == 0;
         float x = 0.0f;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+            const int vv = column_of(t, 4 * g), dd = column_of(wave, l);
+            const F32x4 y = st.four(dd, vv);
 #pragma unroll
-            for (int u = 0; u < VT; ++u) {
-                const int vv = column_of(t, 4 * g), dd = column_of(n0 + u, l);
-                const F32x4 y = st.four(dd, vv);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x += y[r] * M[t][u][r];
-                if (first && p.ds0 && dd < p.Dk && vv < p.Dv) store_four<float>(p.ds0 + of_seq + (long long)dd * p.Dv + vv, M[t][u], p.Dv - vv, wide_ds0);
-            }
+            for (int r = 0; r < 4; ++r) x += y[r] * M[t][r];
+            if (first && p.ds0 && dd < p.Dk && vv < p.Dv) store_four<float>(p.ds0 + of_seq + (long long)dd * p.Dv + vv, M[t], p.Dv - vv, wide_ds0);
+        }
         x = group_sum(x);
         x += __shfl_xor(x, 16);
         x += __shfl_xor(x, 32);

@@ -69,7 +69,7 @@ struct DiagLayout {
 };
 DiagLayout diag_layout(const deer_diagrec_config* c, bool grad) {
     DiagLayout l;
-    l.words = diagrec_words(c->dtype, c->gate, is_packed(c) ? 1 : c->N, c->T, c->D, grad, &l.chunks, &l.groups, &l.agg_words);
+    l.words = diagrec_words(c->dtype, is_packed(c) ? 1 : c->N, c->T, c->D, grad, &l.chunks, &l.groups, &l.agg_words);
     l.total = kAlign + align_up(l.words * 8);
     return l;
 }

@@ -193,7 +193,7 @@ struct DropoutParams {
 };
 
 constexpr int kDiagLanes = 512;   // of a workgroup of the recurrence
-size_t diagrec_words(int dtype, int gate, int N, long long T, int D, bool grad, int* chunks, int* groups, size_t* agg_words);
+size_t diagrec_words(int dtype, int N, long long T, int D, bool grad, int* chunks, int* groups, size_t* agg_words);
 hipError_t launch_diagrec(int dtype, bool grad, const DiagrecParams& p, hipStream_t stream);
 hipError_t launch_diagstep(int dtype, const DiagstepParams& p, hipStream_t stream);
 hipError_t launch_dropout(int dtype, const DropoutParams& p, hipStream_t stream);

@@ -418,9 +418,9 @@ def _zero_rest(bounds, *made):
 
 
 @functools.lru_cache(maxsize=512)
-def _diag_workspace(grad, dtype, gate, N, D, T, packed):
+def _diag_workspace(grad, dtype, N, D, T, packed):
     lib, size = load_library(), ctypes.c_size_t(0)
-    cfg = DiagrecConfig(dtype, gate, N, D, T, packed, 0, 0, 0, 0, 0.0, 0)
+    cfg = DiagrecConfig(dtype, DEER_GATE_FACTOR, N, D, T, packed, 0, 0, 0, 0, 0.0, 0)   # (of every gate)
     st = lib.deer_diagrec_workspace_bytes(ctypes.byref(cfg), grad, ctypes.byref(size))
     if st != DEER_OK:
         _raise(lib, st)
@@ -459,7 +459,7 @@ def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, leng
                         _row_stride(h, "out", lead), drop, seed)
     last = torch.empty((N, D), dtype=w, device=dev)
     h0p = _dense(h0, "h0", last.shape, w, dev)
-    size = _diag_workspace(0, dtype, kind, N, D, T, packed)
+    size = _diag_workspace(0, dtype, N, D, T, packed)
     ws = x.new_empty(size, dtype=torch.uint8)   # (torch's blocks are aligned to 512 bytes)
     st = lib.deer_diagrec_solve(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), last.data_ptr(), ws.data_ptr(), size,
                                 _stream_of(dev))
@@ -500,7 +500,7 @@ def diagrec_grad(gate, x, h, dh, h0=None, dlast=None, *, kind=DEER_GATE_FACTOR, 
     cfg = DiagrecConfig(dtype, kind, N, D, T, packed | rest, draw, stride_g, stride_x, stride_h, drop, seed)
     dh0 = torch.empty((N, D), dtype=w, device=dev)
     h0p, dlp = _dense(h0, "h0", dh0.shape, w, dev), _dense(dlast, "dlast", dh0.shape, w, dev)
-    size = _diag_workspace(1, dtype, kind, N, D, T, packed)
+    size = _diag_workspace(1, dtype, N, D, T, packed)
     ws = x.new_empty(size, dtype=torch.uint8)
     st = lib.deer_diagrec_grad(ctypes.byref(cfg), gate.data_ptr(), x.data_ptr(), h0p, bounds, h.data_ptr(), dh.data_ptr(), dlp, dgate.data_ptr(),
                                dx.data_ptr(), dh0.data_ptr(), ws.data_ptr(), size, _stream_of(dev))
