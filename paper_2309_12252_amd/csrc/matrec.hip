@@ -3,8 +3,8 @@
 //   o_i = scale (e^{c_i} S^T q_i + sum_{j <= i} e^{c_i - c_j} (q_i . k_j) v_j)
 //   S'  = e^{c_64} S + sum_j e^{c_64 - c_j} k_j v_j^T.
 // States are sums over many rows and stay in fp32 accumulators; v_j e^{c_64 - c_j} enters their update as three bf16 pieces, so a state is as exact as
-// fp32 sums make it.  The products of the output take S and the 64 x 64 factors rounded to bf16 once: an output
-// is rounded to bf16 itself.  What is NaN or infinite in a row reaches its chunk (products with factors that are zero) and what follows.
+// fp32 sums make it.  The products of the output take S and the 64 x 64 factors as two pieces (2^-16): an output is as exact as its
+// own rounding to bf16.  What is NaN or infinite in a row reaches its chunk (products with factors that are zero) and what follows.
 #include "matrec_run.h"
 
 namespace deer {

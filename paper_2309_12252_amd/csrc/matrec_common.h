@@ -40,22 +40,17 @@ __device__ __forceinline__ F32x4 mma(F32x8 a, F32x8 b, F32x4 c) {
 }
 
 // fp32 values as an operand: rounded, what that leaves rounded, and so on
-template <typename T>
-__device__ __forceinline__ void pieces_of(F32x8 x, frag_t<T> (&p)[Op<T>::PIECES]) {
+template <typename T, int N>
+__device__ __forceinline__ void pieces_of(F32x8 x, frag_t<T> (&p)[N]) {
     if constexpr (Op<T>::PIECES == 1) {
         p[0] = x;
     } else {
 #pragma unroll
-        for (int q = 0; q < Op<T>::PIECES; ++q) {
+        for (int q = 0; q < N; ++q) {
             p[q] = __builtin_convertvector(x, BF16x8);
-            x -= __builtin_convertvector(p[q], F32x8);
+            if (q + 1 < N) x -= __builtin_convertvector(p[q], F32x8);
         }
     }
-}
-template <typename T>
-__device__ __forceinline__ frag_t<T> rounded(F32x8 x) {
-    if constexpr (Op<T>::PIECES == 1) return x;
-    else return __builtin_convertvector(x, BF16x8);
 }
 __device__ __forceinline__ F32x8 widened(BF16x8 x) { return __builtin_convertvector(x, F32x8); }
 __device__ __forceinline__ F32x8 widened(F32x8 x) { return x; }

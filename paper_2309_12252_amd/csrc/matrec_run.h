@@ -25,8 +25,13 @@ template <typename T, int D1, int D2, int W, int MODE>
 struct RunLds {
     static constexpr bool FOUR = MODE == RUN_DQ;        // q, for the gates
     static constexpr bool SUMS = MODE == RUN_DQ || MODE == RUN_DK;
+    // Pieces in bf16.  READ: of the state in M^T a; all where the gates' sums take it as it is.  TAKE: of what rows add to the state.  PAIRS: of the pairs' factors.
+    // Outputs are as exact as one rounding makes them (all together 1.66e-3 off; with one piece each 2.35e-3, prompts of 8,192 rows 91 us
+    // instead of 95, 32,768 rows 91 and 95); gradients have a piece of the pairs, and of the state in dv, a rounding of the size of their own (a second piece of
+    // the state in dv: training step 518 -> 540 us; of the pairs: the tiles of dq leave no room for it on a CU with two workgroups).
+    static constexpr int P = Op<T>::PIECES, READ = SUMS ? P : MODE == RUN_OUT && P > 1 ? 2 : 1, TAKE = MODE == RUN_DV && P > 1 ? 2 : P, PAIRS = MODE == RUN_OUT && P > 1 ? 2 : 1;
     static constexpr size_t a = 0, b = Tile<T, D1>::bytes, c = b + Tile<T, D1>::bytes, q = c + Tile<T, D2>::bytes, pairs = q + (FOUR ? Tile<T, D2>::bytes : 0),
-                            rows = pairs + Tile<T, kChunk>::bytes,       // cum_hi, cum_lo, f, w, and the chunk's factor
+                            rows = pairs + PAIRS * Tile<T, kChunk>::bytes,       // cum_hi, cum_lo, f, w, and the chunk's factor
                             dots = rows + 4 * 5 * 64,                    // [W][64]
                             by_col = dots + (SUMS ? 4 * 64 * W : 0),   // [row tile][64]
                             by_row = by_col + (FOUR ? 4 * 256 : 0),      // [column tile][64]
@@ -114,8 +119,6 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     }
     // the state behind the run's last chunk is wanted: the final one, or what the gates and ds0 need
     const bool to_the_end = MODE == RUN_OUT ? last && p.last : MODE == RUN_DK;
-    // pieces that rows enter the state as: all where it is handed out or sums are taken of it as it is, two where it is rounded itself
-    const int pieces = to_the_end || L::SUMS || P == 1 ? P : 2;
 
     // ---- a chunk's rows into LDS ----
     const bool wide_a = wide_rows(ra, sa, d1), wide_b = wide_rows(rb, sb, d1), wide_c = wide_rows(rc, sc, d2), wide_q = wide_rows(q, p.stride_q, p.Dk), wide_k = wide_rows(k, p.stride_k, p.Dk);
@@ -140,9 +143,10 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         for (int n = wave; n < 5; n += W) load_floats(cum_hi + 64 * n, from, 64 * (!BACK || n < 2 || n > 3 ? n : 5 - n) + (BACK && n < 4 && i < rows ? rows - 1 - i : i));
     };
     // what is never written but taken in: pairs above the diagonal, sums of tiles there
-    if (wave == 0) {
-        *reinterpret_cast<V4*>(tp + TP::at(l, 16 + 4 * g)) = V4{};
-        *reinterpret_cast<V4*>(tp + TP::at(32 + l, 48 + 4 * g)) = V4{};
+    if (wave < L::PAIRS) {
+        T* to = tp + wave * (int)(TP::bytes / sizeof(T));
+        *reinterpret_cast<V4*>(to + TP::at(l, 16 + 4 * g)) = V4{};
+        *reinterpret_cast<V4*>(to + TP::at(32 + l, 48 + 4 * g)) = V4{};
     }
     if constexpr (L::FOUR) {
         if (threadIdx.x < 256) by_col[threadIdx.x] = by_row[threadIdx.x] = 0.0f;
@@ -194,6 +198,10 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = j0 + r <= i ? p.scale * x[r] * (BACK ? decay_between(hj[r], lj[r], hi_i, lo_i) : decay_between(hi_i, lo_i, hj[r], lj[r])) : 0.0f;
             store_four<T>(tp + TP::at(i, j0), x, 4, true);
+            if constexpr (L::PAIRS > 1) {
+                const F32x4 rest = x - __builtin_convertvector(__builtin_convertvector(x, V4), F32x4);
+                store_four<T>(tp + TP::bytes / sizeof(T) + TP::at(i, j0), rest, 4, true);
+            }
             if constexpr (MODE == RUN_DQ) {
                 // the gates' pairs: (dout_i . v_j) (q_i . k_j), summed over j along every row i, over the rows by groups of 16
                 F32x4 y = {0, 0, 0, 0};
@@ -236,10 +244,8 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         F32x4 square = {0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            constexpr int PIECES = L::SUMS ? P : 1;   // an output's rounded factor; the gates' sums take M as it is
-            frag_t<T> m[P];
-            if constexpr (PIECES > 1) pieces_of<T>(joined(M[2 * s], M[2 * s + 1]), m);
-            else m[0] = rounded<T>(joined(M[2 * s], M[2 * s + 1]));
+            frag_t<T> m[L::READ];
+            pieces_of<T>(joined(M[2 * s], M[2 * s + 1]), m);
             if constexpr (L::SUMS) {
                 if constexpr (P > 1) square = mma(m[0], m[0], square);
                 else square += M[2 * s] * M[2 * s] + M[2 * s + 1] * M[2 * s + 1];
@@ -248,7 +254,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
             for (int t = 0; t < 4; ++t) {
                 const frag_t<T> af = T1::row_frag(ta, 16 * t + l, s, g);
 #pragma unroll
-                for (int n = PIECES - 1; n >= 0; --n) acc[t] = mma(m[n], af, acc[t]);
+                for (int n = L::READ - 1; n >= 0; --n) acc[t] = mma(m[n], af, acc[t]);
             }
         }
         if constexpr (L::SUMS) {
@@ -285,16 +291,13 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const F32x4 w0 = *reinterpret_cast<const F32x4*>(w_in + 32 * s + 8 * g), w1 = *reinterpret_cast<const F32x4*>(w_in + 32 * s + 8 * g + 4);
-                frag_t<T> cp[P];
+                frag_t<T> cp[L::TAKE];
                 pieces_of<T>(widened(cf[s]) * joined(w0, w1), cp);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const frag_t<T> bf = T1::col_frag(tb, s, t, lane);
 #pragma unroll
-                    for (int n = P - 1; n >= 0; --n) {
-                        if (n >= pieces) continue;
-                        M[t] = mma(bf, cp[n], M[t]);
-                    }
+                    for (int n = L::TAKE - 1; n >= 0; --n) M[t] = mma(bf, cp[n], M[t]);
                 }
             }
         }
@@ -311,8 +314,8 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int t = 2 * s; t < 4; ++t) {
-                    const frag_t<T> pf = TP::row_frag(tp, 16 * t + l, s, g);
-                    acc[t] = mma(cf[s], pf, acc[t]);
+#pragma unroll
+                    for (int n = L::PAIRS - 1; n >= 0; --n) acc[t] = mma(cf[s], TP::row_frag(tp + n * (int)(TP::bytes / sizeof(T)), 16 * t + l, s, g), acc[t]);
                 }
         }
         const long long chunk = (long long)(seg.chunk0 + (BACK ? chunks - 1 - c : c)) * p.Hv + head;
