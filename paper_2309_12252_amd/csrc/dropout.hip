@@ -5,7 +5,8 @@ namespace deer {
 namespace {
 
 // A lane has eight rows of V channels: one block of random bits a channel.  Memory bound: x read once, y written once; the generator
-// takes about 20 vector cycles an element, which hides behind the memory: 268 MB of bf16 in 48 us (5.6 TB/s; a large copy 5.2).
+// takes about 20 vector cycles an element, which hides behind the memory: 268 MB of bf16, other arrays in every call, in 47 us (5.7 TB/s; a large copy 5.2); the same
+// arrays again, which the last-level cache has in part, in 41.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void dropout_kernel(const DropoutParams p) {
     using S = wide_t<T>;
@@ -51,7 +52,7 @@ hipError_t launch_type(const DropoutParams& p, hipStream_t stream) {
         return p.D % v == 0 && p.stride_in % v == 0 && p.stride_out % v == 0 && reinterpret_cast<uintptr_t>(p.x) % bytes == 0 &&
                reinterpret_cast<uintptr_t>(p.y) % bytes == 0;
     };
-    // 8 bytes a lane at least (rows of pairs in 16 bits are no faster than single elements): 64 Mi elements in bf16 41 us, one a lane 64; fp32 94, 107
+    // 8 bytes a lane at least (rows of pairs in 16 bits are no faster than single elements): the same 64 Mi elements again in bf16 41 us, one a lane 64; fp32 94, 107
     constexpr int V = sizeof(T) == 2 ? 4 : 2;
     return fits(V) ? launch_vec<T, V>(p, stream) : launch_vec<T, 1>(p, stream);
 }

@@ -127,14 +127,15 @@ const char* bad_config(const deer_matrec_config* c, bool step) {
 
 // How the rows are cut into segments, each a workgroup a head.  A sequence is cut only where whole sequences do not make enough workgroups
 // for 256 CUs, and then into as many as do.  Measured, 128 x 128 in bf16, forward + backward:
-//   whole from 256 N Hv on: 192 (3 x 64 heads of 4,096 rows) 379 + 1,095 us whole, 353 + 1,063 cut; 256 390 us whole, 402 cut (forward); 320 455 and 594
-//   512 workgroups at a time: training step of 4 x 4,096 rows and 16 heads with 256 of them 568 us, 384 544, 512 529, 768 538, 1,024 559
-//   up to 4 chunks whole: 64 heads of 256 rows 32 + 52 us whole, 39 + 82 cut; 4 heads of them 25 + 40 and 21 + 31; with no other least length: 4 heads
-//   of 2,048 rows 30 + 46 us, with segments of 4 chunks at least 40 + 59
-// What the sequences' lengths are is not known here; nearly all rows may be one sequence's.  Forward, 16 heads:
-//   packed, a segment has at most two 512ths of all rows: one sequence of 32,768 rows and 63 of one, 128 x 128, 378 us (cut by the number of sequences
-//   alone 2,830); one of 16,384 and 127 of 128 420 us (1,510); 64 of 1,024 325 us (340); 48 of 2,048 490 us either way
-//   a padded batch with lengths, at most 32 chunks: 16 to 4,096 rows, 128 x 128, all of them 399 us (whole 414), one long 241 us (324); 16 to 32,768, 64 x 64, one long 164 us (1,500)
+//   whole from 256 N Hv on: 192 (3 x 64 heads of 4,096 rows) 413 + 1,062 us whole, 363 + 1,022 cut; 256 428 us whole, 414 cut (forward); 320 472 and 626
+//   512 workgroups at a time: 4 x 4,096 rows and 16 heads with 256 of them 164 + 409 us, 384 144 + 402, 512 130 + 377, 768 153 + 399, 1,024 152 + 428
+//   up to 4 chunks whole: 64 heads of 256 rows 34 + 55 us whole, 39 + 82 cut; 4 heads of them 28 + 41 and 22 + 33; with no other least length: 4 heads
+//   of 2,048 rows 32 + 49 us, with segments of 4 chunks at least 43 + 62
+// What the sequences' lengths are is not known here; nearly all rows may be one sequence's.  Forward, 16 heads, into arrays that are handed in:
+//   packed, a segment has at most two 512ths of all rows: one sequence of 32,768 rows and 63 of one, 128 x 128, 403 us (cut by the number of sequences
+//   alone 3,097); one of 16,384 and 127 of 128 443 us (1,643); 64 of 1,024 352 us either way; 48 of 2,048 538 us (543)
+//   a padded batch with lengths, at most 32 chunks: 16 to 4,096 rows, 128 x 128, all of them 415 us (whole 444), one long 260 us (362); 16 to 32,768, 64 x 64, one
+//   long 171 us (1,609)
 struct MatLayout {
     long long chunks, max_segs;   // at most
     int per;

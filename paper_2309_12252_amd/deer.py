@@ -272,6 +272,7 @@ def linrec_solve_static(A, b, y0=None, reverse=False, out=None, status=None, str
 # and workspaces come from torch's allocator on that stream, a workspace for every call, so calls on several
 # streams, in several threads and captured into several graphs do not meet in one.  Rows that belong to no sequence (behind `lengths`,
 # outside `offsets`) or that a step passes over are zero in arrays that the call makes and left as they are in arrays that are handed in.
+# No call records anything for torch.autograd: results of inputs that require gradients do not, and the gradient is the call of that name.
 # ---------------------------------------------------------------------------------------------------------------------
 _DTYPES = {torch.float32: DEER_F32, torch.float64: DEER_F64, torch.bfloat16: DEER_BF16, torch.float16: DEER_F16}
 
@@ -444,7 +445,8 @@ def _diag_inputs(gate, x, kind, offsets, lengths):
 def diagrec_solve(gate, x, h0=None, *, kind=DEER_GATE_FACTOR, offsets=None, lengths=None, drop=0.0, seed=0, draw=0, out=None):
     """deer_diagrec_solve: h_t = a_t h_{t-1} + u_t for every channel (a, u from gate and x: see deer_gate).  gate, x [N, T, D] with
     optional int64 `lengths` [N], or packed [rows, D] with int64 `offsets` [N + 1]; rows may be slices of wider ones.  h0 [N, D] in
-    float32 (float64 with float64).  Rows of no sequence are zero in the result, left as they are in `out`.  Returns (h, state behind the last rows)."""
+    float32 (float64 with float64).  Rows of no sequence are zero in the result, left as they are in `out`.  Returns (h, state behind the last rows);
+    torch.autograd does not see the call, diagrec_grad is its gradient."""
     lib = load_library()
     dtype, kind, N, D, T, packed, bounds, lead = _diag_inputs(gate, x, kind, offsets, lengths)
     dev, w = x.device, torch.float64 if dtype == DEER_F64 else torch.float32
@@ -584,7 +586,8 @@ def _mat_config(q, k, v, gate, o, offsets, lengths, scale, lead=None):
 def matrec_solve(q, k, v, gate, s0=None, *, offsets=None, lengths=None, scale=None, out=None):
     """deer_matrec_solve: S_t = exp(gate_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t for every head of v.  q, k [N, T, Hk, Dk], v [N, T, Hv, Dv] in
     float32 or bfloat16, gate [N, T, Hv] float32, with optional int64 `lengths` [N]; or packed [rows, ...] with int64 `offsets` [N + 1].  s0 [N, Hv, Dk, Dv]
-    float32.  scale: Dk^-1/2 by default.  Rows of no sequence are zero in the result, left as they are in `out`.  Returns (o, states behind the last rows)."""
+    float32.  scale: Dk^-1/2 by default.  Rows of no sequence are zero in the result, left as they are in `out`.  Returns (o, states behind the last rows);
+    torch.autograd does not see the call, matrec_grad is its gradient."""
     lib = load_library()
     o = out if out is not None else torch.empty_like(v, memory_format=torch.contiguous_format) if isinstance(v, torch.Tensor) else None
     cfg, bounds, gp, _ = _mat_config(q, k, v, gate, o, offsets, lengths, scale)
@@ -662,7 +665,7 @@ def matrec_step(q, k, v, gate, state, *, slots=None, scale=None, out=None):
 @_on_stream
 def dropout(x, p, seed, draw=0, *, out=None):
     """deer_dropout: x [N, T, D] or packed [rows, D] with a share p dropped and the rest divided by 1 - p; the backward pass is the same
-    call on the gradient.  `out` may be x."""
+    call on the gradient (torch.autograd does not see it).  `out` may be x."""
     lib = load_library()
     dtype, lead, dev = _DTYPES.get(x.dtype), x.dim() - 1, x.device
     if dtype is None or lead not in (1, 2):
