@@ -326,8 +326,8 @@ deer_status deer_matrec_workspace_bytes(const deer_matrec_config* cfg, int32_t g
 
 /* d_q, d_k in [rows, Hk, Dk]   d_v in [rows, Hv, Dv]   d_gate in [rows, Hv] float32, the logarithms of the factors (dense)   d_s0 in [N, Hv, Dk, Dv]
  * float32 or NULL (zeros)   d_o out [rows, Hv, Dv]   d_last out [N, Hv, Dk, Dv] float32 or NULL.  By chunks of 64 rows on the matrix cores; states
- * in fp32 (bf16: sums of products in fp32, whose weights enter as three bf16 pieces; an output reads states and weights of pairs as two, 2^-16 of its terms beside
- * its own rounding), two calls with the same inputs return the same bits.
+ * in fp32 (bf16: sums of products in fp32, whose weights enter as three bf16 pieces; an output reads states and weights of pairs as two: it is off by its own rounding
+ * and 2^-16 of its terms), two calls with the same inputs return the same bits.
  * What is not finite in a row reaches the outputs of its chunk, also in front of it, and all that come later. */
 deer_status deer_matrec_solve(const deer_matrec_config* cfg, const void* d_q, const void* d_k, const void* d_v, const float* d_gate,
                               const float* d_s0, const int64_t* d_bounds, void* d_o, float* d_last, void* d_workspace,
@@ -335,7 +335,7 @@ deer_status deer_matrec_solve(const deer_matrec_config* cfg, const void* d_q, co
 
 /* Its gradient.  d_do in dL/do   d_dlast in [N, Hv, Dk, Dv] or NULL (zeros)   d_dq, d_dk, d_dv out   d_dgate out [rows, Hv] float32 or NULL   d_ds0 out
  * [N, Hv, Dk, Dv] float32 or NULL.  The states are computed again; gradients of shared heads are summed in a fixed order.  bf16: weights of pairs, and the state
- * in dv, are rounded to bf16 once in front of their products (2^-8 of their terms beside the gradients' own rounding). */
+ * in dv, enter as two pieces, as in the outputs. */
 deer_status deer_matrec_grad(const deer_matrec_config* cfg, const void* d_q, const void* d_k, const void* d_v, const float* d_gate,
                              const float* d_s0, const int64_t* d_bounds, const void* d_do, const float* d_dlast, void* d_dq, void* d_dk,
                              void* d_dv, float* d_dgate, float* d_ds0, void* d_workspace, size_t workspace_bytes, void* hip_stream);

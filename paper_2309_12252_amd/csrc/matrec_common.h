@@ -93,6 +93,52 @@ template <typename T, int C> struct Tile {
     }
 };
 
+// The weights of a chunk's pairs in LDS, as N pieces.  Whole rows; or (LOWER, bf16) the ten 16 x 16 tiles on and below the diagonal only, where whole rows would
+// leave no room for a second workgroup, the halves of a row turned so that 16 rows of eight terms meet in no bank (outputs of 4 x 4,096 rows and 16 heads of
+// 128 x 128: 83 us with whole rows, 88 with tiles).
+template <typename T, int N, bool LOWER> struct Pairs {
+    using Whole = Tile<T, kChunk>;
+    static_assert(!LOWER || sizeof(T) == 2, "halves of a row are 16 bytes");
+    static constexpr int PIECE = LOWER ? 10 * 256 : kChunk * Whole::LD;
+    static constexpr size_t bytes = sizeof(T) * N * PIECE;
+    // four neighbouring weights from column 4 g on of row l of tile (ti, tj)
+    static __device__ __forceinline__ int at(int ti, int tj, int l, int g) {
+        if constexpr (LOWER) return (ti * (ti + 1) / 2 + tj) * 256 + l * 16 + (((g >> 1) ^ (l >> 3)) << 3) + ((g & 1) << 2);
+        else return Whole::at(16 * ti + l, 16 * tj + 4 * g);
+    }
+    static __device__ __forceinline__ void store(T* p, int ti, int tj, int l, int g, F32x4 x) {
+        using V4 = T __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const V4 v = __builtin_convertvector(x, V4);
+            *reinterpret_cast<V4*>(p + n * PIECE + at(ti, tj, l, g)) = v;
+            if (n + 1 < N) x -= __builtin_convertvector(v, F32x4);
+        }
+    }
+    // piece n of rows 16 t + l, terms of the block of 32 columns s (t >= 2 s)
+    static __device__ __forceinline__ frag_t<T> row_frag(const T* p, int n, int t, int s, int l, int g) {
+        const T* from = p + n * PIECE;
+        if constexpr (LOWER) {
+            const int tj = 2 * s + (g >> 1);
+            const frag_t<T> f = *reinterpret_cast<const frag_t<T>*>(from + at(t, tj < t ? tj : t, l, 2 * (g & 1)));
+            return t > 2 * s || g < 2 ? f : frag_t<T>{};
+        } else {
+            return Whole::row_frag(from, 16 * t + l, s, g);
+        }
+    }
+    // what row_frag reads and nobody writes
+    static __device__ __forceinline__ void clear(T* p, int l, int g) {
+        using V4 = T __attribute__((ext_vector_type(4)));
+        if constexpr (!LOWER) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                *reinterpret_cast<V4*>(p + n * PIECE + Whole::at(l, 16 + 4 * g)) = V4{};
+                *reinterpret_cast<V4*>(p + n * PIECE + Whole::at(32 + l, 48 + 4 * g)) = V4{};
+            }
+        }
+    }
+};
+
 // ---- 64 rows of `cols` columns from memory into a tile; what is not there is zero ----
 // (2 x 8,192 rows, 16 heads of 128 x 128, forward + backward: bf16 124 + 505 us, element by element with rows an odd number apart 273 + 1,051;
 // fp32 389 + 1,225 and 554 + 1,822)

@@ -25,19 +25,19 @@ template <typename T, int D1, int D2, int W, int MODE>
 struct RunLds {
     static constexpr bool FOUR = MODE == RUN_DQ;        // q, for the gates
     static constexpr bool SUMS = MODE == RUN_DQ || MODE == RUN_DK;
-    // Pieces in bf16.  READ: of the state in M^T a; all where the gates' sums take it as it is.  TAKE: of what rows add to the state.  PAIRS: of the pairs' factors.
-    // Outputs are as exact as one rounding makes them (all together 1.66e-3 off; with one piece each 2.35e-3, prompts of 8,192 rows 91 us
-    // instead of 95, 32,768 rows 91 and 95); gradients have a piece of the pairs, and of the state in dv, a rounding of the size of their own (a second piece of
-    // the state in dv: training step 518 -> 540 us; of the pairs: the tiles of dq leave no room for it on a CU with two workgroups).
-    static constexpr int P = Op<T>::PIECES, READ = SUMS ? P : MODE == RUN_OUT && P > 1 ? 2 : 1, TAKE = MODE == RUN_DV && P > 1 ? 2 : P, PAIRS = MODE == RUN_OUT && P > 1 ? 2 : 1;
+    // Pieces in bf16.  READ: of the state in M^T a; all where the gates' sums take it as it is.  TAKE: of what rows add to the state; two where it is only read as
+    // two.  PAIRS: of the pairs' weights.  So results are as exact as their own rounding makes them: all together 1.66e-3 off, with one piece each 2.35e-3 (prompts
+    // of 8,192 rows 92 us instead of 96, training step of 4 x 4,096 rows 518 instead of 540).
+    static constexpr int P = Op<T>::PIECES, READ = SUMS || P == 1 ? P : 2, TAKE = MODE == RUN_DV && P > 1 ? 2 : P, PAIRS = P > 1 ? 2 : 1;
+    using Weights = Pairs<T, PAIRS, FOUR && P != 1>;
     static constexpr size_t a = 0, b = Tile<T, D1>::bytes, c = b + Tile<T, D1>::bytes, q = c + Tile<T, D2>::bytes, pairs = q + (FOUR ? Tile<T, D2>::bytes : 0),
-                            rows = pairs + PAIRS * Tile<T, kChunk>::bytes,       // cum_hi, cum_lo, f, w, and the chunk's factor
+                            rows = pairs + Weights::bytes,               // cum_hi, cum_lo, f, w, and the chunk's factor
                             dots = rows + 4 * 5 * 64,                    // [W][64]
                             by_col = dots + (SUMS ? 4 * 64 * W : 0),   // [row tile][64]
                             by_row = by_col + (FOUR ? 4 * 256 : 0),      // [column tile][64]
                             size = by_row + (FOUR ? 4 * 256 : 0),        // [W][16]: squares of the state's columns
                             total = size + (SUMS ? 4 * 16 * W : 0);
-    static_assert(total <= 160 * 1024, "a workgroup's tiles fit the CU's LDS");
+    static_assert(total <= 160 * 1024 / (sizeof(T) == 2 ? 2 : 1), "a workgroup's tiles fit the CU's LDS, in bf16 two workgroups'");
 };
 
 // a state of Dk x Dv in the caller's layout, or a whole tile DK x DV: element (k row, v column), and four neighbouring columns
@@ -70,7 +70,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
     using L = RunLds<T, D1, D2, W, MODE>;
     using T1 = Tile<T, D1>;
     using T2 = Tile<T, D2>;
-    using TP = Tile<T, kChunk>;
+    using TP = typename L::Weights;
     using V4 = T __attribute__((ext_vector_type(4)));
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int lane = lane0, g = lane >> 4, l = lane & 15;
@@ -143,11 +143,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
         for (int n = wave; n < 5; n += W) load_floats(cum_hi + 64 * n, from, 64 * (!BACK || n < 2 || n > 3 ? n : 5 - n) + (BACK && n < 4 && i < rows ? rows - 1 - i : i));
     };
     // what is never written but taken in: pairs above the diagonal, sums of tiles there
-    if (wave < L::PAIRS) {
-        T* to = tp + wave * (int)(TP::bytes / sizeof(T));
-        *reinterpret_cast<V4*>(to + TP::at(l, 16 + 4 * g)) = V4{};
-        *reinterpret_cast<V4*>(to + TP::at(32 + l, 48 + 4 * g)) = V4{};
-    }
+    if (wave == 0) TP::clear(tp, l, g);
     if constexpr (L::FOUR) {
         if (threadIdx.x < 256) by_col[threadIdx.x] = by_row[threadIdx.x] = 0.0f;
     }
@@ -197,11 +193,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
             const F32x4 hj = *reinterpret_cast<const F32x4*>(cum_hi + j0), lj = *reinterpret_cast<const F32x4*>(cum_lo + j0);
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = j0 + r <= i ? p.scale * x[r] * (BACK ? decay_between(hj[r], lj[r], hi_i, lo_i) : decay_between(hi_i, lo_i, hj[r], lj[r])) : 0.0f;
-            store_four<T>(tp + TP::at(i, j0), x, 4, true);
-            if constexpr (L::PAIRS > 1) {
-                const F32x4 rest = x - __builtin_convertvector(__builtin_convertvector(x, V4), F32x4);
-                store_four<T>(tp + TP::bytes / sizeof(T) + TP::at(i, j0), rest, 4, true);
-            }
+            TP::store(tp, ti, tj, l, g, x);
             if constexpr (MODE == RUN_DQ) {
                 // the gates' pairs: (dout_i . v_j) (q_i . k_j), summed over j along every row i, over the rows by groups of 16
                 F32x4 y = {0, 0, 0, 0};
@@ -226,7 +218,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
             }
         };
         // Products go in front of the other workgroup's wavefronts, which load or store, the state's in front of all: outputs of 4 x 4,096 rows
-        // and 16 heads of 128 x 128 86 -> 75 us, gradient 351 -> 305.
+        // and 16 heads of 128 x 128 99 -> 83 us, gradient 350 -> 321.
         __builtin_amdgcn_s_setprio(1);
         pair_tile(wave);
         if (W < 8) pair_tile(wave + W);
@@ -315,7 +307,7 @@ __device__ __forceinline__ void matrec_run(const MatrecParams& p, unsigned char*
 #pragma unroll
                 for (int t = 2 * s; t < 4; ++t) {
 #pragma unroll
-                    for (int n = L::PAIRS - 1; n >= 0; --n) acc[t] = mma(cf[s], TP::row_frag(tp + n * (int)(TP::bytes / sizeof(T)), 16 * t + l, s, g), acc[t]);
+                    for (int n = L::PAIRS - 1; n >= 0; --n) acc[t] = mma(cf[s], TP::row_frag(tp, n, t, s, l, g), acc[t]);
                 }
         }
         const long long chunk = (long long)(seg.chunk0 + (BACK ? chunks - 1 - c : c)) * p.Hv + head;

@@ -1,7 +1,6 @@
-"""Outputs of the matrix-state recurrence in bf16: what one rounding of the exact values leaves, whoever asks for the final states."""
+"""Outputs and gradients of the matrix-state recurrence in bf16: what one rounding of the exact values leaves, whoever asks for the final states."""
 import ctypes
 
-import numpy as np
 import pytest
 import torch
 
@@ -20,6 +19,18 @@ def test_outputs_are_rounded_once(T, Hk, Hv, Dk, Dv):
     want, absolute, _ = so.matrix(*(tm.host(d[n])[0] for n in ("q", "k", "v", "g")), tm.host(d["s0"]), [(0, T)], Dk ** -0.5)
     # every term has one factor in two pieces, off by at most half a step of the second: 2^-16; and sums as in fp32
     so.check("o", o, want["o"], (4 * (T + 128) * 2.0 ** -24 + 2.0 ** -16) * absolute["o"], "bf16")
+
+
+@pytest.mark.parametrize("N,T,Hk,Hv,Dk,Dv", [(1, 1, 1, 1, 128, 128), (1, 64, 1, 2, 64, 64), (1, 200, 2, 4, 128, 128), (1, 500, 1, 2, 128, 64), (2, 300, 1, 1, 33, 70),
+                                             (1, 700, 2, 2, 64, 128), (1, 1100, 64, 64, 16, 8)])
+def test_gradients_are_rounded_once(N, T, Hk, Hv, Dk, Dv):
+    d = tm.make("bf16", (N, T), N, Hk, Hv, Dk, Dv, T + 1)
+    got = deer.matrec_grad(d["q"], d["k"], d["v"], d["g"], d["do"], d["s0"], d["dlast"])
+    rows = lambda n: tm.host(d[n]).reshape((N * T,) + d[n].shape[2:])   # noqa: E731
+    want, absolute, _ = so.matrix(rows("q"), rows("k"), rows("v"), rows("g"), tm.host(d["s0"]), so.sequences(T, N), Dk ** -0.5, rows("do"), tm.host(d["dlast"]))
+    # as the outputs; the state in dv takes rows in as two pieces as well
+    for n, t, unit in (("dq", got[0], 2.0 ** -16), ("dk", got[1], 2.0 ** -16), ("dv", got[2], 2.0 ** -15)):
+        so.check(n, t, want[n], (4 * (T + 128) * 2.0 ** -24 + unit) * absolute[n], "bf16")
 
 
 @pytest.mark.parametrize("T", [100, 1000])
