@@ -10,44 +10,58 @@
 namespace deer {
 namespace {
 
+__device__ __forceinline__ int segments_of(const MatrecParams& p, long long rows) { return ((int)((rows + kChunk - 1) / kChunk) + p.plan.per - 1) / p.plan.per; }
+
 // One workgroup: sequences' chunks and segments are counted in their order (running sums over the sequences).  5 us for 7 sequences (launch and one
 // chain of loads), so it runs only where there are bounds: without, a segment follows from its number.
 __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p) {
     const MatPlan& plan = p.plan;
-    __shared__ int sums[16];
-    __shared__ int run_s, run_c;
+    __shared__ int sums[3][16], all_cut;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (tid == 0) run_s = run_c = 0;
-    __syncthreads();
-    auto scan = [&](int mine, int* run) {   // exclusive sum over the workgroup, `run` moved on
-        int v = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int o = __shfl_up(v, d);
-            v += lane >= d ? o : 0;
-        }
-        if (lane == 63) sums[wave] = v;
-        __syncthreads();
-        int before = *run;
-        for (int w = 0; w < wave; ++w) before += sums[w];
-        const int total = *run + [&] { int t = 0; for (int w = 0; w < 16; ++w) t += sums[w]; return t; }();
-        __syncthreads();
-        if (tid == 0) *run = total;
-        __syncthreads();
-        return before + v - mine;
-    };
+    if (tid == 0) all_cut = 0;
     // bounds that decrease would ask for more chunks than there is room for: then there are no segments at all
     bool bad = false;
-    if (p.rows.packed)
-        for (int n = tid; n < p.rows.N; n += 1024) bad = bad || clamp_row(p.rows.bounds[n + 1], p.rows.T) < clamp_row(p.rows.bounds[n], p.rows.T);
+    int cut = 0;
+    for (int n = tid; n < p.rows.N; n += 1024) {
+        if (p.rows.packed) bad = bad || clamp_row(p.rows.bounds[n + 1], p.rows.T) < clamp_row(p.rows.bounds[n], p.rows.T);
+        const int segs = segments_of(p, seq_length(p.rows, n));
+        cut += segs > 1 ? segs : 0;
+    }
     bad = __syncthreads_or(bad) != 0;
+    if (cut > 0 && !bad) atomicAdd(&all_cut, cut);
+    __syncthreads();
+    cut = all_cut;
+    int run[3] = {0, 0, 0};   // of the sequences in front: whole ones, chunks, segments of those that are cut
     for (int base = 0; base < p.rows.N; base += 1024) {
         const int n = base + tid;
         const long long len = n < p.rows.N && !bad ? seq_length(p.rows, n) : 0;
-        const int chunks = (int)((len + kChunk - 1) / kChunk), segs = (chunks + plan.per - 1) / plan.per;
-        const int s0 = scan(segs, &run_s), c0 = scan(chunks, &run_c);
+        const int chunks = (int)((len + kChunk - 1) / kChunk), segs = segments_of(p, len);
+        int mine[3] = {segs == 1 ? 1 : 0, chunks, segs > 1 ? segs : 0}, at[3];   // `at`: exclusive sums over the workgroup behind `run`, which moves on
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            int v = mine[k];
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int o = __shfl_up(v, d);
+                v += lane >= d ? o : 0;
+            }
+            at[k] = run[k] + v - mine[k];
+            if (lane == 63) sums[k][wave] = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int w = 0; w < 16; ++w) {
+                const int x = sums[k][w];
+                at[k] += w < wave ? x : 0;
+                run[k] += x;
+            }
+        __syncthreads();
         if (n < p.rows.N) {
-            plan.seq_seg[n] = s0;
+            const int first_seg = segs > 1 ? at[2] : cut + at[0];
+            plan.seq_seg[n] = first_seg;
+            plan.seq_count[n] = segs;
             const long long row = p.rows.packed ? clamp_row(p.rows.bounds[n], p.rows.T) : (long long)n * p.rows.T;
             for (int s = 0; s < segs; ++s) {
                 const long long first = (long long)s * plan.per * kChunk, most = (long long)plan.per * kChunk;
@@ -55,18 +69,17 @@ __global__ __launch_bounds__(1024) void matrec_plan_kernel(const MatrecParams p)
                 g.row0 = row + first;
                 g.rows = len - first < most ? len - first : most;
                 g.seq = n;
-                g.chunk0 = c0 + s * plan.per;
+                g.chunk0 = at[1] + s * plan.per;
                 g.index = s;
                 g.count = segs;
-                plan.segs[s0 + s] = g;
+                plan.segs[first_seg + s] = g;
             }
         }
     }
-    __syncthreads();
     if (tid == 0) {
-        plan.count[0] = run_s;
-        plan.count[1] = run_c;
-        plan.seq_seg[p.rows.N] = run_s;
+        plan.count[0] = run[0] + run[2];
+        plan.count[1] = run[1];
+        plan.count[2] = run[2];
     }
 }
 
@@ -164,7 +177,7 @@ __device__ __forceinline__ void states_of(const MatrecParams& p, unsigned char* 
     float* to = (REV ? p.seg_rstate : p.seg_state) + at * (DK * DV);   // (outside the head: zero in S too)
 #pragma unroll
     for (int t = 0; t < NT; ++t) *reinterpret_cast<F32x4*>(to + column_of(t, l) * DV + column_of(wave, 4 * g)) = S[t];
-    if (threadIdx.x == 0) p.seg_decay[(REV ? (long long)p.plan.max_segs * p.Hv : 0) + at] = (float)exp2(total);
+    if (threadIdx.x == 0) p.seg_decay[(REV ? (long long)p.plan.max_slots * p.Hv : 0) + at] = (float)exp2(total);
 }
 
 // blockIdx.y: 0 the states, 1 their gradients
@@ -186,7 +199,8 @@ __device__ __forceinline__ void join_cell(const MatrecParams& p, int n, int head
     const long long at = (((long long)n * p.Hv + head) * p.Dk + d) * p.Dv + v;
     const float* ends = REV ? p.dlast : p.s0;
     float* outs = REV ? p.ds0 : p.last;
-    const int first = first_segment(p, n), count = first_segment(p, n + 1) - first;
+    int count;
+    const int first = first_segment(p, n, count);
     if (count == 1) return;   // (a run takes what is given in front of a sequence from where it is given)
     float s = ends && inside ? ends[at] : 0.0f;
     if (count == 0) {
@@ -195,7 +209,7 @@ __device__ __forceinline__ void join_cell(const MatrecParams& p, int n, int head
     }
     if (!p.split) return;
     float* states = REV ? p.seg_rstate : p.seg_state;
-    const float* decay = p.seg_decay + (REV ? (long long)p.plan.max_segs * p.Hv : 0);
+    const float* decay = p.seg_decay + (REV ? (long long)p.plan.max_slots * p.Hv : 0);
     constexpr int K = 8;
     for (int i0 = 0; i0 < count; i0 += K) {
         float own[K], f[K];
@@ -298,7 +312,7 @@ template <typename T, int DK, int DV>
 hipError_t join_shape(const MatrecParams& p, bool both, hipStream_t stream) {
     hipError_t e = hipSuccess;
     const unsigned y = both ? 2 : 1;
-    if (p.split) e = launch_lds(matrec_states_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_segs * p.Hv), y), 4 * DV, StatesLds<T, DK, DV>::total, p, stream);
+    if (p.split) e = launch_lds(matrec_states_kernel<T, DK, DV>, dim3((unsigned)((long long)p.plan.max_slots * p.Hv), y), 4 * DV, StatesLds<T, DK, DV>::total, p, stream);
     const bool empty = p.rows.bounds || p.rows.T == 0;   // (there may be sequences without rows)
     if (e != hipSuccess || !(p.split || (empty && (p.last || p.ds0)))) return e;
     const long long blocks = (long long)p.rows.N * p.Hv * (DK * DV / 256);

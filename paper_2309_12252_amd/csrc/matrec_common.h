@@ -286,11 +286,12 @@ struct MatSegment {
     int index, count;    // place among the sequence's segments, and how many there are
 };
 struct MatPlan {
-    // with bounds: filled by the plan's kernel; without, every sequence is cut alike and a segment follows from its number
-    int* count;          // segments, and chunks
+    // With bounds: filled by the plan's kernel; without, every sequence is cut alike and a segment follows from its number.  Segments of sequences that are cut
+    // come first, in their order, then the sequences that are whole: only the former have states in memory.
+    int* count;          // segments, chunks, segments of sequences that are cut
     MatSegment* segs;    // [max_segs]
-    int* seq_seg;        // [N + 1]: a sequence's first segment
-    int max_segs, max_chunks, per;
+    int *seq_seg, *seq_count;   // [N]: a sequence's first segment, and how many it has
+    int max_segs, max_slots, max_chunks, per;
 };
 
 struct MatrecParams {
@@ -305,8 +306,8 @@ struct MatrecParams {
     float *last, *dgate, *ds0;
     bool split;                      // several segments a sequence: their states are joined through memory
     // states in memory between kernels are whole tiles of 64 or 128 rows and columns (the next from Dk and Dv), zero outside the head
-    float *seg_state, *seg_rstate;   // [max_segs][Hv][tile]: a segment's own part, then the state in front of it (gradient: behind it)
-    float *seg_decay;                // [2][max_segs][Hv]
+    float *seg_state, *seg_rstate;   // [max_slots][Hv][tile]: a segment's own part, then the state in front of it (gradient: behind it)
+    float *seg_decay;                // [2][max_slots][Hv]
     float *rows_of;                  // [chunks][Hv][kRowFloats]: a chunk's running gates and the factors that follow from them
     // gradient only
     float *part_q, *part_k;          // [rows][Hv][Dk]: dq and dk by heads of v, where several share one
@@ -345,18 +346,28 @@ __device__ __forceinline__ bool segment_of(const MatrecParams& p, int no, MatSeg
     return true;
 }
 // The segment of chunk number `chunk` of all sequences', and which of its chunks that is; false behind the last.  With bounds all lanes of a wavefront
-// take part: they look at 64 segments at a time, so that up to 4,096 segments are two loads one after another.
+// take part: they look at 64 segments at a time, among those of cut sequences and among whole ones at once, so that up to 4,096 of either are two loads
+// one after another.
 __device__ __forceinline__ bool segment_of_chunk(const MatrecParams& p, int chunk, MatSegment& s, int& place) {
     if (p.rows.bounds) {
         if (chunk >= p.plan.count[1]) return false;
-        int lo = 0, hi = p.plan.count[0];   // segment lo begins at the chunk or in front of it, segment hi behind it
-        while (hi - lo > 1) {
-            const int step = (hi - lo + 63) / 64, at = lo + (int)(threadIdx.x & 63) * step;
-            const bool front = at < hi && p.plan.segs[at < hi ? at : lo].chunk0 <= chunk;
-            lo += (__popcll(__ballot(front)) - 1) * step;
-            if (lo + step < hi) hi = lo + step;
+        // the last one that begins at the chunk or in front of it: in lo .. hi - 1, if there is one
+        int lo[2] = {0, p.plan.count[2]}, hi[2] = {p.plan.count[2], p.plan.count[0]};
+        do {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int step = (hi[k] - lo[k] + 63) / 64, at = lo[k] + (int)(threadIdx.x & 63) * step;
+                const int front = __popcll(__ballot(at < hi[k] && p.plan.segs[at < hi[k] ? at : 0].chunk0 <= chunk));
+                lo[k] += front > 0 ? (front - 1) * step : 0;
+                hi[k] = front == 0 ? lo[k] : lo[k] + step < hi[k] ? lo[k] + step : hi[k];
+            }
+        } while (hi[0] - lo[0] > 1 || hi[1] - lo[1] > 1);
+        const bool cut = hi[0] > lo[0], whole = hi[1] > lo[1];
+        s = p.plan.segs[cut ? lo[0] : lo[1]];
+        if (cut && whole) {
+            const MatSegment other = p.plan.segs[lo[1]];
+            if (other.chunk0 > s.chunk0) s = other;
         }
-        s = p.plan.segs[lo];
     } else {
         const int chunks = (int)((p.rows.T + 63) / 64);
         if (chunks == 0 || chunk / chunks >= p.rows.N) return false;
@@ -365,11 +376,14 @@ __device__ __forceinline__ bool segment_of_chunk(const MatrecParams& p, int chun
     place = chunk - s.chunk0;
     return true;
 }
-// first segment of sequence n (n = N: how many there are)
-__device__ __forceinline__ int first_segment(const MatrecParams& p, int n) {
-    if (p.rows.bounds) return p.plan.seq_seg[n];
-    const int chunks = (int)((p.rows.T + 63) / 64);
-    return n * ((chunks + p.plan.per - 1) / p.plan.per);
+// first segment of sequence n, and how many it has
+__device__ __forceinline__ int first_segment(const MatrecParams& p, int n, int& count) {
+    if (p.rows.bounds) {
+        count = p.plan.seq_count[n];
+        return p.plan.seq_seg[n];
+    }
+    count = ((int)((p.rows.T + 63) / 64) + p.plan.per - 1) / p.plan.per;
+    return n * count;
 }
 
 hipError_t launch_matrec_plan(const MatrecParams& p, const RestRows& rest, hipStream_t stream);   // segments, the gates of their chunks, rows of no sequence

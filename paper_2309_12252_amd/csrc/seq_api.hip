@@ -137,7 +137,7 @@ const char* bad_config(const deer_matrec_config* c, bool step) {
 //   a padded batch with lengths, at most 32 chunks: 16 to 4,096 rows, 128 x 128, all of them 415 us (whole 444), one long 260 us (362); 16 to 32,768, 64 x 64, one
 //   long 171 us (1,609)
 struct MatLayout {
-    long long chunks, max_segs;   // at most
+    long long chunks, max_segs, max_slots;   // at most
     int per;
     bool split;
     size_t off_segs, off_seq, off_state, off_rstate, off_decay, off_part_q, off_part_k, off_gate, off_read, off_put, off_size_in, off_size_out, off_rows, off_front, total;
@@ -160,6 +160,8 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad, bool bounds) {
     l.per = (int)per;
     l.split = per < longest;
     l.max_segs = is_packed(c) ? l.chunks / per + c->N : (longest + per - 1) / per * c->N;
+    // A packed sequence that is cut has r > 64 per rows, and fewer than r / (64 per) + 1 segments: in all fewer than twice as many as all rows make
+    l.max_slots = is_packed(c) && 2 * c->T / (kChunk * per) < l.max_segs ? 2 * c->T / (kChunk * per) : l.max_segs;
     const size_t states = (size_t)c->Hv * (c->Dk <= 64 ? 64 : 128) * (c->Dv <= 64 ? 64 : 128) * 4;
     size_t at = kAlign;
     auto take = [&](size_t bytes) {
@@ -168,12 +170,12 @@ MatLayout mat_layout(const deer_matrec_config* c, bool grad, bool bounds) {
         return here;
     };
     l.off_segs = take((size_t)l.max_segs * sizeof(MatSegment));
-    l.off_seq = take(((size_t)c->N + 1) * 4);
+    l.off_seq = take((size_t)c->N * 8);
     l.off_rows = take((size_t)l.chunks * c->Hv * kRowFloats * 4);
     if (l.split) {
-        l.off_state = take((size_t)l.max_segs * states);
-        if (grad) l.off_rstate = take((size_t)l.max_segs * states);
-        l.off_decay = take((size_t)l.max_segs * c->Hv * 8);
+        l.off_state = take((size_t)l.max_slots * states);
+        if (grad) l.off_rstate = take((size_t)l.max_slots * states);
+        l.off_decay = take((size_t)l.max_slots * c->Hv * 8);
     }
     if (grad) {
         const size_t rows = (size_t)c->T * (is_packed(c) ? 1 : c->N), by_head = (size_t)c->Hv * 4;
@@ -230,7 +232,9 @@ MatrecParams mat_params(const deer_matrec_config* c, const MatLayout& l, bool gr
     p.plan.count = reinterpret_cast<int*>(ws);
     p.plan.segs = reinterpret_cast<MatSegment*>(ws + l.off_segs);
     p.plan.seq_seg = reinterpret_cast<int*>(ws + l.off_seq);
+    p.plan.seq_count = p.plan.seq_seg + c->N;
     p.plan.max_segs = (int)l.max_segs;
+    p.plan.max_slots = (int)l.max_slots;
     p.plan.max_chunks = (int)l.chunks;
     p.plan.per = l.per;
     p.Hk = c->Hk;

@@ -174,12 +174,12 @@ def test_one_long_sequence_among_many_is_cut():
     assert room(N=16, T=32768) >= 16 * 16   # a padded batch, for all may be long
 
 
-# Matrix states: calls whose sequences are cut into segments of several chunks.  segs: for how many there is room
+# Matrix states: calls whose sequences are cut into segments of several chunks.  segs: for how many states there is room
 LONG = {
     "six": dict(H=64, Hk=64, Dk=8, Dv=8, lens=[3001], packed=0, segs=8),                     # 47 chunks on 512 workgroups: 8 segments of 6, the last of 5
     "twelve": dict(H=128, Hk=64, Dk=5, Dv=9, lens=[3001], packed=0, segs=4),                 # 12 chunks, the last 11
     "cap": dict(H=256, Hk=256, Dk=4, Dv=4, lens=[3001], packed=0, segs=2),                   # forward whole (room as with lengths), gradient 32 and 15 chunks
-    "packed": dict(H=64, Hk=32, Dk=8, Dv=4, lens=[1500, 3, 0, 2000, 64, 700], packed=1, segs=11),   # 67 + 6 chunks, by 14
+    "packed": dict(H=64, Hk=32, Dk=8, Dv=4, lens=[1500, 3, 0, 2000, 64, 700], packed=1, segs=9),    # 67 + 6 chunks, by 14: fewer than 4,267 / 32 / 14 segments of cut ones
     "padded": dict(H=128, Hk=128, Dk=4, Dv=4, lens=[2200, 100], packed=0, segs=4),           # 35 chunks: 32 and 3, in either direction
     "wide": dict(H=64, Hk=64, Dk=128, Dv=72, lens=[1100], packed=0, segs=6),                 # 18 chunks by 3
 }
@@ -212,3 +212,17 @@ def test_scale_is_a_number_of_32_bits(scale):
     assert lib.deer_matrec_workspace_bytes(ref, 0, ctypes.byref(size)) == deer.DEER_ERR_INVALID_ARG
     assert lib.deer_matrec_solve(ref, WORD, WORD, WORD, WORD, None, None, WORD, None, WORD, 1 << 40, None) == deer.DEER_ERR_INVALID_ARG
     assert lib.deer_matrec_step(ref, WORD, WORD, WORD, WORD, None, 4, WORD, WORD, None) == deer.DEER_ERR_INVALID_ARG
+
+
+def test_workspace_does_not_grow_with_sequences_that_are_not_cut():
+    """a packed batch of many short sequences: states for what may be cut only, beside 260 floats a chunk and head for the gates"""
+    lib, size = deer.load_library(), ctypes.c_size_t(0)
+    for N, T, H in ((4096, 1 << 18, 16), (16400, 8200, 64), (100000, 200000, 8)):
+        for grad in (0, 1):
+            cfg = mat(packed=1, N=N, T=T, Hk=H, Hv=H, Dk=128, Dv=128)
+            assert lib.deer_matrec_workspace_bytes(ctypes.byref(cfg), grad, ctypes.byref(size)) == deer.DEER_OK
+            chunks, tile = T // 64 + N, H * 128 * 128 * 4
+            # two 512ths of the rows a segment (gradient: 32 chunks at most), a state for each of twice as many as that makes; and small numbers by segment, chunk and row
+            per = min(max(2 * (T // 64) * H // 512, 1), 32 if grad else 1 << 30)
+            assert size.value <= chunks * H * 1200 + 4 * T * H + (1 + grad) * (2 * (T // 64) // per + 1) * tile + 100 * (chunks // per + N) * (1 + H // 8)
+            assert size.value < 0.1 * (1 + grad) * N * tile
