@@ -7,6 +7,7 @@ CPU fallback.
 """
 import ctypes
 import functools
+import operator
 import os
 
 import torch
@@ -331,6 +332,7 @@ def _int32(*sizes):
 
 def _draw_of(seed, draw):
     """number of the draw and seed as the library takes them, in 32 and 64 bits"""
+    seed, draw = operator.index(seed), operator.index(draw)
     if not 0 <= draw < 1 << 32:
         _refuse("draw: must lie in 0 .. 2^32 - 1")
     if not -(1 << 63) <= seed < 1 << 64:

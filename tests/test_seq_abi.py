@@ -226,3 +226,12 @@ def test_workspace_does_not_grow_with_sequences_that_are_not_cut():
             per = min(max(2 * (T // 64) * H // 512, 1), 32 if grad else 1 << 30)
             assert size.value <= chunks * H * 1200 + 4 * T * H + (1 + grad) * (2 * (T // 64) // per + 1) * tile + 100 * (chunks // per + N) * (1 + H // 8)
             assert size.value < 0.1 * (1 + grad) * N * tile
+
+
+def test_draws_and_seeds_of_numpy():
+    import numpy as np
+    for kind in (np.int64, np.uint64, np.int32, np.uint32):
+        assert deer._draw_of(kind(7), kind(9)) == (9, 7)
+    assert deer._draw_of(np.int64(-1), np.uint32(2 ** 32 - 1)) == (2 ** 32 - 1, 2 ** 64 - 1)
+    with pytest.raises(TypeError):
+        deer._draw_of(0.5, 0)
