@@ -158,3 +158,33 @@ def test_captured(poisoned):
         torch.cuda.synchronize()
         for a, b in zip(outs, step()):
             assert torch.equal(a, b) and bool((a[~alive] == 0).all())
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_captured_with_other_lengths_in_every_replay(poisoned, packed):
+    """bounds are device data: a replay takes what they hold then, and rows that belonged to a sequence before are zero again"""
+    lead, more, _ = layout(packed)
+    gate, x, dh = arrays(11, "bf16", lead, (64,), (64,), (64,))
+    q, k, v, do = arrays(12, "bf16", lead, (1, 32), (1, 32), (2, 16), (2, 16))
+    g = -arrays(13, "f32", lead, (2,))[0].abs()
+    bounds = more["offsets" if packed else "lengths"]
+
+    def step():
+        h, last = deer.diagrec_solve(gate, x, kind=1, **more)
+        o, state = deer.matrec_solve(q, k, v, g, **more)
+        return (h, last, o, state) + deer.diagrec_grad(gate, x, h, dh, kind=1, **more) + deer.matrec_grad(q, k, v, g, do, **more)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for now in ([[0, 0, 64, 65, 65, 123], [3, 9, 9, 9, 100, 101], [0] * 6] if packed else [[40, 40, 40, 40, 40], [0, 39, 2, 0, 1], [0] * 5]):
+        bounds.copy_(torch.tensor(now))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, step()):
+            assert bool(torch.isfinite(a).all()) and torch.equal(a, b)
