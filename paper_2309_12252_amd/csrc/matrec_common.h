@@ -140,8 +140,8 @@ template <typename T, int N, bool LOWER> struct Pairs {
 };
 
 // ---- 64 rows of `cols` columns from memory into a tile; what is not there is zero ----
-// (2 x 8,192 rows, 16 heads of 128 x 128, forward + backward: bf16 124 + 505 us, element by element with rows an odd number apart 273 + 1,051;
-// fp32 389 + 1,225 and 554 + 1,822)
+// (2 x 8,192 rows, 16 heads of 128 x 128, forward + backward: bf16 126 + 467 us, element by element with rows an odd number apart 277 + 1,061;
+// fp32 389 + 1,224 and 554 + 1,824)
 template <typename T>
 __device__ __forceinline__ bool wide_rows(const T* base, long long stride, int cols) {   // every row aligned to 16 bytes, a multiple of eight columns
     return cols % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(base) % 16 == 0 && stride < (1 << 20);

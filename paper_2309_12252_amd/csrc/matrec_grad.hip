@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void matrec_gates_kernel(const MatrecParams p)
 
 // dq and dk of shared heads: the heads of v that go with one, in their order; a workgroup has 16 rows of a chunk and up to 64 V columns.
 // Memory bound; the columns are spread over workgroups because a short call is one chain of loads after another (gradient of 128 rows, 8 heads of 128
-// for 16: 69 us with all columns of 16 rows in a workgroup, one a lane; 33 so).
+// for 16: 69 us with all columns of 16 rows in a workgroup, one a lane; 35 so).
 constexpr int kSharedRows = 16;
 template <typename T, int V>
 __global__ __launch_bounds__(256) void matrec_shared_kernel(const MatrecParams p) {

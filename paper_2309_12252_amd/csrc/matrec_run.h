@@ -7,11 +7,11 @@
 //   Dv   a, b, c = k, q, dout      M = R     backwards, the same
 // (S the state in front of a chunk, R the gradient of the state behind it.)  Wavefront w has 16 of c's columns: M's, as
 // results, which are operands of M^T a as they stand, and the outputs', transposed, a lane four neighbouring columns of a row.
-// What bounds it: 60 to 115 matrix instructions of 16 cycles and some 800 other vector instructions a wavefront and chunk of 128 columns, which a SIMD does one
+// What bounds it: 80 to 120 matrix instructions of 16 cycles and some 900 other vector instructions a wavefront and chunk of 128 columns, which a SIMD does one
 // after another, and 64 KiB of rows a chunk.  Two workgroups fill a CU and go on while the other one waits for its rows, which go straight to LDS: no
 // registers for them, so that 128 are enough (one workgroup a CU with its next rows in registers: gradient of 4 x 4,096 rows, 16 heads of
-// 128 x 128, 431 us; so 292 to 320).  Vector instructions take 58 % of a SIMD's cycles there and matrix instructions 24 %, and they do not overlap.  Outputs: 49 us for prompts of 8,192 rows
-// and 16 heads of 128 x 128, 54 for 1 x 32,768 rows and 8 heads of 128 x 64, 82 for 4 x 4,096 rows and 16 heads of 128 x 128.  fp32: the
+// 128 x 128, 431 us; so 309 to 345).  Vector instructions take 60 % of a SIMD's cycles there and matrix instructions 25 %, and they do not overlap.  Outputs: 49 us for prompts of 8,192 rows
+// and 16 heads of 128 x 128, 54 for 1 x 32,768 rows and 8 heads of 128 x 64, 83 for 4 x 4,096 rows and 16 heads of 128 x 128.  fp32: the
 // products are four-term instructions of 32 cycles and bound it.
 #pragma once
 #include "matrec_common.h"
@@ -27,7 +27,7 @@ struct RunLds {
     static constexpr bool SUMS = MODE == RUN_DQ || MODE == RUN_DK;
     // Pieces in bf16.  READ: of the state in M^T a; all where the gates' sums take it as it is.  TAKE: of what rows add to the state; two where it is only read as
     // two.  PAIRS: of the pairs' weights.  So results are as exact as their own rounding makes them: all together 1.66e-3 off, with one piece each 2.35e-3 (prompts
-    // of 8,192 rows 92 us instead of 96, training step of 4 x 4,096 rows 518 instead of 540).
+    // of 8,192 rows 92 us instead of 96, training step of 4 x 4,096 rows 4 % less).
     static constexpr int P = Op<T>::PIECES, READ = SUMS || P == 1 ? P : 2, TAKE = MODE == RUN_DV && P > 1 ? 2 : P, PAIRS = P > 1 ? 2 : 1;
     using Weights = Pairs<T, PAIRS, FOUR && P != 1>;
     static constexpr size_t a = 0, b = Tile<T, D1>::bytes, c = b + Tile<T, D1>::bytes, q = c + Tile<T, D2>::bytes, pairs = q + (FOUR ? Tile<T, D2>::bytes : 0),

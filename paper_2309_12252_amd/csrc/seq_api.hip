@@ -127,15 +127,15 @@ const char* bad_config(const deer_matrec_config* c, bool step) {
 
 // How the rows are cut into segments, each a workgroup a head.  A sequence is cut only where whole sequences do not make enough workgroups
 // for 256 CUs, and then into as many as do.  Measured, 128 x 128 in bf16, forward + backward:
-//   whole from 256 N Hv on: 192 (3 x 64 heads of 4,096 rows) 413 + 1,062 us whole, 363 + 1,022 cut; 256 428 us whole, 414 cut (forward); 320 472 and 626
-//   512 workgroups at a time: 4 x 4,096 rows and 16 heads with 256 of them 164 + 409 us, 384 144 + 402, 512 130 + 377, 768 153 + 399, 1,024 152 + 428
-//   up to 4 chunks whole: 64 heads of 256 rows 34 + 55 us whole, 39 + 82 cut; 4 heads of them 28 + 41 and 22 + 33; with no other least length: 4 heads
-//   of 2,048 rows 32 + 49 us, with segments of 4 chunks at least 43 + 62
+//   whole from 256 N Hv on: 192 (3 x 64 heads of 4,096 rows) 413 + 1,115 us whole, 362 + 1,067 cut; 256 425 us whole, 422 cut (forward); 320 472 and 622
+//   512 workgroups at a time: 4 x 4,096 rows and 16 heads with 256 of them 164 + 429 us, 384 144 + 418, 512 128 + 391, 768 153 + 407, 1,024 150 + 437
+//   up to 4 chunks whole: 64 heads of 256 rows 34 + 57 us whole, 39 + 84 cut; 4 heads of them 28 + 42 and 22 + 33; with no other least length: 4 heads
+//   of 2,048 rows 32 + 50 us, with segments of 4 chunks at least 44 + 63
 // What the sequences' lengths are is not known here; nearly all rows may be one sequence's.  Forward, 16 heads, into arrays that are handed in:
-//   packed, a segment has at most two 512ths of all rows: one sequence of 32,768 rows and 63 of one, 128 x 128, 403 us (cut by the number of sequences
-//   alone 3,097); one of 16,384 and 127 of 128 443 us (1,643); 64 of 1,024 352 us either way; 48 of 2,048 538 us (543)
-//   a padded batch with lengths, at most 32 chunks: 16 to 4,096 rows, 128 x 128, all of them 415 us (whole 444), one long 260 us (362); 16 to 32,768, 64 x 64, one
-//   long 171 us (1,609)
+//   packed, a segment has at most two 512ths of all rows: one sequence of 32,768 rows and 63 of one, 128 x 128, 367 us (cut by the number of sequences
+//   alone 3,080); one of 16,384 and 127 of 128 376 us (1,633); 64 of 1,024 342 us (349); 48 of 2,048 533 us (534)
+//   a padded batch with lengths, at most 32 chunks: 16 to 4,096 rows, 128 x 128, all of them 417 us (whole 443), one long 261 us (364); 16 to 32,768, 64 x 64, one
+//   long 170 us (1,600)
 struct MatLayout {
     long long chunks, max_segs, max_slots;   // at most
     int per;
