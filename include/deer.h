@@ -90,7 +90,10 @@ typedef enum { DEER_F32 = 0, DEER_F64 = 1, DEER_BF16 = 2, DEER_F16 = 3 } deer_dt
 typedef enum { DEER_GATE_FACTOR = 0, DEER_GATE_LOG = 1, DEER_GATE_SIGMOID = 2 } deer_gate;
 /* how rows lie (member `packed`), and what becomes of rows in the outputs that belong to no sequence: left as they are, or zeroed */
 typedef enum { DEER_ROWS_PADDED = 0, DEER_ROWS_PACKED = 1, DEER_REST_ZERO = 256 } deer_rows;
-typedef enum { DEER_ACT_TANH = 0, DEER_ACT_SOFTPLUS = 1 } deer_activation;
+/* TANH, SOFTPLUS: hidden layers of MLP fields.  NONE, SILU (v / (1 + exp(-v))): outputs of deer_shortconv_* and deer_groupnorm_*; NONE, SOFTPLUS: the steps of deer_selscan_* */
+typedef enum { DEER_ACT_TANH = 0, DEER_ACT_SOFTPLUS = 1, DEER_ACT_NONE = 2, DEER_ACT_SILU = 3 } deer_activation;
+/* what a group norm's mean and variance are taken over, beside the channels of a group: one row, or all rows of a sequence */
+typedef enum { DEER_SPAN_ROW = 0, DEER_SPAN_SEQUENCE = 1 } deer_span;
 
 typedef struct {
     int32_t cell;               /* deer_cell                                                             */
@@ -344,6 +347,109 @@ deer_status deer_matrec_grad(const deer_matrec_config* cfg, const void* d_q, con
  * deer_diagrec_step(). */
 deer_status deer_matrec_step(const deer_matrec_config* cfg, const void* d_q, const void* d_k, const void* d_v, const float* d_gate,
                              const int32_t* d_slots, int32_t n_slots, float* d_state, void* d_o, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Layers with selective states: a short causal convolution, the selective scan (a recurrence whose factors come from the inputs), and a group norm behind
+ * heads and channels.  Conventions as for the sequence operators above; weights, statistics, states and the gradients of all of these are dense
+ * arrays of the wider type.  Two calls with the same inputs return the same bits. */
+
+/* Causal convolution of every channel with W weights of its own: y_t = act(bias + sum_j w[.][j] x_{t - W + 1 + j}).  In front of a sequence lie its W - 1 initial
+ * rows s0 (the earliest first; zeros without them), and `last` holds the W - 1 rows in front of what would come next.  All four types. */
+typedef struct {
+    int32_t dtype;     /* deer_dtype: x, y and their gradients                                             */
+    int32_t act;       /* DEER_ACT_NONE or DEER_ACT_SILU                                                   */
+    int32_t N;         /* sequences (deer_shortconv_step: rows), >= 1                                      */
+    int32_t D;         /* channels, >= 1                                                                   */
+    int64_t T;         /* rows of a sequence, packed: of all of them; >= 0                                 */
+    int32_t packed;    /* 0 or 1, and DEER_REST_ZERO                                                       */
+    int32_t W;         /* weights of a channel, 1 .. 8                                                     */
+    int64_t stride_x;  /* rows of d_x and d_dx                                                             */
+    int64_t stride_y;  /* rows of d_y and d_dy                                                             */
+} deer_shortconv_config;
+
+/* Bytes of device workspace (256-byte aligned) that deer_shortconv_grad() needs; the other two need none. */
+deer_status deer_shortconv_workspace_bytes(const deer_shortconv_config* cfg, size_t* bytes);
+
+/* d_x in [rows, D]   d_w in [D, W]   d_bias in [D] or NULL (zeros)   d_s0 in [N, W - 1, D] or NULL (zeros)   d_y out [rows, D]   d_last out [N, W - 1, D] or NULL */
+deer_status deer_shortconv_solve(const deer_shortconv_config* cfg, const void* d_x, const void* d_w, const void* d_bias, const void* d_s0,
+                                 const int64_t* d_bounds, void* d_y, void* d_last, void* hip_stream);
+
+/* Its gradient.  d_dy in [rows, D]   d_dlast in [N, W - 1, D] or NULL (zeros)   d_dx out [rows, D]   d_dw out [D, W]   d_dbias out [D] or NULL   d_ds0 out [N, W - 1, D] or NULL */
+deer_status deer_shortconv_grad(const deer_shortconv_config* cfg, const void* d_x, const void* d_w, const void* d_bias, const void* d_s0,
+                                const int64_t* d_bounds, const void* d_dy, const void* d_dlast, void* d_dx, void* d_dw, void* d_dbias,
+                                void* d_ds0, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One token for each of N rows (T is not looked at, of packed DEER_REST_ZERO only): the rows in front in n_slots slots [n_slots, W - 1, D], moved on by one in
+ * place; slots as in deer_diagrec_step(). */
+deer_status deer_shortconv_step(const deer_shortconv_config* cfg, const void* d_x, const void* d_w, const void* d_bias, const int32_t* d_slots,
+                                int32_t n_slots, void* d_state, void* d_y, void* hip_stream);
+
+/* Selective scan: S states for every channel, h_t = exp(dt_t A) h_{t-1} + dt_t x_t B_t, y_t = <C_t, h_t> + skip x_t, times z_t / (1 + exp(-z_t)) where there is a z.
+ * dt_t = act(d_dt + dt_bias) is a channel's, B_t and C_t are a group's of D / G channels.  DEER_F32, DEER_BF16, DEER_F16. */
+typedef struct {
+    int32_t dtype;     /* deer_dtype: x, dt, B, C, z, y and their gradients                                */
+    int32_t dt_act;    /* DEER_ACT_NONE or DEER_ACT_SOFTPLUS                                               */
+    int32_t N;         /* sequences (deer_selscan_step: rows), >= 1                                        */
+    int32_t D;         /* channels, >= 1                                                                   */
+    int64_t T;         /* rows of a sequence, packed: of all of them; >= 0                                 */
+    int32_t packed;    /* 0 or 1, and DEER_REST_ZERO                                                       */
+    int32_t S;         /* states of a channel, 1 .. 64                                                     */
+    int32_t G;         /* groups of channels, a divisor of D; channel d has group d / (D / G)              */
+    int32_t reserved;  /* must be 0                                                                        */
+    int64_t stride_x, stride_dt, stride_B, stride_C, stride_z, stride_y;   /* rows (0: D, D, G S, G S, D, D); gradients lie like their arrays */
+} deer_selscan_config;
+
+/* Bytes of device workspace (256-byte aligned) that deer_selscan_solve() (grad = 0) or deer_selscan_grad() (grad = 1) needs: states between the segments
+ * that long sequences are cut into; for the gradient the states of every 16th row, and the sums for dB and dC over 256 / S' channels each (S' a quarter of S). */
+deer_status deer_selscan_workspace_bytes(const deer_selscan_config* cfg, int32_t grad, size_t* bytes);
+
+/* d_x, d_dt in [rows, D]   d_A in [D, S]   d_B, d_C in [rows, G, S]   d_skip in [D] or NULL (zeros)   d_z in [rows, D] or NULL   d_dt_bias in [D] or NULL (zeros)
+ * d_h0 in [N, D, S] or NULL (zeros)   d_y out [rows, D]   d_last out [N, D, S] or NULL */
+deer_status deer_selscan_solve(const deer_selscan_config* cfg, const void* d_x, const void* d_dt, const float* d_A, const void* d_B, const void* d_C,
+                               const float* d_skip, const void* d_z, const float* d_dt_bias, const float* d_h0, const int64_t* d_bounds,
+                               void* d_y, float* d_last, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradient.  d_dy in [rows, D]   d_dlast in [N, D, S] or NULL (zeros)   d_dx, d_ddt, d_dB, d_dC out, like d_x, d_dt, d_B, d_C   d_dA out [D, S]   d_dskip out [D] or NULL
+ * d_dz out like d_z (NULL without it)   d_dbias out [D] or NULL: of dt_bias   d_dh0 out [N, D, S] or NULL.  The states are computed again. */
+deer_status deer_selscan_grad(const deer_selscan_config* cfg, const void* d_x, const void* d_dt, const float* d_A, const void* d_B, const void* d_C,
+                              const float* d_skip, const void* d_z, const float* d_dt_bias, const float* d_h0, const int64_t* d_bounds,
+                              const void* d_dy, const float* d_dlast, void* d_dx, void* d_ddt, float* d_dA, void* d_dB, void* d_dC, float* d_dskip,
+                              void* d_dz, float* d_dbias, float* d_dh0, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One token for each of N rows (T is not looked at, of packed DEER_REST_ZERO only): states in n_slots slots [n_slots, D, S], float32, updated in place; slots as in
+ * deer_diagrec_step(). */
+deer_status deer_selscan_step(const deer_selscan_config* cfg, const void* d_x, const void* d_dt, const float* d_A, const void* d_B, const void* d_C,
+                              const float* d_skip, const void* d_z, const float* d_dt_bias, const int32_t* d_slots, int32_t n_slots, float* d_state,
+                              void* d_y, void* hip_stream);
+
+/* Group norm with an activation, channels last: y = act((x - mean) rstd w + bias), times z / (1 + exp(-z)) where there is a z.  mean and rstd = (variance + eps)^-1/2 are those of a group's
+ * D / G channels, in every row by itself (DEER_SPAN_ROW: heads of a recurrence) or over all rows of a sequence (DEER_SPAN_SEQUENCE).  All four types. */
+typedef struct {
+    int32_t dtype;     /* deer_dtype: x, z, y and their gradients                                          */
+    int32_t act;       /* DEER_ACT_NONE or DEER_ACT_SILU                                                   */
+    int32_t span;      /* deer_span                                                                        */
+    int32_t N;         /* sequences, >= 1                                                                  */
+    int32_t D;         /* channels, >= 1                                                                   */
+    int32_t G;         /* groups, a divisor of D                                                           */
+    int64_t T;         /* rows of a sequence, packed: of all of them; >= 0                                 */
+    int32_t packed;    /* 0 or 1, and DEER_REST_ZERO                                                       */
+    int32_t reserved;  /* must be 0                                                                        */
+    double eps;        /* >= 0, finite in 32 bits                                                          */
+    int64_t stride_x, stride_z, stride_y;   /* rows; dx lies like x, dz like z, dy like y                  */
+} deer_groupnorm_config;
+
+/* Bytes of device workspace (256-byte aligned) that deer_groupnorm_solve() (grad = 0) or deer_groupnorm_grad() (grad = 1) needs. */
+deer_status deer_groupnorm_workspace_bytes(const deer_groupnorm_config* cfg, int32_t grad, size_t* bytes);
+
+/* d_x in [rows, D]   d_w in [D] or NULL (ones)   d_bias in [D] or NULL (zeros)   d_z in [rows, D] or NULL   d_y out [rows, D]
+ * d_stats out: mean and rstd, [rows, G, 2] (DEER_SPAN_SEQUENCE: [N, G, 2], zeros for an empty sequence) */
+deer_status deer_groupnorm_solve(const deer_groupnorm_config* cfg, const void* d_x, const void* d_w, const void* d_bias, const void* d_z, const int64_t* d_bounds,
+                                 void* d_y, void* d_stats, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradient, at the statistics that deer_groupnorm_solve() gave.  d_dy in [rows, D]   d_dx out   d_dw, d_dbias out [D] or NULL   d_dz out (NULL without d_z) */
+deer_status deer_groupnorm_grad(const deer_groupnorm_config* cfg, const void* d_x, const void* d_w, const void* d_bias, const void* d_z, const int64_t* d_bounds,
+                                const void* d_stats, const void* d_dy, void* d_dx, void* d_dw, void* d_dbias, void* d_dz, void* d_workspace,
+                                size_t workspace_bytes, void* hip_stream);
 
 /* Switch per-kernel timing with HIP events on the context's stream on or off (off by default;
  * turning it on resets the accumulated numbers), and read the numbers accumulated so far. */

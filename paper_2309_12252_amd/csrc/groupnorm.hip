@@ -1,0 +1,590 @@
+// Group norm with an activation and a gate, channels last: forward and gradient, statistics over rows or over sequences.
+#include "layer_common.h"
+
+namespace deer {
+namespace {
+
+template <typename T, int V>
+__device__ __forceinline__ void load_wide(wide_t<T>* to, const void* from, long long at) {
+    const vec_t<T, V> v = *reinterpret_cast<const vec_t<T, V>*>(reinterpret_cast<const T*>(from) + at);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = (wide_t<T>)vec_at<T, V>(v, i);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_narrow(void* to, long long at, const wide_t<T>* from) {
+    vec_t<T, V> v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) vec_set<T, V>(v, i, (T)from[i]);
+    *reinterpret_cast<vec_t<T, V>*>(reinterpret_cast<T*>(to) + at) = v;
+}
+
+// ---- every row by itself ----
+// How a workgroup goes over rows and groups: L lanes (a power of two) have a group of a row, M vectors of V channels each; groups side by side, then rows
+struct RowShape {
+    int L, groups, rows, blocks;   // lanes of a group; groups and rows side by side in a workgroup; workgroups along the groups
+};
+inline RowShape row_shape(int D, int G, int V, int M) {
+    const int vecs = D / G / V;
+    RowShape s{1, 1, 1, 1};
+    while (s.L * M < vecs && s.L < 256) s.L *= 2;
+    const int units = 256 / s.L;
+    while (s.groups < units && s.groups < G) s.groups *= 2;
+    s.rows = units / s.groups;
+    s.blocks = (G + s.groups - 1) / s.groups;
+    return s;
+}
+
+// sum over the L lanes of a group, the same for all of them
+template <typename S>
+__device__ __forceinline__ S group_sum(S v, int L, S* shared) {
+    for (int d = 1; d < L && d < 64; d *= 2) v += __shfl_xor(v, d);
+    if (L <= 64) return v;
+    const int wave = threadIdx.x >> 6, first = wave / (L / 64) * (L / 64);
+    __syncthreads();
+    shared[wave] = v;
+    __syncthreads();
+    v = S(0);
+    for (int i = 0; i < L / 64; ++i) v += shared[first + i];
+    return v;
+}
+
+// whether row (of sequence n where they are padded) belongs to a sequence
+__device__ __forceinline__ bool row_counts(const SeqRows& s, long long row) {
+    if (!s.bounds) return true;
+    if (s.packed) return row >= clamp_row(s.bounds[0], s.T) && row < clamp_row(s.bounds[s.N], s.T);
+    return row % s.T < clamp_row(s.bounds[row / s.T], s.T);
+}
+
+// M vectors a lane are kept, so that a row is read once; with FEW false groups may have more than 256 M vectors, and are gone over again
+template <typename T, int V, int M, bool GRAD, bool FEW>
+__global__ __launch_bounds__(256) void rownorm_kernel(const NormParams p, const RowShape s, const RestRows rest, long long rows_each) {
+    using S = wide_t<T>;
+    __shared__ S shared[4];
+    clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
+    const int unit = threadIdx.x / s.L, l = threadIdx.x % s.L, n = p.D / p.G, vecs = n / V;
+    const int block = blockIdx.x % s.blocks, g = block * s.groups + unit % s.groups, ch0 = g * n;
+    const long long rows = p.rows.T * (p.rows.packed ? 1 : p.rows.N), lo = (long long)(blockIdx.x / s.blocks) * rows_each, hi = lo + rows_each < rows ? lo + rows_each : rows;
+    const bool has = g < p.G;
+    const S count = S(n);
+    const int turns = FEW ? 1 : (vecs + s.L * M - 1) / (s.L * M);
+    S* part = reinterpret_cast<S*>(p.part) + (long long)(blockIdx.x / s.blocks * s.rows + unit / s.groups) * 2 * p.D;
+    S dw[M][V], db[M][V];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int v = 0; v < V; ++v) dw[m][v] = db[m][v] = S(0);
+    auto at = [&](int turn, int m) { return (turn * M + m) * s.L + l; };   // a lane's vectors
+    if (GRAD && !FEW && has)
+        for (int i = l * V; i < n; i += s.L * V)
+#pragma unroll
+            for (int v = 0; v < V; ++v) part[ch0 + i + v] = part[p.D + ch0 + i + v] = S(0);
+    auto read = [&](const void* from, long long first, int turn, S(*to)[V]) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            if (at(turn, m) < vecs) load_wide<T, V>(to[m], from, first + ch0 + at(turn, m) * V);
+            else
+#pragma unroll
+                for (int v = 0; v < V; ++v) to[m][v] = S(0);
+        }
+    };
+    // (rounds of the same number for all lanes of the workgroup, for the sums over more than one wavefront)
+    for (long long round = lo; round < hi; round += s.rows) {
+        const long long row = round + unit / s.groups;
+        const bool on = has && row < hi && row_counts(p.rows, row);
+        S x[M][V], mean = S(0), rstd = S(0), sum = S(0), dy[M][V], z[M][V];
+        const S* stats = reinterpret_cast<const S*>(p.stats) + (row * p.G + g) * 2;
+        if (!GRAD) {
+            for (int t = 0; t < turns; ++t) {
+                if (on) read(p.x, row * p.stride_x, t, x);
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) sum += on ? x[m][v] : S(0);
+            }
+            mean = group_sum(sum, s.L, shared) / count;
+            sum = S(0);
+            for (int t = 0; t < turns; ++t) {
+                if (!FEW && on) read(p.x, row * p.stride_x, t, x);
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const S off = x[m][v] - mean;
+                        sum += on && at(t, m) < vecs ? off * off : S(0);
+                    }
+            }
+            rstd = S(1) / sqrt(group_sum(sum, s.L, shared) / count + (S)p.eps);
+            if (on && l == 0) {
+                const_cast<S*>(stats)[0] = mean;
+                const_cast<S*>(stats)[1] = rstd;
+            }
+        } else if (on) {
+            mean = stats[0];
+            rstd = stats[1];
+        }
+        S s1 = S(0), s2 = S(0);
+        // gradient: dy through gate and activation, and its sums
+        auto through = [&](int t, int m, int v, S& unit_x, S& dv, S& dz) {
+            const int c = ch0 + at(t, m) * V + v;
+            const S w = p.w ? reinterpret_cast<const S*>(p.w)[c] : S(1), b = p.bias ? reinterpret_cast<const S*>(p.bias)[c] : S(0);
+            unit_x = (x[m][v] - mean) * rstd;
+            const S pre = unit_x * w + b;
+            S f = pre, slope = S(1), gate = S(1), gslope = S(0);
+            if (p.act == DEER_ACT_SILU) silu_both<T>(pre, f, slope);
+            if (p.z) silu_both<T>(z[m][v], gate, gslope);
+            dv = dy[m][v] * gate * slope;
+            dz = dy[m][v] * f * gslope;
+            return dv * w;
+        };
+        if (GRAD)
+            for (int t = 0; t < turns; ++t) {
+                if (!on) break;
+                read(p.x, row * p.stride_x, t, x);
+                read(p.dy, row * p.stride_y, t, dy);
+                if (p.z) read(p.z, row * p.stride_z, t, z);
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    if (at(t, m) >= vecs) continue;
+                    S dz[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        S ux, dv;
+                        const S du = through(t, m, v, ux, dv, dz[v]);
+                        s1 += du;
+                        s2 += du * ux;
+                        if (FEW) {
+                            dw[m][v] += dv * ux;
+                            db[m][v] += dv;
+                            x[m][v] = ux;
+                            dy[m][v] = du;
+                        }
+                    }
+                    if (FEW && p.z) store_narrow<T, V>(p.dz, row * p.stride_z + ch0 + at(t, m) * V, dz);
+                }
+            }
+        if (GRAD) {
+            s1 = group_sum(s1, s.L, shared) / count;
+            s2 = group_sum(s2, s.L, shared) / count;
+        }
+        if (!on) continue;
+        for (int t = 0; t < turns; ++t) {
+            if (!FEW) {
+                read(p.x, row * p.stride_x, t, x);
+                if (GRAD) read(p.dy, row * p.stride_y, t, dy);
+            }
+            if (p.z && (!GRAD || !FEW)) read(p.z, row * p.stride_z, t, z);
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                if (at(t, m) >= vecs) continue;
+                S out[V], dz[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const int c = ch0 + at(t, m) * V + v;
+                    if (!GRAD) {
+                        const S w = p.w ? reinterpret_cast<const S*>(p.w)[c] : S(1), b = p.bias ? reinterpret_cast<const S*>(p.bias)[c] : S(0);
+                        const S pre = (x[m][v] - mean) * rstd * w + b;
+                        out[v] = p.act == DEER_ACT_SILU ? silu<T>(pre) : pre;
+                        if (p.z) out[v] *= silu<T>(z[m][v]);
+                    } else {
+                        S ux = x[m][v], du = dy[m][v], dv;
+                        if (!FEW) {
+                            du = through(t, m, v, ux, dv, dz[v]);
+                            // (a lane's own element of the workgroup's sums: read and written by no other)
+                            S* own = part + c;
+                            own[0] += dv * ux;
+                            own[p.D] += dv;
+                        }
+                        out[v] = rstd * ((du - s1) - ux * s2);
+                    }
+                }
+                store_narrow<T, V>(GRAD ? p.dx : p.y, row * (GRAD ? p.stride_x : p.stride_y) + ch0 + at(t, m) * V, out);
+                if (GRAD && !FEW && p.z) store_narrow<T, V>(p.dz, row * p.stride_z + ch0 + at(t, m) * V, dz);
+            }
+        }
+    }
+    if (GRAD && FEW && has) {
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+            if (at(0, m) < vecs)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    part[ch0 + at(0, m) * V + v] = dw[m][v];
+                    part[p.D + ch0 + at(0, m) * V + v] = db[m][v];
+                }
+    }
+}
+
+
+// ---- statistics over sequences ----
+// Pieces of sequences in tiles have places of their own: tile + sequence where rows are packed (one of the two grows from a piece to the next)
+__device__ __forceinline__ long long piece_at(const SeqRows& s, long long tile, int seq) { return s.packed ? tile + seq : tile; }
+
+struct SpanPlace {
+    int n, ch, phase;
+    long long tile, lo, hi;
+    bool on;
+};
+template <int V>
+__device__ __forceinline__ SpanPlace span_place(const NormParams& p, const Lanes& l, int rows) {
+    const long long tiles = (p.rows.T + rows - 1) / rows;
+    SpanPlace at;
+    at.tile = blockIdx.x / l.blocks;
+    at.n = p.rows.packed ? 0 : (int)(at.tile / tiles);
+    at.ch = ((int)(blockIdx.x % l.blocks) * l.lanes + (int)(threadIdx.x & (l.lanes - 1))) * V;
+    at.phase = threadIdx.x / l.lanes;
+    at.on = at.ch < p.D;
+    const long long in = (p.rows.packed ? at.tile : at.tile % tiles) * rows, base = (long long)at.n * p.rows.T;
+    at.lo = base + in;
+    at.hi = base + (in + rows < p.rows.T ? in + rows : p.rows.T);
+    return at;
+}
+
+// sums of two values a channel over the phases, in the order of the phases; those of phase 0 get them
+template <typename S, int V>
+__device__ __forceinline__ void phase_sums(S (*two)[V], const Lanes& l, S* shared) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < V; ++v) shared[threadIdx.x * V + v] = two[k][v];
+        __syncthreads();
+        if ((int)threadIdx.x < l.lanes) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                S sum = S(0);
+                for (int f = 0; f < l.phases; ++f) sum += shared[(f * l.lanes + threadIdx.x) * V + v];
+                two[k][v] = sum;
+            }
+        }
+    }
+}
+
+// Mean and sum of squares about it, of every channel in every piece: sums of the differences from the piece's first row.  That row is one of the summed, so
+// its distance from the mean is at most the root of the sum of squares: what cancels is at most a factor of the rows of a piece.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {
+    using S = wide_t<T>;
+    __shared__ S shared[256 * V];
+    clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
+    const SpanPlace at = span_place<V>(p, l, rows);
+    for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long, long long, long long r0, long long r1) {
+        S two[2][V], first[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) two[0][v] = two[1][v] = first[v] = S(0);
+        if (at.on) {
+            load_wide<T, V>(first, p.x, r0 * p.stride_x + at.ch);
+#pragma unroll 4
+            for (long long r = r0 + at.phase; r < r1; r += l.phases) {
+                S x[V];
+                load_wide<T, V>(x, p.x, r * p.stride_x + at.ch);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const S off = x[v] - first[v];
+                    two[0][v] += off;
+                    two[1][v] += off * off;
+                }
+            }
+        }
+        phase_sums<S, V>(two, l, shared);
+        if (!at.on || (int)threadIdx.x >= l.lanes) return;
+        S* to = reinterpret_cast<S*>(p.part) + piece_at(p.rows, at.tile, seq) * 2 * p.D + at.ch;
+        const S count = (S)(r1 - r0);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const S mean = two[0][v] / count, squares = two[1][v] - two[0][v] * mean;
+            to[v] = first[v] + mean;
+            to[p.D + v] = squares > S(0) || !(squares <= S(0)) ? squares : S(0);   // (NaN stays)
+        }
+    });
+}
+
+__device__ __forceinline__ double block_sum(double v, double* shared) {
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (shared[0] + shared[1]) + (shared[2] + shared[3]);
+}
+
+// Over a sequence's pieces and a group's channels, in 64 bits: mean and rstd (grad false), or the sums of dL/du and of dL/du u, u = (x - mean) rstd, over the number of
+// values (grad true)
+template <typename S>
+__global__ __launch_bounds__(256) void join_kernel(const NormParams p, int rows, bool grad) {
+    __shared__ double shared[4];
+    const int seq = blockIdx.x / p.G, g = blockIdx.x % p.G, n = p.D / p.G, ch0 = g * n;
+    const long long len = seq_length(p.rows, seq), tiles = (p.rows.T + rows - 1) / rows;
+    S* to = reinterpret_cast<S*>(grad ? p.joined : p.stats) + (long long)blockIdx.x * 2;
+    if (len == 0) {
+        if (threadIdx.x < 2) to[threadIdx.x] = S(0);
+        return;
+    }
+    const long long start = p.rows.packed ? seq_first(p.rows, seq) : 0, first = start / rows, last = (start + len - 1) / rows;
+    const long long items = (last - first + 1) * n;
+    const S* part = reinterpret_cast<const S*>(p.part);
+    auto piece = [&](long long i, double& count) {
+        const long long tile = first + i / n, lo = tile * rows > start ? tile * rows : start, hi = (tile + 1) * rows < start + len ? (tile + 1) * rows : start + len;
+        count = (double)(hi - lo);
+        return part + (p.rows.packed ? tile + seq : (long long)seq * tiles + tile) * 2 * p.D + ch0 + (int)(i % n);
+    };
+    double a = 0, b = 0;
+    if (grad) {
+#pragma unroll 4
+        for (long long i = threadIdx.x; i < items; i += 256) {
+            double count;
+            const S* at = piece(i, count);
+            const double w = p.w ? (double)reinterpret_cast<const S*>(p.w)[ch0 + (int)(i % n)] : 1.0;
+            a += w * (double)at[0];
+            b += w * (double)at[p.D];
+        }
+    } else {
+#pragma unroll 4
+        for (long long i = threadIdx.x; i < items; i += 256) {
+            double count;
+            const S* at = piece(i, count);
+            a += count * (double)at[0];
+        }
+    }
+    const double all = (double)len * n;
+    a = block_sum(a, shared) / all;
+    if (!grad) {
+#pragma unroll 4
+        for (long long i = threadIdx.x; i < items; i += 256) {
+            double count;
+            const S* at = piece(i, count);
+            const double off = (double)at[0] - a;
+            b += (double)at[p.D] + count * off * off;
+        }
+    }
+    b = block_sum(b, shared) / all;
+    if (threadIdx.x == 0) {
+        to[0] = (S)a;
+        to[1] = grad ? (S)b : (S)(1.0 / sqrt(b + p.eps));
+    }
+}
+
+// One element: y of x, or du = dL/du and what else its gradient needs
+template <typename T>
+struct Through {
+    using S = wide_t<T>;
+    S u, dv, dz;
+    __device__ __forceinline__ S operator()(const NormParams& p, S x, S z, S dy, S mean, S rstd, S w, S b) {
+        u = (x - mean) * rstd;
+        const S pre = u * w + b;
+        S f = pre, slope = S(1), gate = S(1), gslope = S(0);
+        if (p.act == DEER_ACT_SILU) silu_both<T>(pre, f, slope);
+        if (p.z) silu_both<T>(z, gate, gslope);
+        dv = dy * gate * slope;
+        dz = dy * f * gslope;
+        return dv * w;
+    }
+};
+
+// STEP 0: y; 1: the sums of dL/dv and dL/dv u of every channel in every piece, v = w u + bias, and in every tile; 2: dx and dz
+template <typename T, int V, int STEP>
+__global__ __launch_bounds__(256) void span_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {
+    using S = wide_t<T>;
+    __shared__ S shared[STEP == 1 ? 256 * V : 1];
+    if (STEP == 1) clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
+    const SpanPlace at = span_place<V>(p, l, rows);
+    S w[V], b[V], total[2][V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        w[v] = p.w && at.on ? reinterpret_cast<const S*>(p.w)[at.ch + v] : S(1);
+        b[v] = p.bias && at.on ? reinterpret_cast<const S*>(p.bias)[at.ch + v] : S(0);
+        total[0][v] = total[1][v] = S(0);
+    }
+    const int g = (at.on ? at.ch : 0) / (p.D / p.G);
+    for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long, long long, long long r0, long long r1) {
+        const S* stats = reinterpret_cast<const S*>(p.stats) + ((long long)seq * p.G + g) * 2;
+        const S mean = stats[0], rstd = stats[1];
+        S s1 = S(0), s2 = S(0), two[2][V];
+        if (STEP == 2) {
+            s1 = reinterpret_cast<const S*>(p.joined)[((long long)seq * p.G + g) * 2];
+            s2 = reinterpret_cast<const S*>(p.joined)[((long long)seq * p.G + g) * 2 + 1];
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) two[0][v] = two[1][v] = S(0);
+        if (at.on)
+#pragma unroll 2
+            for (long long r = r0 + at.phase; r < r1; r += l.phases) {
+                S x[V], z[V], dy[V], out[V], dz[V];
+                load_wide<T, V>(x, p.x, r * p.stride_x + at.ch);
+                if (p.z) load_wide<T, V>(z, p.z, r * p.stride_z + at.ch);
+                if (STEP != 0) load_wide<T, V>(dy, p.dy, r * p.stride_y + at.ch);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if (STEP == 0) {
+                        const S pre = (x[v] - mean) * rstd * w[v] + b[v];
+                        out[v] = p.act == DEER_ACT_SILU ? silu<T>(pre) : pre;
+                        if (p.z) out[v] *= silu<T>(z[v]);
+                    } else {
+                        Through<T> th;
+                        const S du = th(p, x[v], p.z ? z[v] : S(0), dy[v], mean, rstd, w[v], b[v]);
+                        if (STEP == 1) {
+                            two[0][v] += th.dv;
+                            two[1][v] += th.dv * th.u;
+                        }
+                        out[v] = rstd * ((du - s1) - th.u * s2);
+                        dz[v] = th.dz;
+                    }
+                }
+                if (STEP == 0) store_narrow<T, V>(p.y, r * p.stride_y + at.ch, out);
+                if (STEP == 2) {
+                    store_narrow<T, V>(p.dx, r * p.stride_x + at.ch, out);
+                    if (p.z) store_narrow<T, V>(p.dz, r * p.stride_z + at.ch, dz);
+                }
+            }
+        if (STEP != 1) return;
+        phase_sums<S, V>(two, l, shared);
+        if (!at.on || (int)threadIdx.x >= l.lanes) return;
+        S* to = reinterpret_cast<S*>(p.part) + piece_at(p.rows, at.tile, seq) * 2 * p.D + at.ch;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            to[v] = two[0][v];
+            to[p.D + v] = two[1][v];
+            total[0][v] += two[0][v];
+            total[1][v] += two[1][v];
+        }
+    });
+    if (STEP != 1 || !at.on || (int)threadIdx.x >= l.lanes) return;
+    S* to = reinterpret_cast<S*>(p.sums) + at.tile * 2 * p.D + at.ch;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        to[v] = total[1][v];
+        to[p.D + v] = total[0][v];
+    }
+}
+
+int span_rows(int D, int V) { return 32 * lanes_for(D, V).phases; }
+template <typename T> constexpr int vector() { return sizeof(T) == 2 ? 8 : sizeof(T) == 4 ? 4 : 2; }
+
+RestRows rest_of(const NormParams& p, bool grad, long long bytes) {
+    RestRows rest{};
+    if (!p.zero_rest) return rest;
+    auto add = [&](void* first, long long stride, long long width) { rest.array[rest.count++] = RestArray{first, stride * bytes, width * bytes}; };
+    if (grad) {
+        add(p.dx, p.stride_x, p.D);
+        if (p.z) add(p.dz, p.stride_z, p.D);
+        return rest;
+    }
+    add(p.y, p.stride_y, p.D);
+    if (p.span == DEER_SPAN_ROW) {
+        const long long wide = bytes == 8 ? 16 : 8;   // mean and rstd
+        rest.array[rest.count++] = RestArray{p.stats, wide * p.G, wide * p.G};
+    }
+    return rest;
+}
+
+template <typename T, int V>
+hipError_t launch_sequences(bool grad, const NormParams& p, hipStream_t stream) {
+    using S = wide_t<T>;
+    const Lanes l = lanes_for(p.D, V);
+    const int rows = span_rows(p.D, V);
+    const long long tiles = (p.rows.T + rows - 1) / rows * (p.rows.packed ? 1 : p.rows.N);
+    const dim3 grid((unsigned)(tiles * l.blocks)), block(256);
+    const RestRows rest = rest_of(p, grad, sizeof(T));
+    if (tiles) {
+        if (grad) hipLaunchKernelGGL((span_kernel<T, V, 1>), grid, block, 0, stream, p, l, rows, rest);
+        else hipLaunchKernelGGL((moments_kernel<T, V>), grid, block, 0, stream, p, l, rows, rest);
+    }
+    hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)((long long)p.rows.N * p.G)), block, 0, stream, p, rows, grad);
+    if (tiles) {
+        if (grad) hipLaunchKernelGGL((span_kernel<T, V, 2>), grid, block, 0, stream, p, l, rows, rest);
+        else hipLaunchKernelGGL((span_kernel<T, V, 0>), grid, block, 0, stream, p, l, rows, rest);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !grad || (!p.dw && !p.dbias)) return e;
+    SumInto into{};
+    into.each = p.D;
+    into.to[0] = p.dw;
+    into.to[1] = p.dbias;
+    into.stride[0] = into.stride[1] = 1;
+    return launch_sum_tiles(sizeof(S) == 8, p.sums, tiles, 2 * p.D, into, stream);
+}
+
+// rows of a workgroup, and how many workgroups along the rows: about 2,048 in all
+struct RowCut {
+    long long each, blocks;
+};
+RowCut row_cut(const RowShape& s, long long rows) {
+    long long rounds = (rows + s.rows - 1) / s.rows, want = 2048 / s.blocks < 1 ? 1 : 2048 / s.blocks;
+    const long long per = (rounds + want - 1) / want;
+    RowCut c;
+    c.each = (per < 1 ? 1 : per) * s.rows;
+    c.blocks = (rows + c.each - 1) / c.each;
+    return c;
+}
+int vectors_each(int vecs) { return vecs <= 64 ? 1 : 4; }
+
+template <typename T, int V, int M, bool GRAD, bool FEW>
+hipError_t launch_rows_as(const NormParams& p, hipStream_t stream) {
+    using S = wide_t<T>;
+    const RowShape s = row_shape(p.D, p.G, V, M);
+    const RowCut c = row_cut(s, p.rows.T * (p.rows.packed ? 1 : p.rows.N));
+    if (c.blocks) hipLaunchKernelGGL((rownorm_kernel<T, V, M, GRAD, FEW>), dim3((unsigned)(c.blocks * s.blocks)), dim3(256), 0, stream, p, s, rest_of(p, GRAD, sizeof(T)), c.each);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !GRAD || (!p.dw && !p.dbias)) return e;
+    SumInto into{};
+    into.each = p.D;
+    into.to[0] = p.dw;
+    into.to[1] = p.dbias;
+    into.stride[0] = into.stride[1] = 1;
+    return launch_sum_tiles(sizeof(S) == 8, p.part, c.blocks * s.rows, 2 * p.D, into, stream);
+}
+template <typename T, int V, bool GRAD>
+hipError_t launch_rows(const NormParams& p, hipStream_t stream) {
+    const int vecs = p.D / p.G / V;
+    if (vecs > 1024) return launch_rows_as<T, V, 4, GRAD, false>(p, stream);
+    return vectors_each(vecs) == 1 ? launch_rows_as<T, V, 1, GRAD, true>(p, stream) : launch_rows_as<T, V, 4, GRAD, true>(p, stream);
+}
+
+template <typename T>
+hipError_t launch_type(bool grad, const NormParams& p, hipStream_t stream) {
+    constexpr int V = vector<T>();
+    const size_t e = sizeof(T);
+    bool vec = p.D / p.G % V == 0 && rows_fit(p.x, p.stride_x, V, e) && (!p.z || rows_fit(p.z, p.stride_z, V, e));
+    if (grad) vec = vec && rows_fit(p.dy, p.stride_y, V, e) && rows_fit(p.dx, p.stride_x, V, e) && (!p.z || rows_fit(p.dz, p.stride_z, V, e));
+    else vec = vec && rows_fit(p.y, p.stride_y, V, e);
+    if (p.span == DEER_SPAN_SEQUENCE) return vec ? launch_sequences<T, V>(grad, p, stream) : launch_sequences<T, 1>(grad, p, stream);
+    if (vec) return grad ? launch_rows<T, V, true>(p, stream) : launch_rows<T, V, false>(p, stream);
+    return grad ? launch_rows<T, 1, true>(p, stream) : launch_rows<T, 1, false>(p, stream);
+}
+
+}  // namespace
+
+// (which vectors a call can use follows from its pointers: room for either)
+NormLayout norm_layout(int dtype, int D, int G, int span, long long T, int N, bool packed, bool grad) {
+    const int wide = dtype == DEER_F32 ? vector<float>() : dtype == DEER_F64 ? vector<double>() : vector<BF16>();
+    NormLayout l{};
+    for (const int V : {1, wide}) {
+        long long part = 0, sums = 0;
+        if (span == DEER_SPAN_SEQUENCE) {
+            const int rows = span_rows(D, V);
+            const long long tiles = (T + rows - 1) / rows * (packed ? 1 : N);
+            part = (tiles + (packed ? N : 0)) * 2 * D;
+            if (grad) sums = tiles * 2 * D;
+            if (tiles * lanes_for(D, V).blocks > l.tiles) l.tiles = tiles * lanes_for(D, V).blocks;
+        } else if (D / G % V == 0) {
+            const int vecs = D / G / V;
+            const RowShape s = row_shape(D, G, V, vecs > 1024 ? 4 : vectors_each(vecs));
+            const RowCut c = row_cut(s, T * (packed ? 1 : N));
+            if (grad) part = c.blocks * s.rows * 2 * D;
+            if (c.blocks * s.blocks > l.tiles) l.tiles = c.blocks * s.blocks;
+        }
+        if (part > l.part) l.part = part;
+        if (sums > l.sums) l.sums = sums;
+    }
+    if (span == DEER_SPAN_SEQUENCE && grad) l.joined = (long long)N * G * 2;
+    return l;
+}
+
+hipError_t launch_groupnorm(int dtype, bool grad, const NormParams& p, hipStream_t stream) {
+    switch (dtype) {
+        case DEER_F32: return launch_type<float>(grad, p, stream);
+        case DEER_F64: return launch_type<double>(grad, p, stream);
+        case DEER_BF16: return launch_type<BF16>(grad, p, stream);
+        default: return launch_type<F16>(grad, p, stream);
+    }
+}
+
+}  // namespace deer

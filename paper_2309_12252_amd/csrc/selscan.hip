@@ -1,0 +1,279 @@
+// Selective scan: h_t = exp(dt_t A) h_{t-1} + dt_t x_t B_t, y_t = <C_t, h_t> + skip x_t, gated.  Outputs, states between segments, single tokens.
+#include "selscan_common.h"
+
+namespace deer {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+enum { kOutputs, kEnds, kMarks };   // y and the final states; the states behind segments; these and the states in front of every kMarkRows rows
+
+// sum over the Q lanes of a channel
+template <int Q>
+__device__ __forceinline__ float over_lanes(float v) {
+#pragma unroll
+    for (int d = 64 / Q; d < 64; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+template <typename T, int Q, int WHAT>
+__global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, const RestRows rest) {
+    using Sh = ScanShape<Q>;
+    constexpr int R = Sh::kRows, CW = Sh::kChannels, kAcross = CW / 4, kStep = 256 / kAcross;
+    __shared__ Float2 sx[R][CW];       // dt and dt x; y in the place of the latter
+    __shared__ Float4 bc[R][2][Q];
+    if (WHAT == kOutputs) clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
+    const ScanPlace place = scan_place<Q>(p);
+    long long lo = place.lo;
+    const long long hi = place.hi;
+    if (lo >= hi) return;
+    const int lane = threadIdx.x & 63, q = lane / Sh::kWave, c = (threadIdx.x >> 6) * Sh::kWave + lane % Sh::kWave;
+    const ScanLane l{place.ch0 + c, 4 * q, c < place.channels};
+    float A2[4], h[4], sum_dt = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) A2[k] = l.on && l.k0 + k < p.S ? p.A[(long long)l.ch * p.S + l.k0 + k] * kLog2e : 0.0f;
+    ScanSeq seq;
+    if (WHAT == kEnds) {   // only what comes behind the last beginning of a sequence counts
+        seq.at(p.rows, place, hi - 1);
+        const bool reset = seq.start >= lo;
+        if (threadIdx.x == 0) p.resets[place.seg] = reset;
+        if (reset) lo = seq.start;
+        if (reset) load_states(h, p.h0, seq.n, l, p.D, p.S);
+        else
+#pragma unroll
+            for (int k = 0; k < 4; ++k) h[k] = 0.0f;
+    } else {
+        seq.at(p.rows, place, lo);
+        if (seq.start == lo) load_states(h, p.h0, seq.n, l, p.D, p.S);
+        else if (WHAT == kOutputs) load_states(h, p.carry, place.seg, l, p.D, 4 * Q);
+        else
+#pragma unroll
+            for (int k = 0; k < 4; ++k) h[k] = 0.0f;
+    }
+    bool reset = seq.start == lo;
+    // a lane's items: four channels of rows kStep apart
+    const int c4 = (threadIdx.x % kAcross) * 4, row0 = threadIdx.x / kAcross, count = place.channels - c4;
+    float bias[4], skip[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bias[i] = p.bias && i < count ? p.bias[place.ch0 + c4 + i] : 0.0f;
+        skip[i] = WHAT == kOutputs && p.skip && i < count ? p.skip[place.ch0 + c4 + i] : 0.0f;
+    }
+    for (long long r = lo; r < hi; r += R) {
+        const int rows = hi - r < R ? (int)(hi - r) : R;
+        float x[Sh::kItems][4], z[Sh::kItems][4];
+#pragma unroll
+        for (int j = 0; j < Sh::kItems; ++j) {
+            const int i = row0 + j * kStep;
+            if (i >= rows) continue;
+            float dt[4];
+            const long long at = place.ch0 + c4;
+            load4<T>(x[j], p.x, (r + i) * p.stride_x + at, count, p.vec);
+            load4<T>(dt, p.dt, (r + i) * p.stride_dt + at, count, p.vec);
+            if (WHAT == kOutputs && p.z) load4<T>(z[j], p.z, (r + i) * p.stride_z + at, count, p.vec);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float raw = dt[v] + bias[v], step = p.softplus ? softplus(raw) : raw;
+                sx[i][c4 + v] = Float2{step, step * x[j][v]};
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < Sh::kQuads; ++j) {
+            const int e = threadIdx.x + j * 256, qq = e % Q, i = e / Q % R, which = e / Q / R;
+            if (which > 1 || i >= rows) continue;
+            float v[4];
+            if (which == 0) load4<T>(v, p.B, (r + i) * p.stride_B + (long long)place.g * p.S + 4 * qq, p.S - 4 * qq, p.vec_bc);
+            else load4<T>(v, p.C, (r + i) * p.stride_C + (long long)place.g * p.S + 4 * qq, p.S - 4 * qq, p.vec_bc);
+            bc[i][which][qq] = Float4{v[0], v[1], v[2], v[3]};
+        }
+        __syncthreads();
+        for (int i = 0; i < rows; ++i) {
+            if (r + i == seq.end) {
+                if (WHAT == kOutputs) store_states(p.last, seq.n, l, p.D, p.S, h);
+                seq.next(p.rows, r + i);
+                load_states(h, p.h0, seq.n, l, p.D, p.S);
+                reset = true;
+            }
+            if (WHAT == kMarks && (r + i - lo) % kMarkRows == 0) {
+                const long long mark = place.seg * p.marks_each + (r + i - lo) / kMarkRows;
+                store_states(p.marks, mark, l, p.D, 4 * Q, h);
+                if (q == 0 && l.on) p.mark_steps[mark * p.D + l.ch] = sum_dt;
+            }
+            const Float2 s = sx[i][c];
+            const Float4 b = bc[i][0][q];
+            sum_dt += s.x;
+            float y = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) h[k] = __builtin_amdgcn_exp2f(s.x * A2[k]) * h[k] + s.y * b[k];
+            if (WHAT != kOutputs) continue;
+            const Float4 cc = bc[i][1][q];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y += cc[k] * h[k];
+            y = over_lanes<Q>(y);
+            if (q == 0) sx[i][c].y = y;
+        }
+        __syncthreads();
+        if (WHAT == kOutputs)
+#pragma unroll
+            for (int j = 0; j < Sh::kItems; ++j) {
+                const int i = row0 + j * kStep;
+                if (i >= rows || count <= 0) continue;
+                float y[4];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    y[v] = sx[i][c4 + v].y + skip[v] * x[j][v];
+                    if (p.z) y[v] *= fast_silu(z[j][v]);
+                }
+                store4<T>(p.y, (r + i) * p.stride_y + place.ch0 + c4, y, count, p.vec);
+            }
+    }
+    if (WHAT == kOutputs) {
+        if (hi == seq.end) store_states(p.last, seq.n, l, p.D, p.S, h);
+        return;
+    }
+    if (p.segs == 1) return;
+    if (WHAT == kMarks && threadIdx.x == 0) p.resets[place.seg] = reset;
+    store_states(p.local, place.seg, l, p.D, 4 * Q, h);
+    if (q == 0 && l.on) p.steps[place.seg * p.D + l.ch] = sum_dt;
+}
+
+// The states in front of the segments, one after the other, and the final states of sequences without rows
+__global__ __launch_bounds__(256) void selscan_join_kernel(const SelscanParams p, int SP) {
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, cells = (long long)p.D * SP, seqs = p.rows.packed ? 1 : p.rows.N;
+    if (at >= cells * seqs) return;
+    const long long n = at / cells, cell = at % cells;
+    const int ch = (int)(cell / SP), k = (int)(cell % SP);
+    const float A2 = k < p.S ? p.A[(long long)ch * p.S + k] * kLog2e : 0.0f;
+    float h = 0.0f;
+    for (long long s = n * p.segs; s < (n + 1) * p.segs - 1; ++s) {
+        const float local = p.local[s * cells + cell], decay = __builtin_amdgcn_exp2f(A2 * p.steps[s * p.D + ch]);
+        h = p.resets[s] ? local : local + decay * h;
+        p.carry[(s + 1) * cells + cell] = h;
+    }
+}
+
+__global__ __launch_bounds__(256) void selscan_empty_kernel(const SeqRows rows, long long cells, const float* from, float* to) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows.N * cells; i += (long long)gridDim.x * 256)
+        if (seq_length(rows, (int)(i / cells)) == 0) to[i] = from ? from[i] : 0.0f;
+}
+
+// One token for every row.  A lane has four states of a channel, the lanes of a channel lie side by side: states are read and written as they lie.
+template <typename T, int Q>
+__global__ __launch_bounds__(256) void selscan_step_kernel(const SelstepParams p) {
+    constexpr int CW = 256 / Q;
+    const int per = (p.D + CW - 1) / CW, n = blockIdx.x / per, ch = (blockIdx.x % per) * CW + (int)threadIdx.x / Q, q = threadIdx.x % Q;
+    int slot = n;
+    bool twice = false;
+    if (p.rows.slots) {
+        slot = p.rows.slots[n];
+        for (int m = threadIdx.x; m < n; m += 256) twice = twice || p.rows.slots[m] == slot;
+    }
+    const bool in = ch < p.D && slot >= 0 && slot < p.rows.n_slots;
+    const ScanLane l{ch, 4 * q, in};
+    float h[4], a[4], b[4], c[4], x = 0.0f, dt = 0.0f, z = 0.0f, skip = 0.0f;
+    load_states(h, p.state, slot, l, p.D, p.S);
+    load_states(a, p.A, 0, l, p.D, p.S);
+    if (in) {
+        const int g = ch / (p.D / p.G);
+        load4<T>(b, p.B, (long long)n * p.stride_B + (long long)g * p.S + 4 * q, p.S - 4 * q, false);
+        load4<T>(c, p.C, (long long)n * p.stride_C + (long long)g * p.S + 4 * q, p.S - 4 * q, false);
+        x = as_float(reinterpret_cast<const T*>(p.x)[(long long)n * p.stride_x + ch]);
+        dt = as_float(reinterpret_cast<const T*>(p.dt)[(long long)n * p.stride_dt + ch]) + (p.bias ? p.bias[ch] : 0.0f);
+        if (p.z) z = as_float(reinterpret_cast<const T*>(p.z)[(long long)n * p.stride_z + ch]);
+        if (p.skip) skip = p.skip[ch];
+    }
+    twice = p.rows.slots ? __syncthreads_or(twice) != 0 : false;
+    T* y = reinterpret_cast<T*>(p.y) + (long long)n * p.stride_y + ch;
+    if (ch < p.D && (!in || twice)) {
+        if (p.rows.zero_rest && q == 0) *y = (T)0.0f;
+        return;
+    }
+    if (p.softplus) dt = softplus(dt);
+    float sum = 0.0f;
+    if (in) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            h[k] = __builtin_amdgcn_exp2f(dt * a[k] * kLog2e) * h[k] + dt * x * b[k];
+            sum += c[k] * h[k];
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < Q; d *= 2) sum += __shfl_xor(sum, d);
+    if (!in) return;
+    store_states(p.state, slot, l, p.D, p.S, h);
+    if (q != 0) return;
+    sum += skip * x;
+    *y = (T)(p.z ? sum * fast_silu(z) : sum);
+}
+
+template <typename T, int Q>
+hipError_t launch_lanes(const SelscanParams& p, bool marks, hipStream_t stream) {
+    const long long seqs = p.rows.packed ? 1 : p.rows.N, segs = seqs * p.segs, cells = (long long)p.D * 4 * Q;
+    const dim3 grid((unsigned)(segs * p.G * p.blocks)), block(256);
+    RestRows rest{};
+    if (p.zero_rest) rest.array[rest.count++] = RestArray{p.y, p.stride_y * (long long)sizeof(T), p.D * (long long)sizeof(T)};
+    if (marks) {
+        if (p.rows.T) hipLaunchKernelGGL((selscan_kernel<T, Q, kMarks>), grid, block, 0, stream, p, rest);
+    } else if (p.segs > 1) {
+        hipLaunchKernelGGL((selscan_kernel<T, Q, kEnds>), grid, block, 0, stream, p, rest);
+    }
+    if (p.segs > 1) hipLaunchKernelGGL(selscan_join_kernel, dim3((unsigned)((cells * seqs + 255) / 256)), block, 0, stream, p, 4 * Q);
+    if (marks) return hipGetLastError();
+    if (p.rows.T) hipLaunchKernelGGL((selscan_kernel<T, Q, kOutputs>), grid, block, 0, stream, p, rest);
+    if (p.last && (p.rows.bounds || !p.rows.T)) {
+        const long long all = (long long)p.rows.N * p.D * p.S / 1024;
+        hipLaunchKernelGGL(selscan_empty_kernel, dim3((unsigned)(all < 1 ? 1 : all > 1024 ? 1024 : all)), block, 0, stream, p.rows, (long long)p.D * p.S, p.h0, p.last);
+    }
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_type(const SelscanParams& p, bool marks, hipStream_t stream) {
+    switch (scan_lanes(p.S)) {
+        case 1: return launch_lanes<T, 1>(p, marks, stream);
+        case 2: return launch_lanes<T, 2>(p, marks, stream);
+        case 4: return launch_lanes<T, 4>(p, marks, stream);
+        case 8: return launch_lanes<T, 8>(p, marks, stream);
+        default: return launch_lanes<T, 16>(p, marks, stream);
+    }
+}
+hipError_t launch_any(int dtype, const SelscanParams& p, bool marks, hipStream_t stream) {
+    switch (dtype) {
+        case DEER_F32: return launch_type<float>(p, marks, stream);
+        case DEER_BF16: return launch_type<BF16>(p, marks, stream);
+        default: return launch_type<F16>(p, marks, stream);
+    }
+}
+template <typename T, int Q>
+hipError_t launch_step_lanes(const SelstepParams& p, hipStream_t stream) {
+    constexpr int CW = 256 / Q;
+    hipLaunchKernelGGL((selscan_step_kernel<T, Q>), dim3((unsigned)((long long)((p.D + CW - 1) / CW) * p.rows.N)), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_step_type(const SelstepParams& p, hipStream_t stream) {
+    switch (scan_lanes(p.S)) {
+        case 1: return launch_step_lanes<T, 1>(p, stream);
+        case 2: return launch_step_lanes<T, 2>(p, stream);
+        case 4: return launch_step_lanes<T, 4>(p, stream);
+        case 8: return launch_step_lanes<T, 8>(p, stream);
+        default: return launch_step_lanes<T, 16>(p, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_selscan(int dtype, const SelscanParams& p, hipStream_t stream) { return launch_any(dtype, p, false, stream); }
+hipError_t launch_selscan_marks(int dtype, const SelscanParams& p, hipStream_t stream) { return launch_any(dtype, p, true, stream); }
+hipError_t launch_selscan_empty(const SeqRows& rows, long long cells, const float* from, float* to, hipStream_t stream) {
+    const long long all = rows.N * cells / 1024;
+    hipLaunchKernelGGL(selscan_empty_kernel, dim3((unsigned)(all < 1 ? 1 : all > 1024 ? 1024 : all)), dim3(256), 0, stream, rows, cells, from, to);
+    return hipGetLastError();
+}
+hipError_t launch_selscan_step(int dtype, const SelstepParams& p, hipStream_t stream) {
+    switch (dtype) {
+        case DEER_F32: return launch_step_type<float>(p, stream);
+        case DEER_BF16: return launch_step_type<BF16>(p, stream);
+        default: return launch_step_type<F16>(p, stream);
+    }
+}
+
+}  // namespace deer

@@ -47,7 +47,7 @@ struct RestArray {
 };
 struct RestRows {
     int count;
-    RestArray array[4];
+    RestArray array[6];
 };
 template <typename U>
 __device__ __forceinline__ void clear_row(char* row, long long width) {

@@ -1,0 +1,374 @@
+// Short causal convolution of every channel, with an activation: forward, gradient, single tokens.
+#include "layer_common.h"
+
+namespace deer {
+namespace {
+
+template <typename T, int V>
+__device__ __forceinline__ void load_wide(wide_t<T>* to, const T* from) {
+    const vec_t<T, V> v = *reinterpret_cast<const vec_t<T, V>*>(from);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = (wide_t<T>)vec_at<T, V>(v, i);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_narrow(T* to, const wide_t<T>* from) {
+    vec_t<T, V> v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) vec_set<T, V>(v, i, (T)from[i]);
+    *reinterpret_cast<vec_t<T, V>*>(to) = v;
+}
+
+// Row `row` of the sequence that begins at `start`: of x, or of the initial rows in front of it
+template <typename T, int V>
+__device__ __forceinline__ void row_or_initial(wide_t<T>* to, const ConvParams& p, int seq, long long start, long long row, int ch) {
+    using S = wide_t<T>;
+    if (row >= start) {
+        load_wide<T, V>(to, reinterpret_cast<const T*>(p.x) + row * p.stride_x + ch);
+        return;
+    }
+    const S* s0 = reinterpret_cast<const S*>(p.s0);
+    const long long at = ((long long)seq * (p.W - 1) + (row - start + p.W - 1)) * p.D + ch;
+#pragma unroll
+    for (int v = 0; v < V; ++v) to[v] = s0 ? s0[at + v] : S(0);
+}
+
+struct ConvPlace {
+    int n, ch;
+    long long lo, hi;
+    bool on;
+};
+// which rows and channels a lane has: tiles of kConvRows rows a phase, sequences apart where they are padded
+template <int V>
+__device__ __forceinline__ ConvPlace conv_place(const ConvParams& p, const Lanes& l, long long block) {
+    const long long per = (long long)kConvRows * l.phases, tiles = (p.rows.T + per - 1) / per, tile = block / l.blocks;
+    ConvPlace at;
+    at.n = p.rows.packed ? 0 : (int)(tile / tiles);
+    at.ch = ((int)(block % l.blocks) * l.lanes + (int)(threadIdx.x & (l.lanes - 1))) * V;
+    at.on = at.ch < p.D;
+    const long long in = (p.rows.packed ? tile : tile % tiles) * per + (threadIdx.x / l.lanes) * kConvRows, base = (long long)at.n * p.rows.T;
+    at.lo = base + in;
+    at.hi = base + (in + kConvRows < p.rows.T ? in + kConvRows : p.rows.T);
+    return at;
+}
+
+// The rows of the state behind every sequence
+template <typename T>
+__device__ __forceinline__ void conv_last(const ConvParams& p, long long block, long long blocks) {
+    using S = wide_t<T>;
+    const long long all = (long long)p.rows.N * (p.W - 1) * p.D;
+    for (long long i = block * 256 + threadIdx.x; i < all; i += blocks * 256) {
+        const int ch = (int)(i % p.D), k = (int)(i / p.D % (p.W - 1)), n = (int)(i / p.D / (p.W - 1));
+        const long long start = seq_first(p.rows, n), row = start + seq_length(p.rows, n) - (p.W - 1) + k;
+        row_or_initial<T, 1>(reinterpret_cast<S*>(p.last) + i, p, n, start, row, ch);
+    }
+}
+
+// Eight rows at a time: a row is read once (and the W - 1 rows in front of a lane's 32 once more).  M: weights there is room for.
+template <typename T, int V, int M>
+__global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, const Lanes l, const RestRows rest, long long tile_blocks) {
+    using S = wide_t<T>;
+    if ((long long)blockIdx.x >= tile_blocks) {
+        const long long block = blockIdx.x - tile_blocks, blocks = gridDim.x - tile_blocks;
+        clear_rest(p.rows, rest, block, blocks);
+        if (p.last && p.W > 1) conv_last<T>(p, block, blocks);
+        return;
+    }
+    const ConvPlace at = conv_place<V>(p, l, blockIdx.x);
+    if (!at.on) return;
+    S w[M][V], bias[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bias[v] = p.bias ? reinterpret_cast<const S*>(p.bias)[at.ch + v] : S(0);
+#pragma unroll
+        for (int k = 0; k < M; ++k) w[k][v] = k >= M - p.W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - p.W)] : S(0);
+    }
+    for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long start, long long, long long r0, long long r1) {
+        S x[M - 1 + 8][V];
+#pragma unroll
+        for (int k = 0; k < M - 1; ++k) {
+            if (k >= M - p.W) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
+            else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[k][v] = S(0);
+            }
+        }
+        for (long long r = r0; r < r1; r += 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) load_wide<T, V>(x[M - 1 + i], reinterpret_cast<const T*>(p.x) + (r + i < r1 ? r + i : r1 - 1) * p.stride_x + at.ch);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (r + i >= r1) break;
+                S y[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    S sum = bias[v];
+#pragma unroll
+                    for (int k = 0; k < M; ++k)
+                        if (k >= M - p.W) sum = w[k][v] * x[i + k][v] + sum;   // (no weight of zero: what lies in front may be NaN)
+                    y[v] = p.act == DEER_ACT_SILU ? silu<T>(sum) : sum;
+                }
+                store_narrow<T, V>(reinterpret_cast<T*>(p.y) + (r + i) * p.stride_y + at.ch, y);
+            }
+#pragma unroll
+            for (int k = 0; k < M - 1; ++k)
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[k][v] = x[8 + k][v];
+        }
+    });
+}
+
+// Gradient: dv_t = dy_t act'(v_t) with v computed again, dx_t = sum_j w_j dv_{t + W - 1 - j}, dw_j = sum_t dv_t x_{t - W + 1 + j}.  A lane goes on for W - 1 rows behind
+// its own, whose dv its last rows need.
+template <typename T, int V, int M>
+__global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p, const Lanes l, const RestRows rest, long long tile_blocks) {
+    using S = wide_t<T>;
+    constexpr int B = 4;
+    __shared__ S sums[256 * V];
+    if ((long long)blockIdx.x >= tile_blocks) {
+        const long long block = blockIdx.x - tile_blocks, blocks = gridDim.x - tile_blocks, per = (long long)(p.W - 1) * p.D, all = p.rows.N * per;
+        clear_rest(p.rows, rest, block, blocks);
+        if (p.ds0)
+            for (long long i = block * 256 + threadIdx.x; i < all; i += blocks * 256)
+                if (seq_length(p.rows, (int)(i / per)) == 0) reinterpret_cast<S*>(p.ds0)[i] = p.dlast ? reinterpret_cast<const S*>(p.dlast)[i] : S(0);
+        return;
+    }
+    const ConvPlace at = conv_place<V>(p, l, blockIdx.x);
+    const int behind = p.W - 1;
+    S w[M][V], bias[V], dw[M][V], dbias[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bias[v] = p.bias && at.on ? reinterpret_cast<const S*>(p.bias)[at.ch + v] : S(0);
+        dbias[v] = S(0);
+#pragma unroll
+        for (int k = 0; k < M; ++k) {
+            w[k][v] = at.on && k >= M - p.W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - p.W)] : S(0);
+            dw[k][v] = S(0);
+        }
+    }
+    if (at.on)
+        for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long start, long long end, long long r0, long long r1) {
+            S x[M - 1 + B][V], d[M - 1 + B][V];
+            const long long stop = r1 + behind < end ? r1 + behind : end;   // rows whose dv is needed
+#pragma unroll
+            for (int k = 0; k < M - 1; ++k) {
+                if (k >= M - p.W) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if (k < M - p.W) x[k][v] = S(0);
+                    d[k][v] = S(0);
+                }
+            }
+            for (long long r = r0; r < r1 + behind; r += B) {
+                S dy[B][V];
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    const long long row = r + i < stop ? r + i : stop - 1;
+                    load_wide<T, V>(x[M - 1 + i], reinterpret_cast<const T*>(p.x) + row * p.stride_x + at.ch);
+                    load_wide<T, V>(dy[i], reinterpret_cast<const T*>(p.dy) + row * p.stride_y + at.ch);
+                }
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    const long long row = r + i, out = row - behind;
+                    S dx[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        S slope = S(1);
+                        if (p.act == DEER_ACT_SILU) {
+                            S sum = bias[v], f;
+#pragma unroll
+                            for (int k = 0; k < M; ++k)
+                                if (k >= M - p.W) sum = w[k][v] * x[i + k][v] + sum;
+                            silu_both<T>(sum, f, slope);
+                        }
+                        const S dv = row < stop ? dy[i][v] * slope : S(0);
+                        d[M - 1 + i][v] = dv;
+                        if (row < r1) {
+                            dbias[v] += dv;
+#pragma unroll
+                            for (int k = 0; k < M; ++k)
+                                if (k >= M - p.W) dw[k][v] = dv * x[i + k][v] + dw[k][v];
+                        }
+                        // weight j = W - 1 - m goes with the row m in front of this one
+                        S sum = S(0);
+#pragma unroll
+                        for (int m = 0; m < M; ++m)
+                            if (m < p.W) sum = w[M - 1 - (p.W - 1 - m)][v] * d[M - 1 + i - m][v] + sum;
+                        dx[v] = sum;
+                    }
+                    if (out >= r1 || (out < r0 && r0 != start)) continue;
+                    if (out >= end - behind && p.dlast) {
+                        const S* from = reinterpret_cast<const S*>(p.dlast) + ((long long)seq * behind + out - (end - behind)) * p.D + at.ch;
+#pragma unroll
+                        for (int v = 0; v < V; ++v) dx[v] += from[v];
+                    }
+                    if (out >= r0) store_narrow<T, V>(reinterpret_cast<T*>(p.dx) + out * p.stride_x + at.ch, dx);
+                    else if (p.ds0) {
+                        S* to = reinterpret_cast<S*>(p.ds0) + ((long long)seq * behind + out - start + behind) * p.D + at.ch;
+#pragma unroll
+                        for (int v = 0; v < V; ++v) to[v] = dx[v];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < M - 1; ++k)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        x[k][v] = x[B + k][v];
+                        d[k][v] = d[B + k][v];
+                    }
+            }
+        });
+    // the phases' sums, one weight at a time
+    S* part = reinterpret_cast<S*>(p.part) + (long long)(blockIdx.x / l.blocks) * (p.W + 1) * p.D;
+    const int wide = l.lanes * V, first = (int)(blockIdx.x % l.blocks) * wide;
+#pragma unroll
+    for (int k = 0; k <= M; ++k) {
+        if (k < M - p.W) continue;
+        const int j = k == M ? p.W : k - (M - p.W);
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < V; ++v) sums[threadIdx.x * V + v] = k == M ? dbias[v] : dw[k < M ? k : 0][v];
+        __syncthreads();
+        for (int c = threadIdx.x; c < wide; c += 256) {
+            S sum = S(0);
+            for (int f = 0; f < l.phases; ++f) sum += sums[f * wide + c];
+            if (first + c < p.D) part[(long long)j * p.D + first + c] = sum;
+        }
+    }
+}
+
+// One token for every row: latency bound, one launch, a lane a channel; slots as in the recurrences' steps
+template <typename T>
+__global__ __launch_bounds__(256) void shortconv_step_kernel(const ConvStepParams p) {
+    using S = wide_t<T>;
+    const int per = (p.D + 255) / 256, n = blockIdx.x / per, ch = (blockIdx.x % per) * 256 + threadIdx.x;
+    int slot = n;
+    bool twice = false;
+    if (p.rows.slots) {
+        slot = p.rows.slots[n];
+        for (int m = threadIdx.x; m < n; m += 256) twice = twice || p.rows.slots[m] == slot;
+    }
+    const bool in = ch < p.D && slot >= 0 && slot < p.rows.n_slots;
+    S* state = reinterpret_cast<S*>(p.state) + (long long)slot * (p.W - 1) * p.D + ch;
+    S x[8], w[8], sum = S(0);
+    if (in) {
+        sum = p.bias ? reinterpret_cast<const S*>(p.bias)[ch] : S(0);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k >= p.W) break;
+            x[k] = k == p.W - 1 ? (S)reinterpret_cast<const T*>(p.x)[(long long)n * p.stride_x + ch] : state[(long long)k * p.D];
+            w[k] = reinterpret_cast<const S*>(p.w)[(long long)ch * p.W + k];
+        }
+    }
+    twice = p.rows.slots ? __syncthreads_or(twice) != 0 : false;
+    if (!in || twice) {
+        if (p.rows.zero_rest && ch < p.D) reinterpret_cast<T*>(p.y)[(long long)n * p.stride_y + ch] = (T)0;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        if (k >= p.W) break;
+        sum = w[k] * x[k] + sum;
+        if (k > 0) state[(long long)(k - 1) * p.D] = x[k];
+    }
+    reinterpret_cast<T*>(p.y)[(long long)n * p.stride_y + ch] = (T)(p.act == DEER_ACT_SILU ? silu<T>(sum) : sum);
+}
+
+template <typename T, int V, int M>
+hipError_t launch_taps(bool grad, const ConvParams& p, hipStream_t stream) {
+    const Lanes l = lanes_for(p.D, V);
+    const long long per = (long long)kConvRows * l.phases, tiles = (p.rows.T + per - 1) / per * (p.rows.packed ? 1 : p.rows.N), blocks = tiles * l.blocks;
+    RestRows rest{};
+    if (p.zero_rest)
+        rest.array[rest.count++] = grad ? RestArray{p.dx, p.stride_x * (long long)sizeof(T), p.D * (long long)sizeof(T)}
+                                        : RestArray{p.y, p.stride_y * (long long)sizeof(T), p.D * (long long)sizeof(T)};
+    // what is not a tile's: rows of no sequence, and the states' rows, 1,024 elements a workgroup
+    const long long rest_tiles = rest.count ? (p.rows.T + 15) / 16 * (p.rows.packed ? 1 : p.rows.N) : 0, cells = (long long)p.rows.N * (p.W - 1) * p.D / 1024;
+    long long extra = rest_tiles > cells ? rest_tiles : cells;
+    extra = extra < 1 ? 1 : extra > 512 ? 512 : extra;
+    const dim3 grid((unsigned)(blocks + extra)), block(256);
+    if (!grad) {
+        hipLaunchKernelGGL((shortconv_kernel<T, V, M>), grid, block, 0, stream, p, l, rest, blocks);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((shortconv_grad_kernel<T, V, M>), grid, block, 0, stream, p, l, rest, blocks);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    SumInto into{};
+    into.each = p.D;
+    using S = wide_t<T>;
+    for (int j = 0; j < p.W; ++j) {
+        into.to[j] = reinterpret_cast<S*>(p.dw) + j;
+        into.stride[j] = p.W;
+    }
+    into.to[p.W] = p.dbias;
+    into.stride[p.W] = 1;
+    return launch_sum_tiles(sizeof(S) == 8, p.part, tiles, (p.W + 1) * p.D, into, stream);
+}
+
+template <typename T>
+hipError_t launch_type(bool grad, const ConvParams& p, hipStream_t stream) {
+    constexpr int V = sizeof(T) == 2 ? 4 : sizeof(T) == 4 ? 4 : 2;
+    const bool vec = p.D % V == 0 && rows_fit(p.x, p.stride_x, V, sizeof(T)) &&
+                     (grad ? rows_fit(p.dy, p.stride_y, V, sizeof(T)) && rows_fit(p.dx, p.stride_x, V, sizeof(T)) : rows_fit(p.y, p.stride_y, V, sizeof(T)));
+    if (vec) return p.W <= 4 ? launch_taps<T, V, 4>(grad, p, stream) : launch_taps<T, V, 8>(grad, p, stream);
+    return p.W <= 4 ? launch_taps<T, 1, 4>(grad, p, stream) : launch_taps<T, 1, 8>(grad, p, stream);
+}
+
+template <typename T>
+hipError_t launch_step_type(const ConvStepParams& p, hipStream_t stream) {
+    hipLaunchKernelGGL((shortconv_step_kernel<T>), dim3((unsigned)((long long)((p.D + 255) / 256) * p.rows.N)), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+// 16 columns and 16 shares of the tiles a workgroup
+template <typename S>
+__global__ __launch_bounds__(256) void sum_tiles_kernel(const S* part, long long tiles, int cols, const SumInto into) {
+    __shared__ double sums[16][17];
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), f = threadIdx.x >> 4;
+    double sum = 0;
+    if (c < cols)
+        for (long long t = f; t < tiles; t += 16) sum += (double)part[t * cols + c];
+    sums[f][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (f != 0 || c >= cols) return;
+    sum = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += sums[i][threadIdx.x];
+    S* to = reinterpret_cast<S*>(into.to[c / into.each]);
+    if (to) to[(long long)(c % into.each) * into.stride[c / into.each]] = (S)sum;
+}
+
+}  // namespace
+
+hipError_t launch_sum_tiles(bool wide, const void* part, long long tiles, int cols, const SumInto& into, hipStream_t stream) {
+    const dim3 grid((cols + 15) / 16), block(256);
+    if (wide) hipLaunchKernelGGL((sum_tiles_kernel<double>), grid, block, 0, stream, reinterpret_cast<const double*>(part), tiles, cols, into);
+    else hipLaunchKernelGGL((sum_tiles_kernel<float>), grid, block, 0, stream, reinterpret_cast<const float*>(part), tiles, cols, into);
+    return hipGetLastError();
+}
+
+// (with one element a lane there are the fewest lanes along the rows: the most tiles)
+long long conv_tiles(int D, long long T, int N, bool packed) {
+    const long long per = (long long)kConvRows * lanes_for(D, 1).phases;
+    return (T + per - 1) / per * (packed ? 1 : N);
+}
+
+hipError_t launch_shortconv(int dtype, bool grad, const ConvParams& p, hipStream_t stream) {
+    switch (dtype) {
+        case DEER_F32: return launch_type<float>(grad, p, stream);
+        case DEER_F64: return launch_type<double>(grad, p, stream);
+        case DEER_BF16: return launch_type<BF16>(grad, p, stream);
+        default: return launch_type<F16>(grad, p, stream);
+    }
+}
+
+hipError_t launch_shortconv_step(int dtype, const ConvStepParams& p, hipStream_t stream) {
+    switch (dtype) {
+        case DEER_F32: return launch_step_type<float>(p, stream);
+        case DEER_F64: return launch_step_type<double>(p, stream);
+        case DEER_BF16: return launch_step_type<BF16>(p, stream);
+        default: return launch_step_type<F16>(p, stream);
+    }
+}
+
+}  // namespace deer

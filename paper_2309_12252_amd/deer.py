@@ -24,7 +24,10 @@ DEER_ROWS_PADDED, DEER_ROWS_PACKED, DEER_REST_ZERO = 0, 1, 256
 EXPORTS = ["deer_theta_count", "deer_workspace_bytes", "deer_create", "deer_eval", "deer_grad",
            "deer_linrec_solve", "deer_linrec_solve_static", "deer_set_profiling", "deer_get_profile", "deer_last_error", "deer_destroy",
            "deer_diagrec_workspace_bytes", "deer_diagrec_solve", "deer_diagrec_grad", "deer_diagrec_step", "deer_dropout",
-           "deer_matrec_workspace_bytes", "deer_matrec_solve", "deer_matrec_grad", "deer_matrec_step"]
+           "deer_matrec_workspace_bytes", "deer_matrec_solve", "deer_matrec_grad", "deer_matrec_step",
+           "deer_shortconv_workspace_bytes", "deer_shortconv_solve", "deer_shortconv_grad", "deer_shortconv_step",
+           "deer_selscan_workspace_bytes", "deer_selscan_solve", "deer_selscan_grad", "deer_selscan_step",
+           "deer_groupnorm_workspace_bytes", "deer_groupnorm_solve", "deer_groupnorm_grad"]
 
 
 class DeerConfig(ctypes.Structure):
@@ -57,6 +60,26 @@ class MatrecConfig(ctypes.Structure):
                 ("Hk", ctypes.c_int32), ("Hv", ctypes.c_int32), ("Dk", ctypes.c_int32), ("Dv", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("scale", ctypes.c_double), ("stride_q", ctypes.c_int64),
                 ("stride_k", ctypes.c_int64), ("stride_v", ctypes.c_int64), ("stride_o", ctypes.c_int64)]
+
+
+class ShortconvConfig(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("N", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("T", ctypes.c_int64), ("packed", ctypes.c_int32), ("W", ctypes.c_int32), ("stride_x", ctypes.c_int64),
+                ("stride_y", ctypes.c_int64)]
+
+
+class SelscanConfig(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("dt_act", ctypes.c_int32), ("N", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("T", ctypes.c_int64), ("packed", ctypes.c_int32), ("S", ctypes.c_int32), ("G", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("stride_x", ctypes.c_int64), ("stride_dt", ctypes.c_int64),
+                ("stride_B", ctypes.c_int64), ("stride_C", ctypes.c_int64), ("stride_z", ctypes.c_int64), ("stride_y", ctypes.c_int64)]
+
+
+class GroupnormConfig(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("span", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("G", ctypes.c_int32), ("T", ctypes.c_int64), ("packed", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("eps", ctypes.c_double), ("stride_x", ctypes.c_int64),
+                ("stride_z", ctypes.c_int64), ("stride_y", ctypes.c_int64)]
 
 
 class DeerError(RuntimeError):
@@ -103,6 +126,7 @@ def load_library():
     lib.deer_destroy.argtypes = [vp]
     size, i64, u32, u64 = ctypes.c_size_t, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64
     dcp, mcp = ctypes.POINTER(DiagrecConfig), ctypes.POINTER(MatrecConfig)
+    ccp, scp, gcp = ctypes.POINTER(ShortconvConfig), ctypes.POINTER(SelscanConfig), ctypes.POINTER(GroupnormConfig)
     for name, args in (("deer_diagrec_workspace_bytes", [dcp, i32, ctypes.POINTER(size)]),
                        ("deer_diagrec_solve", [dcp] + [vp] * 7 + [size, vp]),
                        ("deer_diagrec_grad", [dcp] + [vp] * 11 + [size, vp]),
@@ -111,6 +135,17 @@ def load_library():
                        ("deer_matrec_solve", [mcp] + [vp] * 9 + [size, vp]),
                        ("deer_matrec_grad", [mcp] + [vp] * 14 + [size, vp]),
                        ("deer_matrec_step", [mcp] + [vp] * 5 + [i32] + [vp] * 3),
+                       ("deer_shortconv_workspace_bytes", [ccp, ctypes.POINTER(size)]),
+                       ("deer_shortconv_solve", [ccp] + [vp] * 8),
+                       ("deer_shortconv_grad", [ccp] + [vp] * 12 + [size, vp]),
+                       ("deer_shortconv_step", [ccp] + [vp] * 4 + [i32] + [vp] * 3),
+                       ("deer_selscan_workspace_bytes", [scp, i32, ctypes.POINTER(size)]),
+                       ("deer_selscan_solve", [scp] + [vp] * 13 + [size, vp]),
+                       ("deer_selscan_grad", [scp] + [vp] * 22 + [size, vp]),
+                       ("deer_selscan_step", [scp] + [vp] * 9 + [i32] + [vp] * 3),
+                       ("deer_groupnorm_workspace_bytes", [gcp, i32, ctypes.POINTER(size)]),
+                       ("deer_groupnorm_solve", [gcp] + [vp] * 8 + [size, vp]),
+                       ("deer_groupnorm_grad", [gcp] + [vp] * 12 + [size, vp]),
                        ("deer_dropout", [i32, i32, i64, i32, vp, i64, vp, i64, dbl, u64, u32, vp])):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = args
@@ -122,7 +157,8 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else None
 
 
-DEER_ACT_TANH, DEER_ACT_SOFTPLUS = 0, 1
+DEER_ACT_TANH, DEER_ACT_SOFTPLUS, DEER_ACT_NONE, DEER_ACT_SILU = 0, 1, 2, 3
+DEER_SPAN_ROW, DEER_SPAN_SEQUENCE = 0, 1
 
 
 def make_config(cell, dtype, B, T, n, d=0, mlp_width=0, mlp_hidden_layers=0, t0=0.0, t1=0.0, mlp_activation=0,
@@ -308,7 +344,8 @@ def _on_stream(f):
                     if isinstance(t, torch.Tensor) and t.is_cuda:
                         t.record_stream(stream)
                 for t in result if isinstance(result, tuple) else (result,):
-                    t.record_stream(here)
+                    if t is not None:
+                        t.record_stream(here)
             return result
         if first.device.index == torch.cuda.current_device():
             return f(*args, **kw)
@@ -685,6 +722,332 @@ def dropout(x, p, seed, draw=0, *, out=None):
     if st != DEER_OK:
         _raise(lib, st)
     return y
+
+
+# ---- layers with selective states ----
+def _rows_out(x, out, what="out"):
+    """an array like x for a result, or the one that is handed in"""
+    if out is None:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+    _check_like(out, what, x.shape, x.dtype, x.device)
+    return out
+
+
+def _gradient_like(x, given, what, of, lead, stride):
+    """the gradient of x: with its row stride; `given`, where there is one"""
+    if given is None:
+        if x.is_contiguous():
+            return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if x.dim() == lead + 2:
+            return _rows_like(x.flatten(-2), stride).unflatten(-1, x.shape[-2:])
+        return _rows_like(x, stride)
+    _check_like(given, what, x.shape, x.dtype, x.device)
+    if _row_stride(given, what, lead) != stride:
+        _refuse("%s: rows must lie like those of %s" % (what, of))
+    return given
+
+
+def _wide(dtype):
+    return torch.float64 if dtype == DEER_F64 else torch.float32
+
+
+def _type_of(x, types="float32, float64, bfloat16 or float16"):
+    dtype = _DTYPES.get(x.dtype) if isinstance(x, torch.Tensor) else None
+    if dtype is None:
+        _refuse("need " + types)
+    return dtype
+
+
+def _slots_of(state, slots, N, shape, dtype, device):
+    """pointers of a pool of states [slots, ...] and of the rows' slots"""
+    if not isinstance(state, torch.Tensor) or state.dim() != len(shape) + 1:
+        _refuse("state: need [slots, %s]" % ", ".join(str(n) for n in shape))
+    sp = _dense(state, "state", state.shape[:1] + tuple(shape), dtype, device)
+    _int32(state.shape[0])
+    return sp, _dense(slots, "slots", torch.Size((N,)), torch.int32, device), state.shape[0]
+
+
+def _conv_inputs(x, w, bias, dtype):
+    """(channels, weights of a channel, pointers of w and bias)"""
+    D, wide = x.shape[-1], _wide(dtype)
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        _refuse("w: need [D, W]")
+    W = w.shape[1]
+    wp = _dense(w, "w", torch.Size((D, W)), wide, x.device)
+    return D, W, wp, _dense(bias, "bias", torch.Size((D,)), wide, x.device)
+
+
+@_on_stream
+def shortconv_solve(x, w, bias=None, s0=None, *, act=DEER_ACT_SILU, offsets=None, lengths=None, out=None):
+    """deer_shortconv_solve: y_t = act(bias + sum_j w[:, j] x_{t - W + 1 + j}) for every channel.  x [N, T, D] with optional int64 `lengths` [N], or packed
+    [rows, D] with int64 `offsets` [N + 1]; rows may be slices of wider ones.  w [D, W] and bias [D] in float32 (float64 with float64), likewise s0 [N, W - 1, D], the
+    rows in front of every sequence, the earliest first.  Rows of no sequence are zero in the result, left as they are in `out`.  Returns (y, the last
+    W - 1 rows of every sequence); torch.autograd does not see the call, shortconv_grad is its gradient."""
+    lib, dtype = load_library(), _type_of(x)
+    N, T, packed, bounds, lead = _rows_of(x, 1, offsets, lengths)
+    D, W, wp, bp = _conv_inputs(x, w, bias, dtype)
+    _int32(N, D)
+    y = _rows_out(x, out)
+    last = torch.empty((N, W - 1, D), dtype=_wide(dtype), device=x.device)
+    s0p = _dense(s0, "s0", last.shape, last.dtype, x.device)
+    rest = _zero_rest(bounds, y if out is None else None)
+    cfg = ShortconvConfig(dtype, int(act), N, D, T, packed | rest, W, _row_stride(x, "x", lead), _row_stride(y, "out", lead))
+    st = lib.deer_shortconv_solve(ctypes.byref(cfg), x.data_ptr(), wp, bp, s0p, bounds, y.data_ptr(), last.data_ptr(), _stream_of(x.device))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return y, last
+
+
+@functools.lru_cache(maxsize=512)
+def _conv_workspace(dtype, N, D, T, packed, W):
+    lib, size = load_library(), ctypes.c_size_t(0)
+    cfg = ShortconvConfig(dtype, DEER_ACT_NONE, N, D, T, packed, W, 0, 0)
+    st = lib.deer_shortconv_workspace_bytes(ctypes.byref(cfg), ctypes.byref(size))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return size.value
+
+
+@_on_stream
+def shortconv_grad(x, w, dy, bias=None, s0=None, dlast=None, *, act=DEER_ACT_SILU, offsets=None, lengths=None, dx=None):
+    """deer_shortconv_grad: (dx, dw, dbias, ds0) from dy = dL/dy and dlast = dL/d(last rows).  dx, where given, has the row stride of x, and its rows of no
+    sequence are left as they are; otherwise these are zero."""
+    lib, dtype = load_library(), _type_of(x)
+    N, T, packed, bounds, lead = _rows_of(x, 1, offsets, lengths)
+    D, W, wp, bp = _conv_inputs(x, w, bias, dtype)
+    _int32(N, D)
+    dev, wide = x.device, _wide(dtype)
+    _check_like(dy, "dy", x.shape, x.dtype, dev)
+    stride = _row_stride(x, "x", lead)
+    given = dx
+    dx = _gradient_like(x, given, "dx", "x", lead, stride)
+    ds0 = torch.empty((N, W - 1, D), dtype=wide, device=dev)
+    s0p, dlp = _dense(s0, "s0", ds0.shape, wide, dev), _dense(dlast, "dlast", ds0.shape, wide, dev)
+    dw, dbias = torch.empty((D, W), dtype=wide, device=dev), torch.empty((D,), dtype=wide, device=dev)
+    size = _conv_workspace(dtype, N, D, T, packed, W)
+    ws = x.new_empty(size, dtype=torch.uint8)
+    rest = _zero_rest(bounds, dx if given is None else None)
+    cfg = ShortconvConfig(dtype, int(act), N, D, T, packed | rest, W, stride, _row_stride(dy, "dy", lead))
+    st = lib.deer_shortconv_grad(ctypes.byref(cfg), x.data_ptr(), wp, bp, s0p, bounds, dy.data_ptr(), dlp, dx.data_ptr(), dw.data_ptr(), dbias.data_ptr(),
+                                 ds0.data_ptr(), ws.data_ptr(), size, _stream_of(dev))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return dx, dw, dbias, ds0
+
+
+@_on_stream
+def shortconv_step(x, w, state, bias=None, *, act=DEER_ACT_SILU, slots=None, out=None):
+    """deer_shortconv_step: one token for each of N rows, x [N, D]; `state` [slots, W - 1, D] (float32; float64 with float64), the rows in front, is moved on in
+    place, row n at slots[n] (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over: zero in the result, left as they are in
+    `out`.  Returns y [N, D]."""
+    lib, dtype = load_library(), _type_of(x)
+    if x.dim() != 2:
+        _refuse("need x [N, D]")
+    D, W, wp, bp = _conv_inputs(x, w, bias, dtype)
+    y, N = _rows_out(x, out), x.shape[0]
+    sp, tp, n_slots = _slots_of(state, slots, N, (W - 1, D), _wide(dtype), x.device)
+    _int32(N, D)
+    cfg = ShortconvConfig(dtype, int(act), N, D, 1, DEER_REST_ZERO if out is None else 0, W, _row_stride(x, "x", 1), _row_stride(y, "out", 1))
+    st = lib.deer_shortconv_step(ctypes.byref(cfg), x.data_ptr(), wp, bp, tp, n_slots, sp, y.data_ptr(), _stream_of(x.device))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return y
+
+
+@functools.lru_cache(maxsize=512)
+def _scan_workspace(grad, dtype, N, D, T, packed, S, G):
+    lib, size = load_library(), ctypes.c_size_t(0)
+    cfg = SelscanConfig(dtype, DEER_ACT_NONE, N, D, T, packed, S, G, 0, 0, 0, 0, 0, 0, 0)
+    st = lib.deer_selscan_workspace_bytes(ctypes.byref(cfg), grad, ctypes.byref(size))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return size.value
+
+
+def _scan_config(x, dt, A, B, C, y, what, skip, z, dt_bias, softplus, offsets, lengths, lead=None):
+    """configuration, pointers of the bounds, A, skip and dt_bias, leading dimensions; y: rows that lie like the result; lead: given for a step"""
+    dtype = _type_of(x, "float32, bfloat16 or float16")
+    if lead is None:
+        N, T, packed, bounds, lead = _rows_of(x, 1, offsets, lengths)
+    else:
+        if x.dim() != 2:
+            _refuse("need x [N, D]")
+        N, T, packed, bounds = x.shape[0], 1, 0, 0
+    dev, D, rows = x.device, x.shape[-1], x.shape[:lead]
+    _check_like(dt, "dt", x.shape, x.dtype, dev)
+    if not isinstance(A, torch.Tensor) or A.dim() != 2:
+        _refuse("A: need [D, S]")
+    S = A.shape[1]
+    ap = _dense(A, "A", torch.Size((D, S)), torch.float32, dev)
+    if not isinstance(B, torch.Tensor) or B.dim() != lead + 2:
+        _refuse("B: need [..., G, S]")
+    G = B.shape[lead]
+    for t, name in ((B, "B"), (C, "C")):
+        _check_like(t, name, rows + torch.Size((G, S)), x.dtype, dev)
+    if z is not None:
+        _check_like(z, "z", x.shape, x.dtype, dev)
+    _int32(N, D, G, S)
+    if G < 1 or D % G:
+        _refuse("the groups of B and C must divide the channels")
+    vector = torch.Size((D,))
+    kp, bp = _dense(skip, "skip", vector, torch.float32, dev), _dense(dt_bias, "dt_bias", vector, torch.float32, dev)
+    cfg = SelscanConfig(dtype, DEER_ACT_SOFTPLUS if softplus else DEER_ACT_NONE, N, D, T, packed, S, G, 0, _row_stride(x, "x", lead), _row_stride(dt, "dt", lead),
+                        _row_stride(B, "B", lead), _row_stride(C, "C", lead), _row_stride(z, "z", lead) if z is not None else 0, _row_stride(y, what, lead))
+    return cfg, bounds, ap, kp, bp, lead
+
+
+@_on_stream
+def selscan_solve(x, dt, A, B, C, skip=None, z=None, dt_bias=None, h0=None, *, softplus=True, offsets=None, lengths=None, out=None):
+    """deer_selscan_solve: h_t = exp(d_t A) h_{t-1} + d_t x_t B_t, y_t = <C_t, h_t> + skip x_t, with d = softplus(dt + dt_bias) (softplus false: dt + dt_bias), times
+    z sigmoid(z) where there is a z.  x, dt, z [N, T, D] and B, C [N, T, G, S] in float32, bfloat16 or float16 with optional int64 `lengths` [N], or packed [rows, ...]
+    with int64 `offsets` [N + 1]; rows may be slices of wider ones.  A [D, S], skip and dt_bias [D], h0 [N, D, S] in float32.  Rows of no sequence are zero
+    in the result, left as they are in `out`.  Returns (y, states behind the last rows); torch.autograd does not see the call, selscan_grad is its gradient."""
+    lib = load_library()
+    _type_of(x, "float32, bfloat16 or float16")
+    y = _rows_out(x, out)
+    cfg, bounds, ap, kp, bp, _ = _scan_config(x, dt, A, B, C, y, "out", skip, z, dt_bias, softplus, offsets, lengths)
+    dev = x.device
+    last = torch.empty((cfg.N, cfg.D, cfg.S), dtype=torch.float32, device=dev)
+    h0p = _dense(h0, "h0", last.shape, torch.float32, dev)
+    size = _scan_workspace(0, cfg.dtype, cfg.N, cfg.D, cfg.T, cfg.packed, cfg.S, cfg.G)
+    ws = x.new_empty(size, dtype=torch.uint8)
+    cfg.packed |= _zero_rest(bounds, y if out is None else None)
+    st = lib.deer_selscan_solve(ctypes.byref(cfg), x.data_ptr(), dt.data_ptr(), ap, B.data_ptr(), C.data_ptr(), kp, z.data_ptr() if z is not None else 0, bp, h0p,
+                                bounds, y.data_ptr(), last.data_ptr(), ws.data_ptr(), size, _stream_of(dev))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return y, last
+
+
+@_on_stream
+def selscan_grad(x, dt, A, B, C, dy, skip=None, z=None, dt_bias=None, h0=None, dlast=None, *, softplus=True, offsets=None, lengths=None,
+                 dx=None, ddt=None, dB=None, dC=None, dz=None):
+    """deer_selscan_grad: (dx, ddt, dA, dB, dC, dskip, dz, d(dt_bias), dh0) from dy = dL/dy and dlast = dL/d(final states); dz is None without z.  dx, ddt, dB, dC and
+    dz, where given, have the row strides of what they are the gradients of; their rows of no sequence are left as they are, and are zero in arrays that are not given."""
+    lib = load_library()
+    _type_of(x, "float32, bfloat16 or float16")
+    _check_like(dy, "dy", x.shape, x.dtype, x.device)
+    cfg, bounds, ap, kp, bp, lead = _scan_config(x, dt, A, B, C, dy, "dy", skip, z, dt_bias, softplus, offsets, lengths)
+    dev, outs, made = x.device, [], []
+    for t, given, name, of, stride in ((x, dx, "dx", "x", cfg.stride_x), (dt, ddt, "ddt", "dt", cfg.stride_dt), (B, dB, "dB", "B", cfg.stride_B),
+                                       (C, dC, "dC", "C", cfg.stride_C), (z, dz, "dz", "z", cfg.stride_z)):
+        if t is None:
+            if given is not None:
+                _refuse("dz: there is no z")
+            outs.append(None)
+            continue
+        outs.append(_gradient_like(t, given, name, of, lead, stride))
+        made.append(outs[-1] if given is None else None)
+    shape = (cfg.N, cfg.D, cfg.S)
+    dh0 = torch.empty(shape, dtype=torch.float32, device=dev)
+    h0p, dlp = _dense(h0, "h0", dh0.shape, torch.float32, dev), _dense(dlast, "dlast", dh0.shape, torch.float32, dev)
+    dA = torch.empty((cfg.D, cfg.S), dtype=torch.float32, device=dev)
+    dskip, dbias = torch.empty((2, cfg.D), dtype=torch.float32, device=dev).unbind(0)
+    size = _scan_workspace(1, cfg.dtype, cfg.N, cfg.D, cfg.T, cfg.packed, cfg.S, cfg.G)
+    ws = x.new_empty(size, dtype=torch.uint8)
+    cfg.packed |= _zero_rest(bounds, *made)
+    st = lib.deer_selscan_grad(ctypes.byref(cfg), x.data_ptr(), dt.data_ptr(), ap, B.data_ptr(), C.data_ptr(), kp, z.data_ptr() if z is not None else 0, bp, h0p,
+                               bounds, dy.data_ptr(), dlp, outs[0].data_ptr(), outs[1].data_ptr(), dA.data_ptr(), outs[2].data_ptr(), outs[3].data_ptr(),
+                               dskip.data_ptr(), outs[4].data_ptr() if z is not None else 0, dbias.data_ptr(), dh0.data_ptr(), ws.data_ptr(), size, _stream_of(dev))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return outs[0], outs[1], dA, outs[2], outs[3], dskip, outs[4], dbias, dh0
+
+
+@_on_stream
+def selscan_step(x, dt, A, B, C, state, skip=None, z=None, dt_bias=None, *, softplus=True, slots=None, out=None):
+    """deer_selscan_step: one token for each of N rows, x, dt, z [N, D], B, C [N, G, S]; `state` [slots, D, S] float32 is updated in place, row n at slots[n]
+    (int32 [N]; None: n).  Rows whose slot is out of range or has come before are passed over: zero in the result, left as they are in `out`.  Returns y [N, D]."""
+    lib = load_library()
+    _type_of(x, "float32, bfloat16 or float16")
+    y = _rows_out(x, out)
+    cfg, _, ap, kp, bp, _ = _scan_config(x, dt, A, B, C, y, "out", skip, z, dt_bias, softplus, None, None, lead=1)
+    sp, tp, n_slots = _slots_of(state, slots, cfg.N, (cfg.D, cfg.S), torch.float32, x.device)
+    cfg.packed = DEER_REST_ZERO if out is None else 0
+    st = lib.deer_selscan_step(ctypes.byref(cfg), x.data_ptr(), dt.data_ptr(), ap, B.data_ptr(), C.data_ptr(), kp, z.data_ptr() if z is not None else 0, bp, tp,
+                               n_slots, sp, y.data_ptr(), _stream_of(x.device))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return y
+
+
+@functools.lru_cache(maxsize=512)
+def _norm_workspace(grad, dtype, span, N, D, G, T, packed):
+    lib, size = load_library(), ctypes.c_size_t(0)
+    cfg = GroupnormConfig(dtype, DEER_ACT_NONE, span, N, D, G, T, packed, 0, 0.0, 0, 0, 0)
+    st = lib.deer_groupnorm_workspace_bytes(ctypes.byref(cfg), grad, ctypes.byref(size))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return size.value
+
+
+def _norm_config(x, groups, y, what, w, bias, z, span, eps, act, offsets, lengths):
+    """configuration, pointers of the bounds, w and bias, shape of the statistics, leading dimensions"""
+    dtype = _type_of(x)
+    N, T, packed, bounds, lead = _rows_of(x, 1, offsets, lengths)
+    D, G, dev = x.shape[-1], operator.index(groups), x.device
+    _int32(N, D, G)
+    if G < 1 or D % G:
+        _refuse("the groups must divide the channels")
+    if span not in (DEER_SPAN_ROW, DEER_SPAN_SEQUENCE):
+        _refuse("unknown span")
+    vector, wide = torch.Size((D,)), _wide(dtype)
+    wp, bp = _dense(w, "w", vector, wide, dev), _dense(bias, "bias", vector, wide, dev)
+    if z is not None:
+        _check_like(z, "z", x.shape, x.dtype, dev)
+    cfg = GroupnormConfig(dtype, int(act), int(span), N, D, G, T, packed, 0, eps, _row_stride(x, "x", lead), _row_stride(z, "z", lead) if z is not None else 0,
+                          _row_stride(y, what, lead))
+    stats = (x.shape[:lead] if span == DEER_SPAN_ROW else torch.Size((N,))) + torch.Size((G, 2))
+    return cfg, bounds, wp, bp, stats, lead
+
+
+@_on_stream
+def groupnorm_solve(x, groups, w=None, bias=None, z=None, *, span=DEER_SPAN_ROW, eps=1e-5, act=DEER_ACT_NONE, offsets=None, lengths=None, out=None):
+    """deer_groupnorm_solve: act((x - mean) rstd w + bias), times z sigmoid(z) where there is a z; mean and rstd of the D / groups channels of a group, over every row by
+    itself (DEER_SPAN_ROW) or over all rows of a sequence (DEER_SPAN_SEQUENCE).  x, z [N, T, D] with optional int64 `lengths` [N], or packed [rows, D] with int64
+    `offsets` [N + 1]; rows may be slices of wider ones.  w and bias [D] in float32 (float64 with float64).  Rows of no sequence are zero in the results, left as
+    they are in `out`.  Returns (y, statistics: mean and rstd, [..., groups, 2], or [N, groups, 2]); torch.autograd does not see the call, groupnorm_grad is its gradient."""
+    lib = load_library()
+    _type_of(x)
+    y = _rows_out(x, out)
+    cfg, bounds, wp, bp, shape, _ = _norm_config(x, groups, y, "out", w, bias, z, span, eps, act, offsets, lengths)
+    stats = torch.empty(shape, dtype=_wide(cfg.dtype), device=x.device)
+    size = _norm_workspace(0, cfg.dtype, cfg.span, cfg.N, cfg.D, cfg.G, cfg.T, cfg.packed)
+    ws = x.new_empty(size, dtype=torch.uint8)
+    cfg.packed |= _zero_rest(bounds, y if out is None else None, stats) if span == DEER_SPAN_ROW else _zero_rest(bounds, y if out is None else None)
+    st = lib.deer_groupnorm_solve(ctypes.byref(cfg), x.data_ptr(), wp, bp, z.data_ptr() if z is not None else 0, bounds, y.data_ptr(), stats.data_ptr(),
+                                  ws.data_ptr(), size, _stream_of(x.device))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return y, stats
+
+
+@_on_stream
+def groupnorm_grad(x, groups, stats, dy, w=None, bias=None, z=None, *, span=DEER_SPAN_ROW, act=DEER_ACT_NONE, offsets=None, lengths=None, dx=None, dz=None):
+    """deer_groupnorm_grad at the statistics that groupnorm_solve gave: (dx, dw, dbias, dz) from dy = dL/dy; dz is None without z.  dx and dz, where given, have the row
+    strides of x and z, and their rows of no sequence are left as they are; otherwise these are zero."""
+    lib = load_library()
+    _type_of(x)
+    _check_like(dy, "dy", x.shape, x.dtype, x.device)
+    cfg, bounds, wp, bp, shape, lead = _norm_config(x, groups, dy, "dy", w, bias, z, span, 0.0, act, offsets, lengths)
+    dev, wide, given = x.device, _wide(cfg.dtype), (dx, dz)
+    sp = _dense(stats, "stats", shape, wide, dev) if stats is not None else _refuse("stats: need those of groupnorm_solve")
+    if z is None and dz is not None:
+        _refuse("dz: there is no z")
+    dx = _gradient_like(x, dx, "dx", "x", lead, cfg.stride_x)
+    made = [dx if given[0] is None else None]
+    if z is not None:
+        dz = _gradient_like(z, dz, "dz", "z", lead, cfg.stride_z)
+        made.append(dz if given[1] is None else None)
+    dw, dbias = torch.empty((2, cfg.D), dtype=wide, device=dev).unbind(0)
+    size = _norm_workspace(1, cfg.dtype, cfg.span, cfg.N, cfg.D, cfg.G, cfg.T, cfg.packed)
+    ws = x.new_empty(size, dtype=torch.uint8)
+    cfg.packed |= _zero_rest(bounds, *made)
+    st = lib.deer_groupnorm_grad(ctypes.byref(cfg), x.data_ptr(), wp, bp, z.data_ptr() if z is not None else 0, bounds, sp, dy.data_ptr(), dx.data_ptr(), dw.data_ptr(),
+                                 dbias.data_ptr(), dz.data_ptr() if z is not None else 0, ws.data_ptr(), size, _stream_of(dev))
+    if st != DEER_OK:
+        _raise(lib, st)
+    return dx, dw, dbias, dz
 
 
 def context_for(workload, dtype=DEER_F32, device="cuda:0"):
