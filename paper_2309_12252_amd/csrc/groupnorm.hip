@@ -494,12 +494,7 @@ hipError_t launch_sequences(bool grad, const NormParams& p, hipStream_t stream) 
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !grad || (!p.dw && !p.dbias)) return e;
-    SumInto into{};
-    into.each = p.D;
-    into.to[0] = p.dw;
-    into.to[1] = p.dbias;
-    into.stride[0] = into.stride[1] = 1;
-    return launch_sum_tiles(sizeof(S) == 8, p.sums, tiles, 2 * p.D, into, stream);
+    return launch_sum_tiles(sizeof(S) == 8, p.sums, tiles, SumInto{p.dw, p.dbias, p.D, 1, true}, stream);
 }
 
 // rows of a workgroup, and how many workgroups along the rows: about 2,048 in all
@@ -524,12 +519,7 @@ hipError_t launch_rows_as(const NormParams& p, hipStream_t stream) {
     if (c.blocks) hipLaunchKernelGGL((rownorm_kernel<T, V, M, GRAD, FEW>), dim3((unsigned)(c.blocks * s.blocks)), dim3(256), 0, stream, p, s, rest_of(p, GRAD, sizeof(T)), c.each);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !GRAD || (!p.dw && !p.dbias)) return e;
-    SumInto into{};
-    into.each = p.D;
-    into.to[0] = p.dw;
-    into.to[1] = p.dbias;
-    into.stride[0] = into.stride[1] = 1;
-    return launch_sum_tiles(sizeof(S) == 8, p.part, c.blocks * s.rows, 2 * p.D, into, stream);
+    return launch_sum_tiles(sizeof(S) == 8, p.part, c.blocks * s.rows, SumInto{p.dw, p.dbias, p.D, 1, true}, stream);
 }
 template <typename T, int V, bool GRAD>
 hipError_t launch_rows(const NormParams& p, hipStream_t stream) {

@@ -92,7 +92,7 @@ ScanLayout scan_layout(const deer_selscan_config* c, bool grad) {
     l.blocks = (per_group + width - 1) / width;
     const long long seqs = is_packed(c) ? 1 : c->N, across = (long long)c->G * l.blocks * seqs;
     // enough workgroups for 256 CUs, of 64 rows at least
-    long long want = is_packed(c) || across < 256 ? (1024 + across - 1) / across : 1;
+    long long want = (2048 + across - 1) / across;
     const long long most = (c->T + 63) / 64;
     want = want > most ? most : want;
     want = want < 1 ? 1 : want;
@@ -131,6 +131,8 @@ const char* unsupported(const deer_selscan_config* c, bool step) {
     if (c->S > 64) return "selective scan: up to 64 states";
     if (c->D > (1 << 24)) return kLarge;
     if (step) return (long double)c->N * ((long long)c->D * scan_lanes(c->S) + 256) > kMostLanes ? kLarge : nullptr;
+    for (const int64_t stride : {c->stride_x, c->stride_dt, c->stride_B, c->stride_C, c->stride_z, c->stride_y, (int64_t)c->D, (int64_t)c->G * c->S})
+        if (stride > kScanStride) return "selective scan: rows at most 2^22 elements apart";
     const long double seqs = is_packed(c) ? 1 : c->N;
     if (c->T > kMostRows || row_count(c) * c->D > 1e15L || seqs * c->D * 64 > kMostLanes) return kLarge;
     const ScanLayout l = scan_layout(c, true);
@@ -180,7 +182,8 @@ SelscanParams scan_params(const deer_selscan_config* c, const ScanLayout& l, con
     return p;
 }
 bool scan_vec(const SelscanParams& p, size_t e, bool grad) {
-    bool vec = p.per_group % 4 == 0 && rows_fit(p.x, p.stride_x, 4, e) && rows_fit(p.dt, p.stride_dt, 4, e) && (!p.z || rows_fit(p.z, p.stride_z, 4, e));
+    bool vec = p.per_group % 4 == 0 && p.S % 4 == 0 && rows_fit(p.x, p.stride_x, 4, e) && rows_fit(p.dt, p.stride_dt, 4, e) && rows_fit(p.B, p.stride_B, 4, e) &&
+               rows_fit(p.C, p.stride_C, 4, e) && (!p.z || rows_fit(p.z, p.stride_z, 4, e));
     if (grad) return vec && rows_fit(p.dy, p.stride_y, 4, e) && rows_fit(p.dx, p.stride_x, 4, e) && rows_fit(p.ddt, p.stride_dt, 4, e) && (!p.z || rows_fit(p.dz, p.stride_z, 4, e));
     return vec && rows_fit(p.y, p.stride_y, 4, e);
 }
@@ -344,7 +347,6 @@ deer_status deer_selscan_solve(const deer_selscan_config* c, const void* d_x, co
     p.y = d_y;
     p.last = d_last;
     p.vec = scan_vec(p, e, false);
-    p.vec_bc = c->S % 4 == 0 && rows_fit(d_B, p.stride_B, 4, e) && rows_fit(d_C, p.stride_C, 4, e);
     return launched("deer_selscan_solve", launch_selscan(c->dtype, p, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
@@ -384,7 +386,6 @@ deer_status deer_selscan_grad(const deer_selscan_config* c, const void* d_x, con
     p.dbias = d_dbias;
     p.dh0 = d_dh0;
     p.vec = scan_vec(p, e, true);
-    p.vec_bc = c->S % 4 == 0 && rows_fit(d_B, p.stride_B, 4, e) && rows_fit(d_C, p.stride_C, 4, e);
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     hipError_t err = launch_selscan_marks(c->dtype, p, stream);
     if (err == hipSuccess) err = launch_selscan_grad(c->dtype, p, stream);

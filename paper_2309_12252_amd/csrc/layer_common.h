@@ -63,13 +63,14 @@ __device__ __forceinline__ void for_runs(const SeqRows& s, int n, long long lo, 
 // first row of sequence n and how many it has
 __device__ __forceinline__ long long seq_first(const SeqRows& s, int n) { return s.packed ? clamp_row(s.bounds[n], s.T) : (long long)n * s.T; }
 
-// Sums over tiles, in the order of the tiles and in 64 bits: part [tiles][cols], column c of it to to[c / each] at (c % each) * stride[c / each].
+// Sums over tiles, in the order of the tiles and in 64 bits: part [tiles][many + 1][each]; the first many rows of sums into first [each][many], the last into second (either may be
+// NULL; without a last row: last false)
 struct SumInto {
-    void* to[10];
-    int stride[10];
-    int each;
+    void *first, *second;
+    int each, many;
+    bool last;
 };
-hipError_t launch_sum_tiles(bool wide, const void* part, long long tiles, int cols, const SumInto& into, hipStream_t stream);
+hipError_t launch_sum_tiles(bool wide, const void* part, long long tiles, const SumInto& into, hipStream_t stream);
 
 // How a launch of 256 lanes goes over rows and channels: `lanes` (a power of two up to 64) side by side along the channels, V each, the others along the rows
 struct Lanes {

@@ -1,21 +1,15 @@
 // Selective scan: h_t = exp(dt_t A) h_{t-1} + dt_t x_t B_t, y_t = <C_t, h_t> + skip x_t, gated.  Outputs, states between segments, single tokens.
+#include <type_traits>
+
 #include "selscan_common.h"
+#include "selscan_sums.h"
 
 namespace deer {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f;
 enum { kOutputs, kEnds, kMarks };   // y and the final states; the states behind segments; these and the states in front of every kMarkRows rows
 
-// sum over the Q lanes of a channel
-template <int Q>
-__device__ __forceinline__ float over_lanes(float v) {
-#pragma unroll
-    for (int d = 64 / Q; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return v;
-}
-
-template <typename T, int Q, int WHAT>
+template <typename T, int Q, int WHAT, bool VEC>
 __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, const RestRows rest) {
     using Sh = ScanShape<Q>;
     constexpr int R = Sh::kRows, CW = Sh::kChannels, kAcross = CW / 4, kStep = 256 / kAcross;
@@ -58,73 +52,141 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
         bias[i] = p.bias && i < count ? p.bias[place.ch0 + c4 + i] : 0.0f;
         skip[i] = WHAT == kOutputs && p.skip && i < count ? p.skip[place.ch0 + c4 + i] : 0.0f;
     }
+    const bool has = c4 < place.channels;
+    Places<Sh::kItems> px, pd, pz, py;
+    px.set(p.stride_x, row0, kStep, c4, T{});
+    pd.set(p.stride_dt, row0, kStep, c4, T{});
+    if (WHAT == kOutputs) {
+        pz.set(p.stride_z, row0, kStep, c4, T{});
+        py.set(p.stride_y, row0, kStep, c4, T{});
+    }
+    // the same for B and C: four states of a row
+    constexpr int kBoth = WHAT == kOutputs ? 2 : 1;
+    auto tile_at = [&](const void* first, long long stride, long long r, long long more) { return Tile(reinterpret_cast<const T*>(first) + r * stride + more); };
+    // what a tile reads is asked for while the one in front of it is worked on
+    Four<T, VEC> nx[Sh::kItems], nd[Sh::kItems], nz[Sh::kItems], nb[kBoth][Sh::kQuads];
+    auto ask = [&](long long r) {
+        const int rows = hi - r < R ? (int)(hi - r) : R;
+        const Tile x = tile_at(p.x, p.stride_x, r, place.ch0), d = tile_at(p.dt, p.stride_dt, r, place.ch0);
+#pragma unroll
+        for (int j = 0; j < Sh::kItems; ++j) {
+            const bool on = has && row0 + j * kStep < rows;
+            nx[j].load(x, on ? px.at[j] : kNoColumn, count);
+            nd[j].load(d, on ? pd.at[j] : kNoColumn, count);
+        }
+        if (WHAT == kOutputs && p.z) {
+            const Tile z = tile_at(p.z, p.stride_z, r, place.ch0);
+#pragma unroll
+            for (int j = 0; j < Sh::kItems; ++j) nz[j].load(z, has && row0 + j * kStep < rows ? pz.at[j] : kNoColumn, count);
+        }
+#pragma unroll
+        for (int w = 0; w < kBoth; ++w) {
+            const Tile s = w ? tile_at(p.C, p.stride_C, r, (long long)place.g * p.S) : tile_at(p.B, p.stride_B, r, (long long)place.g * p.S);
+            const long long stride = w ? p.stride_C : p.stride_B;
+#pragma unroll
+            for (int j = 0; j < Sh::kQuads; ++j) {
+                const int e = threadIdx.x + j * 256, qq = e % Q, i = e / Q;
+                nb[w][j].load(s, i < rows && 4 * qq < p.S ? (unsigned)(i * stride + 4 * qq) * (unsigned)sizeof(T) : kNoColumn, p.S - 4 * qq);
+            }
+        }
+    };
+    ask(lo);
     for (long long r = lo; r < hi; r += R) {
         const int rows = hi - r < R ? (int)(hi - r) : R;
-        float x[Sh::kItems][4], z[Sh::kItems][4];
+        Four<T, VEC> x[Sh::kItems], z[Sh::kItems];
 #pragma unroll
         for (int j = 0; j < Sh::kItems; ++j) {
             const int i = row0 + j * kStep;
-            if (i >= rows) continue;
-            float dt[4];
-            const long long at = place.ch0 + c4;
-            load4<T>(x[j], p.x, (r + i) * p.stride_x + at, count, p.vec);
-            load4<T>(dt, p.dt, (r + i) * p.stride_dt + at, count, p.vec);
-            if (WHAT == kOutputs && p.z) load4<T>(z[j], p.z, (r + i) * p.stride_z + at, count, p.vec);
+            x[j] = nx[j];
+            if (WHAT == kOutputs) z[j] = nz[j];
+            Float2 both[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const float raw = dt[v] + bias[v], step = p.softplus ? softplus(raw) : raw;
-                sx[i][c4 + v] = Float2{step, step * x[j][v]};
+                const float raw = nd[j][v] + bias[v], step = p.softplus ? softplus(raw) : raw;
+                both[v] = Float2{step, step * x[j][v]};
+            }
+            if (kStep * Sh::kItems <= R || i < R) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sx[i][c4 + v] = both[v];
             }
         }
 #pragma unroll
-        for (int j = 0; j < Sh::kQuads; ++j) {
-            const int e = threadIdx.x + j * 256, qq = e % Q, i = e / Q % R, which = e / Q / R;
-            if (which > 1 || i >= rows) continue;
-            float v[4];
-            if (which == 0) load4<T>(v, p.B, (r + i) * p.stride_B + (long long)place.g * p.S + 4 * qq, p.S - 4 * qq, p.vec_bc);
-            else load4<T>(v, p.C, (r + i) * p.stride_C + (long long)place.g * p.S + 4 * qq, p.S - 4 * qq, p.vec_bc);
-            bc[i][which][qq] = Float4{v[0], v[1], v[2], v[3]};
-        }
-        __syncthreads();
-        for (int i = 0; i < rows; ++i) {
-            if (r + i == seq.end) {
-                if (WHAT == kOutputs) store_states(p.last, seq.n, l, p.D, p.S, h);
-                seq.next(p.rows, r + i);
-                load_states(h, p.h0, seq.n, l, p.D, p.S);
-                reset = true;
-            }
-            if (WHAT == kMarks && (r + i - lo) % kMarkRows == 0) {
-                const long long mark = place.seg * p.marks_each + (r + i - lo) / kMarkRows;
-                store_states(p.marks, mark, l, p.D, 4 * Q, h);
-                if (q == 0 && l.on) p.mark_steps[mark * p.D + l.ch] = sum_dt;
-            }
-            const Float2 s = sx[i][c];
-            const Float4 b = bc[i][0][q];
-            sum_dt += s.x;
-            float y = 0.0f;
+        for (int w = 0; w < kBoth; ++w)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) h[k] = __builtin_amdgcn_exp2f(s.x * A2[k]) * h[k] + s.y * b[k];
-            if (WHAT != kOutputs) continue;
-            const Float4 cc = bc[i][1][q];
+            for (int j = 0; j < Sh::kQuads; ++j) {
+                const int e = threadIdx.x + j * 256;
+                if (R * Q >= 256 || e < R * Q) bc[e / Q][w][e % Q] = Float4{nb[w][j][0], nb[w][j][1], nb[w][j][2], nb[w][j][3]};
+            }
+        lds_barrier();
+        if (r + R < hi) ask(r + R);
+        // four rows at a time.  WHOLE: all rows of the tile are there, and of one sequence
+        auto go = [&](auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
+#pragma unroll 2
+            for (int i0 = 0; i0 < R; i0 += 4) {
+                if (!WHOLE && i0 >= rows) break;
+                if (WHAT == kMarks && (r + i0 - lo) % kMarkRows == 0) {
+                    if (!WHOLE && r + i0 == seq.end) {
+                        seq.next(p.rows, r + i0);
+                        load_states(h, p.h0, seq.n, l, p.D, p.S);
+                        reset = true;
+                    }
+                    const long long mark = place.seg * p.marks_each + (r + i0 - lo) / kMarkRows;
+                    store_states(p.marks, mark, l, p.D, 4 * Q, h);
+                    if (q == 0 && l.on) p.mark_steps[mark * p.D + l.ch] = sum_dt;
+                }
+                float y[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) y += cc[k] * h[k];
-            y = over_lanes<Q>(y);
-            if (q == 0) sx[i][c].y = y;
-        }
-        __syncthreads();
-        if (WHAT == kOutputs)
+                for (int u = 0; u < 4; ++u) {
+                    const int i = i0 + u;
+                    y[u] = 0.0f;
+                    if (!WHOLE && i >= rows) continue;
+                    if (!WHOLE && r + i == seq.end) {
+                        if (WHAT == kOutputs) store_states(p.last, seq.n, l, p.D, p.S, h);
+                        seq.next(p.rows, r + i);
+                        load_states(h, p.h0, seq.n, l, p.D, p.S);
+                        reset = true;
+                    }
+                    const Float2 s = sx[i][c];
+                    const Float4 b = bc[i][0][q];
+                    if (WHAT != kOutputs) sum_dt += s.x;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) h[k] = __builtin_amdgcn_exp2f(s.x * A2[k]) * h[k] + s.y * b[k];
+                    if (WHAT != kOutputs) continue;
+                    const Float4 cc = bc[i][1][q];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) y[u] += cc[k] * h[k];
+                }
+                if (WHAT != kOutputs) continue;
+                sum_lanes<Q>(y);
+#pragma unroll
+                for (int j = 0; j < lanes_keep<Q>; ++j) sx[i0 + of_lanes<Q>(lane, j)][c].y = y[j];
+            }
+        };
+        if (rows == R && seq.end >= r + R) go(std::true_type{});
+        else go(std::false_type{});
+        lds_barrier();
+        if (WHAT == kOutputs) {
+            const Tile ys = tile_at(p.y, p.stride_y, r, place.ch0);
 #pragma unroll
             for (int j = 0; j < Sh::kItems; ++j) {
                 const int i = row0 + j * kStep;
-                if (i >= rows || count <= 0) continue;
                 float y[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    y[v] = sx[i][c4 + v].y + skip[v] * x[j][v];
-                    if (p.z) y[v] *= fast_silu(z[j][v]);
-                }
-                store4<T>(p.y, (r + i) * p.stride_y + place.ch0 + c4, y, count, p.vec);
+                for (int v = 0; v < 4; ++v) y[v] = sx[i < R ? i : 0][c4 + v].y + skip[v] * x[j][v];
+                if (p.z)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) y[v] *= fast_silu(z[j][v]);
+                Four<T, VEC>::store(ys, has && i < rows ? py.at[j] : kNoColumn, count, y);
             }
+        }
+        // the tile behind a whole one may begin with another sequence
+        if (r + R < hi && r + R == seq.end) {
+            if (WHAT == kOutputs) store_states(p.last, seq.n, l, p.D, p.S, h);
+            seq.next(p.rows, r + R);
+            load_states(h, p.h0, seq.n, l, p.D, p.S);
+            reset = true;
+        }
     }
     if (WHAT == kOutputs) {
         if (hi == seq.end) store_states(p.last, seq.n, l, p.D, p.S, h);
@@ -174,11 +236,16 @@ __global__ __launch_bounds__(256) void selscan_step_kernel(const SelstepParams p
     load_states(a, p.A, 0, l, p.D, p.S);
     if (in) {
         const int g = ch / (p.D / p.G);
-        load4<T>(b, p.B, (long long)n * p.stride_B + (long long)g * p.S + 4 * q, p.S - 4 * q, false);
-        load4<T>(c, p.C, (long long)n * p.stride_C + (long long)g * p.S + 4 * q, p.S - 4 * q, false);
-        x = as_float(reinterpret_cast<const T*>(p.x)[(long long)n * p.stride_x + ch]);
-        dt = as_float(reinterpret_cast<const T*>(p.dt)[(long long)n * p.stride_dt + ch]) + (p.bias ? p.bias[ch] : 0.0f);
-        if (p.z) z = as_float(reinterpret_cast<const T*>(p.z)[(long long)n * p.stride_z + ch]);
+        const T* bs = reinterpret_cast<const T*>(p.B) + (long long)n * p.stride_B + (long long)g * p.S + 4 * q;
+        const T* cs = reinterpret_cast<const T*>(p.C) + (long long)n * p.stride_C + (long long)g * p.S + 4 * q;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            b[k] = 4 * q + k < p.S ? (float)bs[k] : 0.0f;
+            c[k] = 4 * q + k < p.S ? (float)cs[k] : 0.0f;
+        }
+        x = (float)(reinterpret_cast<const T*>(p.x)[(long long)n * p.stride_x + ch]);
+        dt = (float)(reinterpret_cast<const T*>(p.dt)[(long long)n * p.stride_dt + ch]) + (p.bias ? p.bias[ch] : 0.0f);
+        if (p.z) z = (float)(reinterpret_cast<const T*>(p.z)[(long long)n * p.stride_z + ch]);
         if (p.skip) skip = p.skip[ch];
     }
     twice = p.rows.slots ? __syncthreads_or(twice) != 0 : false;
@@ -205,20 +272,20 @@ __global__ __launch_bounds__(256) void selscan_step_kernel(const SelstepParams p
     *y = (T)(p.z ? sum * fast_silu(z) : sum);
 }
 
-template <typename T, int Q>
+template <typename T, int Q, bool VEC>
 hipError_t launch_lanes(const SelscanParams& p, bool marks, hipStream_t stream) {
     const long long seqs = p.rows.packed ? 1 : p.rows.N, segs = seqs * p.segs, cells = (long long)p.D * 4 * Q;
     const dim3 grid((unsigned)(segs * p.G * p.blocks)), block(256);
     RestRows rest{};
     if (p.zero_rest) rest.array[rest.count++] = RestArray{p.y, p.stride_y * (long long)sizeof(T), p.D * (long long)sizeof(T)};
     if (marks) {
-        if (p.rows.T) hipLaunchKernelGGL((selscan_kernel<T, Q, kMarks>), grid, block, 0, stream, p, rest);
+        if (p.rows.T) hipLaunchKernelGGL((selscan_kernel<T, Q, kMarks, VEC>), grid, block, 0, stream, p, rest);
     } else if (p.segs > 1) {
-        hipLaunchKernelGGL((selscan_kernel<T, Q, kEnds>), grid, block, 0, stream, p, rest);
+        hipLaunchKernelGGL((selscan_kernel<T, Q, kEnds, VEC>), grid, block, 0, stream, p, rest);
     }
     if (p.segs > 1) hipLaunchKernelGGL(selscan_join_kernel, dim3((unsigned)((cells * seqs + 255) / 256)), block, 0, stream, p, 4 * Q);
     if (marks) return hipGetLastError();
-    if (p.rows.T) hipLaunchKernelGGL((selscan_kernel<T, Q, kOutputs>), grid, block, 0, stream, p, rest);
+    if (p.rows.T) hipLaunchKernelGGL((selscan_kernel<T, Q, kOutputs, VEC>), grid, block, 0, stream, p, rest);
     if (p.last && (p.rows.bounds || !p.rows.T)) {
         const long long all = (long long)p.rows.N * p.D * p.S / 1024;
         hipLaunchKernelGGL(selscan_empty_kernel, dim3((unsigned)(all < 1 ? 1 : all > 1024 ? 1024 : all)), block, 0, stream, p.rows, (long long)p.D * p.S, p.h0, p.last);
@@ -228,11 +295,11 @@ hipError_t launch_lanes(const SelscanParams& p, bool marks, hipStream_t stream) 
 template <typename T>
 hipError_t launch_type(const SelscanParams& p, bool marks, hipStream_t stream) {
     switch (scan_lanes(p.S)) {
-        case 1: return launch_lanes<T, 1>(p, marks, stream);
-        case 2: return launch_lanes<T, 2>(p, marks, stream);
-        case 4: return launch_lanes<T, 4>(p, marks, stream);
-        case 8: return launch_lanes<T, 8>(p, marks, stream);
-        default: return launch_lanes<T, 16>(p, marks, stream);
+        case 1: return p.vec ? launch_lanes<T, 1, true>(p, marks, stream) : launch_lanes<T, 1, false>(p, marks, stream);
+        case 2: return p.vec ? launch_lanes<T, 2, true>(p, marks, stream) : launch_lanes<T, 2, false>(p, marks, stream);
+        case 4: return p.vec ? launch_lanes<T, 4, true>(p, marks, stream) : launch_lanes<T, 4, false>(p, marks, stream);
+        case 8: return p.vec ? launch_lanes<T, 8, true>(p, marks, stream) : launch_lanes<T, 8, false>(p, marks, stream);
+        default: return p.vec ? launch_lanes<T, 16, true>(p, marks, stream) : launch_lanes<T, 16, false>(p, marks, stream);
     }
 }
 hipError_t launch_any(int dtype, const SelscanParams& p, bool marks, hipStream_t stream) {

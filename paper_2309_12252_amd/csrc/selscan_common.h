@@ -1,5 +1,7 @@
 // Shared by the kernels of the selective scan: shapes, parameters, how a workgroup finds its rows and channels, what is made of the inputs.
 #pragma once
+#include <type_traits>
+
 #include "layer_common.h"
 
 namespace deer {
@@ -10,7 +12,7 @@ template <int Q> struct ScanShape {
     static constexpr int kWave = 64 / Q, kChannels = 256 / Q;
     static constexpr int kRows = Q == 1 ? 8 : Q == 2 ? 16 : Q <= 8 ? 32 : 64;
     static constexpr int kItems = kRows * kChannels >= 1024 ? kRows * kChannels / 1024 : 1;   // of four channels of a row, a lane
-    static constexpr int kQuads = kRows * Q >= 128 ? kRows * Q / 128 : 1;                     // of four states of B or C of a row, a lane
+    static constexpr int kQuads = kRows * Q >= 256 ? kRows * Q / 256 : 1;                    // of four states of B, and of C, of a row, a lane
 };
 constexpr int kMarkRows = 16;   // rows from one kept state to the next in the gradient, and of its tiles
 
@@ -20,7 +22,7 @@ struct SelscanParams {
     SeqRows rows;
     int D, S, G, softplus;
     int per_group, blocks;            // channels of a group; workgroups along the channels of a group
-    bool vec, vec_bc;                 // rows of channels (of states) can be read four at a time
+    bool vec;                         // rows of channels and of states can be read four at a time
     long long stride_x, stride_dt, stride_B, stride_C, stride_z, stride_y;
     const void *x, *dt, *B, *C, *z;
     const float *A, *skip, *bias, *h0;
@@ -43,9 +45,6 @@ struct SelscanParams {
     float *part_bc, *part_A, *part_d; // sums for dB and dC by workgroups, for dA [segment][D][S], for dskip and dbias [segment][2][D]
     bool zero_rest;
 };
-
-template <typename T>
-__device__ __forceinline__ float as_float(T v) { return (float)v; }
 
 struct ScanPlace {
     long long lo, hi;      // rows, absolute
@@ -123,52 +122,85 @@ struct ScanSeq {
     }
 };
 
+constexpr float kLog2e = 1.44269504088896341f;
+
 // log(1 + exp(v)) = max(v, 0) + 2 atanh(e / (2 + e)), e = exp(-|v|): s = e / (2 + e) is at most 1/3, and 2 atanh(s) / s as a polynomial in s^2, fitted at the Chebyshev
 // points of [0, 1/9], is off by 4e-9; so small values keep their digits, which a logarithm of 1 + e would lose.
 __device__ __forceinline__ float softplus(float v) {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504088896341f * __builtin_fabsf(v));
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * __builtin_fabsf(v));
     const float s = e * __builtin_amdgcn_rcpf(2.0f + e), w = s * s;
     float f = 0.28157779574394226f;
     f = f * w + 0.27965158224105835f;
     f = f * w + 0.4002459645271301f;
     f = f * w + 0.6666632294654846f;
     f = f * w + 2.0f;
-    return __builtin_fmaxf(v, 0.0f) + (v != v ? v : s * f);
+    return (v > 0.0f ? v : 0.0f) + s * f;   // (NaN: e is)
 }
 // its derivative, 1 / (1 + exp(-v))
 __device__ __forceinline__ float softplus_slope(float v) {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504088896341f * __builtin_fabsf(v)), r = __builtin_amdgcn_rcpf(1.0f + e);
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * __builtin_fabsf(v)), r = __builtin_amdgcn_rcpf(1.0f + e);
     return v >= 0.0f ? r : e * r;
 }
-__device__ __forceinline__ float fast_silu(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * v)); }
+__device__ __forceinline__ float fast_silu(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
 
-// four channels of a row; those behind `count` are zero
-template <typename T>
-__device__ __forceinline__ void load4(float* to, const void* from, long long at, int count, bool vec) {
-    const T* f = reinterpret_cast<const T*>(from) + at;
-    if (vec && count >= 4) {
-        const vec_t<T, 4> v = *reinterpret_cast<const vec_t<T, 4>*>(f);
+// Four elements that lie side by side, of a row of a tile, by buffer instructions: asked for in one piece (VEC) or one by one, as they came; those behind `count`, and all of a
+// lane without a row (at kNoColumn), are zero, or not written.  No lane takes another path than the others, so nothing waits for what is on its way.
+constexpr long long kScanStride = 1 << 22;   // elements between rows, at most: the 64 of a tile stay below kNoColumn
+struct Tile {
+    __amdgpu_buffer_rsrc_t rsrc;
+    template <typename T>
+    __device__ __forceinline__ Tile(const T* first) : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(first), 0, (int)kNoColumn, 0x00020000)) {}
+};
+template <typename T, bool VEC>
+struct Four {
+    using U2 = unsigned __attribute__((ext_vector_type(2)));
+    using U4 = unsigned __attribute__((ext_vector_type(4)));
+    using Raw = std::conditional_t<sizeof(T) == 4, U4, U2>;
+    std::conditional_t<VEC, Raw, T[4]> v;
+    __device__ __forceinline__ void load(const Tile& t, unsigned at, int count) {
+        if constexpr (VEC) {
+            if constexpr (sizeof(T) == 4) v = __builtin_amdgcn_raw_buffer_load_b128(t.rsrc, at, 0, 0);
+            else v = __builtin_amdgcn_raw_buffer_load_b64(t.rsrc, at, 0, 0);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[i] = as_float(v[i]);
-        return;
+            for (int i = 0; i < 4; ++i) {
+                const unsigned one = i < count ? at + i * (unsigned)sizeof(T) : kNoColumn;
+                if constexpr (sizeof(T) == 4) v[i] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(t.rsrc, one, 0, 0));
+                else v[i] = __builtin_bit_cast(T, (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(t.rsrc, one, 0, 0));
+            }
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) to[i] = i < count ? as_float(f[i]) : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void store4(void* to, long long at, const float* from, int count, bool vec) {
-    T* t = reinterpret_cast<T*>(to) + at;
-    if (vec && count >= 4) {
-        vec_t<T, 4> v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (T)from[i];
-        *reinterpret_cast<vec_t<T, 4>*>(t) = v;
-        return;
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (VEC) return (float)__builtin_bit_cast(vec_t<T, 4>, v)[i];
+        else return (float)v[i];
     }
+    __device__ static __forceinline__ void store(const Tile& t, unsigned at, int count, const float* from) {
+        if constexpr (VEC) {
+            vec_t<T, 4> w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < count) t[i] = (T)from[i];
-}
+            for (int i = 0; i < 4; ++i) w[i] = (T)from[i];
+            if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(U4, w), t.rsrc, at, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(U2, w), t.rsrc, at, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned one = i < count ? at + i * (unsigned)sizeof(T) : kNoColumn;
+                if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, from[i]), t.rsrc, one, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (T)from[i]), t.rsrc, one, 0, 0);
+            }
+        }
+    }
+};
+// A lane's places in a tile: four channels, from c4 on, of rows `step` apart
+template <int N>
+struct Places {
+    unsigned at[N];
+    template <typename T>
+    __device__ __forceinline__ void set(long long stride, int row0, int step, int c4, T) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) at[j] = (unsigned)((row0 + j * step) * stride + c4) * (unsigned)sizeof(T);
+    }
+};
 
 // a lane's four states of its channel, in arrays [.. D][S] and, padded, [.. D][4 Q]
 struct ScanLane {
@@ -185,6 +217,12 @@ __device__ __forceinline__ void store_states(float* to, long long row, const Sca
 #pragma unroll
     for (int k = 0; k < 4; ++k)
         if (l.k0 + k < S) to[(row * D + l.ch) * S + l.k0 + k] = h[k];
+}
+// Between wavefronts of a workgroup, about LDS alone: what has been asked for from memory stays on its way, which __syncthreads() would wait for
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 using Float4 = float __attribute__((ext_vector_type(4)));
 using Float2 = float __attribute__((ext_vector_type(2)));

@@ -2,7 +2,10 @@
 //   dB_t = sum over a group's channels of lam_t dt_t x_t        dC_t = that of dy_t h_t        dx_t = dt_t <lam_t, B_t> + skip dy_t
 //   d dt_t = <lam_t, A a_t h_{t-1}> + x_t <lam_t, B_t>          dA = sum over the rows of dt_t lam_t a_t h_{t-1}
 // dy here after the gate.  The states are computed again, forwards through 16 rows from a kept state; they stay in registers for the way back.
+#include <type_traits>
+
 #include "selscan_common.h"
+#include "selscan_sums.h"
 
 namespace deer {
 
@@ -10,24 +13,10 @@ hipError_t launch_selscan_empty(const SeqRows& rows, long long cells, const floa
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f;
 constexpr int R = kMarkRows;
 
-template <int Q>
-__device__ __forceinline__ float over_lanes(float v) {
-#pragma unroll
-    for (int d = 64 / Q; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return v;
-}
-template <int Q>
-__device__ __forceinline__ float over_channels(float v) {
-#pragma unroll
-    for (int d = 1; d < 64 / Q; d *= 2) v += __shfl_xor(v, d);
-    return v;
-}
-
 // What comes out at the front of a segment for the rows in front of it: a lam of its first row, from zero behind it (or from a sequence's end inside)
-template <typename T, int Q>
+template <typename T, int Q, bool VEC>
 __global__ __launch_bounds__(256) void selscan_fronts_kernel(const SelscanParams p) {
     using Sh = ScanShape<Q>;
     constexpr int CW = Sh::kChannels, kAcross = CW / 4, kStep = 256 / kAcross;
@@ -47,38 +36,72 @@ __global__ __launch_bounds__(256) void selscan_fronts_kernel(const SelscanParams
 #pragma unroll
     for (int k = 0; k < 4; ++k) A2[k] = l.on && l.k0 + k < p.S ? p.A[(long long)l.ch * p.S + l.k0 + k] * kLog2e : 0.0f;
     load_states(r, reset ? p.dlast : nullptr, seq.n, l, p.D, p.S);
+    constexpr int kItems = R * CW >= 1024 ? R * CW / 1024 : 1;
     const int c4 = (threadIdx.x % kAcross) * 4, row0 = threadIdx.x / kAcross, count = place.channels - c4;
     float bias[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) bias[i] = p.bias && i < count ? p.bias[place.ch0 + c4 + i] : 0.0f;
-    for (long long t0 = lo + (hi - lo - 1) / R * R; t0 >= lo; t0 -= R) {
+    Places<kItems> pd, py, pz;
+    pd.set(p.stride_dt, row0, kStep, c4, T{});
+    py.set(p.stride_y, row0, kStep, c4, T{});
+    pz.set(p.stride_z, row0, kStep, c4, T{});
+    auto tile_at = [&](const void* first, long long stride, long long t0, long long more) { return Tile(reinterpret_cast<const T*>(first) + t0 * stride + more); };
+    Four<T, VEC> nd[kItems], ny[kItems], nz[kItems], nc;
+    auto ask = [&](long long t0) {
         const int rows = hi - t0 < R ? (int)(hi - t0) : R;
-        for (int i = row0; i < rows; i += kStep) {
-            float dt[4], dy[4], z[4];
-            const long long at = place.ch0 + c4;
-            load4<T>(dt, p.dt, (t0 + i) * p.stride_dt + at, count, p.vec);
-            load4<T>(dy, p.dy, (t0 + i) * p.stride_y + at, count, p.vec);
-            if (p.z) load4<T>(z, p.z, (t0 + i) * p.stride_z + at, count, p.vec);
+        const Tile d = tile_at(p.dt, p.stride_dt, t0, place.ch0), y = tile_at(p.dy, p.stride_y, t0, place.ch0);
+#pragma unroll
+        for (int j = 0; j < kItems; ++j) {
+            const bool on = count > 0 && row0 + j * kStep < rows;
+            nd[j].load(d, on ? pd.at[j] : kNoColumn, count);
+            ny[j].load(y, on ? py.at[j] : kNoColumn, count);
+        }
+        if (p.z) {
+            const Tile z = tile_at(p.z, p.stride_z, t0, place.ch0);
+#pragma unroll
+            for (int j = 0; j < kItems; ++j) nz[j].load(z, count > 0 && row0 + j * kStep < rows ? pz.at[j] : kNoColumn, count);
+        }
+        const int i = threadIdx.x / Q, s = 4 * (threadIdx.x % Q);
+        nc.load(tile_at(p.C, p.stride_C, t0, (long long)place.g * p.S), i < rows && s < p.S ? (unsigned)(i * p.stride_C + s) * (unsigned)sizeof(T) : kNoColumn, p.S - s);
+    };
+    const long long t_last = lo + (hi - lo - 1) / R * R;
+    ask(t_last);
+    for (long long t0 = t_last; t0 >= lo; t0 -= R) {
+        const int rows = hi - t0 < R ? (int)(hi - t0) : R;
+#pragma unroll
+        for (int j = 0; j < kItems; ++j) {
+            const int i = row0 + j * kStep;
+            Float2 both[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const float raw = dt[v] + bias[v];
-                sx[i][c4 + v] = Float2{p.softplus ? softplus(raw) : raw, p.z ? dy[v] * fast_silu(z[v]) : dy[v]};
+                const float raw = nd[j][v] + bias[v];
+                both[v] = Float2{p.softplus ? softplus(raw) : raw, ny[j][v]};
             }
-        }
-        for (int e = threadIdx.x; e < rows * Q; e += 256) {
-            float v[4];
-            load4<T>(v, p.C, (t0 + e / Q) * p.stride_C + (long long)place.g * p.S + 4 * (e % Q), p.S - 4 * (e % Q), p.vec_bc);
-            cs[e / Q][e % Q] = Float4{v[0], v[1], v[2], v[3]};
-        }
-        __syncthreads();
-        for (int i = rows - 1; i >= 0; --i) {
-            const Float2 s = sx[i][c];
-            const Float4 cc = cs[i][q];
-            sum_dt += s.x;
+            if (p.z)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) r[k] = __builtin_amdgcn_exp2f(s.x * A2[k]) * (r[k] + cc[k] * s.y);
+                for (int v = 0; v < 4; ++v) both[v].y *= fast_silu(nz[j][v]);
+            if (kStep * kItems <= R || i < R)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sx[i][c4 + v] = both[v];
         }
-        __syncthreads();
+        if (R * Q >= 256 || threadIdx.x < R * Q) cs[threadIdx.x / Q][threadIdx.x % Q] = Float4{nc[0], nc[1], nc[2], nc[3]};
+        lds_barrier();
+        if (t0 > lo) ask(t0 - R);
+        auto go = [&](auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
+#pragma unroll
+            for (int i = R - 1; i >= 0; --i) {
+                if (!WHOLE && i >= rows) continue;
+                const Float2 s = sx[i][c];
+                const Float4 cc = cs[i][q];
+                sum_dt += s.x;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) r[k] = __builtin_amdgcn_exp2f(s.x * A2[k]) * (r[k] + cc[k] * s.y);
+            }
+        };
+        if (rows == R) go(std::true_type{});
+        else go(std::false_type{});
+        lds_barrier();
     }
     store_states(p.rlocal, place.seg, l, p.D, 4 * Q, r);
     if (q == 0 && l.on) p.rsteps[place.seg * p.D + l.ch] = sum_dt;
@@ -99,13 +122,13 @@ __global__ __launch_bounds__(256) void selscan_rjoin_kernel(const SelscanParams 
     }
 }
 
-template <typename T, int Q>
-__global__ __launch_bounds__(256) void selscan_grad_kernel(const SelscanParams p, const RestRows rest) {
+template <typename T, int Q, bool VEC>
+__global__ __launch_bounds__(256, 2) void selscan_grad_kernel(const SelscanParams p, const RestRows rest) {
     using Sh = ScanShape<Q>;
     constexpr int CW = Sh::kChannels, kAcross = CW / 4, kStep = 256 / kAcross, kItems = R * CW >= 1024 ? R * CW / 1024 : 1;
     __shared__ Float4 it[R][CW];         // dt, dt x, dy, y; on the way back <lam, B> and <lam, A a h> in the places of dt x and dy
     __shared__ Float4 bc[R][2][Q];
-    __shared__ float red[4][R][2][4 * Q];   // of a wavefront: lam dt x and dy h summed over its channels
+    __shared__ float red[4][R][Q][8];    // of a wavefront: lam dt x and dy h of four states, summed over its channels
     clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
     const ScanPlace place = scan_place<Q>(p);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q = lane / Sh::kWave, c = wave * Sh::kWave + lane % Sh::kWave;
@@ -131,138 +154,213 @@ __global__ __launch_bounds__(256) void selscan_grad_kernel(const SelscanParams p
         seq.at(p.rows, place, hi - 1);
         if (hi == seq.end) load_states(r, p.dlast, seq.n, l, p.D, p.S);
         else load_states(r, p.rcarry, place.seg, l, p.D, 4 * Q);
-        for (long long t0 = lo + (hi - lo - 1) / R * R; t0 >= lo; t0 -= R) {
+        // what a tile reads is asked for while the tile behind it is worked on
+        Places<kItems> px, pd, py, pz;
+        px.set(p.stride_x, row0, kStep, c4, T{});
+        pd.set(p.stride_dt, row0, kStep, c4, T{});
+        py.set(p.stride_y, row0, kStep, c4, T{});
+        pz.set(p.stride_z, row0, kStep, c4, T{});
+        auto tile_at = [&](const void* first, long long stride, long long t0, long long more) { return Tile(reinterpret_cast<const T*>(first) + t0 * stride + more); };
+        Four<T, VEC> nx[kItems], nd[kItems], ny[kItems], nz[kItems], nb[2];
+        float mark[4], steps = 0.0f;
+        const int quad_row = threadIdx.x / Q, quad = 4 * (threadIdx.x % Q);
+        auto ask = [&](long long t0) {
             const int rows = hi - t0 < R ? (int)(hi - t0) : R;
-            float x[kItems][4], raw[kItems][4], z[kItems][4], dy[kItems][4];
+            const Tile x = tile_at(p.x, p.stride_x, t0, place.ch0), d = tile_at(p.dt, p.stride_dt, t0, place.ch0), y = tile_at(p.dy, p.stride_y, t0, place.ch0);
+#pragma unroll
+            for (int j = 0; j < kItems; ++j) {
+                const bool on = count > 0 && row0 + j * kStep < rows;
+                nx[j].load(x, on ? px.at[j] : kNoColumn, count);
+                nd[j].load(d, on ? pd.at[j] : kNoColumn, count);
+                ny[j].load(y, on ? py.at[j] : kNoColumn, count);
+            }
+            if (p.z) {
+                const Tile z = tile_at(p.z, p.stride_z, t0, place.ch0);
+#pragma unroll
+                for (int j = 0; j < kItems; ++j) nz[j].load(z, count > 0 && row0 + j * kStep < rows ? pz.at[j] : kNoColumn, count);
+            }
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const long long stride = w ? p.stride_C : p.stride_B;
+                nb[w].load(tile_at(w ? p.C : p.B, stride, t0, (long long)place.g * p.S),
+                           quad_row < rows && quad < p.S ? (unsigned)(quad_row * stride + quad) * (unsigned)sizeof(T) : kNoColumn, p.S - quad);
+            }
+            const long long at = place.seg * p.marks_each + (t0 - lo) / R;
+            const __amdgpu_buffer_rsrc_t m = __builtin_amdgcn_make_buffer_rsrc(p.marks + at * p.D * 4 * Q, 0, (int)kNoColumn, 0x00020000);
+            const Float4 four = __builtin_bit_cast(Float4, __builtin_amdgcn_raw_buffer_load_b128(m, l.on ? (unsigned)(l.ch * 4 * Q + l.k0) * 4u : kNoColumn, 0, 0));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mark[k] = four[k];
+            if (p.segs > 1) steps = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(Tile(p.mark_steps + at * p.D).rsrc, l.on ? l.ch * 4u : kNoColumn, 0, 0));
+        };
+        float carry[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (p.segs > 1) {
+            ScanSeq first = seq;
+            if (first.start > lo) first.at(p.rows, place, lo);
+            if (first.start < lo) load_states(carry, p.carry, place.seg, l, p.D, 4 * Q);
+        }
+        const long long t_last = lo + (hi - lo - 1) / R * R;
+        ask(t_last);
+        for (long long t0 = t_last; t0 >= lo; t0 -= R) {
+            const int rows = hi - t0 < R ? (int)(hi - t0) : R;
+            Four<T, VEC> x[kItems], z[kItems], dy[kItems], dt_in[kItems];
 #pragma unroll
             for (int j = 0; j < kItems; ++j) {
                 const int i = row0 + j * kStep;
-                if (i >= rows) continue;
-                const long long at = place.ch0 + c4;
-                load4<T>(x[j], p.x, (t0 + i) * p.stride_x + at, count, p.vec);
-                load4<T>(raw[j], p.dt, (t0 + i) * p.stride_dt + at, count, p.vec);
-                load4<T>(dy[j], p.dy, (t0 + i) * p.stride_y + at, count, p.vec);
-                if (p.z) load4<T>(z[j], p.z, (t0 + i) * p.stride_z + at, count, p.vec);
+                x[j] = nx[j];
+                dt_in[j] = nd[j];
+                dy[j] = ny[j];
+                z[j] = nz[j];
+                Float4 all[4];
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    raw[j][v] += bias[v];
-                    const float dt = p.softplus ? softplus(raw[j][v]) : raw[j][v];
-                    it[i][c4 + v] = Float4{dt, dt * x[j][v], p.z ? dy[j][v] * fast_silu(z[j][v]) : dy[j][v], 0.0f};
+                    const float raw = dt_in[j][v] + bias[v], dt = p.softplus ? softplus(raw) : raw;
+                    all[v] = Float4{dt, dt * x[j][v], dy[j][v], 0.0f};
                 }
+                if (p.z)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) all[v].z *= fast_silu(z[j][v]);
+                if (kStep * kItems <= R || i < R)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) it[i][c4 + v] = all[v];
             }
-            for (int e = threadIdx.x; e < rows * 2 * Q; e += 256) {
-                const int qq = e % Q, which = e / Q % 2, i = e / Q / 2;
-                float v[4];
-                if (which == 0) load4<T>(v, p.B, (t0 + i) * p.stride_B + (long long)place.g * p.S + 4 * qq, p.S - 4 * qq, p.vec_bc);
-                else load4<T>(v, p.C, (t0 + i) * p.stride_C + (long long)place.g * p.S + 4 * qq, p.S - 4 * qq, p.vec_bc);
-                bc[i][which][qq] = Float4{v[0], v[1], v[2], v[3]};
+            if (R * Q >= 256 || threadIdx.x < R * Q) {
+                bc[quad_row][0][threadIdx.x % Q] = Float4{nb[0][0], nb[0][1], nb[0][2], nb[0][3]};
+                bc[quad_row][1][threadIdx.x % Q] = Float4{nb[1][0], nb[1][1], nb[1][2], nb[1][3]};
             }
-            __syncthreads();
-            // forwards from the state in front of the tile
             ScanSeq first = seq;
             if (first.start > t0) first.back(p.rows, t0);
-            float before[4], a[R][4], h[R][4];
-            {
-                const long long mark = place.seg * p.marks_each + (t0 - lo) / R;
-                load_states(before, p.marks, mark, l, p.D, 4 * Q);
-                if (p.segs > 1 && first.start < lo) {
-                    float carry[4];
-                    load_states(carry, p.carry, place.seg, l, p.D, 4 * Q);
-                    const float steps = l.on ? p.mark_steps[mark * p.D + l.ch] : 0.0f;
+            float before[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) before[k] += __builtin_amdgcn_exp2f(steps * A[k] * kLog2e) * carry[k];
-                }
+            for (int k = 0; k < 4; ++k) before[k] = mark[k];
+            if (p.segs > 1 && first.start < lo) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) before[k] += __builtin_amdgcn_exp2f(steps * A[k] * kLog2e) * carry[k];
             }
-            ScanSeq now = first;
+            lds_barrier();
+            if (t0 > lo) ask(t0 - R);
+            // forwards from the state in front of the tile (that of a sequence that begins with it is its initial one), and back.  WHOLE: 16 rows of one sequence
+            auto there_and_back = [&](auto whole) {
+                constexpr bool WHOLE = decltype(whole)::value;
+                float h[R][4];
+                ScanSeq now = first;
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                if (i >= rows) continue;
-                float in[4];
+                for (int i0 = 0; i0 < R; i0 += 4) {
+                    if (!WHOLE && i0 >= rows) continue;
+                    float y[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) in[k] = i ? h[i ? i - 1 : 0][k] : before[k];
-                if (t0 + i == now.end) {
-                    now.next(p.rows, t0 + i);
-                    load_states(in, p.h0, now.n, l, p.D, p.S);
-                }
-                const Float4 s = it[i][c];
-                const Float4 b = bc[i][0][q], cc = bc[i][1][q];
-                float y = 0.0f;
+                    for (int u = 0; u < 4; ++u) {
+                        const int i = i0 + u;
+                        y[u] = 0.0f;
+                        if (!WHOLE && i >= rows) continue;
+                        float in[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    a[i][k] = __builtin_amdgcn_exp2f(s.x * (A[k] * kLog2e));
-                    h[i][k] = a[i][k] * in[k] + s.y * b[k];
-                    y += cc[k] * h[i][k];
-                }
-                if (p.z) {
-                    y = over_lanes<Q>(y);
-                    if (q == 0) it[i][c].w = y;
-                }
-            }
-            // and back
+                        for (int k = 0; k < 4; ++k) in[k] = i ? h[i ? i - 1 : 0][k] : before[k];
+                        if (!WHOLE && t0 + i == now.end) {
+                            now.next(p.rows, t0 + i);
+                            load_states(in, p.h0, now.n, l, p.D, p.S);
+                        }
+                        const Float4 s = it[i][c];
+                        const Float4 b = bc[i][0][q];
 #pragma unroll
-            for (int i = R - 1; i >= 0; --i) {
-                if (i >= rows) continue;
-                if (t0 + i < now.start) {
-                    now.back(p.rows, t0 + i);
-                    load_states(r, p.dlast, now.n, l, p.D, p.S);
-                }
-                float in[4];
+                        for (int k = 0; k < 4; ++k) {
+                            h[i][k] = __builtin_amdgcn_exp2f(s.x * (A[k] * kLog2e)) * in[k] + s.y * b[k];
+                        }
+                        if (p.z) {
+                            const Float4 cc = bc[i][1][q];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) in[k] = i ? h[i ? i - 1 : 0][k] : before[k];
-                const bool begins = t0 + i == now.start;
-                if (begins) load_states(in, p.h0, now.n, l, p.D, p.S);
-                const Float4 s = it[i][c];
-                const Float4 b = bc[i][0][q], cc = bc[i][1][q];
-                float read = 0.0f, ddt = 0.0f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float lam = r[k] + cc[k] * s.z;
-                    const float dB = over_channels<Q>(lam * s.y), dC = over_channels<Q>(s.z * h[i][k]);
-                    if (lane % Sh::kWave == 0) {
-                        red[wave][i][0][4 * q + k] = dB;
-                        red[wave][i][1][4 * q + k] = dC;
+                            for (int k = 0; k < 4; ++k) y[u] += cc[k] * h[i][k];
+                        }
                     }
-                    read += lam * b[k];
-                    r[k] = a[i][k] * lam;
-                    const float g = r[k] * in[k];
-                    dA[k] += s.x * g;
-                    ddt += A[k] * g;
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (p.z) {
+                        sum_lanes<Q>(y);
+#pragma unroll
+                        for (int j = 0; j < lanes_keep<Q>; ++j) it[i0 + of_lanes<Q>(lane, j)][c].w = y[j];
+                    }
                 }
-                read = over_lanes<Q>(read);
-                ddt = over_lanes<Q>(ddt);
-                if (q == 0) {
-                    it[i][c].y = read;
-                    it[i][c].z = ddt;
+#pragma unroll
+                for (int i0 = R - 2; i0 >= 0; i0 -= 2) {
+                    if (!WHOLE && i0 >= rows) continue;
+                    float two[4];   // <lam, B> and <lam, A a h> of both rows
+#pragma unroll
+                    for (int u = 1; u >= 0; --u) {
+                        const int i = i0 + u;
+                        two[2 * u] = two[2 * u + 1] = 0.0f;
+                        if (!WHOLE && i >= rows) continue;
+                        float in[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) in[k] = i ? h[i ? i - 1 : 0][k] : before[k];
+                        bool begins = false;
+                        if (!WHOLE) {
+                            if (t0 + i < now.start) {
+                                now.back(p.rows, t0 + i);
+                                load_states(r, p.dlast, now.n, l, p.D, p.S);
+                            }
+                            begins = t0 + i == now.start;
+                            if (begins) load_states(in, p.h0, now.n, l, p.D, p.S);
+                        }
+                        const Float4 s = it[i][c];
+                        const Float4 b = bc[i][0][q], cc = bc[i][1][q];
+                        float over[8];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float lam = r[k] + cc[k] * s.z;
+                            over[k] = lam * s.y;
+                            over[4 + k] = s.z * h[i][k];
+                            two[2 * u] += lam * b[k];
+                            r[k] = __builtin_amdgcn_exp2f(s.x * (A[k] * kLog2e)) * lam;
+                            const float g = r[k] * in[k];
+                            dA[k] += s.x * g;
+                            two[2 * u + 1] += A[k] * g;
+                        }
+                        sum_channels<Q>(over);
+                        if ((lane & channels_same<Q>) == 0) {
+#pragma unroll
+                            for (int j = 0; j < channels_keep<Q>; ++j) red[wave][i][q][channels_first<Q>(lane) + j] = over[j];
+                        }
+                        if (!WHOLE && begins) store_states(p.dh0, now.n, l, p.D, p.S, r);
+                    }
+                    sum_lanes<Q>(two);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int j = 0; j < lanes_keep<Q>; ++j) {
+                        const int e = of_lanes<Q>(lane, j);
+                        reinterpret_cast<float*>(&it[i0 + (e >> 1)][c])[1 + (e & 1)] = two[j];
+                    }
                 }
-                if (begins) store_states(p.dh0, now.n, l, p.D, p.S, r);
-            }
+                if (WHOLE && first.start == t0) store_states(p.dh0, first.n, l, p.D, p.S, r);
+            };
+            if (rows == R && first.start <= t0 && first.end >= t0 + R) there_and_back(std::true_type{});
+            else there_and_back(std::false_type{});
             seq = first;
             if (t0 > lo && seq.start == t0) {   // the rows in front are another sequence's
                 seq.back(p.rows, t0 - 1);
                 load_states(r, p.dlast, seq.n, l, p.D, p.S);
             }
-            __syncthreads();
+            lds_barrier();
+            {
+                const Tile dxs = tile_at(p.dx, p.stride_x, t0, place.ch0), dds = tile_at(p.ddt, p.stride_dt, t0, place.ch0), dzs = tile_at(p.z ? p.dz : p.dx, p.stride_z, t0, place.ch0);
 #pragma unroll
-            for (int j = 0; j < kItems; ++j) {
-                const int i = row0 + j * kStep;
-                if (i >= rows || count <= 0) continue;
-                float dx[4], ddt[4], dz[4];
+                for (int j = 0; j < kItems; ++j) {
+                    const int i = row0 + j * kStep;
+                    const bool on = count > 0 && i < rows;
+                    float dx[4], ddt[4], dz[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const Float4 s = it[i][c4 + v];
-                    float gate = 1.0f, slope = 0.0f;
-                    if (p.z) silu_both<BF16>(z[j][v], gate, slope);
-                    const float out = dy[j][v] * gate;
-                    dx[v] = s.x * s.y + skip[v] * out;
-                    ddt[v] = (s.z + x[j][v] * s.y) * (p.softplus ? softplus_slope(raw[j][v]) : 1.0f);
-                    dz[v] = dy[j][v] * (s.w + skip[v] * x[j][v]) * slope;
-                    dskip[v] += out * x[j][v];
-                    dbias[v] += ddt[v];
+                    for (int v = 0; v < 4; ++v) {
+                        const Float4 s = it[i < R ? i : 0][c4 + v];
+                        float gate = 1.0f, slope = 0.0f;
+                        if (p.z) silu_both<BF16>(z[j][v], gate, slope);
+                        const float out = dy[j][v] * gate;
+                        dx[v] = s.x * s.y + skip[v] * out;
+                        ddt[v] = (s.z + x[j][v] * s.y) * (p.softplus ? softplus_slope(dt_in[j][v] + bias[v]) : 1.0f);
+                        dz[v] = dy[j][v] * (s.w + skip[v] * x[j][v]) * slope;
+                        dskip[v] += out * x[j][v];
+                        dbias[v] += on ? ddt[v] : 0.0f;
+                    }
+                    Four<T, VEC>::store(dxs, on ? px.at[j] : kNoColumn, count, dx);
+                    Four<T, VEC>::store(dds, on ? pd.at[j] : kNoColumn, count, ddt);
+                    if (p.z) Four<T, VEC>::store(dzs, on ? pz.at[j] : kNoColumn, count, dz);
                 }
-                const long long at = place.ch0 + c4;
-                store4<T>(p.dx, (t0 + i) * p.stride_x + at, dx, count, p.vec);
-                store4<T>(p.ddt, (t0 + i) * p.stride_dt + at, ddt, count, p.vec);
-                if (p.z) store4<T>(p.dz, (t0 + i) * p.stride_z + at, dz, count, p.vec);
             }
             for (int e = threadIdx.x; e < rows * 8 * Q; e += 256) {
                 const int i = e / (8 * Q), k = e % (8 * Q);
@@ -279,10 +377,10 @@ __global__ __launch_bounds__(256) void selscan_grad_kernel(const SelscanParams p
     float* sums = reinterpret_cast<float*>(&it[0][0]);
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int v = 0; v < 4; ++v) sums[row0 * CW + c4 + v] = w ? dbias[v] : dskip[v];
-        __syncthreads();
+        lds_barrier();
         for (int i = threadIdx.x; i < place.channels; i += 256) {
             float sum = 0.0f;
             for (int f = 0; f < kStep; ++f) sum += sums[f * CW + i];
@@ -304,7 +402,7 @@ __global__ __launch_bounds__(256) void selscan_bc_kernel(const SelscanParams p, 
                               : row % p.rows.T >= clamp_row(p.rows.bounds[row / p.rows.T], p.rows.T))
                 continue;
         }
-        const float* f = p.part_bc + ((row * p.G + g) * 2 + which) * SP + k;
+        const float* f = p.part_bc + (row * p.G + g) * 2 * SP + (k / 4) * 8 + which * 4 + k % 4;
         float sum = 0.0f;
         for (int b = 0; b < p.blocks; ++b) sum += f[b * step];
         if (which == 0) reinterpret_cast<T*>(p.dB)[row * p.stride_B + g * p.S + k] = (T)sum;
@@ -312,7 +410,7 @@ __global__ __launch_bounds__(256) void selscan_bc_kernel(const SelscanParams p, 
     }
 }
 
-template <typename T, int Q>
+template <typename T, int Q, bool VEC>
 hipError_t launch_lanes(const SelscanParams& p, hipStream_t stream) {
     const long long seqs = p.rows.packed ? 1 : p.rows.N, segs = seqs * p.segs, cells = (long long)p.D * 4 * Q, rows = p.rows.T * seqs;
     const dim3 grid((unsigned)(segs * p.G * p.blocks)), block(256);
@@ -327,37 +425,30 @@ hipError_t launch_lanes(const SelscanParams& p, hipStream_t stream) {
         if (p.z) add(p.dz, p.stride_z, p.D);
     }
     if (p.segs > 1) {
-        hipLaunchKernelGGL((selscan_fronts_kernel<T, Q>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((selscan_fronts_kernel<T, Q, VEC>), grid, block, 0, stream, p);
         hipLaunchKernelGGL(selscan_rjoin_kernel, dim3((unsigned)((cells * seqs + 255) / 256)), block, 0, stream, p, 4 * Q);
     }
     if (p.rows.T) {
-        hipLaunchKernelGGL((selscan_grad_kernel<T, Q>), grid, block, 0, stream, p, rest);
+        hipLaunchKernelGGL((selscan_grad_kernel<T, Q, VEC>), grid, block, 0, stream, p, rest);
         const long long want = rows * p.G * 2 * p.S / 1024;
         hipLaunchKernelGGL((selscan_bc_kernel<T>), dim3((unsigned)(want < 1 ? 1 : want > 8192 ? 8192 : want)), block, 0, stream, p, 4 * Q);
     }
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && p.dh0 && (p.rows.bounds || !p.rows.T)) err = launch_selscan_empty(p.rows, (long long)p.D * p.S, p.dlast, p.dh0, stream);
     if (err != hipSuccess) return err;
-    SumInto into{};
-    into.each = p.D * p.S;
-    into.to[0] = p.dA;
-    into.stride[0] = 1;
-    err = launch_sum_tiles(false, p.part_A, p.rows.T ? segs : 0, p.D * p.S, into, stream);
+    const long long parts = p.rows.T ? segs : 0;
+    err = launch_sum_tiles(false, p.part_A, parts, SumInto{p.dA, nullptr, p.D * p.S, 1, false}, stream);
     if (err != hipSuccess || (!p.dskip && !p.dbias)) return err;
-    into.each = p.D;
-    into.to[0] = p.dskip;
-    into.to[1] = p.dbias;
-    into.stride[1] = 1;
-    return launch_sum_tiles(false, p.part_d, p.rows.T ? segs : 0, 2 * p.D, into, stream);
+    return launch_sum_tiles(false, p.part_d, parts, SumInto{p.dskip, p.dbias, p.D, 1, true}, stream);
 }
 template <typename T>
 hipError_t launch_type(const SelscanParams& p, hipStream_t stream) {
     switch (scan_lanes(p.S)) {
-        case 1: return launch_lanes<T, 1>(p, stream);
-        case 2: return launch_lanes<T, 2>(p, stream);
-        case 4: return launch_lanes<T, 4>(p, stream);
-        case 8: return launch_lanes<T, 8>(p, stream);
-        default: return launch_lanes<T, 16>(p, stream);
+        case 1: return p.vec ? launch_lanes<T, 1, true>(p, stream) : launch_lanes<T, 1, false>(p, stream);
+        case 2: return p.vec ? launch_lanes<T, 2, true>(p, stream) : launch_lanes<T, 2, false>(p, stream);
+        case 4: return p.vec ? launch_lanes<T, 4, true>(p, stream) : launch_lanes<T, 4, false>(p, stream);
+        case 8: return p.vec ? launch_lanes<T, 8, true>(p, stream) : launch_lanes<T, 8, false>(p, stream);
+        default: return p.vec ? launch_lanes<T, 16, true>(p, stream) : launch_lanes<T, 16, false>(p, stream);
     }
 }
 

@@ -293,16 +293,7 @@ hipError_t launch_taps(bool grad, const ConvParams& p, hipStream_t stream) {
     hipLaunchKernelGGL((shortconv_grad_kernel<T, V, M>), grid, block, 0, stream, p, l, rest, blocks);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    SumInto into{};
-    into.each = p.D;
-    using S = wide_t<T>;
-    for (int j = 0; j < p.W; ++j) {
-        into.to[j] = reinterpret_cast<S*>(p.dw) + j;
-        into.stride[j] = p.W;
-    }
-    into.to[p.W] = p.dbias;
-    into.stride[p.W] = 1;
-    return launch_sum_tiles(sizeof(S) == 8, p.part, tiles, (p.W + 1) * p.D, into, stream);
+    return launch_sum_tiles(sizeof(wide_t<T>) == 8, p.part, tiles, SumInto{p.dw, p.dbias, p.D, p.W, true}, stream);
 }
 
 template <typename T>
@@ -334,13 +325,15 @@ __global__ __launch_bounds__(256) void sum_tiles_kernel(const S* part, long long
     sum = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum += sums[i][threadIdx.x];
-    S* to = reinterpret_cast<S*>(into.to[c / into.each]);
-    if (to) to[(long long)(c % into.each) * into.stride[c / into.each]] = (S)sum;
+    const int row = c / into.each, at = c % into.each;
+    S* to = reinterpret_cast<S*>(row < into.many ? into.first : into.second);
+    if (to) to[row < into.many ? (long long)at * into.many + row : at] = (S)sum;
 }
 
 }  // namespace
 
-hipError_t launch_sum_tiles(bool wide, const void* part, long long tiles, int cols, const SumInto& into, hipStream_t stream) {
+hipError_t launch_sum_tiles(bool wide, const void* part, long long tiles, const SumInto& into, hipStream_t stream) {
+    const int cols = into.each * (into.many + (into.last ? 1 : 0));
     const dim3 grid((cols + 15) / 16), block(256);
     if (wide) hipLaunchKernelGGL((sum_tiles_kernel<double>), grid, block, 0, stream, reinterpret_cast<const double*>(part), tiles, cols, into);
     else hipLaunchKernelGGL((sum_tiles_kernel<float>), grid, block, 0, stream, reinterpret_cast<const float*>(part), tiles, cols, into);
