@@ -404,6 +404,7 @@ __global__ __launch_bounds__(256) void selscan_bc_kernel(const SelscanParams p, 
         }
         const float* f = p.part_bc + (row * p.G + g) * 2 * SP + (k / 4) * 8 + which * 4 + k % 4;
         float sum = 0.0f;
+#pragma unroll 8
         for (int b = 0; b < p.blocks; ++b) sum += f[b * step];
         if (which == 0) reinterpret_cast<T*>(p.dB)[row * p.stride_B + g * p.S + k] = (T)sum;
         else reinterpret_cast<T*>(p.dC)[row * p.stride_C + g * p.S + k] = (T)sum;
@@ -430,8 +431,8 @@ hipError_t launch_lanes(const SelscanParams& p, hipStream_t stream) {
     }
     if (p.rows.T) {
         hipLaunchKernelGGL((selscan_grad_kernel<T, Q, VEC>), grid, block, 0, stream, p, rest);
-        const long long want = rows * p.G * 2 * p.S / 1024;
-        hipLaunchKernelGGL((selscan_bc_kernel<T>), dim3((unsigned)(want < 1 ? 1 : want > 8192 ? 8192 : want)), block, 0, stream, p, 4 * Q);
+        const long long want = rows * p.G * 2 * p.S / 256;
+        hipLaunchKernelGGL((selscan_bc_kernel<T>), dim3((unsigned)(want < 1 ? 1 : want > 16384 ? 16384 : want)), block, 0, stream, p, 4 * Q);
     }
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && p.dh0 && (p.rows.bounds || !p.rows.T)) err = launch_selscan_empty(p.rows, (long long)p.D * p.S, p.dlast, p.dh0, stream);
