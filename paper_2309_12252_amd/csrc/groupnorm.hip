@@ -1,4 +1,5 @@
 // Group norm with an activation and a gate, channels last: forward and gradient, statistics over rows or over sequences.
+#include "lane_sums.h"
 #include "layer_common.h"
 
 namespace deer {
@@ -17,6 +18,23 @@ __device__ __forceinline__ void store_narrow(void* to, long long at, const wide_
     for (int i = 0; i < V; ++i) vec_set<T, V>(v, i, (T)from[i]);
     *reinterpret_cast<vec_t<T, V>*>(reinterpret_cast<T*>(to) + at) = v;
 }
+
+// One element: y of x, or du = dL/du and what else its gradient needs
+template <typename T>
+struct Through {
+    using S = wide_t<T>;
+    S u, dv, dz;
+    __device__ __forceinline__ S operator()(const NormParams& p, S x, S z, S dy, S mean, S rstd, S w, S b) {
+        u = (x - mean) * rstd;
+        const S pre = u * w + b;
+        S f = pre, slope = S(1), gate = S(1), gslope = S(0);
+        if (p.act == DEER_ACT_SILU) silu_both<T>(pre, f, slope);
+        if (p.z) silu_both<T>(z, gate, gslope);
+        dv = dy * gate * slope;
+        dz = dy * f * gslope;
+        return dv * w;
+    }
+};
 
 // ---- every row by itself ----
 // How a workgroup goes over rows and groups: L lanes (a power of two) have a group of a row, M vectors of V channels each; groups side by side, then rows
@@ -215,6 +233,148 @@ __global__ __launch_bounds__(256) void rownorm_kernel(const NormParams p, const 
 }
 
 
+// sums over the L lanes of a group, of B values side by side, the same for all lanes
+template <typename S, int B>
+__device__ __forceinline__ void lanes_sum(S (&v)[B], int L) {
+    if constexpr (sizeof(S) == 8) {
+        for (int d = 1; d < L; d *= 2)
+#pragma unroll
+            for (int b = 0; b < B; ++b) v[b] += __shfl_xor(v[b], d);
+    } else {
+        if (L > 1)
+#pragma unroll
+            for (int b = 0; b < B; ++b) v[b] = dpp_add<kSwapLanes>(v[b]);
+        if (L > 2)
+#pragma unroll
+            for (int b = 0; b < B; ++b) v[b] = dpp_add<kSwapPairs>(v[b]);
+        if (L > 4)
+#pragma unroll
+            for (int b = 0; b < B; ++b) v[b] = dpp_add<kHalfMirror>(v[b]);
+        if (L > 8)
+#pragma unroll
+            for (int b = 0; b < B; ++b) v[b] = dpp_add<kMirror>(v[b]);
+        if (L > 16)
+#pragma unroll
+            for (int b = 0; b < B; ++b) v[b] = sum_rows(v[b], v[b]);
+        if (L > 32)
+#pragma unroll
+            for (int b = 0; b < B; ++b) v[b] = sum_halves(v[b], v[b]);
+    }
+}
+
+// Groups of at most 64 vectors, a vector a lane, B rows at a time so that their loads and sums overlap.  Memory bound.
+template <typename T, int V, int B, bool GRAD>
+__global__ __launch_bounds__(256) void rownorm_few_kernel(const NormParams p, const RowShape s, const RestRows rest, long long rows_each) {
+    using S = wide_t<T>;
+    const int unit = threadIdx.x / s.L, l = threadIdx.x % s.L, n = p.D / p.G, lane_row = unit / s.groups;
+    const int g = blockIdx.x % s.blocks * s.groups + unit % s.groups;
+    const bool has = g < p.G && l * V < n;
+    const int ch = has ? g * n + l * V : 0;
+    const long long block = blockIdx.x / s.blocks, rows = p.rows.T * (p.rows.packed ? 1 : p.rows.N), lo = block * rows_each, hi = lo + rows_each < rows ? lo + rows_each : rows;
+    const long long from = p.rows.packed ? clamp_row(p.rows.bounds[0], p.rows.T) : 0, to = p.rows.packed ? clamp_row(p.rows.bounds[p.rows.N], p.rows.T) : rows;
+    const bool lengths = !p.rows.packed && p.rows.bounds;
+    const S share = S(1) / S(n);
+    S w[V], bias[V], dw[V], db[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        w[v] = p.w && has ? reinterpret_cast<const S*>(p.w)[ch + v] : S(1);
+        bias[v] = p.bias && has ? reinterpret_cast<const S*>(p.bias)[ch + v] : S(0);
+        dw[v] = db[v] = S(0);
+    }
+    for (long long round = lo + lane_row; round < hi; round += s.rows * B) {
+        bool on[B];
+        S x[B][V], y[B][V], z[B][V], mean[B], rstd[B], one[B], two[B];
+        long long row[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            row[b] = round + b * s.rows < hi ? round + b * s.rows : round;   // (a row again where there are no more: not written)
+            on[b] = has && round + b * s.rows < hi && (lengths ? row_counts(p.rows, row[b]) : row[b] >= from && row[b] < to);
+            load_wide<T, V>(x[b], p.x, row[b] * p.stride_x + ch);
+            if (p.z) load_wide<T, V>(z[b], p.z, row[b] * p.stride_z + ch);
+            if (GRAD) {
+                load_wide<T, V>(y[b], p.dy, row[b] * p.stride_y + ch);
+                const S* stats = reinterpret_cast<const S*>(p.stats) + (row[b] * p.G + (has ? g : 0)) * 2;
+                mean[b] = stats[0];
+                rstd[b] = stats[1];
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            one[b] = two[b] = S(0);
+            if (!GRAD)
+#pragma unroll
+                for (int v = 0; v < V; ++v) one[b] += has ? x[b][v] : S(0);
+        }
+        if (!GRAD) {
+            lanes_sum(one, s.L);
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                mean[b] = one[b] / S(n);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const S off = x[b][v] - mean[b];
+                    two[b] += has ? off * off : S(0);
+                }
+            }
+            lanes_sum(two, s.L);
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                rstd[b] = S(1) / sqrt(two[b] * share + (S)p.eps);
+                S* stats = reinterpret_cast<S*>(p.stats) + (row[b] * p.G + g) * 2;
+                if (on[b] && l == 0) {
+                    stats[0] = mean[b];
+                    stats[1] = rstd[b];
+                }
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const S pre = (x[b][v] - mean[b]) * rstd[b] * w[v] + bias[v];
+                    y[b][v] = p.act == DEER_ACT_SILU ? silu<T>(pre) : pre;
+                }
+                if (p.z)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) y[b][v] *= silu<T>(z[b][v]);
+                if (on[b]) store_narrow<T, V>(p.y, row[b] * p.stride_y + ch, y[b]);
+            }
+            continue;
+        }
+        // x becomes u = (x - mean) rstd, y dL/du
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            S dz[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                Through<T> th;
+                const S du = th(p, x[b][v], p.z ? z[b][v] : S(0), y[b][v], mean[b], rstd[b], w[v], bias[v]);
+                x[b][v] = th.u;
+                y[b][v] = du;
+                dz[v] = th.dz;
+                one[b] += has ? du : S(0);
+                two[b] += has ? du * th.u : S(0);
+                dw[v] += on[b] ? th.dv * th.u : S(0);
+                db[v] += on[b] ? th.dv : S(0);
+            }
+            if (p.z && on[b]) store_narrow<T, V>(p.dz, row[b] * p.stride_z + ch, dz);
+        }
+        lanes_sum(one, s.L);
+        lanes_sum(two, s.L);
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const S s1 = n > 1 ? one[b] * share : one[b], s2 = two[b] * share;
+#pragma unroll
+            for (int v = 0; v < V; ++v) y[b][v] = rstd[b] * ((y[b][v] - s1) - x[b][v] * s2);
+            if (on[b]) store_narrow<T, V>(p.dx, row[b] * p.stride_x + ch, y[b]);
+        }
+    }
+    clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
+    if (!GRAD || !has) return;
+    S* part = reinterpret_cast<S*>(p.part) + (block * s.rows + lane_row) * 2 * p.D + ch;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        part[v] = dw[v];
+        part[p.D + v] = db[v];
+    }
+}
+
 // ---- statistics over sequences ----
 // Pieces of sequences in tiles have places of their own: tile + sequence where rows are packed (one of the two grows from a piece to the next)
 __device__ __forceinline__ long long piece_at(const SeqRows& s, long long tile, int seq) { return s.packed ? tile + seq : tile; }
@@ -265,7 +425,6 @@ template <typename T, int V>
 __global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {
     using S = wide_t<T>;
     __shared__ S shared[256 * V];
-    clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
     const SpanPlace at = span_place<V>(p, l, rows);
     for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long, long long, long long r0, long long r1) {
         S two[2][V], first[V];
@@ -273,7 +432,7 @@ __global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const 
         for (int v = 0; v < V; ++v) two[0][v] = two[1][v] = first[v] = S(0);
         if (at.on) {
             load_wide<T, V>(first, p.x, r0 * p.stride_x + at.ch);
-#pragma unroll 4
+#pragma unroll 8
             for (long long r = r0 + at.phase; r < r1; r += l.phases) {
                 S x[V];
                 load_wide<T, V>(x, p.x, r * p.stride_x + at.ch);
@@ -296,21 +455,26 @@ __global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const 
             to[p.D + v] = squares > S(0) || !(squares <= S(0)) ? squares : S(0);   // (NaN stays)
         }
     });
+    clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
 }
 
+constexpr int kJoinLanes = 1024;
 __device__ __forceinline__ double block_sum(double v, double* shared) {
     for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
     __syncthreads();
-    return (shared[0] + shared[1]) + (shared[2] + shared[3]);
+    v = 0;
+#pragma unroll
+    for (int i = 0; i < kJoinLanes / 64; ++i) v += shared[i];
+    return v;
 }
 
 // Over a sequence's pieces and a group's channels, in 64 bits: mean and rstd (grad false), or the sums of dL/du and of dL/du u, u = (x - mean) rstd, over the number of
 // values (grad true)
 template <typename S>
-__global__ __launch_bounds__(256) void join_kernel(const NormParams p, int rows, bool grad) {
-    __shared__ double shared[4];
+__global__ __launch_bounds__(kJoinLanes) void join_kernel(const NormParams p, int rows, bool grad) {
+    __shared__ double shared[kJoinLanes / 64];
     const int seq = blockIdx.x / p.G, g = blockIdx.x % p.G, n = p.D / p.G, ch0 = g * n;
     const long long len = seq_length(p.rows, seq), tiles = (p.rows.T + rows - 1) / rows;
     S* to = reinterpret_cast<S*>(grad ? p.joined : p.stats) + (long long)blockIdx.x * 2;
@@ -319,42 +483,39 @@ __global__ __launch_bounds__(256) void join_kernel(const NormParams p, int rows,
         return;
     }
     const long long start = p.rows.packed ? seq_first(p.rows, seq) : 0, first = start / rows, last = (start + len - 1) / rows;
-    const long long items = (last - first + 1) * n;
-    const S* part = reinterpret_cast<const S*>(p.part);
-    auto piece = [&](long long i, double& count) {
-        const long long tile = first + i / n, lo = tile * rows > start ? tile * rows : start, hi = (tile + 1) * rows < start + len ? (tile + 1) * rows : start + len;
-        count = (double)(hi - lo);
-        return part + (p.rows.packed ? tile + seq : (long long)seq * tiles + tile) * 2 * p.D + ch0 + (int)(i % n);
+    // lanes side by side along the channels (a power of two of them), the others along the tiles
+    int wide = 1;
+    while (wide < n && wide < 256) wide *= 2;
+    const int c0 = threadIdx.x & (wide - 1), step = kJoinLanes / wide;
+    const S* part = reinterpret_cast<const S*>(p.part) + (p.rows.packed ? (long long)seq : (long long)seq * tiles) * 2 * p.D + ch0;
+    auto count = [&](long long tile) {
+        const long long lo = tile * rows > start ? tile * rows : start, hi = (tile + 1) * rows < start + len ? (tile + 1) * rows : start + len;
+        return (double)(hi - lo);
     };
     double a = 0, b = 0;
-    if (grad) {
+    for (int c = c0; c < n; c += wide) {
+        const double w = grad && p.w ? (double)reinterpret_cast<const S*>(p.w)[ch0 + c] : 1.0;
 #pragma unroll 4
-        for (long long i = threadIdx.x; i < items; i += 256) {
-            double count;
-            const S* at = piece(i, count);
-            const double w = p.w ? (double)reinterpret_cast<const S*>(p.w)[ch0 + (int)(i % n)] : 1.0;
-            a += w * (double)at[0];
-            b += w * (double)at[p.D];
-        }
-    } else {
-#pragma unroll 4
-        for (long long i = threadIdx.x; i < items; i += 256) {
-            double count;
-            const S* at = piece(i, count);
-            a += count * (double)at[0];
+        for (long long tile = first + threadIdx.x / wide; tile <= last; tile += step) {
+            const S* at = part + tile * 2 * p.D + c;
+            if (grad) {
+                a += w * (double)at[0];
+                b += w * (double)at[p.D];
+            } else {
+                a += count(tile) * (double)at[0];
+            }
         }
     }
     const double all = (double)len * n;
     a = block_sum(a, shared) / all;
-    if (!grad) {
+    if (!grad)
+        for (int c = c0; c < n; c += wide)
 #pragma unroll 4
-        for (long long i = threadIdx.x; i < items; i += 256) {
-            double count;
-            const S* at = piece(i, count);
-            const double off = (double)at[0] - a;
-            b += (double)at[p.D] + count * off * off;
-        }
-    }
+            for (long long tile = first + threadIdx.x / wide; tile <= last; tile += step) {
+                const S* at = part + tile * 2 * p.D + c;
+                const double off = (double)at[0] - a;
+                b += (double)at[p.D] + count(tile) * off * off;
+            }
     b = block_sum(b, shared) / all;
     if (threadIdx.x == 0) {
         to[0] = (S)a;
@@ -362,29 +523,11 @@ __global__ __launch_bounds__(256) void join_kernel(const NormParams p, int rows,
     }
 }
 
-// One element: y of x, or du = dL/du and what else its gradient needs
-template <typename T>
-struct Through {
-    using S = wide_t<T>;
-    S u, dv, dz;
-    __device__ __forceinline__ S operator()(const NormParams& p, S x, S z, S dy, S mean, S rstd, S w, S b) {
-        u = (x - mean) * rstd;
-        const S pre = u * w + b;
-        S f = pre, slope = S(1), gate = S(1), gslope = S(0);
-        if (p.act == DEER_ACT_SILU) silu_both<T>(pre, f, slope);
-        if (p.z) silu_both<T>(z, gate, gslope);
-        dv = dy * gate * slope;
-        dz = dy * f * gslope;
-        return dv * w;
-    }
-};
-
 // STEP 0: y; 1: the sums of dL/dv and dL/dv u of every channel in every piece, v = w u + bias, and in every tile; 2: dx and dz
 template <typename T, int V, int STEP>
 __global__ __launch_bounds__(256) void span_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {
     using S = wide_t<T>;
     __shared__ S shared[STEP == 1 ? 256 * V : 1];
-    if (STEP == 1) clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
     const SpanPlace at = span_place<V>(p, l, rows);
     S w[V], b[V], total[2][V];
 #pragma unroll
@@ -405,7 +548,7 @@ __global__ __launch_bounds__(256) void span_kernel(const NormParams p, const Lan
 #pragma unroll
         for (int v = 0; v < V; ++v) two[0][v] = two[1][v] = S(0);
         if (at.on)
-#pragma unroll 2
+#pragma unroll 4
             for (long long r = r0 + at.phase; r < r1; r += l.phases) {
                 S x[V], z[V], dy[V], out[V], dz[V];
                 load_wide<T, V>(x, p.x, r * p.stride_x + at.ch);
@@ -446,6 +589,7 @@ __global__ __launch_bounds__(256) void span_kernel(const NormParams p, const Lan
             total[1][v] += two[1][v];
         }
     });
+    if (STEP == 1) clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
     if (STEP != 1 || !at.on || (int)threadIdx.x >= l.lanes) return;
     S* to = reinterpret_cast<S*>(p.sums) + at.tile * 2 * p.D + at.ch;
 #pragma unroll
@@ -455,8 +599,14 @@ __global__ __launch_bounds__(256) void span_kernel(const NormParams p, const Lan
     }
 }
 
-int span_rows(int D, int V) { return 32 * lanes_for(D, V).phases; }
-template <typename T> constexpr int vector() { return sizeof(T) == 2 ? 8 : sizeof(T) == 4 ? 4 : 2; }
+// Rows of a tile: 32 a phase; where that makes few workgroups, fewer, down to 8
+int span_rows(int D, int V, long long rows) {
+    const Lanes l = lanes_for(D, V);
+    int each = 32;
+    while (each > 8 && rows / (each * l.phases) * l.blocks < 1024) each /= 2;
+    return each * l.phases;
+}
+template <typename T> constexpr int vector(int span) { return sizeof(T) == 8 ? 2 : sizeof(T) == 4 || span == DEER_SPAN_SEQUENCE ? 4 : 8; }
 
 RestRows rest_of(const NormParams& p, bool grad, long long bytes) {
     RestRows rest{};
@@ -479,7 +629,7 @@ template <typename T, int V>
 hipError_t launch_sequences(bool grad, const NormParams& p, hipStream_t stream) {
     using S = wide_t<T>;
     const Lanes l = lanes_for(p.D, V);
-    const int rows = span_rows(p.D, V);
+    const int rows = span_rows(p.D, V, p.rows.T * (p.rows.packed ? 1 : p.rows.N));
     const long long tiles = (p.rows.T + rows - 1) / rows * (p.rows.packed ? 1 : p.rows.N);
     const dim3 grid((unsigned)(tiles * l.blocks)), block(256);
     const RestRows rest = rest_of(p, grad, sizeof(T));
@@ -487,7 +637,7 @@ hipError_t launch_sequences(bool grad, const NormParams& p, hipStream_t stream) 
         if (grad) hipLaunchKernelGGL((span_kernel<T, V, 1>), grid, block, 0, stream, p, l, rows, rest);
         else hipLaunchKernelGGL((moments_kernel<T, V>), grid, block, 0, stream, p, l, rows, rest);
     }
-    hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)((long long)p.rows.N * p.G)), block, 0, stream, p, rows, grad);
+    hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)((long long)p.rows.N * p.G)), dim3(kJoinLanes), 0, stream, p, rows, grad);
     if (tiles) {
         if (grad) hipLaunchKernelGGL((span_kernel<T, V, 2>), grid, block, 0, stream, p, l, rows, rest);
         else hipLaunchKernelGGL((span_kernel<T, V, 0>), grid, block, 0, stream, p, l, rows, rest);
@@ -497,12 +647,13 @@ hipError_t launch_sequences(bool grad, const NormParams& p, hipStream_t stream) 
     return launch_sum_tiles(sizeof(S) == 8, p.sums, tiles, SumInto{p.dw, p.dbias, p.D, 1, true}, stream);
 }
 
-// rows of a workgroup, and how many workgroups along the rows: about 2,048 in all
+// rows of a workgroup, and how many workgroups along the rows: about 2,048 in all; 1,024 in the gradient, where each has sums of its own
 struct RowCut {
     long long each, blocks;
 };
-RowCut row_cut(const RowShape& s, long long rows) {
-    long long rounds = (rows + s.rows - 1) / s.rows, want = 2048 / s.blocks < 1 ? 1 : 2048 / s.blocks;
+RowCut row_cut(const RowShape& s, long long rows, bool grad) {
+    const int all = grad ? 1024 : 2048;
+    long long rounds = (rows + s.rows - 1) / s.rows, want = all / s.blocks < 1 ? 1 : all / s.blocks;
     const long long per = (rounds + want - 1) / want;
     RowCut c;
     c.each = (per < 1 ? 1 : per) * s.rows;
@@ -515,8 +666,14 @@ template <typename T, int V, int M, bool GRAD, bool FEW>
 hipError_t launch_rows_as(const NormParams& p, hipStream_t stream) {
     using S = wide_t<T>;
     const RowShape s = row_shape(p.D, p.G, V, M);
-    const RowCut c = row_cut(s, p.rows.T * (p.rows.packed ? 1 : p.rows.N));
-    if (c.blocks) hipLaunchKernelGGL((rownorm_kernel<T, V, M, GRAD, FEW>), dim3((unsigned)(c.blocks * s.blocks)), dim3(256), 0, stream, p, s, rest_of(p, GRAD, sizeof(T)), c.each);
+    const RowCut c = row_cut(s, p.rows.T * (p.rows.packed ? 1 : p.rows.N), GRAD);
+    const dim3 grid((unsigned)(c.blocks * s.blocks)), block(256);
+    const RestRows rest = rest_of(p, GRAD, sizeof(T));
+    if constexpr (M == 1) {
+        if (c.blocks) hipLaunchKernelGGL((rownorm_few_kernel<T, V, GRAD ? 2 : 4, GRAD>), grid, block, 0, stream, p, s, rest, c.each);
+    } else if (c.blocks) {
+        hipLaunchKernelGGL((rownorm_kernel<T, V, M, GRAD, FEW>), grid, block, 0, stream, p, s, rest, c.each);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !GRAD || (!p.dw && !p.dbias)) return e;
     return launch_sum_tiles(sizeof(S) == 8, p.part, c.blocks * s.rows, SumInto{p.dw, p.dbias, p.D, 1, true}, stream);
@@ -530,13 +687,14 @@ hipError_t launch_rows(const NormParams& p, hipStream_t stream) {
 
 template <typename T>
 hipError_t launch_type(bool grad, const NormParams& p, hipStream_t stream) {
-    constexpr int V = vector<T>();
+    constexpr int VR = vector<T>(DEER_SPAN_ROW), VS = vector<T>(DEER_SPAN_SEQUENCE);
+    const int V = p.span == DEER_SPAN_ROW ? VR : VS;
     const size_t e = sizeof(T);
     bool vec = p.D / p.G % V == 0 && rows_fit(p.x, p.stride_x, V, e) && (!p.z || rows_fit(p.z, p.stride_z, V, e));
     if (grad) vec = vec && rows_fit(p.dy, p.stride_y, V, e) && rows_fit(p.dx, p.stride_x, V, e) && (!p.z || rows_fit(p.dz, p.stride_z, V, e));
     else vec = vec && rows_fit(p.y, p.stride_y, V, e);
-    if (p.span == DEER_SPAN_SEQUENCE) return vec ? launch_sequences<T, V>(grad, p, stream) : launch_sequences<T, 1>(grad, p, stream);
-    if (vec) return grad ? launch_rows<T, V, true>(p, stream) : launch_rows<T, V, false>(p, stream);
+    if (p.span == DEER_SPAN_SEQUENCE) return vec ? launch_sequences<T, VS>(grad, p, stream) : launch_sequences<T, 1>(grad, p, stream);
+    if (vec) return grad ? launch_rows<T, VR, true>(p, stream) : launch_rows<T, VR, false>(p, stream);
     return grad ? launch_rows<T, 1, true>(p, stream) : launch_rows<T, 1, false>(p, stream);
 }
 
@@ -544,12 +702,12 @@ hipError_t launch_type(bool grad, const NormParams& p, hipStream_t stream) {
 
 // (which vectors a call can use follows from its pointers: room for either)
 NormLayout norm_layout(int dtype, int D, int G, int span, long long T, int N, bool packed, bool grad) {
-    const int wide = dtype == DEER_F32 ? vector<float>() : dtype == DEER_F64 ? vector<double>() : vector<BF16>();
+    const int wide = dtype == DEER_F32 ? vector<float>(span) : dtype == DEER_F64 ? vector<double>(span) : vector<BF16>(span);
     NormLayout l{};
     for (const int V : {1, wide}) {
         long long part = 0, sums = 0;
         if (span == DEER_SPAN_SEQUENCE) {
-            const int rows = span_rows(D, V);
+            const int rows = span_rows(D, V, T * (packed ? 1 : N));
             const long long tiles = (T + rows - 1) / rows * (packed ? 1 : N);
             part = (tiles + (packed ? N : 0)) * 2 * D;
             if (grad) sums = tiles * 2 * D;
@@ -557,7 +715,7 @@ NormLayout norm_layout(int dtype, int D, int G, int span, long long T, int N, bo
         } else if (D / G % V == 0) {
             const int vecs = D / G / V;
             const RowShape s = row_shape(D, G, V, vecs > 1024 ? 4 : vectors_each(vecs));
-            const RowCut c = row_cut(s, T * (packed ? 1 : N));
+            const RowCut c = row_cut(s, T * (packed ? 1 : N), grad);
             if (grad) part = c.blocks * s.rows * 2 * D;
             if (c.blocks * s.blocks > l.tiles) l.tiles = c.blocks * s.blocks;
         }

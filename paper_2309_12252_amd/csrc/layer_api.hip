@@ -214,7 +214,7 @@ NormRoom norm_room(const deer_groupnorm_config* c, bool grad, const NormLayout& 
 }
 NormLayout norm_layout_of(const deer_groupnorm_config* c, bool grad) { return norm_layout(c->dtype, c->D, c->G, c->span, c->T, c->N, is_packed(c), grad); }
 const char* too_large(const deer_groupnorm_config* c) {
-    if (c->T > kMostRows || c->D > (1 << 27) || row_count(c) * c->D > 1e17L || (long double)c->N * c->G * 256 > kMostLanes) return kLarge;
+    if (c->T > kMostRows || c->D > (1 << 27) || row_count(c) * c->D > 1e17L || (long double)c->N * c->G * 1024 > kMostLanes || (long double)c->D * 2 * 64 > kMostLanes) return kLarge;
     for (const bool grad : {false, true})
         if ((long double)norm_layout_of(c, grad).tiles * 256 > kMostLanes) return kLarge;
     return nullptr;

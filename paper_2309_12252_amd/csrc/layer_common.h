@@ -31,8 +31,44 @@ __device__ __forceinline__ void silu_both(wide_t<T> v, wide_t<T>& f, wide_t<T>& 
     slope = g * (S(1) + v * (S(1) - g));
 }
 
-// Rows lo .. hi - 1 (absolute; of sequence n where sequences are padded) as runs of one sequence each: f(sequence, its first row, the row behind
-// its last, first and last + 1 row of the run).  Rows of no sequence are in none.
+// The bounds of packed sequences as a whole wavefront looks at them, for rows that are the same for all its lanes: 64 of them in registers, one a lane, so that a search costs one
+// trip to memory and not one for each of its steps.
+struct Bounds {
+    const SeqRows& s;
+    long long v;   // bound base + lane
+    int base;
+    __device__ __forceinline__ explicit Bounds(const SeqRows& rows) : s(rows), base(0) { load(0); }
+    __device__ __forceinline__ void load(int from) {
+        base = from;
+        const int i = from + (int)(threadIdx.x & 63);
+        v = clamp_row(s.bounds[i < s.N ? i : s.N], s.T);
+    }
+    __device__ __forceinline__ long long at(int i) {   // 0 .. N
+        if (i < base || i >= base + 64) load(i);
+        const unsigned lo = __builtin_amdgcn_readlane((int)v, i - base), hi = __builtin_amdgcn_readlane((int)(v >> 32), i - base);
+        return (long long)((unsigned long long)hi << 32 | lo);
+    }
+    __device__ __forceinline__ long long last() {
+        return s.N < 64 ? at(s.N) : clamp_row(s.bounds[s.N], s.T);
+    }
+    // how many of the N + 1 bounds are at most `row`
+    __device__ __forceinline__ int up_to(long long row) {
+        int lo = 0, hi = s.N + 1;
+        while (hi - lo > 64) {
+            const int step = (hi - lo + 63) / 64, i = lo + (int)(threadIdx.x & 63) * step;
+            const int many = __popcll(__ballot(i < hi && clamp_row(s.bounds[i < s.N ? i : s.N], s.T) <= row));
+            if (many == 0) return lo;
+            const int behind = lo + many * step;
+            lo += (many - 1) * step + 1;
+            hi = behind < hi ? behind : hi;
+        }
+        if (base != lo) load(lo);
+        return lo + __popcll(__ballot(lo + (int)(threadIdx.x & 63) < hi && v <= row));
+    }
+};
+
+// Rows lo .. hi - 1 (absolute; of sequence n where sequences are padded), the same for all lanes of a wavefront, as runs of one sequence each: f(sequence, its first row, the row
+// behind its last, first and last + 1 row of the run).  Rows of no sequence are in none.
 template <typename F>
 __device__ __forceinline__ void for_runs(const SeqRows& s, int n, long long lo, long long hi, F f) {
     if (!s.packed) {
@@ -42,17 +78,18 @@ __device__ __forceinline__ void for_runs(const SeqRows& s, int n, long long lo, 
         if (lo < hi) f(n, start, end, lo, hi);
         return;
     }
-    const long long first = clamp_row(s.bounds[0], s.T), last = clamp_row(s.bounds[s.N], s.T);
+    Bounds bounds(s);
+    const long long first = bounds.at(0), last = bounds.last();
     if (lo < first) lo = first;
     if (hi > last) hi = last;
     if (lo >= hi) return;
-    int at = bounds_up_to(s, lo) - 1;
+    int at = bounds.up_to(lo) - 1;
     if (at < 0) at = 0;
     long long row = lo;
     while (row < hi && at < s.N) {
-        const long long end = clamp_row(s.bounds[at + 1], s.T);
+        const long long end = bounds.at(at + 1);
         if (end > row) {
-            const long long start = clamp_row(s.bounds[at], s.T), to = end < hi ? end : hi;
+            const long long start = bounds.at(at), to = end < hi ? end : hi;
             f(at, start < row ? start : row, end, row, to);
             row = to;
         }

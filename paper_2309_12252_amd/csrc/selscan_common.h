@@ -94,7 +94,8 @@ struct ScanSeq {
             end = start + seq_length(s, n);
             return;
         }
-        n = bounds_up_to(s, row) - 1;
+        Bounds bounds(s);
+        n = bounds.up_to(row) - 1;
         n = n < 0 ? 0 : n >= s.N ? s.N - 1 : n;
         load(s);
         if (start > row) start = row;   // (bounds that decrease: no meaning, but an end)

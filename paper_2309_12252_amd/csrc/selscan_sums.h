@@ -1,24 +1,8 @@
 // Sums across the lanes of a wavefront for the selective scan: of a channel's lanes (64 / Q apart), and of the channels.
 #pragma once
-#include "layer_common.h"
+#include "lane_sums.h"
 
 namespace deer {
-
-// sums over the halves: lanes 0 .. 31 get a's, lanes 32 .. 63 b's
-__device__ __forceinline__ float sum_halves(float a, float b) {
-    const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-    return __builtin_bit_cast(float, (unsigned)s[0]) + __builtin_bit_cast(float, (unsigned)s[1]);
-}
-// sums over neighbouring rows of 16 lanes: even rows get a's, odd ones b's
-__device__ __forceinline__ float sum_rows(float a, float b) {
-    const auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-    return __builtin_bit_cast(float, (unsigned)s[0]) + __builtin_bit_cast(float, (unsigned)s[1]);
-}
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float v) {
-    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
-}
-constexpr int kRor8 = 0x128, kRor4 = 0x124, kHalfMirror = 0x141, kSwapPairs = 0x4E, kSwapLanes = 0xB1;   // DPP controls
 
 // Four values over the Q lanes of a channel; what a lane gets: value of_lanes<Q>(lane, j) in v[j], j < lanes_keep<Q>
 template <int Q> constexpr int lanes_keep = Q == 1 ? 4 : Q == 2 ? 2 : 1;

@@ -34,7 +34,8 @@ __device__ __forceinline__ void row_or_initial(wide_t<T>* to, const ConvParams& 
 
 struct ConvPlace {
     int n, ch;
-    long long lo, hi;
+    long long lo, hi;             // rows of the lane
+    long long tile_lo, tile_hi;   // and of the workgroup
     bool on;
 };
 // which rows and channels a lane has: tiles of kConvRows rows a phase, sequences apart where they are padded
@@ -48,6 +49,8 @@ __device__ __forceinline__ ConvPlace conv_place(const ConvParams& p, const Lanes
     const long long in = (p.rows.packed ? tile : tile % tiles) * per + (threadIdx.x / l.lanes) * kConvRows, base = (long long)at.n * p.rows.T;
     at.lo = base + in;
     at.hi = base + (in + kConvRows < p.rows.T ? in + kConvRows : p.rows.T);
+    at.tile_lo = base + (p.rows.packed ? tile : tile % tiles) * per;
+    at.tile_hi = at.tile_lo + per < base + p.rows.T ? at.tile_lo + per : base + p.rows.T;
     return at;
 }
 
@@ -74,15 +77,17 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
         return;
     }
     const ConvPlace at = conv_place<V>(p, l, blockIdx.x);
-    if (!at.on) return;
     S w[M][V], bias[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        bias[v] = p.bias ? reinterpret_cast<const S*>(p.bias)[at.ch + v] : S(0);
+        bias[v] = p.bias && at.on ? reinterpret_cast<const S*>(p.bias)[at.ch + v] : S(0);
 #pragma unroll
-        for (int k = 0; k < M; ++k) w[k][v] = k >= M - p.W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - p.W)] : S(0);
+        for (int k = 0; k < M; ++k) w[k][v] = at.on && k >= M - p.W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - p.W)] : S(0);
     }
-    for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long start, long long, long long r0, long long r1) {
+    for_runs(p.rows, at.n, at.tile_lo, at.tile_hi, [&](int seq, long long start, long long, long long r0, long long r1) {
+        if (r0 < at.lo) r0 = at.lo;
+        if (r1 > at.hi) r1 = at.hi;
+        if (!at.on || r0 >= r1) return;
         S x[M - 1 + 8][V];
 #pragma unroll
         for (int k = 0; k < M - 1; ++k) {
@@ -145,8 +150,11 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
             dw[k][v] = S(0);
         }
     }
-    if (at.on)
-        for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long start, long long end, long long r0, long long r1) {
+    {
+        for_runs(p.rows, at.n, at.tile_lo, at.tile_hi, [&](int seq, long long start, long long end, long long r0, long long r1) {
+            if (r0 < at.lo) r0 = at.lo;
+            if (r1 > at.hi) r1 = at.hi;
+            if (!at.on || r0 >= r1) return;
             S x[M - 1 + B][V], d[M - 1 + B][V];
             const long long stop = r1 + behind < end ? r1 + behind : end;   // rows whose dv is needed
 #pragma unroll
@@ -217,6 +225,7 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
                     }
             }
         });
+    }
     // the phases' sums, one weight at a time
     S* part = reinterpret_cast<S*>(p.part) + (long long)(blockIdx.x / l.blocks) * (p.W + 1) * p.D;
     const int wide = l.lanes * V, first = (int)(blockIdx.x % l.blocks) * wide;
@@ -311,20 +320,22 @@ hipError_t launch_step_type(const ConvStepParams& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// 16 columns and 16 shares of the tiles a workgroup
+// 16 columns and 64 shares of the tiles a workgroup: few columns of many tiles are all latency
+constexpr int kSumLanes = 1024, kShares = kSumLanes / 16;
 template <typename S>
-__global__ __launch_bounds__(256) void sum_tiles_kernel(const S* part, long long tiles, int cols, const SumInto into) {
-    __shared__ double sums[16][17];
+__global__ __launch_bounds__(kSumLanes) void sum_tiles_kernel(const S* part, long long tiles, int cols, const SumInto into) {
+    __shared__ double sums[kShares][17];
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), f = threadIdx.x >> 4;
     double sum = 0;
     if (c < cols)
-        for (long long t = f; t < tiles; t += 16) sum += (double)part[t * cols + c];
+#pragma unroll 4
+        for (long long t = f; t < tiles; t += kShares) sum += (double)part[t * cols + c];
     sums[f][threadIdx.x & 15] = sum;
     __syncthreads();
     if (f != 0 || c >= cols) return;
     sum = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum += sums[i][threadIdx.x];
+#pragma unroll 8
+    for (int i = 0; i < kShares; ++i) sum += sums[i][threadIdx.x];
     const int row = c / into.each, at = c % into.each;
     S* to = reinterpret_cast<S*>(row < into.many ? into.first : into.second);
     if (to) to[row < into.many ? (long long)at * into.many + row : at] = (S)sum;
@@ -334,7 +345,7 @@ __global__ __launch_bounds__(256) void sum_tiles_kernel(const S* part, long long
 
 hipError_t launch_sum_tiles(bool wide, const void* part, long long tiles, const SumInto& into, hipStream_t stream) {
     const int cols = into.each * (into.many + (into.last ? 1 : 0));
-    const dim3 grid((cols + 15) / 16), block(256);
+    const dim3 grid((cols + 15) / 16), block(kSumLanes);
     if (wide) hipLaunchKernelGGL((sum_tiles_kernel<double>), grid, block, 0, stream, reinterpret_cast<const double*>(part), tiles, cols, into);
     else hipLaunchKernelGGL((sum_tiles_kernel<float>), grid, block, 0, stream, reinterpret_cast<const float*>(part), tiles, cols, into);
     return hipGetLastError();
