@@ -431,16 +431,38 @@ __global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const 
 #pragma unroll
         for (int v = 0; v < V; ++v) two[0][v] = two[1][v] = first[v] = S(0);
         if (at.on) {
-            load_wide<T, V>(first, p.x, r0 * p.stride_x + at.ch);
-#pragma unroll 8
-            for (long long r = r0 + at.phase; r < r1; r += l.phases) {
-                S x[V];
-                load_wide<T, V>(x, p.x, r * p.stride_x + at.ch);
+            // eight rows at a time, the next eight on their way
+            using TV = vec_t<T, V>;
+            constexpr int B = 8;
+            const long long step = l.phases * p.stride_x;
+            const T* from = reinterpret_cast<const T*>(p.x) + (r0 + at.phase) * p.stride_x + at.ch;
+            TV now[B], next[B];
+            auto ask = [&](long long r) {   // (rows behind the last: the first of the piece)
+                if (r + (B - 1) * l.phases < r1) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const S off = x[v] - first[v];
-                    two[0][v] += off;
-                    two[1][v] += off * off;
+                    for (int i = 0; i < B; ++i) next[i] = *reinterpret_cast<const TV*>(from + i * step);
+                } else {
+                    const T* first_row = reinterpret_cast<const T*>(p.x) + r0 * p.stride_x + at.ch;
+#pragma unroll
+                    for (int i = 0; i < B; ++i) next[i] = *reinterpret_cast<const TV*>(r + i * l.phases < r1 ? from + i * step : first_row);
+                }
+                from += B * step;
+            };
+            ask(r0 + at.phase);
+            load_wide<T, V>(first, p.x, r0 * p.stride_x + at.ch);
+            for (long long r = r0 + at.phase; r < r1; r += B * l.phases) {
+#pragma unroll
+                for (int i = 0; i < B; ++i) now[i] = next[i];
+                if (r + B * l.phases < r1) ask(r + B * l.phases);
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    const bool in = r + i * l.phases < r1;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const S off = in ? (S)vec_at<T, V>(now[i], v) - first[v] : S(0);
+                        two[0][v] += off;
+                        two[1][v] += off * off;
+                    }
                 }
             }
         }

@@ -1,4 +1,6 @@
 // Short causal convolution of every channel, with an activation: forward, gradient, single tokens.
+#include <type_traits>
+
 #include "layer_common.h"
 
 namespace deer {
@@ -66,8 +68,9 @@ __device__ __forceinline__ void conv_last(const ConvParams& p, long long block, 
     }
 }
 
-// Eight rows at a time: a row is read once (and the W - 1 rows in front of a lane's 32 once more).  M: weights there is room for.
-template <typename T, int V, int M>
+// Eight rows at a time: a row is read once (and the W - 1 rows in front of a lane's 32 once more).  M: weights there is room for; EXACT: as many as there are (taps that
+// are looked at one by one take a select each).
+template <typename T, int V, int M, bool EXACT>
 __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, const Lanes l, const RestRows rest, long long tile_blocks) {
     using S = wide_t<T>;
     if ((long long)blockIdx.x >= tile_blocks) {
@@ -76,13 +79,14 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
         if (p.last && p.W > 1) conv_last<T>(p, block, blocks);
         return;
     }
+    const int W = EXACT ? M : p.W;
     const ConvPlace at = conv_place<V>(p, l, blockIdx.x);
     S w[M][V], bias[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         bias[v] = p.bias && at.on ? reinterpret_cast<const S*>(p.bias)[at.ch + v] : S(0);
 #pragma unroll
-        for (int k = 0; k < M; ++k) w[k][v] = at.on && k >= M - p.W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - p.W)] : S(0);
+        for (int k = 0; k < M; ++k) w[k][v] = at.on && k >= M - W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - W)] : S(0);
     }
     for_runs(p.rows, at.n, at.tile_lo, at.tile_hi, [&](int seq, long long start, long long, long long r0, long long r1) {
         if (r0 < at.lo) r0 = at.lo;
@@ -91,28 +95,35 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
         S x[M - 1 + 8][V];
 #pragma unroll
         for (int k = 0; k < M - 1; ++k) {
-            if (k >= M - p.W) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
+            if (k >= M - W) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
             else {
 #pragma unroll
                 for (int v = 0; v < V; ++v) x[k][v] = S(0);
             }
         }
-        for (long long r = r0; r < r1; r += 8) {
+        const T* xs = reinterpret_cast<const T*>(p.x) + r0 * p.stride_x + at.ch;
+        T* ys = reinterpret_cast<T*>(p.y) + r0 * p.stride_y + at.ch;
+        for (long long r = r0; r < r1; r += 8, xs += 8 * p.stride_x, ys += 8 * p.stride_y) {
+            const int rows = r1 - r < 8 ? (int)(r1 - r) : 8;
+            if (rows == 8)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) load_wide<T, V>(x[M - 1 + i], reinterpret_cast<const T*>(p.x) + (r + i < r1 ? r + i : r1 - 1) * p.stride_x + at.ch);
+                for (int i = 0; i < 8; ++i) load_wide<T, V>(x[M - 1 + i], xs + i * p.stride_x);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) load_wide<T, V>(x[M - 1 + i], xs + (i < rows ? i : rows - 1) * p.stride_x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (r + i >= r1) break;
+                if (i >= rows) break;
                 S y[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     S sum = bias[v];
 #pragma unroll
                     for (int k = 0; k < M; ++k)
-                        if (k >= M - p.W) sum = w[k][v] * x[i + k][v] + sum;   // (no weight of zero: what lies in front may be NaN)
+                        if (k >= M - W) sum = w[k][v] * x[i + k][v] + sum;   // (no weight of zero: what lies in front may be NaN)
                     y[v] = p.act == DEER_ACT_SILU ? silu<T>(sum) : sum;
                 }
-                store_narrow<T, V>(reinterpret_cast<T*>(p.y) + (r + i) * p.stride_y + at.ch, y);
+                store_narrow<T, V>(ys + i * p.stride_y, y);
             }
 #pragma unroll
             for (int k = 0; k < M - 1; ++k)
@@ -124,7 +135,7 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
 
 // Gradient: dv_t = dy_t act'(v_t) with v computed again, dx_t = sum_j w_j dv_{t + W - 1 - j}, dw_j = sum_t dv_t x_{t - W + 1 + j}.  A lane goes on for W - 1 rows behind
 // its own, whose dv its last rows need.
-template <typename T, int V, int M>
+template <typename T, int V, int M, bool EXACT>
 __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p, const Lanes l, const RestRows rest, long long tile_blocks) {
     using S = wide_t<T>;
     constexpr int B = 4;
@@ -137,6 +148,7 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
                 if (seq_length(p.rows, (int)(i / per)) == 0) reinterpret_cast<S*>(p.ds0)[i] = p.dlast ? reinterpret_cast<const S*>(p.dlast)[i] : S(0);
         return;
     }
+    const int W = EXACT ? M : p.W;
     const ConvPlace at = conv_place<V>(p, l, blockIdx.x);
     const int behind = p.W - 1;
     S w[M][V], bias[V], dw[M][V], dbias[V];
@@ -146,7 +158,7 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
         dbias[v] = S(0);
 #pragma unroll
         for (int k = 0; k < M; ++k) {
-            w[k][v] = at.on && k >= M - p.W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - p.W)] : S(0);
+            w[k][v] = at.on && k >= M - W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - W)] : S(0);
             dw[k][v] = S(0);
         }
     }
@@ -159,63 +171,100 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
             const long long stop = r1 + behind < end ? r1 + behind : end;   // rows whose dv is needed
 #pragma unroll
             for (int k = 0; k < M - 1; ++k) {
-                if (k >= M - p.W) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
+                if (k >= M - W) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    if (k < M - p.W) x[k][v] = S(0);
+                    if (k < M - W) x[k][v] = S(0);
                     d[k][v] = S(0);
                 }
             }
-            for (long long r = r0; r < r1 + behind; r += B) {
+            // four rows at a time, the next four on their way
+            using TV = vec_t<T, V>;
+            TV nx[B], ny[B];
+            const T* xs = reinterpret_cast<const T*>(p.x) + r0 * p.stride_x + at.ch;
+            const T* ds = reinterpret_cast<const T*>(p.dy) + r0 * p.stride_y + at.ch;
+            T* outs = reinterpret_cast<T*>(p.dx) + (r0 - behind) * p.stride_x + at.ch;   // (of the row that a row completes)
+            auto ask = [&](long long r) {
+                const int rows = stop - r < B ? (int)(stop - r) : B;
+                if (rows == B) {
+#pragma unroll
+                    for (int i = 0; i < B; ++i) {
+                        nx[i] = *reinterpret_cast<const TV*>(xs + i * p.stride_x);
+                        ny[i] = *reinterpret_cast<const TV*>(ds + i * p.stride_y);
+                    }
+                } else if (rows > 0) {
+#pragma unroll
+                    for (int i = 0; i < B; ++i) {
+                        nx[i] = *reinterpret_cast<const TV*>(xs + (i < rows ? i : rows - 1) * p.stride_x);
+                        ny[i] = *reinterpret_cast<const TV*>(ds + (i < rows ? i : rows - 1) * p.stride_y);
+                    }
+                }
+                xs += B * p.stride_x;
+                ds += B * p.stride_y;
+            };
+            ask(r0);
+            for (long long r = r0; r < r1 + behind; r += B, outs += B * p.stride_x) {
                 S dy[B][V];
 #pragma unroll
-                for (int i = 0; i < B; ++i) {
-                    const long long row = r + i < stop ? r + i : stop - 1;
-                    load_wide<T, V>(x[M - 1 + i], reinterpret_cast<const T*>(p.x) + row * p.stride_x + at.ch);
-                    load_wide<T, V>(dy[i], reinterpret_cast<const T*>(p.dy) + row * p.stride_y + at.ch);
-                }
-#pragma unroll
-                for (int i = 0; i < B; ++i) {
-                    const long long row = r + i, out = row - behind;
-                    S dx[V];
+                for (int i = 0; i < B; ++i)
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        S slope = S(1);
-                        if (p.act == DEER_ACT_SILU) {
-                            S sum = bias[v], f;
+                        x[M - 1 + i][v] = (S)vec_at<T, V>(nx[i], v);
+                        dy[i][v] = (S)vec_at<T, V>(ny[i], v);
+                    }
+                if (r + B < r1 + behind) ask(r + B);
+                // INSIDE: all four rows are the lane's own, and so are the rows whose dx they complete, none of which the final states see
+                auto four = [&](auto inside) {
+                    constexpr bool INSIDE = decltype(inside)::value;
 #pragma unroll
-                            for (int k = 0; k < M; ++k)
-                                if (k >= M - p.W) sum = w[k][v] * x[i + k][v] + sum;
-                            silu_both<T>(sum, f, slope);
+                    for (int i = 0; i < B; ++i) {
+                        const long long row = r + i, out = row - behind;
+                        S dx[V];
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            S slope = S(1);
+                            if (p.act == DEER_ACT_SILU) {
+                                S sum = bias[v], f;
+#pragma unroll
+                                for (int k = 0; k < M; ++k)
+                                    if (k >= M - W) sum = w[k][v] * x[i + k][v] + sum;
+                                silu_both<T>(sum, f, slope);
+                            }
+                            const S dv = INSIDE || row < stop ? dy[i][v] * slope : S(0);
+                            d[M - 1 + i][v] = dv;
+                            if (INSIDE || row < r1) {
+                                dbias[v] += dv;
+#pragma unroll
+                                for (int k = 0; k < M; ++k)
+                                    if (k >= M - W) dw[k][v] = dv * x[i + k][v] + dw[k][v];
+                            }
+                            // weight m goes with the row m in front of this one
+                            S sum = S(0);
+#pragma unroll
+                            for (int m = 0; m < M; ++m)
+                                if (m < W) sum = w[M - W + m][v] * d[M - 1 + i - m][v] + sum;
+                            dx[v] = sum;
                         }
-                        const S dv = row < stop ? dy[i][v] * slope : S(0);
-                        d[M - 1 + i][v] = dv;
-                        if (row < r1) {
-                            dbias[v] += dv;
-#pragma unroll
-                            for (int k = 0; k < M; ++k)
-                                if (k >= M - p.W) dw[k][v] = dv * x[i + k][v] + dw[k][v];
+                        if (INSIDE) {
+                            store_narrow<T, V>(outs + i * p.stride_x, dx);
+                            continue;
                         }
-                        // weight j = W - 1 - m goes with the row m in front of this one
-                        S sum = S(0);
+                        if (out >= r1 || (out < r0 && r0 != start)) continue;
+                        if (out >= end - behind && p.dlast) {
+                            const S* from = reinterpret_cast<const S*>(p.dlast) + ((long long)seq * behind + out - (end - behind)) * p.D + at.ch;
 #pragma unroll
-                        for (int m = 0; m < M; ++m)
-                            if (m < p.W) sum = w[M - 1 - (p.W - 1 - m)][v] * d[M - 1 + i - m][v] + sum;
-                        dx[v] = sum;
-                    }
-                    if (out >= r1 || (out < r0 && r0 != start)) continue;
-                    if (out >= end - behind && p.dlast) {
-                        const S* from = reinterpret_cast<const S*>(p.dlast) + ((long long)seq * behind + out - (end - behind)) * p.D + at.ch;
+                            for (int v = 0; v < V; ++v) dx[v] += from[v];
+                        }
+                        if (out >= r0) store_narrow<T, V>(outs + i * p.stride_x, dx);
+                        else if (p.ds0) {
+                            S* to = reinterpret_cast<S*>(p.ds0) + ((long long)seq * behind + out - start + behind) * p.D + at.ch;
 #pragma unroll
-                        for (int v = 0; v < V; ++v) dx[v] += from[v];
+                            for (int v = 0; v < V; ++v) to[v] = dx[v];
+                        }
                     }
-                    if (out >= r0) store_narrow<T, V>(reinterpret_cast<T*>(p.dx) + out * p.stride_x + at.ch, dx);
-                    else if (p.ds0) {
-                        S* to = reinterpret_cast<S*>(p.ds0) + ((long long)seq * behind + out - start + behind) * p.D + at.ch;
-#pragma unroll
-                        for (int v = 0; v < V; ++v) to[v] = dx[v];
-                    }
-                }
+                };
+                if (r >= r0 + behind && r + B <= r1) four(std::true_type{});
+                else four(std::false_type{});
 #pragma unroll
                 for (int k = 0; k < M - 1; ++k)
 #pragma unroll
@@ -231,8 +280,8 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
     const int wide = l.lanes * V, first = (int)(blockIdx.x % l.blocks) * wide;
 #pragma unroll
     for (int k = 0; k <= M; ++k) {
-        if (k < M - p.W) continue;
-        const int j = k == M ? p.W : k - (M - p.W);
+        if (k < M - W) continue;
+        const int j = k == M ? p.W : k - (M - W);
         __syncthreads();
 #pragma unroll
         for (int v = 0; v < V; ++v) sums[threadIdx.x * V + v] = k == M ? dbias[v] : dw[k < M ? k : 0][v];
@@ -282,7 +331,7 @@ __global__ __launch_bounds__(256) void shortconv_step_kernel(const ConvStepParam
     reinterpret_cast<T*>(p.y)[(long long)n * p.stride_y + ch] = (T)(p.act == DEER_ACT_SILU ? silu<T>(sum) : sum);
 }
 
-template <typename T, int V, int M>
+template <typename T, int V, int M, bool EXACT>
 hipError_t launch_taps(bool grad, const ConvParams& p, hipStream_t stream) {
     const Lanes l = lanes_for(p.D, V);
     const long long per = (long long)kConvRows * l.phases, tiles = (p.rows.T + per - 1) / per * (p.rows.packed ? 1 : p.rows.N), blocks = tiles * l.blocks;
@@ -296,22 +345,30 @@ hipError_t launch_taps(bool grad, const ConvParams& p, hipStream_t stream) {
     extra = extra < 1 ? 1 : extra > 512 ? 512 : extra;
     const dim3 grid((unsigned)(blocks + extra)), block(256);
     if (!grad) {
-        hipLaunchKernelGGL((shortconv_kernel<T, V, M>), grid, block, 0, stream, p, l, rest, blocks);
+        hipLaunchKernelGGL((shortconv_kernel<T, V, M, EXACT>), grid, block, 0, stream, p, l, rest, blocks);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((shortconv_grad_kernel<T, V, M>), grid, block, 0, stream, p, l, rest, blocks);
+    hipLaunchKernelGGL((shortconv_grad_kernel<T, V, M, EXACT>), grid, block, 0, stream, p, l, rest, blocks);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     return launch_sum_tiles(sizeof(wide_t<T>) == 8, p.part, tiles, SumInto{p.dw, p.dbias, p.D, p.W, true}, stream);
 }
 
+template <typename T, int V>
+hipError_t launch_width(bool grad, const ConvParams& p, hipStream_t stream) {
+    switch (p.W) {
+        case 2: return launch_taps<T, V, 2, true>(grad, p, stream);
+        case 3: return launch_taps<T, V, 3, true>(grad, p, stream);
+        case 4: return launch_taps<T, V, 4, true>(grad, p, stream);
+        default: return launch_taps<T, V, 8, false>(grad, p, stream);
+    }
+}
 template <typename T>
 hipError_t launch_type(bool grad, const ConvParams& p, hipStream_t stream) {
     constexpr int V = sizeof(T) == 2 ? 4 : sizeof(T) == 4 ? 4 : 2;
     const bool vec = p.D % V == 0 && rows_fit(p.x, p.stride_x, V, sizeof(T)) &&
                      (grad ? rows_fit(p.dy, p.stride_y, V, sizeof(T)) && rows_fit(p.dx, p.stride_x, V, sizeof(T)) : rows_fit(p.y, p.stride_y, V, sizeof(T)));
-    if (vec) return p.W <= 4 ? launch_taps<T, V, 4>(grad, p, stream) : launch_taps<T, V, 8>(grad, p, stream);
-    return p.W <= 4 ? launch_taps<T, 1, 4>(grad, p, stream) : launch_taps<T, 1, 8>(grad, p, stream);
+    return vec ? launch_width<T, V>(grad, p, stream) : launch_width<T, 1>(grad, p, stream);
 }
 
 template <typename T>
