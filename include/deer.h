@@ -438,7 +438,8 @@ typedef struct {
     int64_t stride_x, stride_z, stride_y;   /* rows; dx lies like x, dz like z, dy like y                  */
 } deer_groupnorm_config;
 
-/* Bytes of device workspace (256-byte aligned) that deer_groupnorm_solve() (grad = 0) or deer_groupnorm_grad() (grad = 1) needs. */
+/* Bytes of device workspace (256-byte aligned) that deer_groupnorm_solve() (grad = 0) or deer_groupnorm_grad() (grad = 1) needs; 0, and d_workspace may be NULL, for
+ * deer_groupnorm_solve() over rows. */
 deer_status deer_groupnorm_workspace_bytes(const deer_groupnorm_config* cfg, int32_t grad, size_t* bytes);
 
 /* d_x in [rows, D]   d_w in [D] or NULL (ones)   d_bias in [D] or NULL (zeros)   d_z in [rows, D] or NULL   d_y out [rows, D]

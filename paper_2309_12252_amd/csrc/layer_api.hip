@@ -209,7 +209,7 @@ NormRoom norm_room(const deer_groupnorm_config* c, bool grad, const NormLayout& 
     n.part = r.take((size_t)l.part * w);
     n.sums = r.take((size_t)l.sums * w);
     n.joined = r.take((size_t)l.joined * w);
-    n.total = r.at + kAlign;
+    n.total = r.at ? r.at + kAlign : 0;   // (norms of rows need none)
     return n;
 }
 NormLayout norm_layout_of(const deer_groupnorm_config* c, bool grad) { return norm_layout(c->dtype, c->D, c->G, c->span, c->T, c->N, is_packed(c), grad); }

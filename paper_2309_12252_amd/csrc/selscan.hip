@@ -206,10 +206,23 @@ __global__ __launch_bounds__(256) void selscan_join_kernel(const SelscanParams p
     const int ch = (int)(cell / SP), k = (int)(cell % SP);
     const float A2 = k < p.S ? p.A[(long long)ch * p.S + k] * kLog2e : 0.0f;
     float h = 0.0f;
-    for (long long s = n * p.segs; s < (n + 1) * p.segs - 1; ++s) {
-        const float local = p.local[s * cells + cell], decay = __builtin_amdgcn_exp2f(A2 * p.steps[s * p.D + ch]);
-        h = p.resets[s] ? local : local + decay * h;
-        p.carry[(s + 1) * cells + cell] = h;
+    const long long first = n * p.segs;
+    for (int s0 = 0; s0 < p.segs - 1; s0 += 8) {   // (eight at a time: what is asked for does not wait for what is written)
+        float local[8], steps[8];
+        int reset[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const long long s = first + (s0 + i < p.segs - 1 ? s0 + i : p.segs - 2);
+            local[i] = p.local[s * cells + cell];
+            steps[i] = p.steps[s * p.D + ch];
+            reset[i] = p.resets[s];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (s0 + i >= p.segs - 1) break;
+            h = reset[i] ? local[i] : local[i] + __builtin_amdgcn_exp2f(A2 * steps[i]) * h;
+            p.carry[(first + s0 + i + 1) * cells + cell] = h;
+        }
     }
 }
 
@@ -218,8 +231,8 @@ __global__ __launch_bounds__(256) void selscan_empty_kernel(const SeqRows rows, 
         if (seq_length(rows, (int)(i / cells)) == 0) to[i] = from ? from[i] : 0.0f;
 }
 
-// One token for every row.  A lane has four states of a channel, the lanes of a channel lie side by side: states are read and written as they lie.
-template <typename T, int Q>
+// One token for every row.  A lane has four states of a channel, the lanes of a channel lie side by side: states are read and written as they lie (VEC: in one piece).
+template <typename T, int Q, bool VEC>
 __global__ __launch_bounds__(256) void selscan_step_kernel(const SelstepParams p) {
     constexpr int CW = 256 / Q;
     const int per = (p.D + CW - 1) / CW, n = blockIdx.x / per, ch = (blockIdx.x % per) * CW + (int)threadIdx.x / Q, q = threadIdx.x % Q;
@@ -229,23 +242,40 @@ __global__ __launch_bounds__(256) void selscan_step_kernel(const SelstepParams p
         slot = p.rows.slots[n];
         for (int m = threadIdx.x; m < n; m += 256) twice = twice || p.rows.slots[m] == slot;
     }
-    const bool in = ch < p.D && slot >= 0 && slot < p.rows.n_slots;
+    const bool in = ch < p.D && slot >= 0 && slot < p.rows.n_slots, lane = in && 4 * q < p.S;
     const ScanLane l{ch, 4 * q, in};
-    float h[4], a[4], b[4], c[4], x = 0.0f, dt = 0.0f, z = 0.0f, skip = 0.0f;
-    load_states(h, p.state, slot, l, p.D, p.S);
-    load_states(a, p.A, 0, l, p.D, p.S);
-    if (in) {
-        const int g = ch / (p.D / p.G);
-        const T* bs = reinterpret_cast<const T*>(p.B) + (long long)n * p.stride_B + (long long)g * p.S + 4 * q;
-        const T* cs = reinterpret_cast<const T*>(p.C) + (long long)n * p.stride_C + (long long)g * p.S + 4 * q;
+    Float4 h = {}, a = {}, b = {}, c = {};
+    float x = 0.0f, dt = 0.0f, z = 0.0f, skip = 0.0f;
+    float* const state = p.state + ((long long)slot * p.D + ch) * p.S + 4 * q;
+    if (lane) {
+        const long long group = (long long)(ch / (p.D / p.G)) * p.S + 4 * q;
+        const T* bs = reinterpret_cast<const T*>(p.B) + (long long)n * p.stride_B + group;
+        const T* cs = reinterpret_cast<const T*>(p.C) + (long long)n * p.stride_C + group;
+        const float* as = p.A + (long long)ch * p.S + 4 * q;
+        if constexpr (VEC) {
+            h = *reinterpret_cast<const Float4*>(state);
+            a = *reinterpret_cast<const Float4*>(as);
+            const vec_t<T, 4> b4 = *reinterpret_cast<const vec_t<T, 4>*>(bs), c4 = *reinterpret_cast<const vec_t<T, 4>*>(cs);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            b[k] = 4 * q + k < p.S ? (float)bs[k] : 0.0f;
-            c[k] = 4 * q + k < p.S ? (float)cs[k] : 0.0f;
+            for (int k = 0; k < 4; ++k) {
+                b[k] = (float)b4[k];
+                c[k] = (float)c4[k];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (4 * q + k < p.S) {
+                    h[k] = state[k];
+                    a[k] = as[k];
+                    b[k] = (float)bs[k];
+                    c[k] = (float)cs[k];
+                }
         }
-        x = (float)(reinterpret_cast<const T*>(p.x)[(long long)n * p.stride_x + ch]);
-        dt = (float)(reinterpret_cast<const T*>(p.dt)[(long long)n * p.stride_dt + ch]) + (p.bias ? p.bias[ch] : 0.0f);
-        if (p.z) z = (float)(reinterpret_cast<const T*>(p.z)[(long long)n * p.stride_z + ch]);
+    }
+    if (in) {
+        x = (float)reinterpret_cast<const T*>(p.x)[(long long)n * p.stride_x + ch];
+        dt = (float)reinterpret_cast<const T*>(p.dt)[(long long)n * p.stride_dt + ch] + (p.bias ? p.bias[ch] : 0.0f);
+        if (p.z) z = (float)reinterpret_cast<const T*>(p.z)[(long long)n * p.stride_z + ch];
         if (p.skip) skip = p.skip[ch];
     }
     twice = p.rows.slots ? __syncthreads_or(twice) != 0 : false;
@@ -256,18 +286,21 @@ __global__ __launch_bounds__(256) void selscan_step_kernel(const SelstepParams p
     }
     if (p.softplus) dt = softplus(dt);
     float sum = 0.0f;
-    if (in) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            h[k] = __builtin_amdgcn_exp2f(dt * a[k] * kLog2e) * h[k] + dt * x * b[k];
-            sum += c[k] * h[k];
-        }
+    for (int k = 0; k < 4; ++k) {
+        h[k] = __builtin_amdgcn_exp2f(dt * a[k] * kLog2e) * h[k] + dt * x * b[k];
+        sum += c[k] * h[k];
     }
 #pragma unroll
     for (int d = 1; d < Q; d *= 2) sum += __shfl_xor(sum, d);
-    if (!in) return;
-    store_states(p.state, slot, l, p.D, p.S, h);
-    if (q != 0) return;
+    if (lane) {
+        if constexpr (VEC) *reinterpret_cast<Float4*>(state) = h;
+        else
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (4 * q + k < p.S) state[k] = h[k];
+    }
+    if (!in || q != 0) return;
     sum += skip * x;
     *y = (T)(p.z ? sum * fast_silu(z) : sum);
 }
@@ -312,7 +345,10 @@ hipError_t launch_any(int dtype, const SelscanParams& p, bool marks, hipStream_t
 template <typename T, int Q>
 hipError_t launch_step_lanes(const SelstepParams& p, hipStream_t stream) {
     constexpr int CW = 256 / Q;
-    hipLaunchKernelGGL((selscan_step_kernel<T, Q>), dim3((unsigned)((long long)((p.D + CW - 1) / CW) * p.rows.N)), dim3(256), 0, stream, p);
+    const dim3 grid((unsigned)((long long)((p.D + CW - 1) / CW) * p.rows.N)), block(256);
+    const bool vec = p.S % 4 == 0 && rows_fit(p.state, 0, 4, 4) && rows_fit(p.A, 0, 4, 4) && rows_fit(p.B, p.stride_B, 4, sizeof(T)) && rows_fit(p.C, p.stride_C, 4, sizeof(T));
+    if (vec) hipLaunchKernelGGL((selscan_step_kernel<T, Q, true>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((selscan_step_kernel<T, Q, false>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 template <typename T>

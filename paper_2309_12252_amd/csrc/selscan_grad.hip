@@ -115,10 +115,23 @@ __global__ __launch_bounds__(256) void selscan_rjoin_kernel(const SelscanParams 
     const int ch = (int)(cell / SP), k = (int)(cell % SP);
     const float A2 = k < p.S ? p.A[(long long)ch * p.S + k] * kLog2e : 0.0f;
     float r = 0.0f;
-    for (long long s = (n + 1) * p.segs - 1; s > n * p.segs; --s) {
-        const float local = p.rlocal[s * cells + cell], decay = __builtin_amdgcn_exp2f(A2 * p.rsteps[s * p.D + ch]);
-        r = p.rresets[s] ? local : local + decay * r;
-        p.rcarry[(s - 1) * cells + cell] = r;
+    const long long first = n * p.segs;
+    for (int s0 = p.segs - 1; s0 > 0; s0 -= 8) {
+        float local[8], steps[8];
+        int reset[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const long long s = first + (s0 - i > 0 ? s0 - i : 1);
+            local[i] = p.rlocal[s * cells + cell];
+            steps[i] = p.rsteps[s * p.D + ch];
+            reset[i] = p.rresets[s];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (s0 - i <= 0) break;
+            r = reset[i] ? local[i] : local[i] + __builtin_amdgcn_exp2f(A2 * steps[i]) * r;
+            p.rcarry[(first + s0 - i - 1) * cells + cell] = r;
+        }
     }
 }
 

@@ -33,6 +33,7 @@ constexpr int64_t kMostRows = (int64_t)1 << 33;
 constexpr long double kMostLanes = 4294967295.0L;   // of a launch: its size in work items is a number of 32 bits
 
 inline deer_status check_workspace(const void* ws, size_t have, size_t need) {
+    if (need == 0) return DEER_OK;
     if (!ws || misaligned(ws, kAlign) || have < need) {
         char text[160];
         std::snprintf(text, sizeof(text), "workspace NULL, misaligned or smaller than the %zu bytes needed", need);

@@ -1013,10 +1013,10 @@ def groupnorm_solve(x, groups, w=None, bias=None, z=None, *, span=DEER_SPAN_ROW,
     cfg, bounds, wp, bp, shape, _ = _norm_config(x, groups, y, "out", w, bias, z, span, eps, act, offsets, lengths)
     stats = torch.empty(shape, dtype=_wide(cfg.dtype), device=x.device)
     size = _norm_workspace(0, cfg.dtype, cfg.span, cfg.N, cfg.D, cfg.G, cfg.T, cfg.packed)
-    ws = x.new_empty(size, dtype=torch.uint8)
+    ws = x.new_empty(size, dtype=torch.uint8) if size else None   # (none over rows)
     cfg.packed |= _zero_rest(bounds, y if out is None else None, stats) if span == DEER_SPAN_ROW else _zero_rest(bounds, y if out is None else None)
     st = lib.deer_groupnorm_solve(ctypes.byref(cfg), x.data_ptr(), wp, bp, z.data_ptr() if z is not None else 0, bounds, y.data_ptr(), stats.data_ptr(),
-                                  ws.data_ptr(), size, _stream_of(x.device))
+                                  ws.data_ptr() if size else 0, size, _stream_of(x.device))
     if st != DEER_OK:
         _raise(lib, st)
     return y, stats
