@@ -385,7 +385,8 @@ deer_status deer_shortconv_step(const deer_shortconv_config* cfg, const void* d_
                                 int32_t n_slots, void* d_state, void* d_y, void* hip_stream);
 
 /* Selective scan: S states for every channel, h_t = exp(dt_t A) h_{t-1} + dt_t x_t B_t, y_t = <C_t, h_t> + skip x_t, times z_t / (1 + exp(-z_t)) where there is a z.
- * dt_t = act(d_dt + dt_bias) is a channel's, B_t and C_t are a group's of D / G channels.  DEER_F32, DEER_BF16, DEER_F16. */
+ * dt_t = act(d_dt + dt_bias) is a channel's, B_t and C_t are a group's of D / G channels.  DEER_F32, DEER_BF16, DEER_F16; rows and strides of at most 2^22 elements.
+ * Long sequences are cut into segments whose states are joined with the exponential of A times the sum of dt: where factors overflow in 32 bits, so do these. */
 typedef struct {
     int32_t dtype;     /* deer_dtype: x, dt, B, C, z, y and their gradients                                */
     int32_t dt_act;    /* DEER_ACT_NONE or DEER_ACT_SOFTPLUS                                               */
@@ -400,7 +401,8 @@ typedef struct {
 } deer_selscan_config;
 
 /* Bytes of device workspace (256-byte aligned) that deer_selscan_solve() (grad = 0) or deer_selscan_grad() (grad = 1) needs: states between the segments
- * that long sequences are cut into; for the gradient the states of every 16th row, and the sums for dB and dC over 256 / S' channels each (S' a quarter of S). */
+ * that long sequences are cut into; for the gradient the states of every 16th row, and the sums for dB and dC over 256 / Q channels each, Q = 1, 2, 4, 8 or 16 for up to
+ * 4, 8, 16, 32 and 64 states. */
 deer_status deer_selscan_workspace_bytes(const deer_selscan_config* cfg, int32_t grad, size_t* bytes);
 
 /* d_x, d_dt in [rows, D]   d_A in [D, S]   d_B, d_C in [rows, G, S]   d_skip in [D] or NULL (zeros)   d_z in [rows, D] or NULL   d_dt_bias in [D] or NULL (zeros)

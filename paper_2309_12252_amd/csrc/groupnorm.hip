@@ -70,10 +70,11 @@ __device__ __forceinline__ S group_sum(S v, int L, S* shared) {
 __device__ __forceinline__ bool row_counts(const SeqRows& s, long long row) {
     if (!s.bounds) return true;
     if (s.packed) return row >= clamp_row(s.bounds[0], s.T) && row < clamp_row(s.bounds[s.N], s.T);
-    return row % s.T < clamp_row(s.bounds[row / s.T], s.T);
+    const long long n = row <= 0xFFFFFFFFll && s.T <= 0xFFFFFFFFll ? (unsigned)row / (unsigned)s.T : row / s.T;   // (64 bits take many times as long)
+    return row - n * s.T < clamp_row(s.bounds[n], s.T);
 }
 
-// M vectors a lane are kept, so that a row is read once; with FEW false groups may have more than 256 M vectors, and are gone over again
+// Wider groups.  M vectors a lane are kept, so that a row is read once; with FEW false groups may have more than 256 M vectors, and are gone over again
 template <typename T, int V, int M, bool GRAD, bool FEW>
 __global__ __launch_bounds__(256) void rownorm_kernel(const NormParams p, const RowShape s, const RestRows rest, long long rows_each) {
     using S = wide_t<T>;
@@ -262,7 +263,8 @@ __device__ __forceinline__ void lanes_sum(S (&v)[B], int L) {
     }
 }
 
-// Groups of at most 64 vectors, a vector a lane, B rows at a time so that their loads and sums overlap.  Memory bound.
+// Groups of at most 64 vectors, a vector a lane, B rows at a time so that their loads and sums overlap.  Memory bound: 16,384 rows of 16 x 128 channels in bf16 with a gate, 201 MB in 54 us
+// (3.7 TB/s), the gradient's 335 MB in 87; a row at a time, sums through LDS, 155 and 176.  16 bytes a lane: with 8 the gradient takes 110.
 template <typename T, int V, int B, bool GRAD>
 __global__ __launch_bounds__(256) void rownorm_few_kernel(const NormParams p, const RowShape s, const RestRows rest, long long rows_each) {
     using S = wide_t<T>;
@@ -420,7 +422,8 @@ __device__ __forceinline__ void phase_sums(S (*two)[V], const Lanes& l, S* share
 }
 
 // Mean and sum of squares about it, of every channel in every piece: sums of the differences from the piece's first row.  That row is one of the summed, so
-// its distance from the mean is at most the root of the sum of squares: what cancels is at most a factor of the rows of a piece.
+// its distance from the mean is at most the root of the sum of squares: what cancels is at most a factor of the rows of a piece.  32,768 rows of 2,560 channels in bf16, 168 MB, 45 us (3.7 TB/s; 75
+// without rows on their way).
 template <typename T, int V>
 __global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {
     using S = wide_t<T>;
@@ -545,6 +548,7 @@ __global__ __launch_bounds__(kJoinLanes) void join_kernel(const NormParams p, in
     }
 }
 
+// Memory bound: y of 32,768 rows of 2,560 channels in bf16 73 us for 335 MB (4.6 TB/s).  Statistics over a sequence read x twice: it is read again while the last-level cache has some of it.
 // STEP 0: y; 1: the sums of dL/dv and dL/dv u of every channel in every piece, v = w u + bias, and in every tile; 2: dx and dz
 template <typename T, int V, int STEP>
 __global__ __launch_bounds__(256) void span_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {

@@ -49,7 +49,8 @@ const char* bad_config(const deer_shortconv_config* c, bool step) {
     return nullptr;
 }
 const char* too_large(const deer_shortconv_config* c) {
-    if (c->T > kMostRows || c->D > (1 << 27) || row_count(c) * c->D > 1e17L) return kLarge;
+    // (the last: the sums over tiles, 64 lanes a column)
+    if (c->T > kMostRows || c->D > (1 << 27) || row_count(c) * c->D > 1e17L || (long double)c->D * (c->W + 1) * 64 > kMostLanes - 1024) return kLarge;
     const Lanes l = lanes_for(c->D, 1);   // (a channel a lane: most workgroups)
     return ((long double)conv_tiles(c->D, c->T, c->N, is_packed(c)) * l.blocks + 512) * 256 > kMostLanes ? kLarge : nullptr;
 }
@@ -85,14 +86,18 @@ struct ScanLayout {
     long long seg_rows, all_segs;
     size_t local, carry, steps, resets, rlocal, rcarry, rsteps, rresets, marks, mark_steps, part_bc, part_A, part_d, total;
 };
-ScanLayout scan_layout(const deer_selscan_config* c, bool grad) {
+// How the rows are cut into segments, each a workgroup for 256 / Q channels.  A cut costs a second look at the rows (and in the gradient one backwards), so sequences are whole where they make
+// 512 workgroups.  Measured on 4 x 4,096 rows of 4,096 channels with 16 states in bf16 (whole: 256 workgroups), as so many workgroups in all:
+//   outputs 256 670 us, 512 401, 1,024 312, 2,048 304; states behind segments 512 280, 1,024 229, 2,048 212
+//   gradient with its kept states 256 498 + 1,716 us, 512 304 + 1,105, 1,024 239 + 1,131, 2,048 221 + 1,133; backwards 512 248, 1,024 229, 2,048 218
+// Packed rows, and padded ones with lengths, may be nearly all one sequence's: always cut.  8,192 packed rows: 512 200 + 132 us, 1,024 156 + 109, 2,048 153 + 103.
+ScanLayout scan_layout(const deer_selscan_config* c, bool grad, bool bounds) {
     ScanLayout l{};
     l.lanes = scan_lanes(c->S);
     const int width = 256 / l.lanes, per_group = c->D / c->G;
     l.blocks = (per_group + width - 1) / width;
     const long long seqs = is_packed(c) ? 1 : c->N, across = (long long)c->G * l.blocks * seqs;
-    // enough workgroups for 256 CUs, of 64 rows at least
-    long long want = (2048 + across - 1) / across;
+    long long want = !is_packed(c) && !bounds && across >= 512 ? 1 : (2048 + across - 1) / across;   // of 64 rows at least
     const long long most = (c->T + 63) / 64;
     want = want > most ? most : want;
     want = want < 1 ? 1 : want;
@@ -134,8 +139,8 @@ const char* unsupported(const deer_selscan_config* c, bool step) {
     for (const int64_t stride : {c->stride_x, c->stride_dt, c->stride_B, c->stride_C, c->stride_z, c->stride_y, (int64_t)c->D, (int64_t)c->G * c->S})
         if (stride > kScanStride) return "selective scan: rows at most 2^22 elements apart";
     const long double seqs = is_packed(c) ? 1 : c->N;
-    if (c->T > kMostRows || row_count(c) * c->D > 1e15L || seqs * c->D * 64 > kMostLanes) return kLarge;
-    const ScanLayout l = scan_layout(c, true);
+    if (c->T > kMostRows || row_count(c) * c->D > 1e15L || seqs * c->D * 64 > kMostLanes || (long double)c->D * c->S * 64 > kMostLanes - 1024) return kLarge;
+    const ScanLayout l = scan_layout(c, true, true);   // (no fewer segments than without bounds)
     return (long double)l.all_segs * c->G * l.blocks * 256 > kMostLanes || l.all_segs > 0x7FFFFFFF / 4 ? kLarge : nullptr;
 }
 SelscanParams scan_params(const deer_selscan_config* c, const ScanLayout& l, const int64_t* bounds, void* workspace, bool grad) {
@@ -214,7 +219,7 @@ NormRoom norm_room(const deer_groupnorm_config* c, bool grad, const NormLayout& 
 }
 NormLayout norm_layout_of(const deer_groupnorm_config* c, bool grad) { return norm_layout(c->dtype, c->D, c->G, c->span, c->T, c->N, is_packed(c), grad); }
 const char* too_large(const deer_groupnorm_config* c) {
-    if (c->T > kMostRows || c->D > (1 << 27) || row_count(c) * c->D > 1e17L || (long double)c->N * c->G * 1024 > kMostLanes || (long double)c->D * 2 * 64 > kMostLanes) return kLarge;
+    if (c->T > kMostRows || c->D > (1 << 27) || row_count(c) * c->D > 1e17L || (long double)c->N * c->G * 1024 > kMostLanes || (long double)c->D * 2 * 64 > kMostLanes - 1024) return kLarge;
     for (const bool grad : {false, true})
         if ((long double)norm_layout_of(c, grad).tiles * 256 > kMostLanes) return kLarge;
     return nullptr;
@@ -319,7 +324,8 @@ deer_status deer_selscan_workspace_bytes(const deer_selscan_config* c, int32_t g
     if (!bytes) return fail(DEER_ERR_INVALID_ARG, "bytes is NULL");
     if (const char* why = bad_config(c, false)) return fail(DEER_ERR_INVALID_ARG, why);
     if (const char* why = unsupported(c, false)) return fail(DEER_ERR_UNSUPPORTED, why);
-    *bytes = scan_layout(c, grad != 0).total;
+    const size_t with = scan_layout(c, grad != 0, true).total, without = scan_layout(c, grad != 0, false).total;
+    *bytes = with > without ? with : without;
     return DEER_OK;
 }
 
@@ -332,7 +338,7 @@ deer_status deer_selscan_solve(const deer_selscan_config* c, const void* d_x, co
     const size_t e = type_bytes(c->dtype);
     if (any_misaligned(e, d_x, d_dt, d_B, d_C, d_z, d_y) || any_misaligned(4, d_A, d_skip, d_dt_bias, d_h0, d_last) || misaligned(d_bounds, 8))
         return fail(DEER_ERR_INVALID_ARG, kAligned);
-    const ScanLayout l = scan_layout(c, false);
+    const ScanLayout l = scan_layout(c, false, d_bounds != nullptr);
     if (deer_status st = check_workspace(d_workspace, workspace_bytes, l.total)) return st;
     SelscanParams p = scan_params(c, l, d_bounds, d_workspace, false);
     p.x = d_x;
@@ -362,7 +368,7 @@ deer_status deer_selscan_grad(const deer_selscan_config* c, const void* d_x, con
     if (any_misaligned(e, d_x, d_dt, d_B, d_C, d_z, d_dy, d_dx, d_ddt, d_dB, d_dC, d_dz) ||
         any_misaligned(4, d_A, d_skip, d_dt_bias, d_h0, d_dlast, d_dA, d_dskip, d_dbias, d_dh0) || misaligned(d_bounds, 8))
         return fail(DEER_ERR_INVALID_ARG, kAligned);
-    const ScanLayout l = scan_layout(c, true);
+    const ScanLayout l = scan_layout(c, true, d_bounds != nullptr);
     if (deer_status st = check_workspace(d_workspace, workspace_bytes, l.total)) return st;
     SelscanParams p = scan_params(c, l, d_bounds, d_workspace, true);
     p.x = d_x;

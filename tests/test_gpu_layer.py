@@ -263,3 +263,35 @@ def test_rows_beyond_32_bits():
     y, h = deer.selscan_solve(x, x, A, B, B, dt_bias=torch.full((D,), 4.0, device=DEV))
     y2, h2 = deer.selscan_solve(last, last, A, B[:, -tail:].contiguous(), B[:, -tail:].contiguous(), dt_bias=torch.full((D,), 4.0, device=DEV))
     assert torch.equal(y[:, -tail + 100:], y2[:, 100:]) and torch.equal(h, h2)
+
+
+def test_refusals_of_the_binding():
+    w, i = layer_weights(16, 4, 2, 4, "bf16", 1), layer_inputs((2, 9), 16, 4, 2, "bf16", 2)
+    x, z, dt, B, C = i["x"], i["z"], i["dt"], i["B"], i["C"]
+    state, pool = torch.zeros(2, 16, 4, device=DEV), torch.zeros(2, 3, 16, device=DEV)
+    _, stats = deer.groupnorm_solve(x, 4)
+    lengths = torch.tensor([3, 9], device=DEV)
+    for call in (
+            lambda: deer.shortconv_solve(x, w["cw"].bfloat16()), lambda: deer.shortconv_solve(x, w["cw"][:8]), lambda: deer.shortconv_solve(x, w["cw"], w["cb"][:8]),
+            lambda: deer.shortconv_solve(x, w["cw"], s0=pool[:, :2]), lambda: deer.shortconv_solve(x, w["cw"], lengths=lengths.int()),
+            lambda: deer.shortconv_solve(x, w["cw"], lengths=lengths, offsets=lengths), lambda: deer.shortconv_solve(x[0], w["cw"]),
+            lambda: deer.shortconv_solve(x.long(), w["cw"]), lambda: deer.shortconv_solve(x, w["cw"].cpu()), lambda: deer.shortconv_solve(x, w["cw"], act=1),
+            lambda: deer.shortconv_solve(x[..., ::2], w["cw"][::2].contiguous()), lambda: deer.shortconv_solve(x[:, :1].expand(2, 9, 16), w["cw"]),
+            lambda: deer.shortconv_step(x, w["cw"], pool), lambda: deer.shortconv_step(x[0], w["cw"], pool[:, :2]), lambda: deer.shortconv_step(x[0], w["cw"], pool, slots=lengths),
+            lambda: deer.shortconv_grad(x, w["cw"], x[:, :5]), lambda: deer.shortconv_grad(x, w["cw"], x, dx=torch.zeros(2, 9, 32, dtype=x.dtype, device=DEV)[..., :16]),
+            lambda: deer.selscan_solve(x.double(), dt, w["A"], B, C), lambda: deer.selscan_solve(x, dt.float(), w["A"], B, C), lambda: deer.selscan_solve(x, dt, w["A"][:8], B, C),
+            lambda: deer.selscan_solve(x, dt, w["A"], B, C[..., :3]), lambda: deer.selscan_solve(x, dt, w["A"], B[..., 0, :], C[..., 0, :]),
+            lambda: deer.selscan_solve(x, dt, w["A"], B, C, w["skip"][:8]), lambda: deer.selscan_solve(x, dt, w["A"], B, C, z=z[:, :4]),
+            lambda: deer.selscan_solve(x, dt, w["A"], B.expand(2, 9, 2, 4)[:, :, :1].expand(2, 9, 3, 4).contiguous(), C, h0=state),
+            lambda: deer.selscan_solve(x, dt, w["A"], B, C, h0=state[:1]), lambda: deer.selscan_grad(x, dt, w["A"], B, C, x, dz=x.clone()),
+            lambda: deer.selscan_grad(x, dt, w["A"], B, C, x.float()), lambda: deer.selscan_step(x[0], dt[0], w["A"], B[0], C[0], state.double()),
+            lambda: deer.selscan_step(x, dt, w["A"], B, C, state), lambda: deer.groupnorm_solve(x, 3), lambda: deer.groupnorm_solve(x, 4, span=2),
+            lambda: deer.groupnorm_solve(x, 4, eps=-1.0), lambda: deer.groupnorm_solve(x, 4, w["nw"].double()), lambda: deer.groupnorm_solve(x, 4, z=z[:1]),
+            lambda: deer.groupnorm_grad(x, 4, stats[..., :1], x), lambda: deer.groupnorm_grad(x, 4, None, x), lambda: deer.groupnorm_grad(x, 4, stats, x, dz=x.clone()),
+            lambda: deer.groupnorm_grad(x, 4, stats, x, span=deer.DEER_SPAN_SEQUENCE)):
+        with pytest.raises(deer.DeerError) as e:
+            call()
+        assert e.value.status == deer.DEER_ERR_INVALID_ARG
+    with pytest.raises(deer.DeerError) as e:
+        deer.selscan_solve(x, dt, torch.zeros(16, 65, device=DEV), torch.zeros(2, 9, 1, 65, dtype=x.dtype, device=DEV), torch.zeros(2, 9, 1, 65, dtype=x.dtype, device=DEV))
+    assert e.value.status == deer.DEER_ERR_UNSUPPORTED

@@ -160,3 +160,19 @@ def test_binding_needs_device_tensors():
         with pytest.raises(deer.DeerError) as e:
             call()
         assert e.value.status == deer.DEER_ERR_INVALID_ARG
+
+
+def test_more_work_items_than_a_launch_holds():
+    """2^32 - 1 of them, in any of a call's launches: sums over tiles have 64 a column"""
+    lib, size = deer.load_library(), ctypes.c_size_t(0)
+    ask = lambda c: lib.deer_shortconv_workspace_bytes(ctypes.byref(c), ctypes.byref(size))   # noqa: E731
+    assert ask(conv(N=1, T=1, D=(1 << 26) // 5 - 100)) == 0 and ask(conv(N=1, T=1, D=(1 << 26) // 5 + 1)) == 2
+    for grad in (0, 1):
+        ask = lambda c: lib.deer_selscan_workspace_bytes(ctypes.byref(c), grad, ctypes.byref(size))   # noqa: E731, B023
+        assert ask(scan(N=1, T=1, D=1 << 20, G=1, S=63)) == 0 and ask(scan(N=1, T=1, D=1 << 20, G=1, S=64)) == 2
+        assert ask(scan(D=1 << 22, G=1, S=4)) == 0 and ask(scan(D=(1 << 22) + 1, G=1, S=1)) == 2
+        assert ask(scan(stride_x=1 << 22)) == 0 and ask(scan(stride_z=(1 << 22) + 1)) == 2 and ask(scan(stride_B=(1 << 22) + 1)) == 2
+        assert ask(scan(N=1 << 20, D=64, G=1, T=1)) == 2   # 2^32 states between segments
+        ask = lambda c: lib.deer_groupnorm_workspace_bytes(ctypes.byref(c), grad, ctypes.byref(size))   # noqa: E731, B023
+        assert ask(norm(N=1, T=1, D=1 << 24)) == 0 and ask(norm(N=1, T=1, D=1 << 25)) == 2
+        assert ask(norm(N=1 << 20, T=1, D=8, G=4, span=1)) == 2   # 1,024 lanes for each of 2^22 groups of sequences
