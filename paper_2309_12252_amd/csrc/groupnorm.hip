@@ -263,8 +263,8 @@ __device__ __forceinline__ void lanes_sum(S (&v)[B], int L) {
     }
 }
 
-// Groups of at most 64 vectors, a vector a lane, B rows at a time so that their loads and sums overlap.  Memory bound: 16,384 rows of 16 x 128 channels in bf16 with a gate, 201 MB in 54 us
-// (3.7 TB/s), the gradient's 335 MB in 87; a row at a time, sums through LDS, 155 and 176.  16 bytes a lane: with 8 the gradient takes 110.
+// Groups of at most 64 vectors, a vector a lane, B rows at a time so that their loads and sums overlap.  Memory bound: 16,384 rows of 16 x 128 channels in bf16 with a gate, 201 MB in 52 us
+// (3.9 TB/s), the gradient's 335 MB in 81; a row at a time, sums through LDS, 155 and 176.  16 bytes a lane: with 8 the gradient takes 110.
 template <typename T, int V, int B, bool GRAD>
 __global__ __launch_bounds__(256) void rownorm_few_kernel(const NormParams p, const RowShape s, const RestRows rest, long long rows_each) {
     using S = wide_t<T>;
@@ -401,25 +401,31 @@ __device__ __forceinline__ SpanPlace span_place(const NormParams& p, const Lanes
     return at;
 }
 
-// sums of two values a channel over the phases, in the order of the phases; those of phase 0 get them
+// sums of two values a channel over the phases; those of phase 0 get them: over the phases of a wavefront, then over the wavefronts
 template <typename S, int V>
 __device__ __forceinline__ void phase_sums(S (*two)[V], const Lanes& l, S* shared) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int d = l.lanes; d < 64; d *= 2)
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        __syncthreads();
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int v = 0; v < V; ++v) shared[threadIdx.x * V + v] = two[k][v];
-        __syncthreads();
-        if ((int)threadIdx.x < l.lanes) {
+            for (int v = 0; v < V; ++v) two[k][v] += __shfl_xor(two[k][v], d);
+    __syncthreads();
+    if (wave > 0 && lane < l.lanes)
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                S sum = S(0);
-                for (int f = 0; f < l.phases; ++f) sum += shared[(f * l.lanes + threadIdx.x) * V + v];
-                two[k][v] = sum;
-            }
-        }
-    }
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int v = 0; v < V; ++v) shared[((wave * 2 + k) * 64 + lane) * V + v] = two[k][v];
+    __syncthreads();
+    if ((int)threadIdx.x < l.lanes)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int f = 1; f < 4; ++f) two[k][v] += shared[((f * 2 + k) * 64 + lane) * V + v];
 }
+constexpr int kPhaseRoom = 4 * 2 * 64;
 
 // Mean and sum of squares about it, of every channel in every piece: sums of the differences from the piece's first row.  That row is one of the summed, so
 // its distance from the mean is at most the root of the sum of squares: what cancels is at most a factor of the rows of a piece.  32,768 rows of 2,560 channels in bf16, 168 MB, 45 us (3.7 TB/s; 75
@@ -427,7 +433,7 @@ __device__ __forceinline__ void phase_sums(S (*two)[V], const Lanes& l, S* share
 template <typename T, int V>
 __global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {
     using S = wide_t<T>;
-    __shared__ S shared[256 * V];
+    __shared__ S shared[kPhaseRoom * V];
     const SpanPlace at = span_place<V>(p, l, rows);
     for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long, long long, long long r0, long long r1) {
         S two[2][V], first[V];
@@ -496,7 +502,7 @@ __device__ __forceinline__ double block_sum(double v, double* shared) {
 }
 
 // Over a sequence's pieces and a group's channels, in 64 bits: mean and rstd (grad false), or the sums of dL/du and of dL/du u, u = (x - mean) rstd, over the number of
-// values (grad true)
+// values (grad true).  Nine sequences of 32,768 rows in all, 32 groups of 80 channels: 10 us, mostly the way of two rounds of loads (16 with lanes in rows of 128 a tile)
 template <typename S>
 __global__ __launch_bounds__(kJoinLanes) void join_kernel(const NormParams p, int rows, bool grad) {
     __shared__ double shared[kJoinLanes / 64];
@@ -508,39 +514,67 @@ __global__ __launch_bounds__(kJoinLanes) void join_kernel(const NormParams p, in
         return;
     }
     const long long start = p.rows.packed ? seq_first(p.rows, seq) : 0, first = start / rows, last = (start + len - 1) / rows;
-    // lanes side by side along the channels (a power of two of them), the others along the tiles
-    int wide = 1;
-    while (wide < n && wide < 256) wide *= 2;
-    const int c0 = threadIdx.x & (wide - 1), step = kJoinLanes / wide;
     const S* part = reinterpret_cast<const S*>(p.part) + (p.rows.packed ? (long long)seq : (long long)seq * tiles) * 2 * p.D + ch0;
+    const S* w = grad ? reinterpret_cast<const S*>(p.w) : nullptr;
     auto count = [&](long long tile) {
         const long long lo = tile * rows > start ? tile * rows : start, hi = (tile + 1) * rows < start + len ? (tile + 1) * rows : start + len;
         return (double)(hi - lo);
     };
+    // a lane takes every 1,024th of the pieces' channels, eight of them on their way; those stay for the second time
+    constexpr int B = 8;
+    struct Place {
+        long long tile;
+        int c;
+    };
+    const Place begin{first + threadIdx.x / n, (int)threadIdx.x % n};
+    const int far = kJoinLanes / n, more = kJoinLanes % n;
+    auto go_on = [&](Place& at) {
+        at.c += more;
+        at.tile += far;
+        if (at.c >= n) {
+            at.c -= n;
+            ++at.tile;
+        }
+    };
+    S one[B], two[B], scale[B];
+    auto ask = [&](Place at) {
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const bool on = at.tile <= last;
+            const S* from = part + (on ? at.tile : first) * 2 * p.D + at.c;
+            one[i] = from[0];
+            two[i] = from[p.D];
+            scale[i] = w ? w[ch0 + at.c] : S(1);
+            go_on(at);
+        }
+    };
     double a = 0, b = 0;
-    for (int c = c0; c < n; c += wide) {
-        const double w = grad && p.w ? (double)reinterpret_cast<const S*>(p.w)[ch0 + c] : 1.0;
-#pragma unroll 4
-        for (long long tile = first + threadIdx.x / wide; tile <= last; tile += step) {
-            const S* at = part + tile * 2 * p.D + c;
-            if (grad) {
-                a += w * (double)at[0];
-                b += w * (double)at[p.D];
-            } else {
-                a += count(tile) * (double)at[0];
+    const bool whole = (last - first + 1) * n <= (long long)B * kJoinLanes;
+    for (Place at = begin; at.tile <= last;) {
+        ask(at);
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            if (at.tile <= last) {
+                a += (grad ? (double)scale[i] : count(at.tile)) * (double)one[i];
+                if (grad) b += (double)scale[i] * (double)two[i];
             }
+            go_on(at);
         }
     }
     const double all = (double)len * n;
     a = block_sum(a, shared) / all;
     if (!grad)
-        for (int c = c0; c < n; c += wide)
-#pragma unroll 4
-            for (long long tile = first + threadIdx.x / wide; tile <= last; tile += step) {
-                const S* at = part + tile * 2 * p.D + c;
-                const double off = (double)at[0] - a;
-                b += (double)at[p.D] + count(tile) * off * off;
+        for (Place at = begin; at.tile <= last;) {
+            if (!whole) ask(at);
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                if (at.tile <= last) {
+                    const double off = (double)one[i] - a;
+                    b += (double)two[i] + count(at.tile) * off * off;
+                }
+                go_on(at);
             }
+        }
     b = block_sum(b, shared) / all;
     if (threadIdx.x == 0) {
         to[0] = (S)a;
@@ -553,7 +587,7 @@ __global__ __launch_bounds__(kJoinLanes) void join_kernel(const NormParams p, in
 template <typename T, int V, int STEP>
 __global__ __launch_bounds__(256) void span_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {
     using S = wide_t<T>;
-    __shared__ S shared[STEP == 1 ? 256 * V : 1];
+    __shared__ S shared[STEP == 1 ? kPhaseRoom * V : 1];
     const SpanPlace at = span_place<V>(p, l, rows);
     S w[V], b[V], total[2][V];
 #pragma unroll
@@ -625,13 +659,15 @@ __global__ __launch_bounds__(256) void span_kernel(const NormParams p, const Lan
     }
 }
 
-// Rows of a tile: 32 a phase; where that makes few workgroups, fewer, down to 8
+// Rows of a tile: 32 a phase; where that makes few workgroups, fewer, down to 8.  32 x 17,984 rows of 16 channels in fp32: y with 32 (281 workgroups) 29 us, with 8 17; the gradient's two passes
+// 66 and 46
 int span_rows(int D, int V, long long rows) {
     const Lanes l = lanes_for(D, V);
     int each = 32;
     while (each > 8 && rows / (each * l.phases) * l.blocks < 1024) each /= 2;
     return each * l.phases;
 }
+// Channels of a lane: 16 bytes; over sequences of 16 bits 8 bytes (moments of 32,768 rows of 2,560 in bf16 45 us, with 16 bytes 53)
 template <typename T> constexpr int vector(int span) { return sizeof(T) == 8 ? 2 : sizeof(T) == 4 || span == DEER_SPAN_SEQUENCE ? 4 : 8; }
 
 RestRows rest_of(const NormParams& p, bool grad, long long bytes) {
@@ -673,12 +709,13 @@ hipError_t launch_sequences(bool grad, const NormParams& p, hipStream_t stream) 
     return launch_sum_tiles(sizeof(S) == 8, p.sums, tiles, SumInto{p.dw, p.dbias, p.D, 1, true}, stream);
 }
 
-// rows of a workgroup, and how many workgroups along the rows: about 2,048 in all; 1,024 in the gradient, where each has sums of its own
+// rows of a workgroup, and how many workgroups along the rows: about 1,024 in all; 512 in the gradient, where each has sums of its own.  16,384 rows of 16 x 128 channels in bf16, as so many:
+// forward 512 57 us, 1,024 52, 2,048 53, 4,096 59; gradient with the sums over workgroups 256 126, 512 86, 1,024 94, 2,048 112
 struct RowCut {
     long long each, blocks;
 };
 RowCut row_cut(const RowShape& s, long long rows, bool grad) {
-    const int all = grad ? 1024 : 2048;
+    const int all = grad ? 512 : 1024;
     long long rounds = (rows + s.rows - 1) / s.rows, want = all / s.blocks < 1 ? 1 : all / s.blocks;
     const long long per = (rounds + want - 1) / want;
     RowCut c;
