@@ -69,9 +69,8 @@ __device__ __forceinline__ void conv_last(const ConvParams& p, long long block, 
 }
 
 // Memory bound: 32,768 packed rows of 2,560 channels in bf16, 335 MB, 74 us (4.5 TB/s; a large copy 5.2).  Eight rows at a time: a row is read once (and the W - 1 rows in front of a
-// lane's 32 once more).  M: weights there is room for; EXACT: as many as there are (taps that
-// are looked at one by one take a select each).
-template <typename T, int V, int M, bool EXACT>
+// lane's 32 once more).  M weights.
+template <typename T, int V, int M>
 __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, const Lanes l, const RestRows rest, long long tile_blocks) {
     using S = wide_t<T>;
     if ((long long)blockIdx.x >= tile_blocks) {
@@ -80,14 +79,13 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
         if (p.last && p.W > 1) conv_last<T>(p, block, blocks);
         return;
     }
-    const int W = EXACT ? M : p.W;
     const ConvPlace at = conv_place<V>(p, l, blockIdx.x);
     S w[M][V], bias[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         bias[v] = p.bias && at.on ? reinterpret_cast<const S*>(p.bias)[at.ch + v] : S(0);
 #pragma unroll
-        for (int k = 0; k < M; ++k) w[k][v] = at.on && k >= M - W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - W)] : S(0);
+        for (int k = 0; k < M; ++k) w[k][v] = at.on ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * M + k] : S(0);
     }
     for_runs(p.rows, at.n, at.tile_lo, at.tile_hi, [&](int seq, long long start, long long, long long r0, long long r1) {
         if (r0 < at.lo) r0 = at.lo;
@@ -95,13 +93,7 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
         if (!at.on || r0 >= r1) return;
         S x[M - 1 + 8][V];
 #pragma unroll
-        for (int k = 0; k < M - 1; ++k) {
-            if (k >= M - W) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
-            else {
-#pragma unroll
-                for (int v = 0; v < V; ++v) x[k][v] = S(0);
-            }
-        }
+        for (int k = 0; k < M - 1; ++k) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
         const T* xs = reinterpret_cast<const T*>(p.x) + r0 * p.stride_x + at.ch;
         T* ys = reinterpret_cast<T*>(p.y) + r0 * p.stride_y + at.ch;
         for (long long r = r0; r < r1; r += 8, xs += 8 * p.stride_x, ys += 8 * p.stride_y) {
@@ -120,8 +112,7 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
                 for (int v = 0; v < V; ++v) {
                     S sum = bias[v];
 #pragma unroll
-                    for (int k = 0; k < M; ++k)
-                        if (k >= M - W) sum = w[k][v] * x[i + k][v] + sum;   // (no weight of zero: what lies in front may be NaN)
+                    for (int k = 0; k < M; ++k) sum = w[k][v] * x[i + k][v] + sum;
                     y[v] = p.act == DEER_ACT_SILU ? silu<T>(sum) : sum;
                 }
                 store_narrow<T, V>(ys + i * p.stride_y, y);
@@ -135,12 +126,13 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
 }
 
 // Gradient: dv_t = dy_t act'(v_t) with v computed again, dx_t = sum_j w_j dv_{t + W - 1 - j}, dw_j = sum_t dv_t x_{t - W + 1 + j}.  A lane goes on for W - 1 rows behind
-// its own, whose dv its last rows need.  503 MB (the same rows, dy and dx) in 158 us, 3.2 TB/s: with two wavefronts a SIMD by registers the loads four rows ahead do not cover all of the way to memory;
-// two channels a lane 155 (and the outputs 84 for 74), three wavefronts a SIMD 216 (spills).  Rows times strides in 64 bits for every load took a third of the time (218 us).
-template <typename T, int V, int M, bool EXACT>
+// its own, whose dv its last rows need.  503 MB (the same rows, dy and dx) in 150 us, 3.4 TB/s: vector instructions take some 60 % of the time (36 an element), and with
+// three wavefronts a SIMD the loads ahead do not cover all of the way to memory.  Two channels a lane are no faster, four wavefronts a SIMD spill (422).  B: 16 bits four rows at a time 158, one 182; fp32
+// two rows 235, four 224.  Rows times strides in 64 bits for every load took a third of the time; widths that the compiler does not know, with a test for every weight: 539 us for 217 with 8 weights.
+template <typename T, int V, int M>
 __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p, const Lanes l, const RestRows rest, long long tile_blocks) {
     using S = wide_t<T>;
-    constexpr int B = 4;
+    constexpr int B = sizeof(T) == 2 ? 2 : 4;
     __shared__ S sums[256 * V];
     if ((long long)blockIdx.x >= tile_blocks) {
         const long long block = blockIdx.x - tile_blocks, blocks = gridDim.x - tile_blocks, per = (long long)(p.W - 1) * p.D, all = p.rows.N * per;
@@ -150,9 +142,8 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
                 if (seq_length(p.rows, (int)(i / per)) == 0) reinterpret_cast<S*>(p.ds0)[i] = p.dlast ? reinterpret_cast<const S*>(p.dlast)[i] : S(0);
         return;
     }
-    const int W = EXACT ? M : p.W;
     const ConvPlace at = conv_place<V>(p, l, blockIdx.x);
-    const int behind = p.W - 1;
+    constexpr int behind = M - 1;
     S w[M][V], bias[V], dw[M][V], dbias[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -160,7 +151,7 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
         dbias[v] = S(0);
 #pragma unroll
         for (int k = 0; k < M; ++k) {
-            w[k][v] = at.on && k >= M - W ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * p.W + k - (M - W)] : S(0);
+            w[k][v] = at.on ? reinterpret_cast<const S*>(p.w)[(long long)(at.ch + v) * M + k] : S(0);
             dw[k][v] = S(0);
         }
     }
@@ -173,14 +164,11 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
             const long long stop = r1 + behind < end ? r1 + behind : end;   // rows whose dv is needed
 #pragma unroll
             for (int k = 0; k < M - 1; ++k) {
-                if (k >= M - W) row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
+                row_or_initial<T, V>(x[k], p, seq, start, r0 - (M - 1) + k, at.ch);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    if (k < M - W) x[k][v] = S(0);
-                    d[k][v] = S(0);
-                }
+                for (int v = 0; v < V; ++v) d[k][v] = S(0);
             }
-            // four rows at a time, the next four on their way
+            // B rows at a time, the next B on their way
             using TV = vec_t<T, V>;
             TV nx[B], ny[B];
             const T* xs = reinterpret_cast<const T*>(p.x) + r0 * p.stride_x + at.ch;
@@ -215,8 +203,8 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
                         dy[i][v] = (S)vec_at<T, V>(ny[i], v);
                     }
                 if (r + B < r1 + behind) ask(r + B);
-                // INSIDE: all four rows are the lane's own, and so are the rows whose dx they complete, none of which the final states see
-                auto four = [&](auto inside) {
+                // INSIDE: all B rows are the lane's own, and so are the rows whose dx they complete, none of which the final states see
+                auto go = [&](auto inside) {
                     constexpr bool INSIDE = decltype(inside)::value;
 #pragma unroll
                     for (int i = 0; i < B; ++i) {
@@ -228,8 +216,7 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
                             if (p.act == DEER_ACT_SILU) {
                                 S sum = bias[v], f;
 #pragma unroll
-                                for (int k = 0; k < M; ++k)
-                                    if (k >= M - W) sum = w[k][v] * x[i + k][v] + sum;
+                                for (int k = 0; k < M; ++k) sum = w[k][v] * x[i + k][v] + sum;
                                 silu_both<T>(sum, f, slope);
                             }
                             const S dv = INSIDE || row < stop ? dy[i][v] * slope : S(0);
@@ -237,14 +224,12 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
                             if (INSIDE || row < r1) {
                                 dbias[v] += dv;
 #pragma unroll
-                                for (int k = 0; k < M; ++k)
-                                    if (k >= M - W) dw[k][v] = dv * x[i + k][v] + dw[k][v];
+                                for (int k = 0; k < M; ++k) dw[k][v] = dv * x[i + k][v] + dw[k][v];
                             }
                             // weight m goes with the row m in front of this one
                             S sum = S(0);
 #pragma unroll
-                            for (int m = 0; m < M; ++m)
-                                if (m < W) sum = w[M - W + m][v] * d[M - 1 + i - m][v] + sum;
+                            for (int m = 0; m < M; ++m) sum = w[m][v] * d[M - 1 + i - m][v] + sum;
                             dx[v] = sum;
                         }
                         if (INSIDE) {
@@ -265,8 +250,8 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
                         }
                     }
                 };
-                if (r >= r0 + behind && r + B <= r1) four(std::true_type{});
-                else four(std::false_type{});
+                if (r >= r0 + behind && r + B <= r1) go(std::true_type{});
+                else go(std::false_type{});
 #pragma unroll
                 for (int k = 0; k < M - 1; ++k)
 #pragma unroll
@@ -278,12 +263,10 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
         });
     }
     // the phases' sums, one weight at a time
-    S* part = reinterpret_cast<S*>(p.part) + (long long)(blockIdx.x / l.blocks) * (p.W + 1) * p.D;
+    S* part = reinterpret_cast<S*>(p.part) + (long long)(blockIdx.x / l.blocks) * (M + 1) * p.D;
     const int wide = l.lanes * V, first = (int)(blockIdx.x % l.blocks) * wide;
 #pragma unroll
     for (int k = 0; k <= M; ++k) {
-        if (k < M - W) continue;
-        const int j = k == M ? p.W : k - (M - W);
         __syncthreads();
 #pragma unroll
         for (int v = 0; v < V; ++v) sums[threadIdx.x * V + v] = k == M ? dbias[v] : dw[k < M ? k : 0][v];
@@ -291,7 +274,7 @@ __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p,
         for (int c = threadIdx.x; c < wide; c += 256) {
             S sum = S(0);
             for (int f = 0; f < l.phases; ++f) sum += sums[f * wide + c];
-            if (first + c < p.D) part[(long long)j * p.D + first + c] = sum;
+            if (first + c < p.D) part[(long long)k * p.D + first + c] = sum;
         }
     }
 }
@@ -333,7 +316,7 @@ __global__ __launch_bounds__(256) void shortconv_step_kernel(const ConvStepParam
     reinterpret_cast<T*>(p.y)[(long long)n * p.stride_y + ch] = (T)(p.act == DEER_ACT_SILU ? silu<T>(sum) : sum);
 }
 
-template <typename T, int V, int M, bool EXACT>
+template <typename T, int V, int M>
 hipError_t launch_taps(bool grad, const ConvParams& p, hipStream_t stream) {
     const Lanes l = lanes_for(p.D, V);
     const long long per = (long long)kConvRows * l.phases, tiles = (p.rows.T + per - 1) / per * (p.rows.packed ? 1 : p.rows.N), blocks = tiles * l.blocks;
@@ -347,10 +330,10 @@ hipError_t launch_taps(bool grad, const ConvParams& p, hipStream_t stream) {
     extra = extra < 1 ? 1 : extra > 512 ? 512 : extra;
     const dim3 grid((unsigned)(blocks + extra)), block(256);
     if (!grad) {
-        hipLaunchKernelGGL((shortconv_kernel<T, V, M, EXACT>), grid, block, 0, stream, p, l, rest, blocks);
+        hipLaunchKernelGGL((shortconv_kernel<T, V, M>), grid, block, 0, stream, p, l, rest, blocks);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((shortconv_grad_kernel<T, V, M, EXACT>), grid, block, 0, stream, p, l, rest, blocks);
+    hipLaunchKernelGGL((shortconv_grad_kernel<T, V, M>), grid, block, 0, stream, p, l, rest, blocks);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     return launch_sum_tiles(sizeof(wide_t<T>) == 8, p.part, tiles, SumInto{p.dw, p.dbias, p.D, p.W, true}, stream);
@@ -358,11 +341,17 @@ hipError_t launch_taps(bool grad, const ConvParams& p, hipStream_t stream) {
 
 template <typename T, int V>
 hipError_t launch_width(bool grad, const ConvParams& p, hipStream_t stream) {
+    // half as many channels a lane for registers' sake: gradient of 32,768 rows of 2,560 channels with 8 weights, fp32 289 us for 368, fp64 511 for 586; bf16 227 for 217, so not there
+    constexpr int H = sizeof(T) > 2 && V > 1 ? V / 2 : V;
     switch (p.W) {
-        case 2: return launch_taps<T, V, 2, true>(grad, p, stream);
-        case 3: return launch_taps<T, V, 3, true>(grad, p, stream);
-        case 4: return launch_taps<T, V, 4, true>(grad, p, stream);
-        default: return launch_taps<T, V, 8, false>(grad, p, stream);
+        case 1: return launch_taps<T, V, 1>(grad, p, stream);
+        case 2: return launch_taps<T, V, 2>(grad, p, stream);
+        case 3: return launch_taps<T, V, 3>(grad, p, stream);
+        case 4: return launch_taps<T, V, 4>(grad, p, stream);
+        case 5: return launch_taps<T, H, 5>(grad, p, stream);
+        case 6: return launch_taps<T, H, 6>(grad, p, stream);
+        case 7: return launch_taps<T, H, 7>(grad, p, stream);
+        default: return launch_taps<T, H, 8>(grad, p, stream);
     }
 }
 template <typename T>
