@@ -86,10 +86,10 @@ struct ScanLayout {
     long long seg_rows, all_segs;
     size_t local, carry, steps, resets, rlocal, rcarry, rsteps, rresets, marks, mark_steps, part_bc, part_A, part_d, total;
 };
-// How the rows are cut into segments, each a workgroup for 256 / Q channels.  A cut costs a second look at the rows (and in the gradient one backwards), so sequences are whole where they make
+// How the rows are cut into segments, each a workgroup for 256 / Q channels.  A cut costs a second look at the rows (the gradient's first look takes more), so sequences are whole where they make
 // 512 workgroups.  Measured on 4 x 4,096 rows of 4,096 channels with 16 states in bf16 (whole: 256 workgroups), as so many workgroups in all:
 //   outputs 256 670 us, 512 401, 1,024 312, 2,048 304; states behind segments 512 280, 1,024 229, 2,048 212
-//   gradient with its kept states 256 498 + 1,716 us, 512 304 + 1,105, 1,024 239 + 1,131, 2,048 221 + 1,133; backwards 512 248, 1,024 229, 2,048 218
+//   gradient with its kept states 256 498 + 1,716 us, 512 304 + 1,105, 1,024 239 + 1,131, 2,048 221 + 1,133; what comes out at segments' fronts, by itself 512 248, 1,024 229, 2,048 218
 // Packed rows, and padded ones with lengths, may be nearly all one sequence's: always cut.  8,192 packed rows: 512 200 + 132 us, 1,024 156 + 109, 2,048 153 + 103.
 ScanLayout scan_layout(const deer_selscan_config* c, bool grad, bool bounds) {
     ScanLayout l{};
@@ -219,7 +219,7 @@ NormRoom norm_room(const deer_groupnorm_config* c, bool grad, const NormLayout& 
 }
 NormLayout norm_layout_of(const deer_groupnorm_config* c, bool grad) { return norm_layout(c->dtype, c->D, c->G, c->span, c->T, c->N, is_packed(c), grad); }
 const char* too_large(const deer_groupnorm_config* c) {
-    if (c->T > kMostRows || c->D > (1 << 27) || row_count(c) * c->D > 1e17L || (long double)c->N * c->G * 1024 > kMostLanes || (long double)c->D * 2 * 64 > kMostLanes - 1024) return kLarge;
+    if (c->T > kMostRows || c->D > (1 << 27) || row_count(c) * c->D > 1e17L || (c->span == DEER_SPAN_SEQUENCE && (long double)c->N * c->G * 1024 > kMostLanes) || (long double)c->D * 2 * 64 > kMostLanes - 1024) return kLarge;
     for (const bool grad : {false, true})
         if ((long double)norm_layout_of(c, grad).tiles * 256 > kMostLanes) return kLarge;
     return nullptr;

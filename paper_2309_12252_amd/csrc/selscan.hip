@@ -7,18 +7,21 @@
 namespace deer {
 namespace {
 
-enum { kOutputs, kEnds, kMarks };   // y and the final states; the states behind segments; these and the states in front of every kMarkRows rows
+// y and the final states; the states behind segments; these and the states in front of every kMarkRows rows; these and what comes out at the front of a segment on the way back
+enum { kOutputs, kEnds, kMarks, kFronts };
 
 // Bound by the rate of vector instructions once there are eight workgroups a CU: 16,384 rows of 4,096 channels and 16 states in bf16 304 us for outputs (the bytes 104), 212 for the states
-// behind segments, 221 with states kept (268 MB).  With one a CU (670 us) half of the time is waiting for LDS; reading it two rows ahead brings that to 480, and costs 340 us with
+// behind segments, 221 with states kept (268 MB); 345 with what comes out at the front too (439 in two kernels; with five wavefronts a SIMD, which spill, 375).  With one a CU (670 us) half of the time is waiting for LDS; reading it two rows ahead brings that to 480, and costs 340 us with
 // eight.  Loads by buffer instructions whose offsets lie out of bounds where there is nothing, so that no lane takes another path and what is ahead stays on its way over the
 // barriers.
 template <typename T, int Q, int WHAT, bool VEC>
-__global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, const RestRows rest) {
+__global__ __launch_bounds__(256, WHAT == kFronts ? 4 : 1) void selscan_kernel(const SelscanParams p, const RestRows rest) {
     using Sh = ScanShape<Q>;
     constexpr int R = Sh::kRows, CW = Sh::kChannels, kAcross = CW / 4, kStep = 256 / kAcross;
     __shared__ Float2 sx[R][CW];       // dt and dt x; y in the place of the latter
     __shared__ Float4 bc[R][2][Q];
+    constexpr bool MARKS = WHAT == kMarks || WHAT == kFronts, FRONTS = WHAT == kFronts;
+    __shared__ float sdy[FRONTS ? R : 1][FRONTS ? CW : 1];
     if (WHAT == kOutputs) clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
     const ScanPlace place = scan_place<Q>(p);
     long long lo = place.lo;
@@ -48,6 +51,29 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
             for (int k = 0; k < 4; ++k) h[k] = 0.0f;
     }
     bool reset = seq.start == lo;
+    // What the rows in front of the segment get from it, a lam of its first row, from zero behind it (or from the end of the sequence that reaches into it): with the product of the
+    // factors from its first row on it is a sum along the rows, sum_t (a_lo .. a_t) C_t dy_t, and needs no second pass from the last row.
+    bool front = FRONTS && seq.start < lo;
+    float through[4], out[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        through[k] = 1.0f;
+        out[k] = 0.0f;
+    }
+    auto front_ends = [&](bool with_sequence) {
+        if (!FRONTS || !front) return;
+        front = false;
+        if (with_sequence) {
+            float d[4];
+            load_states(d, p.dlast, seq.n, l, p.D, p.S);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) out[k] += through[k] * d[k];
+        }
+        if (threadIdx.x == 0) p.rresets[place.seg] = with_sequence;
+        store_states(p.rlocal, place.seg, l, p.D, 4 * Q, out);
+        if (q == 0 && l.on) p.rsteps[place.seg * p.D + l.ch] = sum_dt;
+    };
+    if (FRONTS && !front && threadIdx.x == 0) p.rresets[place.seg] = seq.end <= hi;   // (the segment in front ends with its sequence: nothing is asked of this one)
     // a lane's items: four channels of rows kStep apart
     const int c4 = (threadIdx.x % kAcross) * 4, row0 = threadIdx.x / kAcross, count = place.channels - c4;
     float bias[4], skip[4];
@@ -60,15 +86,15 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
     Places<Sh::kItems> px, pd, pz, py;
     px.set(p.stride_x, row0, kStep, c4, T{});
     pd.set(p.stride_dt, row0, kStep, c4, T{});
-    if (WHAT == kOutputs) {
+    if (WHAT == kOutputs || FRONTS) {
         pz.set(p.stride_z, row0, kStep, c4, T{});
         py.set(p.stride_y, row0, kStep, c4, T{});
     }
     // the same for B and C: four states of a row
-    constexpr int kBoth = WHAT == kOutputs ? 2 : 1;
+    constexpr int kBoth = WHAT == kOutputs || FRONTS ? 2 : 1;
     auto tile_at = [&](const void* first, long long stride, long long r, long long more) { return Tile(reinterpret_cast<const T*>(first) + r * stride + more); };
     // what a tile reads is asked for while the one in front of it is worked on
-    Four<T, VEC> nx[Sh::kItems], nd[Sh::kItems], nz[Sh::kItems], nb[kBoth][Sh::kQuads];
+    Four<T, VEC> nx[Sh::kItems], nd[Sh::kItems], nz[Sh::kItems], ny[Sh::kItems], nb[kBoth][Sh::kQuads];
     auto ask = [&](long long r) {
         const int rows = hi - r < R ? (int)(hi - r) : R;
         const Tile x = tile_at(p.x, p.stride_x, r, place.ch0), d = tile_at(p.dt, p.stride_dt, r, place.ch0);
@@ -78,7 +104,12 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
             nx[j].load(x, on ? px.at[j] : kNoColumn, count);
             nd[j].load(d, on ? pd.at[j] : kNoColumn, count);
         }
-        if (WHAT == kOutputs && p.z) {
+        if (FRONTS) {
+            const Tile y = tile_at(p.dy, p.stride_y, r, place.ch0);
+#pragma unroll
+            for (int j = 0; j < Sh::kItems; ++j) ny[j].load(y, has && row0 + j * kStep < rows ? py.at[j] : kNoColumn, count);
+        }
+        if ((WHAT == kOutputs || FRONTS) && p.z) {
             const Tile z = tile_at(p.z, p.stride_z, r, place.ch0);
 #pragma unroll
             for (int j = 0; j < Sh::kItems; ++j) nz[j].load(z, has && row0 + j * kStep < rows ? pz.at[j] : kNoColumn, count);
@@ -112,6 +143,10 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
             if (kStep * Sh::kItems <= R || i < R) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) sx[i][c4 + v] = both[v];
+                if constexpr (FRONTS) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) sdy[i][c4 + v] = p.z ? ny[j][v] * fast_silu(nz[j][v]) : ny[j][v];
+                }
             }
         }
 #pragma unroll
@@ -124,13 +159,14 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
         lds_barrier();
         if (r + R < hi) ask(r + R);
         // four rows at a time.  WHOLE: all rows of the tile are there, and of one sequence
-        auto go = [&](auto whole) {
-            constexpr bool WHOLE = decltype(whole)::value;
+        auto go = [&](auto whole, auto fronts) {
+            constexpr bool WHOLE = decltype(whole)::value, TO_FRONT = decltype(fronts)::value;
 #pragma unroll 2
             for (int i0 = 0; i0 < R; i0 += 4) {
                 if (!WHOLE && i0 >= rows) break;
-                if (WHAT == kMarks && (r + i0 - lo) % kMarkRows == 0) {
+                if (MARKS && (r + i0 - lo) % kMarkRows == 0) {
                     if (!WHOLE && r + i0 == seq.end) {
+                        front_ends(true);
                         seq.next(p.rows, r + i0);
                         load_states(h, p.h0, seq.n, l, p.D, p.S);
                         reset = true;
@@ -147,6 +183,7 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
                     if (!WHOLE && i >= rows) continue;
                     if (!WHOLE && r + i == seq.end) {
                         if (WHAT == kOutputs) store_states(p.last, seq.n, l, p.D, p.S, h);
+                        front_ends(true);
                         seq.next(p.rows, r + i);
                         load_states(h, p.h0, seq.n, l, p.D, p.S);
                         reset = true;
@@ -154,8 +191,23 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
                     const Float2 s = sx[i][c];
                     const Float4 b = bc[i][0][q];
                     if (WHAT != kOutputs) sum_dt += s.x;
+                    float a[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) h[k] = __builtin_amdgcn_exp2f(s.x * A2[k]) * h[k] + s.y * b[k];
+                    for (int k = 0; k < 4; ++k) {
+                        a[k] = __builtin_amdgcn_exp2f(s.x * A2[k]);
+                        h[k] = a[k] * h[k] + s.y * b[k];
+                    }
+                    if constexpr (TO_FRONT) {
+                        if (WHOLE || front) {
+                            const float dy = sdy[i][c];
+                            const Float4 cc = bc[i][1][q];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                through[k] *= a[k];
+                                out[k] += through[k] * (cc[k] * dy);
+                            }
+                        }
+                    }
                     if (WHAT != kOutputs) continue;
                     const Float4 cc = bc[i][1][q];
 #pragma unroll
@@ -167,8 +219,10 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
                 for (int j = 0; j < lanes_keep<Q>; ++j) sx[i0 + of_lanes<Q>(lane, j)][c].y = y[j];
             }
         };
-        if (rows == R && seq.end >= r + R) go(std::true_type{});
-        else go(std::false_type{});
+        using Fronts = std::bool_constant<FRONTS>;
+        if (!(rows == R && seq.end >= r + R)) go(std::false_type{}, Fronts{});
+        else if (FRONTS && front) go(std::true_type{}, Fronts{});
+        else go(std::true_type{}, std::false_type{});
         lds_barrier();
         if (WHAT == kOutputs) {
             const Tile ys = tile_at(p.y, p.stride_y, r, place.ch0);
@@ -187,6 +241,7 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
         // the tile behind a whole one may begin with another sequence
         if (r + R < hi && r + R == seq.end) {
             if (WHAT == kOutputs) store_states(p.last, seq.n, l, p.D, p.S, h);
+            front_ends(true);
             seq.next(p.rows, r + R);
             load_states(h, p.h0, seq.n, l, p.D, p.S);
             reset = true;
@@ -197,7 +252,8 @@ __global__ __launch_bounds__(256) void selscan_kernel(const SelscanParams p, con
         return;
     }
     if (p.segs == 1) return;
-    if (WHAT == kMarks && threadIdx.x == 0) p.resets[place.seg] = reset;
+    front_ends(hi == seq.end);
+    if (MARKS && threadIdx.x == 0) p.resets[place.seg] = reset;
     store_states(p.local, place.seg, l, p.D, 4 * Q, h);
     if (q == 0 && l.on) p.steps[place.seg * p.D + l.ch] = sum_dt;
 }
@@ -317,7 +373,8 @@ hipError_t launch_lanes(const SelscanParams& p, bool marks, hipStream_t stream) 
     RestRows rest{};
     if (p.zero_rest) rest.array[rest.count++] = RestArray{p.y, p.stride_y * (long long)sizeof(T), p.D * (long long)sizeof(T)};
     if (marks) {
-        if (p.rows.T) hipLaunchKernelGGL((selscan_kernel<T, Q, kMarks, VEC>), grid, block, 0, stream, p, rest);
+        if (p.segs > 1) hipLaunchKernelGGL((selscan_kernel<T, Q, kFronts, VEC>), grid, block, 0, stream, p, rest);
+        else if (p.rows.T) hipLaunchKernelGGL((selscan_kernel<T, Q, kMarks, VEC>), grid, block, 0, stream, p, rest);
     } else if (p.segs > 1) {
         hipLaunchKernelGGL((selscan_kernel<T, Q, kEnds, VEC>), grid, block, 0, stream, p, rest);
     }

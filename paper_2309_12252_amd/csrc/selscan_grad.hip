@@ -15,98 +15,6 @@ namespace {
 
 constexpr int R = kMarkRows;
 
-// What comes out at the front of a segment for the rows in front of it: a lam of its first row, from zero behind it (or from a sequence's end inside): 218 us in the training step below
-template <typename T, int Q, bool VEC>
-__global__ __launch_bounds__(256) void selscan_fronts_kernel(const SelscanParams p) {
-    using Sh = ScanShape<Q>;
-    constexpr int CW = Sh::kChannels, kAcross = CW / 4, kStep = 256 / kAcross;
-    __shared__ Float2 sx[R][CW];   // dt and dy
-    __shared__ Float4 cs[R][Q];
-    const ScanPlace place = scan_place<Q>(p);
-    if (place.lo >= place.hi) return;
-    ScanSeq seq;
-    seq.at(p.rows, place, place.lo);
-    const bool reset = seq.end <= place.hi;
-    if (threadIdx.x == 0) p.rresets[place.seg] = reset;
-    if (seq.start == place.lo) return;   // nothing of it is in front
-    const long long lo = place.lo, hi = reset ? seq.end : place.hi;
-    const int lane = threadIdx.x & 63, q = lane / Sh::kWave, c = (threadIdx.x >> 6) * Sh::kWave + lane % Sh::kWave;
-    const ScanLane l{place.ch0 + c, 4 * q, c < place.channels};
-    float A2[4], r[4], sum_dt = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) A2[k] = l.on && l.k0 + k < p.S ? p.A[(long long)l.ch * p.S + l.k0 + k] * kLog2e : 0.0f;
-    load_states(r, reset ? p.dlast : nullptr, seq.n, l, p.D, p.S);
-    constexpr int kItems = R * CW >= 1024 ? R * CW / 1024 : 1;
-    const int c4 = (threadIdx.x % kAcross) * 4, row0 = threadIdx.x / kAcross, count = place.channels - c4;
-    float bias[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) bias[i] = p.bias && i < count ? p.bias[place.ch0 + c4 + i] : 0.0f;
-    Places<kItems> pd, py, pz;
-    pd.set(p.stride_dt, row0, kStep, c4, T{});
-    py.set(p.stride_y, row0, kStep, c4, T{});
-    pz.set(p.stride_z, row0, kStep, c4, T{});
-    auto tile_at = [&](const void* first, long long stride, long long t0, long long more) { return Tile(reinterpret_cast<const T*>(first) + t0 * stride + more); };
-    Four<T, VEC> nd[kItems], ny[kItems], nz[kItems], nc;
-    auto ask = [&](long long t0) {
-        const int rows = hi - t0 < R ? (int)(hi - t0) : R;
-        const Tile d = tile_at(p.dt, p.stride_dt, t0, place.ch0), y = tile_at(p.dy, p.stride_y, t0, place.ch0);
-#pragma unroll
-        for (int j = 0; j < kItems; ++j) {
-            const bool on = count > 0 && row0 + j * kStep < rows;
-            nd[j].load(d, on ? pd.at[j] : kNoColumn, count);
-            ny[j].load(y, on ? py.at[j] : kNoColumn, count);
-        }
-        if (p.z) {
-            const Tile z = tile_at(p.z, p.stride_z, t0, place.ch0);
-#pragma unroll
-            for (int j = 0; j < kItems; ++j) nz[j].load(z, count > 0 && row0 + j * kStep < rows ? pz.at[j] : kNoColumn, count);
-        }
-        const int i = threadIdx.x / Q, s = 4 * (threadIdx.x % Q);
-        nc.load(tile_at(p.C, p.stride_C, t0, (long long)place.g * p.S), i < rows && s < p.S ? (unsigned)(i * p.stride_C + s) * (unsigned)sizeof(T) : kNoColumn, p.S - s);
-    };
-    const long long t_last = lo + (hi - lo - 1) / R * R;
-    ask(t_last);
-    for (long long t0 = t_last; t0 >= lo; t0 -= R) {
-        const int rows = hi - t0 < R ? (int)(hi - t0) : R;
-#pragma unroll
-        for (int j = 0; j < kItems; ++j) {
-            const int i = row0 + j * kStep;
-            Float2 both[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float raw = nd[j][v] + bias[v];
-                both[v] = Float2{p.softplus ? softplus(raw) : raw, ny[j][v]};
-            }
-            if (p.z)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) both[v].y *= fast_silu(nz[j][v]);
-            if (kStep * kItems <= R || i < R)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) sx[i][c4 + v] = both[v];
-        }
-        if (R * Q >= 256 || threadIdx.x < R * Q) cs[threadIdx.x / Q][threadIdx.x % Q] = Float4{nc[0], nc[1], nc[2], nc[3]};
-        lds_barrier();
-        if (t0 > lo) ask(t0 - R);
-        auto go = [&](auto whole) {
-            constexpr bool WHOLE = decltype(whole)::value;
-#pragma unroll
-            for (int i = R - 1; i >= 0; --i) {
-                if (!WHOLE && i >= rows) continue;
-                const Float2 s = sx[i][c];
-                const Float4 cc = cs[i][q];
-                sum_dt += s.x;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) r[k] = __builtin_amdgcn_exp2f(s.x * A2[k]) * (r[k] + cc[k] * s.y);
-            }
-        };
-        if (rows == R) go(std::true_type{});
-        else go(std::false_type{});
-        lds_barrier();
-    }
-    store_states(p.rlocal, place.seg, l, p.D, 4 * Q, r);
-    if (q == 0 && l.on) p.rsteps[place.seg * p.D + l.ch] = sum_dt;
-}
-
 // a lam of the first row behind every segment, from the last segment on
 __global__ __launch_bounds__(256) void selscan_rjoin_kernel(const SelscanParams p, int SP) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x, cells = (long long)p.D * SP, seqs = p.rows.packed ? 1 : p.rows.N;
@@ -441,10 +349,7 @@ hipError_t launch_lanes(const SelscanParams& p, hipStream_t stream) {
         add(p.dC, p.stride_C, (long long)p.G * p.S);
         if (p.z) add(p.dz, p.stride_z, p.D);
     }
-    if (p.segs > 1) {
-        hipLaunchKernelGGL((selscan_fronts_kernel<T, Q, VEC>), grid, block, 0, stream, p);
-        hipLaunchKernelGGL(selscan_rjoin_kernel, dim3((unsigned)((cells * seqs + 255) / 256)), block, 0, stream, p, 4 * Q);
-    }
+    if (p.segs > 1) hipLaunchKernelGGL(selscan_rjoin_kernel, dim3((unsigned)((cells * seqs + 255) / 256)), block, 0, stream, p, 4 * Q);
     if (p.rows.T) {
         hipLaunchKernelGGL((selscan_grad_kernel<T, Q, VEC>), grid, block, 0, stream, p, rest);
         const long long want = rows * p.G * 2 * p.S / 256;

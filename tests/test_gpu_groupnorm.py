@@ -176,3 +176,13 @@ def test_empty_arrays():
         got = run(c, 3, by_row, True)
         assert got["y"].shape == (2, 0, 12) and bool((got["dw"] == 0).all()) and bool((got["dbias"] == 0).all())
         assert got["stats"].shape == ((2, 0, 3, 2) if by_row else (2, 3, 2)) and bool((got["stats"] == 0).all())
+
+
+def test_rows_of_many_sequences():
+    """2^16 and some sequences of one row, 64 groups each, are what as many rows of one sequence are"""
+    N, D, G = 70001, 256, 64
+    c = make("f32", (N, 1), D, True, 9)
+    one = {k: t.reshape(1, N, D) if t.dim() == 3 else t for k, t in c.items()}
+    got, want = run(c, G, True, True), run(one, G, True, True)
+    for name, t in got.items():
+        assert torch.equal(t.reshape(want[name].shape), want[name]), name

@@ -247,3 +247,13 @@ def test_empty_arrays():
     got = run(c)
     assert got["y"].shape == (2, 0, 10) and torch.equal(got["last"], c["h0"]) and torch.equal(got["dh0"], c["dlast"])
     assert bool((got["dA"] == 0).all()) and bool((got["dskip"] == 0).all())
+
+
+@pytest.mark.parametrize("N,D,S", [(64, 128, 64), (256, 512, 4)])
+def test_many_whole_sequences(N, D, S):
+    """as many workgroups as there need be without a cut: the same call with lengths is cut"""
+    T = 130
+    c = make("f32", (N, T), N, D, S, 1, True, 17)
+    whole, cut = run(c), run(c, lengths=torch.full((N,), T, dtype=torch.int64, device=DEV))
+    compare(c, whole, "f32", lo.sequences(T, N))
+    compare(c, cut, "f32", lo.sequences(T, N))

@@ -176,3 +176,11 @@ def test_more_work_items_than_a_launch_holds():
         ask = lambda c: lib.deer_groupnorm_workspace_bytes(ctypes.byref(c), grad, ctypes.byref(size))   # noqa: E731, B023
         assert ask(norm(N=1, T=1, D=1 << 24)) == 0 and ask(norm(N=1, T=1, D=1 << 25)) == 2
         assert ask(norm(N=1 << 20, T=1, D=8, G=4, span=1)) == 2   # 1,024 lanes for each of 2^22 groups of sequences
+
+
+def test_groups_of_rows_are_not_counted_like_those_of_sequences():
+    """2^17 sequences of 64 groups: no launch of 1,024 lanes for each where statistics are over rows"""
+    lib, size = deer.load_library(), ctypes.c_size_t(0)
+    for grad in (0, 1):
+        ask = lambda c: lib.deer_groupnorm_workspace_bytes(ctypes.byref(c), grad, ctypes.byref(size))   # noqa: E731, B023
+        assert ask(norm(N=1 << 17, T=1, D=512, G=64, span=0)) == 0 and ask(norm(N=1 << 17, T=1, D=512, G=64, span=1)) == 2
