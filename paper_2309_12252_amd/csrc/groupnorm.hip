@@ -427,19 +427,99 @@ __device__ __forceinline__ void phase_sums(S (*two)[V], const Lanes& l, S* share
 }
 constexpr int kPhaseRoom = 4 * 2 * 64;
 
-// Mean and sum of squares about it, of every channel in every piece: sums of the differences from the piece's first row.  That row is one of the summed, so
-// its distance from the mean is at most the root of the sum of squares: what cancels is at most a factor of the rows of a piece.  32,768 rows of 2,560 channels in bf16, 168 MB, 45 us (3.7 TB/s; 75
-// without rows on their way).
+// Of a lane's rows of a piece: mean = hi + lo, and the sum of squares about it
+template <typename S, int V>
+struct Moments {
+    S hi[V], lo[V], squares[V];
+    int rows;
+};
+// sum over the phases of a wavefront, `lanes` apart, the same for all of them
+template <typename S>
+__device__ __forceinline__ S wave_phases(S v, int lanes) {
+    if constexpr (sizeof(S) == 8) {
+        for (int d = lanes; d < 64; d *= 2) v += __shfl_xor(v, d);
+    } else {
+        if (lanes <= 1) v = dpp_add<kSwapLanes>(v);
+        if (lanes <= 2) v = dpp_add<kSwapPairs>(v);
+        if (lanes <= 4) v = dpp_add<kRor4>(v);
+        if (lanes <= 8) v = dpp_add<kRor8>(v);
+        if (lanes <= 16) v = sum_rows(v, v);
+        if (lanes <= 32) v = sum_halves(v, v);
+    }
+    return v;
+}
+__device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }   // (of a number of rows: off by 1 ulp, which a mean's distance from its offset takes)
+__device__ __forceinline__ double inverse(double v) { return 1.0 / v; }
+
+// The phases' moments joined; those of phase 0 get them.  Within a wavefront in two passes as over single values, first the mean and then the squares about it, in differences from its first phase's mean;
+// then the wavefronts' one after another: nothing is the small difference of large sums.  hi + lo: differences between means far from zero keep their digits.
+template <typename S, int V>
+__device__ __forceinline__ void phase_moments(Moments<S, V>& m, const Lanes& l, S* shared, int* rows) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (l.lanes < 64) {
+        S first[V], off[V], sum[V];
+        const S all = wave_phases((S)m.rows, l.lanes);   // (at most 2,048: exact)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            first[v] = __shfl(m.hi[v], lane & (l.lanes - 1));
+            off[v] = m.rows ? (m.hi[v] - first[v]) + m.lo[v] : S(0);
+            sum[v] = wave_phases((S)m.rows * off[v], l.lanes);
+        }
+        const S share = all > S(0) ? inverse(all) : S(0);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            sum[v] *= share;
+            off[v] -= sum[v];
+            m.squares[v] = wave_phases(m.squares[v] + (S)m.rows * off[v] * off[v], l.lanes);
+            m.hi[v] = first[v] + sum[v];
+            m.lo[v] = (first[v] - m.hi[v]) + sum[v];
+        }
+        m.rows = (int)all;
+    }
+    __syncthreads();
+    if (wave > 0 && lane < l.lanes) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            shared[((wave * 3 + 0) * 64 + lane) * V + v] = m.hi[v];
+            shared[((wave * 3 + 1) * 64 + lane) * V + v] = m.lo[v];
+            shared[((wave * 3 + 2) * 64 + lane) * V + v] = m.squares[v];
+        }
+        if (lane == 0) rows[wave] = m.rows;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x >= l.lanes) return;
+    for (int f = 1; f < 4; ++f) {
+        if (rows[f] == 0) break;   // (nor do those behind it have any)
+        const int all = m.rows + rows[f];
+        const S share = (S)rows[f] * inverse((S)all);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const S hi = shared[((f * 3 + 0) * 64 + lane) * V + v], lo = shared[((f * 3 + 1) * 64 + lane) * V + v];
+            const S apart = (hi - m.hi[v]) + (lo - m.lo[v]), by = m.lo[v] + share * apart, mean = m.hi[v] + by;
+            m.squares[v] += shared[((f * 3 + 2) * 64 + lane) * V + v] + (S)m.rows * share * apart * apart;
+            m.lo[v] = (m.hi[v] - mean) + by;
+            m.hi[v] = mean;
+        }
+        m.rows = all;
+    }
+}
+constexpr int kMomentRoom = 4 * 3 * 64;
+
+// Mean and sum of squares about it, of every channel in every piece.  A lane sums the differences from the mean of its first eight rows: whatever value lies far off is one of the summed, and the squares about the
+// lane's own mean are at least a quarter of those about that offset (32 rows at most), so that no more than two bits cancel.  (Differences from a piece's first row lose a factor of the piece's rows, up to 8,192, where that row lies far
+// off: rstd was off by 7e-5 behind a first row 100 deviations away.)  32,768 rows of 2,560 channels in bf16, 168 MB, 44 us (3.8 TB/s; 75
+// without rows on their way); 32 x 17,984 rows of 16 in fp32 11.8 (10.0 with differences from first rows, 13.7 with sums by shuffles).
 template <typename T, int V>
 __global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const Lanes l, int rows, const RestRows rest) {
     using S = wide_t<T>;
-    __shared__ S shared[kPhaseRoom * V];
+    __shared__ S shared[kMomentRoom * V];
+    __shared__ int counts[4];
     const SpanPlace at = span_place<V>(p, l, rows);
     for_runs(p.rows, at.n, at.lo, at.hi, [&](int seq, long long, long long, long long r0, long long r1) {
-        S two[2][V], first[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) two[0][v] = two[1][v] = first[v] = S(0);
-        if (at.on) {
+        const int many = (int)(r1 - r0) - at.phase;
+        Moments<S, V> m{};
+        m.rows = many > 0 ? (int)((unsigned)(many + l.phases - 1) / (unsigned)l.phases) : 0;
+        if (at.on && m.rows) {
             // eight rows at a time, the next eight on their way
             using TV = vec_t<T, V>;
             constexpr int B = 8;
@@ -458,32 +538,50 @@ __global__ __launch_bounds__(256) void moments_kernel(const NormParams p, const 
                 from += B * step;
             };
             ask(r0 + at.phase);
-            load_wide<T, V>(first, p.x, r0 * p.stride_x + at.ch);
-            for (long long r = r0 + at.phase; r < r1; r += B * l.phases) {
+            S first[V] = {}, two[2][V] = {};
+            const S part = inverse((S)(m.rows < B ? m.rows : B));
+#pragma unroll
+            for (int i = 0; i < B; ++i)
+                if (i < m.rows)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) first[v] += part * (S)vec_at<T, V>(next[i], v);
+            for (int left = m.rows; left > 0; left -= B) {
 #pragma unroll
                 for (int i = 0; i < B; ++i) now[i] = next[i];
-                if (r + B * l.phases < r1) ask(r + B * l.phases);
-#pragma unroll
-                for (int i = 0; i < B; ++i) {
-                    const bool in = r + i * l.phases < r1;
+                if (left > B) ask(r0 + at.phase + (long long)(m.rows - left + B) * l.phases);
+                auto add = [&](int i) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        const S off = in ? (S)vec_at<T, V>(now[i], v) - first[v] : S(0);
+                        const S off = (S)vec_at<T, V>(now[i], v) - first[v];
                         two[0][v] += off;
                         two[1][v] += off * off;
                     }
+                };
+                if (left >= B) {
+#pragma unroll
+                    for (int i = 0; i < B; ++i) add(i);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < B; ++i)
+                        if (i < left) add(i);
                 }
             }
+            const S share = inverse((S)m.rows);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const S mean = two[0][v] * share, squares = two[1][v] - two[0][v] * mean;
+                m.hi[v] = first[v] + mean;
+                m.lo[v] = (first[v] - m.hi[v]) + mean;
+                m.squares[v] = squares > S(0) || !(squares <= S(0)) ? squares : S(0);   // (NaN stays)
+            }
         }
-        phase_sums<S, V>(two, l, shared);
+        phase_moments<S, V>(m, l, shared, counts);
         if (!at.on || (int)threadIdx.x >= l.lanes) return;
         S* to = reinterpret_cast<S*>(p.part) + piece_at(p.rows, at.tile, seq) * 2 * p.D + at.ch;
-        const S count = (S)(r1 - r0);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const S mean = two[0][v] / count, squares = two[1][v] - two[0][v] * mean;
-            to[v] = first[v] + mean;
-            to[p.D + v] = squares > S(0) || !(squares <= S(0)) ? squares : S(0);   // (NaN stays)
+            to[v] = m.hi[v] + m.lo[v];
+            to[p.D + v] = m.squares[v];
         }
     });
     clear_rest(p.rows, rest, blockIdx.x, gridDim.x);
