@@ -82,7 +82,7 @@ const char* bad_config(const deer_selscan_config* c, bool step) {
     return nullptr;
 }
 struct ScanLayout {
-    int lanes, blocks, segs, marks_each;   // lanes of a channel, workgroups along a group's channels
+    int lanes, blocks, segs, marks_each, parts_each;   // lanes of a channel, workgroups along a group's channels
     long long seg_rows, all_segs;
     size_t local, carry, steps, resets, rlocal, rcarry, rsteps, rresets, marks, mark_steps, part_bc, part_A, part_d, total;
 };
@@ -107,6 +107,7 @@ ScanLayout scan_layout(const deer_selscan_config* c, bool grad, bool bounds) {
     if (l.segs < 1) l.segs = 1;
     l.all_segs = seqs * l.segs;
     l.marks_each = (int)(l.seg_rows / kMarkRows);
+    l.parts_each = (int)((l.seg_rows + kSumRows - 1) / kSumRows);
     const size_t cells = (size_t)c->D * 4 * l.lanes * 4, channels = (size_t)c->D * 4;
     Room r;
     if (l.segs > 1) {
@@ -125,8 +126,8 @@ ScanLayout scan_layout(const deer_selscan_config* c, bool grad, bool bounds) {
         l.marks = r.take((size_t)l.all_segs * l.marks_each * cells);
         l.mark_steps = r.take((size_t)l.all_segs * l.marks_each * channels);
         l.part_bc = r.take((size_t)l.blocks * c->T * seqs * c->G * 8 * l.lanes * 4);
-        l.part_A = r.take((size_t)l.all_segs * c->D * c->S * 4);
-        l.part_d = r.take((size_t)l.all_segs * 2 * channels);
+        l.part_A = r.take((size_t)l.all_segs * l.parts_each * c->D * c->S * 4);
+        l.part_d = r.take((size_t)l.all_segs * l.parts_each * 2 * channels);
     }
     l.total = r.at + kAlign;
     return l;
@@ -164,6 +165,7 @@ SelscanParams scan_params(const deer_selscan_config* c, const ScanLayout& l, con
     p.segs = l.segs;
     p.seg_rows = l.seg_rows;
     p.marks_each = l.marks_each;
+    p.parts_each = l.parts_each;
     p.zero_rest = zero_rest(c);
     if (l.segs > 1) {
         p.local = floats(l.local);

@@ -18,6 +18,7 @@ template <int Q> struct ScanShape {
     static constexpr int kQuads = kRows * Q >= 256 ? kRows * Q / 256 : 1;                    // of four states of B, and of C, of a row, a lane
 };
 constexpr int kMarkRows = 16;   // rows from one kept state to the next in the gradient, and of its tiles
+constexpr int kSumRows = 1024;  // at most so many rows are summed in 32 bits for dA, dskip and dbias, their sums in 64: equal values over 65,536 rows would be off by 6e-4, over these by 1e-5
 
 inline int scan_lanes(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : S <= 16 ? 4 : S <= 32 ? 8 : 16; }
 
@@ -45,7 +46,8 @@ struct SelscanParams {
     float *marks, *mark_steps;        // states in front of every kMarkRows rows [D][4 Q], sums of dt since the segment's first row [D]
     float *rlocal, *rcarry, *rsteps;  // the same backwards
     int* rresets;
-    float *part_bc, *part_A, *part_d; // sums for dB and dC by workgroups, for dA [segment][D][S], for dskip and dbias [segment][2][D]
+    float *part_bc, *part_A, *part_d; // sums for dB and dC by workgroups; of every kSumRows rows of a segment for dA [part][D][S], and for dskip and dbias [part][2][D]
+    int parts_each;                   // of a segment
     bool zero_rest;
 };
 

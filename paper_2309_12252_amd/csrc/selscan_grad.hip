@@ -72,6 +72,38 @@ __global__ __launch_bounds__(256, 2) void selscan_grad_kernel(const SelscanParam
         dbias[i] = dskip[i] = 0.0f;
     }
     const long long lo = place.lo, hi = place.hi;
+    // sums over kSumRows rows, once the first of them is done
+    auto hand_over = [&](int part) {
+        const long long at = place.seg * p.parts_each + part;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (l.on && l.k0 + k < p.S) p.part_A[(at * p.D + l.ch) * p.S + l.k0 + k] = dA[k];
+            dA[k] = 0.0f;
+        }
+        float* sums = reinterpret_cast<float*>(&it[0][0]);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            lds_barrier();
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                sums[row0 * CW + c4 + v] = w ? dbias[v] : dskip[v];
+                (w ? dbias[v] : dskip[v]) = 0.0f;
+            }
+            lds_barrier();
+            for (int i = threadIdx.x; i < place.channels; i += 256) {
+                float sum = 0.0f;
+                for (int f = 0; f < kStep; ++f) sum += sums[f * CW + i];
+                p.part_d[(at * 2 + w) * p.D + place.ch0 + i] = sum;
+            }
+        }
+        lds_barrier();
+    };
+    // (parts without rows)
+    for (int part = lo < hi ? (int)((hi - lo + kSumRows - 1) / kSumRows) : 0; part < p.parts_each; ++part) {
+        const long long at = place.seg * p.parts_each + part;
+        for (int i = threadIdx.x; i < place.channels * p.S; i += 256) p.part_A[(at * p.D + place.ch0) * p.S + i] = 0.0f;
+        for (int i = threadIdx.x; i < place.channels; i += 256) p.part_d[at * 2 * p.D + place.ch0 + i] = p.part_d[(at * 2 + 1) * p.D + place.ch0 + i] = 0.0f;
+    }
     const long long all_rows = p.rows.T * (p.rows.packed ? 1 : p.rows.N);
     if (lo < hi) {
         ScanSeq seq;   // of the last row of the tile
@@ -292,23 +324,7 @@ __global__ __launch_bounds__(256, 2) void selscan_grad_kernel(const SelscanParam
                 constexpr int step = R * 8 * Q;
                 p.part_bc[(((long long)place.block * all_rows + t0 + i) * p.G + place.g) * 8 * Q + k] = (f[0] + f[step]) + (f[2 * step] + f[3 * step]);
             }
-        }
-    }
-    // sums over the segment's rows
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (l.on && l.k0 + k < p.S) p.part_A[(place.seg * p.D + l.ch) * p.S + l.k0 + k] = dA[k];
-    float* sums = reinterpret_cast<float*>(&it[0][0]);
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        lds_barrier();
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sums[row0 * CW + c4 + v] = w ? dbias[v] : dskip[v];
-        lds_barrier();
-        for (int i = threadIdx.x; i < place.channels; i += 256) {
-            float sum = 0.0f;
-            for (int f = 0; f < kStep; ++f) sum += sums[f * CW + i];
-            p.part_d[(place.seg * 2 + w) * p.D + place.ch0 + i] = sum;
+            if ((t0 - lo) % kSumRows == 0) hand_over((int)((t0 - lo) / kSumRows));
         }
     }
 }
@@ -358,7 +374,7 @@ hipError_t launch_lanes(const SelscanParams& p, hipStream_t stream) {
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && p.dh0 && (p.rows.bounds || !p.rows.T)) err = launch_selscan_empty(p.rows, (long long)p.D * p.S, p.dlast, p.dh0, stream);
     if (err != hipSuccess) return err;
-    const long long parts = p.rows.T ? segs : 0;
+    const long long parts = p.rows.T ? segs * p.parts_each : 0;
     err = launch_sum_tiles(false, p.part_A, parts, SumInto{p.dA, nullptr, p.D * p.S, 1, false}, stream);
     if (err != hipSuccess || (!p.dskip && !p.dbias)) return err;
     return launch_sum_tiles(false, p.part_d, parts, SumInto{p.dskip, p.dbias, p.D, 1, true}, stream);
