@@ -808,14 +808,17 @@ hipError_t launch_sequences(bool grad, const NormParams& p, hipStream_t stream) 
 }
 
 // rows of a workgroup, and how many workgroups along the rows: about 1,024 in all; 512 in the gradient, where each has sums of its own.  16,384 rows of 16 x 128 channels in bf16, as so many:
-// forward 512 57 us, 1,024 52, 2,048 53, 4,096 59; gradient with the sums over workgroups 256 126, 512 86, 1,024 94, 2,048 112
+// forward 512 57 us, 1,024 52, 2,048 53, 4,096 59; gradient with the sums over workgroups 256 126, 512 86, 1,024 94, 2,048 112.  No lane sums more than kSumRounds rows for dw and dbias in 32 bits: equal
+// rows would be off by 1.5e-4 over 16,384 of them, over these by 1e-5
+constexpr long long kSumRounds = 1024;
 struct RowCut {
     long long each, blocks;
 };
 RowCut row_cut(const RowShape& s, long long rows, bool grad) {
     const int all = grad ? 512 : 1024;
     long long rounds = (rows + s.rows - 1) / s.rows, want = all / s.blocks < 1 ? 1 : all / s.blocks;
-    const long long per = (rounds + want - 1) / want;
+    long long per = (rounds + want - 1) / want;
+    if (grad && per > kSumRounds) per = kSumRounds;
     RowCut c;
     c.each = (per < 1 ? 1 : per) * s.rows;
     c.blocks = (rows + c.each - 1) / c.each;

@@ -59,6 +59,17 @@ def test_long_pieces():
     assert float((stats[:, 0, 1].double() / want - 1).abs().max()) <= 320 * lo.U["f32"]
 
 
+def test_sums_over_many_rows():
+    """2^23 equal rows, one channel a group (dbias is all that there is): a lane sums at most 1,024 of them in 32 bits, u each, 64 bits take the rest; 16 for what else is rounded"""
+    rows, D = 1 << 23, 256
+    x = torch.zeros(1, rows, D, device=DEV)
+    dy = torch.full_like(x, 0.7)
+    _, _, dbias, _ = deer.groupnorm_grad(x, D, torch.zeros(1, rows, D, 2, device=DEV), dy)
+    off = float((dbias.double() / (rows * float(dy[0, 0, 0])) - 1).abs().max())
+    print("dbias off by %.1f u" % (off / lo.U["f32"]), flush=True)
+    assert off <= (1024 + 16) * lo.U["f32"]
+
+
 def test_large_constants():
     """no sum of eight values overflows"""
     x = torch.full((2, 40, 8), 2.0 ** 127, device=DEV)
