@@ -770,8 +770,8 @@ def _slots_of(state, slots, N, shape, dtype, device):
 def _conv_inputs(x, w, bias, dtype):
     """(channels, weights of a channel, pointers of w and bias)"""
     D, wide = x.shape[-1], _wide(dtype)
-    if not isinstance(w, torch.Tensor) or w.dim() != 2:
-        _refuse("w: need [D, W]")
+    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] < 1:
+        _refuse("w: need [D, W], W >= 1")
     W = w.shape[1]
     wp = _dense(w, "w", torch.Size((D, W)), wide, x.device)
     return D, W, wp, _dense(bias, "bias", torch.Size((D,)), wide, x.device)

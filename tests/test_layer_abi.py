@@ -162,6 +162,16 @@ def test_binding_needs_device_tensors():
         assert e.value.status == deer.DEER_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("call", [
+    lambda x, w: deer.shortconv_solve.__wrapped__(x, w), lambda x, w: deer.shortconv_grad.__wrapped__(x, w, x),
+    lambda x, w: deer.shortconv_step.__wrapped__(x[0], w, torch.zeros(8, 0, 4))])
+def test_no_weights_are_refused_by_the_binding(call):
+    """in front of an array of -1 rows for the states"""
+    with pytest.raises(deer.DeerError) as e:
+        call(torch.zeros(2, 8, 4), torch.zeros(4, 0))
+    assert e.value.status == deer.DEER_ERR_INVALID_ARG
+
+
 def test_more_work_items_than_a_launch_holds():
     """2^32 - 1 of them, in any of a call's launches: sums over tiles have 64 a column"""
     lib, size = deer.load_library(), ctypes.c_size_t(0)
