@@ -386,8 +386,8 @@ deer_status deer_shortconv_step(const deer_shortconv_config* cfg, const void* d_
 
 /* Selective scan: S states for every channel, h_t = exp(dt_t A) h_{t-1} + dt_t x_t B_t, y_t = <C_t, h_t> + skip x_t, times z_t / (1 + exp(-z_t)) where there is a z.
  * dt_t = act(d_dt + dt_bias) is a channel's, B_t and C_t are a group's of D / G channels.  DEER_F32, DEER_BF16, DEER_F16; rows and strides of at most 2^22 elements.
- * Long sequences are cut into segments whose states are joined with the exponential of A times the sum of dt: where factors overflow in 32 bits, so do these.
- * The gradient multiplies the factors of a segment's rows: where those of 64 rows or more overflow, it is not finite, also from rows whose dy is zero. */
+ * Long sequences are cut into segments whose states are joined with the exponential of A times the sum of dt.  Factors above one may multiply to more than 32 bits hold, as
+ * long as the states and gradients themselves do not.  (Gradient: where the factors from a segment's first row multiply to less than 2^-126 and such factors follow, what goes through all of them counts as nothing.) */
 typedef struct {
     int32_t dtype;     /* deer_dtype: x, dt, B, C, z, y and their gradients                                */
     int32_t dt_act;    /* DEER_ACT_NONE or DEER_ACT_SOFTPLUS                                               */

@@ -69,6 +69,10 @@ __global__ __launch_bounds__(256, WHAT == kFronts ? 4 : 1) void selscan_kernel(c
 #pragma unroll
             for (int k = 0; k < 4; ++k) out[k] += through[k] * d[k];
         }
+        // (a product that 32 bits do not hold, and that stays so: the join goes over these rows one by one)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (!(through[k] <= __FLT_MAX__)) out[k] = __builtin_inff();
         if (threadIdx.x == 0) p.rresets[place.seg] = with_sequence;
         store_states(p.rlocal, place.seg, l, p.D, 4 * Q, out);
         if (q == 0 && l.on) p.rsteps[place.seg * p.D + l.ch] = sum_dt;
@@ -280,7 +284,7 @@ __global__ __launch_bounds__(256) void selscan_join_kernel(const SelscanParams p
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (s0 + i >= p.segs - 1) break;
-            h = reset[i] ? local[i] : local[i] + __builtin_amdgcn_exp2f(A2 * steps[i]) * h;
+            h = reset[i] ? local[i] : local[i] + scaled(h, A2 * steps[i]);
             p.carry[(first + s0 + i + 1) * cells + cell] = h;
         }
     }

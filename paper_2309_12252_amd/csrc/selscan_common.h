@@ -149,6 +149,12 @@ __device__ __forceinline__ float softplus_slope(float v) {
 }
 __device__ __forceinline__ float fast_silu(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
 
+// v 2^e in two halves, for factors of many rows that 32 bits need not hold by themselves: zero stays zero, and what fits is kept
+__device__ __forceinline__ float scaled(float v, float e) {
+    const float half = __builtin_amdgcn_exp2f(0.5f * __builtin_fminf(e, 254.0f));
+    return half * v * half;
+}
+
 // Four elements that lie side by side, of a row of a tile, by buffer instructions: asked for in one piece (VEC) or one by one, as they came; those behind `count`, and all of a
 // lane without a row (at kNoColumn), are zero, or not written.  No lane takes another path than the others, so nothing waits for what is on its way.
 constexpr long long kScanStride = 1 << 22;   // elements between rows, at most: the 64 of a tile stay below kNoColumn

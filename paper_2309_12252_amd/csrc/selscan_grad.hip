@@ -15,7 +15,33 @@ namespace {
 
 constexpr int R = kMarkRows;
 
+// What the rows in front of a segment get from it, row by row, where the product of its factors has overflowed: rows of no weight do not make it infinite
+template <typename T>
+__device__ float front_by_rows(const SelscanParams& p, long long n, int seg, int ch, int k, float A2) {
+    const long long base = n * p.rows.T, first = p.rows.packed ? clamp_row(p.rows.bounds[0], p.rows.T) : base;
+    const long long behind = p.rows.packed ? clamp_row(p.rows.bounds[p.rows.N], p.rows.T) : base + seq_length(p.rows, (int)n);
+    long long lo = base + seg * p.seg_rows, hi = lo + p.seg_rows, end = behind, at = n;
+    lo = lo < first ? first : lo;
+    hi = hi > behind ? behind : hi;
+    if (lo >= hi || k >= p.S) return 0.0f;
+    if (p.rows.packed) {
+        at = bounds_up_to(p.rows, lo) - 1;
+        at = at < 0 ? 0 : at >= p.rows.N ? p.rows.N - 1 : at;
+        end = clamp_row(p.rows.bounds[at + 1], p.rows.T);
+    }
+    float r = end <= hi && p.dlast ? p.dlast[(at * p.D + ch) * p.S + k] : 0.0f;
+    for (long long t = (end < hi ? end : hi) - 1; t >= lo && r == r; --t) {
+        const float raw = (float)reinterpret_cast<const T*>(p.dt)[t * p.stride_dt + ch] + (p.bias ? p.bias[ch] : 0.0f), dt = p.softplus ? softplus(raw) : raw;
+        float dy = (float)reinterpret_cast<const T*>(p.dy)[t * p.stride_y + ch];
+        if (p.z) dy *= fast_silu((float)reinterpret_cast<const T*>(p.z)[t * p.stride_z + ch]);
+        const float c = (float)reinterpret_cast<const T*>(p.C)[t * p.stride_C + (long long)(ch / p.per_group) * p.S + k];
+        r = __builtin_amdgcn_exp2f(dt * A2) * (r + c * dy);
+    }
+    return r;
+}
+
 // a lam of the first row behind every segment, from the last segment on
+template <typename T>
 __global__ __launch_bounds__(256) void selscan_rjoin_kernel(const SelscanParams p, int SP) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x, cells = (long long)p.D * SP, seqs = p.rows.packed ? 1 : p.rows.N;
     if (at >= cells * seqs) return;
@@ -37,7 +63,8 @@ __global__ __launch_bounds__(256) void selscan_rjoin_kernel(const SelscanParams 
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (s0 - i <= 0) break;
-            r = reset[i] ? local[i] : local[i] + __builtin_amdgcn_exp2f(A2 * steps[i]) * r;
+            if (local[i] == __builtin_inff()) local[i] = front_by_rows<T>(p, n, s0 - i, ch, k, A2);
+            r = reset[i] ? local[i] : local[i] + scaled(r, A2 * steps[i]);
             p.rcarry[(first + s0 - i - 1) * cells + cell] = r;
         }
     }
@@ -190,7 +217,7 @@ __global__ __launch_bounds__(256, 2) void selscan_grad_kernel(const SelscanParam
             for (int k = 0; k < 4; ++k) before[k] = mark[k];
             if (p.segs > 1 && first.start < lo) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) before[k] += __builtin_amdgcn_exp2f(steps * A[k] * kLog2e) * carry[k];
+                for (int k = 0; k < 4; ++k) before[k] += scaled(carry[k], steps * A[k] * kLog2e);
             }
             lds_barrier();
             if (t0 > lo) ask(t0 - R);
@@ -365,7 +392,7 @@ hipError_t launch_lanes(const SelscanParams& p, hipStream_t stream) {
         add(p.dC, p.stride_C, (long long)p.G * p.S);
         if (p.z) add(p.dz, p.stride_z, p.D);
     }
-    if (p.segs > 1) hipLaunchKernelGGL(selscan_rjoin_kernel, dim3((unsigned)((cells * seqs + 255) / 256)), block, 0, stream, p, 4 * Q);
+    if (p.segs > 1) hipLaunchKernelGGL((selscan_rjoin_kernel<T>), dim3((unsigned)((cells * seqs + 255) / 256)), block, 0, stream, p, 4 * Q);
     if (p.rows.T) {
         hipLaunchKernelGGL((selscan_grad_kernel<T, Q, VEC>), grid, block, 0, stream, p, rest);
         const long long want = rows * p.G * 2 * p.S / 256;
