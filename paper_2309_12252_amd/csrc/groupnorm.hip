@@ -146,14 +146,12 @@ __global__ __launch_bounds__(256) void rownorm_kernel(const NormParams p, const 
         auto through = [&](int t, int m, int v, S& unit_x, S& dv, S& dz) {
             const int c = ch0 + at(t, m) * V + v;
             const S w = p.w ? reinterpret_cast<const S*>(p.w)[c] : S(1), b = p.bias ? reinterpret_cast<const S*>(p.bias)[c] : S(0);
-            unit_x = (x[m][v] - mean) * rstd;
-            const S pre = unit_x * w + b;
-            S f = pre, slope = S(1), gate = S(1), gslope = S(0);
-            if (p.act == DEER_ACT_SILU) silu_both<T>(pre, f, slope);
-            if (p.z) silu_both<T>(z[m][v], gate, gslope);
-            dv = dy[m][v] * gate * slope;
-            dz = dy[m][v] * f * gslope;
-            return dv * w;
+            Through<T> th;
+            const S du = th(p, x[m][v], p.z ? z[m][v] : S(0), dy[m][v], mean, rstd, w, b);
+            unit_x = th.u;
+            dv = th.dv;
+            dz = th.dz;
+            return du;
         };
         if (GRAD)
             for (int t = 0; t < turns; ++t) {

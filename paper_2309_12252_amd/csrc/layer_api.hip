@@ -209,7 +209,7 @@ const char* bad_config(const deer_groupnorm_config* c) {
 struct NormRoom {
     size_t part, sums, joined, total;
 };
-NormRoom norm_room(const deer_groupnorm_config* c, bool grad, const NormLayout& l) {
+NormRoom norm_room(const deer_groupnorm_config* c, const NormLayout& l) {
     const size_t w = wide_bytes(c->dtype);
     Room r;
     NormRoom n{};
@@ -439,7 +439,7 @@ deer_status deer_groupnorm_workspace_bytes(const deer_groupnorm_config* c, int32
     if (!bytes) return fail(DEER_ERR_INVALID_ARG, "bytes is NULL");
     if (const char* why = bad_config(c)) return fail(DEER_ERR_INVALID_ARG, why);
     if (const char* why = too_large(c)) return fail(DEER_ERR_UNSUPPORTED, why);
-    *bytes = norm_room(c, grad != 0, norm_layout_of(c, grad != 0)).total;
+    *bytes = norm_room(c, norm_layout_of(c, grad != 0)).total;
     return DEER_OK;
 }
 
@@ -451,7 +451,7 @@ deer_status deer_groupnorm_solve(const deer_groupnorm_config* c, const void* d_x
     if ((stats && !d_stats) || (c->T > 0 && (!d_x || !d_y)) || (is_packed(c) && !d_bounds)) return fail(DEER_ERR_INVALID_ARG, kMissing);
     if (any_misaligned(type_bytes(c->dtype), d_x, d_z, d_y) || any_misaligned(wide_bytes(c->dtype), d_w, d_bias, d_stats) || misaligned(d_bounds, 8))
         return fail(DEER_ERR_INVALID_ARG, kAligned);
-    const NormRoom room = norm_room(c, false, norm_layout_of(c, false));
+    const NormRoom room = norm_room(c, norm_layout_of(c, false));
     if (deer_status st = check_workspace(d_workspace, workspace_bytes, room.total)) return st;
     NormParams p = norm_params(c, room, d_bounds, d_workspace);
     p.x = d_x;
@@ -472,7 +472,7 @@ deer_status deer_groupnorm_grad(const deer_groupnorm_config* c, const void* d_x,
     if (any_misaligned(type_bytes(c->dtype), d_x, d_z, d_dy, d_dx, d_dz) || any_misaligned(wide_bytes(c->dtype), d_w, d_bias, d_stats, d_dw, d_dbias) ||
         misaligned(d_bounds, 8))
         return fail(DEER_ERR_INVALID_ARG, kAligned);
-    const NormRoom room = norm_room(c, true, norm_layout_of(c, true));
+    const NormRoom room = norm_room(c, norm_layout_of(c, true));
     if (deer_status st = check_workspace(d_workspace, workspace_bytes, room.total)) return st;
     NormParams p = norm_params(c, room, d_bounds, d_workspace);
     p.x = d_x;

@@ -39,7 +39,7 @@ __device__ __forceinline__ long long seq_length(const SeqRows& s, int n) {
     return s.bounds ? clamp_row(s.bounds[n], s.T) : s.T;
 }
 
-// Arrays whose rows that belong to no sequence are zeroed on request, by the call's first kernel over rows (16 rows of a sequence at a time, LANES lanes a
+// Arrays whose rows that belong to no sequence are zeroed on request, by the call's first kernel over rows (16 rows of a sequence at a time, 256 lanes a
 // workgroup).  Packed sequences lie one behind the other, so that these rows are those in front of the first and behind the last.
 struct RestArray {
     void* first;
@@ -47,13 +47,12 @@ struct RestArray {
 };
 struct RestRows {
     int count;
-    RestArray array[6];
+    RestArray array[5];
 };
-template <typename U, int LANES>
+template <typename U>
 __device__ __forceinline__ void clear_row(char* row, long long width) {
-    for (long long i = threadIdx.x; i < width / (long long)sizeof(U); i += LANES) reinterpret_cast<U*>(row)[i] = U{};
+    for (long long i = threadIdx.x; i < width / (long long)sizeof(U); i += 256) reinterpret_cast<U*>(row)[i] = U{};
 }
-template <int LANES = 256>
 __device__ __forceinline__ void clear_rest(const SeqRows& s, const RestRows& rest, long long block, long long blocks) {
     using U4 = unsigned __attribute__((ext_vector_type(4)));
     if (rest.count == 0 || !s.bounds) return;
@@ -68,9 +67,9 @@ __device__ __forceinline__ void clear_rest(const SeqRows& s, const RestRows& res
                 const long long pitch = rest.array[a].pitch, width = rest.array[a].width;
                 char* row = reinterpret_cast<char*>(rest.array[a].first) + (n * s.T + r) * pitch;
                 const unsigned long long low = reinterpret_cast<unsigned long long>(row) | (unsigned long long)width;
-                if (low % 16 == 0) clear_row<U4, LANES>(row, width);
-                else if (low % 4 == 0) clear_row<unsigned, LANES>(row, width);
-                else clear_row<unsigned short, LANES>(row, width);
+                if (low % 16 == 0) clear_row<U4>(row, width);
+                else if (low % 4 == 0) clear_row<unsigned>(row, width);
+                else clear_row<unsigned short>(row, width);
             }
         }
     }
