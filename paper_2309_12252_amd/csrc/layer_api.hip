@@ -88,9 +88,11 @@ struct ScanLayout {
 };
 // How the rows are cut into segments, each a workgroup for 256 / Q channels.  A cut costs a second look at the rows (the gradient's first look takes more), so sequences are whole where they make
 // 512 workgroups.  Measured on 4 x 4,096 rows of 4,096 channels with 16 states in bf16 (whole: 256 workgroups), as so many workgroups in all:
-//   outputs 256 670 us, 512 401, 1,024 312, 2,048 304; states behind segments 512 280, 1,024 229, 2,048 212
-//   gradient with its kept states 256 498 + 1,716 us, 512 304 + 1,105, 1,024 239 + 1,131, 2,048 221 + 1,133; what comes out at segments' fronts, by itself 512 248, 1,024 229, 2,048 218
-// Packed rows, and padded ones with lengths, may be nearly all one sequence's: always cut.  8,192 packed rows: 512 200 + 132 us, 1,024 156 + 109, 2,048 153 + 103.
+//   outputs 256 669 us, 512 411, 1,024 321, 2,048 310; states behind segments 512 285, 1,024 235, 2,048 215
+//   gradient with its kept states 256 496 + 1,680 us; with fronts too 512 452 + 1,144, 1,024 362 + 1,172, 2,048 350 + 1,152; solve and gradient 2,863, 2,215, 1,963, 1,877
+// 8 x 2,048 rows of them, solve and gradient: whole (512 workgroups) 1,774 us, cut (2,048) 1,893.
+// Packed rows, and padded ones with lengths, may be nearly all one sequence's: always cut.  8,192 rows in all: 256 332 + 225 us, 512 195 + 136, 1,024 158 + 115, 2,048 149 + 108; gradient 372 + 857, 218 + 539, 165 +
+// 524, 160 + 514.
 ScanLayout scan_layout(const deer_selscan_config* c, bool grad, bool bounds) {
     ScanLayout l{};
     l.lanes = scan_lanes(c->S);

@@ -5,7 +5,7 @@
 
 namespace deer {
 
-// exp and 1 / v: the functions for fp32 and fp64, the hardware's (1 ulp of 2^x and 1 / x) where the results are rounded to 16 bits
+// exp and 1 / v of the convolution and the norm: the functions for fp32 and fp64, the hardware's (1 ulp of 2^x and 1 / x) where the results are rounded to 16 bits
 template <typename T>
 __device__ __forceinline__ wide_t<T> exp_of(wide_t<T> v) {
     if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(v * 1.44269504088896341f);

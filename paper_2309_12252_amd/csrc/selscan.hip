@@ -11,7 +11,8 @@ namespace {
 enum { kOutputs, kEnds, kMarks, kFronts };
 
 // Bound by the rate of vector instructions once there are eight workgroups a CU: 16,384 rows of 4,096 channels and 16 states in bf16 304 us for outputs (the bytes 104), 212 for the states
-// behind segments, 221 with states kept (268 MB); 345 with what comes out at the front too (439 in two kernels; with five wavefronts a SIMD, which spill, 375).  With one a CU (670 us) half of the time is waiting for LDS; reading it two rows ahead brings that to 480, and costs 340 us with
+// behind segments, 221 with states kept (268 MB); 345 with what comes out at the front too (439 in two kernels; with five wavefronts a SIMD, which spill, 375).  Four wavefronts a SIMD for that one: 309 us for
+// 326 without a bound in bf16; in fp32, where 7 to 12 registers spill, 425 for 416, and 320 for 264 with 8 states.  With one workgroup a CU (670 us) half of the time is waiting for LDS; reading it two rows ahead brings that to 480, and costs 340 us with
 // eight.  Loads by buffer instructions whose offsets lie out of bounds where there is nothing, so that no lane takes another path and what is ahead stays on its way over the
 // barriers.
 template <typename T, int Q, int WHAT, bool VEC>

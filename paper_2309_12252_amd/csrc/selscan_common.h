@@ -11,6 +11,9 @@ namespace deer {
 // lane's slots, and some four of the row's preparation and of sums over lanes; at 16 states the bytes take a third of that time.  One state a lane more than doubles the sums over
 // lanes; a channel with all 16 states a lane, B and C through scalar registers and nothing through LDS, left so few wavefronts that it was slower (outputs of 16,384 rows of
 // 4,096 channels 412 us against 304, gradient 1,890 against 1,132 with its 248 accumulation registers).
+// Lanes of a channel, as many as its states take.  16,384 rows of 4,096 channels with a gate, us of states behind segments + outputs, and of kept states with fronts + gradient:
+//   4 states, bf16: one lane 94 + 136 and 171 + 914, two 133 + 203 and 229 + 737; fp32: one 143 + 277 and 317 + 1,020, two 138 + 210 and 308 + 902 (one lane a channel, the gradient spills)
+//   8 states, bf16: two lanes 119 + 180 and 205 + 652, four 184 + 267 and 305 + 1,003; fp32: two 139 + 207 and 314 + 913, four 189 + 285 and 370 + 1,017
 template <int Q> struct ScanShape {
     static constexpr int kWave = 64 / Q, kChannels = 256 / Q;
     static constexpr int kRows = Q == 1 ? 8 : Q == 2 ? 16 : Q <= 8 ? 32 : 64;
@@ -128,6 +131,8 @@ struct ScanSeq {
     }
 };
 
+// The scan takes the hardware's 2^x and 1 / x (1 ulp) for fp32 too: an exponential is most of a state's row, and an argument v times log2 e rounds to |v| 2^-24, no more than the product dt A that
+// it comes from; gates and slopes keep to it.  (|v| + 6) 2^-24 of a sigmoid, where the functions leave 6.
 constexpr float kLog2e = 1.44269504088896341f;
 
 // log(1 + exp(v)) = max(v, 0) + 2 atanh(e / (2 + e)), e = exp(-|v|): s = e / (2 + e) is at most 1/3, and 2 atanh(s) / s as a polynomial in s^2, fitted at the Chebyshev

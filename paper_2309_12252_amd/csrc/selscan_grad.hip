@@ -332,7 +332,7 @@ __global__ __launch_bounds__(256, 2) void selscan_grad_kernel(const SelscanParam
                     for (int v = 0; v < 4; ++v) {
                         const Float4 s = it[i < R ? i : 0][c4 + v];
                         float gate = 1.0f, slope = 0.0f;
-                        if (p.z) silu_both<BF16>(z[j][v], gate, slope);
+                        if (p.z) silu_both<BF16>(z[j][v], gate, slope);   // (the hardware's functions, as fast_silu)
                         const float out = dy[j][v] * gate;
                         dx[v] = s.x * s.y + skip[v] * out;
                         ddt[v] = (s.z + x[j][v] * s.y) * (p.softplus ? softplus_slope(dt_in[j][v] + bias[v]) : 1.0f);

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) void shortconv_kernel(const ConvParams p, cons
 // Gradient: dv_t = dy_t act'(v_t) with v computed again, dx_t = sum_j w_j dv_{t + W - 1 - j}, dw_j = sum_t dv_t x_{t - W + 1 + j}.  A lane goes on for W - 1 rows behind
 // its own, whose dv its last rows need.  503 MB (the same rows, dy and dx) in 150 us, 3.4 TB/s: vector instructions take some 60 % of the time (36 an element), and with
 // three wavefronts a SIMD the loads ahead do not cover all of the way to memory.  Two channels a lane are no faster, four wavefronts a SIMD spill (422).  B: 16 bits four rows at a time 158, one 182; fp32
-// two rows 235, four 224.  Rows times strides in 64 bits for every load took a third of the time; widths that the compiler does not know, with a test for every weight: 539 us for 217 with 8 weights.
+// two rows 235, four 224; fp64, 16,384 rows of 1,280 channels, 114 (outputs 64).  Rows times strides in 64 bits for every load took a third of the time; widths that the compiler does not know, with a test for every weight: 539 us for 217 with 8 weights.
 template <typename T, int V, int M>
 __global__ __launch_bounds__(256) void shortconv_grad_kernel(const ConvParams p, const Lanes l, const RestRows rest, long long tile_blocks) {
     using S = wide_t<T>;
